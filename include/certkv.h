@@ -82,6 +82,10 @@ extern "C" {
                                          a slot, a radix destination, a budget)
                                          was outside its extent; the access was
                                          skipped, the outputs are invalid      */
+#define CERTKV_STATUS_STORE      16u  /* in a certkv_store's status word: a slot
+                                         had no page, or a select or accepted
+                                         entry was out of range; the row was not
+                                         written, or not read by attention      */
 
 /* ---- problem description ------------------------------------------------- */
 typedef struct {
@@ -444,6 +448,169 @@ int certkv_read_status(const void* workspace, void* stream);
  * CERTKV_ECUDA. */
 int certkv_trace_enable(int on);
 int certkv_trace_report(char* buf, size_t len);
+
+/* ==========================================================================
+ * Verifying drafted tokens over the compressed cache (no counterpart in the
+ * paper, whose method ends with single-token decode over a cache that cannot
+ * grow): rotary positions, a paged store the packed cache and later tokens are
+ * quantised into, and attention of a tree of drafted tokens over that store.
+ * ========================================================================== */
+
+/* Rows of d = 128 bf16 elements indexed [b][l][t][h] with strides in elements:
+ * row (b, l, t, h) starts at data + b stride_b + l stride_l + t stride_t +
+ * h stride_h and is contiguous.  data is 16-byte aligned, every stride a
+ * multiple of 8 (any sign; 0 broadcasts an input).  A view of a fused
+ * projection, or the [B][L][H][n][d] layout of certkv_compress, is described
+ * without a copy.  The rows of an output must not overlap one another (a
+ * stride of 0 over more than one row is refused). */
+typedef struct {
+  void*   data;
+  int64_t stride_b, stride_l, stride_t, stride_h;
+} certkv_rows;
+
+/* ---- rotary positions ------------------------------------------------------
+ * Pair i < dim / 2 of a row at position pos turns by pos theta_i:
+ *   (x_a, x_b) -> magnitude (x_a cos - x_b sin, x_a sin + x_b cos),
+ * a, b = i, i + dim / 2 (CERTKV_ROPE_HALF) or 2 i, 2 i + 1
+ * (CERTKV_ROPE_INTERLEAVED); elements from dim on are copied bit for bit.  The
+ * inverse turns by -pos theta_i and divides by the magnitude (the transpose of
+ * the rotation, so with magnitude 1 also its gradient). */
+#define CERTKV_ROPE_HALF        0
+#define CERTKV_ROPE_INTERLEAVED 1
+
+/* theta_i = base^(-2 i / dim), changed for contexts longer than trained on:
+ * LINEAR  theta_i / factor (positions interpolated);
+ * NTK     base replaced by base factor^(dim / (dim - 2)) (dim > 2);
+ * RAMP    with r_i = original theta_i / 2 pi turns over the original context and
+ *         g_i = clamp((r_i - low) / (high - low), 0, 1):
+ *         (1 - g_i) theta_i / factor + g_i theta_i (low < high). */
+#define CERTKV_ROPE_NONE   0
+#define CERTKV_ROPE_LINEAR 1
+#define CERTKV_ROPE_NTK    2
+#define CERTKV_ROPE_RAMP   3
+typedef struct {
+  int32_t kind;      /* CERTKV_ROPE_NONE .. CERTKV_ROPE_RAMP                      */
+  double  factor;    /* > 0; not used by NONE                                   */
+  double  original;  /* RAMP: the original context length, > 0                  */
+  double  low, high; /* RAMP: turns below / above which a pair is interpolated / kept */
+  double  magnitude; /* factor on the rotated elements, > 0 (1: a pure rotation) */
+} certkv_rope_scaling;
+
+/* A rotation worked out once on the host: the turns per position of every pair
+ * as an unevaluated float sum, so that angles keep fp32 accuracy at positions
+ * of any size.  Plain data, kept and passed by the caller. */
+typedef struct {
+  int32_t dim;       /* elements rotated, even, 2..128 */
+  int32_t layout;    /* CERTKV_ROPE_HALF / CERTKV_ROPE_INTERLEAVED */
+  float   magnitude;
+  float   inverse_magnitude;
+  float   turns_hi[64], turns_lo[64];
+} certkv_rope_angles;
+
+/* Fill `out` for base > 1; scaling NULL: none, magnitude 1.  Host call. */
+int certkv_rope_plan(int32_t dim, int32_t layout, double base,
+                     const certkv_rope_scaling* scaling, certkv_rope_angles* out);
+
+/* Rotate the rows of q [batch][layers][tokens][hq] and, when k is not NULL, of
+ * k [batch][layers][tokens][hkv] into q_out and k_out, in one launch.
+ * positions: int32 [batch][tokens], any value, shared by the layers and heads.
+ * An output may be its input (same data and strides); it must not overlap it
+ * otherwise.  fp32 arithmetic, one rounding to bf16. */
+int certkv_rope(int32_t batch, int32_t layers, int32_t tokens, int32_t hq, int32_t hkv,
+                const certkv_rows* q, const certkv_rows* q_out, const certkv_rows* k,
+                const certkv_rows* k_out, const int32_t* positions,
+                const certkv_rope_angles* angles, int32_t inverse, void* stream);
+
+/* ---- paged store -----------------------------------------------------------
+ * One segment per unit u = (b L + l) H + h: slot s of segment u is slot
+ * s % 64 of page table[u][s / 64] of the pool.  A row of 128 values is held as
+ *   CERTKV_STORE_BF16  itself;
+ *   CERTKV_STORE_FP8   code_j = e4m3(x_j r), r = 448 (1 / A), A = max |x_j|, and
+ *                      the fp32 scale s = A (1 / 448): x_j stands as code_j s;
+ *   CERTKV_STORE_FP4   per group g of 16 elements an e4m3 scale
+ *                      gs = e4m3((A_g r) (1 / 6)), r = 2688 (1 / A), A_g the
+ *                      group's maximum; code_j = e2m1(x_j (r (1 / gs))) (0 where
+ *                      gs = 0) and the fp32 scale s = A (1 / 2688): x_j stands as
+ *                      code_j gs s.  Two codes a byte, the even element low.
+ * e4m3 and e2m1 round to nearest, ties to even, and saturate; every reciprocal
+ * and every product is one fp32 operation, rounded to nearest.  A row with A < 2^-100 is held as zeros with s = 1; a row with a
+ * NaN or infinity has s = NaN and stands for NaN in every element (FP8, FP4). */
+#define CERTKV_STORE_PAGE 64
+#define CERTKV_STORE_BF16 0
+#define CERTKV_STORE_FP8  1
+#define CERTKV_STORE_FP4  2
+typedef struct {
+  int32_t   units;       /* segments, 1..2^24                                       */
+  int32_t   format;      /* CERTKV_STORE_*                                          */
+  int32_t   max_pages;   /* entries of a table row, 1..2^18                         */
+  int32_t   pool_pages;  /* pages of the pool, 1..2^25 - 1                          */
+  void     *k, *v;       /* codes [pool_pages][64][256 / 128 / 64 bytes], 128-byte
+                            aligned                                                 */
+  void     *k_group, *v_group;  /* FP4: e4m3 [pool_pages][64][8], 16-byte aligned,
+                                   else not used                                    */
+  float    *k_scale, *v_scale;  /* FP8, FP4: fp32 [pool_pages][64], 16-byte aligned,
+                                   else not used                                    */
+  int32_t  *table;       /* [units][max_pages] page of the pool; outside
+                            0..pool_pages - 1: none                               */
+  int32_t  *counts;      /* [units] live slots (read as clamped to
+                            0..64 max_pages)                                      */
+  uint32_t *status;      /* optional (NULL = skip) CERTKV_STATUS_STORE is or-ed in  */
+} certkv_store;
+
+/* Quantise a packed cache into the store as its first contents: segment u gets
+ * the real slots and, with tail_slot = 1, the tail slot of packed segment u (not
+ * cluster summaries), in order.  Pages are handed out from page 0 of the pool,
+ * segment after segment, ceil((slots + reserve) / 64) each; table rows are
+ * written whole (-1 past a segment's pages) and counts[u] = slots.  Where the
+ * pool or a table row is too short the segment is cut and CERTKV_STATUS_STORE
+ * raised.  packed: k, v, offsets, real_counts and capacity_slots are used.
+ * Workspace: certkv_store_workspace_bytes(units), 256-byte aligned. */
+size_t certkv_store_workspace_bytes(int32_t units);
+int certkv_store_load(const certkv_packed* packed, int32_t tail_slot, int32_t reserve,
+                      const certkv_store* store, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* Quantise token rows as they are written: row i < m of sequence b goes to slot
+ * start[u] + i of every segment u = (b, l, h), and counts[u] = start[u] + m.
+ * k, v [batch][layers][tokens][hkv].  m = accepted[b] (device int32 [batch],
+ * 0..tokens; NULL: tokens), row i is token select[b][i] (device int32
+ * [batch][tokens]; NULL: i), so the accepted path of a draft tree is written
+ * from the drafts' own rows.  start: device int32 [units], NULL: store->counts
+ * (tokens are appended).  Rows whose page the table does not have, and entries
+ * out of range, are skipped with CERTKV_STATUS_STORE (counts still advance by m
+ * clamped to 0..tokens, to at most 64 max_pages). */
+int certkv_store_append(int32_t batch, int32_t layers, int32_t hkv, int32_t tokens,
+                        const certkv_rows* k, const certkv_rows* v, const int32_t* select,
+                        const int32_t* accepted, const int32_t* start, const certkv_store* store,
+                        void* stream);
+
+/* Read back `tokens` slots of every segment from slot start[u] (device int32
+ * [units]; NULL: 0) as bf16 rows k_out, v_out [units][tokens][128]; slots from
+ * counts[u] on, before 0 or without a page read as 0. */
+int certkv_store_read(const certkv_store* store, const int32_t* start, int32_t tokens, void* k_out,
+                      void* v_out, void* stream);
+
+/* ---- attention of a tree of drafted tokens ------------------------------------
+ * For drafted token t and query head qh of unit u = (b, l, qh / G):
+ *   out[b][l][t][qh] = softmax-weighted sum of values over all counts[u] slots of
+ * store segment u and over the drafted tokens j that t sees, with logits
+ * scale <q, k>.  t sees draft j when bit j of mask[b][t] is set (device uint64
+ * [batch][tokens]; bits from `tokens` on are ignored; NULL: j <= t).  k_new,
+ * v_new: the drafts' own keys and values [batch][layers][tokens][hkv] (both
+ * NULL: none).  tokens = 1 is a decode step.  A row that sees nothing gets 0 and
+ * lse -inf; a draft a row does not see does not touch it, whatever it holds.
+ * lse (may be NULL): fp32 [batch][layers][tokens][hq], the natural log of the
+ * row's sum of exponentials.  shape: batch, layers, hq, hkv and d = 128 are
+ * used; G = hq / hkv may be any integer 1..32, 1 <= tokens <= 64.  scale 0
+ * selects 1/sqrt(d).  Slots without a page are left out (CERTKV_STATUS_STORE).
+ * Workspace: certkv_tree_workspace_bytes(shape, tokens), 256-byte aligned. */
+#define CERTKV_TREE_MAX_TOKENS 64
+#define CERTKV_TREE_MAX_GROUP 32
+size_t certkv_tree_workspace_bytes(const certkv_shape* shape, int32_t tokens);
+int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const certkv_rows* q,
+                     const certkv_rows* k_new, const certkv_rows* v_new, const uint64_t* mask,
+                     const certkv_store* store, float scale, const certkv_rows* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static description of a return code. */
 const char* certkv_strerror(int code);

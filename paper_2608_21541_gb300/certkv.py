@@ -23,6 +23,11 @@ STATUS_NONFINITE = 1
 STATUS_ZERO_TAIL = 2
 STATUS_TIMEOUT = 4
 STATUS_BOUNDS = 8
+STATUS_STORE = 16
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
+STORE_FORMATS = {"bf16": 0, "fp8": 1, "fp4": 2}
+STORE_PAGE = 64
 STAT_CENTERED, STAT_UNCENTERED, STAT_TAIL_MASS = 0, 1, 2
 
 
@@ -48,6 +53,33 @@ class certkv_packed(ctypes.Structure):
                 ("kept_vmax", ctypes.c_void_p)]
 
 
+class certkv_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_l", ctypes.c_int64), ("stride_t", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64)]
+
+
+class certkv_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("original", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class certkv_rope_angles(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("inverse_magnitude", ctypes.c_float),
+                ("turns_hi", ctypes.c_float * 64), ("turns_lo", ctypes.c_float * 64)]
+
+
+class certkv_store(ctypes.Structure):
+    _fields_ = [("units", ctypes.c_int32), ("format", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("pool_pages", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_group", ctypes.c_void_p),
+                ("v_group", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("counts", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
 EXPORTED = ("certkv_default_params", "certkv_live_budget", "certkv_workspace_bytes",
             "certkv_decode_workspace_bytes", "certkv_score", "certkv_curves",
             "certkv_compress_scored", "certkv_compress", "certkv_decode_attn",
@@ -58,7 +90,9 @@ EXPORTED = ("certkv_default_params", "certkv_live_budget", "certkv_workspace_byt
             "certkv_coverage_profile", "certkv_sampled_workspace_bytes",
             "certkv_sampled_compensation", "certkv_compress_host_copyback",
             "certkv_workspace_guard_arm", "certkv_workspace_guard_check",
-            "certkv_selftest_bounded_wait")
+            "certkv_selftest_bounded_wait", "certkv_rope_plan", "certkv_rope",
+            "certkv_store_workspace_bytes", "certkv_store_load", "certkv_store_append",
+            "certkv_store_read", "certkv_tree_workspace_bytes", "certkv_tree_attn")
 
 _lock = threading.Lock()
 _lib = None
@@ -143,6 +177,26 @@ def load_library(path: Optional[str] = None):
         lib.certkv_sampled_compensation.argtypes = [sp, P, P, P, kp, ctypes.c_float, I32, P, P, P,
                                                     P, SZ, P]
         lib.certkv_sampled_compensation.restype = ctypes.c_int
+        rp, ap, tp = (ctypes.POINTER(certkv_rows), ctypes.POINTER(certkv_rope_angles),
+                      ctypes.POINTER(certkv_store))
+        lib.certkv_rope_plan.argtypes = [I32, I32, ctypes.c_double,
+                                         ctypes.POINTER(certkv_rope_scaling), ap]
+        lib.certkv_rope_plan.restype = ctypes.c_int
+        lib.certkv_rope.argtypes = [I32, I32, I32, I32, I32, rp, rp, rp, rp, P, ap, I32, P]
+        lib.certkv_rope.restype = ctypes.c_int
+        lib.certkv_store_workspace_bytes.argtypes = [I32]
+        lib.certkv_store_workspace_bytes.restype = SZ
+        lib.certkv_store_load.argtypes = [kp, I32, I32, tp, P, SZ, P]
+        lib.certkv_store_load.restype = ctypes.c_int
+        lib.certkv_store_append.argtypes = [I32, I32, I32, I32, rp, rp, P, P, P, tp, P]
+        lib.certkv_store_append.restype = ctypes.c_int
+        lib.certkv_store_read.argtypes = [tp, P, I32, P, P, P]
+        lib.certkv_store_read.restype = ctypes.c_int
+        lib.certkv_tree_workspace_bytes.argtypes = [sp, I32]
+        lib.certkv_tree_workspace_bytes.restype = SZ
+        lib.certkv_tree_attn.argtypes = [sp, I32, rp, rp, rp, P, tp, ctypes.c_float, rp, P, P, SZ,
+                                         P]
+        lib.certkv_tree_attn.restype = ctypes.c_int
         _lib = lib
         return lib
 
@@ -607,4 +661,277 @@ def certkv_decode_attn_noalloc(q, packed: Packed, *, hkv: int, scale: float = 0.
                                                    int(packed.tail_slot), _ptr(out),
                                                    _stream(stream))
     _check(rc, "certkv_decode_attn_noalloc")
+    return out
+
+
+# ------------------------------------------------------------------------------
+# Drafted tokens over the compressed cache: rotary positions, the paged store and
+# attention of a tree of drafted tokens (see include/certkv.h).
+
+def _rows(t: torch.Tensor, name: str) -> certkv_rows:
+    """The certkv_rows view of a bf16 CUDA tensor [B][L][T][heads][128] with
+    contiguous rows and any other strides."""
+    if t.dim() != 5 or t.shape[4] != 128 or t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be a bfloat16 tensor [B][L][T][heads][128]")
+    sb, sl, st, sh, sd = t.stride()
+    if not t.is_cuda or sd != 1:
+        raise ValueError(f"{name} must be a CUDA tensor whose rows are contiguous")
+    return certkv_rows(t.data_ptr(), sb, sl, st, sh)
+
+
+def _index(t: Optional[torch.Tensor], name: str, shape: tuple, dtype=torch.int32):
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {shape}")
+    return _ptr(t)
+
+
+def _keep_for(stream, *made):
+    """Tensors this module allocated for a call on another stream than the current
+    one stay allocated until that stream has used them."""
+    if stream is not None and stream != torch.cuda.current_stream():
+        for t in made:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def certkv_rope_plan(dim: int = 128, *, layout: str = "half", base: float = 10000.0,
+                     scaling: str = "none", factor: float = 1.0, original: float = 8192.0,
+                     low: float = 1.0, high: float = 32.0,
+                     magnitude: float = 1.0) -> certkv_rope_angles:
+    """The rotation of the first `dim` elements of every row, worked out once.
+    layout: "half" (pairs i, i + dim / 2) or "interleaved" (2 i, 2 i + 1);
+    scaling: "none", "linear", "ntk" or "ramp" (original, low and high are the
+    ramp's)."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise ValueError(f"layout is one of {tuple(ROPE_LAYOUTS)}, scaling of "
+                         f"{tuple(ROPE_SCALINGS)}")
+    sc = certkv_rope_scaling(ROPE_SCALINGS[scaling], factor, original, low, high, magnitude)
+    plan = certkv_rope_angles()
+    rc = load_library().certkv_rope_plan(int(dim), ROPE_LAYOUTS[layout], float(base),
+                                         ctypes.byref(sc), ctypes.byref(plan))
+    _check(rc, "certkv_rope_plan")
+    return plan
+
+
+def certkv_rope(q, positions, plan: certkv_rope_angles, k=None, *, out=None, k_out=None,
+                inverse: bool = False, stream=None):
+    """Rotate q [B][L][T][Hq][128] and, when given, k [B][L][T][H][128] to
+    positions int32 [B][T], in one launch.  out / k_out may be the inputs
+    (rotation in place).  Returns out, or (out, k_out) when k is given."""
+    B, L, T, Hq, _ = q.shape
+    rq = _rows(q, "q")
+    made = []
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        made.append(out)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    ro = _rows(out, "out")
+    H, rk, rko = 0, None, None
+    if k is not None:
+        H = k.shape[3]
+        if tuple(k.shape[:3]) != (B, L, T):
+            raise ValueError("k must have the sequences, layers and tokens of q")
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            made.append(k_out)
+        elif k_out.shape != k.shape:
+            raise ValueError("k_out must have the shape of k")
+        rk, rko = ctypes.byref(_rows(k, "k")), ctypes.byref(_rows(k_out, "k_out"))
+    rc = load_library().certkv_rope(B, L, T, Hq, H, ctypes.byref(rq), ctypes.byref(ro), rk, rko,
+                                    _index(positions, "positions", (B, T)), ctypes.byref(plan),
+                                    int(bool(inverse)), _stream(stream))
+    _check(rc, "certkv_rope")
+    _keep_for(stream, *made)
+    return out if k is None else (out, k_out)
+
+
+@dataclass(frozen=True)
+class Store:
+    """Caller-owned paged store (certkv_store in include/certkv.h): k, v codes
+    [pool_pages][64][128] (bf16, 8-bit) or [pool_pages][64][64] (two 4-bit codes a
+    byte); scales fp32 [pool_pages][64] for fp8 and fp4; group scales 8-bit
+    [pool_pages][64][8] for fp4; table int32 [units][max_pages]; counts int32
+    [units]; status (optional) int32 [1]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    counts: torch.Tensor
+    format: str = "bf16"
+    k_group: Optional[torch.Tensor] = None
+    v_group: Optional[torch.Tensor] = None
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    status: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        if self.format not in STORE_FORMATS:
+            raise ValueError(f"format is one of {tuple(STORE_FORMATS)}")
+        pages, width = self.k.shape[0], {"bf16": 256, "fp8": 128, "fp4": 64}[self.format]
+        for name in ("k", "v"):
+            t = getattr(self, name)
+            if t.dim() != 3 or tuple(t.shape[:2]) != (pages, STORE_PAGE) or \
+                    t.shape[2] * t.element_size() != width:
+                raise ValueError(f"{name} must be [pool_pages][{STORE_PAGE}][{width} bytes]")
+            s, g = getattr(self, name + "_scale"), getattr(self, name + "_group")
+            if self.format != "bf16" and (s is None or s.dtype != torch.float32 or
+                                          tuple(s.shape) != (pages, STORE_PAGE)):
+                raise ValueError(f"{name}_scale must be float32 [pool_pages][{STORE_PAGE}]")
+            if self.format == "fp4" and (g is None or g.element_size() != 1 or
+                                         tuple(g.shape) != (pages, STORE_PAGE, 8)):
+                raise ValueError(f"{name}_group must be 8-bit [pool_pages][{STORE_PAGE}][8]")
+        if self.table.dtype != torch.int32 or self.table.dim() != 2 or \
+                self.counts.dtype != torch.int32 or self.counts.shape != self.table.shape[:1]:
+            raise ValueError("table must be int32 [units][max_pages], counts int32 [units]")
+        if self.status is not None and (self.status.element_size() != 4 or
+                                        self.status.numel() != 1):
+            raise ValueError("status must be one 32-bit integer")
+        quant, four = self.format != "bf16", self.format == "fp4"
+        object.__setattr__(self, "_struct", certkv_store(
+            self.table.shape[0], STORE_FORMATS[self.format], self.table.shape[1], pages,
+            _ptr(self.k), _ptr(self.v), _ptr(self.k_group) if four else None,
+            _ptr(self.v_group) if four else None, _ptr(self.k_scale) if quant else None,
+            _ptr(self.v_scale) if quant else None, _ptr(self.table), _ptr(self.counts),
+            _ptr(self.status)))
+
+    @property
+    def units(self) -> int:
+        return self.table.shape[0]
+
+    def struct(self) -> certkv_store:
+        return self._struct
+
+    def read_status(self) -> int:
+        """CERTKV_STATUS_STORE when a call met a slot without a page (synchronises)."""
+        return 0 if self.status is None else int(self.status.item())
+
+    @staticmethod
+    def empty(units: int, max_pages: int, format: str = "bf16", *, pool_pages: Optional[int] = None,
+              device="cuda") -> "Store":
+        """An empty store.  Without pool_pages every segment owns max_pages pages;
+        with it the table starts without pages (certkv_store_load hands them out,
+        or the caller writes the table)."""
+        own = pool_pages is None
+        pages = units * max_pages if own else pool_pages
+        table = (torch.arange(pages, dtype=torch.int32, device=device).view(units, max_pages)
+                 if own else torch.full((units, max_pages), -1, dtype=torch.int32, device=device))
+        kw = {}
+        for name in ("k", "v"):
+            if format == "bf16":
+                kw[name] = torch.empty((pages, STORE_PAGE, 128), dtype=torch.bfloat16,
+                                       device=device)
+                continue
+            kw[name + "_scale"] = torch.empty((pages, STORE_PAGE), dtype=torch.float32,
+                                              device=device)
+            if format == "fp8":
+                kw[name] = torch.empty((pages, STORE_PAGE, 128), dtype=torch.float8_e4m3fn,
+                                       device=device)
+            else:
+                kw[name] = torch.empty((pages, STORE_PAGE, 64), dtype=torch.uint8, device=device)
+                kw[name + "_group"] = torch.empty((pages, STORE_PAGE, 8),
+                                                  dtype=torch.float8_e4m3fn, device=device)
+        return Store(table=table, counts=torch.zeros(units, dtype=torch.int32, device=device),
+                     format=format, status=torch.zeros(1, dtype=torch.int32, device=device), **kw)
+
+
+def certkv_store_workspace_bytes(units: int) -> int:
+    return int(load_library().certkv_store_workspace_bytes(int(units)))
+
+
+def certkv_store_load(packed: Packed, store: Store, reserve: int = 0, *, ws=None,
+                      stream=None) -> Store:
+    """Quantise a packed cache into the store as its first contents, with room for
+    at least `reserve` further slots per segment."""
+    if packed.real_counts.numel() != store.units:
+        raise ValueError("the store must have one segment per unit of the packed cache")
+    made = None
+    if ws is None:
+        ws = made = workspace(certkv_store_workspace_bytes(store.units), store.k.device)
+    pst = packed.struct()
+    rc = load_library().certkv_store_load(ctypes.byref(pst), int(packed.tail_slot), int(reserve),
+                                          ctypes.byref(store.struct()), _ptr(ws),
+                                          ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "certkv_store_load")
+    _keep_for(stream, made)
+    return store
+
+
+def certkv_store_append(k, v, store: Store, *, select=None, accepted=None, start=None,
+                        stream=None) -> Store:
+    """Quantise the rows k, v [B][L][T][H][128] into the slots from start[u] (int32
+    [units]; None: after the live ones).  accepted int32 [B]: rows of each
+    sequence (None: T); select int32 [B][T]: the token of each row (None: in
+    order)."""
+    B, L, T, H, _ = k.shape
+    if v.shape != k.shape:
+        raise ValueError("v must have the shape of k")
+    rk, rv = _rows(k, "k"), _rows(v, "v")
+    rc = load_library().certkv_store_append(
+        B, L, H, T, ctypes.byref(rk), ctypes.byref(rv), _index(select, "select", (B, T)),
+        _index(accepted, "accepted", (B,)), _index(start, "start", (store.units,)),
+        ctypes.byref(store.struct()), _stream(stream))
+    _check(rc, "certkv_store_append")
+    return store
+
+
+def certkv_store_read(store: Store, tokens: int, *, start=None, k_out=None, v_out=None,
+                      stream=None):
+    """`tokens` slots of every segment from start[u] (int32 [units]; None: 0) as bf16
+    (k, v) [units][tokens][128]; slots past the live ones read as 0."""
+    shape, made = (store.units, int(tokens), 128), []
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=torch.bfloat16, device=store.k.device)
+        made.append(k_out)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=torch.bfloat16, device=store.k.device)
+        made.append(v_out)
+    rc = load_library().certkv_store_read(
+        ctypes.byref(store.struct()), _index(start, "start", (store.units,)), int(tokens),
+        _index(k_out, "k_out", shape, torch.bfloat16),
+        _index(v_out, "v_out", shape, torch.bfloat16), _stream(stream))
+    _check(rc, "certkv_store_read")
+    _keep_for(stream, *made)
+    return k_out, v_out
+
+
+def certkv_tree_workspace_bytes(B: int, L: int, Hq: int, H: int, tokens: int) -> int:
+    shape = certkv_shape(B, L, Hq, H, 2, 128, 1)  # n and w are not used
+    return int(load_library().certkv_tree_workspace_bytes(ctypes.byref(shape), int(tokens)))
+
+
+def certkv_tree_attn(q, store: Store, *, hkv: int, k_new=None, v_new=None, mask=None,
+                     scale: float = 0.0, out=None, lse=None, ws=None, stream=None) -> torch.Tensor:
+    """Attention of the drafted tokens' queries q [B][L][T][Hq][128] over the store's
+    segments and the drafts' own keys and values k_new, v_new [B][L][T][H][128].
+    mask int64 [B][T]: bit j of word t set where token t sees draft j (None: j <= t).
+    lse (optional output) fp32 [B][L][T][Hq]."""
+    B, L, T, Hq, _ = q.shape
+    shape = certkv_shape(B, L, Hq, int(hkv), 2, 128, 1)
+    rq = _rows(q, "q")
+    made = []
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        made.append(out)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    ro = _rows(out, "out")
+    rk = rv = None
+    if k_new is not None or v_new is not None:
+        if k_new is None or v_new is None or k_new.shape != v_new.shape or \
+                tuple(k_new.shape[:4]) != (B, L, T, hkv):
+            raise ValueError("k_new and v_new must both be [B][L][T][hkv][128]")
+        rk, rv = ctypes.byref(_rows(k_new, "k_new")), ctypes.byref(_rows(v_new, "v_new"))
+    lib = load_library()
+    if ws is None:
+        ws = workspace(int(lib.certkv_tree_workspace_bytes(ctypes.byref(shape), T)), q.device)
+        made.append(ws)
+    rc = lib.certkv_tree_attn(
+        ctypes.byref(shape), T, ctypes.byref(rq), rk, rv,
+        _index(mask, "mask", (B, T), torch.int64), ctypes.byref(store.struct()), float(scale),
+        ctypes.byref(ro), _index(lse, "lse", (B, L, T, Hq), torch.float32), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream(stream))
+    _check(rc, "certkv_tree_attn")
+    _keep_for(stream, *made)
     return out

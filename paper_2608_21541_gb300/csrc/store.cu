@@ -1,0 +1,426 @@
+// store.cu — the paged store: quantising rows as they are written, from the
+// packed cache or from token rows, and reading them back.
+//
+// Eight lanes hold a row, sixteen elements each: a 32-byte load, three shuffles
+// for the row's maximum, and one scale group of the 4-bit format per lane, so
+// its group maximum needs no exchange.  Every row is read once and written
+// once; the kernels are bound by those bytes.
+#include "../../include/certkv.h"
+#include "common.cuh"
+#include "internal.cuh"
+#include "rows.cuh"
+#include "store.cuh"
+
+namespace certkv {
+namespace {
+
+constexpr int kStoreThreads = 256;
+constexpr float kTiny = 7.8886091e-31f;  // 2^-100: rows below are held as zeros
+
+struct Words16 {
+  uint32_t w[8];  // sixteen bf16
+};
+
+__device__ __forceinline__ Words16 load32(const void* p) {
+  Words16 x;
+  const uint4* q = reinterpret_cast<const uint4*>(p);
+  const uint4 a = __ldg(q), b = __ldg(q + 1);
+  x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w;
+  x.w[4] = b.x; x.w[5] = b.y; x.w[6] = b.z; x.w[7] = b.w;
+  return x;
+}
+
+// Encode the row held by this lane's group of eight lanes (sub = lane & 7 holds
+// elements 16 sub .. 16 sub + 15) and write it to pool slot `to` (to < 0:
+// nowhere).  Every lane of the warp takes part in the shuffles.
+template <int FMT>
+__device__ __forceinline__ void put_row(const Words16& x, int sub, int64_t to, uint8_t* codes,
+                                        uint8_t* group, float* scale) {
+  if (FMT == CERTKV_STORE_BF16) {
+    if (to < 0) return;
+    uint4* o = reinterpret_cast<uint4*>(codes + to * 256 + sub * 32);
+    o[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    o[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+    return;
+  }
+  // magnitudes of bf16 order as integers; a NaN or infinity is >= 0x7f80
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    top = max(top, (x.w[i] & 0x7fffu) << 16);
+    top = max(top, x.w[i] & 0x7fff0000u);
+  }
+  const float ag = __uint_as_float(top);  // the lane's own maximum (its group's)
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
+  const float amax = __uint_as_float(top);
+  const float kTop = FMT == CERTKV_STORE_FP8 ? 448.f : 2688.f;
+  const bool bad = top >= 0x7f800000u;
+  const bool zero = amax < kTiny || bad;
+  const float s = bad ? __int_as_float(0x7fc00000) : zero ? 1.f : __fmul_rn(amax, 1.f / kTop);
+  const float r = zero ? 0.f : __fmul_rn(__frcp_rn(amax), kTop);
+  if (to < 0) return;
+  if (sub == 0) scale[to] = s;
+  float m = r;
+  if (FMT == CERTKV_STORE_FP4) {
+    const uint32_t g8 = bad ? 0u : e4m3x2(__fmul_rn(__fmul_rn(ag, r), 1.f / 6.f), 0.f) & 0xffu;
+    const float gs = f16x2_to_f32(e4m3x2_to_f16x2(g8)).x;
+    m = gs > 0.f ? __fmul_rn(r, __frcp_rn(gs)) : 0.f;
+    group[to * kGroups + sub] = (uint8_t)g8;
+  }
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[2 * i] = bad ? 0.f : __fmul_rn(__uint_as_float(x.w[i] << 16), m);
+    v[2 * i + 1] = bad ? 0.f : __fmul_rn(__uint_as_float(x.w[i] & 0xffff0000u), m);
+  }
+  if (FMT == CERTKV_STORE_FP8) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      o[i] = e4m3x2(v[4 * i], v[4 * i + 1]) | (e4m3x2(v[4 * i + 2], v[4 * i + 3]) << 16);
+    *reinterpret_cast<uint4*>(codes + to * 128 + sub * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+  } else {
+    uint32_t o[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      o[i] = e2m1x2(v[8 * i], v[8 * i + 1]) | (e2m1x2(v[8 * i + 2], v[8 * i + 3]) << 8) |
+             (e2m1x2(v[8 * i + 4], v[8 * i + 5]) << 16) | (e2m1x2(v[8 * i + 6], v[8 * i + 7]) << 24);
+    *reinterpret_cast<uint2*>(codes + to * 64 + sub * 8) = make_uint2(o[0], o[1]);
+  }
+}
+
+// Sixteen elements of pool slot `at` as bf16 words.
+template <int FMT>
+__device__ __forceinline__ Words16 get_row(int sub, int64_t at, const uint8_t* codes,
+                                           const uint8_t* group, const float* scale) {
+  if (FMT == CERTKV_STORE_BF16) return load32(codes + at * 256 + sub * 32);
+  Words16 x;
+  const float s = scale[at];
+  if (FMT == CERTKV_STORE_FP8) {
+    const uint4 c = __ldg(reinterpret_cast<const uint4*>(codes + at * 128 + sub * 16));
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = f16x2_to_f32(e4m3x2_to_f16x2((w[i >> 1] >> (16 * (i & 1))) & 0xffffu));
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f.x * s, f.y * s);
+      x.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  } else {
+    const uint2 c = __ldg(reinterpret_cast<const uint2*>(codes + at * 64 + sub * 8));
+    const float gs = f16x2_to_f32(e4m3x2_to_f16x2(group[at * kGroups + sub])).x;
+    const uint32_t h[8] = {e2m1x2_to_f16x2<0>(c.x), e2m1x2_to_f16x2<1>(c.x),
+                           e2m1x2_to_f16x2<2>(c.x), e2m1x2_to_f16x2<3>(c.x),
+                           e2m1x2_to_f16x2<0>(c.y), e2m1x2_to_f16x2<1>(c.y),
+                           e2m1x2_to_f16x2<2>(c.y), e2m1x2_to_f16x2<3>(c.y)};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = f16x2_to_f32(h[i]);
+      const __nv_bfloat162 b = __floats2bfloat162_rn((f.x * gs) * s, (f.y * gs) * s);
+      x.w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+  }
+  return x;
+}
+
+// ------------------------------------------------------------------ load --
+// One block: first[u] = pages of the segments before u (as wanted, not cut),
+// first[units] = their sum, saturating at INT32_MAX.
+__global__ void __launch_bounds__(1024) load_plan_kernel(int units, const int32_t* __restrict__ real,
+                                                         int tail_slot, int reserve,
+                                                         int32_t* __restrict__ first) {
+  __shared__ long long wsum[32];
+  __shared__ long long carry;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) carry = 0;
+  __syncthreads();
+  for (int base = 0; base < units; base += 1024) {
+    const int u = base + threadIdx.x;
+    const long long v =
+        u < units ? ((long long)max(real[u], 0) + tail_slot + reserve + kPage - 1) / kPage : 0;
+    long long x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(kFull, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) wsum[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+      long long w = wsum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(kFull, w, o);
+        if (lane >= o) w += y;
+      }
+      wsum[lane] = w;
+    }
+    __syncthreads();
+    const long long excl = carry + (warp > 0 ? wsum[warp - 1] : 0) + x - v;
+    if (u < units) first[u] = (int32_t)min(excl, (long long)INT32_MAX);
+    __syncthreads();
+    if (threadIdx.x == 0) carry += wsum[31];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) first[units] = (int32_t)min(carry, (long long)INT32_MAX);
+}
+
+// Persistent: tables and counts, then the pages, one page of K and V rows per
+// block and step.
+template <int FMT>
+__global__ void __launch_bounds__(kStoreThreads) load_kernel(
+    Store st, const uint16_t* __restrict__ pk, const uint16_t* __restrict__ pv,
+    const int64_t* __restrict__ offsets, const int32_t* __restrict__ real, int tail_slot,
+    int64_t capacity, const int32_t* __restrict__ first) {
+  const int64_t entries = (int64_t)st.units * st.max_pages;
+  const int64_t tid = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x;
+  const int64_t step = (int64_t)gridDim.x * kStoreThreads;
+  for (int64_t e = tid; e < entries; e += step) {
+    const int u = (int)(e / st.max_pages), i = (int)(e - (int64_t)u * st.max_pages);
+    const int64_t page = (int64_t)first[u] + i;
+    st.table[e] = page < first[u + 1] && page < st.pool_pages ? (int)page : -1;
+  }
+  for (int64_t u = tid; u < st.units; u += step) {
+    const int n = max(real[u], 0) + tail_slot;
+    const int64_t have = min((int64_t)min(first[u + 1], st.pool_pages) - min(first[u], st.pool_pages),
+                             (int64_t)st.max_pages) * kPage;
+    const bool outside = offsets[u] < 0 || offsets[u] + n > capacity;
+    st.counts[u] = outside ? 0 : (int)min((int64_t)n, have);
+    if (outside || n > have) st.raise();
+  }
+  const int total = min(first[st.units], st.pool_pages);
+  const int grp = threadIdx.x >> 3, sub = threadIdx.x & 7;  // 32 rows at a time
+  for (int page = blockIdx.x; page < total; page += gridDim.x) {
+    int lo = 0, hi = st.units;  // the segment of this page: the last u with first[u] <= page
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= page) lo = mid;
+      else hi = mid;
+    }
+    const int u = lo, s0 = (page - first[u]) * kPage;
+    const int n = max(real[u], 0) + tail_slot;
+    const bool outside = offsets[u] < 0 || offsets[u] + n > capacity;
+    if (outside || page - first[u] >= st.max_pages) continue;  // uniform over the block
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int s = s0 + half * 32 + grp;
+      const bool live = s < n;
+      const int64_t from = (offsets[u] + s) * kD + sub * 16;
+      Words16 a = {}, b = {};
+      if (live) {
+        a = load32(pk + from);
+        b = load32(pv + from);
+      }
+      const int64_t to = live ? (int64_t)page * kPage + half * 32 + grp : -1;
+      put_row<FMT>(a, sub, to, st.k, st.kg, st.ks);
+      put_row<FMT>(b, sub, to, st.v, st.vg, st.vs);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- append --
+struct AppendArgs {
+  Rows k, v;
+  int L, H, T;
+  const int32_t *select, *accepted, *start;
+  int64_t rows;  // units T
+  int bump;      // write counts here (start does not alias them)
+};
+
+__device__ __forceinline__ int accepted_of(const AppendArgs& p, int b) {
+  return p.accepted ? min(max(p.accepted[b], 0), p.T) : p.T;
+}
+__device__ __forceinline__ int grown(const Store& st, int start, int m) {
+  return (int)min((int64_t)max(start, 0) + m, (int64_t)st.max_pages * kPage);
+}
+
+// Eight lanes per (segment, row): both K and V of it.
+template <int FMT>
+__global__ void __launch_bounds__(kStoreThreads) append_kernel(Store st, AppendArgs p) {
+  const int64_t id = ((int64_t)blockIdx.x * kStoreThreads + threadIdx.x) >> 3;
+  const int sub = threadIdx.x & 7;
+  Words16 a = {}, c = {};
+  int64_t to = -1;
+  if (id < p.rows) {
+    const int64_t u = id / p.T;
+    const int i = (int)(id - u * p.T);
+    const int bl = (int)(u / p.H), h = (int)(u - (int64_t)bl * p.H);
+    const int b = bl / p.L, l = bl - b * p.L;
+    const int m = accepted_of(p, b);
+    const int start = p.start[u];
+    if (i < m) {
+      const int t = p.select ? p.select[(int64_t)b * p.T + i] : i;
+      const int64_t s = (int64_t)start + i;
+      if (start >= 0 && s < (int64_t)st.max_pages * kPage && t >= 0 && t < p.T) to = st.slot(u, (int)s);
+      if (to >= 0) {
+        a = load32(p.k.at(b, l, t, h) + sub * 16);
+        c = load32(p.v.at(b, l, t, h) + sub * 16);
+      } else if (sub == 0) {
+        st.raise();
+      }
+    }
+    if (p.bump && i == 0 && sub == 0) {
+      st.counts[u] = grown(st, start, m);
+      if (p.accepted && p.accepted[b] != m) st.raise();
+    }
+  }
+  put_row<FMT>(a, sub, to, st.k, st.kg, st.ks);
+  put_row<FMT>(c, sub, to, st.v, st.vg, st.vs);
+}
+
+// counts[u] += m, after the rows were written at the old counts.
+__global__ void __launch_bounds__(kStoreThreads) append_count_kernel(Store st, AppendArgs p) {
+  const int64_t u = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x;
+  if (u >= st.units) return;
+  const int b = (int)(u / ((int64_t)p.L * p.H));
+  const int m = accepted_of(p, b);
+  if (p.accepted && p.accepted[b] != m) st.raise();
+  st.counts[u] = grown(st, p.start[u], m);
+}
+
+// ------------------------------------------------------------------ read --
+template <int FMT>
+__global__ void __launch_bounds__(kStoreThreads) read_kernel(Store st, const int32_t* __restrict__ start,
+                                                             int T, int64_t rows,
+                                                             uint16_t* __restrict__ ko,
+                                                             uint16_t* __restrict__ vo) {
+  const int64_t id = ((int64_t)blockIdx.x * kStoreThreads + threadIdx.x) >> 3;
+  const int sub = threadIdx.x & 7;
+  if (id >= rows) return;
+  const int64_t u = id / T;
+  const int64_t s = (start ? start[u] : 0) + (id - u * T);
+  const int64_t at = s >= 0 && s < st.count(u) ? st.slot(u, (int)s) : -1;
+  Words16 a = {}, b = {};
+  if (at >= 0) {
+    a = get_row<FMT>(sub, at, st.k, st.kg, st.ks);
+    b = get_row<FMT>(sub, at, st.v, st.vg, st.vs);
+  }
+  uint4* oa = reinterpret_cast<uint4*>(ko + id * kD + sub * 16);
+  uint4* ob = reinterpret_cast<uint4*>(vo + id * kD + sub * 16);
+  oa[0] = make_uint4(a.w[0], a.w[1], a.w[2], a.w[3]);
+  oa[1] = make_uint4(a.w[4], a.w[5], a.w[6], a.w[7]);
+  ob[0] = make_uint4(b.w[0], b.w[1], b.w[2], b.w[3]);
+  ob[1] = make_uint4(b.w[4], b.w[5], b.w[6], b.w[7]);
+}
+
+int last_error() { return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA; }
+
+// blocks for `rows` rows of eight lanes; 0: too many
+unsigned row_blocks(int64_t rows) {
+  const int64_t blocks = (rows + kStoreThreads / 8 - 1) / (kStoreThreads / 8);
+  return blocks <= INT32_MAX ? (unsigned)blocks : 0u;
+}
+
+}  // namespace
+}  // namespace certkv
+
+extern "C" size_t certkv_store_workspace_bytes(int32_t units) {
+  if (units < 1 || units > (1 << 24)) return 0;
+  return ((size_t)units + 1) * sizeof(int32_t);
+}
+
+extern "C" int certkv_store_load(const certkv_packed* packed, int32_t tail_slot, int32_t reserve,
+                                 const certkv_store* store, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  using namespace certkv;
+  Store s;
+  int rc = store_of(store, &s);
+  if (rc) return rc;
+  if (!packed || !packed->k || !packed->v || !packed->offsets || !packed->real_counts ||
+      packed->capacity_slots < 1)
+    return CERTKV_EINVAL;
+  if (((uintptr_t)packed->k | (uintptr_t)packed->v) % 16 != 0) return CERTKV_EINVAL;
+  if (((uintptr_t)packed->offsets % 8 | (uintptr_t)packed->real_counts % 4) != 0) return CERTKV_EINVAL;
+  if ((tail_slot != 0 && tail_slot != 1) || reserve < 0) return CERTKV_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 256 != 0 ||
+      workspace_bytes < certkv_store_workspace_bytes(s.units))
+    return CERTKV_EWORKSPACE;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  int32_t* first = reinterpret_cast<int32_t*>(workspace);
+  {
+    TraceScope ts_("store_plan", st);
+    load_plan_kernel<<<1, 1024, 0, st>>>(s.units, packed->real_counts, tail_slot, reserve, first);
+  }
+  // enough blocks for every page, at most eight on each SM
+  const int grid = s.pool_pages < 152 * 8 ? s.pool_pages : 152 * 8;
+  const uint16_t* pk = reinterpret_cast<const uint16_t*>(packed->k);
+  const uint16_t* pv = reinterpret_cast<const uint16_t*>(packed->v);
+  TraceScope ts_("store_load", st);
+#define CERTKV_LOAD(F)                                                                          \
+  load_kernel<F><<<grid, kStoreThreads, 0, st>>>(s, pk, pv, packed->offsets, packed->real_counts, \
+                                                 tail_slot, packed->capacity_slots, first)
+  if (store->format == CERTKV_STORE_BF16) CERTKV_LOAD(CERTKV_STORE_BF16);
+  else if (store->format == CERTKV_STORE_FP8) CERTKV_LOAD(CERTKV_STORE_FP8);
+  else CERTKV_LOAD(CERTKV_STORE_FP4);
+#undef CERTKV_LOAD
+  return last_error();
+}
+
+extern "C" int certkv_store_append(int32_t batch, int32_t layers, int32_t hkv, int32_t tokens,
+                                   const certkv_rows* k, const certkv_rows* v,
+                                   const int32_t* select, const int32_t* accepted,
+                                   const int32_t* start, const certkv_store* store, void* stream) {
+  using namespace certkv;
+  Store s;
+  int rc = store_of(store, &s);
+  if (rc) return rc;
+  if (batch < 1 || layers < 1 || hkv < 1 || tokens < 1 || tokens > (1 << 24)) return CERTKV_EINVAL;
+  if ((int64_t)batch * layers > (1 << 24) || (int64_t)batch * layers * hkv != s.units)
+    return CERTKV_EINVAL;
+  if (!rows_ok(k, batch, layers, tokens, hkv) || !rows_ok(v, batch, layers, tokens, hkv))
+    return CERTKV_EINVAL;
+  if (((uintptr_t)select | (uintptr_t)accepted | (uintptr_t)start) % 4 != 0) return CERTKV_EINVAL;
+  AppendArgs p;
+  p.k = rows_of(k);
+  p.v = rows_of(v);
+  p.L = layers;
+  p.H = hkv;
+  p.T = tokens;
+  p.select = select;
+  p.accepted = accepted;
+  p.start = start ? start : s.counts;
+  p.bump = p.start != s.counts;
+  p.rows = (int64_t)s.units * tokens;
+  const unsigned grid = row_blocks(p.rows);
+  if (!grid) return CERTKV_EINVAL;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  {
+    TraceScope ts_("store_append", st);
+    if (store->format == CERTKV_STORE_BF16)
+      append_kernel<CERTKV_STORE_BF16><<<grid, kStoreThreads, 0, st>>>(s, p);
+    else if (store->format == CERTKV_STORE_FP8)
+      append_kernel<CERTKV_STORE_FP8><<<grid, kStoreThreads, 0, st>>>(s, p);
+    else
+      append_kernel<CERTKV_STORE_FP4><<<grid, kStoreThreads, 0, st>>>(s, p);
+  }
+  if (!p.bump) {
+    TraceScope ts_("store_count", st);
+    append_count_kernel<<<(s.units + kStoreThreads - 1) / kStoreThreads, kStoreThreads, 0, st>>>(s, p);
+  }
+  return last_error();
+}
+
+extern "C" int certkv_store_read(const certkv_store* store, const int32_t* start, int32_t tokens,
+                                 void* k_out, void* v_out, void* stream) {
+  using namespace certkv;
+  Store s;
+  int rc = store_of(store, &s);
+  if (rc) return rc;
+  if (tokens < 1 || tokens > (1 << 24) || !k_out || !v_out ||
+      ((uintptr_t)k_out | (uintptr_t)v_out) % 16 != 0 || (uintptr_t)start % 4 != 0)
+    return CERTKV_EINVAL;
+  const int64_t rows = (int64_t)s.units * tokens;
+  const unsigned grid = row_blocks(rows);
+  if (!grid) return CERTKV_EINVAL;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  uint16_t* ko = reinterpret_cast<uint16_t*>(k_out);
+  uint16_t* vo = reinterpret_cast<uint16_t*>(v_out);
+  TraceScope ts_("store_read", st);
+  if (store->format == CERTKV_STORE_BF16)
+    read_kernel<CERTKV_STORE_BF16><<<grid, kStoreThreads, 0, st>>>(s, start, tokens, rows, ko, vo);
+  else if (store->format == CERTKV_STORE_FP8)
+    read_kernel<CERTKV_STORE_FP8><<<grid, kStoreThreads, 0, st>>>(s, start, tokens, rows, ko, vo);
+  else
+    read_kernel<CERTKV_STORE_FP4><<<grid, kStoreThreads, 0, st>>>(s, start, tokens, rows, ko, vo);
+  return last_error();
+}
