@@ -5,117 +5,109 @@
 // over all counts[u] stored slots and the drafts j whose bit is set in token
 // t's mask word.  A draft that a row does not see is never read for it, so a
 // NaN there cannot reach it.
+//
+// Three launches: a scan of the segments' tile counts, the split kernel
+// (tree_tc.cu) over equal shares of all tiles, and the merge below, which joins
+// the records of the CTAs that met a unit in the log-sum-exp domain.
 #include <math.h>
 
 #include "../../include/certkv.h"
 #include "common.cuh"
 #include "internal.cuh"
-#include "rows.cuh"
-#include "store.cuh"
+#include "tree.cuh"
 
 namespace certkv {
 
-struct TreeArgs {
-  int L, H, G, T;     // layers, KV heads, query heads per KV head, drafted tokens
-  int units, rows;    // B L H, T G query rows per unit
-  Rows q, kn, vn, o;  // kn.p null: the drafts have no keys of their own
-  const uint64_t* mask;
-  float* lse;
-  float scale_log2;
-  Store st;
-};
-
-constexpr float kLn2 = 0.69314718055994531f;
-
-// Elements 4 lane .. 4 lane + 3 of pool slot `at` in fp32.
-template <int FMT>
-__device__ __forceinline__ float4 held4(int lane, int64_t at, const uint8_t* codes,
-                                        const uint8_t* group, const float* scale) {
-  if (FMT == CERTKV_STORE_BF16) {
-    const uint2 x = *reinterpret_cast<const uint2*>(codes + at * 256 + lane * 8);
-    return make_float4(bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y));
-  }
-  const float s = scale[at];
-  float2 a, b;
-  float f = s;
-  if (FMT == CERTKV_STORE_FP8) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + at * 128 + lane * 4);
-    a = f16x2_to_f32(e4m3x2_to_f16x2(w & 0xffffu));
-    b = f16x2_to_f32(e4m3x2_to_f16x2(w >> 16));
-  } else {
-    const uint32_t w = *reinterpret_cast<const uint16_t*>(codes + at * 64 + lane * 2);
-    a = f16x2_to_f32(e2m1x2_to_f16x2<0>(w));
-    b = f16x2_to_f32(e2m1x2_to_f16x2<1>(w));
-    f = s * f16x2_to_f32(e4m3x2_to_f16x2(group[at * kGroups + lane / 4])).x;
-  }
-  return make_float4(a.x * f, a.y * f, b.x * f, b.y * f);
-}
-
-__device__ __forceinline__ float4 row4(const uint16_t* row, int lane) {
-  const uint2 x = *reinterpret_cast<const uint2*>(row + 4 * lane);
-  return make_float4(bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y));
-}
-
-struct RowState {
-  float m, l;
-  float4 a;
-  __device__ __forceinline__ void take(float x, float4 v) {  // log2-domain logit x
-    const float nm = fmaxf(m, x);
-    const float c = m == nm ? 1.f : exp2f(m - nm);
-    const float p = x == -INFINITY ? 0.f : exp2f(x - nm);  // a NaN logit stays one
-    m = nm;
-    l = l * c + p;
-    a.x = fmaf(p, v.x, a.x * c);
-    a.y = fmaf(p, v.y, a.y * c);
-    a.z = fmaf(p, v.z, a.z * c);
-    a.w = fmaf(p, v.w, a.w * c);
-  }
-};
-
-__device__ __forceinline__ float dot4(float4 a, float4 b) {
-  float x = a.x * b.x + a.y * b.y + a.z * b.z + a.w * b.w;
+// One block: first[u] = tiles of the segments before u, first[units] their sum.
+__global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int with_drafts,
+                                                         int64_t* __restrict__ first) {
+  __shared__ long long wsum[32];
+  __shared__ long long carry;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) carry = 0;
+  __syncthreads();
+  for (int base = 0; base < st.units; base += 1024) {
+    const int u = base + threadIdx.x;
+    const long long v =
+        u < st.units ? (st.count(u) + kTreeTile - 1) / kTreeTile + with_drafts : 0;
+    long long x = v;
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(kFull, x, o);
-  return x;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(kFull, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) wsum[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+      long long w = wsum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(kFull, w, o);
+        if (lane >= o) w += y;
+      }
+      wsum[lane] = w;
+    }
+    __syncthreads();
+    if (u < st.units) first[u] = carry + (warp > 0 ? wsum[warp - 1] : 0) + x - v;
+    __syncthreads();
+    if (threadIdx.x == 0) carry += wsum[31];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) first[st.units] = carry;
 }
 
-// One warp per (unit, row); a lane holds four dimensions.
-template <int FMT>
-__global__ void __launch_bounds__(128) tree_row_kernel(TreeArgs p) {
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+// One warp per (unit, row), a lane four dimensions: the records of the CTAs that
+// met the row's block, each weighted by its sum 2^C l, and what the split left
+// out: the NaN and infinite elements of drafts the row sees.
+__global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs p) {
+  const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (w >= (int64_t)p.units * p.rows) return;
   const int lane = threadIdx.x & 31;
-  const int64_t u = w / p.rows;
-  const int r = (int)(w - u * p.rows), t = r / p.G, g = r - t * p.G;
-  const int bl = (int)(u / p.H), h = (int)(u - (int64_t)bl * p.H);
-  const int b = bl / p.L, l = bl - b * p.L;
-  const float4 q = row4(p.q.at(b, l, t, h * p.G + g), lane);
-  RowState s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-  const int n = p.st.count(u);
-  for (int i = 0; i < n; ++i) {
-    const int64_t at = p.st.slot(u, i);
-    if (at < 0) {
-      if (lane == 0) p.st.raise();
-      continue;
+  const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
+  const int bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
+  const int blk = r / p.rb, br = r - blk * p.rb;
+  const int64_t n = p.first[u + 1] - p.first[u];
+  float M = -INFINITY, L = 0.f;
+  float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (n > 0) {
+    const int64_t per = tiles_per_cta(p), at = p.first[u] * p.nblk + blk * n;
+    const int64_t vu = (int64_t)u * p.nblk + blk;
+    const int c0 = (int)(at / per), c1 = (int)((at + n - 1) / per);
+    for (int c = c0; c <= c1; ++c) M = fmaxf(M, p.rec_ml[(c + vu) * p.rb + br].x);
+    for (int c = c0; c <= c1; ++c) {
+      const int64_t rec = (c + vu) * p.rb + br;
+      const float2 ml = p.rec_ml[rec];
+      if (ml.y == 0.f) continue;  // this CTA's tiles held nothing the row sees
+      const float4 a = *reinterpret_cast<const float4*>(p.rec_acc + rec * kD + 4 * lane);
+      const float f = ml.y * exp2f(ml.x - M);
+      L += f;
+      A.x = fmaf(a.x, f, A.x);
+      A.y = fmaf(a.y, f, A.y);
+      A.z = fmaf(a.z, f, A.z);
+      A.w = fmaf(a.w, f, A.w);
     }
-    const float x = dot4(q, held4<FMT>(lane, at, p.st.k, p.st.kg, p.st.ks)) * p.scale_log2;
-    s.take(x, held4<FMT>(lane, at, p.st.v, p.st.vg, p.st.vs));
   }
+  const float inv = L != 0.f ? 1.f / L : 0.f;  // a NaN sum stays a NaN
+  A.x *= inv;
+  A.y *= inv;
+  A.z *= inv;
+  A.w *= inv;
   if (p.kn.p) {
-    const uint64_t word = p.mask ? p.mask[(int64_t)b * p.T + t] : ~0ull >> (63 - t);
-    for (int j = 0; j < p.T; ++j)
-      if (word >> j & 1)
-        s.take(dot4(q, row4(p.kn.at(b, l, j, h), lane)) * p.scale_log2,
-               row4(p.vn.at(b, l, j, h), lane));
+    for (uint64_t odd = p.odd[u] & seen(p, b, t); odd; odd &= odd - 1) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p.vn.at(b, l, __ffsll((long long)odd) - 1, h) + 4 * lane);
+      const float v[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
+      if (!(fabsf(v[0]) < INFINITY)) A.x += v[0];
+      if (!(fabsf(v[1]) < INFINITY)) A.y += v[1];
+      if (!(fabsf(v[2]) < INFINITY)) A.z += v[2];
+      if (!(fabsf(v[3]) < INFINITY)) A.w += v[3];
+    }
   }
-  const float inv = s.l != 0.f ? 1.f / s.l : 0.f;  // a NaN sum stays a NaN
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(s.a.x * inv, s.a.y * inv);
-  const __nv_bfloat162 hi = __floats2bfloat162_rn(s.a.z * inv, s.a.w * inv);
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(A.x, A.y), hi = __floats2bfloat162_rn(A.z, A.w);
   *reinterpret_cast<uint2*>(p.o.at(b, l, t, h * p.G + g) + 4 * lane) =
       make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   if (p.lse && lane == 0)
     p.lse[((int64_t)bl * p.T + t) * p.H * p.G + h * p.G + g] =
-        s.l != 0.f ? (s.m + log2f(s.l)) * kLn2 : -INFINITY;
+        L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
 }
 
 namespace {
@@ -130,12 +122,40 @@ int tree_shape(const certkv_shape* s, int32_t tokens) {
   return CERTKV_OK;
 }
 
+// Query rows of a unit in blocks of at most 256, as equal as they come: up to
+// 128 rows go to the tensor cores as one M = 128 operand, up to 256 as two.
+void row_blocks(int rows, int* nblk, int* rb) {
+  *nblk = (rows + 255) / 256;
+  *rb = (rows + *nblk - 1) / *nblk;
+}
+
+constexpr int kTreeMaxCtas = 1024;  // records are sized for at most this many CTAs
+
+struct TreeLayout {
+  size_t first, odd, ml, acc, total;
+};
+TreeLayout tree_layout(int units, int rows) {
+  auto a = [](size_t x) { return (x + 255) / 256 * 256; };
+  int nblk, rb;
+  row_blocks(rows, &nblk, &rb);
+  const size_t recs = ((size_t)units * nblk + kTreeMaxCtas) * rb;
+  TreeLayout ly;
+  ly.first = 0;
+  ly.odd = a(((size_t)units + 1) * sizeof(int64_t));
+  ly.ml = ly.odd + a((size_t)units * sizeof(uint64_t));
+  ly.acc = ly.ml + a(recs * sizeof(float2));
+  ly.total = ly.acc + recs * kD * sizeof(float);
+  return ly;
+}
+
 }  // namespace
 }  // namespace certkv
 
 extern "C" size_t certkv_tree_workspace_bytes(const certkv_shape* shape, int32_t tokens) {
   if (certkv::tree_shape(shape, tokens)) return 0;
-  return 256;
+  return certkv::tree_layout(shape->batch * shape->layers * shape->hkv,
+                             tokens * (shape->hq / shape->hkv))
+      .total;
 }
 
 extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const certkv_rows* q,
@@ -173,15 +193,28 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   p.mask = mask;
   p.lse = lse;
   p.scale_log2 = (float)((scale > 0.0f ? scale : 1.0 / sqrt((double)kD)) * 1.4426950408889634);
+  row_blocks(p.rows, &p.nblk, &p.rb);
+  const int64_t merge = ((int64_t)p.units * p.rows + 7) / 8;
+  if (merge > INT32_MAX) return CERTKV_EINVAL;
+  p.ctas = tree_ctas();
+  if (p.ctas < 1) return CERTKV_ECUDA;
+  if (p.ctas > kTreeMaxCtas) p.ctas = kTreeMaxCtas;
+  const TreeLayout ly = tree_layout(p.units, p.rows);
+  char* ws = reinterpret_cast<char*>(workspace);
+  int64_t* first = reinterpret_cast<int64_t*>(ws + ly.first);
+  p.first = first;
+  p.odd = reinterpret_cast<uint64_t*>(ws + ly.odd);
+  p.rec_ml = reinterpret_cast<float2*>(ws + ly.ml);
+  p.rec_acc = reinterpret_cast<float*>(ws + ly.acc);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const int64_t blocks = ((int64_t)p.units * p.rows + 3) / 4;
-  if (blocks > INT32_MAX) return CERTKV_EINVAL;
-  TraceScope ts_("tree_row", st);
-  if (store->format == CERTKV_STORE_BF16)
-    tree_row_kernel<CERTKV_STORE_BF16><<<(unsigned)blocks, 128, 0, st>>>(p);
-  else if (store->format == CERTKV_STORE_FP8)
-    tree_row_kernel<CERTKV_STORE_FP8><<<(unsigned)blocks, 128, 0, st>>>(p);
-  else
-    tree_row_kernel<CERTKV_STORE_FP4><<<(unsigned)blocks, 128, 0, st>>>(p);
+  {
+    TraceScope ts_("tree_plan", st);
+    tree_plan_kernel<<<1, 1024, 0, st>>>(p.st, p.kn.p ? 1 : 0, first);
+  }
+  if (!launch_tree_tc(p, store->format, st)) return CERTKV_ECUDA;
+  {
+    TraceScope ts_("tree_merge", st);
+    tree_merge_kernel<<<(unsigned)merge, 256, 0, st>>>(p);
+  }
   return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA;
 }

@@ -1,0 +1,86 @@
+// tree.cuh — what the launches of one tree-attention call share.
+#pragma once
+
+#include <cuda.h>
+#include <stdint.h>
+
+#include "rows.cuh"
+#include "store.cuh"
+
+namespace certkv {
+
+constexpr int kTreeTile = 128;  // slots per tile: two pages
+constexpr float kLn2 = 0.69314718055994531f;
+
+struct TreeArgs {
+  int L, H, G, T;     // layers, KV heads, query heads per KV head, drafted tokens
+  int units, rows;    // B L H, T G query rows per unit
+  int nblk, rb;       // row blocks of a unit, rows of a block (the last may have fewer)
+  int ctas;           // CTAs the tiles are divided among
+  Rows q, kn, vn, o;  // kn.p null: the drafts have no keys of their own
+  const uint64_t* mask;
+  float* lse;
+  float scale_log2;
+  Store st;
+  // workspace
+  const int64_t* first;  // [units + 1] tiles of the segments before (one row block)
+  uint64_t* odd;         // [units] drafts whose value row holds a NaN or infinity
+  float2* rec_ml;        // [records][rb] log2-domain reference and sum
+  float* rec_acc;        // [records][rb][128] weighted mean of the values
+};
+
+// Drafts that token t of sequence b sees, as bits.
+__device__ __forceinline__ uint64_t seen(const TreeArgs& p, int b, int t) {
+  const uint64_t all = ~0ull >> (64 - p.T);
+  return (p.mask ? p.mask[(int64_t)b * p.T + t] : ~0ull >> (63 - t)) & all;
+}
+
+// Tiles [g0, g1) of CTA c: the global sequence (unit, row block, tile) in equal
+// consecutive shares.
+__device__ __forceinline__ int64_t tiles_per_cta(const TreeArgs& p) {
+  return (p.first[p.units] * p.nblk + p.ctas - 1) / p.ctas;
+}
+
+// One (CTA, unit, row block) that meet: their partial results are record
+// c + unit nblk + block.
+struct Item {
+  int u, blk;      // unit, row block
+  int ka, kb, n;   // its tiles [ka, kb) of n, the last of them the drafts' own
+};
+
+// Walks over the items of a CTA.
+struct Items {
+  int64_t g, g1;
+  int u, blk;
+  bool fresh;
+  __device__ __forceinline__ Items(const TreeArgs& p, int64_t per) {
+    const int64_t total = p.first[p.units] * p.nblk;
+    g = per * blockIdx.x;
+    g1 = min(total, g + per);
+    int lo = 0, hi = p.units;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (p.first[mid] * p.nblk <= g) lo = mid;
+      else hi = mid;
+    }
+    u = lo;
+  }
+  __device__ __forceinline__ bool next(const TreeArgs& p, Item* it) {
+    if (g >= g1) return false;
+    while (p.first[u + 1] * p.nblk <= g) ++u;
+    const int n = (int)(p.first[u + 1] - p.first[u]);
+    const int64_t in = g - p.first[u] * p.nblk;
+    it->u = u;
+    it->blk = (int)(in / n);
+    it->ka = (int)(in - (int64_t)it->blk * n);
+    it->kb = (int)min((int64_t)n, it->ka + (g1 - g));
+    it->n = n;
+    g += it->kb - it->ka;
+    return true;
+  }
+};
+
+int tree_ctas();  // CTAs of the split kernel on the current device; 0 on an error
+bool launch_tree_tc(const TreeArgs& p, int format, cudaStream_t st);
+
+}  // namespace certkv
