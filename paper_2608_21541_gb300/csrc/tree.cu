@@ -199,6 +199,8 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   p.ctas = tree_ctas();
   if (p.ctas < 1) return CERTKV_ECUDA;
   if (p.ctas > kTreeMaxCtas) p.ctas = kTreeMaxCtas;
+  // a CTA counts its tiles in 32 bits
+  if ((int64_t)p.units * (p.st.max_pages / 2 + 2) / p.ctas * p.nblk >= (1 << 30)) return CERTKV_EINVAL;
   const TreeLayout ly = tree_layout(p.units, p.rows);
   char* ws = reinterpret_cast<char*>(workspace);
   int64_t* first = reinterpret_cast<int64_t*>(ws + ly.first);

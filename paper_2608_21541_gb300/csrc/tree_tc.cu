@@ -14,10 +14,13 @@
 //
 // Roles per CTA (one per SM, persistent over a share of all tiles):
 //   warps 0..7   softmax: warp (stream, lane quadrant), a thread owns a row;
-//   warps 8..15  loaders: bf16 tiles by TMA; 8- and 4-bit tiles through
-//                registers, expanded to f16 in the MMAs' swizzled layout; the
-//                drafts' own tile in either case;
-//   warp 16      tensor-memory allocation, and the thread that issues the MMAs.
+//   warps 8..23  loaders: 8- and 4-bit tiles through registers, expanded to f16
+//                in the MMAs' swizzled layout; for every store the drafts' own
+//                tile and bf16 tiles that are not whole;
+//   warp 24      tensor-memory allocation, and the thread that issues the MMAs;
+//   warp 25      scout: walks the page table ahead of the loaders, states each
+//                tile's facts, copies whole bf16 tiles by TMA and has the pages
+//                of later tiles brought into L2.
 //
 // Precision.  bf16 store: bf16 products, and a weight enters P V as a bf16 part
 // plus the bf16 rounding of its remainder (2^-16).  8- and 4-bit stores: codes
@@ -43,44 +46,76 @@ namespace certkv {
 namespace {
 
 constexpr int kSoftWarps = 8, kLoadWarps = 8;
-constexpr int kThreads = (kSoftWarps + kLoadWarps + 1) * 32;
+constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
 constexpr int kLoaders = kLoadWarps * 32;
-constexpr int kStages = 2;
-constexpr int kMeta = 4;  // see Meta
-constexpr int kHalf = 128 * 128;           // bytes of 128 rows x 64 16-bit elements
-constexpr int kOperand = 2 * kHalf;        // 128 rows x 128 elements
-constexpr int kQOff = 0;                   // two row blocks
-constexpr int kKVOff = 2 * kOperand;       // stages of K | V
-constexpr int kMiscOff = kKVOff + kStages * 2 * kOperand;
-constexpr uint32_t kColS = 0, kColO = 256; // + 128 stream
-constexpr float kLazy = 8.f;               // growth of the maximum that moves the reference
+constexpr int kPieces = 4;  // (slot, 16-element) pieces of an operand per loader thread
+static_assert(kLoaders * kPieces == 128 * 8, "the loaders cover an operand");
+// Registers a thread: the launch gives 96 (640 threads), which the roles share
+// out among themselves.  A spill costs more here than elsewhere: next to 200 KB
+// of shared memory the L1 holds hardly any of it.
+constexpr int kSoftRegs = 112, kLoadRegs = 96, kIssueRegs = 56;
+static_assert(kSoftWarps * 32 * kSoftRegs + kLoaders * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
+              "a larger split would wait for registers for ever");
+constexpr int kHalf = 128 * 128;     // bytes of 128 rows x 64 16-bit elements
+constexpr int kOperand = 2 * kHalf;  // 128 rows x 128 elements
+constexpr int kAhead = 6;            // tiles the L2 prefetch runs ahead
+// Shared memory: the query blocks (two when both streams hold rows of their
+// own), then a ring of operands, then Misc.
+template <bool PAIR>
+struct Plan {
+  static constexpr int kRing = PAIR ? 4 : 5;
+  static constexpr int kRingOff = (PAIR ? 2 : 1) * kOperand;
+  static constexpr int kMiscOff = kRingOff + kRing * kOperand;
+};
+// The operands of the n tiles of a CTA pass through the ring in the order K(0),
+// then K(t + 1), V(t) for t = 0 .., near the order the MMAs take them in.
+__device__ __forceinline__ uint32_t k_seq(uint32_t t) { return t == 0 ? 0u : 2u * t - 1u; }
+__device__ __forceinline__ uint32_t v_seq(uint32_t t, uint32_t n) { return min(2u * t + 2u, 2u * n - 1u); }
+// Place of operand i in the ring, and the parity of that use.
+template <bool PAIR>
+struct Place {
+  uint32_t slot, phase;
+  __device__ __forceinline__ explicit Place(uint32_t i)
+      : slot(i % Plan<PAIR>::kRing), phase((i / Plan<PAIR>::kRing) & 1u) {}
+};
+constexpr uint32_t kColS = 0, kColO = 256;  // + 128 stream
+constexpr float kLazy = 8.f;                // growth of the maximum that moves the reference
 
-// Per-tile facts for the softmax.  Slot t % kMeta is written again with tile
-// t + kMeta, whose key stage is free only once the products with tile
-// t + kMeta - kStages are done; those were issued after P of tile t had been
-// written, so the softmax has read slot t by then (kMeta >= kStages + 2).
+// A tile's facts, stated by the scout four tiles ahead of its keys.  Slot t % 8 is
+// written again, for tile t + 8, once the place of K(t + 4) is free; that place
+// held V(t) (ring of 5) or K(t + 2) (ring of 4), both released by products issued
+// after P of tile t had been written, so every reader of slot t is done.
+constexpr uint32_t kMeta = 8;
 struct Meta {
-  float ks[kTreeTile];  // scale of the key of each slot (8- and 4-bit stores)
+  float ks[kTreeTile];  // scale of each slot's key (8- and 4-bit stores)
+  float vf[kTreeTile];  // scale of each slot's value over 2^shift
   uint32_t live[4];     // slots to take
-  int shift;            // exponent the tile's values were divided by
+  int a, b;             // the tile's pages (-1: none)
+  int count;            // live slots from the tile's first on
+  int shift;            // exponent the tile's values are divided by
   int whole;            // every slot is live
   int drafts;           // the drafts' own tile: live comes from the row's mask
-  int pad;
+  int unit, first_block;
 };
 
 struct Misc {
-  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full, meta_full[kMeta], done;
+  uint64_t full[5], empty[5];                // places of the ring
+  uint64_t stated[kMeta], ready[kMeta];      // scout -> loaders, loaders -> softmax
+  uint64_t s_full[2], p_full[2], o_full[2], q_full, done;
   uint32_t tmem;
   int abort;
   unsigned long long odd;
   float red[kLoadWarps];
-  float qs[256];                    // per row: scale of its f16 queries
-  float cm[128], l[128], sh[128];   // stream 1's reference, sum and shift
+  float qs[256];                   // per row: scale of its f16 queries
+  float cm[128], l[128], sh[128];  // stream 1's reference, sum and shift
   Meta meta[kMeta];
 };
-constexpr int kSmemBytes = kMiscOff + (int)sizeof(Misc) + 1024;
-static_assert(kSmemBytes <= 232448, "over the 227 KB of shared memory a CTA can have");
+template <bool PAIR>
+constexpr int smem_bytes() {
+  return Plan<PAIR>::kMiscOff + (int)sizeof(Misc) + 1024;
+}
+static_assert(smem_bytes<true>() <= 232448 && smem_bytes<false>() <= 232448,
+              "over the 227 KB of shared memory a CTA can have");
 
 __device__ __forceinline__ uint32_t bar(const uint64_t* b) { return tc::saddr(b); }
 __device__ __forceinline__ void loaders_sync() {
@@ -104,21 +139,33 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // |e| < 127
 
-// The 32 bytes of elements 16 sub .. 16 sub + 15 of a row into the swizzled
-// operand at `base`.  The eight lanes of a row store their two chunks in
-// opposite order above and below element 64, so that they meet different banks.
-__device__ __forceinline__ void put32(uint32_t base, int row, int sub, const uint32_t (&w)[8]) {
-  const uint32_t r = base + (uint32_t)((sub >> 2) * kHalf + row * 128);
-  const int c = 2 * (sub & 3), x = row & 7;
-  const uint32_t a0 = r + (uint32_t)((c ^ x) << 4), a1 = r + (uint32_t)(((c + 1) ^ x) << 4);
-  if (sub < 4) {
-    sts128(a0, w[0], w[1], w[2], w[3]);
-    sts128(a1, w[4], w[5], w[6], w[7]);
-  } else {
-    sts128(a1, w[4], w[5], w[6], w[7]);
-    sts128(a0, w[0], w[1], w[2], w[3]);
+// A loader thread's part of an operand: elements 16 sub .. 16 sub + 15 of the
+// rows grp, grp + 32, + 64 and + 96.  A quarter warp holds the same half of two
+// neighbouring rows, which the swizzle puts into different banks.
+struct Piece {
+  int grp, sub;
+  uint32_t at0, at1;  // its two 16-byte chunks of row grp in a swizzled operand
+  __device__ __forceinline__ explicit Piece(int tid) {
+    const int lane = tid & 31;
+    grp = 4 * (tid >> 5) + 2 * (lane >> 4) + ((lane >> 2) & 1);
+    sub = (lane & 3) + 4 * ((lane >> 3) & 1);
+    const int c = 2 * (sub & 3), x = grp & 7;
+    const uint32_t r = (uint32_t)((sub >> 2) * kHalf + grp * 128);
+    at0 = r + (uint32_t)((c ^ x) << 4);
+    at1 = r + (uint32_t)(((c + 1) ^ x) << 4);
   }
-}
+  // row grp + 32 q of the operand at `to`
+  __device__ __forceinline__ void put(uint32_t to, int q, const uint32_t (&w)[8]) const {
+    sts128(to + at0 + (uint32_t)(q * 32 * 128), w[0], w[1], w[2], w[3]);
+    sts128(to + at1 + (uint32_t)(q * 32 * 128), w[4], w[5], w[6], w[7]);
+  }
+  // the eight lanes of a row
+  __device__ __forceinline__ static uint32_t row_max(uint32_t x) {
+    x = max(x, __shfl_xor_sync(kFull, x, 1));
+    x = max(x, __shfl_xor_sync(kFull, x, 2));
+    return max(x, __shfl_xor_sync(kFull, x, 8));
+  }
+};
 
 __device__ __forceinline__ void load32g(const void* p, uint32_t (&w)[8]) {
   const uint4* q = reinterpret_cast<const uint4*>(p);
@@ -149,464 +196,597 @@ __device__ __forceinline__ int exponent(float x) {
   return e == 0 || e == 255 ? 0 : e - 127;
 }
 
-// Raw codes of this thread's four (slot, 16-element) pieces of one operand.
+// Raw codes of this thread's pieces of one operand.
 template <int FMT>
 struct Raw {
-  uint32_t w[4][FMT == CERTKV_STORE_FP8 ? 4 : 2];
-  uint32_t g[FMT == CERTKV_STORE_FP4 ? 4 : 1];
+  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
+  uint32_t w[kPieces][kWords];
+  uint32_t g[FMT == CERTKV_STORE_FP4 ? kPieces : 1];
+
+  // the tile's pages a, b (-1: none), live slots from its first on
+  __device__ __forceinline__ void load(const Piece& pc, int a, int b, int live, const uint8_t* codes,
+                                       const uint8_t* group) {
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const int page = q < 2 ? a : b, row = pc.grp + 32 * (q & 1);
+      const bool on = page >= 0 && pc.grp + 32 * q < live;
+      const int64_t at = (int64_t)page * kPage + row;
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) w[q][j] = 0u;
+      if (on) {
+        if constexpr (FMT == CERTKV_STORE_FP8) {
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(codes + at * 128 + pc.sub * 16));
+          w[q][0] = x.x;
+          w[q][1] = x.y;
+          w[q][2] = x.z;
+          w[q][3] = x.w;
+        } else {
+          const uint2 x = __ldg(reinterpret_cast<const uint2*>(codes + at * 64 + pc.sub * 8));
+          w[q][0] = x.x;
+          w[q][1] = x.y;
+        }
+      }
+      if constexpr (FMT == CERTKV_STORE_FP4) g[q] = on ? (uint32_t)__ldg(group + at * kGroups + pc.sub) : 0u;
+    }
+  }
 };
 
-template <int FMT>
-__device__ __forceinline__ void load_raw(Raw<FMT>& r, const int64_t (&at)[4], int sub,
-                                         const uint8_t* codes, const uint8_t* group) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (FMT == CERTKV_STORE_FP8) {
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (at[i] >= 0) x = __ldg(reinterpret_cast<const uint4*>(codes + at[i] * 128 + sub * 16));
-      r.w[i][0] = x.x;
-      r.w[i][1] = x.y;
-      r.w[i][2 % (FMT == CERTKV_STORE_FP8 ? 4 : 2)] = x.z;
-      r.w[i][3 % (FMT == CERTKV_STORE_FP8 ? 4 : 2)] = x.w;
-    } else {
-      uint2 x = make_uint2(0u, 0u);
-      uint32_t g = 0;
-      if (at[i] >= 0) {
-        x = __ldg(reinterpret_cast<const uint2*>(codes + at[i] * 64 + sub * 8));
-        g = __ldg(group + at[i] * kGroups + sub);
-      }
-      r.w[i][0] = x.x;
-      r.w[i][1] = x.y;
-      r.g[i % (FMT == CERTKV_STORE_FP4 ? 4 : 1)] = g;
-    }
-  }
-}
-
-// One piece as f16: codes (with their group scale) times f; f unused for keys.
+// Piece q as f16: codes with their group scale, and for values times f.
 template <int FMT, bool VALUE>
-__device__ __forceinline__ void expand(const Raw<FMT>& r, int i, float f, uint32_t (&w)[8]) {
-  if (FMT == CERTKV_STORE_FP8) {
-    const uint32_t f2 = VALUE ? pack_f16(f, f) : 0u;
+__device__ __forceinline__ void expand(const Raw<FMT>& r, int q, float f, uint32_t (&w)[8]) {
+  if constexpr (FMT == CERTKV_STORE_FP8) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = e4m3x2_to_f16x2(r.w[i][(j >> 1) % (FMT == CERTKV_STORE_FP8 ? 4 : 2)] >> (16 * (j & 1)));
-      if (VALUE) w[j] = hmul2(w[j], f2);
+    for (int j = 0; j < 8; ++j) w[j] = e4m3x2_to_f16x2(r.w[q][j >> 1] >> (16 * (j & 1)));
+    if (VALUE) {
+      const uint32_t f2 = pack_f16(f, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = hmul2(w[j], f2);
     }
   } else {
-    const float gs = f16x2_to_f32(e4m3x2_to_f16x2(r.g[i % (FMT == CERTKV_STORE_FP4 ? 4 : 1)])).x;
-    const float x = VALUE ? gs * f : gs;
-    const uint32_t f2 = pack_f16(x, x);
+    uint32_t f2 = e4m3x2_to_f16x2(r.g[q] | (r.g[q] << 8));
+    if (VALUE) {
+      const float x = f16x2_to_f32(f2).x * f;
+      f2 = pack_f16(x, x);
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      w[4 * j] = hmul2(e2m1x2_to_f16x2<0>(r.w[i][j]), f2);
-      w[4 * j + 1] = hmul2(e2m1x2_to_f16x2<1>(r.w[i][j]), f2);
-      w[4 * j + 2] = hmul2(e2m1x2_to_f16x2<2>(r.w[i][j]), f2);
-      w[4 * j + 3] = hmul2(e2m1x2_to_f16x2<3>(r.w[i][j]), f2);
+      w[4 * j] = hmul2(e2m1x2_to_f16x2<0>(r.w[q][j]), f2);
+      w[4 * j + 1] = hmul2(e2m1x2_to_f16x2<1>(r.w[q][j]), f2);
+      w[4 * j + 2] = hmul2(e2m1x2_to_f16x2<2>(r.w[q][j]), f2);
+      w[4 * j + 3] = hmul2(e2m1x2_to_f16x2<3>(r.w[q][j]), f2);
     }
   }
 }
 
-// --------------------------------------------------------------- loaders --
-template <int FMT>
-struct Loader {
+// Exponent that brings the largest magnitude t to 2^13 .. 2^14.
+__device__ __forceinline__ int shift_of(float t) {
+  return t > 0.f && t < INFINITY ? min(max(exponent(t) - 13, -110), 114) : 0;
+}
+
+// ----------------------------------------------------------------- scout --
+// One warp.  Walks the CTA's tiles, through the page table, ahead of everybody:
+// states the facts of tile t + 4 when it handles K(t), and has the pages of the
+// tile kAhead further brought into L2.  Copies whole bf16 tiles by TMA; for the
+// rest of the operands it only counts along.
+template <int FMT, bool PAIR>
+struct Scout {
   static constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
-  using Pieces = Raw<kQuant ? FMT : CERTKV_STORE_FP8>;
   const TreeArgs& p;
   Misc* m;
   const CUtensorMap *tmK, *tmV;
-  uint32_t kv0;
-  int tid, warp, lane, grp, sub;
-  volatile int* ab;
-  bool ok = true;    // false after a wait gave up; the walk over the tiles goes on (the
-                     // loaders' barriers must stay in step) without further copies
-  int64_t tile = 0;  // tiles of this CTA so far
-  int pages_at = 0, pages_lo = -1, pages_hi = -1;  // table entries of 64 pages from pages_at on
-  uint32_t k_copy = 0, v_copy = 0;  // stages whose last tile came by bulk copy
+  uint32_t ring;
+  int lane;
+  bool ok = true;
+  // the walk: tile k of item it, of `stored` tiles of stored slots
+  Items items;
+  Item it;
+  int k = 0, count = 0, stored = 0;
+  int at = 0, lo = -1, hi = -1;  // table entries of 64 pages from page `at` on
 
-  __device__ __forceinline__ Loader(const TreeArgs& p_, Misc* m_, uint32_t kv, const CUtensorMap* a,
-                                    const CUtensorMap* b, int tid_)
-      : p(p_), m(m_), tmK(a), tmV(b), kv0(kv), tid(tid_) {
-    warp = tid >> 5;
-    lane = tid & 31;
-    grp = tid >> 3;
-    sub = tid & 7;
-    ab = &m->abort;
-  }
-
-  __device__ __forceinline__ int entry(int u, int page) const {
+  __device__ __forceinline__ int entry(int page) const {
     if (page >= p.st.max_pages) return -1;
-    const int e = __ldg(p.st.table + (int64_t)u * p.st.max_pages + page);
+    const int e = __ldg(p.st.table + (int64_t)it.u * p.st.max_pages + page);
     return e >= 0 && e < p.st.pool_pages ? e : -1;
   }
-  // Pages of tile k (-1: none).  Every lane of the warp; k ascends by one after
-  // `start`.
-  __device__ __forceinline__ void pages(int u, int k, bool start, int& a, int& b) {
-    const int page = 2 * k;
-    if (start) {
-      pages_at = page;
-      pages_lo = entry(u, page + lane);
-      pages_hi = entry(u, page + 32 + lane);
-    } else if (page >= pages_at + 32) {
-      pages_at += 32;
-      pages_lo = pages_hi;
-      pages_hi = entry(u, pages_at + 32 + lane);
-    }
-    a = __shfl_sync(kFull, pages_lo, page - pages_at);
-    b = __shfl_sync(kFull, pages_lo, page + 1 - pages_at);
+  __device__ __forceinline__ int page(int i) const {  // at <= i < at + 64
+    const int x = __shfl_sync(kFull, lo, (i - at) & 31), y = __shfl_sync(kFull, hi, (i - at) & 31);
+    return i - at < 32 ? x : y;
   }
-  // Pool slots of this thread's pieces (slots grp + 32 i of the tile; -1: none).
-  __device__ __forceinline__ void pieces(int a, int b, int live, int64_t (&at)[4]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int s = grp + 32 * i, page = i < 2 ? a : b;
-      at[i] = s < live && page >= 0 ? (int64_t)page * kPage + (s & (kPage - 1)) : -1;
+  __device__ __forceinline__ void prefetch_page(int i) const {
+    if (i >= 2 * stored) return;
+    const int pg = page(i);
+    if (pg < 0) return;
+    const int64_t s = (int64_t)pg * kPage;
+    const uint8_t* x = nullptr;
+    uint32_t bytes = kPage * row_bytes(FMT);
+    if (lane == 0) x = p.st.k + s * row_bytes(FMT);
+    if (lane == 1) x = p.st.v + s * row_bytes(FMT);
+    if (FMT == CERTKV_STORE_FP4 && (lane == 2 || lane == 3)) {
+      x = (lane == 2 ? p.st.kg : p.st.vg) + s * kGroups;
+      bytes = kPage * kGroups;
     }
+    if (x)
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(reinterpret_cast<uint64_t>(x)),
+                   "r"(bytes)
+                   : "memory");
   }
-  // Scales of slots 4 lane .. 4 lane + 3 of the tile (0: no slot).
+  // Scales of slots 4 lane .. 4 lane + 3 of a tile (0: no slot).
   __device__ __forceinline__ float4 scales(const float* s, int a, int b, int live) const {
-    const int page = lane < 16 ? a : b, n = live - 4 * lane;
+    const int pg = lane < 16 ? a : b, n = live - 4 * lane;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (page >= 0)
-      x = __ldg(reinterpret_cast<const float4*>(s + (int64_t)page * kPage + ((4 * lane) & (kPage - 1))));
+    if (pg >= 0)
+      x = __ldg(reinterpret_cast<const float4*>(s + (int64_t)pg * kPage + ((4 * lane) & (kPage - 1))));
     if (n < 1) x.x = 0.f;
     if (n < 2) x.y = 0.f;
     if (n < 3) x.z = 0.f;
     if (n < 4) x.w = 0.f;
     return x;
   }
-  __device__ __forceinline__ void wait(const uint64_t* b) {  // a stage's earlier use
-    if (ok && tile >= kStages) ok = tc::mbar_wait(bar(b), (uint32_t)((tile / kStages - 1) & 1), ab);
-  }
-  __device__ __forceinline__ void arrive(const uint64_t* b) const {
-    um::fence_async();
-    __syncwarp();
-    if (lane == 0) tc::mbar_arrive(bar(b));
-  }
-  // One operand of a whole bf16 tile: two pages, two 64-element halves.
-  __device__ __forceinline__ void copy(const CUtensorMap* map, uint32_t to, const uint64_t* full, int a,
-                                       int b) const {
-    if (!ok) return;
-    if (tid == 0) {
-      tc::mbar_expect_tx(bar(full), kOperand);
-      tc::tma_load_2d(to, map, 0, a * kPage, bar(full));
-      tc::tma_load_2d(to + kHalf, map, 64, a * kPage, bar(full));
-      tc::tma_load_2d(to + kHalf / 2, map, 0, b * kPage, bar(full));
-      tc::tma_load_2d(to + kHalf + kHalf / 2, map, 64, b * kPage, bar(full));
+  // State tile t, the next of the walk.
+  __device__ __forceinline__ void state(uint32_t t) {
+    if (k == it.kb) {  // the next item (there is one: t is a tile of this CTA)
+      items.next(p, &it);
+      k = it.ka;
+      count = p.st.count(it.u);
+      stored = (count + kTreeTile - 1) / kTreeTile;
+      at = 2 * k;
+      lo = entry(at + lane);
+      hi = entry(at + 32 + lane);
+      if (kQuant)
+        for (int i = 2; i < 2 * kAhead; ++i) prefetch_page(at + i);
+    } else if (2 * k >= at + 32) {
+      at += 32;
+      lo = hi;
+      hi = entry(at + 32 + lane);
+    }
+    Meta& mt = m->meta[t % kMeta];
+    if (k < stored) {
+      const int live = count - k * kTreeTile, a = page(2 * k), b = page(2 * k + 1);
+      int shift = 0;
+      if (kQuant) {
+        const float4 ks = scales(p.st.ks, a, b, live);
+        float4 vs = scales(p.st.vs, a, b, live);
+        // from the tile's largest row maximum, a NaN left out
+        float x = fmaxf(fmaxf(vs.x, vs.y), fmaxf(vs.z, vs.w));
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, o));
+        shift = shift_of(x * (FMT == CERTKV_STORE_FP8 ? 448.f : 2688.f));
+        const float down = pow2(-shift);
+        *reinterpret_cast<float4*>(&mt.ks[4 * lane]) = ks;
+        *reinterpret_cast<float4*>(&mt.vf[4 * lane]) =
+            make_float4(vs.x * down, vs.y * down, vs.z * down, vs.w * down);
+        prefetch_page(2 * (k + kAhead));
+        prefetch_page(2 * (k + kAhead) + 1);
+      }
+      if (lane < 4) {
+        const int c = min(max(live - 32 * lane, 0), 32);
+        mt.live[lane] = (lane < 2 ? a : b) < 0 || c == 0 ? 0u : 0xffffffffu >> (32 - c);
+      }
+      if (lane == 0) {
+        mt.a = a;
+        mt.b = b;
+        mt.count = live;
+        mt.shift = shift;
+        mt.whole = live >= kTreeTile && a >= 0 && b >= 0;
+        mt.drafts = 0;
+        if (a < 0 || (b < 0 && live > kPage)) p.st.raise();
+      }
     } else if (lane == 0) {
-      tc::mbar_arrive(bar(full));
+      mt.a = mt.b = -1;
+      mt.count = 0;
+      mt.whole = 0;
+      mt.drafts = 1;
+      mt.unit = it.u;
+      mt.first_block = it.blk == 0;
+    }
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(bar(&m->stated[t % kMeta]));
+    ++k;
+  }
+  // The scout's arrival for operand i, tile t: a whole bf16 tile by four bulk
+  // copies, two pages x two 64-element halves.
+  __device__ __forceinline__ bool operand(const CUtensorMap* map, uint32_t i, uint32_t t) {
+    const Place<PAIR> pl(i);
+    if (ok) ok = tc::mbar_wait(bar(&m->empty[pl.slot]), pl.phase ^ 1u, &m->abort);
+    const Meta& mt = m->meta[t % kMeta];
+    const uint32_t full = bar(&m->full[pl.slot]), to = ring + pl.slot * kOperand;
+    const bool copied = !kQuant && ok && mt.whole;
+    if (lane == 0) {
+      if (copied) {
+        const int ya = mt.a * kPage, yb = mt.b * kPage;
+        tc::mbar_expect_tx(full, kOperand);
+        tc::tma_load_2d(to, map, 0, ya, full);
+        tc::tma_load_2d(to + kHalf, map, 64, ya, full);
+        tc::tma_load_2d(to + kHalf / 2, map, 0, yb, full);
+        tc::tma_load_2d(to + kHalf + kHalf / 2, map, 64, yb, full);
+      } else {
+        tc::mbar_arrive(full);
+      }
+    }
+    return copied;
+  }
+  __device__ __forceinline__ void run(uint32_t n) {
+    it.kb = 0;
+    uint32_t stated = 0, copies = 0;  // places whose last operand came by bulk copy
+    for (; stated < min(n, 4u); ++stated) state(stated);
+    for (uint32_t t = 0; t <= n; ++t) {  // K(t), V(t - 1)
+      if (t < n) {
+        const uint32_t bit = 1u << Place<PAIR>(k_seq(t)).slot;
+        copies = operand(tmK, k_seq(t), t) ? copies | bit : copies & ~bit;
+        if (stated < n) state(stated++);
+      }
+      if (t > 0) {
+        const uint32_t bit = 1u << Place<PAIR>(v_seq(t - 1, n)).slot;
+        copies = operand(tmV, v_seq(t - 1, n), t - 1) ? copies | bit : copies & ~bit;
+      }
+    }
+    if (!kQuant && lane == 0) {  // bulk copies land before the CTA may exit
+      volatile int dummy = 0;
+      for (uint32_t i = 2 * n > Plan<PAIR>::kRing ? 2 * n - Plan<PAIR>::kRing : 0; i < 2 * n; ++i) {
+        const Place<PAIR> pl(i);
+        if (copies >> pl.slot & 1u) tc::mbar_wait(bar(&m->full[pl.slot]), pl.phase, &dummy);
+      }
     }
   }
-  // The exponent that brings the largest magnitude t to 2^13 .. 2^14.
-  __device__ __forceinline__ int shift_of(float t) const {
-    return t > 0.f && t < INFINITY ? min(max(exponent(t) - 13, -110), 114) : 0;
-  }
+};
 
-  // The drafts' own tile: bf16 rows, converted for the 8- and 4-bit stores.
-  __device__ __forceinline__ void drafts(int u, bool first_block) {
-    const int st = (int)(tile % kStages);
-    const uint32_t kb = kv0 + (uint32_t)(st * 2 * kOperand), vb = kb + kOperand;
-    wait(&m->k_empty[st]);
-    k_copy &= ~(1u << st);
-    Meta& mt = m->meta[tile % kMeta];
-    const int bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
-    uint32_t v[2][8], top = 0;
+// --------------------------------------------------------------- loaders --
+template <int FMT, bool PAIR>
+struct Loader {
+  static constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
+  static constexpr int kRawFmt = kQuant ? FMT : CERTKV_STORE_FP8;
+  const TreeArgs& p;
+  Misc* m;
+  uint32_t ring;
+  int tid;
+  Piece pc;
+  bool ok = true;  // false after a wait gave up; the walk over the tiles goes on (the
+                   // loaders' barriers must stay in step)
+
+  // NaN and infinities of sixteen bf16 to 0 (in the product they would reach every
+  // row, seen or not; the merge adds them to the rows that see their draft).
+  __device__ __forceinline__ bool finite_only(uint32_t (&v)[8]) const {
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if ((v[j] & 0x7f80u) == 0x7f80u) {
+        v[j] &= 0xffff0000u;
+        odd = true;
+      }
+      if ((v[j] & 0x7f800000u) == 0x7f800000u) {
+        v[j] &= 0xffffu;
+        odd = true;
+      }
+    }
+    return odd;
+  }
+  __device__ __forceinline__ void stated(uint32_t t) {
+    if (ok) ok = tc::mbar_wait(bar(&m->stated[t % kMeta]), (t / kMeta) & 1u, &m->abort);
+  }
+  // Keys of the drafts' own tile and the facts that follow from its rows.
+  __device__ __forceinline__ void draft_keys(uint32_t to, Meta& mt) {
+    const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
+    uint32_t top = 0;
     if (tid == 0) m->odd = 0ull;
     loaders_sync();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t k[8] = {};
-      const int s = grp + 32 * i;
-      if (i < 2) {
-        // values: a NaN or infinity is left out of the product (it would reach
-        // every row, seen or not); the merge adds it to the rows that see its draft
-        bool odd = false;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i & 1][j] = 0u;
-        if (s < p.T) {
-          load32g(p.kn.at(b, l, s, h) + sub * 16, k);
-          load32g(p.vn.at(b, l, s, h) + sub * 16, v[i & 1]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if ((v[i & 1][j] & 0x7f80u) == 0x7f80u) {
-            v[i & 1][j] &= 0xffff0000u;
-            odd = true;
-          }
-          if ((v[i & 1][j] & 0x7f800000u) == 0x7f800000u) {
-            v[i & 1][j] &= 0xffffu;
-            odd = true;
-          }
-        }
-        if (odd) atomicOr(&m->odd, 1ull << s);
-        top = max(top, top16(v[i & 1]));
-        if (kQuant) {
-          uint32_t kt = top16(k);
-#pragma unroll
-          for (int o = 1; o < 8; o <<= 1) kt = max(kt, __shfl_xor_sync(kFull, kt, o));
-          const int e = min(max(exponent(__uint_as_float(kt)), -120), 120);
-          to_f16(k, pow2(-e));
-          if (sub == 0) mt.ks[s] = pow2(e);
-        }
-      } else if (kQuant && sub == 0) {
-        mt.ks[s] = 0.f;
+#pragma unroll 1
+    for (int q = 0; q < kPieces; ++q) {
+      const int s = pc.grp + 32 * q;
+      uint32_t k[8] = {}, v[8] = {};
+      if (s < p.T) {
+        load32g(p.kn.at(b, l, s, h) + pc.sub * 16, k);
+        load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
       }
-      put32(kb, s, sub, k);
+      if (finite_only(v)) atomicOr(&m->odd, 1ull << (s & 63));
+      top = max(top, top16(v));
+      if (kQuant) {
+        const int e = min(max(exponent(__uint_as_float(Piece::row_max(top16(k)))), -120), 120);
+        to_f16(k, pow2(-e));
+        if (pc.sub == 0) mt.ks[s] = pow2(e);
+      }
+      pc.put(to, q, k);
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
-    if (lane == 0) m->red[warp] = __uint_as_float(top);
+    if ((tid & 31) == 0) m->red[tid >> 5] = __uint_as_float(top);
     loaders_sync();
-    int shift = 0;
-    if (kQuant) {
-      float t = 0.f;
-#pragma unroll
-      for (int i = 0; i < kLoadWarps; ++i) t = fmaxf(t, m->red[i]);
-      shift = shift_of(t);
-    }
     if (tid == 0) {
-      mt.shift = shift;
-      mt.whole = 0;
-      mt.drafts = 1;
-      if (first_block) p.odd[u] = m->odd;
-      tc::mbar_arrive(bar(&m->meta_full[tile % kMeta]));
-    }
-    arrive(&m->k_full[st]);
-    wait(&m->v_empty[st]);
-    v_copy &= ~(1u << st);
+      float x = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+      for (int q = 0; q < kLoadWarps; ++q) x = fmaxf(x, m->red[q]);
+      mt.shift = kQuant ? shift_of(x) : 0;
+      if (mt.first_block) p.odd[u] = m->odd;
+    }
+    loaders_sync();
+  }
+  __device__ __forceinline__ void draft_values(uint32_t to, const Meta& mt) {
+    const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
+#pragma unroll 1
+    for (int q = 0; q < kPieces; ++q) {
+      const int s = pc.grp + 32 * q;
+      uint32_t v[8] = {};
+      if (s < p.T) {
+        load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
+        finite_only(v);
+        if (kQuant) to_f16(v, pow2(-mt.shift));
+      }
+      pc.put(to, q, v);
+    }
+  }
+  // One operand of a bf16 tile that is not whole.
+  __device__ __forceinline__ void ragged(uint32_t to, const uint8_t* rows, const Meta& mt) {
+#pragma unroll 1
+    for (int q = 0; q < kPieces; ++q) {
+      const int pg = q < 2 ? mt.a : mt.b;
       uint32_t w[8] = {};
-      if (i < 2) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = v[i & 1][j];
-        if (kQuant) to_f16(w, pow2(-shift));
-      }
-      put32(vb, grp + 32 * i, sub, w);
+      if (pg >= 0 && pc.grp + 32 * q < mt.count)
+        load32g(rows + ((int64_t)pg * kPage + pc.grp + 32 * (q & 1)) * 256 + pc.sub * 32, w);
+      pc.put(to, q, w);
     }
-    arrive(&m->v_full[st]);
   }
-
-  // Tiles [ka, ke) of the stored slots of segment u.
-  __device__ __forceinline__ void stored(int u, int count, int ka, int ke) {
-    Pieces kr, vr;
-    float4 ks4 = {}, vs4 = {};
-    float vs[4] = {};
-    int64_t at[4];
-    int a, b;
-    pages(u, ka, true, a, b);
+  template <bool VALUE>
+  __device__ __forceinline__ void operand(uint32_t i, uint32_t t, Raw<kRawFmt>& raw) {
+    const Place<PAIR> pl(i);
+    if (ok) ok = tc::mbar_wait(bar(&m->empty[pl.slot]), pl.phase ^ 1u, &m->abort);
+    const uint32_t to = ring + pl.slot * kOperand;
+    Meta& mt = m->meta[t % kMeta];
+    bool wrote = true;
+    if (mt.drafts) {
+      if (VALUE) draft_values(to, mt);
+      else draft_keys(to, mt);
+    } else if (kQuant) {
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) {
+        uint32_t w[8];
+        expand<kRawFmt, VALUE>(raw, q, VALUE ? mt.vf[pc.grp + 32 * q] : 0.f, w);
+        pc.put(to, q, w);
+      }
+    } else {
+      wrote = !mt.whole;
+      if (wrote) ragged(to, VALUE ? p.st.v : p.st.k, mt);
+    }
+    if (!VALUE && tid == 0) tc::mbar_arrive(bar(&m->ready[t % kMeta]));
+    if (wrote) um::fence_async();
+    __syncwarp();
+    if ((tid & 31) == 0) tc::mbar_arrive(bar(&m->full[pl.slot]));
+  }
+  // Quantised codes travel through registers: those of the next keys and of the
+  // next values are loaded while the ones before are expanded.
+  __device__ __forceinline__ void run(uint32_t n) {
+    Raw<kRawFmt> kr, vr;
+    stated(0);
     if (kQuant) {
-      const int live = count - ka * kTreeTile;
-      pieces(a, b, live, at);
-      load_raw(kr, at, sub, p.st.k, p.st.kg);
-      ks4 = scales(p.st.ks, a, b, live);
-      load_raw(vr, at, sub, p.st.v, p.st.vg);
-      vs4 = scales(p.st.vs, a, b, live);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) vs[i] = at[i] >= 0 ? __ldg(p.st.vs + at[i]) : 0.f;
+      const Meta& mt = m->meta[0];
+      kr.load(pc, mt.a, mt.b, mt.count, p.st.k, p.st.kg);
+      vr.load(pc, mt.a, mt.b, mt.count, p.st.v, p.st.vg);
     }
-    for (int k = ka; k < ke; ++k, ++tile) {
-      const int live = count - k * kTreeTile;
-      const int st = (int)(tile % kStages), a0 = a, b0 = b;
-      const uint32_t kb = kv0 + (uint32_t)(st * 2 * kOperand), vb = kb + kOperand;
-      const bool whole = live >= kTreeTile && a >= 0 && b >= 0;
-      int shift = 0;
-      if (kQuant) {  // from the tile's largest row maximum, a NaN left out
-        float t = fmaxf(fmaxf(vs4.x, vs4.y), fmaxf(vs4.z, vs4.w));
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) t = fmaxf(t, __shfl_xor_sync(kFull, t, o));
-        shift = shift_of(t * (FMT == CERTKV_STORE_FP8 ? 448.f : 2688.f));
-      }
-      wait(&m->k_empty[st]);
-      if (warp == 0) {
-        Meta& mt = m->meta[tile % kMeta];
-        if (kQuant) *reinterpret_cast<float4*>(&mt.ks[4 * lane]) = ks4;
-        if (lane < 4) {
-          const int n = min(max(live - 32 * lane, 0), 32);
-          mt.live[lane] = (lane < 2 ? a : b) < 0 || n == 0 ? 0u : 0xffffffffu >> (32 - n);
-        }
-        if (lane == 0) {
-          mt.shift = shift;
-          mt.whole = whole;
-          mt.drafts = 0;
-          if (a < 0 || (b < 0 && live > kPage)) p.st.raise();
-        }
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(bar(&m->meta_full[tile % kMeta]));
-      }
-      if (!kQuant && whole) {
-        copy(tmK, kb, &m->k_full[st], a, b);
-        k_copy |= 1u << st;
-      } else {
-        if (!kQuant) pieces(a, b, live, at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t w[8] = {};
-          if (kQuant) expand<kQuant ? FMT : CERTKV_STORE_FP8, false>(kr, i, 0.f, w);
-          else if (at[i] >= 0) load32g(p.st.k + at[i] * 256 + sub * 32, w);
-          put32(kb, grp + 32 * i, sub, w);
-        }
-        k_copy &= ~(1u << st);
-        arrive(&m->k_full[st]);
-      }
-      const int next = count - (k + 1) * kTreeTile;
-      if (k + 1 < ke) {
-        pages(u, k + 1, false, a, b);
-        if (kQuant) {
-          pieces(a, b, next, at);
-          load_raw(kr, at, sub, p.st.k, p.st.kg);
-          ks4 = scales(p.st.ks, a, b, next);
-          vs4 = scales(p.st.vs, a, b, next);
+#pragma unroll 1
+    for (uint32_t t = 0; t <= n; ++t) {  // K(t), V(t - 1)
+      if (t < n) {
+        operand<false>(k_seq(t), t, kr);
+        if (t + 1 < n) {
+          stated(t + 1);
+          if (kQuant) {
+            const Meta& mt = m->meta[(t + 1) % kMeta];
+            kr.load(pc, mt.a, mt.b, mt.count, p.st.k, p.st.kg);
+          }
         }
       }
-      wait(&m->v_empty[st]);
-      if (!kQuant && whole) {
-        copy(tmV, vb, &m->v_full[st], a0, b0);
-        v_copy |= 1u << st;
-      } else {
-        if (!kQuant) pieces(a0, b0, live, at);
-        const float down = pow2(-shift);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t w[8] = {};
-          if (kQuant) expand<kQuant ? FMT : CERTKV_STORE_FP8, true>(vr, i, vs[i] * down, w);
-          else if (at[i] >= 0) load32g(p.st.v + at[i] * 256 + sub * 32, w);
-          put32(vb, grp + 32 * i, sub, w);
+      if (t > 0) {
+        operand<true>(v_seq(t - 1, n), t - 1, vr);
+        if (kQuant && t < n) {
+          const Meta& mt = m->meta[t % kMeta];
+          vr.load(pc, mt.a, mt.b, mt.count, p.st.v, p.st.vg);
         }
-        v_copy &= ~(1u << st);
-        arrive(&m->v_full[st]);
-      }
-      if (kQuant && k + 1 < ke) {
-        load_raw(vr, at, sub, p.st.v, p.st.vg);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) vs[i] = at[i] >= 0 ? __ldg(p.st.vs + at[i]) : 0.f;
-      }
-    }
-  }
-
-  __device__ __forceinline__ void run(int64_t per) {
-    Items items(p, per);
-    Item it;
-    while (items.next(p, &it)) {
-      const int count = p.st.count(it.u);
-      const int nst = (count + kTreeTile - 1) / kTreeTile;  // tiles of stored slots
-      if (it.ka < nst) stored(it.u, count, it.ka, min(it.kb, nst));
-      if (it.kb > nst) {
-        drafts(it.u, it.blk == 0);
-        ++tile;
-      }
-    }
-    if (!kQuant && tid == 0) {  // bulk copies land before the CTA may exit
-      volatile int dummy = 0;
-      for (int s = 0; s < kStages; ++s) {
-        const int64_t t = (tile - 1 - s) / kStages * kStages + s;  // the last tile of stage s
-        const uint32_t phase = (uint32_t)((t / kStages) & 1);
-        if (tile > s && (k_copy >> s & 1)) tc::mbar_wait(bar(&m->k_full[s]), phase, &dummy);
-        if (tile > s && (v_copy >> s & 1)) tc::mbar_wait(bar(&m->v_full[s]), phase, &dummy);
       }
     }
   }
 };
 
 // ------------------------------------------------------------ MMA issuer --
-// Per item, products i = 0 .. N - 1 alternate between the streams: product i
-// belongs to stream i & 1 and, with both streams on every tile (`pair`), to
-// tile i / 2, else to tile i.  Issued in the order S(0), S(1), then O(i),
-// S(i + 2): S(i + 2) overwrites what O(i) has read, which the tensor core's
-// in-order execution makes safe, and its completion tells the softmax that
-// O(i) is done.
-template <int FMT>
-__device__ __forceinline__ void issue(const TreeArgs& p, Misc* m, uint32_t base, uint32_t tmem,
-                                      int64_t per) {
-  constexpr bool kBf16 = FMT == CERTKV_STORE_BF16;
-  volatile int* ab = &m->abort;
-  const bool pair = p.rb > 128;
-  const uint64_t qd = um::desc(base + kQOff, 16), kd = um::desc(base + kKVOff, 16);
-  const uint64_t vd = um::desc(base + kKVOff + kOperand, kHalf);
-  constexpr uint32_t idS = um::idesc(kBf16, false), idO = um::idesc(kBf16, true);
-  int64_t tile0 = 0;             // tiles of this CTA before the item
-  uint32_t uses[2] = {0u, 0u};   // products of each stream so far
-  uint32_t item = 0;
+// Products per tile: S = Q K^T and O += P V.  Streams on tiles of their own:
+// S(0), S(1), then O(i), S(i + 2) with stream i & 1 on tile i; both streams on
+// every tile: S0(0), S1(0), then O0(j), S0(j + 1), O1(j), S1(j + 1).  A stream's
+// next S overwrites the P that its O has read, which the tensor core's in-order
+// execution makes safe, and its completion tells the softmax that O is done.
+template <int FMT, bool PAIR>
+struct Issuer {
+  static constexpr bool kBf16 = FMT == CERTKV_STORE_BF16;
+  Misc* m;
+  uint32_t tmem;
+  uint32_t q_lo, r_lo;  // descriptor address fields of the queries and the ring
+  uint32_t n;           // tiles of the CTA
   bool ok = true;
-  Items items(p, per);
-  Item it;
-  auto stage_phase = [](int64_t t) { return (uint32_t)((t / kStages) & 1); };
-  while (ok && items.next(p, &it)) {
-    ok = tc::mbar_wait(bar(&m->q_full), item & 1, ab);
-    if (!ok) break;
-    um::fence_after();
-    const int n = it.kb - it.ka, N = pair ? 2 * n : n;
-    auto issue_s = [&](int i) {
-      const int s = i & 1;
-      const int64_t t = tile0 + (pair ? i >> 1 : i);
-      const int st = (int)(t % kStages);
-      if ((!pair || s == 0) && !tc::mbar_wait(bar(&m->k_full[st]), stage_phase(t), ab)) return false;
-      um::fence_after();
-      const uint64_t a = qd + (uint64_t)((pair && s ? kOperand : 0) >> 4);
-      const uint64_t b = kd + (uint64_t)((st * 2 * kOperand) >> 4);
-      const uint32_t d = tmem + kColS + 128u * s;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const uint64_t o = (uint64_t)(((ks >> 2) * kHalf + (ks & 3) * 32) >> 4);
-        um::mma_ss(d, a + o, b + o, idS, ks > 0);
-      }
-      um::commit(bar(&m->s_full[s]));
-      if (!pair || s == 1) um::commit(bar(&m->k_empty[st]));
-      return true;
-    };
-    auto issue_o = [&](int i) {
-      const int s = i & 1;
-      const int64_t t = tile0 + (pair ? i >> 1 : i);
-      const int st = (int)(t % kStages);
-      if (!tc::mbar_wait(bar(&m->p_full[s]), uses[s] & 1, ab)) return false;
-      ++uses[s];
-      if ((!pair || s == 0) && !tc::mbar_wait(bar(&m->v_full[st]), stage_phase(t), ab)) return false;
-      um::fence_after();
-      const uint64_t b = vd + (uint64_t)((st * 2 * kOperand) >> 4);
-      const uint32_t d = tmem + kColO + 128u * s, a = tmem + kColS + 128u * s;
-      const bool first = i < 2;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {  // 16 slots each: 8 columns of P
-        const uint32_t pa = a + (uint32_t)((ks >> 1) * 32 + (ks & 1) * 8);
-        const uint64_t bb = b + (uint64_t)((ks * 2048) >> 4);
-        um::mma_ts(d, pa, bb, idO, !first || ks > 0);
-        if (kBf16) um::mma_ts(d, pa + 16, bb, idO, true);  // the remainders
-      }
-      if (!pair || s == 1) um::commit(bar(&m->v_empty[st]));
-      if (i + 2 >= N) um::commit(bar(&m->o_full[s]));
-      return true;
-    };
-    ok = issue_s(0) && (N < 2 || issue_s(1));
-    for (int i = 0; ok && i < N; ++i) ok = issue_o(i) && (i + 2 >= N || issue_s(i + 2));
-    tile0 += n;
-    ++item;
+  uint32_t odd = 0;     // bit st: parity of the O's of stream st so far
+
+  __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
+    if (ok) ok = tc::mbar_wait(bar(b), phase, &m->abort);
   }
-  um::commit(bar(&m->done));  // everything issued above has finished
-  volatile int dummy = 0;
-  tc::mbar_wait(bar(&m->done), 0, &dummy);
-}
+  // S of stream st with the keys of tile t; `last`: the tile's last S
+  __device__ __forceinline__ void s(int st, uint32_t t, bool last) {
+    const Place<PAIR> k(k_seq(t));
+    wait(&m->full[k.slot], k.phase);
+    if (!ok) return;
+    um::fence_after();
+    const uint64_t a = um::desc(0, 16) + q_lo + (PAIR ? (uint32_t)st * (kOperand >> 4) : 0u);
+    const uint64_t b = um::desc(0, 16) + r_lo + k.slot * (kOperand >> 4);
+    const uint32_t d = tmem + kColS + 128u * st;
+#pragma unroll 2
+    for (int ks = 0; ks < 8; ++ks) {
+      const uint32_t o = (uint32_t)(((ks >> 2) * kHalf + (ks & 3) * 32) >> 4);
+      um::mma_ss(d, a + o, b + o, um::idesc(kBf16, false), ks > 0);
+    }
+    um::commit(bar(&m->s_full[st]));
+    if (last) um::commit(bar(&m->empty[k.slot]));
+  }
+  // O += P V of stream st with tile t's values; `first`, `fin`: of the item
+  __device__ __forceinline__ void o(int st, uint32_t t, bool last, bool first, bool fin) {
+    const Place<PAIR> v(v_seq(t, n));
+    wait(&m->p_full[st], odd >> st & 1u);
+    odd ^= 1u << st;
+    wait(&m->full[v.slot], v.phase);
+    if (!ok) return;
+    um::fence_after();
+    const uint64_t b = um::desc(0, kHalf) + r_lo + v.slot * (kOperand >> 4);
+    const uint32_t d = tmem + kColO + 128u * st, a = tmem + kColS + 128u * st;
+#pragma unroll 2
+    for (int ks = 0; ks < 8; ++ks) {  // 16 slots each: 8 columns of P
+      const uint32_t pa = a + (uint32_t)((ks >> 1) * 32 + (ks & 1) * 8);
+      const uint64_t bb = b + (uint32_t)((ks * 2048) >> 4);
+      um::mma_ts(d, pa, bb, um::idesc(kBf16, true), !first || ks > 0);
+      if (kBf16) um::mma_ts(d, pa + 16, bb, um::idesc(kBf16, true), true);  // the remainders
+    }
+    if (last) um::commit(bar(&m->empty[v.slot]));
+    if (fin) um::commit(bar(&m->o_full[st]));
+  }
+
+  __device__ __forceinline__ void run(const TreeArgs& p, int64_t per) {
+    Items items(p, per);
+    Item it;
+    uint32_t t0 = 0, item = 0;  // tiles and items before
+    while (ok && items.next(p, &it)) {
+      wait(&m->q_full, item & 1u);
+      ++item;
+      const int c = it.kb - it.ka;
+      if (PAIR) {
+        s(0, t0, false);
+        s(1, t0, true);
+        for (int j = 0; ok && j < c; ++j) {
+          const bool more = j + 1 < c;
+          o(0, t0 + j, false, j == 0, !more);
+          if (more) s(0, t0 + j + 1, false);
+          o(1, t0 + j, true, j == 0, !more);
+          if (more) s(1, t0 + j + 1, true);
+        }
+      } else {
+        s(0, t0, true);
+        if (c > 1) s(1, t0 + 1, true);
+        for (int i = 0; ok && i < c; ++i) {
+          o(i & 1, t0 + i, true, i < 2, i + 2 >= c);
+          if (i + 2 < c) s(i & 1, t0 + i + 2, true);
+        }
+      }
+      t0 += c;
+    }
+    um::commit(bar(&m->done));  // everything issued above has finished
+    volatile int dummy = 0;
+    tc::mbar_wait(bar(&m->done), 0, &dummy);
+  }
+};
 
 // --------------------------------------------------------------- softmax --
-template <int FMT>
+// The largest logit of a row over a tile (times the keys' scales), from tensor
+// memory; MASK: only of the slots in live.
+template <bool QUANT, bool MASK>
+__device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt, const uint32_t (&live)[4]) {
+  float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+#pragma unroll 1
+  for (int c = 0; c < 2; ++c) {
+    uint32_t r[64];
+    um::ld64(tS + 64u * c, r);
+    const uint32_t w0 = c ? live[2] : live[0], w1 = c ? live[3] : live[1];
+#pragma unroll
+    for (int j = 0; j < 64; j += 4) {
+      float2 x = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+      float2 y = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
+      if (QUANT) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[64 * c + j]);
+        x = fmul2(x, make_float2(k4.x, k4.y));
+        y = fmul2(y, make_float2(k4.z, k4.w));
+      }
+      if (MASK) {
+        const uint32_t w = j < 32 ? w0 : w1;
+        if (!(w >> (j & 31) & 1u)) x.x = -INFINITY;
+        if (!(w >> ((j + 1) & 31) & 1u)) x.y = -INFINITY;
+        if (!(w >> ((j + 2) & 31) & 1u)) y.x = -INFINITY;
+        if (!(w >> ((j + 3) & 31) & 1u)) y.y = -INFINITY;
+      }
+      if (j & 4) {
+        m0 = um::max3(m0, x.x, x.y);
+        m1 = um::max3(m1, y.x, y.y);
+      } else {
+        m2 = um::max3(m2, x.x, x.y);
+        m3 = um::max3(m3, y.x, y.y);
+      }
+    }
+  }
+  return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+}
+
+// Weights 2^(x sl + off) of a row over a tile, written over its logits as the
+// MMAs' A operand (32 columns of S: 16 of weights, for bf16 then 16 of their
+// remainders); returns their sum.
+template <bool QUANT, bool MASK>
+__device__ __forceinline__ float tile_weights(uint32_t tS, const Meta& mt, const uint32_t (&live)[4],
+                                              float sl, float off) {
+  const float2 sl2 = make_float2(sl, sl), off2 = make_float2(off, off);
+  float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    uint32_t r[32];
+    um::ld32(tS + 32u * c, r);
+    const uint32_t w = c < 2 ? (c ? live[1] : live[0]) : (c == 2 ? live[2] : live[3]);
+    uint32_t hi[16], lo[16];
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      float2 x = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+      float2 y = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
+      if (QUANT) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[32 * c + j]);
+        x = fmul2(x, make_float2(k4.x, k4.y));
+        y = fmul2(y, make_float2(k4.z, k4.w));
+      }
+      x = ffma2(x, sl2, off2);
+      y = ffma2(y, sl2, off2);
+      if (MASK) {
+        if (!(w >> j & 1u)) x.x = -INFINITY;
+        if (!(w >> (j + 1) & 1u)) x.y = -INFINITY;
+        if (!(w >> (j + 2) & 1u)) y.x = -INFINITY;
+        if (!(w >> (j + 3) & 1u)) y.y = -INFINITY;
+      }
+      x.x = um::ex2(x.x);
+      x.y = um::ex2(x.y);
+      y.x = um::ex2(y.x);
+      y.y = um::ex2(y.y);
+      sum0 = fadd2(sum0, x);
+      sum1 = fadd2(sum1, y);
+      if (QUANT) {
+        hi[j / 2] = pack_f16(x.x, x.y);
+        hi[j / 2 + 1] = pack_f16(y.x, y.y);
+      } else {
+        hi[j / 2] = pack_bf16(x.x, x.y);
+        hi[j / 2 + 1] = pack_bf16(y.x, y.y);
+        lo[j / 2] = pack_bf16(x.x - bf16lo(hi[j / 2]), x.y - bf16hi(hi[j / 2]));
+        lo[j / 2 + 1] = pack_bf16(y.x - bf16lo(hi[j / 2 + 1]), y.y - bf16hi(hi[j / 2 + 1]));
+      }
+    }
+    um::st16(tS + 32u * c, hi);
+    if (!QUANT) um::st16(tS + 32u * c + 16u, lo);
+  }
+  return (sum0.x + sum0.y) + (sum1.x + sum1.y);
+}
+
+template <int FMT, bool PAIR>
 __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t base, uint32_t tmem,
                                         int tid, int64_t per) {
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
   volatile int* ab = &m->abort;
-  const bool pair = p.rb > 128;
   const int warp = tid >> 5, lane = tid & 31, s = warp >> 2, quad = warp & 3;
   const int lrow = quad * 32 + lane;  // row of the stream, lane of tensor memory
+  const int brow = PAIR ? 128 * s + lrow : lrow;  // row of the block
+  const bool busy = (PAIR ? 128 * s : 0) + quad * 32 < p.rb;  // some block has a row here
   const uint32_t tS = tmem + kColS + 128u * s + ((uint32_t)(quad * 32) << 16);
   const uint32_t tO = tmem + kColO + 128u * s + ((uint32_t)(quad * 32) << 16);
-  int64_t tile0 = 0;
-  uint32_t uses = 0, finals = 0;  // S and final O of this stream so far
-  bool ok = true;                 // false after a wait gave up, for good
+  uint32_t t0 = 0, uses = 0, finals = 0;  // tiles before; S and final O of this stream so far
+  bool ok = true;                         // false after a wait gave up, for good
   Items items(p, per);
   Item it;
   while (items.next(p, &it)) {
     const int rows = min(p.rb, p.rows - it.blk * p.rb);  // of the block
     const int bl = it.u / p.H, h = it.u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
     // ---- queries into shared memory: 16 lanes a row
-    const int qrows = pair ? 256 : 128;
-    for (int r = tid >> 4; r < qrows; r += 16) {
+#pragma unroll 1
+    for (int r = tid >> 4; r < (PAIR ? 256 : 128); r += 16) {
       uint4 x = make_uint4(0u, 0u, 0u, 0u);
       const int c = tid & 15;
       if (r < rows) {
@@ -627,236 +807,165 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
         x = make_uint4(w[0], w[1], w[2], w[3]);
         if (c == 0) m->qs[r] = pow2(e);
       }
-      const uint32_t at = base + kQOff + (uint32_t)((r >> 7) * kOperand + (c >> 3) * kHalf +
-                                                    (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4));
+      const uint32_t at = base + (uint32_t)((r >> 7) * kOperand + (c >> 3) * kHalf + (r & 127) * 128 +
+                                            (((c & 7) ^ (r & 7)) << 4));
       sts128(at, x.x, x.y, x.z, x.w);
     }
     um::fence_async();
     softmax_sync();  // also: qs of every row is there
-
-    const int brow = pair ? 128 * s + lrow : lrow;  // row of the block
-    const bool mine = brow < rows;
-    const bool busy = (pair ? 128 * s + quad * 32 : quad * 32) < rows;  // warp has a row
-    const int row = it.blk * p.rb + min(brow, rows - 1), tok = row / p.G;
-    const uint64_t word = p.kn.p ? seen(p, b, tok) : 0ull;
     const float sl = fmaxf(kQuant ? m->qs[brow] * p.scale_log2 : p.scale_log2, 1.1754944e-38f);
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(bar(&m->q_full));  // rows written, qs read by the warp
-    const int n = it.kb - it.ka;
+
+    const int n = it.kb - it.ka, steps = PAIR ? n : (n - s + 1) / 2;
+    const int tok = (it.blk * p.rb + min(brow, rows - 1)) / p.G;
+    const uint64_t word = p.kn.p ? seen(p, b, tok) : 0ull;
     // C: reference of the weights (log2 domain, less 6 bits of head room for f16);
     // lsum: their sum; shift0: exponent the accumulator is relative to
     float C = -INFINITY, lsum = 0.f;
     int shift0 = 0;
-    const int steps = pair ? n : (n - s + 1) / 2;
-    for (int i = 0; i < steps; ++i) {
-      const int64_t t = tile0 + (pair ? i : 2 * i + s);
-      ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[s]), uses & 1, ab));
+    for (int i = 0; busy && i < steps; ++i) {
+      const uint32_t t = t0 + (uint32_t)(PAIR ? i : 2 * i + s);
+      ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[s]), uses & 1u, ab)) &&
+           __all_sync(kFull, tc::mbar_wait(bar(&m->ready[t % kMeta]), (t / kMeta) & 1u, ab));
       ++uses;
       if (!ok) break;
-      if (busy) {
-        um::fence_after();
-        ok = __all_sync(kFull, tc::mbar_wait(bar(&m->meta_full[t % kMeta]), (uint32_t)((t / kMeta) & 1), ab));
-        if (!ok) break;
-        const Meta& mt = m->meta[t % kMeta];
-        const bool whole = mt.whole;
-        uint32_t live[4];
-        if (!whole) {
-          if (mt.drafts) {
-            live[0] = (uint32_t)word;
-            live[1] = (uint32_t)(word >> 32);
-            live[2] = live[3] = 0u;
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) live[j] = mt.live[j];
-          }
-        }
-        if (i == 0) shift0 = mt.shift;
-        const float dE = kQuant ? (float)(mt.shift - shift0) : 0.f;
-        // the row's maximum
-        float mx = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32];
-          um::ld32(tS + 32u * c, r);
-          if (kQuant) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[32 * c + j]);
-              const float2 x0 = fmul2(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])),
-                                      make_float2(k4.x, k4.y));
-              const float2 x1 = fmul2(make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])),
-                                      make_float2(k4.z, k4.w));
-              r[j] = __float_as_uint(x0.x);
-              r[j + 1] = __float_as_uint(x0.y);
-              r[j + 2] = __float_as_uint(x1.x);
-              r[j + 3] = __float_as_uint(x1.y);
-            }
-          }
-          if (!whole) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!(live[c] >> j & 1u)) r[j] = 0xff800000u;
-          }
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) mx = um::max3(mx, __uint_as_float(r[j]), __uint_as_float(r[j + 1]));
-        }
-        mx = fmaf(mx, sl, dE - (kQuant ? 6.f : 0.f));  // sl > 0; -inf stays
-        const bool grow = mx > C + kLazy || C == -INFINITY;
-        float f = 1.f;
-        if (grow) {
-          const float nc = fmaxf(mx, C);
-          f = C == -INFINITY ? 1.f : um::ex2(C - nc);
-          C = nc;
-        }
-        if (i > 0 && __any_sync(kFull, f != 1.f)) {  // O of the tiles before is done (see issue)
-          lsum *= f;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t r[32];
-            um::ld32(tO + 32u * c, r);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * f);
-            um::st32(tO + 32u * c, r);
-          }
-        }
-        // weights
-        const float cc = C == -INFINITY ? 0.f : C;
-        const float2 sl2 = make_float2(sl, sl), off2 = make_float2(dE - cc, dE - cc);
-        float2 sum2 = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32];
-          um::ld32(tS + 32u * c, r);
-          uint32_t hi[16], lo[16];
-#pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            float2 x0 = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
-            float2 x1 = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-            if (kQuant) {
-              const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[32 * c + j]);
-              x0 = fmul2(x0, make_float2(k4.x, k4.y));
-              x1 = fmul2(x1, make_float2(k4.z, k4.w));
-            }
-            x0 = ffma2(x0, sl2, off2);
-            x1 = ffma2(x1, sl2, off2);
-            if (!whole) {
-              if (!(live[c] >> j & 1u)) x0.x = -INFINITY;
-              if (!(live[c] >> (j + 1) & 1u)) x0.y = -INFINITY;
-              if (!(live[c] >> (j + 2) & 1u)) x1.x = -INFINITY;
-              if (!(live[c] >> (j + 3) & 1u)) x1.y = -INFINITY;
-            }
-            x0.x = um::ex2(x0.x);
-            x0.y = um::ex2(x0.y);
-            x1.x = um::ex2(x1.x);
-            x1.y = um::ex2(x1.y);
-            sum2 = fadd2(sum2, fadd2(x0, x1));
-            if (kQuant) {
-              hi[j / 2] = pack_f16(x0.x, x0.y);
-              hi[j / 2 + 1] = pack_f16(x1.x, x1.y);
-            } else {
-              hi[j / 2] = pack_bf16(x0.x, x0.y);
-              hi[j / 2 + 1] = pack_bf16(x1.x, x1.y);
-              lo[j / 2] = pack_bf16(x0.x - bf16lo(hi[j / 2]), x0.y - bf16hi(hi[j / 2]));
-              lo[j / 2 + 1] = pack_bf16(x1.x - bf16lo(hi[j / 2 + 1]), x1.y - bf16hi(hi[j / 2 + 1]));
-            }
-          }
-          um::st16(tS + 32u * c, hi);
-          if (!kQuant) um::st16(tS + 32u * c + 16u, lo);
-        }
-        lsum = fmaf(sum2.x + sum2.y, kQuant ? um::ex2(-dE) : 1.f, lsum);
-        um::wait_st();
-        um::fence_before();
-      }
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bar(&m->p_full[s]));
-    }
-    // ---- the item's result: one record per row
-    if (ok && steps > 0) {
-      ok = __all_sync(kFull, tc::mbar_wait(bar(&m->o_full[s]), finals & 1, ab));
-      ++finals;
-    }
-    um::fence_after();
-    const int64_t rec = (int64_t)blockIdx.x + (int64_t)it.u * p.nblk + it.blk;
-    // stream s: sum 2^C lsum, accumulator relative to 2^(C + shift0)
-    float f0 = 1.f, f1 = 0.f, Cj = C, lj = lsum;
-    const bool both = !pair && n > 1;  // join the streams: stream 0 writes
-    if (!pair) {
-      if (s == 1 && busy) {
-        m->cm[lrow] = C;
-        m->l[lrow] = lsum;
-        m->sh[lrow] = (float)shift0;
-      }
-      um::fence_before();
-      softmax_sync();
       um::fence_after();
-    }
-    if (pair || s == 0) {
-      if (busy) {
-        if (both) {
-          const float C1 = m->cm[lrow], l1 = m->l[lrow];
-          Cj = fmaxf(C, C1);
-          f0 = C == -INFINITY ? 0.f : exp2f(C - Cj);
-          f1 = C1 == -INFINITY ? 0.f : exp2f(C1 - Cj);
-          lj = lsum * f0 + l1 * f1;
-          f1 *= kQuant ? exp2f(m->sh[lrow] - (float)shift0) : 1.f;
-        }
-        const float inv = lj != 0.f ? 1.f / lj : 0.f, up = kQuant ? exp2f((float)shift0) : 1.f;
-        const float g0 = f0 == 0.f ? 0.f : f0 * inv * up, g1 = f1 == 0.f ? 0.f : f1 * inv * up;
-        float* acc = p.rec_acc + (rec * p.rb + brow) * kD;
+      const Meta& mt = m->meta[t % kMeta];
+      const bool whole = mt.whole;
+      uint32_t live[4] = {~0u, ~0u, ~0u, ~0u};
+      if (!whole) {
+        const bool own = mt.drafts;
+        live[0] = own ? (uint32_t)word : mt.live[0];
+        live[1] = own ? (uint32_t)(word >> 32) : mt.live[1];
+        live[2] = own ? 0u : mt.live[2];
+        live[3] = own ? 0u : mt.live[3];
+      }
+      if (i == 0) shift0 = mt.shift;
+      const float dE = kQuant ? (float)(mt.shift - shift0) : 0.f;
+      float mx = whole ? tile_max<kQuant, false>(tS, mt, live) : tile_max<kQuant, true>(tS, mt, live);
+      mx = fmaf(mx, sl, dE - (kQuant ? 6.f : 0.f));  // sl > 0; -inf stays
+      float f = 1.f;
+      if (mx > C + kLazy || C == -INFINITY) {
+        const float nc = fmaxf(mx, C);
+        f = C == -INFINITY ? 1.f : um::ex2(C - nc);
+        C = nc;
+      }
+      if (i > 0 && __any_sync(kFull, f != 1.f)) {  // O of the tiles before is done (see Issuer)
+        lsum *= f;
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t r[32];
           um::ld32(tO + 32u * c, r);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) r[j] = g0 == 0.f ? 0u : __float_as_uint(__uint_as_float(r[j]) * g0);
-          if (both) {
-            uint32_t r1[32];
-            um::ld32(tO + 128u + 32u * c, r1);
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (g1 != 0.f) r[j] = __float_as_uint(fmaf(__uint_as_float(r1[j]), g1, __uint_as_float(r[j])));
-          }
-          if (mine) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<float4*>(acc + 32 * c + j) =
-                  ok ? make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]),
-                                   __uint_as_float(r[j + 3]))
-                     : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
+          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * f);
+          um::st32(tO + 32u * c, r);
         }
-        if (mine) p.rec_ml[rec * p.rb + brow] = ok ? make_float2(Cj, lj) : make_float2(0.f, __int_as_float(0x7fc00000));
       }
+      const float off = dE - (C == -INFINITY ? 0.f : C);
+      const float sum = whole ? tile_weights<kQuant, false>(tS, mt, live, sl, off)
+                              : tile_weights<kQuant, true>(tS, mt, live, sl, off);
+      lsum = fmaf(sum, kQuant ? um::ex2(-dE) : 1.f, lsum);
+      um::wait_st();
+      um::fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar(&m->p_full[s]));
+    }
+    // ---- the item's result: one record per row
+    if (ok && busy && steps > 0) {
+      ok = __all_sync(kFull, tc::mbar_wait(bar(&m->o_full[s]), finals & 1u, ab));
+      ++finals;
+    }
+    um::fence_after();
+    const bool both = !PAIR && n > 1;  // join the streams: stream 0 writes
+    if (!PAIR && s == 1 && busy) {
+      m->cm[lrow] = C;
+      m->l[lrow] = lsum;
+      m->sh[lrow] = (float)shift0;
     }
     um::fence_before();
-    tile0 += n;
+    softmax_sync();  // from here on nothing reads the queries any more either
+    um::fence_after();
+    if (busy && (PAIR || s == 0)) {
+      // stream s: sum 2^C lsum, accumulator relative to 2^(C + shift0)
+      float f0 = 1.f, f1 = 0.f, Cj = C, lj = lsum;
+      if (both) {
+        const float C1 = m->cm[lrow], l1 = m->l[lrow];
+        Cj = fmaxf(C, C1);
+        f0 = C == -INFINITY ? 0.f : exp2f(C - Cj);
+        f1 = C1 == -INFINITY ? 0.f : exp2f(C1 - Cj);
+        lj = lsum * f0 + l1 * f1;
+        f1 *= kQuant ? exp2f(m->sh[lrow] - (float)shift0) : 1.f;
+      }
+      const float inv = lj != 0.f ? 1.f / lj : 0.f, up = kQuant ? exp2f((float)shift0) : 1.f;
+      const float g0 = f0 == 0.f ? 0.f : f0 * inv * up, g1 = f1 == 0.f ? 0.f : f1 * inv * up;
+      const int64_t rec = ((int64_t)blockIdx.x + (int64_t)it.u * p.nblk + it.blk) * p.rb + brow;
+      const bool mine = brow < rows;
+#pragma unroll 1
+      for (int c = 0; c < 8; ++c) {
+        uint32_t r[16];
+        um::ld16(tO + 16u * c, r);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[j] = g0 == 0.f ? 0u : __float_as_uint(__uint_as_float(r[j]) * g0);
+        if (both) {
+          uint32_t r1[16];
+          um::ld16(tO + 128u + 16u * c, r1);
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (g1 != 0.f) r[j] = __float_as_uint(fmaf(__uint_as_float(r1[j]), g1, __uint_as_float(r[j])));
+        }
+        if (mine) {
+#pragma unroll
+          for (int j = 0; j < 16; j += 4)
+            *reinterpret_cast<uint4*>(p.rec_acc + rec * kD + 16 * c + j) =
+                make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+        }
+      }
+      if (mine) p.rec_ml[rec] = ok ? make_float2(Cj, lj) : make_float2(0.f, __int_as_float(0x7fc00000));
+    }
+    um::fence_before();
+    t0 += n;
   }
 }
 
-// grid = p.ctas (one CTA per SM), block = kThreads.
-template <int FMT>
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// grid = p.ctas (one CTA per SM), block = kThreads; PAIR: blocks of more than
+// 128 rows.
+template <int FMT, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap tmK,
                                                               const __grid_constant__ CUtensorMap tmV,
                                                               const __grid_constant__ TreeArgs p) {
   extern __shared__ char smem_raw[];
   char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  Misc* m = reinterpret_cast<Misc*>(sm + kMiscOff);
+  Misc* m = reinterpret_cast<Misc*>(sm + Plan<PAIR>::kMiscOff);
   const int64_t per = tiles_per_cta(p);
-  if (per * blockIdx.x >= p.first[p.units] * p.nblk) return;  // uniform, before any barrier
+  const int64_t left = p.first[p.units] * p.nblk - per * blockIdx.x;
+  if (left <= 0) return;  // uniform, before any barrier
+  const uint32_t n = (uint32_t)min(left, per);  // tiles of this CTA
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      tc::mbar_init(bar(&m->k_full[i]), kLoadWarps);
-      tc::mbar_init(bar(&m->k_empty[i]), 1);
-      tc::mbar_init(bar(&m->v_full[i]), kLoadWarps);
-      tc::mbar_init(bar(&m->v_empty[i]), 1);
+    for (int i = 0; i < Plan<PAIR>::kRing; ++i) {
+      tc::mbar_init(bar(&m->full[i]), kLoadWarps + 1);  // and the scout
+      tc::mbar_init(bar(&m->empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
+      const int rows = PAIR ? (i ? p.rb - 128 : 128) : p.rb;
       tc::mbar_init(bar(&m->s_full[i]), 1);
-      tc::mbar_init(bar(&m->p_full[i]), 4);
+      tc::mbar_init(bar(&m->p_full[i]), (rows + 31) / 32);  // the warps with rows
       tc::mbar_init(bar(&m->o_full[i]), 1);
     }
-    for (int i = 0; i < kMeta; ++i) tc::mbar_init(bar(&m->meta_full[i]), 1);
+    for (uint32_t i = 0; i < kMeta; ++i) {
+      tc::mbar_init(bar(&m->stated[i]), 1);
+      tc::mbar_init(bar(&m->ready[i]), 1);
+    }
     tc::mbar_init(bar(&m->q_full), kSoftWarps);
     tc::mbar_init(bar(&m->done), 1);
     m->abort = 0;
@@ -869,14 +978,24 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&m->tmem);
   const uint32_t base = tc::saddr(sm);
   if (warp < kSoftWarps) {
-    softmax<FMT>(p, m, base, tmem, threadIdx.x, per);
+    regs_up<kSoftRegs>();
+    softmax<FMT, PAIR>(p, m, base, tmem, threadIdx.x, per);
   } else if (warp < kSoftWarps + kLoadWarps) {
-    Loader<FMT> ld(p, m, base + kKVOff, &tmK, &tmV, threadIdx.x - kSoftWarps * 32);
-    ld.run(per);
-  } else if ((threadIdx.x & 31) == 0) {
-    issue<FMT>(p, m, base, tmem, per);
+    regs_down<kLoadRegs>();
+    const int tid = (int)threadIdx.x - kSoftWarps * 32;
+    Loader<FMT, PAIR> ld{p, m, base + Plan<PAIR>::kRingOff, tid, Piece(tid)};
+    ld.run(n);
+  } else {
+    regs_down<kIssueRegs>();
+    if (threadIdx.x == (kSoftWarps + kLoadWarps) * 32) {
+      Issuer<FMT, PAIR> is{m, tmem, base >> 4, (base + Plan<PAIR>::kRingOff) >> 4, n};
+      is.run(p, per);
+    } else if (warp == kSoftWarps + kLoadWarps + 1) {
+      Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
+      sc.run(n);
+    }
+    __syncwarp();
   }
-  __syncwarp();
   um::fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && m->abort && p.st.status) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
@@ -888,6 +1007,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 
 constexpr int kMaxDevices = 64;
 
+template <int FMT, bool PAIR>
+bool opt_in() {
+  return cudaFuncSetAttribute(tree_tc_kernel<FMT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              smem_bytes<PAIR>()) == cudaSuccess;
+}
+
 // CTAs: one per SM.  Set up once per device: the shared-memory opt-in.
 int ctas_of_device() {
   static int cached[kMaxDevices] = {};
@@ -896,15 +1021,20 @@ int ctas_of_device() {
   if (dev < kMaxDevices && cached[dev] > 0) return cached[dev];
   int sms = 0;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1 ||
-      cudaFuncSetAttribute(tree_tc_kernel<CERTKV_STORE_BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           kSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(tree_tc_kernel<CERTKV_STORE_FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           kSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(tree_tc_kernel<CERTKV_STORE_FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           kSmemBytes) != cudaSuccess)
+      !opt_in<CERTKV_STORE_BF16, true>() || !opt_in<CERTKV_STORE_BF16, false>() ||
+      !opt_in<CERTKV_STORE_FP8, true>() || !opt_in<CERTKV_STORE_FP8, false>() ||
+      !opt_in<CERTKV_STORE_FP4, true>() || !opt_in<CERTKV_STORE_FP4, false>())
     return 0;
   if (dev < kMaxDevices) cached[dev] = sms;
   return sms;
+}
+
+template <int FMT>
+void launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& p, cudaStream_t st) {
+  if (p.rb > 128)
+    tree_tc_kernel<FMT, true><<<p.ctas, kThreads, smem_bytes<true>(), st>>>(mk, mv, p);
+  else
+    tree_tc_kernel<FMT, false><<<p.ctas, kThreads, smem_bytes<false>(), st>>>(mk, mv, p);
 }
 
 }  // namespace
@@ -918,12 +1048,9 @@ bool launch_tree_tc(const TreeArgs& p, int format, cudaStream_t st) {
     if (!make_row_map(&mk, p.st.k, rows, kPage) || !make_row_map(&mv, p.st.v, rows, kPage)) return false;
   }
   TraceScope ts_("tree_split", st);
-  if (format == CERTKV_STORE_BF16)
-    tree_tc_kernel<CERTKV_STORE_BF16><<<p.ctas, kThreads, kSmemBytes, st>>>(mk, mv, p);
-  else if (format == CERTKV_STORE_FP8)
-    tree_tc_kernel<CERTKV_STORE_FP8><<<p.ctas, kThreads, kSmemBytes, st>>>(mk, mv, p);
-  else
-    tree_tc_kernel<CERTKV_STORE_FP4><<<p.ctas, kThreads, kSmemBytes, st>>>(mk, mv, p);
+  if (format == CERTKV_STORE_BF16) launch<CERTKV_STORE_BF16>(mk, mv, p, st);
+  else if (format == CERTKV_STORE_FP8) launch<CERTKV_STORE_FP8>(mk, mv, p, st);
+  else launch<CERTKV_STORE_FP4>(mk, mv, p, st);
   return true;
 }
 
