@@ -14,11 +14,11 @@
 //
 // Roles per CTA (one per SM, persistent over a share of all tiles):
 //   warps 0..7   softmax: warp (stream, lane quadrant), a thread owns a row;
-//   warps 8..23  loaders: 8- and 4-bit tiles through registers, expanded to f16
+//   warps 8..15  loaders: 8- and 4-bit tiles through registers, expanded to f16
 //                in the MMAs' swizzled layout; for every store the drafts' own
 //                tile and bf16 tiles that are not whole;
-//   warp 24      tensor-memory allocation, and the thread that issues the MMAs;
-//   warp 25      scout: walks the page table ahead of the loaders, states each
+//   warp 16      tensor-memory allocation, and issues the MMAs;
+//   warp 17      scout: walks the page table ahead of the loaders, states each
 //                tile's facts, copies whole bf16 tiles by TMA and has the pages
 //                of later tiles brought into L2.
 //
@@ -594,13 +594,17 @@ struct Issuer {
   static constexpr bool kBf16 = FMT == CERTKV_STORE_BF16;
   Misc* m;
   uint32_t tmem;
-  uint32_t q_lo, r_lo;  // descriptor address fields of the queries and the ring
-  uint32_t n;           // tiles of the CTA
+  uint32_t q, ring;  // shared-memory addresses of the queries and the ring
+  uint32_t n;        // tiles of the CTA
   bool ok = true;
-  uint32_t odd = 0;     // bit st: parity of the O's of stream st so far
+  uint32_t odd = 0;  // bit st: parity of the O's of stream st so far
 
+  // The warp runs as one: the values below are the same in every lane, and are made
+  // so for the compiler too, which then keeps the MMAs' operands in uniform
+  // registers instead of moving them there for every MMA.
+  static __device__ __forceinline__ uint32_t uni(uint32_t x) { return __shfl_sync(kFull, x, 0); }
   __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
-    if (ok) ok = tc::mbar_wait(bar(b), phase, &m->abort);
+    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(b), phase, &m->abort));
   }
   // S of stream st with the keys of tile t; `last`: the tile's last S
   __device__ __forceinline__ void s(int st, uint32_t t, bool last) {
@@ -608,16 +612,11 @@ struct Issuer {
     wait(&m->full[k.slot], k.phase);
     if (!ok) return;
     um::fence_after();
-    const uint64_t a = um::desc(0, 16) + q_lo + (PAIR ? (uint32_t)st * (kOperand >> 4) : 0u);
-    const uint64_t b = um::desc(0, 16) + r_lo + k.slot * (kOperand >> 4);
-    const uint32_t d = tmem + kColS + 128u * st;
-#pragma unroll 2
-    for (int ks = 0; ks < 8; ++ks) {
-      const uint32_t o = (uint32_t)(((ks >> 2) * kHalf + (ks & 3) * 32) >> 4);
-      um::mma_ss(d, a + o, b + o, um::idesc(kBf16, false), ks > 0);
-    }
-    um::commit(bar(&m->s_full[st]));
-    if (last) um::commit(bar(&m->empty[k.slot]));
+    const uint32_t slot = uni(k.slot);
+    um::mma_s(uni(tmem + kColS + 128u * st), uni(um::desc_lo(q, 16) + (PAIR ? (uint32_t)st * (kOperand >> 4) : 0u)),
+              uni(um::desc_lo(ring, 16) + slot * (kOperand >> 4)), um::kDescHi, um::idesc(kBf16, false));
+    um::commit(uni(bar(&m->s_full[st])));
+    if (last) um::commit(uni(bar(&m->empty[slot])));
   }
   // O += P V of stream st with tile t's values; `first`, `fin`: of the item
   __device__ __forceinline__ void o(int st, uint32_t t, bool last, bool first, bool fin) {
@@ -627,17 +626,12 @@ struct Issuer {
     wait(&m->full[v.slot], v.phase);
     if (!ok) return;
     um::fence_after();
-    const uint64_t b = um::desc(0, kHalf) + r_lo + v.slot * (kOperand >> 4);
-    const uint32_t d = tmem + kColO + 128u * st, a = tmem + kColS + 128u * st;
-#pragma unroll 2
-    for (int ks = 0; ks < 8; ++ks) {  // 16 slots each: 8 columns of P
-      const uint32_t pa = a + (uint32_t)((ks >> 1) * 32 + (ks & 1) * 8);
-      const uint64_t bb = b + (uint32_t)((ks * 2048) >> 4);
-      um::mma_ts(d, pa, bb, um::idesc(kBf16, true), !first || ks > 0);
-      if (kBf16) um::mma_ts(d, pa + 16, bb, um::idesc(kBf16, true), true);  // the remainders
-    }
-    if (last) um::commit(bar(&m->empty[v.slot]));
-    if (fin) um::commit(bar(&m->o_full[st]));
+    const uint32_t slot = uni(v.slot), d = uni(tmem + kColO + 128u * st), a = uni(tmem + kColS + 128u * st);
+    const uint32_t b = uni(um::desc_lo(ring, kHalf) + slot * (kOperand >> 4)), acc = uni(!first);
+    if (kBf16) um::mma_o2(d, a, b, um::kDescHi, um::idesc(true, true), acc);  // weights and remainders
+    else um::mma_o(d, a, b, um::kDescHi, um::idesc(false, true), acc);
+    if (last) um::commit(uni(bar(&m->empty[slot])));
+    if (fin) um::commit(uni(bar(&m->o_full[st])));
   }
 
   __device__ __forceinline__ void run(const TreeArgs& p, int64_t per) {
@@ -671,6 +665,7 @@ struct Issuer {
     um::commit(bar(&m->done));  // everything issued above has finished
     volatile int dummy = 0;
     tc::mbar_wait(bar(&m->done), 0, &dummy);
+    __syncwarp();
   }
 };
 
@@ -784,32 +779,41 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
   while (items.next(p, &it)) {
     const int rows = min(p.rb, p.rows - it.blk * p.rb);  // of the block
     const int bl = it.u / p.H, h = it.u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
-    // ---- queries into shared memory: 16 lanes a row
+    // ---- queries into shared memory: 16 lanes a row, eight rows in flight a thread
 #pragma unroll 1
-    for (int r = tid >> 4; r < (PAIR ? 256 : 128); r += 16) {
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    for (int r0 = tid >> 4; r0 < (PAIR ? 256 : 128); r0 += 128) {
+      uint4 x[8];
       const int c = tid & 15;
-      if (r < rows) {
-        const int row = it.blk * p.rb + r, t = row / p.G, g = row - t * p.G;
-        x = __ldg(reinterpret_cast<const uint4*>(p.q.at(b, l, t, h * p.G + g)) + c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows) {
+          const int row = it.blk * p.rb + r, t = row / p.G, g = row - t * p.G;
+          x[i] = __ldg(reinterpret_cast<const uint4*>(p.q.at(b, l, t, h * p.G + g)) + c);
+        }
       }
-      if (kQuant) {
-        uint32_t w[4] = {x.x, x.y, x.z, x.w}, top = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, max((w[j] & 0x7fffu) << 16, w[j] & 0x7fff0000u));
+      for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        if (kQuant) {
+          uint32_t top = 0;
 #pragma unroll
-        for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
-        const int e = min(max(exponent(__uint_as_float(top)), -120), 120);
-        const float f = pow2(-e);
+          for (int j = 0; j < 4; ++j) top = max(top, max((w[j] & 0x7fffu) << 16, w[j] & 0x7fff0000u));
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = pack_f16(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
-        x = make_uint4(w[0], w[1], w[2], w[3]);
-        if (c == 0) m->qs[r] = pow2(e);
+          for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
+          const int e = min(max(exponent(__uint_as_float(top)), -120), 120);
+          const float f = pow2(-e);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = pack_f16(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
+          if (c == 0) m->qs[r] = pow2(e);
+        }
+        sts128(base + (uint32_t)((r >> 7) * kOperand + (c >> 3) * kHalf + (r & 127) * 128 +
+                                 (((c & 7) ^ (r & 7)) << 4)),
+               w[0], w[1], w[2], w[3]);
       }
-      const uint32_t at = base + (uint32_t)((r >> 7) * kOperand + (c >> 3) * kHalf + (r & 127) * 128 +
-                                            (((c & 7) ^ (r & 7)) << 4));
-      sts128(at, x.x, x.y, x.z, x.w);
     }
     um::fence_async();
     softmax_sync();  // also: qs of every row is there
@@ -987,8 +991,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     ld.run(n);
   } else {
     regs_down<kIssueRegs>();
-    if (threadIdx.x == (kSoftWarps + kLoadWarps) * 32) {
-      Issuer<FMT, PAIR> is{m, tmem, base >> 4, (base + Plan<PAIR>::kRingOff) >> 4, n};
+    if (warp == kSoftWarps + kLoadWarps) {
+      Issuer<FMT, PAIR> is{m, tmem, base, base + Plan<PAIR>::kRingOff, n};
       is.run(p, per);
     } else if (warp == kSoftWarps + kLoadWarps + 1) {
       Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};

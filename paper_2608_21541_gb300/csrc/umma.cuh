@@ -12,15 +12,11 @@ namespace um {
 // n; atoms follow each other along m or n.  MN-major: a row holds 64 consecutive
 // n of one k; atoms follow each other along k, and the next 64 n lie `lbo`
 // bytes on.
-__device__ __forceinline__ uint64_t desc(uint32_t smem, uint32_t lbo) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem >> 4) & 0x3FFFu);
-  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
-  d |= (uint64_t)(1024u >> 4) << 32;
-  d |= (uint64_t)1u << 46;
-  d |= (uint64_t)2u << 61;
-  return d;
+__device__ __forceinline__ uint32_t desc_lo(uint32_t smem, uint32_t lbo) {
+  return ((smem >> 4) & 0x3FFFu) | (((lbo >> 4) & 0x3FFFu) << 16);
 }
+// high word: 1024 bytes between atoms, descriptor version, 128-byte swizzle
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 
 // Instruction descriptor of kind::f16: fp32 accumulate, M = 128, N = 128; A and
 // B both bf16 or both f16; B K-major or MN-major.
@@ -29,25 +25,177 @@ __host__ __device__ constexpr uint32_t idesc(bool bf16, bool b_mn) {
          ((128u >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, bool acc) {
+// The eight k-steps of S = Q K^T over a 128 x 128 x 128 tile, both operands
+// K-major in two 64-element halves; a, b: low words of their descriptors.  The
+// whole warp calls (uniform operands); one elected lane issues.
+__device__ __forceinline__ void mma_s(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(id), "r"((uint32_t)acc)
+      "{\n"
+      ".reg .pred pe, pz, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 da, db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "setp.eq.b32 pz, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, pz;\n"
+      "add.u32 x, %1, 2;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 2;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 4;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 4;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 6;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 6;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1024;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 1024;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1026;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 1026;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1028;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 1028;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1030;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 1030;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id)
       : "memory");
 }
-// A from tensor memory (two 16-bit elements of consecutive k per column)
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, bool acc) {
+// The eight k-steps of O (+)= P V: P in tensor memory, 16 slots in each 8 columns
+// of every 32; V MN-major, 2048 bytes a k-step.  acc = 0: O is overwritten.
+__device__ __forceinline__ void mma_o(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(id), "r"((uint32_t)acc)
+      "{\n"
+      ".reg .pred pe, p0, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 p0, %5, 0;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, p0;\n"
+      "add.u32 x, %1, 8;\n"
+      "add.u32 y, %2, 128;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 32;\n"
+      "add.u32 y, %2, 256;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 40;\n"
+      "add.u32 y, %2, 384;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 64;\n"
+      "add.u32 y, %2, 512;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 72;\n"
+      "add.u32 y, %2, 640;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 96;\n"
+      "add.u32 y, %2, 768;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 104;\n"
+      "add.u32 y, %2, 896;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
       : "memory");
 }
+// The same with a second P, 16 columns on, added to the first.
+__device__ __forceinline__ void mma_o2(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n"
+      ".reg .pred pe, p0, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 p0, %5, 0;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, p0;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 8;\n"
+      "add.u32 y, %2, 128;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 32;\n"
+      "add.u32 y, %2, 256;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 40;\n"
+      "add.u32 y, %2, 384;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 64;\n"
+      "add.u32 y, %2, 512;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 72;\n"
+      "add.u32 y, %2, 640;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 96;\n"
+      "add.u32 y, %2, 768;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 104;\n"
+      "add.u32 y, %2, 896;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, x, 16;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
+      : "memory");
+}
+// The whole warp calls; the lane that issues the MMAs commits them.
 __device__ __forceinline__ void commit(uint32_t mbar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                   mbar)
-               : "memory");
+  asm volatile(
+      "{\n .reg .pred pe;\n elect.sync _|pe, 0xffffffff;\n"
+      " @pe tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(mbar)
+      : "memory");
 }
 __device__ __forceinline__ void fence_before() {
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
