@@ -594,6 +594,20 @@ bool make_row_map(CUtensorMap* map, const void* base, uint64_t rows, uint32_t bo
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_code_map(CUtensorMap* map, const void* base, uint32_t row_bytes, uint64_t rows,
+                   uint32_t box_rows) {
+  auto fn = encode_fn();
+  if (!fn || (row_bytes != 64 && row_bytes != 128)) return false;
+  cuuint64_t dims[2] = {row_bytes, rows};
+  cuuint64_t strides[1] = {row_bytes};
+  cuuint32_t box[2] = {row_bytes, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // R = G w observation rows per KV head: pass 1 takes 128-row halves, pass 2
 // groups of min(R, 256) rows (one MMA's N each).
 bool score_tc_supported(const Prob& p) {

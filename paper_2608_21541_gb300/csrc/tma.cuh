@@ -14,6 +14,11 @@ namespace certkv {
 // entry point is missing or rejects the map (host).
 bool make_row_map(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
 
+// 2-D view [rows][row_bytes] of byte rows (64 or 128 bytes, dense) with boxes of
+// whole rows and a swizzle as wide as a row; false as above.
+bool make_code_map(CUtensorMap* map, const void* base, uint32_t row_bytes, uint64_t rows,
+                   uint32_t box_rows);
+
 namespace tc {
 
 constexpr uint32_t kSpinLimit = 1u << 22;

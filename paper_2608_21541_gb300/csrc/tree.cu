@@ -6,9 +6,10 @@
 // t's mask word.  A draft that a row does not see is never read for it, so a
 // NaN there cannot reach it.
 //
-// Three launches: a scan of the segments' tile counts, the split kernel
-// (tree_tc.cu) over equal shares of all tiles, and the merge below, which joins
-// the records of the CTAs that met a unit in the log-sum-exp domain.
+// Three launches: a scan of the segments' tile counts, a split kernel over equal
+// shares of all tiles (tree_mma.cu for up to 16 query rows per unit, else
+// tree_tc.cu), and the merge below, which joins the records of the CTAs that met
+// a unit in the log-sum-exp domain and, for few rows, adds the drafts.
 #include <math.h>
 
 #include "../../include/certkv.h"
@@ -19,7 +20,7 @@
 namespace certkv {
 
 // One block: first[u] = tiles of the segments before u, first[units] their sum.
-__global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int with_drafts,
+__global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int tile, int with_drafts,
                                                          int64_t* __restrict__ first) {
   __shared__ long long wsum[32];
   __shared__ long long carry;
@@ -29,7 +30,7 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int with_draf
   for (int base = 0; base < st.units; base += 1024) {
     const int u = base + threadIdx.x;
     const long long v =
-        u < st.units ? (st.count(u) + kTreeTile - 1) / kTreeTile + with_drafts : 0;
+        u < st.units ? (st.count(u) + tile - 1) / tile + with_drafts : 0;
     long long x = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -87,12 +88,35 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
       A.w = fmaf(a.w, f, A.w);
     }
   }
+  if (p.small && p.kn.p) {
+    // the drafts the row sees, four dimensions a lane; a draft it does not see is
+    // not read
+    const uint2 x = *reinterpret_cast<const uint2*>(p.q.at(b, l, t, h * p.G + g) + 4 * lane);
+    const float q[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
+    for (uint64_t see = seen(p, b, t); see; see &= see - 1) {
+      const int j = __ffsll((long long)see) - 1;
+      const uint2 k = *reinterpret_cast<const uint2*>(p.kn.at(b, l, j, h) + 4 * lane);
+      const uint2 v = *reinterpret_cast<const uint2*>(p.vn.at(b, l, j, h) + 4 * lane);
+      float z = q[0] * bf16lo(k.x) + q[1] * bf16hi(k.x) + q[2] * bf16lo(k.y) + q[3] * bf16hi(k.y);
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
+      z *= p.scale_log2;
+      const float m = fmaxf(M, z);
+      const float c = M == m ? 1.f : exp2f(M - m), f = z == -INFINITY ? 0.f : exp2f(z - m);  // a NaN logit stays one
+      M = m;
+      L = fmaf(L, c, f);
+      A.x = fmaf(f, bf16lo(v.x), A.x * c);
+      A.y = fmaf(f, bf16hi(v.x), A.y * c);
+      A.z = fmaf(f, bf16lo(v.y), A.z * c);
+      A.w = fmaf(f, bf16hi(v.y), A.w * c);
+    }
+  }
   const float inv = L != 0.f ? 1.f / L : 0.f;  // a NaN sum stays a NaN
   A.x *= inv;
   A.y *= inv;
   A.z *= inv;
   A.w *= inv;
-  if (p.kn.p) {
+  if (!p.small && p.kn.p) {
     for (uint64_t odd = p.odd[u] & seen(p, b, t); odd; odd &= odd - 1) {
       const uint2 x = *reinterpret_cast<const uint2*>(p.vn.at(b, l, __ffsll((long long)odd) - 1, h) + 4 * lane);
       const float v[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
@@ -196,11 +220,12 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   row_blocks(p.rows, &p.nblk, &p.rb);
   const int64_t merge = ((int64_t)p.units * p.rows + 7) / 8;
   if (merge > INT32_MAX) return CERTKV_EINVAL;
-  p.ctas = tree_ctas();
+  p.small = p.rows <= kSmallRows;
+  p.ctas = p.small ? tree_mma_ctas(store->format) : tree_ctas();
   if (p.ctas < 1) return CERTKV_ECUDA;
   if (p.ctas > kTreeMaxCtas) p.ctas = kTreeMaxCtas;
   // a CTA counts its tiles in 32 bits
-  if ((int64_t)p.units * (p.st.max_pages / 2 + 2) / p.ctas * p.nblk >= (1 << 30)) return CERTKV_EINVAL;
+  if ((int64_t)p.units * (p.st.max_pages + 2) / p.ctas * p.nblk >= (1 << 29)) return CERTKV_EINVAL;
   const TreeLayout ly = tree_layout(p.units, p.rows);
   char* ws = reinterpret_cast<char*>(workspace);
   int64_t* first = reinterpret_cast<int64_t*>(ws + ly.first);
@@ -211,9 +236,11 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   {
     TraceScope ts_("tree_plan", st);
-    tree_plan_kernel<<<1, 1024, 0, st>>>(p.st, p.kn.p ? 1 : 0, first);
+    tree_plan_kernel<<<1, 1024, 0, st>>>(p.st, p.small ? small_tile(store->format) : kTreeTile,
+                                         !p.small && p.kn.p ? 1 : 0, first);
   }
-  if (!launch_tree_tc(p, store->format, st)) return CERTKV_ECUDA;
+  if (!(p.small ? launch_tree_mma(p, store->format, st) : launch_tree_tc(p, store->format, st)))
+    return CERTKV_ECUDA;
   {
     TraceScope ts_("tree_merge", st);
     tree_merge_kernel<<<(unsigned)merge, 256, 0, st>>>(p);

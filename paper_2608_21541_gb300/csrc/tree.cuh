@@ -9,7 +9,12 @@
 
 namespace certkv {
 
-constexpr int kTreeTile = 128;  // slots per tile: two pages
+constexpr int kTreeTile = 128;  // slots per tile of the tcgen05 kernel: two pages
+constexpr int kSmallRows = 16;  // up to this many query rows: the mma.sync kernel
+// slots per tile of that kernel
+__host__ __device__ constexpr int small_tile(int format) {
+  return format == CERTKV_STORE_BF16 ? 32 : CERTKV_STORE_PAGE;
+}
 constexpr float kLn2 = 0.69314718055994531f;
 
 struct TreeArgs {
@@ -17,6 +22,7 @@ struct TreeArgs {
   int units, rows;    // B L H, T G query rows per unit
   int nblk, rb;       // row blocks of a unit, rows of a block (the last may have fewer)
   int ctas;           // CTAs the tiles are divided among
+  int small;          // the mma.sync kernel: the merge takes the drafts
   Rows q, kn, vn, o;  // kn.p null: the drafts have no keys of their own
   const uint64_t* mask;
   float* lse;
@@ -80,7 +86,11 @@ struct Items {
   }
 };
 
-int tree_ctas();  // CTAs of the split kernel on the current device; 0 on an error
+// CTAs of the split kernels on the current device (0 on an error), and their
+// launches (false: nothing launched).
+int tree_ctas();
+int tree_mma_ctas(int format);
 bool launch_tree_tc(const TreeArgs& p, int format, cudaStream_t st);
+bool launch_tree_mma(const TreeArgs& p, int format, cudaStream_t st);
 
 }  // namespace certkv
