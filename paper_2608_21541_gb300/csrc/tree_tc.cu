@@ -28,12 +28,14 @@
 // fp32 scale multiplies its logit; a value is rounded once to f16 (2^-11) with
 // its scale taken relative to the tile's largest, and a weight once to f16.
 // Logits, sums, and accumulators are fp32.  A weight is 2^(x - C) for a
-// reference C that follows the row's maximum only when it grows by more than
-// 2^8, which keeps weights in f16's range and most tiles free of rescaling.
+// reference C that moves to the row's maximum only when weights would leave
+// their range (f16: 2^15), so that most tiles are formed in one pass over the
+// logits, without their maximum and without rescaling.
 //
 // Every wait is bounded; on a timeout the roles stop waiting, the rows in
 // question read NaN and the store's status word gets CERTKV_STATUS_TIMEOUT.
 #include <cuda.h>
+#include <stddef.h>
 
 #include "../../include/certkv.h"
 #include "common.cuh"
@@ -79,14 +81,13 @@ struct Place {
       : slot(i % Plan<PAIR>::kRing), phase((i / Plan<PAIR>::kRing) & 1u) {}
 };
 constexpr uint32_t kColS = 0, kColO = 256;  // + 128 stream
-constexpr float kLazy = 8.f;                // growth of the maximum that moves the reference
 
 // A tile's facts, stated by the scout four tiles ahead of its keys.  Slot t % 8 is
 // written again, for tile t + 8, once the place of K(t + 4) is free; that place
 // held V(t) (ring of 5) or K(t + 2) (ring of 4), both released by products issued
 // after P of tile t had been written, so every reader of slot t is done.
 constexpr uint32_t kMeta = 8;
-struct Meta {
+struct alignas(16) Meta {  // its arrays are read and written as float4
   float ks[kTreeTile];  // scale of each slot's key (8- and 4-bit stores)
   float vf[kTreeTile];  // scale of each slot's value over 2^shift
   uint32_t live[4];     // slots to take
@@ -110,6 +111,7 @@ struct Misc {
   float cm[128], l[128], sh[128];  // stream 1's reference, sum and shift
   Meta meta[kMeta];
 };
+static_assert(sizeof(Meta) % 16 == 0 && offsetof(Misc, meta) % 16 == 0, "float4 accesses");
 template <bool PAIR>
 constexpr int smem_bytes() {
   return Plan<PAIR>::kMiscOff + (int)sizeof(Misc) + 1024;
@@ -310,16 +312,16 @@ struct Scout {
                    "r"(bytes)
                    : "memory");
   }
-  // Scales of slots 4 lane .. 4 lane + 3 of a tile (0: no slot).
-  __device__ __forceinline__ float4 scales(const float* s, int a, int b, int live) const {
+  // Scales of slots 4 lane .. 4 lane + 3 of a tile (`none` where there is no slot).
+  __device__ __forceinline__ float4 scales(const float* s, int a, int b, int live, float none) const {
     const int pg = lane < 16 ? a : b, n = live - 4 * lane;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 x = make_float4(none, none, none, none);
     if (pg >= 0)
       x = __ldg(reinterpret_cast<const float4*>(s + (int64_t)pg * kPage + ((4 * lane) & (kPage - 1))));
-    if (n < 1) x.x = 0.f;
-    if (n < 2) x.y = 0.f;
-    if (n < 3) x.z = 0.f;
-    if (n < 4) x.w = 0.f;
+    if (n < 1) x.x = none;
+    if (n < 2) x.y = none;
+    if (n < 3) x.z = none;
+    if (n < 4) x.w = none;
     return x;
   }
   // State tile t, the next of the walk.
@@ -344,8 +346,8 @@ struct Scout {
       const int live = count - k * kTreeTile, a = page(2 * k), b = page(2 * k + 1);
       int shift = 0;
       if (kQuant) {
-        const float4 ks = scales(p.st.ks, a, b, live);
-        float4 vs = scales(p.st.vs, a, b, live);
+        const float4 ks = scales(p.st.ks, a, b, live, 1.f);  // finite where there is no slot
+        const float4 vs = scales(p.st.vs, a, b, live, 0.f);
         // from the tile's largest row maximum, a NaN left out
         float x = fmaxf(fmaxf(vs.x, vs.y), fmaxf(vs.z, vs.w));
 #pragma unroll
@@ -670,31 +672,39 @@ struct Issuer {
 };
 
 // --------------------------------------------------------------- softmax --
-// The largest logit of a row over a tile (times the keys' scales), from tensor
-// memory; MASK: only of the slots in live.
-template <bool QUANT, bool MASK>
-__device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt, const uint32_t (&live)[4]) {
+// -inf over the logits of the slots that a row does not take (tiles that are not
+// whole), so that the passes below need not ask.
+__device__ __forceinline__ void mask_tile(uint32_t tS, const uint32_t (&live)[4]) {
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t w = c < 2 ? (c ? live[1] : live[0]) : (c == 2 ? live[2] : live[3]);
+    uint32_t r[32];
+    um::ld32(tS + 32u * c, r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (!(w >> j & 1u)) r[j] = 0xff800000u;
+    um::st32(tS + 32u * c, r);
+  }
+  um::wait_st();
+}
+
+// The largest logit of a row over a tile, from tensor memory; SCALE: times the
+// keys' scales.
+template <bool SCALE>
+__device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt) {
   float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll 1
-  for (int c = 0; c < 2; ++c) {
-    uint32_t r[64];
-    um::ld64(tS + 64u * c, r);
-    const uint32_t w0 = c ? live[2] : live[0], w1 = c ? live[3] : live[1];
+  for (int c = 0; c < 4; ++c) {
+    uint32_t r[32];
+    um::ld32(tS + 32u * c, r);
 #pragma unroll
-    for (int j = 0; j < 64; j += 4) {
+    for (int j = 0; j < 32; j += 4) {
       float2 x = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
       float2 y = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-      if (QUANT) {
-        const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[64 * c + j]);
+      if (SCALE) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[32 * c + j]);
         x = fmul2(x, make_float2(k4.x, k4.y));
         y = fmul2(y, make_float2(k4.z, k4.w));
-      }
-      if (MASK) {
-        const uint32_t w = j < 32 ? w0 : w1;
-        if (!(w >> (j & 31) & 1u)) x.x = -INFINITY;
-        if (!(w >> ((j + 1) & 31) & 1u)) x.y = -INFINITY;
-        if (!(w >> ((j + 2) & 31) & 1u)) y.x = -INFINITY;
-        if (!(w >> ((j + 3) & 31) & 1u)) y.y = -INFINITY;
       }
       if (j & 4) {
         m0 = um::max3(m0, x.x, x.y);
@@ -708,58 +718,133 @@ __device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt, const uin
   return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
 }
 
-// Weights 2^(x sl + off) of a row over a tile, written over its logits as the
-// MMAs' A operand (32 columns of S: 16 of weights, for bf16 then 16 of their
-// remainders); returns their sum.
-template <bool QUANT, bool MASK>
-__device__ __forceinline__ float tile_weights(uint32_t tS, const Meta& mt, const uint32_t (&live)[4],
-                                              float sl, float off) {
-  const float2 sl2 = make_float2(sl, sl), off2 = make_float2(off, off);
-  float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
-#pragma unroll 1
-  for (int c = 0; c < 4; ++c) {
+// A row's running reference, sum and accumulator over the tiles it has met.
+template <bool QUANT>
+struct Row {
+  float C = -INFINITY;  // reference (an integer; log2 domain, less 6 bits of head room for f16)
+  float lsum = 0.f;     // sum of the weights relative to it
+  float sl;             // scale of the row's logits, > 0
+
+  // Largest sum of 32 weights that needs no new reference: within f16's range, or
+  // far within fp32's and bf16's.
+  static constexpr float kLimit = QUANT ? 32768.f : 1.152921504606847e18f;
+  __device__ __forceinline__ float reference(float mx, float dE) const {
+    return ceilf(fmaf(mx, sl, dE - (QUANT ? 6.f : 0.f)));  // -inf stays
+  }
+  __device__ __forceinline__ float offset(float dE) const { return dE - (C == -INFINITY ? 0.f : C); }
+
+  // Weights of columns 32 c ..: the packed A operand in hi (and remainders in
+  // lo); returns their sum.  The keys' scales are fetched before the logits,
+  // while nothing waits for them.
+  __device__ __forceinline__ float chunk(uint32_t tS, int c, const Meta& mt, float off, uint32_t (&hi)[16],
+                                         uint32_t (&lo)[16]) const {
+    const float2 sl2 = make_float2(sl, sl), off2 = make_float2(off, off);
+    float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
+    float4 k4[8];
+    if (QUANT) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) k4[j] = *reinterpret_cast<const float4*>(&mt.ks[32 * c + 4 * j]);
+    }
     uint32_t r[32];
     um::ld32(tS + 32u * c, r);
-    const uint32_t w = c < 2 ? (c ? live[1] : live[0]) : (c == 2 ? live[2] : live[3]);
-    uint32_t hi[16], lo[16];
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-      float2 x = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
-      float2 y = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-      if (QUANT) {
-        const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[32 * c + j]);
-        x = fmul2(x, make_float2(k4.x, k4.y));
-        y = fmul2(y, make_float2(k4.z, k4.w));
-      }
+    for (int j = 0; j < 16; ++j) {
+      float2 x = make_float2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+      if (QUANT)
+        x = fmul2(x, j & 1 ? make_float2(k4[j / 2].z, k4[j / 2].w) : make_float2(k4[j / 2].x, k4[j / 2].y));
       x = ffma2(x, sl2, off2);
-      y = ffma2(y, sl2, off2);
-      if (MASK) {
-        if (!(w >> j & 1u)) x.x = -INFINITY;
-        if (!(w >> (j + 1) & 1u)) x.y = -INFINITY;
-        if (!(w >> (j + 2) & 1u)) y.x = -INFINITY;
-        if (!(w >> (j + 3) & 1u)) y.y = -INFINITY;
-      }
       x.x = um::ex2(x.x);
       x.y = um::ex2(x.y);
-      y.x = um::ex2(y.x);
-      y.y = um::ex2(y.y);
-      sum0 = fadd2(sum0, x);
-      sum1 = fadd2(sum1, y);
+      if (j & 1) sum1 = fadd2(sum1, x);
+      else sum0 = fadd2(sum0, x);
       if (QUANT) {
-        hi[j / 2] = pack_f16(x.x, x.y);
-        hi[j / 2 + 1] = pack_f16(y.x, y.y);
+        hi[j] = pack_f16(x.x, x.y);
       } else {
-        hi[j / 2] = pack_bf16(x.x, x.y);
-        hi[j / 2 + 1] = pack_bf16(y.x, y.y);
-        lo[j / 2] = pack_bf16(x.x - bf16lo(hi[j / 2]), x.y - bf16hi(hi[j / 2]));
-        lo[j / 2 + 1] = pack_bf16(y.x - bf16lo(hi[j / 2 + 1]), y.y - bf16hi(hi[j / 2 + 1]));
+        hi[j] = pack_bf16(x.x, x.y);
+        lo[j] = pack_bf16(x.x - bf16lo(hi[j]), x.y - bf16hi(hi[j]));
       }
     }
-    um::st16(tS + 32u * c, hi);
-    if (!QUANT) um::st16(tS + 32u * c + 16u, lo);
+    return (sum0.x + sum0.y) + (sum1.x + sum1.y);
   }
-  return (sum0.x + sum0.y) + (sum1.x + sum1.y);
-}
+
+  // A new reference from columns 32 c .. of the tile: the accumulator, the sums
+  // and the weights of the tile's earlier columns are scaled to it (by a power
+  // of two).  `acc`: there is an accumulator.
+  __device__ __forceinline__ void regrow(uint32_t tS, uint32_t tO, int c, const Meta& mt, float dE, bool acc,
+                                         float& sum) {
+    float mx = -INFINITY;
+    um::wait_st();  // earlier columns' weights are read back below
+    {
+      uint32_t r[32];
+      um::ld32(tS + 32u * c, r);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) mx = fmaxf(mx, __uint_as_float(r[j]) * (QUANT ? mt.ks[32 * c + j] : 1.f));
+    }
+    const float nc = reference(mx, dE);
+    float f = 1.f;
+    if (nc > C) {
+      f = um::ex2(C - nc);
+      C = nc;
+    }
+    lsum *= f;
+    sum *= f;
+    if (acc) {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        uint32_t r[32];
+        um::ld32(tO + 32u * i, r);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * f);
+        um::st32(tO + 32u * i, r);
+      }
+    }
+#pragma unroll 1
+    for (int i = 0; i < (QUANT ? c : 2 * c); ++i) {  // sixteen columns each
+      const uint32_t at = tS + (QUANT ? 32u * i : 16u * i);
+      uint32_t r[16];
+      um::ld16(at, r);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (QUANT) {
+          const float2 x = f16x2_to_f32(r[j]);
+          r[j] = pack_f16(x.x * f, x.y * f);
+        } else {
+          r[j] = pack_bf16(bf16lo(r[j]) * f, bf16hi(r[j]) * f);
+        }
+      }
+      um::st16(at, r);
+    }
+  }
+
+  // One tile: its weights are written over its logits as the MMAs' A operand, 16
+  // columns of every 32 (for bf16 the next 16 hold the remainders).  The
+  // reference at hand is tried first: only columns whose weights leave the
+  // range have their maximum taken and the reference moved.
+  __device__ __forceinline__ void tile(uint32_t tS, uint32_t tO, const Meta& mt, float dE, bool acc) {
+    if (__any_sync(kFull, C == -INFINITY)) {  // a row that has met nothing yet: no accumulator to scale
+      const float mx = tile_max<QUANT>(tS, mt);
+      if (C == -INFINITY) C = reference(mx, dE);
+    }
+    float sum = 0.f;
+    bool again = false;
+#pragma unroll 1
+    for (int c = 0; c < 4;) {
+      uint32_t hi[16], lo[16];
+      const float x = chunk(tS, c, mt, offset(dE), hi, lo);
+      if (!again && __any_sync(kFull, !(x < kLimit))) {
+        regrow(tS, tO, c, mt, dE, acc, sum);
+        again = true;
+        continue;
+      }
+      again = false;
+      um::st16(tS + 32u * c, hi);
+      if (!QUANT) um::st16(tS + 32u * c + 16u, lo);
+      sum += x;
+      ++c;
+    }
+    lsum = fmaf(sum, QUANT ? um::ex2(-dE) : 1.f, lsum);
+  }
+};
 
 template <int FMT, bool PAIR>
 __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t base, uint32_t tmem,
@@ -789,7 +874,7 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
         const int r = r0 + 16 * i;
         x[i] = make_uint4(0u, 0u, 0u, 0u);
         if (r < rows) {
-          const int row = it.blk * p.rb + r, t = row / p.G, g = row - t * p.G;
+          const int br = it.blk * p.rb + r, t = br / p.G, g = br - t * p.G;
           x[i] = __ldg(reinterpret_cast<const uint4*>(p.q.at(b, l, t, h * p.G + g)) + c);
         }
       }
@@ -817,17 +902,15 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
     }
     um::fence_async();
     softmax_sync();  // also: qs of every row is there
-    const float sl = fmaxf(kQuant ? m->qs[brow] * p.scale_log2 : p.scale_log2, 1.1754944e-38f);
+    Row<kQuant> row;
+    row.sl = fmaxf(kQuant ? m->qs[brow] * p.scale_log2 : p.scale_log2, 1.1754944e-38f);
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(bar(&m->q_full));  // rows written, qs read by the warp
 
     const int n = it.kb - it.ka, steps = PAIR ? n : (n - s + 1) / 2;
     const int tok = (it.blk * p.rb + min(brow, rows - 1)) / p.G;
     const uint64_t word = p.kn.p ? seen(p, b, tok) : 0ull;
-    // C: reference of the weights (log2 domain, less 6 bits of head room for f16);
-    // lsum: their sum; shift0: exponent the accumulator is relative to
-    float C = -INFINITY, lsum = 0.f;
-    int shift0 = 0;
+    int shift0 = 0;  // exponent the accumulator is relative to
     for (int i = 0; busy && i < steps; ++i) {
       const uint32_t t = t0 + (uint32_t)(PAIR ? i : 2 * i + s);
       ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[s]), uses & 1u, ab)) &&
@@ -836,40 +919,15 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
       if (!ok) break;
       um::fence_after();
       const Meta& mt = m->meta[t % kMeta];
-      const bool whole = mt.whole;
-      uint32_t live[4] = {~0u, ~0u, ~0u, ~0u};
-      if (!whole) {
+      if (!mt.whole) {
         const bool own = mt.drafts;
-        live[0] = own ? (uint32_t)word : mt.live[0];
-        live[1] = own ? (uint32_t)(word >> 32) : mt.live[1];
-        live[2] = own ? 0u : mt.live[2];
-        live[3] = own ? 0u : mt.live[3];
+        const uint32_t live[4] = {own ? (uint32_t)word : mt.live[0], own ? (uint32_t)(word >> 32) : mt.live[1],
+                                  own ? 0u : mt.live[2], own ? 0u : mt.live[3]};
+        mask_tile(tS, live);
       }
       if (i == 0) shift0 = mt.shift;
       const float dE = kQuant ? (float)(mt.shift - shift0) : 0.f;
-      float mx = whole ? tile_max<kQuant, false>(tS, mt, live) : tile_max<kQuant, true>(tS, mt, live);
-      mx = fmaf(mx, sl, dE - (kQuant ? 6.f : 0.f));  // sl > 0; -inf stays
-      float f = 1.f;
-      if (mx > C + kLazy || C == -INFINITY) {
-        const float nc = fmaxf(mx, C);
-        f = C == -INFINITY ? 1.f : um::ex2(C - nc);
-        C = nc;
-      }
-      if (i > 0 && __any_sync(kFull, f != 1.f)) {  // O of the tiles before is done (see Issuer)
-        lsum *= f;
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32];
-          um::ld32(tO + 32u * c, r);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * f);
-          um::st32(tO + 32u * c, r);
-        }
-      }
-      const float off = dE - (C == -INFINITY ? 0.f : C);
-      const float sum = whole ? tile_weights<kQuant, false>(tS, mt, live, sl, off)
-                              : tile_weights<kQuant, true>(tS, mt, live, sl, off);
-      lsum = fmaf(sum, kQuant ? um::ex2(-dE) : 1.f, lsum);
+      row.tile(tS, tO, mt, dE, i > 0);  // O of the tiles before is done (see Issuer)
       um::wait_st();
       um::fence_before();
       __syncwarp();
@@ -883,8 +941,8 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
     um::fence_after();
     const bool both = !PAIR && n > 1;  // join the streams: stream 0 writes
     if (!PAIR && s == 1 && busy) {
-      m->cm[lrow] = C;
-      m->l[lrow] = lsum;
+      m->cm[lrow] = row.C;
+      m->l[lrow] = row.lsum;
       m->sh[lrow] = (float)shift0;
     }
     um::fence_before();
@@ -892,6 +950,7 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
     um::fence_after();
     if (busy && (PAIR || s == 0)) {
       // stream s: sum 2^C lsum, accumulator relative to 2^(C + shift0)
+      const float C = row.C, lsum = row.lsum;
       float f0 = 1.f, f1 = 0.f, Cj = C, lj = lsum;
       if (both) {
         const float C1 = m->cm[lrow], l1 = m->l[lrow];
