@@ -671,20 +671,36 @@ def certkv_decode_attn_noalloc(q, packed: Packed, *, hkv: int, scale: float = 0.
 def _rows(t: torch.Tensor, name: str) -> certkv_rows:
     """The certkv_rows view of a bf16 CUDA tensor [B][L][T][heads][128] with
     contiguous rows and any other strides."""
-    if t.dim() != 5 or t.shape[4] != 128 or t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16 or t.dim() != 5 or t.shape[4] != 128:
         raise TypeError(f"{name} must be a bfloat16 tensor [B][L][T][heads][128]")
-    sb, sl, st, sh, sd = t.stride()
-    if not t.is_cuda or sd != 1:
+    st = t.stride()
+    if st[4] != 1 or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor whose rows are contiguous")
-    return certkv_rows(t.data_ptr(), sb, sl, st, sh)
+    return certkv_rows(t.data_ptr(), st[0], st[1], st[2], st[3])
 
 
 def _index(t: Optional[torch.Tensor], name: str, shape: tuple, dtype=torch.int32):
+    """Address of a dense CUDA tensor of this shape and type (None: none)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {shape}")
-    return _ptr(t)
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor")
+    return t.data_ptr()
+
+
+def _workspace(ws: torch.Tensor) -> tuple:
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("the workspace must be a contiguous CUDA tensor")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _on(stream) -> int:
+    """The CUDA stream a call is enqueued on (None: the current one)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _keep_for(stream, *made):
@@ -724,7 +740,7 @@ def certkv_rope(q, positions, plan: certkv_rope_angles, k=None, *, out=None, k_o
     rq = _rows(q, "q")
     made = []
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
         made.append(out)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
@@ -732,17 +748,17 @@ def certkv_rope(q, positions, plan: certkv_rope_angles, k=None, *, out=None, k_o
     H, rk, rko = 0, None, None
     if k is not None:
         H = k.shape[3]
-        if tuple(k.shape[:3]) != (B, L, T):
+        if k.shape[:3] != (B, L, T):
             raise ValueError("k must have the sequences, layers and tokens of q")
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            k_out = k.new_empty(k.shape)
             made.append(k_out)
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have the shape of k")
         rk, rko = ctypes.byref(_rows(k, "k")), ctypes.byref(_rows(k_out, "k_out"))
     rc = load_library().certkv_rope(B, L, T, Hq, H, ctypes.byref(rq), ctypes.byref(ro), rk, rko,
                                     _index(positions, "positions", (B, T)), ctypes.byref(plan),
-                                    int(bool(inverse)), _stream(stream))
+                                    int(bool(inverse)), _on(stream))
     _check(rc, "certkv_rope")
     _keep_for(stream, *made)
     return out if k is None else (out, k_out)
@@ -851,8 +867,7 @@ def certkv_store_load(packed: Packed, store: Store, reserve: int = 0, *, ws=None
         ws = made = workspace(certkv_store_workspace_bytes(store.units), store.k.device)
     pst = packed.struct()
     rc = load_library().certkv_store_load(ctypes.byref(pst), int(packed.tail_slot), int(reserve),
-                                          ctypes.byref(store.struct()), _ptr(ws),
-                                          ws.numel() * ws.element_size(), _stream(stream))
+                                          ctypes.byref(store.struct()), *_workspace(ws), _on(stream))
     _check(rc, "certkv_store_load")
     _keep_for(stream, made)
     return store
@@ -871,7 +886,7 @@ def certkv_store_append(k, v, store: Store, *, select=None, accepted=None, start
     rc = load_library().certkv_store_append(
         B, L, H, T, ctypes.byref(rk), ctypes.byref(rv), _index(select, "select", (B, T)),
         _index(accepted, "accepted", (B,)), _index(start, "start", (store.units,)),
-        ctypes.byref(store.struct()), _stream(stream))
+        ctypes.byref(store.struct()), _on(stream))
     _check(rc, "certkv_store_append")
     return store
 
@@ -890,7 +905,7 @@ def certkv_store_read(store: Store, tokens: int, *, start=None, k_out=None, v_ou
     rc = load_library().certkv_store_read(
         ctypes.byref(store.struct()), _index(start, "start", (store.units,)), int(tokens),
         _index(k_out, "k_out", shape, torch.bfloat16),
-        _index(v_out, "v_out", shape, torch.bfloat16), _stream(stream))
+        _index(v_out, "v_out", shape, torch.bfloat16), _on(stream))
     _check(rc, "certkv_store_read")
     _keep_for(stream, *made)
     return k_out, v_out
@@ -912,7 +927,7 @@ def certkv_tree_attn(q, store: Store, *, hkv: int, k_new=None, v_new=None, mask=
     rq = _rows(q, "q")
     made = []
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
         made.append(out)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
@@ -920,7 +935,7 @@ def certkv_tree_attn(q, store: Store, *, hkv: int, k_new=None, v_new=None, mask=
     rk = rv = None
     if k_new is not None or v_new is not None:
         if k_new is None or v_new is None or k_new.shape != v_new.shape or \
-                tuple(k_new.shape[:4]) != (B, L, T, hkv):
+                k_new.shape[:4] != (B, L, T, hkv):
             raise ValueError("k_new and v_new must both be [B][L][T][hkv][128]")
         rk, rv = ctypes.byref(_rows(k_new, "k_new")), ctypes.byref(_rows(v_new, "v_new"))
     lib = load_library()
@@ -930,8 +945,7 @@ def certkv_tree_attn(q, store: Store, *, hkv: int, k_new=None, v_new=None, mask=
     rc = lib.certkv_tree_attn(
         ctypes.byref(shape), T, ctypes.byref(rq), rk, rv,
         _index(mask, "mask", (B, T), torch.int64), ctypes.byref(store.struct()), float(scale),
-        ctypes.byref(ro), _index(lse, "lse", (B, L, T, Hq), torch.float32), _ptr(ws),
-        ws.numel() * ws.element_size(), _stream(stream))
+        ctypes.byref(ro), _index(lse, "lse", (B, L, T, Hq), torch.float32), *_workspace(ws), _on(stream))
     _check(rc, "certkv_tree_attn")
     _keep_for(stream, *made)
     return out

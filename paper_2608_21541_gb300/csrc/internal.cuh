@@ -138,6 +138,29 @@ bool launch_decode_certified(const Prob& p, const void* q, const void* pk, const
 void trace_begin(const char* name, cudaStream_t st);
 void trace_end(cudaStream_t st);
 
+// Launch of a kernel that may start while the one before it in the stream still
+// runs; it waits for that kernel's results with await_previous() before it reads
+// them (the kernel before it lets it start with release_next()).
+template <class... P, class... A>
+void launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st,
+                  A&&... args) {
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = dim3(block);
+  c.dynamicSmemBytes = smem;
+  c.stream = st;
+  c.attrs = &at;
+  c.numAttrs = 1;
+  cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...);  // an error stays for cudaGetLastError
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void release_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+#endif
+
 struct TraceScope {
   cudaStream_t st;
   TraceScope(const char* name, cudaStream_t s) : st(s) { trace_begin(name, s); }

@@ -25,6 +25,7 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int tile, int
   __shared__ long long wsum[32];
   __shared__ long long carry;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  release_next();
   if (threadIdx.x == 0) carry = 0;
   __syncthreads();
   for (int base = 0; base < st.units; base += 1024) {
@@ -62,6 +63,7 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int tile, int
 // out: the NaN and infinite elements of drafts the row sees.
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs p) {
   const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  await_previous();
   if (w >= (int64_t)p.units * p.rows) return;
   const int lane = threadIdx.x & 31;
   const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
@@ -243,7 +245,7 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
     return CERTKV_ECUDA;
   {
     TraceScope ts_("tree_merge", st);
-    tree_merge_kernel<<<(unsigned)merge, 256, 0, st>>>(p);
+    launch_after(tree_merge_kernel, (unsigned)merge, 256, 0, st, p);
   }
   return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA;
 }

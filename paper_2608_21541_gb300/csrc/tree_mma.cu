@@ -600,8 +600,6 @@ __global__ void __launch_bounds__(kThreads, 2) tree_mma_kernel(const __grid_cons
   char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float* wacc = reinterpret_cast<float*>(sm + G::kStages * G::kStage);
   Tail* tl = reinterpret_cast<Tail*>(wacc + kConsumers * kRows * kD);
-  const int64_t per = tiles_per_cta(p);
-  if (per * blockIdx.x >= p.first[p.units] * p.nblk) return;  // uniform, before any barrier
   if (threadIdx.x == 0) {
     for (int i = 0; i < G::kStages; ++i) {
       tc::mbar_init(bar(&tl->full[i]), 1);
@@ -610,6 +608,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_mma_kernel(const __grid_cons
     tl->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  release_next();
+  await_previous();
+  const int64_t per = tiles_per_cta(p);
+  if (per * blockIdx.x >= p.first[p.units] * p.nblk) return;  // uniform, before any barrier
   __syncthreads();
   if (threadIdx.x < 32) produce<FMT>(p, &tmK, &tmV, tc::saddr(sm), tl, threadIdx.x, per);
   else consume<FMT>(p, sm, wacc, tl, threadIdx.x - 32, per);
@@ -647,7 +649,7 @@ bool launch(const TreeArgs& p, cudaStream_t st) {
              !make_code_map(&mv, p.st.v, row_bytes(FMT), rows, Geo<FMT>::kSlots)) {
     return false;
   }
-  tree_mma_kernel<FMT><<<p.ctas, kThreads, smem_bytes<FMT>(), st>>>(mk, mv, p);
+  launch_after(tree_mma_kernel<FMT>, p.ctas, kThreads, smem_bytes<FMT>(), st, mk, mv, p);
   return true;
 }
 

@@ -1009,10 +1009,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   extern __shared__ char smem_raw[];
   char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Misc* m = reinterpret_cast<Misc*>(sm + Plan<PAIR>::kMiscOff);
-  const int64_t per = tiles_per_cta(p);
-  const int64_t left = p.first[p.units] * p.nblk - per * blockIdx.x;
-  if (left <= 0) return;  // uniform, before any barrier
-  const uint32_t n = (uint32_t)min(left, per);  // tiles of this CTA
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < Plan<PAIR>::kRing; ++i) {
@@ -1034,6 +1030,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     m->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  release_next();
+  await_previous();
+  const int64_t per = tiles_per_cta(p), left = p.first[p.units] * p.nblk - per * blockIdx.x;
+  if (left <= 0) return;  // uniform, before any barrier
+  const uint32_t n = (uint32_t)min(left, per);  // tiles of this CTA
   if (warp == kSoftWarps + kLoadWarps) um::alloc(tc::saddr(&m->tmem), 512);
   um::fence_before();
   __syncthreads();
@@ -1095,9 +1096,9 @@ int ctas_of_device() {
 template <int FMT>
 void launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& p, cudaStream_t st) {
   if (p.rb > 128)
-    tree_tc_kernel<FMT, true><<<p.ctas, kThreads, smem_bytes<true>(), st>>>(mk, mv, p);
+    launch_after(tree_tc_kernel<FMT, true>, p.ctas, kThreads, smem_bytes<true>(), st, mk, mv, p);
   else
-    tree_tc_kernel<FMT, false><<<p.ctas, kThreads, smem_bytes<false>(), st>>>(mk, mv, p);
+    launch_after(tree_tc_kernel<FMT, false>, p.ctas, kThreads, smem_bytes<false>(), st, mk, mv, p);
 }
 
 }  // namespace
