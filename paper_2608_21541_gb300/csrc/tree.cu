@@ -76,41 +76,84 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
     const int64_t per = tiles_per_cta(p), at = p.first[u] * p.nblk + blk * n;
     const int64_t vu = (int64_t)u * p.nblk + blk;
     const int c0 = (int)(at / per), c1 = (int)((at + n - 1) / per);
-    for (int c = c0; c <= c1; ++c) M = fmaxf(M, p.rec_ml[(c + vu) * p.rb + br].x);
-    for (int c = c0; c <= c1; ++c) {
-      const int64_t rec = (c + vu) * p.rb + br;
-      const float2 ml = p.rec_ml[rec];
-      if (ml.y == 0.f) continue;  // this CTA's tiles held nothing the row sees
-      const float4 a = *reinterpret_cast<const float4*>(p.rec_acc + rec * kD + 4 * lane);
-      const float f = ml.y * exp2f(ml.x - M);
-      L += f;
-      A.x = fmaf(a.x, f, A.x);
-      A.y = fmaf(a.y, f, A.y);
-      A.z = fmaf(a.z, f, A.z);
-      A.w = fmaf(a.w, f, A.w);
+    for (int c = c0; c <= c1; c += 4) {
+      float2 ml[4];
+      float4 a[4];
+      float m = M;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t rec = (min(c + i, c1) + vu) * p.rb + br;
+        ml[i] = p.rec_ml[rec];
+        a[i] = *reinterpret_cast<const float4*>(p.rec_acc + rec * kD + 4 * lane);
+        if (c + i > c1) ml[i] = make_float2(-INFINITY, 0.f);
+        m = fmaxf(m, ml[i].x);
+      }
+      const float back = M == m ? 1.f : exp2f(M - m);
+      M = m;
+      L *= back;
+      A.x *= back;
+      A.y *= back;
+      A.z *= back;
+      A.w *= back;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (ml[i].y == 0.f) continue;  // this CTA's tiles held nothing the row sees
+        const float f = ml[i].y * exp2f(ml[i].x - m);
+        L += f;
+        A.x = fmaf(a[i].x, f, A.x);
+        A.y = fmaf(a[i].y, f, A.y);
+        A.z = fmaf(a[i].z, f, A.z);
+        A.w = fmaf(a[i].w, f, A.w);
+      }
     }
   }
   if (p.small && p.kn.p) {
-    // the drafts the row sees, four dimensions a lane; a draft it does not see is
-    // not read
+    // the drafts the row sees, four at a time, four dimensions a lane; a draft it
+    // does not see is not read
     const uint2 x = *reinterpret_cast<const uint2*>(p.q.at(b, l, t, h * p.G + g) + 4 * lane);
     const float q[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
-    for (uint64_t see = seen(p, b, t); see; see &= see - 1) {
-      const int j = __ffsll((long long)see) - 1;
-      const uint2 k = *reinterpret_cast<const uint2*>(p.kn.at(b, l, j, h) + 4 * lane);
-      const uint2 v = *reinterpret_cast<const uint2*>(p.vn.at(b, l, j, h) + 4 * lane);
-      float z = q[0] * bf16lo(k.x) + q[1] * bf16hi(k.x) + q[2] * bf16lo(k.y) + q[3] * bf16hi(k.y);
+    const uint64_t see = seen(p, b, t);
+    for (int j = 0; j < p.T; j += 4) {
+      if (!(see >> j & 15u)) continue;
+      uint2 k[4], v[4];
+      float z[4];
 #pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
-      z *= p.scale_log2;
-      const float m = fmaxf(M, z);
-      const float c = M == m ? 1.f : exp2f(M - m), f = z == -INFINITY ? 0.f : exp2f(z - m);  // a NaN logit stays one
+      for (int i = 0; i < 4; ++i) {
+        k[i] = v[i] = make_uint2(0u, 0u);
+        if (see >> (j + i) & 1u) {
+          k[i] = *reinterpret_cast<const uint2*>(p.kn.at(b, l, j + i, h) + 4 * lane);
+          v[i] = *reinterpret_cast<const uint2*>(p.vn.at(b, l, j + i, h) + 4 * lane);
+        }
+        z[i] = q[0] * bf16lo(k[i].x) + q[1] * bf16hi(k[i].x) + q[2] * bf16lo(k[i].y) + q[3] * bf16hi(k[i].y);
+      }
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += __shfl_xor_sync(kFull, z[i], o);
+      }
+      float m = M;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[i] = see >> (j + i) & 1u ? z[i] * p.scale_log2 : -INFINITY;
+        m = fmaxf(m, z[i]);
+      }
+      const float back = M == m ? 1.f : exp2f(M - m);
       M = m;
-      L = fmaf(L, c, f);
-      A.x = fmaf(f, bf16lo(v.x), A.x * c);
-      A.y = fmaf(f, bf16hi(v.x), A.y * c);
-      A.z = fmaf(f, bf16lo(v.y), A.z * c);
-      A.w = fmaf(f, bf16hi(v.y), A.w * c);
+      L *= back;
+      A.x *= back;
+      A.y *= back;
+      A.z *= back;
+      A.w *= back;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (!(see >> (j + i) & 1u)) continue;
+        const float f = z[i] == -INFINITY ? 0.f : exp2f(z[i] - m);  // a NaN logit stays one
+        L += f;
+        A.x = fmaf(f, bf16lo(v[i].x), A.x);
+        A.y = fmaf(f, bf16hi(v[i].x), A.y);
+        A.z = fmaf(f, bf16lo(v[i].y), A.z);
+        A.w = fmaf(f, bf16hi(v[i].y), A.w);
+      }
     }
   }
   const float inv = L != 0.f ? 1.f / L : 0.f;  // a NaN sum stays a NaN
@@ -148,10 +191,12 @@ int tree_shape(const certkv_shape* s, int32_t tokens) {
   return CERTKV_OK;
 }
 
-// Query rows of a unit in blocks of at most 256, as equal as they come: up to
-// 128 rows go to the tensor cores as one M = 128 operand, up to 256 as two.
+// Query rows of a unit in blocks, as equal as they come: few rows in blocks of at
+// most 16 (mma.sync), more in blocks of at most 256 (tcgen05: up to 128 rows are
+// one M = 128 operand, up to 256 two).
 void row_blocks(int rows, int* nblk, int* rb) {
-  *nblk = (rows + 255) / 256;
+  const int most = rows <= kSmallMax ? kSmallRows : 256;
+  *nblk = (rows + most - 1) / most;
   *rb = (rows + *nblk - 1) / *nblk;
 }
 
@@ -222,8 +267,9 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   row_blocks(p.rows, &p.nblk, &p.rb);
   const int64_t merge = ((int64_t)p.units * p.rows + 7) / 8;
   if (merge > INT32_MAX) return CERTKV_EINVAL;
-  p.small = p.rows <= kSmallRows;
+  p.small = p.rows <= kSmallMax;
   p.ctas = p.small ? tree_mma_ctas(store->format) : tree_ctas();
+  p.least = p.small ? 4 : p.rb <= 128 ? 2 : 1;  // consumer warps, streams on tiles of their own
   if (p.ctas < 1) return CERTKV_ECUDA;
   if (p.ctas > kTreeMaxCtas) p.ctas = kTreeMaxCtas;
   // a CTA counts its tiles in 32 bits

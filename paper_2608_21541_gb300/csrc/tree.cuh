@@ -10,7 +10,8 @@
 namespace certkv {
 
 constexpr int kTreeTile = 128;  // slots per tile of the tcgen05 kernel: two pages
-constexpr int kSmallRows = 16;  // up to this many query rows: the mma.sync kernel
+constexpr int kSmallRows = 16;  // query rows of a block of the mma.sync kernel
+constexpr int kSmallMax = 32;   // up to this many query rows: that kernel
 // slots per tile of that kernel
 __host__ __device__ constexpr int small_tile(int format) {
   return format == CERTKV_STORE_BF16 ? 32 : CERTKV_STORE_PAGE;
@@ -22,6 +23,7 @@ struct TreeArgs {
   int units, rows;    // B L H, T G query rows per unit
   int nblk, rb;       // row blocks of a unit, rows of a block (the last may have fewer)
   int ctas;           // CTAs the tiles are divided among
+  int least;          // tiles a CTA takes at least: what its warps work on side by side
   int small;          // the mma.sync kernel: the merge takes the drafts
   Rows q, kn, vn, o;  // kn.p null: the drafts have no keys of their own
   const uint64_t* mask;
@@ -44,7 +46,7 @@ __device__ __forceinline__ uint64_t seen(const TreeArgs& p, int b, int t) {
 // Tiles [g0, g1) of CTA c: the global sequence (unit, row block, tile) in equal
 // consecutive shares.
 __device__ __forceinline__ int64_t tiles_per_cta(const TreeArgs& p) {
-  return (p.first[p.units] * p.nblk + p.ctas - 1) / p.ctas;
+  return max((p.first[p.units] * p.nblk + p.ctas - 1) / p.ctas, (int64_t)p.least);
 }
 
 // One (CTA, unit, row block) that meet: their partial results are record

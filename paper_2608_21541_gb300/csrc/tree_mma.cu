@@ -1,5 +1,5 @@
-// tree_mma.cu — the split kernel of tree attention for up to 16 query rows per
-// unit (decode steps and small trees).
+// tree_mma.cu — the split kernel of tree attention for few query rows per unit
+// (decode steps and small trees), in blocks of up to 16.
 //
 // With so few rows the work is reading the store: a 128-row tcgen05 tile would be
 // nearly empty, and expanding 8- and 4-bit codes into its shared-memory operands
@@ -245,13 +245,14 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
   Item it;
   while (items.next(p, &it)) {
     const int bl = it.u / p.H, h = it.u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
+    const int row0 = it.blk * p.rb, rows = min(p.rb, p.rows - row0);  // of the block
     // ---- queries as A fragments
     uint32_t qa[8][4];
     float sl[2];  // per row: scale of its logits (log2 domain)
 #pragma unroll
     for (int rr = 0; rr < 2; ++rr) {
-      const int r = qr + 8 * rr, t = r / p.G, g = r - t * p.G;
-      const uint16_t* row = r < p.rows ? p.q.at(b, l, t, h * p.G + g) : nullptr;
+      const int r = row0 + qr + 8 * rr, t = r / p.G, g = r - t * p.G;
+      const uint16_t* row = qr + 8 * rr < rows ? p.q.at(b, l, t, h * p.G + g) : nullptr;
       if (kQuant) {
         uint32_t w[16], top = 0;
 #pragma unroll
@@ -546,7 +547,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       ls[rr] += __shfl_xor_sync(kFull, ls[rr], 1);
       ls[rr] += __shfl_xor_sync(kFull, ls[rr], 2);
       const int r = qr + 8 * rr;
-      if (r >= p.rows) continue;
+      if (r >= rows) continue;
       if (qc == 0) {
         tl->m[cw][r] = C[rr];
         tl->l[cw][r] = ls[rr];
@@ -554,15 +555,15 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float* a = wacc + (cw * p.rows + r) * kD;
+        float* a = wacc + (cw * rows + r) * kD;
         a[element_of<FMT>(i, qc, 0)] = o[i][2 * rr];
         a[element_of<FMT>(i, qc, 1)] = o[i][2 * rr + 1];
       }
     }
     consumers_sync();
-    const int64_t rec = (int64_t)blockIdx.x + it.u;
+    const int64_t rec = (int64_t)blockIdx.x + (int64_t)it.u * p.nblk + it.blk;
     const bool failed = tl->abort != 0;
-    for (int i = tid; i < p.rows * (kD / 4); i += kConsumers * 32) {
+    for (int i = tid; i < rows * (kD / 4); i += kConsumers * 32) {
       const int r = i / (kD / 4), d = 4 * (i - r * (kD / 4));
       float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -572,7 +573,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       for (int w = 0; w < kConsumers; ++w) {
         if (tl->l[w][r] == 0.f) continue;
         const float f = exp2f(tl->m[w][r] - M), g = f * exp2f(tl->e[w][r]);
-        const float4 a = *reinterpret_cast<const float4*>(wacc + (w * p.rows + r) * kD + d);
+        const float4 a = *reinterpret_cast<const float4*>(wacc + (w * rows + r) * kD + d);
         L = fmaf(tl->l[w][r], f, L);
         A.x = fmaf(a.x, g, A.x);
         A.y = fmaf(a.y, g, A.y);

@@ -608,28 +608,42 @@ struct Issuer {
   __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
     if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(b), phase, &m->abort));
   }
-  // S of stream st with the keys of tile t; `last`: the tile's last S
-  __device__ __forceinline__ void s(int st, uint32_t t, bool last) {
-    const Place<PAIR> k(k_seq(t));
-    wait(&m->full[k.slot], k.phase);
+  // Operand i is in place.  A poll takes hundreds of cycles even of a barrier long
+  // complete (it queues behind the loaders' stores), so the operands of O and of
+  // the S after it are asked for before the wait for P, which is then the only
+  // one between P and both; what is not there yet is waited for when it is due.
+  struct Operand {
+    uint32_t slot, phase;
+    bool there;
+  };
+  __device__ __forceinline__ Operand operand(uint32_t i) {
+    const Place<PAIR> pl(i);
+    return {uni(pl.slot), pl.phase, __all_sync(kFull, tc::mbar_try(bar(&m->full[pl.slot]), pl.phase)) != 0};
+  }
+  __device__ __forceinline__ void due(const Operand& x) {
+    if (!x.there) wait(&m->full[x.slot], x.phase);
+  }
+  // S of stream st with the keys x; `last`: the tile's last S
+  __device__ __forceinline__ void s(int st, const Operand& x, bool last) {
+    const uint32_t slot = x.slot;
+    due(x);
     if (!ok) return;
     um::fence_after();
-    const uint32_t slot = uni(k.slot);
     um::mma_s(uni(tmem + kColS + 128u * st), uni(um::desc_lo(q, 16) + (PAIR ? (uint32_t)st * (kOperand >> 4) : 0u)),
               uni(um::desc_lo(ring, 16) + slot * (kOperand >> 4)), um::kDescHi, um::idesc(kBf16, false));
     um::commit(uni(bar(&m->s_full[st])));
     if (last) um::commit(uni(bar(&m->empty[slot])));
   }
-  // O += P V of stream st with tile t's values; `first`, `fin`: of the item
-  __device__ __forceinline__ void o(int st, uint32_t t, bool last, bool first, bool fin) {
-    const Place<PAIR> v(v_seq(t, n));
+  // O += P V of stream st with the values x; `first`, `fin`: of the item
+  __device__ __forceinline__ void o(int st, const Operand& x, bool last, bool first, bool fin) {
+    const uint32_t slot = x.slot;
+    const uint32_t d = uni(tmem + kColO + 128u * st), a = uni(tmem + kColS + 128u * st);
+    const uint32_t b = uni(um::desc_lo(ring, kHalf) + slot * (kOperand >> 4)), acc = uni(!first);
+    due(x);
     wait(&m->p_full[st], odd >> st & 1u);
     odd ^= 1u << st;
-    wait(&m->full[v.slot], v.phase);
     if (!ok) return;
     um::fence_after();
-    const uint32_t slot = uni(v.slot), d = uni(tmem + kColO + 128u * st), a = uni(tmem + kColS + 128u * st);
-    const uint32_t b = uni(um::desc_lo(ring, kHalf) + slot * (kOperand >> 4)), acc = uni(!first);
     if (kBf16) um::mma_o2(d, a, b, um::kDescHi, um::idesc(true, true), acc);  // weights and remainders
     else um::mma_o(d, a, b, um::kDescHi, um::idesc(false, true), acc);
     if (last) um::commit(uni(bar(&m->empty[slot])));
@@ -641,25 +655,30 @@ struct Issuer {
     Item it;
     uint32_t t0 = 0, item = 0;  // tiles and items before
     while (ok && items.next(p, &it)) {
+      const int c = it.kb - it.ka;
+      Operand k = operand(k_seq(t0));
       wait(&m->q_full, item & 1u);
       ++item;
-      const int c = it.kb - it.ka;
       if (PAIR) {
-        s(0, t0, false);
-        s(1, t0, true);
+        s(0, k, false);
+        s(1, k, true);
         for (int j = 0; ok && j < c; ++j) {
           const bool more = j + 1 < c;
-          o(0, t0 + j, false, j == 0, !more);
-          if (more) s(0, t0 + j + 1, false);
-          o(1, t0 + j, true, j == 0, !more);
-          if (more) s(1, t0 + j + 1, true);
+          const Operand v = operand(v_seq(t0 + j, n));
+          if (more) k = operand(k_seq(t0 + j + 1));
+          o(0, v, false, j == 0, !more);
+          if (more) s(0, k, false);
+          o(1, v, true, j == 0, !more);
+          if (more) s(1, k, true);
         }
       } else {
-        s(0, t0, true);
-        if (c > 1) s(1, t0 + 1, true);
+        s(0, k, true);
+        if (c > 1) s(1, operand(k_seq(t0 + 1)), true);
         for (int i = 0; ok && i < c; ++i) {
-          o(i & 1, t0 + i, true, i < 2, i + 2 >= c);
-          if (i + 2 < c) s(i & 1, t0 + i + 2, true);
+          const Operand v = operand(v_seq(t0 + i, n));
+          if (i + 2 < c) k = operand(k_seq(t0 + i + 2));
+          o(i & 1, v, true, i < 2, i + 2 >= c);
+          if (i + 2 < c) s(i & 1, k, true);
         }
       }
       t0 += c;
