@@ -82,10 +82,8 @@ struct Place {
 };
 constexpr uint32_t kColS = 0, kColO = 256;  // + 128 stream
 
-// A tile's facts, stated by the scout four tiles ahead of its keys.  Slot t % 8 is
-// written again, for tile t + 8, once the place of K(t + 4) is free; that place
-// held V(t) (ring of 5) or K(t + 2) (ring of 4), both released by products issued
-// after P of tile t had been written, so every reader of slot t is done.
+// A tile's facts, stated by the scout ahead of its keys.  Slot t % 8 is written
+// again, for tile t + 8, when the loaders and the softmax warps have given it back.
 constexpr uint32_t kMeta = 8;
 struct alignas(16) Meta {  // its arrays are read and written as float4
   float ks[kTreeTile];  // scale of each slot's key (8- and 4-bit stores)
@@ -102,6 +100,7 @@ struct alignas(16) Meta {  // its arrays are read and written as float4
 struct Misc {
   uint64_t full[5], empty[5];                // places of the ring
   uint64_t stated[kMeta], ready[kMeta];      // scout -> loaders, loaders -> softmax
+  uint64_t back[kMeta];                      // loaders, softmax -> scout
   uint64_t s_full[2], p_full[2], o_full[2], q_full, done;
   uint32_t tmem;
   int abort;
@@ -267,9 +266,9 @@ __device__ __forceinline__ int shift_of(float t) {
 
 // ----------------------------------------------------------------- scout --
 // One warp.  Walks the CTA's tiles, through the page table, ahead of everybody:
-// states the facts of tile t + 4 when it handles K(t), and has the pages of the
-// tile kAhead further brought into L2.  Copies whole bf16 tiles by TMA; for the
-// rest of the operands it only counts along.
+// states their facts and has the pages of the tile kAhead further brought into
+// L2.  Whole bf16 tiles it copies by TMA; of the other operands of a bf16 store it
+// keeps count.
 template <int FMT, bool PAIR>
 struct Scout {
   static constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
@@ -284,6 +283,8 @@ struct Scout {
   Item it;
   int k = 0, count = 0, stored = 0;
   int at = 0, lo = -1, hi = -1;  // table entries of 64 pages from page `at` on
+  int a = -1, b = -1;            // pages of tile k
+  float4 ks, vs;                 // its scales, on their way
 
   __device__ __forceinline__ int entry(int page) const {
     if (page >= p.st.max_pages) return -1;
@@ -294,17 +295,21 @@ struct Scout {
     const int x = __shfl_sync(kFull, lo, (i - at) & 31), y = __shfl_sync(kFull, hi, (i - at) & 31);
     return i - at < 32 ? x : y;
   }
+  // Page i of the segment on its way into L2: each lane one of its arrays.
   __device__ __forceinline__ void prefetch_page(int i) const {
     if (i >= 2 * stored) return;
     const int pg = page(i);
     if (pg < 0) return;
     const int64_t s = (int64_t)pg * kPage;
-    const uint8_t* x = nullptr;
+    const void* x = nullptr;
     uint32_t bytes = kPage * row_bytes(FMT);
-    if (lane == 0) x = p.st.k + s * row_bytes(FMT);
-    if (lane == 1) x = p.st.v + s * row_bytes(FMT);
-    if (FMT == CERTKV_STORE_FP4 && (lane == 2 || lane == 3)) {
-      x = (lane == 2 ? p.st.kg : p.st.vg) + s * kGroups;
+    if (lane < 2) x = (lane ? p.st.v : p.st.k) + s * row_bytes(FMT);
+    if (lane == 2 || lane == 3) {
+      x = (lane & 1 ? p.st.vs : p.st.ks) + s;
+      bytes = kPage * 4;
+    }
+    if (FMT == CERTKV_STORE_FP4 && (lane == 4 || lane == 5)) {
+      x = (lane & 1 ? p.st.vg : p.st.kg) + s * kGroups;
       bytes = kPage * kGroups;
     }
     if (x)
@@ -313,7 +318,7 @@ struct Scout {
                    : "memory");
   }
   // Scales of slots 4 lane .. 4 lane + 3 of a tile (`none` where there is no slot).
-  __device__ __forceinline__ float4 scales(const float* s, int a, int b, int live, float none) const {
+  __device__ __forceinline__ float4 scales(const float* s, int live, float none) const {
     const int pg = lane < 16 ? a : b, n = live - 4 * lane;
     float4 x = make_float4(none, none, none, none);
     if (pg >= 0)
@@ -323,6 +328,24 @@ struct Scout {
     if (n < 3) x.z = none;
     if (n < 4) x.w = none;
     return x;
+  }
+  // Pages and scales of tile k, asked for a tile before they are stated.
+  __device__ __forceinline__ void fetch() {
+    if (k >= min(stored, it.kb)) return;
+    if (2 * k >= at + 32) {
+      at += 32;
+      lo = hi;
+      hi = entry(at + 32 + lane);
+    }
+    a = page(2 * k);
+    b = page(2 * k + 1);
+    if (kQuant) {
+      const int live = count - k * kTreeTile;
+      ks = scales(p.st.ks, live, 1.f);  // finite where there is no slot
+      vs = scales(p.st.vs, live, 0.f);
+      prefetch_page(2 * (k + kAhead));
+      prefetch_page(2 * (k + kAhead) + 1);
+    }
   }
   // State tile t, the next of the walk.
   __device__ __forceinline__ void state(uint32_t t) {
@@ -336,18 +359,14 @@ struct Scout {
       hi = entry(at + 32 + lane);
       if (kQuant)
         for (int i = 2; i < 2 * kAhead; ++i) prefetch_page(at + i);
-    } else if (2 * k >= at + 32) {
-      at += 32;
-      lo = hi;
-      hi = entry(at + 32 + lane);
+      fetch();
     }
+    if (ok && t >= kMeta) ok = tc::mbar_wait(bar(&m->back[t % kMeta]), (t / kMeta - 1) & 1u, &m->abort);
     Meta& mt = m->meta[t % kMeta];
     if (k < stored) {
-      const int live = count - k * kTreeTile, a = page(2 * k), b = page(2 * k + 1);
+      const int live = count - k * kTreeTile;
       int shift = 0;
       if (kQuant) {
-        const float4 ks = scales(p.st.ks, a, b, live, 1.f);  // finite where there is no slot
-        const float4 vs = scales(p.st.vs, a, b, live, 0.f);
         // from the tile's largest row maximum, a NaN left out
         float x = fmaxf(fmaxf(vs.x, vs.y), fmaxf(vs.z, vs.w));
 #pragma unroll
@@ -357,8 +376,6 @@ struct Scout {
         *reinterpret_cast<float4*>(&mt.ks[4 * lane]) = ks;
         *reinterpret_cast<float4*>(&mt.vf[4 * lane]) =
             make_float4(vs.x * down, vs.y * down, vs.z * down, vs.w * down);
-        prefetch_page(2 * (k + kAhead));
-        prefetch_page(2 * (k + kAhead) + 1);
       }
       if (lane < 4) {
         const int c = min(max(live - 32 * lane, 0), 32);
@@ -384,15 +401,16 @@ struct Scout {
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(bar(&m->stated[t % kMeta]));
     ++k;
+    fetch();
   }
-  // The scout's arrival for operand i, tile t: a whole bf16 tile by four bulk
-  // copies, two pages x two 64-element halves.
+  // Operand i, tile t, of a bf16 store: a whole tile by four bulk copies, two
+  // pages x two 64-element halves; else the scout's arrival alone.
   __device__ __forceinline__ bool operand(const CUtensorMap* map, uint32_t i, uint32_t t) {
     const Place<PAIR> pl(i);
     if (ok) ok = tc::mbar_wait(bar(&m->empty[pl.slot]), pl.phase ^ 1u, &m->abort);
     const Meta& mt = m->meta[t % kMeta];
     const uint32_t full = bar(&m->full[pl.slot]), to = ring + pl.slot * kOperand;
-    const bool copied = !kQuant && ok && mt.whole;
+    const bool copied = ok && mt.whole;
     if (lane == 0) {
       if (copied) {
         const int ya = mt.a * kPage, yb = mt.b * kPage;
@@ -405,24 +423,29 @@ struct Scout {
         tc::mbar_arrive(full);
       }
     }
+    __syncwarp();
     return copied;
   }
   __device__ __forceinline__ void run(uint32_t n) {
     it.kb = 0;
+    if (kQuant) {
+      for (uint32_t t = 0; t < n; ++t) state(t);
+      return;
+    }
     uint32_t stated = 0, copies = 0;  // places whose last operand came by bulk copy
     for (; stated < min(n, 4u); ++stated) state(stated);
     for (uint32_t t = 0; t <= n; ++t) {  // K(t), V(t - 1)
       if (t < n) {
         const uint32_t bit = 1u << Place<PAIR>(k_seq(t)).slot;
         copies = operand(tmK, k_seq(t), t) ? copies | bit : copies & ~bit;
-        if (stated < n) state(stated++);
       }
       if (t > 0) {
         const uint32_t bit = 1u << Place<PAIR>(v_seq(t - 1, n)).slot;
         copies = operand(tmV, v_seq(t - 1, n), t - 1) ? copies | bit : copies & ~bit;
       }
+      if (t < n && stated < n) state(stated++);
     }
-    if (!kQuant && lane == 0) {  // bulk copies land before the CTA may exit
+    if (lane == 0) {  // bulk copies land before the CTA may exit
       volatile int dummy = 0;
       for (uint32_t i = 2 * n > Plan<PAIR>::kRing ? 2 * n - Plan<PAIR>::kRing : 0; i < 2 * n; ++i) {
         const Place<PAIR> pl(i);
@@ -550,7 +573,10 @@ struct Loader {
     if (!VALUE && tid == 0) tc::mbar_arrive(bar(&m->ready[t % kMeta]));
     if (wrote) um::fence_async();
     __syncwarp();
-    if ((tid & 31) == 0) tc::mbar_arrive(bar(&m->full[pl.slot]));
+    if ((tid & 31) == 0) {
+      tc::mbar_arrive(bar(&m->full[pl.slot]));
+      if (VALUE) tc::mbar_arrive(bar(&m->back[t % kMeta]));
+    }
   }
   // Quantised codes travel through registers: those of the next keys and of the
   // next values are loaded while the ones before are expanded.
@@ -950,7 +976,10 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
       um::wait_st();
       um::fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bar(&m->p_full[s]));
+      if (lane == 0) {
+        tc::mbar_arrive(bar(&m->p_full[s]));
+        tc::mbar_arrive(bar(&m->back[t % kMeta]));
+      }
     }
     // ---- the item's result: one record per row
     if (ok && busy && steps > 0) {
@@ -1031,7 +1060,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < Plan<PAIR>::kRing; ++i) {
-      tc::mbar_init(bar(&m->full[i]), kLoadWarps + 1);  // and the scout
+      tc::mbar_init(bar(&m->full[i]), kLoadWarps + (FMT == CERTKV_STORE_BF16));  // and the scout
       tc::mbar_init(bar(&m->empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -1043,6 +1072,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     for (uint32_t i = 0; i < kMeta; ++i) {
       tc::mbar_init(bar(&m->stated[i]), 1);
       tc::mbar_init(bar(&m->ready[i]), 1);
+      tc::mbar_init(bar(&m->back[i]), kLoadWarps + (p.rb + 31) / 32);  // a tile's loaders and softmax warps
     }
     tc::mbar_init(bar(&m->q_full), kSoftWarps);
     tc::mbar_init(bar(&m->done), 1);
