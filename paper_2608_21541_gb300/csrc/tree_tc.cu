@@ -19,8 +19,8 @@
 //                tile and bf16 tiles that are not whole;
 //   warp 16      tensor-memory allocation, and issues the MMAs;
 //   warp 17      scout: walks the page table ahead of the loaders, states each
-//                tile's facts, copies whole bf16 tiles by TMA and has the pages
-//                of later tiles brought into L2.
+//                tile's facts and has the pages of later tiles brought into L2;
+//   warps 17, 18 whole bf16 tiles: keys and values by TMA.
 //
 // Precision.  bf16 store: bf16 products, and a weight enters P V as a bf16 part
 // plus the bf16 rounding of its remainder (2^-16).  8- and 4-bit stores: codes
@@ -47,28 +47,31 @@
 namespace certkv {
 namespace {
 
-constexpr int kSoftWarps = 8, kLoadWarps = 8;
+constexpr int kSoftWarps = 8;
+constexpr int kGroupWarps = 4, kLoadGroups = 2, kLoadWarps = kGroupWarps * kLoadGroups;
 constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
-constexpr int kLoaders = kLoadWarps * 32;
-constexpr int kPieces = 4;  // (slot, 16-element) pieces of an operand per loader thread
-static_assert(kLoaders * kPieces == 128 * 8, "the loaders cover an operand");
+constexpr int kPieces = 8;  // (slot, 16-element) pieces of an operand per loader thread
+static_assert(kGroupWarps * 32 * kPieces == 128 * 8, "a group of loaders covers an operand");
 // Registers a thread: the launch gives 96 (640 threads), which the roles share
 // out among themselves.  A spill costs more here than elsewhere: next to 200 KB
 // of shared memory the L1 holds hardly any of it.
 constexpr int kSoftRegs = 112, kLoadRegs = 96, kIssueRegs = 56;
-static_assert(kSoftWarps * 32 * kSoftRegs + kLoaders * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
+static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
               "a larger split would wait for registers for ever");
 constexpr int kHalf = 128 * 128;     // bytes of 128 rows x 64 16-bit elements
 constexpr int kOperand = 2 * kHalf;  // 128 rows x 128 elements
 constexpr int kAhead = 6;            // tiles the L2 prefetch runs ahead
 // Shared memory: the query blocks (two when both streams hold rows of their
-// own), then a ring of operands, then Misc.
+// own), then a ring of operands, then Misc.  Operand i is place i % 4.
 template <bool PAIR>
 struct Plan {
-  static constexpr int kRing = PAIR ? 4 : 5;
+  static constexpr int kRing = 4;
   static constexpr int kRingOff = (PAIR ? 2 : 1) * kOperand;
   static constexpr int kMiscOff = kRingOff + kRing * kOperand;
 };
+// A waiter for a place's release must itself have waited for the release before
+// it (a parity tells only neighbouring phases apart): a place belongs to one group.
+static_assert(Plan<true>::kRing % kLoadGroups == 0 && Plan<false>::kRing % kLoadGroups == 0, "one group per place");
 // The operands of the n tiles of a CTA pass through the ring in the order K(0),
 // then K(t + 1), V(t) for t = 0 .., near the order the MMAs take them in.
 __device__ __forceinline__ uint32_t k_seq(uint32_t t) { return t == 0 ? 0u : 2u * t - 1u; }
@@ -98,13 +101,14 @@ struct alignas(16) Meta {  // its arrays are read and written as float4
 };
 
 struct Misc {
-  uint64_t full[5], empty[5];                // places of the ring
+  uint64_t full[4], empty[4];                // places of the ring
   uint64_t stated[kMeta], ready[kMeta];      // scout -> loaders, loaders -> softmax
   uint64_t back[kMeta];                      // loaders, softmax -> scout
   uint64_t s_full[2], p_full[2], o_full[2], q_full, done;
+  uint64_t group[kLoadGroups];               // barriers of the loader groups
   uint32_t tmem;
   int abort;
-  unsigned long long odd;
+  unsigned long long odd[kLoadGroups];
   float red[kLoadWarps];
   float qs[256];                   // per row: scale of its f16 queries
   float cm[128], l[128], sh[128];  // stream 1's reference, sum and shift
@@ -119,11 +123,8 @@ static_assert(smem_bytes<true>() <= 232448 && smem_bytes<false>() <= 232448,
               "over the 227 KB of shared memory a CTA can have");
 
 __device__ __forceinline__ uint32_t bar(const uint64_t* b) { return tc::saddr(b); }
-__device__ __forceinline__ void loaders_sync() {
-  asm volatile("bar.sync 1, %0;" ::"n"(kLoaders) : "memory");
-}
 __device__ __forceinline__ void softmax_sync() {
-  asm volatile("bar.sync 2, %0;" ::"n"(kSoftWarps * 32) : "memory");
+  asm volatile("bar.sync 1, %0;" ::"n"(kSoftWarps * 32) : "memory");
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
@@ -141,7 +142,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // |e| < 127
 
 // A loader thread's part of an operand: elements 16 sub .. 16 sub + 15 of the
-// rows grp, grp + 32, + 64 and + 96.  A quarter warp holds the same half of two
+// rows grp, grp + 16 .. grp + 112.  A quarter warp holds the same half of two
 // neighbouring rows, which the swizzle puts into different banks.
 struct Piece {
   int grp, sub;
@@ -155,10 +156,10 @@ struct Piece {
     at0 = r + (uint32_t)((c ^ x) << 4);
     at1 = r + (uint32_t)(((c + 1) ^ x) << 4);
   }
-  // row grp + 32 q of the operand at `to`
+  // row grp + 16 q of the operand at `to`
   __device__ __forceinline__ void put(uint32_t to, int q, const uint32_t (&w)[8]) const {
-    sts128(to + at0 + (uint32_t)(q * 32 * 128), w[0], w[1], w[2], w[3]);
-    sts128(to + at1 + (uint32_t)(q * 32 * 128), w[4], w[5], w[6], w[7]);
+    sts128(to + at0 + (uint32_t)(q * 16 * 128), w[0], w[1], w[2], w[3]);
+    sts128(to + at1 + (uint32_t)(q * 16 * 128), w[4], w[5], w[6], w[7]);
   }
   // the eight lanes of a row
   __device__ __forceinline__ static uint32_t row_max(uint32_t x) {
@@ -209,8 +210,8 @@ struct Raw {
                                        const uint8_t* group) {
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
-      const int page = q < 2 ? a : b, row = pc.grp + 32 * (q & 1);
-      const bool on = page >= 0 && pc.grp + 32 * q < live;
+      const int page = q < 4 ? a : b, row = pc.grp + 16 * (q & 3);
+      const bool on = page >= 0 && pc.grp + 16 * q < live;
       const int64_t at = (int64_t)page * kPage + row;
 #pragma unroll
       for (int j = 0; j < kWords; ++j) w[q][j] = 0u;
@@ -361,7 +362,10 @@ struct Scout {
         for (int i = 2; i < 2 * kAhead; ++i) prefetch_page(at + i);
       fetch();
     }
-    if (ok && t >= kMeta) ok = tc::mbar_wait(bar(&m->back[t % kMeta]), (t / kMeta - 1) & 1u, &m->abort);
+    // a bf16 store's walk is paced by its K places: that of K(t - 4), free by now,
+    // held K(t - 6), released by a product issued after P of tile t - 8 was written
+    if (kQuant && ok && t >= kMeta)
+      ok = tc::mbar_wait(bar(&m->back[t % kMeta]), (t / kMeta - 1) & 1u, &m->abort);
     Meta& mt = m->meta[t % kMeta];
     if (k < stored) {
       const int live = count - k * kTreeTile;
@@ -426,36 +430,47 @@ struct Scout {
     __syncwarp();
     return copied;
   }
+  // Bulk copies of the last operands land before the CTA may exit.
+  __device__ __forceinline__ void drain(uint32_t n, uint32_t copies) const {
+    if (lane != 0) return;
+    volatile int dummy = 0;
+    for (uint32_t i = 2 * n > Plan<PAIR>::kRing ? 2 * n - Plan<PAIR>::kRing : 0; i < 2 * n; ++i) {
+      const Place<PAIR> pl(i);
+      if (copies >> pl.slot & 1u) tc::mbar_wait(bar(&m->full[pl.slot]), pl.phase, &dummy);
+    }
+  }
   __device__ __forceinline__ void run(uint32_t n) {
     it.kb = 0;
     if (kQuant) {
       for (uint32_t t = 0; t < n; ++t) state(t);
       return;
     }
-    uint32_t stated = 0, copies = 0;  // places whose last operand came by bulk copy
+    uint32_t stated = 0, copies = 0;  // places whose last operand this warp copied
     for (; stated < min(n, 4u); ++stated) state(stated);
-    for (uint32_t t = 0; t <= n; ++t) {  // K(t), V(t - 1)
-      if (t < n) {
-        const uint32_t bit = 1u << Place<PAIR>(k_seq(t)).slot;
-        copies = operand(tmK, k_seq(t), t) ? copies | bit : copies & ~bit;
-      }
-      if (t > 0) {
-        const uint32_t bit = 1u << Place<PAIR>(v_seq(t - 1, n)).slot;
-        copies = operand(tmV, v_seq(t - 1, n), t - 1) ? copies | bit : copies & ~bit;
-      }
-      if (t < n && stated < n) state(stated++);
+    for (uint32_t t = 0; t < n; ++t) {
+      const uint32_t bit = 1u << Place<PAIR>(k_seq(t)).slot;
+      copies = operand(tmK, k_seq(t), t) ? copies | bit : copies & ~bit;
+      if (stated < n) state(stated++);
     }
-    if (lane == 0) {  // bulk copies land before the CTA may exit
-      volatile int dummy = 0;
-      for (uint32_t i = 2 * n > Plan<PAIR>::kRing ? 2 * n - Plan<PAIR>::kRing : 0; i < 2 * n; ++i) {
-        const Place<PAIR> pl(i);
-        if (copies >> pl.slot & 1u) tc::mbar_wait(bar(&m->full[pl.slot]), pl.phase, &dummy);
-      }
+    drain(n, copies);
+  }
+  // The values of a bf16 store, by a warp of their own: a poll takes hundreds of
+  // cycles, and one warp's polls for keys, facts and values add up to a tile's time.
+  __device__ __forceinline__ void run_values(uint32_t n) {
+    uint32_t copies = 0;
+    for (uint32_t t = 0; t < n; ++t) {
+      const uint32_t bit = 1u << Place<PAIR>(v_seq(t, n)).slot;
+      if (ok) ok = tc::mbar_wait(bar(&m->stated[t % kMeta]), (t / kMeta) & 1u, &m->abort);
+      copies = operand(tmV, v_seq(t, n), t) ? copies | bit : copies & ~bit;
     }
+    drain(n, copies);
   }
 };
 
 // --------------------------------------------------------------- loaders --
+// Two groups of four warps take the operands in turn, so that the latencies of one
+// operand (its place, its codes' way from L2, the fence before the MMAs)
+// pass under the work on the others.
 template <int FMT, bool PAIR>
 struct Loader {
   static constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
@@ -463,10 +478,10 @@ struct Loader {
   const TreeArgs& p;
   Misc* m;
   uint32_t ring;
-  int tid;
+  int group, tid;  // thread of the group
   Piece pc;
-  bool ok = true;  // false after a wait gave up; the walk over the tiles goes on (the
-                   // loaders' barriers must stay in step)
+  bool ok = true;         // false after a wait gave up
+  uint32_t syncs = 0;     // of the group so far
 
   // NaN and infinities of sixteen bf16 to 0 (in the product they would reach every
   // row, seen or not; the merge adds them to the rows that see their draft).
@@ -485,24 +500,31 @@ struct Loader {
     }
     return odd;
   }
-  __device__ __forceinline__ void stated(uint32_t t) {
-    if (ok) ok = tc::mbar_wait(bar(&m->stated[t % kMeta]), (t / kMeta) & 1u, &m->abort);
+  __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
+    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(b), phase, &m->abort));
+  }
+  // A barrier of the group whose wait is bounded like every other.
+  __device__ __forceinline__ void group_sync() {
+    __syncwarp();
+    if ((tid & 31) == 0) tc::mbar_arrive(bar(&m->group[group]));
+    wait(&m->group[group], syncs & 1u);
+    ++syncs;
   }
   // Keys of the drafts' own tile and the facts that follow from its rows.
   __device__ __forceinline__ void draft_keys(uint32_t to, Meta& mt) {
     const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
     uint32_t top = 0;
-    if (tid == 0) m->odd = 0ull;
-    loaders_sync();
+    if (tid == 0) m->odd[group] = 0ull;
+    group_sync();
 #pragma unroll 1
     for (int q = 0; q < kPieces; ++q) {
-      const int s = pc.grp + 32 * q;
+      const int s = pc.grp + 16 * q;
       uint32_t k[8] = {}, v[8] = {};
       if (s < p.T) {
         load32g(p.kn.at(b, l, s, h) + pc.sub * 16, k);
         load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
       }
-      if (finite_only(v)) atomicOr(&m->odd, 1ull << (s & 63));
+      if (finite_only(v)) atomicOr(&m->odd[group], 1ull << (s & 63));
       top = max(top, top16(v));
       if (kQuant) {
         const int e = min(max(exponent(__uint_as_float(Piece::row_max(top16(k)))), -120), 120);
@@ -513,22 +535,21 @@ struct Loader {
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
-    if ((tid & 31) == 0) m->red[tid >> 5] = __uint_as_float(top);
-    loaders_sync();
+    if ((tid & 31) == 0) m->red[group * kGroupWarps + (tid >> 5)] = __uint_as_float(top);
+    group_sync();
     if (tid == 0) {
       float x = 0.f;
 #pragma unroll
-      for (int q = 0; q < kLoadWarps; ++q) x = fmaxf(x, m->red[q]);
+      for (int q = 0; q < kGroupWarps; ++q) x = fmaxf(x, m->red[group * kGroupWarps + q]);
       mt.shift = kQuant ? shift_of(x) : 0;
-      if (mt.first_block) p.odd[u] = m->odd;
+      if (mt.first_block) p.odd[u] = m->odd[group];
     }
-    loaders_sync();
   }
   __device__ __forceinline__ void draft_values(uint32_t to, const Meta& mt) {
     const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
 #pragma unroll 1
     for (int q = 0; q < kPieces; ++q) {
-      const int s = pc.grp + 32 * q;
+      const int s = pc.grp + 16 * q;
       uint32_t v[8] = {};
       if (s < p.T) {
         load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
@@ -542,71 +563,62 @@ struct Loader {
   __device__ __forceinline__ void ragged(uint32_t to, const uint8_t* rows, const Meta& mt) {
 #pragma unroll 1
     for (int q = 0; q < kPieces; ++q) {
-      const int pg = q < 2 ? mt.a : mt.b;
+      const int pg = q < 4 ? mt.a : mt.b;
       uint32_t w[8] = {};
-      if (pg >= 0 && pc.grp + 32 * q < mt.count)
-        load32g(rows + ((int64_t)pg * kPage + pc.grp + 32 * (q & 1)) * 256 + pc.sub * 32, w);
+      if (pg >= 0 && pc.grp + 16 * q < mt.count)
+        load32g(rows + ((int64_t)pg * kPage + pc.grp + 16 * (q & 3)) * 256 + pc.sub * 32, w);
       pc.put(to, q, w);
     }
   }
-  template <bool VALUE>
-  __device__ __forceinline__ void operand(uint32_t i, uint32_t t, Raw<kRawFmt>& raw) {
-    const Place<PAIR> pl(i);
-    if (ok) ok = tc::mbar_wait(bar(&m->empty[pl.slot]), pl.phase ^ 1u, &m->abort);
-    const uint32_t to = ring + pl.slot * kOperand;
-    Meta& mt = m->meta[t % kMeta];
-    bool wrote = true;
-    if (mt.drafts) {
-      if (VALUE) draft_values(to, mt);
-      else draft_keys(to, mt);
-    } else if (kQuant) {
-#pragma unroll
-      for (int q = 0; q < kPieces; ++q) {
-        uint32_t w[8];
-        expand<kRawFmt, VALUE>(raw, q, VALUE ? mt.vf[pc.grp + 32 * q] : 0.f, w);
-        pc.put(to, q, w);
-      }
-    } else {
-      wrote = !mt.whole;
-      if (wrote) ragged(to, VALUE ? p.st.v : p.st.k, mt);
-    }
-    if (!VALUE && tid == 0) tc::mbar_arrive(bar(&m->ready[t % kMeta]));
-    if (wrote) um::fence_async();
-    __syncwarp();
-    if ((tid & 31) == 0) {
-      tc::mbar_arrive(bar(&m->full[pl.slot]));
-      if (VALUE) tc::mbar_arrive(bar(&m->back[t % kMeta]));
-    }
-  }
-  // Quantised codes travel through registers: those of the next keys and of the
-  // next values are loaded while the ones before are expanded.
   __device__ __forceinline__ void run(uint32_t n) {
-    Raw<kRawFmt> kr, vr;
-    stated(0);
-    if (kQuant) {
-      const Meta& mt = m->meta[0];
-      kr.load(pc, mt.a, mt.b, mt.count, p.st.k, p.st.kg);
-      vr.load(pc, mt.a, mt.b, mt.count, p.st.v, p.st.vg);
-    }
 #pragma unroll 1
-    for (uint32_t t = 0; t <= n; ++t) {  // K(t), V(t - 1)
-      if (t < n) {
-        operand<false>(k_seq(t), t, kr);
-        if (t + 1 < n) {
-          stated(t + 1);
-          if (kQuant) {
-            const Meta& mt = m->meta[(t + 1) % kMeta];
-            kr.load(pc, mt.a, mt.b, mt.count, p.st.k, p.st.kg);
+    for (uint32_t i = group; i < 2 * n; i += kLoadGroups) {
+      // operand i: keys of tile 0, (i + 1) / 2, .. or values of tile i / 2 - 1, .., n - 1
+      const bool value = i == 2 * n - 1 || (i > 0 && (i & 1) == 0);
+      const uint32_t t = i == 2 * n - 1 ? n - 1 : value ? i / 2 - 1 : (i + 1) / 2;
+      Meta& mt = m->meta[t % kMeta];
+      wait(&m->stated[t % kMeta], (t / kMeta) & 1u);
+      const bool own = mt.drafts;
+      Raw<kRawFmt> raw;
+      if (kQuant && !own)
+        raw.load(pc, mt.a, mt.b, mt.count, value ? p.st.v : p.st.k, value ? p.st.vg : p.st.kg);
+      // values of the drafts: their exponent comes from the group that had the keys
+      if (own && value) wait(&m->ready[t % kMeta], (t / kMeta) & 1u);
+      const Place<PAIR> pl(i);
+      wait(&m->empty[pl.slot], pl.phase ^ 1u);
+      if (!ok) break;
+      const uint32_t to = ring + pl.slot * kOperand;
+      bool wrote = true;
+      if (own) {
+        if (value) draft_values(to, mt);
+        else draft_keys(to, mt);
+      } else if (kQuant) {
+        if (value) {
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q) {
+            uint32_t w[8];
+            expand<kRawFmt, true>(raw, q, mt.vf[pc.grp + 16 * q], w);
+            pc.put(to, q, w);
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q) {
+            uint32_t w[8];
+            expand<kRawFmt, false>(raw, q, 0.f, w);
+            pc.put(to, q, w);
           }
         }
+      } else {
+        wrote = !mt.whole;
+        if (wrote) ragged(to, value ? p.st.v : p.st.k, mt);
       }
-      if (t > 0) {
-        operand<true>(v_seq(t - 1, n), t - 1, vr);
-        if (kQuant && t < n) {
-          const Meta& mt = m->meta[t % kMeta];
-          vr.load(pc, mt.a, mt.b, mt.count, p.st.v, p.st.vg);
-        }
+      if (wrote) um::fence_async();
+      __syncwarp();
+      if ((tid & 31) == 0) {
+        tc::mbar_arrive(bar(&m->full[pl.slot]));
+        if (value) tc::mbar_arrive(bar(&m->back[t % kMeta]));
       }
+      if (!value && tid == 0) tc::mbar_arrive(bar(&m->ready[t % kMeta]));
     }
   }
 };
@@ -1060,7 +1072,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < Plan<PAIR>::kRing; ++i) {
-      tc::mbar_init(bar(&m->full[i]), kLoadWarps + (FMT == CERTKV_STORE_BF16));  // and the scout
+      tc::mbar_init(bar(&m->full[i]), kGroupWarps + (FMT == CERTKV_STORE_BF16));  // a group, and the scout
       tc::mbar_init(bar(&m->empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -1072,8 +1084,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     for (uint32_t i = 0; i < kMeta; ++i) {
       tc::mbar_init(bar(&m->stated[i]), 1);
       tc::mbar_init(bar(&m->ready[i]), 1);
-      tc::mbar_init(bar(&m->back[i]), kLoadWarps + (p.rb + 31) / 32);  // a tile's loaders and softmax warps
+      tc::mbar_init(bar(&m->back[i]), kGroupWarps + (p.rb + 31) / 32);  // the values' group, the softmax warps
     }
+    for (int i = 0; i < kLoadGroups; ++i) tc::mbar_init(bar(&m->group[i]), kGroupWarps);
     tc::mbar_init(bar(&m->q_full), kSoftWarps);
     tc::mbar_init(bar(&m->done), 1);
     m->abort = 0;
@@ -1096,7 +1109,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   } else if (warp < kSoftWarps + kLoadWarps) {
     regs_down<kLoadRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
-    Loader<FMT, PAIR> ld{p, m, base + Plan<PAIR>::kRingOff, tid, Piece(tid)};
+    const int group = tid / (kGroupWarps * 32), gt = tid % (kGroupWarps * 32);
+    Loader<FMT, PAIR> ld{p, m, base + Plan<PAIR>::kRingOff, group, gt, Piece(gt)};
     ld.run(n);
   } else {
     regs_down<kIssueRegs>();
@@ -1106,6 +1120,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     } else if (warp == kSoftWarps + kLoadWarps + 1) {
       Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
       sc.run(n);
+    } else if (FMT == CERTKV_STORE_BF16 && warp == kSoftWarps + kLoadWarps + 2) {
+      Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
+      sc.run_values(n);
     }
     __syncwarp();
   }
