@@ -50,8 +50,8 @@ namespace {
 constexpr int kSoftWarps = 8;
 constexpr int kGroupWarps = 4, kLoadGroups = 2, kLoadWarps = kGroupWarps * kLoadGroups;
 constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
-constexpr int kPieces = 8;  // (slot, 16-element) pieces of an operand per loader thread
-static_assert(kGroupWarps * 32 * kPieces == 128 * 8, "a group of loaders covers an operand");
+// A loader thread's (slot, 16-element) pieces of an operand, kStep slots apart.
+constexpr int kPieces = 128 * 8 / (kGroupWarps * 32), kStep = 128 / kPieces;
 // Registers a thread: the launch gives 96 (640 threads), which the roles share
 // out among themselves.  A spill costs more here than elsewhere: next to 200 KB
 // of shared memory the L1 holds hardly any of it.
@@ -142,7 +142,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // |e| < 127
 
 // A loader thread's part of an operand: elements 16 sub .. 16 sub + 15 of the
-// rows grp, grp + 16 .. grp + 112.  A quarter warp holds the same half of two
+// rows grp, grp + kStep ..  A quarter warp holds the same half of two
 // neighbouring rows, which the swizzle puts into different banks.
 struct Piece {
   int grp, sub;
@@ -156,10 +156,10 @@ struct Piece {
     at0 = r + (uint32_t)((c ^ x) << 4);
     at1 = r + (uint32_t)(((c + 1) ^ x) << 4);
   }
-  // row grp + 16 q of the operand at `to`
+  // row grp + kStep q of the operand at `to`
   __device__ __forceinline__ void put(uint32_t to, int q, const uint32_t (&w)[8]) const {
-    sts128(to + at0 + (uint32_t)(q * 16 * 128), w[0], w[1], w[2], w[3]);
-    sts128(to + at1 + (uint32_t)(q * 16 * 128), w[4], w[5], w[6], w[7]);
+    sts128(to + at0 + (uint32_t)(q * kStep * 128), w[0], w[1], w[2], w[3]);
+    sts128(to + at1 + (uint32_t)(q * kStep * 128), w[4], w[5], w[6], w[7]);
   }
   // the eight lanes of a row
   __device__ __forceinline__ static uint32_t row_max(uint32_t x) {
@@ -210,8 +210,8 @@ struct Raw {
                                        const uint8_t* group) {
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
-      const int page = q < 4 ? a : b, row = pc.grp + 16 * (q & 3);
-      const bool on = page >= 0 && pc.grp + 16 * q < live;
+      const int page = q < kPieces / 2 ? a : b, row = pc.grp + kStep * (q % (kPieces / 2));
+      const bool on = page >= 0 && pc.grp + kStep * q < live;
       const int64_t at = (int64_t)page * kPage + row;
 #pragma unroll
       for (int j = 0; j < kWords; ++j) w[q][j] = 0u;
@@ -518,7 +518,7 @@ struct Loader {
     group_sync();
 #pragma unroll 1
     for (int q = 0; q < kPieces; ++q) {
-      const int s = pc.grp + 16 * q;
+      const int s = pc.grp + kStep * q;
       uint32_t k[8] = {}, v[8] = {};
       if (s < p.T) {
         load32g(p.kn.at(b, l, s, h) + pc.sub * 16, k);
@@ -549,7 +549,7 @@ struct Loader {
     const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
 #pragma unroll 1
     for (int q = 0; q < kPieces; ++q) {
-      const int s = pc.grp + 16 * q;
+      const int s = pc.grp + kStep * q;
       uint32_t v[8] = {};
       if (s < p.T) {
         load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
@@ -563,10 +563,10 @@ struct Loader {
   __device__ __forceinline__ void ragged(uint32_t to, const uint8_t* rows, const Meta& mt) {
 #pragma unroll 1
     for (int q = 0; q < kPieces; ++q) {
-      const int pg = q < 4 ? mt.a : mt.b;
+      const int pg = q < kPieces / 2 ? mt.a : mt.b;
       uint32_t w[8] = {};
-      if (pg >= 0 && pc.grp + 16 * q < mt.count)
-        load32g(rows + ((int64_t)pg * kPage + pc.grp + 16 * (q & 3)) * 256 + pc.sub * 32, w);
+      if (pg >= 0 && pc.grp + kStep * q < mt.count)
+        load32g(rows + ((int64_t)pg * kPage + pc.grp + kStep * (q % (kPieces / 2))) * 256 + pc.sub * 32, w);
       pc.put(to, q, w);
     }
   }
@@ -597,7 +597,7 @@ struct Loader {
 #pragma unroll
           for (int q = 0; q < kPieces; ++q) {
             uint32_t w[8];
-            expand<kRawFmt, true>(raw, q, mt.vf[pc.grp + 16 * q], w);
+            expand<kRawFmt, true>(raw, q, mt.vf[pc.grp + kStep * q], w);
             pc.put(to, q, w);
           }
         } else {
@@ -656,7 +656,7 @@ struct Issuer {
   };
   __device__ __forceinline__ Operand operand(uint32_t i) {
     const Place<PAIR> pl(i);
-    return {uni(pl.slot), pl.phase, __all_sync(kFull, tc::mbar_try(bar(&m->full[pl.slot]), pl.phase)) != 0};
+    return {uni(pl.slot), pl.phase, __all_sync(kFull, tc::mbar_test(bar(&m->full[pl.slot]), pl.phase)) != 0};
   }
   __device__ __forceinline__ void due(const Operand& x) {
     if (!x.there) wait(&m->full[x.slot], x.phase);
