@@ -18,9 +18,10 @@
 //                in the MMAs' swizzled layout; for every store the drafts' own
 //                tile and bf16 tiles that are not whole;
 //   warp 16      tensor-memory allocation, and issues the MMAs;
-//   warp 17      scout: walks the page table ahead of the loaders, states each
-//                tile's facts and has the pages of later tiles brought into L2;
-//   warps 17, 18 whole bf16 tiles: keys and values by TMA.
+//   warp 17      scout: walks the page table ahead of the loaders and states each
+//                tile's facts;
+//   warps 17, 18 whole bf16 tiles: keys and values by TMA;
+//   warp 18      8- and 4-bit stores: has the pages of later tiles brought into L2.
 //
 // Precision.  bf16 store: bf16 products, and a weight enters P V as a bf16 part
 // plus the bf16 rounding of its remainder (2^-16).  8- and 4-bit stores: codes
@@ -266,10 +267,10 @@ __device__ __forceinline__ int shift_of(float t) {
 }
 
 // ----------------------------------------------------------------- scout --
-// One warp.  Walks the CTA's tiles, through the page table, ahead of everybody:
-// states their facts and has the pages of the tile kAhead further brought into
-// L2.  Whole bf16 tiles it copies by TMA; of the other operands of a bf16 store it
-// keeps count.
+// One warp walks the CTA's tiles, through the page table, ahead of everybody and
+// states their facts; a second one walks with it.  Whole bf16 tiles they copy by
+// TMA (keys and values), keeping count of a bf16 store's other operands; for the
+// other stores the second brings later pages into L2.
 template <int FMT, bool PAIR>
 struct Scout {
   static constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
@@ -330,36 +331,39 @@ struct Scout {
     if (n < 4) x.w = none;
     return x;
   }
-  // Pages and scales of tile k, asked for a tile before they are stated.
-  __device__ __forceinline__ void fetch() {
-    if (k >= min(stored, it.kb)) return;
+  __device__ __forceinline__ void advance() {
     if (2 * k >= at + 32) {
       at += 32;
       lo = hi;
       hi = entry(at + 32 + lane);
     }
+  }
+  // Pages and scales of tile k, asked for a tile before they are stated.
+  __device__ __forceinline__ void fetch() {
+    if (k >= min(stored, it.kb)) return;
+    advance();
     a = page(2 * k);
     b = page(2 * k + 1);
     if (kQuant) {
       const int live = count - k * kTreeTile;
       ks = scales(p.st.ks, live, 1.f);  // finite where there is no slot
       vs = scales(p.st.vs, live, 0.f);
-      prefetch_page(2 * (k + kAhead));
-      prefetch_page(2 * (k + kAhead) + 1);
     }
+  }
+  // The next item (there is one).
+  __device__ __forceinline__ void enter() {
+    items.next(p, &it);
+    k = it.ka;
+    count = p.st.count(it.u);
+    stored = (count + kTreeTile - 1) / kTreeTile;
+    at = 2 * k;
+    lo = entry(at + lane);
+    hi = entry(at + 32 + lane);
   }
   // State tile t, the next of the walk.
   __device__ __forceinline__ void state(uint32_t t) {
-    if (k == it.kb) {  // the next item (there is one: t is a tile of this CTA)
-      items.next(p, &it);
-      k = it.ka;
-      count = p.st.count(it.u);
-      stored = (count + kTreeTile - 1) / kTreeTile;
-      at = 2 * k;
-      lo = entry(at + lane);
-      hi = entry(at + 32 + lane);
-      if (kQuant)
-        for (int i = 2; i < 2 * kAhead; ++i) prefetch_page(at + i);
+    if (k == it.kb) {
+      enter();
       fetch();
     }
     // a bf16 store's walk is paced by its K places: that of K(t - 4), free by now,
@@ -453,6 +457,21 @@ struct Scout {
       if (stated < n) state(stated++);
     }
     drain(n, copies);
+  }
+  // 8- and 4-bit stores, a warp of its own (a bulk prefetch is slow to issue): as
+  // tile t is stated, the pages kAhead tiles on are brought into L2.
+  __device__ __forceinline__ void run_ahead(uint32_t n) {
+    it.kb = 0;
+    for (uint32_t t = 0; t < n && ok; ++t, ++k) {
+      if (k == it.kb) {
+        enter();
+        for (int i = 2; i < 2 * kAhead; ++i) prefetch_page(at + i);
+      }
+      advance();
+      prefetch_page(2 * (k + kAhead));
+      prefetch_page(2 * (k + kAhead) + 1);
+      ok = __all_sync(kFull, tc::mbar_wait(bar(&m->stated[t % kMeta]), (t / kMeta) & 1u, &m->abort));
+    }
   }
   // The values of a bf16 store, by a warp of their own: a poll takes hundreds of
   // cycles, and one warp's polls for keys, facts and values add up to a tile's time.
@@ -1120,9 +1139,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     } else if (warp == kSoftWarps + kLoadWarps + 1) {
       Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
       sc.run(n);
-    } else if (FMT == CERTKV_STORE_BF16 && warp == kSoftWarps + kLoadWarps + 2) {
+    } else if (warp == kSoftWarps + kLoadWarps + 2) {
       Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
-      sc.run_values(n);
+      if (FMT == CERTKV_STORE_BF16) sc.run_values(n);
+      else sc.run_ahead(n);
     }
     __syncwarp();
   }
