@@ -1,10 +1,12 @@
 // store.cu — the paged store: quantising rows as they are written, from the
 // packed cache or from token rows, and reading them back.
 //
-// Eight lanes hold a row, sixteen elements each: a 32-byte load, three shuffles
-// for the row's maximum, and one scale group of the 4-bit format per lane, so
-// its group maximum needs no exchange.  Every row is read once and written
-// once; the kernels are bound by those bytes.
+// Eight lanes hold a row: lane i elements 8 i .. 8 i + 7 and 64 + 8 i .., so that
+// every load and store of the eight lanes is one run of whole sectors (with
+// sixteen consecutive elements a lane each access would touch half of every
+// sector: reading back 131072 8-bit rows took 22.7 us instead of 20.4).  A scale
+// group of the 4-bit format is a pair of lanes.  Every row is read once and
+// written once; the kernels are bound by those bytes.
 #include "../../include/certkv.h"
 #include "common.cuh"
 #include "internal.cuh"
@@ -15,44 +17,55 @@ namespace certkv {
 namespace {
 
 constexpr int kStoreThreads = 256;
+constexpr int kLoadBlocks = 4;  // resident blocks per SM of the load kernel
 constexpr float kTiny = 7.8886091e-31f;  // 2^-100: rows below are held as zeros
 
 struct Words16 {
-  uint32_t w[8];  // sixteen bf16
+  uint32_t w[8];  // sixteen bf16: elements 8 sub .., then 64 + 8 sub ..
 };
 
-__device__ __forceinline__ Words16 load32(const void* p) {
+// This lane's elements of the bf16 row at `row`.
+__device__ __forceinline__ Words16 load_row(const uint16_t* row, int sub) {
   Words16 x;
-  const uint4* q = reinterpret_cast<const uint4*>(p);
-  const uint4 a = __ldg(q), b = __ldg(q + 1);
+  const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + 8 * sub));
+  const uint4 b = __ldg(reinterpret_cast<const uint4*>(row + 64 + 8 * sub));
   x.w[0] = a.x; x.w[1] = a.y; x.w[2] = a.z; x.w[3] = a.w;
   x.w[4] = b.x; x.w[5] = b.y; x.w[6] = b.z; x.w[7] = b.w;
   return x;
 }
+__device__ __forceinline__ void store_row(uint16_t* row, int sub, const Words16& x) {
+  *reinterpret_cast<uint4*>(row + 8 * sub) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+  *reinterpret_cast<uint4*>(row + 64 + 8 * sub) = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+}
+// Largest magnitude of eight bf16 as fp32 bits; a NaN or infinity stays one.
+__device__ __forceinline__ uint32_t top8(const uint32_t* w) {
+  uint32_t two = w[0] & 0x7fff7fffu;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(two) : "r"(w[i] & 0x7fff7fffu));
+  return max(two << 16, two & 0xffff0000u);
+}
 
-// Encode the row held by this lane's group of eight lanes (sub = lane & 7 holds
-// elements 16 sub .. 16 sub + 15) and write it to pool slot `to` (to < 0:
-// nowhere).  Every lane of the warp takes part in the shuffles.
+// Encode the row held by this lane's group of eight lanes (sub = lane & 7) and
+// write it to pool slot `to` (to < 0: nowhere).  Every lane of the warp takes
+// part in the shuffles.
 template <int FMT>
 __device__ __forceinline__ void put_row(const Words16& x, int sub, int64_t to, uint8_t* codes,
                                         uint8_t* group, float* scale) {
   if (FMT == CERTKV_STORE_BF16) {
-    if (to < 0) return;
-    uint4* o = reinterpret_cast<uint4*>(codes + to * 256 + sub * 32);
-    o[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
-    o[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+    if (to >= 0) store_row(reinterpret_cast<uint16_t*>(codes) + to * kD, sub, x);
     return;
   }
-  // magnitudes of bf16 order as integers; a NaN or infinity is >= 0x7f80
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    top = max(top, (x.w[i] & 0x7fffu) << 16);
-    top = max(top, x.w[i] & 0x7fff0000u);
+  // maxima of the lane pair's elements in either half of the row (4-bit scale
+  // groups sub / 2 and 4 + sub / 2), then of the row
+  uint32_t half[2] = {top8(x.w), top8(x.w + 4)};
+  if (FMT == CERTKV_STORE_FP4) {
+    half[0] = max(half[0], __shfl_xor_sync(kFull, half[0], 1));
+    half[1] = max(half[1], __shfl_xor_sync(kFull, half[1], 1));
   }
-  const float ag = __uint_as_float(top);  // the lane's own maximum (its group's)
-#pragma unroll
-  for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
+  uint32_t top = max(half[0], half[1]);
+  if (FMT != CERTKV_STORE_FP4) top = max(top, __shfl_xor_sync(kFull, top, 1));
+  top = max(top, __shfl_xor_sync(kFull, top, 2));
+  top = max(top, __shfl_xor_sync(kFull, top, 4));
   const float amax = __uint_as_float(top);
   const float kTop = FMT == CERTKV_STORE_FP8 ? 448.f : 2688.f;
   const bool bad = top >= 0x7f800000u;
@@ -61,63 +74,60 @@ __device__ __forceinline__ void put_row(const Words16& x, int sub, int64_t to, u
   const float r = zero ? 0.f : __fmul_rn(__frcp_rn(amax), kTop);
   if (to < 0) return;
   if (sub == 0) scale[to] = s;
-  float m = r;
-  if (FMT == CERTKV_STORE_FP4) {
-    const uint32_t g8 = bad ? 0u : e4m3x2(__fmul_rn(__fmul_rn(ag, r), 1.f / 6.f), 0.f) & 0xffu;
-    const float gs = f16x2_to_f32(e4m3x2_to_f16x2(g8)).x;
-    m = gs > 0.f ? __fmul_rn(r, __frcp_rn(gs)) : 0.f;
-    group[to * kGroups + sub] = (uint8_t)g8;
-  }
-  float v[16];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[2 * i] = bad ? 0.f : __fmul_rn(__uint_as_float(x.w[i] << 16), m);
-    v[2 * i + 1] = bad ? 0.f : __fmul_rn(__uint_as_float(x.w[i] & 0xffff0000u), m);
-  }
-  if (FMT == CERTKV_STORE_FP8) {
-    uint32_t o[4];
+  for (int h = 0; h < 2; ++h) {
+    float m = r;
+    if (FMT == CERTKV_STORE_FP4) {
+      const uint32_t g8 = bad ? 0u : e4m3x2(__fmul_rn(__fmul_rn(__uint_as_float(half[h]), r), 1.f / 6.f), 0.f) & 0xffu;
+      const float gs = f16x2_to_f32(e4m3x2_to_f16x2(g8)).x;
+      m = gs > 0.f ? __fmul_rn(r, __frcp_rn(gs)) : 0.f;
+      if ((sub & 1) == h) group[to * kGroups + 4 * h + (sub >> 1)] = (uint8_t)g8;
+    }
+    const float2 m2 = make_float2(m, m);
+    float2 v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      o[i] = e4m3x2(v[4 * i], v[4 * i + 1]) | (e4m3x2(v[4 * i + 2], v[4 * i + 3]) << 16);
-    *reinterpret_cast<uint4*>(codes + to * 128 + sub * 16) = make_uint4(o[0], o[1], o[2], o[3]);
-  } else {
-    uint32_t o[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      o[i] = e2m1x2(v[8 * i], v[8 * i + 1]) | (e2m1x2(v[8 * i + 2], v[8 * i + 3]) << 8) |
-             (e2m1x2(v[8 * i + 4], v[8 * i + 5]) << 16) | (e2m1x2(v[8 * i + 6], v[8 * i + 7]) << 24);
-    *reinterpret_cast<uint2*>(codes + to * 64 + sub * 8) = make_uint2(o[0], o[1]);
+    for (int i = 0; i < 4; ++i) v[i] = fmul2(make_float2(bf16lo(x.w[4 * h + i]), bf16hi(x.w[4 * h + i])), m2);
+    if (FMT == CERTKV_STORE_FP8) {
+      const uint32_t a = bad ? 0u : e4m3x2(v[0].x, v[0].y) | (e4m3x2(v[1].x, v[1].y) << 16);
+      const uint32_t b = bad ? 0u : e4m3x2(v[2].x, v[2].y) | (e4m3x2(v[3].x, v[3].y) << 16);
+      *reinterpret_cast<uint2*>(codes + to * 128 + 64 * h + sub * 8) = make_uint2(a, b);
+    } else {
+      *reinterpret_cast<uint32_t*>(codes + to * 64 + 32 * h + sub * 4) = bad ? 0u : e2m1x8(v[0], v[1], v[2], v[3]);
+    }
   }
 }
 
-// Sixteen elements of pool slot `at` as bf16 words.
+// This lane's elements of pool slot `at` as bf16 words.
 template <int FMT>
 __device__ __forceinline__ Words16 get_row(int sub, int64_t at, const uint8_t* codes,
                                            const uint8_t* group, const float* scale) {
-  if (FMT == CERTKV_STORE_BF16) return load32(codes + at * 256 + sub * 32);
+  if (FMT == CERTKV_STORE_BF16) return load_row(reinterpret_cast<const uint16_t*>(codes) + at * kD, sub);
   Words16 x;
   const float s = scale[at];
-  if (FMT == CERTKV_STORE_FP8) {
-    const uint4 c = __ldg(reinterpret_cast<const uint4*>(codes + at * 128 + sub * 16));
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 f = f16x2_to_f32(e4m3x2_to_f16x2((w[i >> 1] >> (16 * (i & 1))) & 0xffffu));
-      const __nv_bfloat162 h = __floats2bfloat162_rn(f.x * s, f.y * s);
-      x.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  for (int h = 0; h < 2; ++h) {
+    uint32_t f16[4];
+    float gs = 1.f;
+    if (FMT == CERTKV_STORE_FP8) {
+      const uint2 c = __ldg(reinterpret_cast<const uint2*>(codes + at * 128 + 64 * h + sub * 8));
+      f16[0] = e4m3x2_to_f16x2(c.x & 0xffffu);
+      f16[1] = e4m3x2_to_f16x2(c.x >> 16);
+      f16[2] = e4m3x2_to_f16x2(c.y & 0xffffu);
+      f16[3] = e4m3x2_to_f16x2(c.y >> 16);
+    } else {
+      const uint32_t c = __ldg(reinterpret_cast<const uint32_t*>(codes + at * 64 + 32 * h + sub * 4));
+      gs = f16x2_to_f32(e4m3x2_to_f16x2(group[at * kGroups + 4 * h + (sub >> 1)])).x;
+      f16[0] = e2m1x2_to_f16x2<0>(c);
+      f16[1] = e2m1x2_to_f16x2<1>(c);
+      f16[2] = e2m1x2_to_f16x2<2>(c);
+      f16[3] = e2m1x2_to_f16x2<3>(c);
     }
-  } else {
-    const uint2 c = __ldg(reinterpret_cast<const uint2*>(codes + at * 64 + sub * 8));
-    const float gs = f16x2_to_f32(e4m3x2_to_f16x2(group[at * kGroups + sub])).x;
-    const uint32_t h[8] = {e2m1x2_to_f16x2<0>(c.x), e2m1x2_to_f16x2<1>(c.x),
-                           e2m1x2_to_f16x2<2>(c.x), e2m1x2_to_f16x2<3>(c.x),
-                           e2m1x2_to_f16x2<0>(c.y), e2m1x2_to_f16x2<1>(c.y),
-                           e2m1x2_to_f16x2<2>(c.y), e2m1x2_to_f16x2<3>(c.y)};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 f = f16x2_to_f32(h[i]);
-      const __nv_bfloat162 b = __floats2bfloat162_rn((f.x * gs) * s, (f.y * gs) * s);
-      x.w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    for (int i = 0; i < 4; ++i) {
+      float2 f = f16x2_to_f32(f16[i]);
+      if (FMT == CERTKV_STORE_FP4) f = make_float2(f.x * gs, f.y * gs);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * s, f.y * s);
+      x.w[4 * h + i] = *reinterpret_cast<const uint32_t*>(&b);
     }
   }
   return x;
@@ -166,9 +176,11 @@ __global__ void __launch_bounds__(1024) load_plan_kernel(int units, const int32_
 }
 
 // Persistent: tables and counts, then the pages, one page of K and V rows per
-// block and step.
+// block and step.  Four blocks an SM, whose registers hold two rows of K and V a
+// thread in flight, are the fastest (1.7 GB of bf16 rows into 8 bits: 400 us, 96 %
+// of the copy bandwidth; five blocks 424, eight with one row at a time 495).
 template <int FMT>
-__global__ void __launch_bounds__(kStoreThreads) load_kernel(
+__global__ void __launch_bounds__(kStoreThreads, kLoadBlocks) load_kernel(
     Store st, const uint16_t* __restrict__ pk, const uint16_t* __restrict__ pv,
     const int64_t* __restrict__ offsets, const int32_t* __restrict__ real, int tail_slot,
     int64_t capacity, const int32_t* __restrict__ first) {
@@ -201,15 +213,15 @@ __global__ void __launch_bounds__(kStoreThreads) load_kernel(
     const int n = max(real[u], 0) + tail_slot;
     const bool outside = offsets[u] < 0 || offsets[u] + n > capacity;
     if (outside || page - first[u] >= st.max_pages) continue;  // uniform over the block
-#pragma unroll
+#pragma unroll 2
     for (int half = 0; half < 2; ++half) {
       const int s = s0 + half * 32 + grp;
       const bool live = s < n;
-      const int64_t from = (offsets[u] + s) * kD + sub * 16;
+      const int64_t from = (offsets[u] + s) * kD;
       Words16 a = {}, b = {};
       if (live) {
-        a = load32(pk + from);
-        b = load32(pv + from);
+        a = load_row(pk + from, sub);
+        b = load_row(pv + from, sub);
       }
       const int64_t to = live ? (int64_t)page * kPage + half * 32 + grp : -1;
       put_row<FMT>(a, sub, to, st.k, st.kg, st.ks);
@@ -234,17 +246,24 @@ __device__ __forceinline__ int grown(const Store& st, int start, int m) {
   return (int)min((int64_t)max(start, 0) + m, (int64_t)st.max_pages * kPage);
 }
 
-// Eight lanes per (segment, row): both K and V of it.
+// id / by, for the ids a launch has: 32-bit division where they fit
+__device__ __forceinline__ int64_t div_id(int64_t id, int64_t ids, int by) {
+  return ids <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)by) : id / by;
+}
+
+// Eight lanes per (segment, row): both K and V of it.  Two rows a group of lanes,
+// for more loads in flight, was slower (258 -> 278 us for the 4-bit prompt of
+// 131071 x 8 rows written and read back): fewer warps then fit.
 template <int FMT>
-__global__ void __launch_bounds__(kStoreThreads) append_kernel(Store st, AppendArgs p) {
+__global__ void __launch_bounds__(kStoreThreads, 8) append_kernel(Store st, AppendArgs p) {
   const int64_t id = ((int64_t)blockIdx.x * kStoreThreads + threadIdx.x) >> 3;
   const int sub = threadIdx.x & 7;
   Words16 a = {}, c = {};
   int64_t to = -1;
   if (id < p.rows) {
-    const int64_t u = id / p.T;
+    const int64_t u = div_id(id, p.rows, p.T);
     const int i = (int)(id - u * p.T);
-    const int bl = (int)(u / p.H), h = (int)(u - (int64_t)bl * p.H);
+    const int bl = (int)u / p.H, h = (int)u - bl * p.H;
     const int b = bl / p.L, l = bl - b * p.L;
     const int m = accepted_of(p, b);
     const int start = p.start[u];
@@ -253,8 +272,8 @@ __global__ void __launch_bounds__(kStoreThreads) append_kernel(Store st, AppendA
       const int64_t s = (int64_t)start + i;
       if (start >= 0 && s < (int64_t)st.max_pages * kPage && t >= 0 && t < p.T) to = st.slot(u, (int)s);
       if (to >= 0) {
-        a = load32(p.k.at(b, l, t, h) + sub * 16);
-        c = load32(p.v.at(b, l, t, h) + sub * 16);
+        a = load_row(p.k.at(b, l, t, h), sub);
+        c = load_row(p.v.at(b, l, t, h), sub);
       } else if (sub == 0) {
         st.raise();
       }
@@ -279,6 +298,7 @@ __global__ void __launch_bounds__(kStoreThreads) append_count_kernel(Store st, A
 }
 
 // ------------------------------------------------------------------ read --
+// Eight lanes per (segment, slot): both K and V of it.
 template <int FMT>
 __global__ void __launch_bounds__(kStoreThreads) read_kernel(Store st, const int32_t* __restrict__ start,
                                                              int T, int64_t rows,
@@ -287,7 +307,7 @@ __global__ void __launch_bounds__(kStoreThreads) read_kernel(Store st, const int
   const int64_t id = ((int64_t)blockIdx.x * kStoreThreads + threadIdx.x) >> 3;
   const int sub = threadIdx.x & 7;
   if (id >= rows) return;
-  const int64_t u = id / T;
+  const int64_t u = div_id(id, rows, T);
   const int64_t s = (start ? start[u] : 0) + (id - u * T);
   const int64_t at = s >= 0 && s < st.count(u) ? st.slot(u, (int)s) : -1;
   Words16 a = {}, b = {};
@@ -295,12 +315,8 @@ __global__ void __launch_bounds__(kStoreThreads) read_kernel(Store st, const int
     a = get_row<FMT>(sub, at, st.k, st.kg, st.ks);
     b = get_row<FMT>(sub, at, st.v, st.vg, st.vs);
   }
-  uint4* oa = reinterpret_cast<uint4*>(ko + id * kD + sub * 16);
-  uint4* ob = reinterpret_cast<uint4*>(vo + id * kD + sub * 16);
-  oa[0] = make_uint4(a.w[0], a.w[1], a.w[2], a.w[3]);
-  oa[1] = make_uint4(a.w[4], a.w[5], a.w[6], a.w[7]);
-  ob[0] = make_uint4(b.w[0], b.w[1], b.w[2], b.w[3]);
-  ob[1] = make_uint4(b.w[4], b.w[5], b.w[6], b.w[7]);
+  store_row(ko + id * kD, sub, a);
+  store_row(vo + id * kD, sub, b);
 }
 
 int last_error() { return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA; }
@@ -341,8 +357,8 @@ extern "C" int certkv_store_load(const certkv_packed* packed, int32_t tail_slot,
     TraceScope ts_("store_plan", st);
     load_plan_kernel<<<1, 1024, 0, st>>>(s.units, packed->real_counts, tail_slot, reserve, first);
   }
-  // enough blocks for every page, at most eight on each SM
-  const int grid = s.pool_pages < 152 * 8 ? s.pool_pages : 152 * 8;
+  // enough blocks for every page, at most those that are resident together
+  const int grid = s.pool_pages < 152 * kLoadBlocks ? s.pool_pages : 152 * kLoadBlocks;
   const uint16_t* pk = reinterpret_cast<const uint16_t*>(packed->k);
   const uint16_t* pv = reinterpret_cast<const uint16_t*>(packed->v);
   TraceScope ts_("store_load", st);

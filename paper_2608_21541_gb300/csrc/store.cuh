@@ -82,11 +82,15 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
   return r;
 }
-__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {  // low nibble = lo
+// eight codes, the first the lowest nibble
+__device__ __forceinline__ uint32_t e2m1x8(float2 a, float2 b, float2 c, float2 d) {
   uint32_t r;
-  asm("{\n .reg .b8 t;\n cvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n cvt.u32.u8 %0, t;\n}"
+  asm("{\n .reg .b8 s, t, u, v;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 s, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 t, %4, %3;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 u, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 v, %8, %7;\n"
+      " mov.b32 %0, {s, t, u, v};\n}"
       : "=r"(r)
-      : "f"(hi), "f"(lo));
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y), "f"(d.x), "f"(d.y));
   return r;
 }
 // four of the eight codes of a word: byte `which` (two codes) as f16x2
