@@ -6,7 +6,8 @@
 // t's mask word.  A draft that a row does not see is never read for it, so a
 // NaN there cannot reach it.
 //
-// Three launches: a scan of the segments' tile counts, a split kernel over equal
+// Three launches: a scan of the segments' tile counts (the split kernels do it
+// themselves for few units), a split kernel over equal
 // shares of all tiles (tree_mma.cu for up to 16 query rows per unit, else
 // tree_tc.cu), and the merge below, which joins the records of the CTAs that met
 // a unit in the log-sum-exp domain and, for few rows, adds the drafts.
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   float M = -INFINITY, L = 0.f;
   float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
   if (n > 0) {
-    const int64_t per = tiles_per_cta(p), at = p.first[u] * p.nblk + blk * n;
+    const int64_t per = tiles_per_cta(p, p.first), at = p.first[u] * p.nblk + blk * n;
     const int64_t vu = (int64_t)u * p.nblk + blk;
     const int c0 = (int)(at / per), c1 = (int)((at + n - 1) / per);
     for (int c = c0; c <= c1; c += 4) {
@@ -282,7 +283,7 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   p.rec_ml = reinterpret_cast<float2*>(ws + ly.ml);
   p.rec_acc = reinterpret_cast<float*>(ws + ly.acc);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  {
+  if (p.units > kInlineUnits) {
     TraceScope ts_("tree_plan", st);
     tree_plan_kernel<<<1, 1024, 0, st>>>(p.st, p.small ? small_tile(store->format) : kTreeTile,
                                          !p.small && p.kn.p ? 1 : 0, first);

@@ -31,7 +31,7 @@ struct TreeArgs {
   float scale_log2;
   Store st;
   // workspace
-  const int64_t* first;  // [units + 1] tiles of the segments before (one row block)
+  int64_t* first;        // [units + 1] tiles of the segments before (one row block)
   uint64_t* odd;         // [units] drafts whose value row holds a NaN or infinity
   float2* rec_ml;        // [records][rb] log2-domain reference and sum
   float* rec_acc;        // [records][rb][128] weighted mean of the values
@@ -45,8 +45,50 @@ __device__ __forceinline__ uint64_t seen(const TreeArgs& p, int b, int t) {
 
 // Tiles [g0, g1) of CTA c: the global sequence (unit, row block, tile) in equal
 // consecutive shares.
-__device__ __forceinline__ int64_t tiles_per_cta(const TreeArgs& p) {
-  return max((p.first[p.units] * p.nblk + p.ctas - 1) / p.ctas, (int64_t)p.least);
+__device__ __forceinline__ int64_t tiles_per_cta(const TreeArgs& p, const int64_t* first) {
+  return max((first[p.units] * p.nblk + p.ctas - 1) / p.ctas, (int64_t)p.least);
+}
+
+// Up to this many units every CTA of a split kernel scans the tile counts itself,
+// which saves the launch of the scan (attention of one token over eight heads: 18
+// -> 16 us).
+constexpr int kInlineUnits = 256;
+// The tiles before each unit, as p.first: read from there, or worked out into
+// shared memory by the whole block (and by CTA 0 for the merge as well).
+__device__ __forceinline__ const int64_t* tree_first(const TreeArgs& p, int64_t* smem, int tile, int drafts) {
+  if (p.units > kInlineUnits) return p.first;
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    int64_t v[kInlineUnits / 32], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kInlineUnits / 32; ++i) {  // units 8 lane ..
+      const int u = lane * (kInlineUnits / 32) + i;
+      v[i] = u < p.units ? (p.st.count(u) + tile - 1) / tile + drafts : 0;
+      sum += v[i];
+    }
+    int64_t x = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(kFull, x, o);
+      if (lane >= o) x += y;
+    }
+    x -= sum;
+#pragma unroll
+    for (int i = 0; i < kInlineUnits / 32; ++i) {
+      const int u = lane * (kInlineUnits / 32) + i;
+      if (u <= p.units) {
+        smem[u] = x;
+        if (blockIdx.x == 0) p.first[u] = x;
+      }
+      x += v[i];
+    }
+    if (lane == 31 && p.units == kInlineUnits) {
+      smem[kInlineUnits] = x;
+      if (blockIdx.x == 0) p.first[kInlineUnits] = x;
+    }
+  }
+  __syncthreads();
+  return smem;
 }
 
 // One (CTA, unit, row block) that meet: their partial results are record
@@ -58,26 +100,26 @@ struct Item {
 
 // Walks over the items of a CTA.
 struct Items {
+  const int64_t* first;
   int64_t g, g1;
-  int u, blk;
-  bool fresh;
-  __device__ __forceinline__ Items(const TreeArgs& p, int64_t per) {
-    const int64_t total = p.first[p.units] * p.nblk;
+  int u;
+  __device__ __forceinline__ Items(const TreeArgs& p, const int64_t* first_, int64_t per) : first(first_) {
+    const int64_t total = first[p.units] * p.nblk;
     g = per * blockIdx.x;
     g1 = min(total, g + per);
     int lo = 0, hi = p.units;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (p.first[mid] * p.nblk <= g) lo = mid;
+      if (first[mid] * p.nblk <= g) lo = mid;
       else hi = mid;
     }
     u = lo;
   }
   __device__ __forceinline__ bool next(const TreeArgs& p, Item* it) {
     if (g >= g1) return false;
-    while (p.first[u + 1] * p.nblk <= g) ++u;
-    const int n = (int)(p.first[u + 1] - p.first[u]);
-    const int64_t in = g - p.first[u] * p.nblk;
+    while (first[u + 1] * p.nblk <= g) ++u;
+    const int n = (int)(first[u + 1] - first[u]);
+    const int64_t in = g - first[u] * p.nblk;
     it->u = u;
     it->blk = (int)(in / n);
     it->ka = (int)(in - (int64_t)it->blk * n);

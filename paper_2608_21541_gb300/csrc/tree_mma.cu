@@ -61,6 +61,7 @@ struct Tail {
   int live[8];  // slots of the stage's tile to take
   int abort;
   float m[kConsumers][kRows], l[kConsumers][kRows], e[kConsumers][kRows];
+  int64_t first[kInlineUnits + 1];  // see tree_first
 };
 template <int FMT>
 constexpr int smem_bytes() {
@@ -158,12 +159,12 @@ __device__ __forceinline__ int element_of(int i, int qc, int e) {
 // ------------------------------------------------------------- producer --
 template <int FMT>
 __device__ __forceinline__ void produce(const TreeArgs& p, const CUtensorMap* tmK, const CUtensorMap* tmV,
-                                        uint32_t sm, Tail* tl, int lane, int64_t per) {
+                                        uint32_t sm, Tail* tl, int lane, const int64_t* first, int64_t per) {
   using G = Geo<FMT>;
   constexpr int kPer = kPage / G::kSlots;  // tiles of a page
   int64_t issued = 0;
   bool ok = true;
-  Items items(p, per);
+  Items items(p, first, per);
   Item it;
   uint32_t copied = 0;  // stages whose last tile came by copies
   while (ok && items.next(p, &it)) {
@@ -233,7 +234,7 @@ __device__ __forceinline__ void produce(const TreeArgs& p, const CUtensorMap* tm
 // ------------------------------------------------------------ consumers --
 template <int FMT>
 __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wacc, Tail* tl, int tid,
-                                        int64_t per) {
+                                        const int64_t* first, int64_t per) {
   using G = Geo<FMT>;
   constexpr bool kQuant = G::kQuant;
   constexpr int kNb = G::kSlots / 8;  // eight-slot blocks of a tile
@@ -241,7 +242,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
   const uint32_t sm = tc::saddr(smem);
   int64_t tile = 0;  // tiles of this CTA before the item
   bool ok = true;
-  Items items(p, per);
+  Items items(p, first, per);
   Item it;
   while (items.next(p, &it)) {
     const int bl = it.u / p.H, h = it.u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
@@ -611,11 +612,12 @@ __global__ void __launch_bounds__(kThreads, 2) tree_mma_kernel(const __grid_cons
   }
   release_next();
   await_previous();
-  const int64_t per = tiles_per_cta(p);
-  if (per * blockIdx.x >= p.first[p.units] * p.nblk) return;  // uniform, before any barrier
+  const int64_t* first = tree_first(p, tl->first, small_tile(FMT), false);
+  const int64_t per = tiles_per_cta(p, first);
+  if (per * blockIdx.x >= first[p.units] * p.nblk) return;  // uniform, before any barrier
   __syncthreads();
-  if (threadIdx.x < 32) produce<FMT>(p, &tmK, &tmV, tc::saddr(sm), tl, threadIdx.x, per);
-  else consume<FMT>(p, sm, wacc, tl, threadIdx.x - 32, per);
+  if (threadIdx.x < 32) produce<FMT>(p, &tmK, &tmV, tc::saddr(sm), tl, threadIdx.x, first, per);
+  else consume<FMT>(p, sm, wacc, tl, threadIdx.x - 32, first, per);
   __syncthreads();
   if (threadIdx.x == 0 && tl->abort && p.st.status) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
 }

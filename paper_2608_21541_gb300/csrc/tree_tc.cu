@@ -114,6 +114,7 @@ struct Misc {
   float qs[256];                   // per row: scale of its f16 queries
   float cm[128], l[128], sh[128];  // stream 1's reference, sum and shift
   Meta meta[kMeta];
+  int64_t first[kInlineUnits + 1];  // see tree_first
 };
 static_assert(sizeof(Meta) % 16 == 0 && offsetof(Misc, meta) % 16 == 0, "float4 accesses");
 template <bool PAIR>
@@ -707,8 +708,8 @@ struct Issuer {
     if (fin) um::commit(uni(bar(&m->o_full[st])));
   }
 
-  __device__ __forceinline__ void run(const TreeArgs& p, int64_t per) {
-    Items items(p, per);
+  __device__ __forceinline__ void run(const TreeArgs& p, const int64_t* first, int64_t per) {
+    Items items(p, first, per);
     Item it;
     uint32_t t0 = 0, item = 0;  // tiles and items before
     while (ok && items.next(p, &it)) {
@@ -843,11 +844,11 @@ struct Row {
     return (sum0.x + sum0.y) + (sum1.x + sum1.y);
   }
 
-  // A new reference from columns 32 c .. of the tile: the accumulator, the sums
-  // and the weights of the tile's earlier columns are scaled to it (by a power
-  // of two).  `acc`: there is an accumulator.
-  __device__ __forceinline__ void regrow(uint32_t tS, uint32_t tO, int c, const Meta& mt, float dE, bool acc,
-                                         float& sum) {
+  // A new reference from columns 32 c .. of the tile for a row that needs one
+  // (`over`): its accumulator, its sums and the weights of the tile's earlier
+  // columns are scaled to it (by a power of two).  `acc`: there is an accumulator.
+  __device__ __forceinline__ void regrow(uint32_t tS, uint32_t tO, int c, const Meta& mt, float dE, bool over,
+                                         bool acc, float& sum) {
     float mx = -INFINITY;
     um::wait_st();  // earlier columns' weights are read back below
     {
@@ -858,7 +859,7 @@ struct Row {
     }
     const float nc = reference(mx, dE);
     float f = 1.f;
-    if (nc > C) {
+    if (over && nc > C) {
       f = um::ex2(C - nc);
       C = nc;
     }
@@ -907,8 +908,9 @@ struct Row {
     for (int c = 0; c < 4;) {
       uint32_t hi[16], lo[16];
       const float x = chunk(tS, c, mt, offset(dE), hi, lo);
-      if (!again && __any_sync(kFull, !(x < kLimit))) {
-        regrow(tS, tO, c, mt, dE, acc, sum);
+      const bool over = !(x < kLimit);
+      if (!again && __any_sync(kFull, over)) {
+        regrow(tS, tO, c, mt, dE, over, acc, sum);
         again = true;
         continue;
       }
@@ -924,7 +926,7 @@ struct Row {
 
 template <int FMT, bool PAIR>
 __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t base, uint32_t tmem,
-                                        int tid, int64_t per) {
+                                        int tid, const int64_t* first, int64_t per) {
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
   volatile int* ab = &m->abort;
   const int warp = tid >> 5, lane = tid & 31, s = warp >> 2, quad = warp & 3;
@@ -935,7 +937,7 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
   const uint32_t tO = tmem + kColO + 128u * s + ((uint32_t)(quad * 32) << 16);
   uint32_t t0 = 0, uses = 0, finals = 0;  // tiles before; S and final O of this stream so far
   bool ok = true;                         // false after a wait gave up, for good
-  Items items(p, per);
+  Items items(p, first, per);
   Item it;
   while (items.next(p, &it)) {
     const int rows = min(p.rb, p.rows - it.blk * p.rb);  // of the block
@@ -1113,7 +1115,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   }
   release_next();
   await_previous();
-  const int64_t per = tiles_per_cta(p), left = p.first[p.units] * p.nblk - per * blockIdx.x;
+  const int64_t* first = tree_first(p, m->first, kTreeTile, p.kn.p != nullptr);
+  const int64_t per = tiles_per_cta(p, first), left = first[p.units] * p.nblk - per * blockIdx.x;
   if (left <= 0) return;  // uniform, before any barrier
   const uint32_t n = (uint32_t)min(left, per);  // tiles of this CTA
   if (warp == kSoftWarps + kLoadWarps) um::alloc(tc::saddr(&m->tmem), 512);
@@ -1124,7 +1127,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   const uint32_t base = tc::saddr(sm);
   if (warp < kSoftWarps) {
     regs_up<kSoftRegs>();
-    softmax<FMT, PAIR>(p, m, base, tmem, threadIdx.x, per);
+    softmax<FMT, PAIR>(p, m, base, tmem, threadIdx.x, first, per);
   } else if (warp < kSoftWarps + kLoadWarps) {
     regs_down<kLoadRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
@@ -1135,12 +1138,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     regs_down<kIssueRegs>();
     if (warp == kSoftWarps + kLoadWarps) {
       Issuer<FMT, PAIR> is{m, tmem, base, base + Plan<PAIR>::kRingOff, n};
-      is.run(p, per);
+      is.run(p, first, per);
     } else if (warp == kSoftWarps + kLoadWarps + 1) {
-      Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
+      Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, first, per)};
       sc.run(n);
     } else if (warp == kSoftWarps + kLoadWarps + 2) {
-      Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, per)};
+      Scout<FMT, PAIR> sc{p, m, &tmK, &tmV, base + Plan<PAIR>::kRingOff, (int)threadIdx.x & 31, true, Items(p, first, per)};
       if (FMT == CERTKV_STORE_BF16) sc.run_values(n);
       else sc.run_ahead(n);
     }

@@ -240,3 +240,28 @@ def test_matches_decode_over_the_packed_cache():
     a = ck.certkv_decode_attn(q, packed, hkv=wl.H).float()
     b = ck.certkv_tree_attn(q.unsqueeze(2), st, hkv=wl.H)[:, :, 0].float()
     assert (a - b).abs().max() <= 2.0 ** -7 * a.abs().max()
+
+
+@pytest.mark.parametrize("T,G", [(1, 4), (9, 8)])
+@pytest.mark.parametrize("units", [255, 256, 257, 1100])
+def test_many_segments(units, T, G):
+    """Around the number of segments up to which a CTA scans the lengths itself, and
+    more than one block's scan takes in one go."""
+    st, n = store_with([3, 0, 70, 129, 1], 1, units, 1, "fp8", 270)
+    q = randn((1, units, T, G, 128), 1)
+    k, v = randn((1, units, T, 1, 128), 2), randn((1, units, T, 1, 128), 3)
+    out = ck.certkv_tree_attn(q, st, hkv=1, k_new=k, v_new=v)
+    check_attention(out, None, attention(q, st, n, 1, k, v))
+    alone = ck.Store(k=st.k, v=st.v, table=st.table[-2:], counts=st.counts[-2:], format="fp8",
+                     k_scale=st.k_scale, v_scale=st.v_scale)
+    two = ck.certkv_tree_attn(q[:, -2:], alone, hkv=1, k_new=k[:, -2:], v_new=v[:, -2:])
+    # the same rows, split over the CTAs in another way
+    assert (two.float() - out[:, -2:].float()).abs().max() <= 2.0 ** -7 * out.float().abs().max()
+
+
+def test_no_slots_anywhere():
+    st, _ = store_with([0], 2, 1, 3, "bf16", 280)
+    q = randn((2, 1, 4, 6, 128), 1)
+    lse = torch.empty((2, 1, 4, 6), device="cuda")
+    out = ck.certkv_tree_attn(q, st, hkv=3, lse=lse)
+    assert not out.float().any() and torch.isinf(lse).all() and (lse < 0).all()
