@@ -7,11 +7,13 @@
 // NaN there cannot reach it.
 //
 // Three launches: a scan of the segments' tile counts (the split kernels do it
-// themselves for few units), a split kernel over equal
-// shares of all tiles (tree_mma.cu for up to 16 query rows per unit, else
-// tree_tc.cu), and the merge below, which joins the records of the CTAs that met
-// a unit in the log-sum-exp domain and, for few rows, adds the drafts.
+// themselves for few units), a split kernel over equal shares of all tiles
+// (tree_mma.cu for few query rows per unit, else tree_tc.cu: small_max), and the
+// merge below, which joins the records of the CTAs that met a unit in the
+// log-sum-exp domain and, for few rows, adds the drafts.
 #include <math.h>
+
+#include <algorithm>
 
 #include "../../include/certkv.h"
 #include "common.cuh"
@@ -195,8 +197,8 @@ int tree_shape(const certkv_shape* s, int32_t tokens) {
 // Query rows of a unit in blocks, as equal as they come: few rows in blocks of at
 // most 16 (mma.sync), more in blocks of at most 256 (tcgen05: up to 128 rows are
 // one M = 128 operand, up to 256 two).
-void row_blocks(int rows, int* nblk, int* rb) {
-  const int most = rows <= kSmallMax ? kSmallRows : 256;
+void row_blocks(int rows, int format, int* nblk, int* rb) {
+  const int most = rows <= small_max(format) ? kSmallRows : 256;
   *nblk = (rows + most - 1) / most;
   *rb = (rows + *nblk - 1) / *nblk;
 }
@@ -206,11 +208,15 @@ constexpr int kTreeMaxCtas = 1024;  // records are sized for at most this many C
 struct TreeLayout {
   size_t first, odd, ml, acc, total;
 };
+// The same for every format: what the format with the most records takes.
 TreeLayout tree_layout(int units, int rows) {
   auto a = [](size_t x) { return (x + 255) / 256 * 256; };
-  int nblk, rb;
-  row_blocks(rows, &nblk, &rb);
-  const size_t recs = ((size_t)units * nblk + kTreeMaxCtas) * rb;
+  size_t recs = 0;
+  for (int format : {CERTKV_STORE_BF16, CERTKV_STORE_FP8, CERTKV_STORE_FP4}) {
+    int nblk, rb;
+    row_blocks(rows, format, &nblk, &rb);
+    recs = std::max(recs, ((size_t)units * nblk + kTreeMaxCtas) * rb);
+  }
   TreeLayout ly;
   ly.first = 0;
   ly.odd = a(((size_t)units + 1) * sizeof(int64_t));
@@ -265,10 +271,10 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   p.mask = mask;
   p.lse = lse;
   p.scale_log2 = (float)((scale > 0.0f ? scale : 1.0 / sqrt((double)kD)) * 1.4426950408889634);
-  row_blocks(p.rows, &p.nblk, &p.rb);
+  row_blocks(p.rows, store->format, &p.nblk, &p.rb);
   const int64_t merge = ((int64_t)p.units * p.rows + 7) / 8;
   if (merge > INT32_MAX) return CERTKV_EINVAL;
-  p.small = p.rows <= kSmallMax;
+  p.small = p.rows <= small_max(store->format);
   p.ctas = p.small ? tree_mma_ctas(store->format) : tree_ctas();
   p.least = p.small ? 4 : p.rb <= 128 ? 2 : 1;  // consumer warps, streams on tiles of their own
   if (p.ctas < 1) return CERTKV_ECUDA;

@@ -11,7 +11,15 @@ namespace certkv {
 
 constexpr int kTreeTile = 128;  // slots per tile of the tcgen05 kernel: two pages
 constexpr int kSmallRows = 16;  // query rows of a block of the mma.sync kernel
-constexpr int kSmallMax = 32;   // up to this many query rows: that kernel
+// Up to this many query rows go to that kernel.  The tcgen05 kernel costs the same for 1 to
+// 128 rows, the mma.sync kernel in proportion to its blocks of 16: one is always cheaper,
+// two are where codes have to be expanded, but not where they only read a bf16 store twice.
+// 32 rows, 256 segments of 13107 slots, mma.sync against tcgen05: 8-bit 323 and 351 us, 4-bit
+// 318 and 374, bf16 512 and 275; 8 segments of 409 slots: 20.4 and 24.5, 21.5 and 23.5, 16.5
+// and 20.2.
+__host__ __device__ constexpr int small_max(int format) {
+  return format == CERTKV_STORE_BF16 ? kSmallRows : 2 * kSmallRows;
+}
 // slots per tile of that kernel
 __host__ __device__ constexpr int small_tile(int format) {
   return format == CERTKV_STORE_BF16 ? 32 : CERTKV_STORE_PAGE;
