@@ -107,6 +107,8 @@ def load_library(path: Optional[str] = None):
     CERTKV_LIBRARY may name another build of it, such as the bounds-checking
     one); raise if it is missing."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -690,6 +692,11 @@ def _index(t: Optional[torch.Tensor], name: str, shape: tuple, dtype=torch.int32
     return t.data_ptr()
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """An uninitialised dense tensor of t's shape (a third of new_empty's host time)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _workspace(ws: torch.Tensor) -> tuple:
     if not ws.is_cuda or not ws.is_contiguous():
         raise ValueError("the workspace must be a contiguous CUDA tensor")
@@ -740,7 +747,7 @@ def certkv_rope(q, positions, plan: certkv_rope_angles, k=None, *, out=None, k_o
     rq = _rows(q, "q")
     made = []
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _like(q)
         made.append(out)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
@@ -751,7 +758,7 @@ def certkv_rope(q, positions, plan: certkv_rope_angles, k=None, *, out=None, k_o
         if k.shape[:3] != (B, L, T):
             raise ValueError("k must have the sequences, layers and tokens of q")
         if k_out is None:
-            k_out = k.new_empty(k.shape)
+            k_out = _like(k)
             made.append(k_out)
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have the shape of k")
@@ -927,7 +934,7 @@ def certkv_tree_attn(q, store: Store, *, hkv: int, k_new=None, v_new=None, mask=
     rq = _rows(q, "q")
     made = []
     if out is None:
-        out = q.new_empty(q.shape)
+        out = _like(q)
         made.append(out)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
