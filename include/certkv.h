@@ -554,7 +554,8 @@ typedef struct {
                             0..pool_pages - 1: none                               */
   int32_t  *counts;      /* [units] live slots (read as clamped to
                             0..64 max_pages)                                      */
-  uint32_t *status;      /* optional (NULL = skip) CERTKV_STATUS_STORE is or-ed in  */
+  uint32_t *status;      /* optional (NULL = skip): CERTKV_STATUS_STORE, and
+                            CERTKV_STATUS_TIMEOUT by the attention, are or-ed in  */
 } certkv_store;
 
 /* Quantise a packed cache into the store as its first contents: segment u gets
@@ -603,6 +604,10 @@ int certkv_store_read(const certkv_store* store, const int32_t* start, int32_t t
  * row's sum of exponentials.  shape: batch, layers, hq, hkv and d = 128 are
  * used; G = hq / hkv may be any integer 1..32, 1 <= tokens <= 64.  scale 0
  * selects 1/sqrt(d).  Slots without a page are left out (CERTKV_STATUS_STORE).
+ * Every wait inside is bounded; if one runs out, the rows concerned get NaN and
+ * CERTKV_STATUS_TIMEOUT is or-ed into the store's status word.  A store whose
+ * segments could hold 2^29 tiles per CTA (units max_pages over the CTAs, times a
+ * unit's row blocks) is refused with CERTKV_EINVAL.
  * Workspace: certkv_tree_workspace_bytes(shape, tokens), 256-byte aligned. */
 #define CERTKV_TREE_MAX_TOKENS 64
 #define CERTKV_TREE_MAX_GROUP 32

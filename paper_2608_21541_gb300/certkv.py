@@ -827,7 +827,8 @@ class Store:
         return self._struct
 
     def read_status(self) -> int:
-        """CERTKV_STATUS_STORE when a call met a slot without a page (synchronises)."""
+        """STATUS_STORE when a call met a slot without a page, STATUS_TIMEOUT when a
+        wait of the attention gave up (synchronises)."""
         return 0 if self.status is None else int(self.status.item())
 
     @staticmethod
