@@ -287,6 +287,49 @@ __global__ void __launch_bounds__(kStoreThreads, 8) append_kernel(Store st, Appe
   put_row<FMT>(c, sub, to, st.v, st.vg, st.vs);
 }
 
+// Many rows of each segment: a block takes kRun consecutive rows of one segment, a
+// group of lanes every 32nd of them, and the segment's indices and addresses are
+// worked out once.
+constexpr int kRun = 128;
+template <int FMT>
+__global__ void __launch_bounds__(kStoreThreads, 6) append_run_kernel(Store st, AppendArgs p, int runs) {
+  const int u = blockIdx.x / runs, i0 = (blockIdx.x - u * runs) * kRun;
+  const int sub = threadIdx.x & 7;
+  const int bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
+  const int m = accepted_of(p, b), start = p.start[u];
+  const uint16_t *k = p.k.at(b, l, 0, h), *v = p.v.at(b, l, 0, h);
+  const int32_t* select = p.select ? p.select + (int64_t)b * p.T : nullptr;
+  const int32_t* table = st.table + (int64_t)u * st.max_pages;
+  const int64_t room = start < 0 ? INT64_MIN : (int64_t)st.max_pages * kPage;
+  const int i1 = min(m, i0 + kRun);
+#pragma unroll 1
+  for (int r = i0; r < i1; r += 32) {
+    const int i = r + (threadIdx.x >> 3);
+    Words16 a = {}, c = {};
+    int64_t to = -1;
+    if (i < i1) {
+      const int t = select ? select[i] : i;
+      const int64_t s = (int64_t)start + i;
+      if (s < room && t >= 0 && t < p.T) {
+        const int page = table[(int)s / kPage];
+        if (page >= 0 && page < st.pool_pages) to = (int64_t)page * kPage + (int)s % kPage;
+      }
+      if (to >= 0) {
+        a = load_row(k + t * p.k.st, sub);
+        c = load_row(v + t * p.v.st, sub);
+      } else if (sub == 0) {
+        st.raise();
+      }
+    }
+    put_row<FMT>(a, sub, to, st.k, st.kg, st.ks);
+    put_row<FMT>(c, sub, to, st.v, st.vg, st.vs);
+  }
+  if (p.bump && i0 == 0 && threadIdx.x == 0) {
+    st.counts[u] = grown(st, start, m);
+    if (p.accepted && p.accepted[b] != m) st.raise();
+  }
+}
+
 // counts[u] += m, after the rows were written at the old counts.
 __global__ void __launch_bounds__(kStoreThreads) append_count_kernel(Store st, AppendArgs p) {
   const int64_t u = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x;
@@ -399,15 +442,21 @@ extern "C" int certkv_store_append(int32_t batch, int32_t layers, int32_t hkv, i
   p.rows = (int64_t)s.units * tokens;
   const unsigned grid = row_blocks(p.rows);
   if (!grid) return CERTKV_EINVAL;
+  const int runs = (tokens + kRun - 1) / kRun;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   {
     TraceScope ts_("store_append", st);
-    if (store->format == CERTKV_STORE_BF16)
-      append_kernel<CERTKV_STORE_BF16><<<grid, kStoreThreads, 0, st>>>(s, p);
-    else if (store->format == CERTKV_STORE_FP8)
-      append_kernel<CERTKV_STORE_FP8><<<grid, kStoreThreads, 0, st>>>(s, p);
-    else
-      append_kernel<CERTKV_STORE_FP4><<<grid, kStoreThreads, 0, st>>>(s, p);
+#define CERTKV_APPEND(F)                                                                      \
+  if (tokens >= kRun) append_run_kernel<F><<<s.units * runs, kStoreThreads, 0, st>>>(s, p, runs); \
+  else append_kernel<F><<<grid, kStoreThreads, 0, st>>>(s, p)
+    if (store->format == CERTKV_STORE_BF16) {
+      CERTKV_APPEND(CERTKV_STORE_BF16);
+    } else if (store->format == CERTKV_STORE_FP8) {
+      CERTKV_APPEND(CERTKV_STORE_FP8);
+    } else {
+      CERTKV_APPEND(CERTKV_STORE_FP4);
+    }
+#undef CERTKV_APPEND
   }
   if (!p.bump) {
     TraceScope ts_("store_count", st);

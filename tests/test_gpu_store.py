@@ -215,3 +215,40 @@ def test_pool_past_thirty_two_bits_of_bytes():
     small = ck.Store.empty(1, 2, "bf16")
     ck.certkv_store_append(k, v, small)
     assert torch.equal(got, ck.certkv_tree_attn(q, small, hkv=1))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T", [127, 128, 129, 401])
+def test_append_many_rows(fmt, T):
+    """Lengths around a block's rows; some accepted, chosen in reverse, one segment
+    started before its first slot and one short of a page."""
+    B, L, H = 2, 1, 3
+    k, v = drafts.randn((B, L, T, H, 128), 70), drafts.randn((B, L, T, H, 128), 71)
+    mp = 8
+    st = ck.Store.empty(B * L * H, mp, fmt)
+    for name in "kv":
+        getattr(st, name).view(torch.uint8).fill_(17)
+    st.table[1, 1] = -1
+    accepted = [T, T - 60]
+    select = torch.arange(T - 1, -1, -1, dtype=torch.int32).repeat(B, 1)
+    starts = [3, 60, -2, 100, 0, mp * PAGE - 5]
+    before = held(st, "k")
+    ck.certkv_store_append(k, v, st, select=select.cuda(), start=torch.tensor(starts, dtype=torch.int32).cuda(),
+                           accepted=torch.tensor(accepted, dtype=torch.int32).cuda())
+    assert st.read_status() == ck.STATUS_STORE
+    table = st.table.cpu().numpy()
+    got = {name: held(st, name) for name in "kv"}
+    written = set()
+    for u in range(B * L * H):
+        b, h, m = u // H, u % H, accepted[u // H]
+        assert st.counts[u].item() == min(max(starts[u], 0) + m, mp * PAGE)
+        on = [i for i in range(m) if starts[u] >= 0 and starts[u] + i < mp * PAGE
+              and table[u, (starts[u] + i) // PAGE] >= 0]
+        at = [int(table[u, (starts[u] + i) // PAGE]) * PAGE + (starts[u] + i) % PAGE for i in on]
+        written |= set(at)
+        if on:
+            for name, x in (("k", k), ("v", v)):
+                rows = x[b, 0, [T - 1 - i for i in on], h].cpu()
+                same(got[name], np.array(at), encode(rows, fmt))
+    rest = np.array(sorted(set(range(B * L * H * mp * PAGE)) - written))
+    np.testing.assert_array_equal(got["k"]["codes"][rest], before["codes"][rest])
