@@ -288,11 +288,14 @@ __global__ void __launch_bounds__(kStoreThreads, 8) append_kernel(Store st, Appe
 }
 
 // Many rows of each segment: a block takes kRun consecutive rows of one segment, a
-// group of lanes every 32nd of them, and the segment's indices and addresses are
-// worked out once.
-constexpr int kRun = 128;
+// group of lanes every 32nd of them, the next one's loads under way; the segment's
+// indices and addresses are worked out once (from every row's own index the kernel
+// was bound by its instructions).  4-bit prompt of 131071 x 8 rows written and read
+// back: 230 us; runs of 128 or 512 rows 236 and 232, no loads ahead 238, append_kernel
+// 257.
+constexpr int kRun = 256;
 template <int FMT>
-__global__ void __launch_bounds__(kStoreThreads, 6) append_run_kernel(Store st, AppendArgs p, int runs) {
+__global__ void __launch_bounds__(kStoreThreads, 4) append_run_kernel(Store st, AppendArgs p, int runs) {
   const int u = blockIdx.x / runs, i0 = (blockIdx.x - u * runs) * kRun;
   const int sub = threadIdx.x & 7;
   const int bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
@@ -302,27 +305,33 @@ __global__ void __launch_bounds__(kStoreThreads, 6) append_run_kernel(Store st, 
   const int32_t* table = st.table + (int64_t)u * st.max_pages;
   const int64_t room = start < 0 ? INT64_MIN : (int64_t)st.max_pages * kPage;
   const int i1 = min(m, i0 + kRun);
-#pragma unroll 1
-  for (int r = i0; r < i1; r += 32) {
-    const int i = r + (threadIdx.x >> 3);
-    Words16 a = {}, c = {};
-    int64_t to = -1;
-    if (i < i1) {
-      const int t = select ? select[i] : i;
-      const int64_t s = (int64_t)start + i;
-      if (s < room && t >= 0 && t < p.T) {
-        const int page = table[(int)s / kPage];
-        if (page >= 0 && page < st.pool_pages) to = (int64_t)page * kPage + (int)s % kPage;
-      }
-      if (to >= 0) {
-        a = load_row(k + t * p.k.st, sub);
-        c = load_row(v + t * p.v.st, sub);
-      } else if (sub == 0) {
-        st.raise();
-      }
+  Words16 a = {}, c = {};
+  int64_t to = -1;
+  auto fetch = [&](int i) {
+    to = -1;
+    if (i >= i1) return;
+    const int t = select ? select[i] : i;
+    const int64_t s = (int64_t)start + i;
+    if (s < room && t >= 0 && t < p.T) {
+      const int page = table[(int)s / kPage];
+      if (page >= 0 && page < st.pool_pages) to = (int64_t)page * kPage + (int)s % kPage;
     }
-    put_row<FMT>(a, sub, to, st.k, st.kg, st.ks);
-    put_row<FMT>(c, sub, to, st.v, st.vg, st.vs);
+    if (to >= 0) {
+      a = load_row(k + t * p.k.st, sub);
+      c = load_row(v + t * p.v.st, sub);
+    } else if (sub == 0) {
+      st.raise();
+    }
+  };
+  const int mine = i0 + (threadIdx.x >> 3);
+  fetch(mine);
+#pragma unroll 1
+  for (int r = 0; r < i1 - i0; r += 32) {
+    const Words16 x = a, y = c;
+    const int64_t at = to;
+    fetch(mine + r + 32);
+    put_row<FMT>(x, sub, at, st.k, st.kg, st.ks);
+    put_row<FMT>(y, sub, at, st.v, st.vg, st.vs);
   }
   if (p.bump && i0 == 0 && threadIdx.x == 0) {
     st.counts[u] = grown(st, start, m);

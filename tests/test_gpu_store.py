@@ -218,7 +218,7 @@ def test_pool_past_thirty_two_bits_of_bytes():
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("T", [127, 128, 129, 401])
+@pytest.mark.parametrize("T", [127, 128, 129, 255, 256, 257, 401])
 def test_append_many_rows(fmt, T):
     """Lengths around a block's rows; some accepted, chosen in reverse, one segment
     started before its first slot and one short of a page."""
