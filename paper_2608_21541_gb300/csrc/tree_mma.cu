@@ -22,6 +22,14 @@
 // Weights as in the tcgen05 kernel: 2^(x - C), C following the maximum when it
 // grows by more than 2^8; f16 weights carry the value's scale relative to the
 // tile's largest, bf16 ones come in two parts (2^-16).
+//
+// What bounds it, 256 segments of 13107 slots, up to 4 rows: bf16 260 us, the copy
+// bandwidth.  8-bit 156 us; the copies alone, with nothing done to the tiles, 138.
+// 4-bit 155 and 94: the consumers' expansion and products, which eight warps of 168
+// registers on an SM do not overlap further.  Slower were tiles of 32 slots (8-bit
+// 198; with three CTAs per SM 169), values in stages of their own (161, 4-bit 192:
+// their expansion then no longer fills the softmax's gaps) and five consumers with
+// one stage each (4-bit 172).
 #include <cuda.h>
 
 #include "../../include/certkv.h"
@@ -247,7 +255,9 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
   while (items.next(p, &it)) {
     const int bl = it.u / p.H, h = it.u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
     const int row0 = it.blk * p.rb, rows = min(p.rb, p.rows - row0);  // of the block
-    // ---- queries as A fragments
+    // ---- queries as A fragments; for an 8-bit store kept where the warp's sums go
+    // at the end, which makes room for four blocks' keys at a time (161 -> 156 us;
+    // a 4-bit store's keys are half the registers: 155 -> 167)
     uint32_t qa[8][4];
     float sl[2];  // per row: scale of its logits (log2 domain)
 #pragma unroll
@@ -288,6 +298,14 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
           qa[ks][rr + 2] = row ? __ldg(x + 4) : 0u;
         }
       }
+    }
+    float* acc = wacc + cw * kRows * kD;  // this warp's
+    const uint32_t qf = tc::saddr(acc) + (uint32_t)(lane * 16);
+    if (FMT == CERTKV_STORE_FP8) {
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks)
+        *reinterpret_cast<uint4*>(acc + (ks * 32 + lane) * 4) = make_uint4(qa[ks][0], qa[ks][1], qa[ks][2], qa[ks][3]);
+      __syncwarp();
     }
     float C[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f};
     float o[16][4];
@@ -353,32 +371,62 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
             }
           }
         } else if constexpr (FMT == CERTKV_STORE_FP8) {
+          // four blocks at a time: a block's products depend on one another
 #pragma unroll
-          for (int nb = 0; nb < kNb; ++nb) {
-            const int row = 8 * nb + qr;
+          for (int nb = 0; nb < kNb; nb += 4) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const uint4 x = lds128(st + G::kK + (uint32_t)(row * 128 + (((2 * qc + c) ^ (row & 7)) << 4)));
-              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+              uint32_t w[4][4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                mma<false>(sc[nb], qa[4 * c + i], e4m3x2_to_f16x2(w[i] & 0xffffu), e4m3x2_to_f16x2(w[i] >> 16));
+              for (int y = 0; y < 4; ++y) {
+                const int row = 8 * (nb + y) + qr;
+                const uint4 x = lds128(st + G::kK + (uint32_t)(row * 128 + (((2 * qc + c) ^ (row & 7)) << 4)));
+                w[y][0] = x.x;
+                w[y][1] = x.y;
+                w[y][2] = x.z;
+                w[y][3] = x.w;
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint4 q = lds128(qf + (uint32_t)((4 * c + i) * 512));
+                const uint32_t a[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                  mma<false>(sc[nb + y], a, e4m3x2_to_f16x2(w[y][i] & 0xffffu),
+                             e4m3x2_to_f16x2(w[y][i] >> 16));
+              }
             }
           }
         } else {
 #pragma unroll
-          for (int nb = 0; nb < kNb; ++nb) {
-            const int row = 8 * nb + slot_of<FMT>(qr);
-            const uint4 x = lds128(st + G::kK + (uint32_t)(row * 64 + ((qc ^ ((row >> 1) & 3)) << 4)));
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            const uint32_t g2 = e4m3x2_to_f16x2(lds16(st + G::kKg + (uint32_t)(row * kGroups + 2 * qc)));
-            const uint32_t ga = __byte_perm(g2, g2, 0x1010), gb = __byte_perm(g2, g2, 0x3232);
+          for (int nb = 0; nb < kNb; nb += 4) {
+            uint32_t w[4][4], ga[4], gb[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int row = 8 * (nb + y) + slot_of<FMT>(qr);
+              const uint4 x = lds128(st + G::kK + (uint32_t)(row * 64 + ((qc ^ ((row >> 1) & 3)) << 4)));
+              const uint32_t g2 = e4m3x2_to_f16x2(lds16(st + G::kKg + (uint32_t)(row * kGroups + 2 * qc)));
+              w[y][0] = x.x;
+              w[y][1] = x.y;
+              w[y][2] = x.z;
+              w[y][3] = x.w;
+              ga[y] = __byte_perm(g2, g2, 0x1010);
+              gb[y] = __byte_perm(g2, g2, 0x3232);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t g = i < 2 ? ga : gb;
-              mma<false>(sc[nb], qa[2 * i], hmul2(e2m1x2_to_f16x2<0>(w[i]), g), hmul2(e2m1x2_to_f16x2<1>(w[i]), g));
-              mma<false>(sc[nb], qa[2 * i + 1], hmul2(e2m1x2_to_f16x2<2>(w[i]), g),
-                         hmul2(e2m1x2_to_f16x2<3>(w[i]), g));
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                const uint32_t g = i < 2 ? ga[y] : gb[y];
+                mma<false>(sc[nb + y], qa[2 * i], hmul2(e2m1x2_to_f16x2<0>(w[y][i]), g),
+                           hmul2(e2m1x2_to_f16x2<1>(w[y][i]), g));
+              }
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                const uint32_t g = i < 2 ? ga[y] : gb[y];
+                mma<false>(sc[nb + y], qa[2 * i + 1], hmul2(e2m1x2_to_f16x2<2>(w[y][i]), g),
+                           hmul2(e2m1x2_to_f16x2<3>(w[y][i]), g));
+              }
             }
           }
         }
@@ -556,7 +604,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float* a = wacc + (cw * rows + r) * kD;
+        float* a = acc + r * kD;
         a[element_of<FMT>(i, qc, 0)] = o[i][2 * rr];
         a[element_of<FMT>(i, qc, 1)] = o[i][2 * rr + 1];
       }
@@ -574,7 +622,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       for (int w = 0; w < kConsumers; ++w) {
         if (tl->l[w][r] == 0.f) continue;
         const float f = exp2f(tl->m[w][r] - M), g = f * exp2f(tl->e[w][r]);
-        const float4 a = *reinterpret_cast<const float4*>(wacc + (w * rows + r) * kD + d);
+        const float4 a = *reinterpret_cast<const float4*>(wacc + (w * kRows + r) * kD + d);
         L = fmaf(tl->l[w][r], f, L);
         A.x = fmaf(a.x, g, A.x);
         A.y = fmaf(a.y, g, A.y);
