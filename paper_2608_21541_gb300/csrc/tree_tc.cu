@@ -991,20 +991,23 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
     int shift0 = 0;  // exponent the accumulator is relative to
     for (int i = 0; busy && i < steps; ++i) {
       const uint32_t t = t0 + (uint32_t)(PAIR ? i : 2 * i + s);
-      ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[s]), uses & 1u, ab)) &&
-           __all_sync(kFull, tc::mbar_wait(bar(&m->ready[t % kMeta]), (t / kMeta) & 1u, ab));
+      // the tile's facts are there long before its logits: asked for first, the poll
+      // and the reads pass while S is awaited
+      ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->ready[t % kMeta]), (t / kMeta) & 1u, ab));
+      const Meta& mt = m->meta[t % kMeta];
+      const bool whole = mt.whole, own = mt.drafts;
+      const int shift = mt.shift;
+      ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[s]), uses & 1u, ab));
       ++uses;
       if (!ok) break;
       um::fence_after();
-      const Meta& mt = m->meta[t % kMeta];
-      if (!mt.whole) {
-        const bool own = mt.drafts;
+      if (!whole) {
         const uint32_t live[4] = {own ? (uint32_t)word : mt.live[0], own ? (uint32_t)(word >> 32) : mt.live[1],
                                   own ? 0u : mt.live[2], own ? 0u : mt.live[3]};
         mask_tile(tS, live);
       }
-      if (i == 0) shift0 = mt.shift;
-      const float dE = kQuant ? (float)(mt.shift - shift0) : 0.f;
+      if (i == 0) shift0 = shift;
+      const float dE = kQuant ? (float)(shift - shift0) : 0.f;
       row.tile(tS, tO, mt, dE, i > 0);  // O of the tiles before is done (see Issuer)
       um::wait_st();
       um::fence_before();
