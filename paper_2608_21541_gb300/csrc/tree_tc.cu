@@ -1063,9 +1063,12 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
         }
         if (mine) {
 #pragma unroll
-          for (int j = 0; j < 16; j += 4)
-            *reinterpret_cast<uint4*>(p.rec_acc + rec * kD + 16 * c + j) =
-                make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+          for (int j = 0; j < 16; j += 8)  // whole sectors
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
+                             p.rec_acc + rec * kD + 16 * c + j),
+                         "r"(r[j]), "r"(r[j + 1]), "r"(r[j + 2]), "r"(r[j + 3]), "r"(r[j + 4]), "r"(r[j + 5]),
+                         "r"(r[j + 6]), "r"(r[j + 7])
+                         : "memory");
         }
       }
       if (mine) p.rec_ml[rec] = ok ? make_float2(Cj, lj) : make_float2(0.f, __int_as_float(0x7fc00000));
