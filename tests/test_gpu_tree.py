@@ -265,3 +265,23 @@ def test_no_slots_anywhere():
     lse = torch.empty((2, 1, 4, 6), device="cuda")
     out = ck.certkv_tree_attn(q, st, hkv=3, lse=lse)
     assert not out.float().any() and torch.isinf(lse).all() and (lse < 0).all()
+
+
+@pytest.mark.parametrize("fmt,pages", [("bf16", 262144 + 9), ("fp8", 524288 + 9), ("fp4", 1048576 + 9)])
+@pytest.mark.parametrize("T,G", [(1, 4), (9, 16)])
+def test_pool_past_thirty_two_bits_of_bytes(fmt, pages, T, G):
+    """Pages at the end of a pool whose codes pass 2^32 bytes."""
+    small, n = store_with([300, 65], 1, 1, 2, fmt, 290)
+    st = ck.Store.empty(2, small.table.shape[1], fmt, pool_pages=pages)
+    old = [p for p in small.table.flatten().tolist() if p >= 0]
+    new = [pages - 1 - i for i in range(len(old))]
+    for name in ("k", "v", "k_scale", "v_scale", "k_group", "v_group"):
+        a, b = getattr(small, name), getattr(st, name)
+        if a is not None:
+            b.view(torch.uint8)[new] = a.view(torch.uint8)[old]
+    move = dict(zip(old, new))
+    st.table.copy_(torch.tensor([[move.get(p, -1) for p in row] for row in small.table.tolist()]))
+    st.counts.copy_(small.counts)
+    q = randn((1, 1, T, 2 * G, 128), 1)
+    kw = dict(hkv=2)
+    assert torch.equal(ck.certkv_tree_attn(q, st, **kw), ck.certkv_tree_attn(q, small, **kw))
