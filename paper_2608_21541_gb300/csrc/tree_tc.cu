@@ -56,7 +56,7 @@ constexpr int kPieces = 128 * 8 / (kGroupWarps * 32), kStep = 128 / kPieces;
 // Registers a thread: the launch gives 96 (640 threads), which the roles share
 // out among themselves.  A spill costs more here than elsewhere: next to 200 KB
 // of shared memory the L1 holds hardly any of it.
-constexpr int kSoftRegs = 112, kLoadRegs = 96, kIssueRegs = 56;
+constexpr int kSoftRegs = 120, kLoadRegs = 88, kIssueRegs = 64;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
               "a larger split would wait for registers for ever");
 constexpr int kHalf = 128 * 128;     // bytes of 128 rows x 64 16-bit elements
