@@ -23,6 +23,7 @@
 namespace certkv {
 
 // One block: first[u] = tiles of the segments before u, first[units] their sum.
+// Latency of one launch; only for more segments than kInlineUnits.
 __global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int tile, int with_drafts,
                                                          int64_t* __restrict__ first) {
   __shared__ long long wsum[32];
@@ -61,6 +62,10 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(Store st, int tile, int
   if (threadIdx.x == 0) first[st.units] = carry;
 }
 
+// Bound by the records' bytes where there are many (32 segments of 256 rows, 24 MB
+// from DRAM: 13 us) and by the latency of a launch else; four records' loads are in
+// flight at a time.
+//
 // One warp per (unit, row), a lane four dimensions: the records of the CTAs that
 // met the row's block, each weighted by its sum 2^C l, and what the split left
 // out: the NaN and infinite elements of drafts the row sees.
