@@ -84,7 +84,17 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
     const int64_t per = tiles_per_cta(p, p.first), at = p.first[u] * p.nblk + blk * n;
     const int64_t vu = (int64_t)u * p.nblk + blk;
     const int c0 = (int)(at / per), c1 = (int)((at + n - 1) / per);
-    for (int c = c0; c <= c1; c += 4) {
+    if (c0 == c1) {  // one record, as where segments are short: as it is
+      const int64_t rec = (c0 + vu) * p.rb + br;
+      const float2 ml = p.rec_ml[rec];
+      const float4 a = *reinterpret_cast<const float4*>(p.rec_acc + rec * kD + 4 * lane);
+      if (ml.y != 0.f) {
+        M = ml.x;
+        L = ml.y;
+        A = make_float4(a.x * L, a.y * L, a.z * L, a.w * L);
+      }
+    }
+    for (int c = c0; c0 < c1 && c <= c1; c += 4) {
       float2 ml[4];
       float4 a[4];
       float m = M;
