@@ -50,6 +50,7 @@
 
 #include "../../include/certkv.h"
 #include "common.cuh"
+#include "follow.cuh"
 #include "internal.cuh"
 #include "tma.cuh"
 #include "tree.cuh"
@@ -119,6 +120,7 @@ struct Misc {
   uint64_t group[kLoadGroups];               // barriers of the loader groups
   uint32_t tmem;
   int abort;
+  uint32_t walked;  // tiles stated so far (8- and 4-bit stores)
   unsigned long long odd[kLoadGroups];
   float red[kLoadWarps];
   float qs[256];                   // per row: scale of its f16 queries
@@ -418,7 +420,10 @@ struct Scout {
       mt.first_block = it.blk == 0;
     }
     __syncwarp();
-    if (lane == 0) tc::mbar_arrive(bar(&m->stated[t % kMeta]));
+    if (lane == 0) {
+      tc::mbar_arrive(bar(&m->stated[t % kMeta]));
+      if (kQuant) *(volatile uint32_t*)&m->walked = t + 1;
+    }
     ++k;
     fetch();
   }
@@ -470,7 +475,8 @@ struct Scout {
     drain(n, copies);
   }
   // 8- and 4-bit stores, a warp of its own (a bulk prefetch is slow to issue): as
-  // tile t is stated, the pages kAhead tiles on are brought into L2.
+  // tile t is stated, the pages kAhead tiles on are brought into L2.  Only a help: it
+  // holds nobody up and never aborts.
   __device__ __forceinline__ void run_ahead(uint32_t n) {
     it.kb = 0;
     for (uint32_t t = 0; t < n && ok; ++t, ++k) {
@@ -481,7 +487,10 @@ struct Scout {
       advance();
       prefetch_page(2 * (k + kAhead));
       prefetch_page(2 * (k + kAhead) + 1);
-      ok = __all_sync(kFull, tc::mbar_wait(bar(&m->stated[t % kMeta]), (t / kMeta) & 1u, &m->abort));
+      // nobody waits for this warp: see follow.cuh
+      ok = __all_sync(kFull, follow(
+                                 t, tc::kSpinLimit, [&] { return *(volatile uint32_t*)&m->walked; },
+                                 [&] { return *(volatile int*)&m->abort != 0; }, [] { __nanosleep(64); }));
     }
   }
   // The values of a bf16 store, by a warp of their own: a poll takes hundreds of
@@ -1127,6 +1136,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     tc::mbar_init(bar(&m->q_full), kSoftWarps);
     tc::mbar_init(bar(&m->done), 1);
     m->abort = 0;
+    m->walked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   release_next();
