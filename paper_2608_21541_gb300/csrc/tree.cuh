@@ -26,6 +26,25 @@ __host__ __device__ constexpr int small_tile(int format) {
 }
 constexpr float kLn2 = 0.69314718055994531f;
 
+// 8- and 4-bit stores: a weight meets the codes as an f16 operand that carries the scale of
+// its value row, 2^(x - E) vs.  The reference E of a row follows the largest of x + log2 vs, so
+// that what counts most in the sum is what f16 holds best, however much value rows differ in
+// size and whatever weight falls on rows that are zero.
+constexpr float kHead = 6.f;  // the largest operand is below 2^kHead when E is taken from it
+// log2 of a value scale, low by at most 0.09 (its bits read as a fixed-point number).  Not
+// below -74, and that for a scale of 0 (nothing in the row) or NaN (no reference helps): E is
+// then within 80 of the largest logit x, and the fp32 sum of 2^(x - E) finite.
+__device__ __forceinline__ float log2_scale(float s) {
+  const int b = __float_as_int(s);
+  return b < 0x7f800000 ? fmaxf(fmaf((float)b, 1.1920929e-7f, -127.f), -74.f) : -74.f;
+}
+// The store holds a row of zeros with scale 1.  Whether anything of such a row is left: codes
+// that are not +0 or -0, of the four bytes each.
+template <int FMT>
+__device__ __forceinline__ uint32_t nonzero_codes(uint32_t four) {
+  return four & (FMT == CERTKV_STORE_FP8 ? 0x7f7f7f7fu : 0x77777777u);
+}
+
 struct TreeArgs {
   int L, H, G, T;     // layers, KV heads, query heads per KV head, drafted tokens
   int units, rows;    // B L H, T G query rows per unit

@@ -19,9 +19,10 @@
 // accumulator per row; where the CTA's share passes into the next unit they are
 // joined into one record.  Two CTAs per SM.
 //
-// Weights as in the tcgen05 kernel: 2^(x - C), C following the maximum when it
-// grows by more than 2^8; f16 weights carry the value's scale relative to the
-// tile's largest, bf16 ones come in two parts (2^-16).
+// Weights 2^(x - C), C following the maximum when it grows by more than 2^8.  bf16
+// ones come in two parts (2^-16).  f16 ones carry their value row's scale and are
+// rounded once (2^-11), C following the largest of those products (log2_scale);
+// codes are exact.
 //
 // What bounds it, 256 segments of 13107 slots, up to 4 rows: bf16 260 us, the copy
 // bandwidth.  8-bit 156 us; the copies alone, with nothing done to the tiles, 138.
@@ -99,6 +100,14 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 __device__ __forceinline__ float lds32f(uint32_t a) {
   float x;
   asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(a));
+  return x;
+}
+__device__ __forceinline__ void sts32f(uint32_t a, float x) {
+  asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(x) : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t x;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(a));
   return x;
 }
 __device__ __forceinline__ uint32_t lds16(uint32_t a) {
@@ -301,6 +310,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
     }
     float* acc = wacc + cw * kRows * kD;  // this warp's
     const uint32_t qf = tc::saddr(acc) + (uint32_t)(lane * 16);
+    const uint32_t lv = tc::saddr(acc) + kRows * kD * 2;  // a tile's log2_scale, behind the queries
     if (FMT == CERTKV_STORE_FP8) {
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks)
@@ -311,8 +321,6 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
     float o[16][4];
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    int e0 = 0;
-    bool begun = false;
     const int n = it.kb - it.ka;
     for (int k = (int)((cw - tile % kConsumers + kConsumers) % kConsumers); k < n; k += kConsumers) {
       const int64_t ti = tile + k;
@@ -336,21 +344,33 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
             for (int i = live * kGroups + lane; i < G::kSlots * kGroups; i += 32) smem[s * G::kStage + G::kVg + i] = 0;
           __syncwarp();
         }
-        // ---- exponent of the tile's largest value scale (a NaN left out)
-        float dE = 0.f, down = 1.f;
+        // ---- logarithms of the value scales (see tree.cuh)
+        bool zeroed = live < G::kSlots;
         if (kQuant) {
-          float x = 0.f;
+          uint32_t one[G::kSlots / 32];  // slots of scale 1: whether they are zero
 #pragma unroll
           for (int i = 0; i < G::kSlots / 32; ++i) {
-            const int sl_ = lane + 32 * i;
-            if (sl_ < live) x = fmaxf(x, lds32f(st + G::kVs + 4 * sl_));
+            const uint32_t at = 4u * (lane + 32 * i);
+            const float x = lane + 32 * i < live ? lds32f(st + G::kVs + at) : 0.f;
+            if (lane + 32 * i >= live) sts32f(st + G::kVs + at, 0.f);
+            sts32f(lv + at, log2_scale(x));
+            one[i] = __ballot_sync(kFull, x == 1.f);
           }
 #pragma unroll
-          for (int i = 16; i >= 1; i >>= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, i));
-          const int e = x < INFINITY ? min(max(exponent(x) + 1, -120), 120) : 0;
-          if (!begun) e0 = e;
-          dE = (float)(e - e0);
-          down = pow2(-e);
+          for (int i = 0; i < G::kSlots / 32; ++i) {
+            for (; one[i]; one[i] &= one[i] - 1) {
+              const int r = 32 * i + __ffs(one[i]) - 1;
+              constexpr int kRow = row_bytes(FMT);
+              const uint32_t c = 4 * lane < kRow ? lds32(st + (uint32_t)(G::kV + r * kRow + 4 * lane)) : 0u;
+              if (__any_sync(kFull, nonzero_codes<FMT>(c) != 0u)) continue;
+              zeroed = true;
+              if (lane == (r & 31)) {
+                sts32f(st + G::kVs + 4u * r, 0.f);
+                sts32f(lv + 4u * r, log2_scale(0.f));
+              }
+            }
+          }
+          __syncwarp();
         }
         // ---- S = Q K^T
         float sc[kNb][4];
@@ -432,7 +452,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
         }
         // ---- weights; this thread's slots of block nb: columns 2 qc, 2 qc + 1
         const int c0 = slot_of<FMT>(2 * qc), c1 = slot_of<FMT>(2 * qc + 1);
-        float mx[2] = {-INFINITY, -INFINITY};
+        float mx[2] = {-INFINITY, -INFINITY};  // of the products, or of x + log2 vs
 #pragma unroll
         for (int nb = 0; nb < kNb; ++nb) {
           if (kQuant) {
@@ -446,26 +466,40 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
             if (8 * nb + c0 >= live) sc[nb][0] = sc[nb][2] = -INFINITY;
             if (8 * nb + c1 >= live) sc[nb][1] = sc[nb][3] = -INFINITY;
           }
-          mx[0] = um::max3(mx[0], sc[nb][0], sc[nb][1]);
-          mx[1] = um::max3(mx[1], sc[nb][2], sc[nb][3]);
+          if (kQuant) {
+            const float l0 = lds32f(lv + 4 * (8 * nb + c0)), l1 = lds32f(lv + 4 * (8 * nb + c1));
+            mx[0] = um::max3(mx[0], fmaf(sc[nb][0], sl[0], l0), fmaf(sc[nb][1], sl[0], l1));
+            mx[1] = um::max3(mx[1], fmaf(sc[nb][2], sl[1], l0), fmaf(sc[nb][3], sl[1], l1));
+          } else {
+            mx[0] = um::max3(mx[0], sc[nb][0], sc[nb][1]);
+            mx[1] = um::max3(mx[1], sc[nb][2], sc[nb][3]);
+          }
         }
         float f[2], off[2];
 #pragma unroll
         for (int rr = 0; rr < 2; ++rr) {
           mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(kFull, mx[rr], 1));
           mx[rr] = fmaxf(mx[rr], __shfl_xor_sync(kFull, mx[rr], 2));
-          const float x = fmaf(mx[rr], sl[rr], dE - (kQuant ? 6.f : 0.f));
+          const float x = kQuant ? ceilf(mx[rr] - kHead) : mx[rr] * sl[rr];
           f[rr] = 1.f;
           if (x > C[rr] + kLazy || C[rr] == -INFINITY) {
             const float nc = fmaxf(x, C[rr]);
-            if (C[rr] > -INFINITY) f[rr] = um::ex2(C[rr] - nc);
+            // quantised: of half the step, as a step of 2^127 and more, whose factor is 0, may
+            // leave much of a sum
+            if (C[rr] > -INFINITY) f[rr] = um::ex2((kQuant ? 0.5f : 1.f) * (C[rr] - nc));
             C[rr] = nc;
           }
-          off[rr] = dE - (C[rr] == -INFINITY ? 0.f : C[rr]);
+          off[rr] = C[rr] == -INFINITY ? 0.f : -C[rr];
         }
         if (__any_sync(kFull, f[0] != 1.f || f[1] != 1.f)) {
           ls[0] *= f[0];
           ls[1] *= f[1];
+          if (kQuant) {
+            ls[0] *= f[0];
+            ls[1] *= f[1];
+            f[0] *= f[0];
+            f[1] *= f[1];
+          }
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             o[i][0] *= f[0];
@@ -484,21 +518,15 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
           sum0 += sc[nb][0] + sc[nb][1];
           sum1 += sc[nb][2] + sc[nb][3];
           if (kQuant) {
-            float v0 = lds32f(st + G::kVs + 4 * (8 * nb + c0)) * down, v1 = lds32f(st + G::kVs + 4 * (8 * nb + c1)) * down;
-            if (live < G::kSlots) {
-              if (8 * nb + c0 >= live) v0 = 0.f;
-              if (8 * nb + c1 >= live) v1 = 0.f;
-            }
+            const float v0 = lds32f(st + G::kVs + 4 * (8 * nb + c0)), v1 = lds32f(st + G::kVs + 4 * (8 * nb + c1));
             sc[nb][0] *= v0;
             sc[nb][1] *= v1;
             sc[nb][2] *= v0;
             sc[nb][3] *= v1;
           }
         }
-        const float back = kQuant ? um::ex2(-dE) : 1.f;
-        ls[0] = fmaf(sum0, back, ls[0]);
-        ls[1] = fmaf(sum1, back, ls[1]);
-        begun = true;
+        ls[0] += sum0;
+        ls[1] += sum1;
         // ---- O += P V, sixteen slots a k-step
 #pragma unroll
         for (int kb = 0; kb < kNb / 2; ++kb) {
@@ -585,12 +613,13 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
           }
         }
         // zeros written above come before the next copy into the stage
-        if (live < G::kSlots) um::fence_async();
+        if (zeroed) um::fence_async();
       }
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bar(&tl->empty[s]));
     }
-    // ---- join the consumers: sums relative to 2^C, accumulators to 2^(C + e0)
+    // ---- join the consumers: sums and accumulators relative to 2^C; a quantised store's C
+    // goes with the values, so a sum's own exponent is taken into its reference
 #pragma unroll
     for (int rr = 0; rr < 2; ++rr) {
       ls[rr] += __shfl_xor_sync(kFull, ls[rr], 1);
@@ -598,9 +627,10 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       const int r = qr + 8 * rr;
       if (r >= rows) continue;
       if (qc == 0) {
-        tl->m[cw][r] = C[rr];
-        tl->l[cw][r] = ls[rr];
-        tl->e[cw][r] = (float)e0;
+        const int e = kQuant ? exponent(ls[rr]) : 0;
+        tl->m[cw][r] = C[rr] + (float)e;
+        tl->l[cw][r] = ls[rr] * pow2(-e);
+        tl->e[cw][r] = (float)e;
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -621,7 +651,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
 #pragma unroll
       for (int w = 0; w < kConsumers; ++w) {
         if (tl->l[w][r] == 0.f) continue;
-        const float f = exp2f(tl->m[w][r] - M), g = f * exp2f(tl->e[w][r]);
+        const float x = tl->m[w][r] - M, f = exp2f(x), g = kQuant ? exp2f(x - tl->e[w][r]) : f;
         const float4 a = *reinterpret_cast<const float4*>(wacc + (w * kRows + r) * kD + d);
         L = fmaf(tl->l[w][r], f, L);
         A.x = fmaf(a.x, g, A.x);
