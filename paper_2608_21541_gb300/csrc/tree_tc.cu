@@ -25,13 +25,14 @@
 //
 // Precision.  bf16 store: bf16 products, and a weight enters P V as a bf16 part
 // plus the bf16 rounding of its remainder (2^-16).  8- and 4-bit stores: codes
-// are exact in f16, so are query rows once divided by a power of two; a key's
-// fp32 scale multiplies its logit; a value is rounded once to f16 (2^-11) with
-// its scale taken relative to the tile's largest, and a weight once to f16.
-// Logits, sums, and accumulators are fp32.  A weight is 2^(x - C) for a
-// reference C that moves to the row's maximum only when weights would leave
-// their range (f16: 2^15), so that most tiles are formed in one pass over the
-// logits, without their maximum and without rescaling.
+// are exact in f16, so are query rows once divided by a power of two (elements
+// within 2^-17 of the row's largest; smaller ones to 2^-25 of it); a key's fp32
+// scale multiplies its logit, a value's fp32 scale the weight, and that product is
+// rounded once to f16 (2^-11).  Logits, sums, and accumulators are fp32.  A weight
+// is 2^(x - C) for a reference C that moves to the row's maximum (of the products,
+// where they are what is rounded: log2_scale) only when the operand would leave
+// its range (f16: 2^15), so that most tiles are formed in one pass over the logits,
+// without their maximum and without rescaling.
 //
 // What bounds it, 256 segments of 13107 slots: a bf16 store of 64 rows 280 us, 91 %
 // of the copy bandwidth, of 256 rows 495, 46 % of the tensor rate.  8- and 4-bit
@@ -67,7 +68,7 @@ constexpr int kPieces = 128 * 8 / (kGroupWarps * 32), kStep = 128 / kPieces;
 // Registers a thread: the launch gives 96 (640 threads), which the roles share
 // out among themselves.  A spill costs more here than elsewhere: next to 200 KB
 // of shared memory the L1 holds hardly any of it.
-constexpr int kSoftRegs = 120, kLoadRegs = 88, kIssueRegs = 64;
+constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
               "a larger split would wait for registers for ever");
 constexpr int kHalf = 128 * 128;     // bytes of 128 rows x 64 16-bit elements
@@ -102,11 +103,11 @@ constexpr uint32_t kColS = 0, kColO = 256;  // + 128 stream
 constexpr uint32_t kMeta = 8;
 struct alignas(16) Meta {  // its arrays are read and written as float4
   float ks[kTreeTile];  // scale of each slot's key (8- and 4-bit stores)
-  float vf[kTreeTile];  // scale of each slot's value over 2^shift
+  float vs[kTreeTile];  // scale of each slot's value, 0 where the row is zero
+  float lv[kTreeTile];  // log2_scale of it
   uint32_t live[4];     // slots to take
   int a, b;             // the tile's pages (-1: none)
   int count;            // live slots from the tile's first on
-  int shift;            // exponent the tile's values are divided by
   int whole;            // every slot is live
   int drafts;           // the drafts' own tile: live comes from the row's mask
   int unit, first_block;
@@ -122,9 +123,8 @@ struct Misc {
   int abort;
   uint32_t walked;  // tiles stated so far (8- and 4-bit stores)
   unsigned long long odd[kLoadGroups];
-  float red[kLoadWarps];
   float qs[256];                   // per row: scale of its f16 queries
-  float cm[128], l[128], sh[128];  // stream 1's reference, sum and shift
+  float cm[128], l[128];           // stream 1's reference and sum
   Meta meta[kMeta];
   int64_t first[kInlineUnits + 1];  // see tree_first
 };
@@ -247,23 +247,14 @@ struct Raw {
   }
 };
 
-// Piece q as f16: codes with their group scale, and for values times f.
-template <int FMT, bool VALUE>
-__device__ __forceinline__ void expand(const Raw<FMT>& r, int q, float f, uint32_t (&w)[8]) {
+// Piece q as f16: codes, with their group scale (exact).
+template <int FMT>
+__device__ __forceinline__ void expand(const Raw<FMT>& r, int q, uint32_t (&w)[8]) {
   if constexpr (FMT == CERTKV_STORE_FP8) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[j] = e4m3x2_to_f16x2(r.w[q][j >> 1] >> (16 * (j & 1)));
-    if (VALUE) {
-      const uint32_t f2 = pack_f16(f, f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = hmul2(w[j], f2);
-    }
   } else {
-    uint32_t f2 = e4m3x2_to_f16x2(r.g[q] | (r.g[q] << 8));
-    if (VALUE) {
-      const float x = f16x2_to_f32(f2).x * f;
-      f2 = pack_f16(x, x);
-    }
+    const uint32_t f2 = e4m3x2_to_f16x2(r.g[q] | (r.g[q] << 8));
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       w[4 * j] = hmul2(e2m1x2_to_f16x2<0>(r.w[q][j]), f2);
@@ -273,10 +264,10 @@ __device__ __forceinline__ void expand(const Raw<FMT>& r, int q, float f, uint32
     }
   }
 }
-
-// Exponent that brings the largest magnitude t to 2^13 .. 2^14.
-__device__ __forceinline__ int shift_of(float t) {
-  return t > 0.f && t < INFINITY ? min(max(exponent(t) - 13, -110), 114) : 0;
+// Exponent a draft's value row is divided by: its elements then reach as far as codes do.
+template <int FMT>
+__device__ __forceinline__ int draft_shift(float largest) {
+  return min(max(exponent(largest) - (FMT == CERTKV_STORE_FP8 ? 8 : 11), -120), 120);
 }
 
 // ----------------------------------------------------------------- scout --
@@ -373,6 +364,37 @@ struct Scout {
     lo = entry(at + lane);
     hi = entry(at + 32 + lane);
   }
+  // Scale 0 for the rows of tile k that are zero.  The four rows of a lane's scales lie
+  // behind one another; the warp reads them together, for the lanes that have a scale of 1.
+  __device__ __forceinline__ void find_zeros() {
+    constexpr int kLanes = row_bytes(FMT) / 16;  // of a row, 16 bytes each
+    uint32_t some = __ballot_sync(kFull, vs.x == 1.f || vs.y == 1.f || vs.z == 1.f || vs.w == 1.f);
+    while (some) {  // two lanes' rows at a time: a look takes the way to L2
+      uint4 x[2];
+      int of[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        of[i] = __ffs(some) - 1;
+        const int64_t row = (int64_t)(of[i] < 16 ? a : b) * kPage + (4 * of[i]) % kPage;
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (of[i] >= 0 && lane < 4 * kLanes)
+          x[i] = __ldg(reinterpret_cast<const uint4*>(p.st.v + row * row_bytes(FMT)) + lane);
+        some &= some - 1;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t on = __ballot_sync(kFull, nonzero_codes<FMT>(x[i].x | x[i].y | x[i].z | x[i].w) != 0u);
+        constexpr uint32_t kRow = (1u << kLanes) - 1u;
+        if (lane == of[i]) {
+          if (vs.x == 1.f && !(on & kRow)) vs.x = 0.f;
+          if (vs.y == 1.f && !(on >> kLanes & kRow)) vs.y = 0.f;
+          if (vs.z == 1.f && !(on >> 2 * kLanes & kRow)) vs.z = 0.f;
+          if (vs.w == 1.f && !(on >> 3 * kLanes & kRow)) vs.w = 0.f;
+        }
+        __syncwarp();
+      }
+    }
+  }
   // State tile t, the next of the walk.
   __device__ __forceinline__ void state(uint32_t t) {
     if (k == it.kb) {
@@ -386,17 +408,12 @@ struct Scout {
     Meta& mt = m->meta[t % kMeta];
     if (k < stored) {
       const int live = count - k * kTreeTile;
-      int shift = 0;
-      if (kQuant) {
-        // from the tile's largest row maximum, a NaN left out
-        float x = fmaxf(fmaxf(vs.x, vs.y), fmaxf(vs.z, vs.w));
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kFull, x, o));
-        shift = shift_of(x * (FMT == CERTKV_STORE_FP8 ? 448.f : 2688.f));
-        const float down = pow2(-shift);
+      if constexpr (kQuant) {
+        find_zeros();
         *reinterpret_cast<float4*>(&mt.ks[4 * lane]) = ks;
-        *reinterpret_cast<float4*>(&mt.vf[4 * lane]) =
-            make_float4(vs.x * down, vs.y * down, vs.z * down, vs.w * down);
+        *reinterpret_cast<float4*>(&mt.vs[4 * lane]) = vs;
+        *reinterpret_cast<float4*>(&mt.lv[4 * lane]) =
+            make_float4(log2_scale(vs.x), log2_scale(vs.y), log2_scale(vs.z), log2_scale(vs.w));
       }
       if (lane < 4) {
         const int c = min(max(live - 32 * lane, 0), 32);
@@ -406,7 +423,6 @@ struct Scout {
         mt.a = a;
         mt.b = b;
         mt.count = live;
-        mt.shift = shift;
         mt.whole = live >= kTreeTile && a >= 0 && b >= 0;
         mt.drafts = 0;
         if (a < 0 || (b < 0 && live > kPage)) p.st.raise();
@@ -552,7 +568,6 @@ struct Loader {
   // Keys of the drafts' own tile and the facts that follow from its rows.
   __device__ __forceinline__ void draft_keys(uint32_t to, Meta& mt) {
     const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
-    uint32_t top = 0;
     if (tid == 0) m->odd[group] = 0ull;
     group_sync();
 #pragma unroll 1
@@ -564,25 +579,21 @@ struct Loader {
         load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
       }
       if (finite_only(v)) atomicOr(&m->odd[group], 1ull << (s & 63));
-      top = max(top, top16(v));
       if (kQuant) {
+        const float top = __uint_as_float(Piece::row_max(top16(v)));
+        const float f = top > 0.f ? pow2(draft_shift<kRawFmt>(top)) : 0.f;
+        if (pc.sub == 0) {
+          mt.vs[s] = f;
+          mt.lv[s] = log2_scale(f);
+        }
         const int e = min(max(exponent(__uint_as_float(Piece::row_max(top16(k)))), -120), 120);
         to_f16(k, pow2(-e));
         if (pc.sub == 0) mt.ks[s] = pow2(e);
       }
       pc.put(to, q, k);
     }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
-    if ((tid & 31) == 0) m->red[group * kGroupWarps + (tid >> 5)] = __uint_as_float(top);
     group_sync();
-    if (tid == 0) {
-      float x = 0.f;
-#pragma unroll
-      for (int q = 0; q < kGroupWarps; ++q) x = fmaxf(x, m->red[group * kGroupWarps + q]);
-      mt.shift = kQuant ? shift_of(x) : 0;
-      if (mt.first_block) p.odd[u] = m->odd[group];
-    }
+    if (tid == 0 && mt.first_block) p.odd[u] = m->odd[group];
   }
   __device__ __forceinline__ void draft_values(uint32_t to, const Meta& mt) {
     const int u = mt.unit, bl = u / p.H, h = u - bl * p.H, b = bl / p.L, l = bl - b * p.L;
@@ -593,7 +604,7 @@ struct Loader {
       if (s < p.T) {
         load32g(p.vn.at(b, l, s, h) + pc.sub * 16, v);
         finite_only(v);
-        if (kQuant) to_f16(v, pow2(-mt.shift));
+        if (kQuant) to_f16(v, mt.vs[s] > 0.f ? 1.f / mt.vs[s] : 0.f);  // a power of two
       }
       pc.put(to, q, v);
     }
@@ -621,7 +632,7 @@ struct Loader {
       Raw<kRawFmt> raw;
       if (kQuant && !own)
         raw.load(pc, mt.a, mt.b, mt.count, value ? p.st.v : p.st.k, value ? p.st.vg : p.st.kg);
-      // values of the drafts: their exponent comes from the group that had the keys
+      // values of the drafts: their scales come from the group that had the keys
       if (own && value) wait(&m->ready[t % kMeta], (t / kMeta) & 1u);
       const Place<PAIR> pl(i);
       wait(&m->empty[pl.slot], pl.phase ^ 1u);
@@ -632,20 +643,11 @@ struct Loader {
         if (value) draft_values(to, mt);
         else draft_keys(to, mt);
       } else if (kQuant) {
-        if (value) {
 #pragma unroll
-          for (int q = 0; q < kPieces; ++q) {
-            uint32_t w[8];
-            expand<kRawFmt, true>(raw, q, mt.vf[pc.grp + kStep * q], w);
-            pc.put(to, q, w);
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < kPieces; ++q) {
-            uint32_t w[8];
-            expand<kRawFmt, false>(raw, q, 0.f, w);
-            pc.put(to, q, w);
-          }
+        for (int q = 0; q < kPieces; ++q) {
+          uint32_t w[8];
+          expand<kRawFmt>(raw, q, w);
+          pc.put(to, q, w);
         }
       } else {
         wrote = !mt.whole;
@@ -784,11 +786,12 @@ __device__ __forceinline__ void mask_tile(uint32_t tS, const uint32_t (&live)[4]
   um::wait_st();
 }
 
-// The largest logit of a row over a tile, from tensor memory; SCALE: times the
-// keys' scales.
-template <bool SCALE>
-__device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt) {
+// The largest logit of a row over a tile, from tensor memory (times the scale sl only where
+// QUANT: there with log2 of the value's scale added).
+template <bool QUANT>
+__device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt, float sl) {
   float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+  const float2 sl2 = make_float2(sl, sl);
 #pragma unroll 1
   for (int c = 0; c < 4; ++c) {
     uint32_t r[32];
@@ -797,10 +800,11 @@ __device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt) {
     for (int j = 0; j < 32; j += 4) {
       float2 x = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
       float2 y = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-      if (SCALE) {
+      if (QUANT) {
         const float4 k4 = *reinterpret_cast<const float4*>(&mt.ks[32 * c + j]);
-        x = fmul2(x, make_float2(k4.x, k4.y));
-        y = fmul2(y, make_float2(k4.z, k4.w));
+        const float4 l4 = *reinterpret_cast<const float4*>(&mt.lv[32 * c + j]);
+        x = ffma2(fmul2(x, make_float2(k4.x, k4.y)), sl2, make_float2(l4.x, l4.y));
+        y = ffma2(fmul2(y, make_float2(k4.z, k4.w)), sl2, make_float2(l4.z, l4.w));
       }
       if (j & 4) {
         m0 = um::max3(m0, x.x, x.y);
@@ -817,26 +821,28 @@ __device__ __forceinline__ float tile_max(uint32_t tS, const Meta& mt) {
 // A row's running reference, sum and accumulator over the tiles it has met.
 template <bool QUANT>
 struct Row {
-  float C = -INFINITY;  // reference (an integer; log2 domain, less 6 bits of head room for f16)
+  float C = -INFINITY;  // reference (an integer; log2 domain)
   float lsum = 0.f;     // sum of the weights relative to it
   float sl;             // scale of the row's logits, > 0
 
-  // Largest sum of 32 weights that needs no new reference: within f16's range, or
-  // far within fp32's and bf16's.
-  static constexpr float kLimit = QUANT ? 32768.f : 1.152921504606847e18f;
-  __device__ __forceinline__ float reference(float mx, float dE) const {
-    return ceilf(fmaf(mx, sl, dE - (QUANT ? 6.f : 0.f)));  // -inf stays
+  // Largest sum of 32 weights that needs no new reference: far within fp32's and bf16's
+  // range.  QUANT: and the largest f16 operand below 2^15 (kTop, as bits of two).
+  static constexpr float kLimit = QUANT ? 1.237940039285380e27f : 1.152921504606847e18f;
+  static constexpr uint32_t kTop = 0x78007800u;
+  // from what tile_max gives
+  __device__ __forceinline__ float reference(float mx) const {
+    return ceilf(QUANT ? mx - kHead : mx * sl);  // -inf stays
   }
-  __device__ __forceinline__ float offset(float dE) const { return dE - (C == -INFINITY ? 0.f : C); }
+  __device__ __forceinline__ float offset() const { return C == -INFINITY ? 0.f : -C; }
 
   // Weights of columns 32 c ..: the packed A operand in hi (and remainders in
-  // lo); returns their sum.  The keys' scales are fetched before the logits,
-  // while nothing waits for them.
+  // lo); returns their sum, and in `top` the largest operand of each half (QUANT).  The
+  // keys' scales are fetched before the logits, while nothing waits for them.
   __device__ __forceinline__ float chunk(uint32_t tS, int c, const Meta& mt, float off, uint32_t (&hi)[16],
-                                         uint32_t (&lo)[16]) const {
+                                         uint32_t (&lo)[16], uint32_t& top) const {
     const float2 sl2 = make_float2(sl, sl), off2 = make_float2(off, off);
     float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
-    float4 k4[8];
+    float4 k4[8], v4;
     if (QUANT) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) k4[j] = *reinterpret_cast<const float4*>(&mt.ks[32 * c + 4 * j]);
@@ -854,7 +860,10 @@ struct Row {
       if (j & 1) sum1 = fadd2(sum1, x);
       else sum0 = fadd2(sum0, x);
       if (QUANT) {
+        if (!(j & 1)) v4 = *reinterpret_cast<const float4*>(&mt.vs[32 * c + 2 * j]);
+        x = fmul2(x, j & 1 ? make_float2(v4.z, v4.w) : make_float2(v4.x, v4.y));
         hi[j] = pack_f16(x.x, x.y);
+        if (j & 1) top = __vimax3_u16x2(top, hi[j - 1], hi[j]);  // none is negative
       } else {
         hi[j] = pack_bf16(x.x, x.y);
         lo[j] = pack_bf16(x.x - bf16lo(hi[j]), x.y - bf16hi(hi[j]));
@@ -866,24 +875,32 @@ struct Row {
   // A new reference from columns 32 c .. of the tile for a row that needs one
   // (`over`): its accumulator, its sums and the weights of the tile's earlier
   // columns are scaled to it (by a power of two).  `acc`: there is an accumulator.
-  __device__ __forceinline__ void regrow(uint32_t tS, uint32_t tO, int c, const Meta& mt, float dE, bool over,
-                                         bool acc, float& sum) {
+  __device__ __forceinline__ void regrow(uint32_t tS, uint32_t tO, int c, const Meta& mt, bool over, bool acc,
+                                         float& sum) {
     float mx = -INFINITY;
     um::wait_st();  // earlier columns' weights are read back below
     {
       uint32_t r[32];
       um::ld32(tS + 32u * c, r);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) mx = fmaxf(mx, __uint_as_float(r[j]) * (QUANT ? mt.ks[32 * c + j] : 1.f));
+      for (int j = 0; j < 32; ++j) {
+        const float x = __uint_as_float(r[j]);
+        mx = fmaxf(mx, QUANT ? fmaf(x * mt.ks[32 * c + j], sl, mt.lv[32 * c + j]) : x);
+      }
     }
-    const float nc = reference(mx, dE);
+    const float nc = reference(mx);
     float f = 1.f;
     if (over && nc > C) {
-      f = um::ex2(C - nc);
+      // the factor of a step of 2^127 and more is 0, but may leave much of a quantised sum: in two
+      const float half = QUANT ? floorf(0.5f * (C - nc)) : 0.f, g = um::ex2(half);
+      f = um::ex2(C - nc - half);
+      lsum *= g;
+      sum *= g;
+      lsum *= f;
+      sum *= f;
+      f *= g;
       C = nc;
     }
-    lsum *= f;
-    sum *= f;
     if (acc) {
 #pragma unroll 1
       for (int i = 0; i < 4; ++i) {
@@ -916,20 +933,21 @@ struct Row {
   // columns of every 32 (for bf16 the next 16 hold the remainders).  The
   // reference at hand is tried first: only columns whose weights leave the
   // range have their maximum taken and the reference moved.
-  __device__ __forceinline__ void tile(uint32_t tS, uint32_t tO, const Meta& mt, float dE, bool acc) {
+  __device__ __forceinline__ void tile(uint32_t tS, uint32_t tO, const Meta& mt, bool acc) {
     if (__any_sync(kFull, C == -INFINITY)) {  // a row that has met nothing yet: no accumulator to scale
-      const float mx = tile_max<QUANT>(tS, mt);
-      if (C == -INFINITY) C = reference(mx, dE);
+      const float mx = tile_max<QUANT>(tS, mt, sl);
+      if (C == -INFINITY) C = reference(mx);
     }
     float sum = 0.f;
     bool again = false;
 #pragma unroll 1
     for (int c = 0; c < 4;) {
       uint32_t hi[16], lo[16];
-      const float x = chunk(tS, c, mt, offset(dE), hi, lo);
-      const bool over = !(x < kLimit);
+      uint32_t top = 0;
+      const float x = chunk(tS, c, mt, offset(), hi, lo, top);
+      const bool over = !(x < kLimit) || (QUANT && __vmaxu2(top, kTop) != kTop);
       if (!again && __any_sync(kFull, over)) {
-        regrow(tS, tO, c, mt, dE, over, acc, sum);
+        regrow(tS, tO, c, mt, over, acc, sum);
         again = true;
         continue;
       }
@@ -939,7 +957,7 @@ struct Row {
       sum += x;
       ++c;
     }
-    lsum = fmaf(sum, QUANT ? um::ex2(-dE) : 1.f, lsum);
+    lsum += sum;
   }
 };
 
@@ -1007,7 +1025,6 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
     const int n = it.kb - it.ka, steps = PAIR ? n : (n - s + 1) / 2;
     const int tok = (it.blk * p.rb + min(brow, rows - 1)) / p.G;
     const uint64_t word = p.kn.p ? seen(p, b, tok) : 0ull;
-    int shift0 = 0;  // exponent the accumulator is relative to
     for (int i = 0; busy && i < steps; ++i) {
       const uint32_t t = t0 + (uint32_t)(PAIR ? i : 2 * i + s);
       // the tile's facts are there long before its logits: asked for first, the poll
@@ -1015,7 +1032,6 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
       ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->ready[t % kMeta]), (t / kMeta) & 1u, ab));
       const Meta& mt = m->meta[t % kMeta];
       const bool whole = mt.whole, own = mt.drafts;
-      const int shift = mt.shift;
       ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[s]), uses & 1u, ab));
       ++uses;
       if (!ok) break;
@@ -1025,9 +1041,7 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
                                   own ? 0u : mt.live[2], own ? 0u : mt.live[3]};
         mask_tile(tS, live);
       }
-      if (i == 0) shift0 = shift;
-      const float dE = kQuant ? (float)(shift - shift0) : 0.f;
-      row.tile(tS, tO, mt, dE, i > 0);  // O of the tiles before is done (see Issuer)
+      row.tile(tS, tO, mt, i > 0);  // O of the tiles before is done (see Issuer)
       um::wait_st();
       um::fence_before();
       __syncwarp();
@@ -1046,25 +1060,18 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
     if (!PAIR && s == 1 && busy) {
       m->cm[lrow] = row.C;
       m->l[lrow] = row.lsum;
-      m->sh[lrow] = (float)shift0;
     }
     um::fence_before();
     softmax_sync();  // from here on nothing reads the queries any more either
     um::fence_after();
     if (busy && (PAIR || s == 0)) {
-      // stream s: sum 2^C lsum, accumulator relative to 2^(C + shift0)
-      const float C = row.C, lsum = row.lsum;
-      float f0 = 1.f, f1 = 0.f, Cj = C, lj = lsum;
-      if (both) {
-        const float C1 = m->cm[lrow], l1 = m->l[lrow];
-        Cj = fmaxf(C, C1);
-        f0 = C == -INFINITY ? 0.f : exp2f(C - Cj);
-        f1 = C1 == -INFINITY ? 0.f : exp2f(C1 - Cj);
-        lj = lsum * f0 + l1 * f1;
-        f1 *= kQuant ? exp2f(m->sh[lrow] - (float)shift0) : 1.f;
-      }
-      const float inv = lj != 0.f ? 1.f / lj : 0.f, up = kQuant ? exp2f((float)shift0) : 1.f;
-      const float g0 = f0 == 0.f ? 0.f : f0 * inv * up, g1 = f1 == 0.f ? 0.f : f1 * inv * up;
+      // sum and accumulator are relative to 2^C; a quantised store's C goes with the values, so
+      // the sum's own exponent is taken into the record's reference
+      const float C = row.C, lsum = row.lsum, C1 = both ? m->cm[lrow] : -INFINITY, l1 = both ? m->l[lrow] : 0.f;
+      const float Cj = fmaxf(C + (kQuant ? (float)exponent(lsum) : 0.f), C1 + (kQuant ? (float)exponent(l1) : 0.f));
+      const float f0 = C == -INFINITY ? 0.f : exp2f(C - Cj), f1 = C1 == -INFINITY ? 0.f : exp2f(C1 - Cj);
+      const float lj = both ? lsum * f0 + l1 * f1 : C == -INFINITY ? lsum : lsum * f0;
+      const float inv = lj != 0.f ? 1.f / lj : 0.f, g0 = f0 * inv, g1 = f1 * inv;
       const int64_t rec = ((int64_t)blockIdx.x + (int64_t)it.u * p.nblk + it.blk) * p.rb + brow;
       const bool mine = brow < rows;
 #pragma unroll 1

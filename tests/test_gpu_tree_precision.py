@@ -59,8 +59,8 @@ def inputs(T, G, n, size, seed, sink=None, bits=0.0):
     return q, k, v
 
 
-# few query rows (mma.sync; over a bf16 store 24 are for tcgen05)
-ROWS = [(1, 4), (3, 8)]
+# query rows: few (mma.sync; over a bf16 store 24 are for tcgen05), up to 128, more
+ROWS = [(1, 4), (3, 8), (16, 4), (9, 16)]
 
 
 @pytest.mark.parametrize("fmt", ("bf16", "fp8", "fp4"))
