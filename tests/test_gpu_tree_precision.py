@@ -119,3 +119,25 @@ def test_drafts_of_another_size(fmt, T, G):
     for i in range(T):
         vn[0, 0, i] *= (0.0, 1e-6, 1e3, 1.0)[i % 4]
     run(fmt, k, v, q, kn, vn)
+
+
+@pytest.mark.parametrize("fmt", ("bf16", "fp8", "fp4"))
+@pytest.mark.parametrize("T,G", ROWS)
+def test_weights_keep_their_bits_where_values_cancel(fmt, T, G):
+    """Slots in pairs of nearly the same weight and opposite values: the result is 2^-8 of what
+    is summed, so a weight's rounding shows undiminished by the result's own."""
+    n = 256
+    q, k, v = inputs(T, G, n, 1.0, 350)
+    q[..., 1:] *= 0.125
+    k[0, 0, 1::2] = k[0, 0, ::2]
+    k[0, 0, 1::2, 0, 0] += 2.0 ** -8  # logit 2^-8 / sqrt(2) higher
+    v[0, 0, ::2] = randn((1, 1, 128), 353).sign()
+    v[0, 0, 1::2] = -v[0, 0, ::2]
+    run(fmt, k, v, q)
+
+
+@pytest.mark.parametrize("fmt", ("bf16", "fp8", "fp4"))
+@pytest.mark.parametrize("T,G,n", [(1, 4, 20011), (3, 8, 9001), (16, 4, 20011), (9, 16, 9001)])
+def test_long_segments(fmt, T, G, n):
+    q, k, v = inputs(T, G, n, 1.0, 360)
+    run(fmt, k, v, q)
