@@ -64,6 +64,13 @@ struct TreeArgs {
   float* rec_acc;        // [records][rb][128] weighted mean of the values
 };
 
+// What the merge reads for a row: its reference and sum, or NaN where a wait ran out, the
+// writer's own (`ok`) or one of any role whose part the row may hold (`aborted`, read after the
+// barrier at which those parts were handed over).
+__host__ __device__ __forceinline__ float2 tree_record(bool ok, bool aborted, float ref, float sum) {
+  return ok && !aborted ? make_float2(ref, sum) : make_float2(0.f, nanf(""));
+}
+
 // Drafts that token t of sequence b sees, as bits.
 __device__ __forceinline__ uint64_t seen(const TreeArgs& p, int b, int t) {
   const uint64_t all = ~0ull >> (64 - p.T);

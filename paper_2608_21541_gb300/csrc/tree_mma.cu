@@ -663,7 +663,7 @@ __device__ __forceinline__ void consume(const TreeArgs& p, char* smem, float* wa
       *reinterpret_cast<float4*>(p.rec_acc + (rec * p.rb + r) * kD + d) =
           make_float4(A.x * inv, A.y * inv, A.z * inv, A.w * inv);
       if (d == 0)
-        p.rec_ml[rec * p.rb + r] = failed ? make_float2(0.f, __int_as_float(0x7fc00000)) : make_float2(M, L);
+        p.rec_ml[rec * p.rb + r] = tree_record(true, failed, M, L);
     }
     consumers_sync();
     tile += n;

@@ -1097,7 +1097,8 @@ __device__ __forceinline__ void softmax(const TreeArgs& p, Misc* m, uint32_t bas
                          : "memory");
         }
       }
-      if (mine) p.rec_ml[rec] = ok ? make_float2(Cj, lj) : make_float2(0.f, __int_as_float(0x7fc00000));
+      // a stream that gave up has handed over what it had
+      if (mine) p.rec_ml[rec] = tree_record(ok, *ab != 0, Cj, lj);
     }
     um::fence_before();
     t0 += n;
