@@ -193,11 +193,11 @@ __global__ void __launch_bounds__(kStoreThreads, kLoadBlocks) load_kernel(
     st.table[e] = page < first[u + 1] && page < st.pool_pages ? (int)page : -1;
   }
   for (int64_t u = tid; u < st.units; u += step) {
-    const int n = max(real[u], 0) + tail_slot;
+    const int64_t n = (int64_t)max(real[u], 0) + tail_slot;
     const int64_t have = min((int64_t)min(first[u + 1], st.pool_pages) - min(first[u], st.pool_pages),
                              (int64_t)st.max_pages) * kPage;
-    const bool outside = offsets[u] < 0 || offsets[u] + n > capacity;
-    st.counts[u] = outside ? 0 : (int)min((int64_t)n, have);
+    const bool outside = !lies_in(offsets[u], n, capacity);
+    st.counts[u] = outside ? 0 : (int)min(n, have);
     if (outside || n > have) st.raise();
   }
   const int total = min(first[st.units], st.pool_pages);
@@ -210,9 +210,8 @@ __global__ void __launch_bounds__(kStoreThreads, kLoadBlocks) load_kernel(
       else hi = mid;
     }
     const int u = lo, s0 = (page - first[u]) * kPage;
-    const int n = max(real[u], 0) + tail_slot;
-    const bool outside = offsets[u] < 0 || offsets[u] + n > capacity;
-    if (outside || page - first[u] >= st.max_pages) continue;  // uniform over the block
+    const int64_t n = (int64_t)max(real[u], 0) + tail_slot;
+    if (!lies_in(offsets[u], n, capacity) || page - first[u] >= st.max_pages) continue;  // uniform over the block
 #pragma unroll 2
     for (int half = 0; half < 2; ++half) {
       const int s = s0 + half * 32 + grp;

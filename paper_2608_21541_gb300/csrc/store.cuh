@@ -32,6 +32,11 @@ struct Store {
   }
 };
 
+// Whether n >= 0 slots from `first` on lie in `capacity` >= 0 slots, for any `first`.
+__host__ __device__ constexpr bool lies_in(int64_t first, int64_t n, int64_t capacity) {
+  return first >= 0 && n <= capacity && first <= capacity - n;
+}
+
 // bytes of a row's codes
 __host__ __device__ constexpr int row_bytes(int format) {
   return format == CERTKV_STORE_BF16 ? 2 * kD : format == CERTKV_STORE_FP8 ? kD : kD / 2;
