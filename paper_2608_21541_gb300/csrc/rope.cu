@@ -35,7 +35,7 @@ struct RopeArgs {
   float mag, sgn;     // factor, direction of the turn
 };
 
-// Fractional turns of pos * (hi + lo), in [-0.75, 0.75].
+// Fractional turns of pos * (hi + lo), in [-0.5, 0.5].
 __device__ __forceinline__ float turns_of(int pos, float hi, float lo) {
   const float pl = (float)(pos & 4095), ph = (float)(pos - (pos & 4095));  // both exact
   float a = __fmul_rn(ph, hi), b = __fmul_rn(pl, hi);

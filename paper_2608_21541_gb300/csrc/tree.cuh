@@ -14,9 +14,9 @@ constexpr int kSmallRows = 16;  // query rows of a block of the mma.sync kernel
 // Up to this many query rows go to that kernel.  The tcgen05 kernel costs the same for 1 to
 // 128 rows, the mma.sync kernel in proportion to its blocks of 16: one is always cheaper,
 // two are where codes have to be expanded, but not where they only read a bf16 store twice.
-// 32 rows, 256 segments of 13107 slots, mma.sync against tcgen05: 8-bit 310 and 336 us, 4-bit
-// 316 and 377, bf16 512 and 271; 8 segments of 409 slots: 19.8 and 22.7, 21.6 and 22.6, 16.5
-// and 19.4.
+// 32 rows, 256 segments of 13107 slots, mma.sync against tcgen05: 8-bit 309 and 312 us, 4-bit
+// 322 and 331, bf16 512 and 272; 8 segments of 409 slots: 19.9 and 23.7, 21.8 and 23.7, 16.5
+// and 19.8.
 __host__ __device__ constexpr int small_max(int format) {
   return format == CERTKV_STORE_BF16 ? kSmallRows : 2 * kSmallRows;
 }

@@ -26,7 +26,7 @@
 //
 // What bounds it, 256 segments of 13107 slots, up to 4 rows: bf16 260 us, the copy
 // bandwidth.  8-bit 156 us; the copies alone, with nothing done to the tiles, 138.
-// 4-bit 155 and 94: the consumers' expansion and products, which eight warps of 168
+// 4-bit 160 and 94: the consumers' expansion and products, which eight warps of 168
 // registers on an SM do not overlap further.  Slower were tiles of 32 slots (8-bit
 // 198; with three CTAs per SM 169), values in stages of their own (161, 4-bit 192:
 // their expansion then no longer fills the softmax's gaps) and five consumers with

@@ -34,15 +34,17 @@
 // its range (f16: 2^15), so that most tiles are formed in one pass over the logits,
 // without their maximum and without rescaling.
 //
-// What bounds it, 256 segments of 13107 slots: a bf16 store of 64 rows 280 us, 91 %
-// of the copy bandwidth, of 256 rows 495, 46 % of the tensor rate.  8- and 4-bit
-// stores: up to 128 rows 343 to 402 us, the expansion of every code into an operand
-// by eight warps and the softmax beside it (36 % of the issue slots); 256 rows 588,
-// 39 % of the tensor rate, the chain softmax, hand-over, products, hand-over of each
-// stream: a poll of a barrier queues behind the loaders' stores for hundreds of
-// cycles.  Slower were half tiles, also with the next half's S issued before P V
-// (721), an issuing warp per stream, sixteen loader warps, and logits loaded a step
-// ahead of their use.
+// What bounds it, 256 segments of 13107 slots: a bf16 store of 64 rows 282 us, 90 %
+// of the copy bandwidth, of 256 rows 480, 48 % of the tensor rate.  8- and 4-bit
+// stores: 33 to 128 rows 318 to 362 us, the expansion of every code into an operand
+// by eight warps and the softmax beside it (40 % of the issue slots); 256 rows 615 and
+// 599, 37 and 38 % of the tensor rate, the chain softmax, hand-over, products,
+// hand-over of each stream: a poll of a barrier queues behind the loaders' stores for
+// hundreds of cycles.  Value scales on the weights rather than on the values cost the
+// softmax a product a weight (256 rows 588 -> 615 us) and save the loaders one (64
+// rows, 4-bit, 382 -> 337).  Slower were half tiles, also with the next half's S issued
+// before P V (588 -> 721), an issuing warp per stream, sixteen loader warps, and logits
+// loaded a step ahead of their use.
 //
 // Every wait is bounded; on a timeout the roles stop waiting, the rows in
 // question read NaN and the store's status word gets CERTKV_STATUS_TIMEOUT.
@@ -67,7 +69,8 @@ constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroup
 constexpr int kPieces = 128 * 8 / (kGroupWarps * 32), kStep = 128 / kPieces;
 // Registers a thread: the launch gives 96 (640 threads), which the roles share
 // out among themselves.  A spill costs more here than elsewhere: next to 200 KB
-// of shared memory the L1 holds hardly any of it.
+// of shared memory the L1 holds hardly any of it.  256 segments of 13107 slots, 256
+// rows, 8-bit: 120 / 88 / 64 657 us, 120 / 80 / 80 631, 112 / 88 / 80 618.
 constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
               "a larger split would wait for registers for ever");
@@ -366,6 +369,7 @@ struct Scout {
   }
   // Scale 0 for the rows of tile k that are zero.  The four rows of a lane's scales lie
   // behind one another; the warp reads them together, for the lanes that have a scale of 1.
+  // Nothing where no scale is 1; a store of zeros alone takes 3.4 times as long.
   __device__ __forceinline__ void find_zeros() {
     constexpr int kLanes = row_bytes(FMT) / 16;  // of a row, 16 bytes each
     uint32_t some = __ballot_sync(kFull, vs.x == 1.f || vs.y == 1.f || vs.z == 1.f || vs.w == 1.f);

@@ -208,7 +208,7 @@ __device__ __forceinline__ void fence_async() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-// 16, 32 or 64 consecutive columns of this warp's 32 lanes, one lane per thread; the
+// 16 or 32 consecutive columns of this warp's 32 lanes, one lane per thread; the
 // wait is part of the statement, so no use can be scheduled before it.
 __device__ __forceinline__ void ld32(uint32_t a, uint32_t (&r)[32]) {
   asm volatile(
