@@ -138,12 +138,14 @@ bool launch_decode_certified(const Prob& p, const void* q, const void* pk, const
 void trace_begin(const char* name, cudaStream_t st);
 void trace_end(cudaStream_t st);
 
-// Launch of a kernel that may start while the one before it in the stream still
-// runs; it waits for that kernel's results with await_previous() before it reads
-// them (the kernel before it lets it start with release_next()).
+// Launch of a kernel: whether it was launched (the error stays for cudaGetLastError).
+// What reads a workspace that another kernel of the same call writes is not launched
+// after that kernel was not.  `early`: it may start while the one before it in the
+// stream still runs; it waits for that kernel's results with await_previous() before it
+// reads them (the kernel before it lets it start with release_next()).
 template <class... P, class... A>
-void launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st,
-                  A&&... args) {
+bool launch_kernel(bool early, void (*kernel)(P...), unsigned grid, unsigned block, size_t smem,
+                   cudaStream_t st, A&&... args) {
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
@@ -153,8 +155,13 @@ void launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t sm
   c.dynamicSmemBytes = smem;
   c.stream = st;
   c.attrs = &at;
-  c.numAttrs = 1;
-  cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...);  // an error stays for cudaGetLastError
+  c.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) == cudaSuccess;
+}
+// The code of a call that could not be launched; the CUDA error is taken, as at a call's end.
+inline int cuda_failed() {
+  cudaGetLastError();
+  return CERTKV_ECUDA;
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -407,7 +407,9 @@ extern "C" int certkv_store_load(const certkv_packed* packed, int32_t tail_slot,
   int32_t* first = reinterpret_cast<int32_t*>(workspace);
   {
     TraceScope ts_("store_plan", st);
-    load_plan_kernel<<<1, 1024, 0, st>>>(s.units, packed->real_counts, tail_slot, reserve, first);
+    if (!launch_kernel(false, load_plan_kernel, 1, 1024, 0, st, s.units, packed->real_counts, tail_slot,
+                       reserve, first))
+      return cuda_failed();
   }
   // enough blocks for every page, at most those that are resident together
   const int grid = s.pool_pages < 152 * kLoadBlocks ? s.pool_pages : 152 * kLoadBlocks;
@@ -455,17 +457,15 @@ extern "C" int certkv_store_append(int32_t batch, int32_t layers, int32_t hkv, i
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   {
     TraceScope ts_("store_append", st);
-#define CERTKV_APPEND(F)                                                                      \
-  if (tokens >= kRun) append_run_kernel<F><<<s.units * runs, kStoreThreads, 0, st>>>(s, p, runs); \
-  else append_kernel<F><<<grid, kStoreThreads, 0, st>>>(s, p)
-    if (store->format == CERTKV_STORE_BF16) {
-      CERTKV_APPEND(CERTKV_STORE_BF16);
-    } else if (store->format == CERTKV_STORE_FP8) {
-      CERTKV_APPEND(CERTKV_STORE_FP8);
-    } else {
-      CERTKV_APPEND(CERTKV_STORE_FP4);
-    }
+#define CERTKV_APPEND(F)                                                                             \
+  (tokens >= kRun                                                                                    \
+       ? launch_kernel(false, append_run_kernel<F>, s.units * runs, kStoreThreads, 0, st, s, p, runs) \
+       : launch_kernel(false, append_kernel<F>, grid, kStoreThreads, 0, st, s, p))
+    const bool launched = store->format == CERTKV_STORE_BF16  ? CERTKV_APPEND(CERTKV_STORE_BF16)
+                          : store->format == CERTKV_STORE_FP8 ? CERTKV_APPEND(CERTKV_STORE_FP8)
+                                                              : CERTKV_APPEND(CERTKV_STORE_FP4);
 #undef CERTKV_APPEND
+    if (!launched) return cuda_failed();  // the counts stay with what is written
   }
   if (!p.bump) {
     TraceScope ts_("store_count", st);

@@ -306,14 +306,15 @@ extern "C" int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (p.units > kInlineUnits) {
     TraceScope ts_("tree_plan", st);
-    tree_plan_kernel<<<1, 1024, 0, st>>>(p.st, p.small ? small_tile(store->format) : kTreeTile,
-                                         !p.small && p.kn.p ? 1 : 0, first);
+    if (!launch_kernel(false, tree_plan_kernel, 1, 1024, 0, st, p.st,
+                       p.small ? small_tile(store->format) : kTreeTile, !p.small && p.kn.p ? 1 : 0, first))
+      return cuda_failed();
   }
   if (!(p.small ? launch_tree_mma(p, store->format, st) : launch_tree_tc(p, store->format, st)))
-    return CERTKV_ECUDA;
+    return cuda_failed();
   {
     TraceScope ts_("tree_merge", st);
-    launch_after(tree_merge_kernel, (unsigned)merge, 256, 0, st, p);
+    launch_kernel(true, tree_merge_kernel, (unsigned)merge, 256, 0, st, p);
   }
   return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA;
 }

@@ -730,8 +730,7 @@ bool launch(const TreeArgs& p, cudaStream_t st) {
              !make_code_map(&mv, p.st.v, row_bytes(FMT), rows, Geo<FMT>::kSlots)) {
     return false;
   }
-  launch_after(tree_mma_kernel<FMT>, p.ctas, kThreads, smem_bytes<FMT>(), st, mk, mv, p);
-  return true;
+  return launch_kernel(true, tree_mma_kernel<FMT>, p.ctas, kThreads, smem_bytes<FMT>(), st, mk, mv, p);
 }
 
 }  // namespace

@@ -1221,11 +1221,10 @@ int ctas_of_device() {
 }
 
 template <int FMT>
-void launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& p, cudaStream_t st) {
-  if (p.rb > 128)
-    launch_after(tree_tc_kernel<FMT, true>, p.ctas, kThreads, smem_bytes<true>(), st, mk, mv, p);
-  else
-    launch_after(tree_tc_kernel<FMT, false>, p.ctas, kThreads, smem_bytes<false>(), st, mk, mv, p);
+bool launch(const CUtensorMap& mk, const CUtensorMap& mv, const TreeArgs& p, cudaStream_t st) {
+  return p.rb > 128
+             ? launch_kernel(true, tree_tc_kernel<FMT, true>, p.ctas, kThreads, smem_bytes<true>(), st, mk, mv, p)
+             : launch_kernel(true, tree_tc_kernel<FMT, false>, p.ctas, kThreads, smem_bytes<false>(), st, mk, mv, p);
 }
 
 }  // namespace
@@ -1239,10 +1238,9 @@ bool launch_tree_tc(const TreeArgs& p, int format, cudaStream_t st) {
     if (!make_row_map(&mk, p.st.k, rows, kPage) || !make_row_map(&mv, p.st.v, rows, kPage)) return false;
   }
   TraceScope ts_("tree_split", st);
-  if (format == CERTKV_STORE_BF16) launch<CERTKV_STORE_BF16>(mk, mv, p, st);
-  else if (format == CERTKV_STORE_FP8) launch<CERTKV_STORE_FP8>(mk, mv, p, st);
-  else launch<CERTKV_STORE_FP4>(mk, mv, p, st);
-  return true;
+  return format == CERTKV_STORE_BF16  ? launch<CERTKV_STORE_BF16>(mk, mv, p, st)
+         : format == CERTKV_STORE_FP8 ? launch<CERTKV_STORE_FP8>(mk, mv, p, st)
+                                      : launch<CERTKV_STORE_FP4>(mk, mv, p, st);
 }
 
 }  // namespace certkv
