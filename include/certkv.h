@@ -591,6 +591,61 @@ int certkv_store_append(int32_t batch, int32_t layers, int32_t hkv, int32_t toke
 int certkv_store_read(const certkv_store* store, const int32_t* start, int32_t tokens, void* k_out,
                       void* v_out, void* stream);
 
+/* ---- pages of a store -----------------------------------------------------------
+ * certkv_store_load hands pages out once.  These calls keep them on the GPU while
+ * sequences grow, are cut back and end, without the host knowing any length.  A page
+ * belongs to one segment: these calls do not count owners.  The caller owns the
+ * three arrays and the store's table; pages that are not in the list are some
+ * segment's. */
+typedef struct {
+  int32_t *held;        /* [units] table entries of each segment that are its own (the
+                           first ones; read as clamped to 0..max_pages)             */
+  int32_t *free;        /* [pool_pages] the free pages: the first free_count entries,
+                           the last of them handed out first                        */
+  int32_t *free_count;  /* [1] (read as clamped to 0..pool_pages)                   */
+} certkv_pages;
+
+/* The store's free pages from its table, as after certkv_store_load: held[u] = the
+ * entries of table row u up to its last page, free = the pages that no row names,
+ * the lowest to be handed out first.  Workspace, here and below:
+ * certkv_pages_workspace_bytes(units, pool_pages), 256-byte aligned. */
+size_t certkv_pages_workspace_bytes(int32_t units, int32_t pool_pages);
+int certkv_pages_list(const certkv_store* store, const certkv_pages* pages, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* Bring every segment to the pages that its length needs.  Segment u of sequence
+ * b = u / (units / batch) is to hold s = base + room[b] slots, base = want[u] or, with
+ * want NULL, counts[u]; room NULL: 0; s < 0 is 0 (a large negative room ends a
+ * sequence), s beyond 64 max_pages is that, with CERTKV_STATUS_STORE.  A segment
+ * with more than ceil(s / 64) pages gives its last ones back, one with fewer is given
+ * pages behind its own, and counts[u] is cut to s where it is larger.  want, room:
+ * device int32 [units], [batch].  With r_0, r_1 .. the pages given back, segment
+ * after segment and each in the order of its table row, m of them, and n free pages
+ * before the call: r_i becomes free[n + m - 1 - i]; then the j-th page handed out, in
+ * the same order, is free[n + m - 1 - j].  So a call that takes back what the one
+ * before it gave leaves the list as it was.  Where the list runs out the segment and
+ * those behind it get no more (held says what they have) and CERTKV_STATUS_STORE is
+ * raised; so it is where the list would grow beyond pool_pages (the last pages given
+ * back are then dropped) or holds an entry that is no page.  Entries given back
+ * become -1. */
+int certkv_pages_reserve(int32_t batch, const int32_t* room, const int32_t* want,
+                         const certkv_store* store, const certkv_pages* pages, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Where a step's rows go, and their positions.  slots (may be NULL): int32
+ * [units][tokens], the pool slot (page 64 + offset) of slot start[u] + i of segment u
+ * for i < rows[b], -1 for the others and where there is no page (a row i < rows[b]
+ * without a page raises CERTKV_STATUS_STORE).  start: device int32 [units], NULL:
+ * counts; rows: device int32 [batch] (clamped to 0..tokens), NULL: tokens.
+ * positions (may be NULL): int32 [batch][tokens], base[b] + the depth of token t:
+ * the number of other drafts that mask[b][t] names (uint64 [batch][tokens], as for
+ * certkv_tree_attn; bits from `tokens` on are ignored), with mask NULL t.  base:
+ * device int32 [batch], NULL: 0; positions wrap at 2^31.  mask needs tokens <= 64;
+ * units * tokens < 2^40. */
+int certkv_slot_map(int32_t batch, int32_t tokens, const int32_t* rows, const int32_t* start,
+                    const int32_t* base, const uint64_t* mask, const certkv_store* store,
+                    int32_t* slots, int32_t* positions, void* stream);
+
 /* ---- attention of a tree of drafted tokens ------------------------------------
  * For drafted token t and query head qh of unit u = (b, l, qh / G):
  *   out[b][l][t][qh] = softmax-weighted sum of values over all counts[u] slots of

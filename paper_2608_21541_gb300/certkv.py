@@ -80,6 +80,11 @@ class certkv_store(ctypes.Structure):
                 ("counts", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
+class certkv_pages(ctypes.Structure):
+    _fields_ = [("held", ctypes.c_void_p), ("free", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p)]
+
+
 EXPORTED = ("certkv_default_params", "certkv_live_budget", "certkv_workspace_bytes",
             "certkv_decode_workspace_bytes", "certkv_score", "certkv_curves",
             "certkv_compress_scored", "certkv_compress", "certkv_decode_attn",
@@ -92,7 +97,9 @@ EXPORTED = ("certkv_default_params", "certkv_live_budget", "certkv_workspace_byt
             "certkv_workspace_guard_arm", "certkv_workspace_guard_check",
             "certkv_selftest_bounded_wait", "certkv_rope_plan", "certkv_rope",
             "certkv_store_workspace_bytes", "certkv_store_load", "certkv_store_append",
-            "certkv_store_read", "certkv_tree_workspace_bytes", "certkv_tree_attn")
+            "certkv_store_read", "certkv_tree_workspace_bytes", "certkv_tree_attn",
+            "certkv_pages_workspace_bytes", "certkv_pages_list", "certkv_pages_reserve",
+            "certkv_slot_map")
 
 _lock = threading.Lock()
 _lib = None
@@ -199,6 +206,15 @@ def load_library(path: Optional[str] = None):
         lib.certkv_tree_attn.argtypes = [sp, I32, rp, rp, rp, P, tp, ctypes.c_float, rp, P, P, SZ,
                                          P]
         lib.certkv_tree_attn.restype = ctypes.c_int
+        gp = ctypes.POINTER(certkv_pages)
+        lib.certkv_pages_workspace_bytes.argtypes = [I32, I32]
+        lib.certkv_pages_workspace_bytes.restype = SZ
+        lib.certkv_pages_list.argtypes = [tp, gp, P, SZ, P]
+        lib.certkv_pages_list.restype = ctypes.c_int
+        lib.certkv_pages_reserve.argtypes = [I32, P, P, tp, gp, P, SZ, P]
+        lib.certkv_pages_reserve.restype = ctypes.c_int
+        lib.certkv_slot_map.argtypes = [I32, I32, P, P, P, P, tp, P, P, P]
+        lib.certkv_slot_map.restype = ctypes.c_int
         _lib = lib
         return lib
 
@@ -917,6 +933,99 @@ def certkv_store_read(store: Store, tokens: int, *, start=None, k_out=None, v_ou
     _check(rc, "certkv_store_read")
     _keep_for(stream, *made)
     return k_out, v_out
+
+
+@dataclass(frozen=True)
+class Pages:
+    """Caller-owned account of a store's pages (certkv_pages in include/certkv.h): held
+    int32 [units], free int32 [pool_pages], free_count int32 [1]."""
+    held: torch.Tensor
+    free: torch.Tensor
+    free_count: torch.Tensor
+
+    def __post_init__(self):
+        for name, size in (("held", None), ("free", None), ("free_count", 1)):
+            t = getattr(self, name)
+            if t.dtype != torch.int32 or t.dim() != 1 or size not in (None, t.shape[0]):
+                raise ValueError("held, free and free_count must be int32 [units], [pool_pages], [1]")
+        object.__setattr__(self, "_struct", certkv_pages(_ptr(self.held), _ptr(self.free),
+                                                         _ptr(self.free_count)))
+
+    def of(self, store: Store) -> certkv_pages:
+        if self.held.shape[0] != store.units or self.free.shape[0] != store.k.shape[0]:
+            raise ValueError("pages must be of the store's units and pool")
+        return self._struct
+
+    @staticmethod
+    def empty(store: Store) -> "Pages":
+        """Room for a store's account (certkv_pages_list fills it)."""
+        def ints(n):
+            return torch.zeros(n, dtype=torch.int32, device=store.table.device)
+        return Pages(held=ints(store.units), free=ints(store.k.shape[0]), free_count=ints(1))
+
+
+def certkv_pages_workspace_bytes(store: Store) -> int:
+    return int(load_library().certkv_pages_workspace_bytes(store.units, store.k.shape[0]))
+
+
+def certkv_pages_list(store: Store, pages: Optional[Pages] = None, *, ws=None, stream=None) -> Pages:
+    """The pages that no row of the store's table names, and how many each row holds."""
+    made = []
+    if pages is None:
+        pages = Pages.empty(store)
+        made += [pages.held, pages.free, pages.free_count]
+    if ws is None:
+        ws = workspace(certkv_pages_workspace_bytes(store), store.k.device)
+        made.append(ws)
+    rc = load_library().certkv_pages_list(ctypes.byref(store.struct()), ctypes.byref(pages.of(store)),
+                                          *_workspace(ws), _on(stream))
+    _check(rc, "certkv_pages_list")
+    _keep_for(stream, *made)
+    return pages
+
+
+def certkv_pages_reserve(store: Store, pages: Pages, room=None, *, want=None, batch: int = 1,
+                         ws=None, stream=None) -> Pages:
+    """Pages for counts[u] + room[b] slots of every segment u of sequence b (want[u] + room[b]
+    where want is given): segments that hold more give them back, others are handed
+    more.  room int32 [B] (None: 0, with `batch` sequences), want int32 [units]."""
+    if room is not None:
+        batch = room.shape[0]
+    made = None
+    if ws is None:
+        ws = made = workspace(certkv_pages_workspace_bytes(store), store.k.device)
+    rc = load_library().certkv_pages_reserve(
+        batch, _index(room, "room", (batch,)), _index(want, "want", (store.units,)),
+        ctypes.byref(store.struct()), ctypes.byref(pages.of(store)), *_workspace(ws), _on(stream))
+    _check(rc, "certkv_pages_reserve")
+    _keep_for(stream, made)
+    return pages
+
+
+def certkv_slot_map(store: Store, tokens: int, *, rows=None, start=None, base=None, mask=None,
+                    batch: int = 1, slots=None, positions=None, stream=None):
+    """(slots int32 [units][tokens], positions int32 [B][tokens]) of a step's rows: the pool slot
+    of slot start[u] + i (start None: behind the live ones; -1 for i >= rows[b]), and
+    base[b] + the depth of each token (mask int64 [B][tokens], the drafts it sees; None: in
+    order).  B is that of rows, base or mask, else `batch`."""
+    for t in (rows, base, mask):
+        if t is not None:
+            batch = t.shape[0]
+    made = []
+    if slots is None:
+        slots = torch.empty((store.units, int(tokens)), dtype=torch.int32, device=store.k.device)
+        made.append(slots)
+    if positions is None:
+        positions = torch.empty((batch, int(tokens)), dtype=torch.int32, device=store.k.device)
+        made.append(positions)
+    rc = load_library().certkv_slot_map(
+        batch, int(tokens), _index(rows, "rows", (batch,)), _index(start, "start", (store.units,)),
+        _index(base, "base", (batch,)), _index(mask, "mask", (batch, int(tokens)), torch.int64),
+        ctypes.byref(store.struct()), _index(slots, "slots", (store.units, int(tokens))),
+        _index(positions, "positions", (batch, int(tokens))), _on(stream))
+    _check(rc, "certkv_slot_map")
+    _keep_for(stream, *made)
+    return slots, positions
 
 
 def certkv_tree_workspace_bytes(B: int, L: int, Hq: int, H: int, tokens: int) -> int:
