@@ -672,6 +672,37 @@ int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const certkv_row
                      const certkv_store* store, float scale, const certkv_rows* out, float* lse,
                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- gradients of that attention -------------------------------------------------
+ * What a loss changes by through certkv_tree_attn, whose q, k_new, v_new, mask, store,
+ * scale, out and lse are given with dout = the loss's gradient for out and dlse (fp32
+ * [batch][layers][tokens][hq], NULL: 0) that for lse.  The probabilities are worked
+ * out again.  For row r (token t, query head qh of unit u) and what it sees, slot or
+ * draft s:
+ *   p = exp(scale <q_r, k_s> - lse_r),  delta_r = <dout_r, out_r> - dlse_r,
+ *   e = scale p (<dout_r, v_s> - delta_r),
+ *   dq_r = sum_s e k_s,  dk_s = sum_r e q_r,  dv_s = sum_r p dout_r,
+ * the last two over all tokens and all G query heads of the segment.  dq bf16
+ * [batch][layers][tokens][hq]; dk_new, dv_new bf16 [batch][layers][tokens][hkv];
+ * dk_store, dv_store bf16 [pool_pages][64][128], 128-byte aligned: the gradient of the
+ * value that a slot stands for, whatever the store's format, in the slot's place
+ * (slots that are not live are not written; no page may be two segments').  dq may be
+ * NULL, and both of dk_new, dv_new (must be, without k_new), and both of dk_store,
+ * dv_store; not all.  Outputs are overwritten; they overlap neither one another
+ * nor an input.  A row whose lse is -inf gives and gets 0; what a row does not see
+ * does not touch it, nor does the row touch that.  Sums are fp32, in an order that
+ * does not change from call to call; p and e enter the sums as bf16 (2^-9 of each
+ * product).  Limits and refusals are those of certkv_tree_attn, on a wait that runs
+ * out the rows and slots concerned get NaN (CERTKV_STATUS_TIMEOUT).  Workspace:
+ * certkv_tree_grad_workspace_bytes(shape, tokens), 256-byte aligned. */
+size_t certkv_tree_grad_workspace_bytes(const certkv_shape* shape, int32_t tokens);
+int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, const certkv_rows* q,
+                          const certkv_rows* k_new, const certkv_rows* v_new,
+                          const uint64_t* mask, const certkv_store* store, float scale,
+                          const certkv_rows* out, const float* lse, const certkv_rows* dout,
+                          const float* dlse, const certkv_rows* dq, const certkv_rows* dk_new,
+                          const certkv_rows* dv_new, void* dk_store, void* dv_store,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static description of a return code. */
 const char* certkv_strerror(int code);
 

@@ -99,7 +99,7 @@ EXPORTED = ("certkv_default_params", "certkv_live_budget", "certkv_workspace_byt
             "certkv_store_workspace_bytes", "certkv_store_load", "certkv_store_append",
             "certkv_store_read", "certkv_tree_workspace_bytes", "certkv_tree_attn",
             "certkv_pages_workspace_bytes", "certkv_pages_list", "certkv_pages_reserve",
-            "certkv_slot_map")
+            "certkv_slot_map", "certkv_tree_grad_workspace_bytes", "certkv_tree_attn_grad")
 
 _lock = threading.Lock()
 _lib = None
@@ -215,6 +215,11 @@ def load_library(path: Optional[str] = None):
         lib.certkv_pages_reserve.restype = ctypes.c_int
         lib.certkv_slot_map.argtypes = [I32, I32, P, P, P, P, tp, P, P, P]
         lib.certkv_slot_map.restype = ctypes.c_int
+        lib.certkv_tree_grad_workspace_bytes.argtypes = [sp, I32]
+        lib.certkv_tree_grad_workspace_bytes.restype = SZ
+        lib.certkv_tree_attn_grad.argtypes = [sp, I32, rp, rp, rp, P, tp, ctypes.c_float, rp, P, rp,
+                                              P, rp, rp, rp, P, P, P, SZ, P]
+        lib.certkv_tree_attn_grad.restype = ctypes.c_int
         _lib = lib
         return lib
 
@@ -1066,3 +1071,59 @@ def certkv_tree_attn(q, store: Store, *, hkv: int, k_new=None, v_new=None, mask=
     _check(rc, "certkv_tree_attn")
     _keep_for(stream, *made)
     return out
+
+
+def certkv_tree_grad_workspace_bytes(B: int, L: int, Hq: int, H: int, tokens: int) -> int:
+    shape = certkv_shape(B, L, Hq, H, 2, 128, 1)  # n and w are not used
+    return int(load_library().certkv_tree_grad_workspace_bytes(ctypes.byref(shape), int(tokens)))
+
+
+def certkv_tree_attn_grad(dout, q, store: Store, out, lse, *, hkv: int, k_new=None, v_new=None,
+                          mask=None, scale: float = 0.0, dlse=None, dq=None, dk_new=None,
+                          dv_new=None, dk_store=None, dv_store=None, ws=None, stream=None):
+    """Gradients of certkv_tree_attn(q, store, ..) = out, lse for dout [B][L][T][Hq][128] and,
+    where given, dlse fp32 [B][L][T][Hq].  Returns (dq, dk_new, dv_new) in the inputs' shapes
+    (None for drafts that were not given); dk_store and dv_store, bf16 [pool_pages][64][128],
+    receive the gradients of the values of the store's live slots where both are given."""
+    B, L, T, Hq, _ = q.shape
+    shape = certkv_shape(B, L, Hq, int(hkv), 2, 128, 1)
+    made = []
+
+    def result(t, like, name):
+        if t is None:
+            t = _like(like)
+            made.append(t)
+        elif t.shape != like.shape:
+            raise ValueError(f"{name} must have the shape of {name[1:]}")
+        return t, ctypes.byref(_rows(t, name))
+
+    if dout.shape != q.shape or out.shape != q.shape:
+        raise ValueError("dout and out must have the shape of q")
+    dq, rdq = result(dq, q, "dq")
+    rk = rv = rdk = rdv = None
+    if k_new is not None or v_new is not None:
+        if k_new is None or v_new is None or k_new.shape != v_new.shape or \
+                k_new.shape[:4] != (B, L, T, hkv):
+            raise ValueError("k_new and v_new must both be [B][L][T][hkv][128]")
+        rk, rv = ctypes.byref(_rows(k_new, "k_new")), ctypes.byref(_rows(v_new, "v_new"))
+        dk_new, rdk = result(dk_new, k_new, "dk_new")
+        dv_new, rdv = result(dv_new, v_new, "dv_new")
+    elif dk_new is not None or dv_new is not None:
+        raise ValueError("dk_new and dv_new need k_new and v_new")
+    if (dk_store is None) != (dv_store is None):
+        raise ValueError("dk_store and dv_store are given together")
+    pool = (store.k.shape[0], STORE_PAGE, 128)
+    lib = load_library()
+    if ws is None:
+        ws = workspace(int(lib.certkv_tree_grad_workspace_bytes(ctypes.byref(shape), T)), q.device)
+        made.append(ws)
+    rc = lib.certkv_tree_attn_grad(
+        ctypes.byref(shape), T, ctypes.byref(_rows(q, "q")), rk, rv,
+        _index(mask, "mask", (B, T), torch.int64), ctypes.byref(store.struct()), float(scale),
+        ctypes.byref(_rows(out, "out")), _index(lse, "lse", (B, L, T, Hq), torch.float32),
+        ctypes.byref(_rows(dout, "dout")), _index(dlse, "dlse", (B, L, T, Hq), torch.float32), rdq,
+        rdk, rdv, _index(dk_store, "dk_store", pool, torch.bfloat16),
+        _index(dv_store, "dv_store", pool, torch.bfloat16), *_workspace(ws), _on(stream))
+    _check(rc, "certkv_tree_attn_grad")
+    _keep_for(stream, *made)
+    return dq, dk_new, dv_new
