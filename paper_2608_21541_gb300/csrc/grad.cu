@@ -4,8 +4,18 @@
 //   p = exp(scale <q_r, k_s> - lse_r),  e = scale p (<dout_r, v_s> - delta_r),
 //   delta_r = <dout_r, out_r> - dlse_r,
 //   dq_r = sum_s e k_s,  dk_s = sum_r e q_r,  dv_s = sum_r p dout_r.
-// The simple form: one warp for each row that is summed into.
+//
+// Launches: what is known of each row, and the segments' tiles (grad_rows); the stored slots
+// (grad_q.cu for dq, grad_kv.cu for dk and dv; with few rows grad_kv.cu for all three); the
+// drafts' own keys and values (grad_drafts); and the sums over the shares and chunks that those
+// left (grad_merge), in one order.
+//
+// What a row does not see cannot reach it, nor the row that, though matrix products sum over all
+// rows and drafts of a tile: rows that take no part enter them as zeros with probability 0, and
+// rows or keys with a NaN or infinity as zeros too, with the probabilities of what sees them NaN.
 #include <math.h>
+
+#include <algorithm>
 
 #include "../../include/certkv.h"
 #include "common.cuh"
@@ -16,12 +26,8 @@ namespace certkv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kChunkRows = 128;  // query rows of a block of the drafts' kernel
 
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(kFull, x, o);
-  return x;
-}
 __device__ __forceinline__ float4 load4(const uint16_t* row, int lane) {
   const uint2 x = *reinterpret_cast<const uint2*>(row + 4 * lane);
   return make_float4(bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y));
@@ -31,135 +37,342 @@ __device__ __forceinline__ void store4(uint16_t* row, int lane, float4 a) {
   *reinterpret_cast<uint2*>(row + 4 * lane) =
       make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
-__device__ __forceinline__ float dot(float4 a, float4 b) {
-  return warp_sum(a.x * b.x + a.y * b.y + a.z * b.z + a.w * b.w);
-}
-__device__ __forceinline__ void axpy(float f, float4 x, float4& a) {
-  a.x = fmaf(f, x.x, a.x);
-  a.y = fmaf(f, x.y, a.y);
-  a.z = fmaf(f, x.z, a.z);
-  a.w = fmaf(f, x.w, a.w);
+__device__ __forceinline__ bool finite4(float4 a) {
+  return fabsf(a.x) < INFINITY && fabsf(a.y) < INFINITY && fabsf(a.z) < INFINITY && fabsf(a.w) < INFINITY;
 }
 
-// Elements 4 lane .. of pool slot `at`.
-template <int FMT>
-__device__ __forceinline__ float4 stored4(const uint8_t* codes, const uint8_t* group, const float* scale,
-                                          int64_t at, int lane) {
-  if (FMT == CERTKV_STORE_BF16) return load4(reinterpret_cast<const uint16_t*>(codes) + at * kD, lane);
-  const float s = scale[at];
-  uint32_t a, b;
-  if (FMT == CERTKV_STORE_FP8) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + at * 128 + 4 * lane);
-    a = e4m3x2_to_f16x2(w);
-    b = e4m3x2_to_f16x2(w >> 16);
-  } else {
-    const uint32_t w = *reinterpret_cast<const uint16_t*>(codes + at * 64 + 2 * lane);
-    const uint32_t g = group[at * kGroups + lane / 4];
-    const uint32_t g2 = e4m3x2_to_f16x2(g | g << 8);
-    a = hmul2(e2m1x2_to_f16x2<0>(w), g2);
-    b = hmul2(e2m1x2_to_f16x2<1>(w), g2);
+// Block 0: the tiles of the segments before each.  Latency of one launch.
+__device__ __forceinline__ void scan_tiles(const GradArgs& p) {
+  __shared__ long long part[kThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  long long carry = 0;
+  for (int base = 0; base < p.units; base += 4 * kThreads) {
+    int n[4];
+    long long sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int u = base + 4 * (int)threadIdx.x + i;
+      n[i] = u < p.units ? (p.st.count(u) + kGradTile - 1) / kGradTile : 0;
+      sum += n[i];
+    }
+    long long x = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(kFull, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) part[warp] = x;
+    __syncthreads();
+    long long before = carry;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += part[w];
+      carry += part[w];
+    }
+    before += x - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int u = base + 4 * (int)threadIdx.x + i;
+      if (u < p.units) p.first[u] = before;
+      before += n[i];
+    }
+    __syncthreads();
   }
-  const float2 x = f16x2_to_f32(a), y = f16x2_to_f32(b);
-  return make_float4(x.x * s, x.y * s, y.x * s, y.y * s);
+  if (threadIdx.x == 0) p.first[p.units] = carry;
 }
 
-// One warp per row: its log-sum-exp and delta.
+// One warp per row: its log-sum-exp in the log2 domain and delta; +inf and 0 where it takes no
+// part; NaN where its query or its output's gradient holds a NaN or infinity.
 __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_constant__ GradArgs p) {
-  const int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
   release_next();
+  if (blockIdx.x == 0) {
+    scan_tiles(p);
+    return;
+  }
+  const int64_t w = ((int64_t)(blockIdx.x - 1) * kThreads + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31;
   if (w >= (int64_t)p.units * p.rows) return;
   const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
   const GradUnit x(p, u);
   const int qh = x.h * p.G + g;
   const int64_t at = (((int64_t)x.b * p.L + x.l) * p.T + t) * p.H * p.G + qh;
+  const float4 q = load4(p.q.at(x.b, x.l, t, qh), lane), go = load4(p.go.at(x.b, x.l, t, qh), lane);
+  const float4 o = load4(p.o.at(x.b, x.l, t, qh), lane);
   const float lse = p.lse[at];
-  float delta = 0.f;
-  if (lse != -INFINITY) {
-    delta = dot(load4(p.go.at(x.b, x.l, t, qh), lane), load4(p.o.at(x.b, x.l, t, qh), lane));
-    if (p.dlse) delta -= p.dlse[at];
-  }
-  if (lane == 0) p.row[w] = make_float2(lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f, delta);
+  float delta = go.x * o.x + go.y * o.y + go.z * o.z + go.w * o.w;
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) delta += __shfl_xor_sync(kFull, delta, s);
+  if (p.dlse) delta -= p.dlse[at];
+  const bool good = __all_sync(kFull, finite4(q) && finite4(go));
+  if (lane == 0)
+    p.row[w] = lse == -INFINITY ? make_float2(INFINITY, 0.f)
+               : good           ? make_float2(lse * 1.4426950408889634f, delta)
+                                : make_float2(nanf(""), nanf(""));
 }
 
-template <int FMT>
-__global__ void __launch_bounds__(kThreads) grad_q_kernel(const __grid_constant__ GradArgs p) {
-  const int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
+// One warp per query row: the records of the shares that met its segment, and the drafts' part;
+// behind them one per draft: its chunks, where there are several.
+__global__ void __launch_bounds__(kThreads) grad_merge_kernel(const __grid_constant__ GradArgs p) {
+  int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
   await_previous();
-  if (w >= (int64_t)p.units * p.rows) return;
-  const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
-  const GradUnit x(p, u);
-  const int qh = x.h * p.G + g;
-  const float2 row = p.row[w];
+  const int64_t rows = p.dq.p ? (int64_t)p.units * p.rows : 0;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row.x != INFINITY) {
-    const float4 q = load4(p.q.at(x.b, x.l, t, qh), lane), go = load4(p.go.at(x.b, x.l, t, qh), lane);
-    auto add = [&](float4 k, float4 v) {
-      const float pr = exp2f(fmaf(dot(q, k), p.scale_log2, -row.x));
-      axpy(pr * (dot(go, v) - row.y) * p.scale, k, a);
-    };
-    const int n = p.st.count(u);
-    for (int s = 0; s < n; ++s) {
-      const int64_t at = p.st.slot(u, s);
-      if (at < 0) {
-        if (lane == 0) p.st.raise();
-        continue;
-      }
-      add(stored4<FMT>(p.st.k, p.st.kg, p.st.ks, at, lane), stored4<FMT>(p.st.v, p.st.vg, p.st.vs, at, lane));
+  auto add = [&](const float* from) {
+    const float4 x = *reinterpret_cast<const float4*>(from + 4 * lane);
+    a.x += x.x;
+    a.y += x.y;
+    a.z += x.z;
+    a.w += x.w;
+  };
+  if (w < rows) {
+    const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
+    const GradUnit x(p, u);
+    const int blk = r / p.rb, br = r - blk * p.rb;
+    const int64_t f0 = p.first[u], f1 = p.first[u + 1];
+    if (f1 > f0) {
+      const int64_t per = tiles_per_share(p);
+      const int c1 = (int)((f1 - 1) / per);
+#pragma unroll 4
+      for (int c = (int)(f0 / per); c <= c1; ++c) add(p.rec + (grad_record(p, c, u, blk) + br) * kD);
     }
-    if (p.kn.p)
-      for (uint64_t see = grad_seen(p, x.b, t); see; see &= see - 1) {
-        const int j = __ffsll((long long)see) - 1;
-        add(load4(p.kn.at(x.b, x.l, j, x.h), lane), load4(p.vn.at(x.b, x.l, j, x.h), lane));
-      }
+    if (p.kn.p) add(p.dq_new + w * kD);
+    store4(p.dq.at(x.b, x.l, t, x.h * p.G + g), lane,
+           make_float4(a.x * p.scale, a.y * p.scale, a.z * p.scale, a.w * p.scale));
+    return;
   }
-  store4(p.dq.at(x.b, x.l, t, qh), lane, a);
-}
-
-// What row s of keys and values gets from the rows that see it.
-__device__ __forceinline__ void grad_kv(const GradArgs& p, int u, const GradUnit& x, int draft, float4 k, float4 v,
-                                        int lane, float4* dk, float4* dv) {
-  *dk = *dv = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int r = 0; r < p.rows; ++r) {
-    const int t = r / p.G, qh = x.h * p.G + r - t * p.G;
-    const float2 row = p.row[(int64_t)u * p.rows + r];
-    if (row.x == INFINITY || (draft >= 0 && !(grad_seen(p, x.b, t) >> draft & 1u))) continue;
-    const float4 q = load4(p.q.at(x.b, x.l, t, qh), lane), go = load4(p.go.at(x.b, x.l, t, qh), lane);
-    const float pr = exp2f(fmaf(dot(q, k), p.scale_log2, -row.x));
-    axpy(pr, go, *dv);
-    axpy(pr * (dot(go, v) - row.y) * p.scale, q, *dk);
-  }
-}
-
-template <int FMT>
-__global__ void __launch_bounds__(kThreads) grad_store_kernel(const __grid_constant__ GradArgs p) {
-  const int u = blockIdx.x, lane = threadIdx.x & 31;
-  await_previous();
+  w -= rows;
+  if (!p.dkn.p || p.chunks == 1 || w >= (int64_t)p.units * p.T * 2) return;
+  const int u = (int)(w / (2 * p.T)), i = (int)(w - (int64_t)u * 2 * p.T), key = i < p.T, j = key ? i : i - p.T;
   const GradUnit x(p, u);
-  const int n = p.st.count(u);
-  for (int s = threadIdx.x >> 5; s < n; s += kThreads / 32) {
-    const int64_t at = p.st.slot(u, s);
-    if (at < 0) continue;
-    float4 dk, dv;
-    grad_kv(p, u, x, -1, stored4<FMT>(p.st.k, p.st.kg, p.st.ks, at, lane),
-            stored4<FMT>(p.st.v, p.st.vg, p.st.vs, at, lane), lane, &dk, &dv);
-    store4(p.dks + at * kD, lane, dk);
-    store4(p.dvs + at * kD, lane, dv);
-  }
+#pragma unroll 4
+  for (int c = 0; c < p.chunks; ++c) add(p.part + (((int64_t)u * p.chunks + c) * 2 * p.T + i) * kD);
+  const float f = key ? p.scale : 1.f;
+  store4((key ? p.dkn : p.dvn).at(x.b, x.l, j, x.h), lane, make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }
 
+// ----------------------------------------------------------------- drafts --
+__device__ __forceinline__ uint32_t smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void ldm4(uint32_t a, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t a, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+constexpr int kPitch = 2 * kD + 16;  // bytes of a row of 128 elements in shared memory: odd in 16 bytes
+template <int TD>
+struct Drafts {  // TD: the drafts, filled up with zeros
+  static constexpr int kWide = 2 * TD + 16;
+  static constexpr int kKeyOff = 0, kValueOff = TD * kPitch;
+  static constexpr int kRowOff = 2 * TD * kPitch, kGradOff = kRowOff + kChunkRows * kPitch;
+  static constexpr int kPOff = kGradOff + kChunkRows * kPitch, kEOff = kPOff + kChunkRows * kWide;
+  static constexpr int kInfoOff = kEOff + kChunkRows * kWide, kSeenOff = kInfoOff + kChunkRows * 8;
+  static constexpr int kBadOff = kSeenOff + kChunkRows * 8, kBytes = kBadOff + 16;
+};
+
+// One block per (unit, 128 query rows), on mma.sync: products of at most 128 x 64 x 128, whose
+// time is that of bringing the rows in.  A warp makes p and e of 16 rows and their dq; then each
+// warp 16 elements of dk and dv over all rows.
+template <int TD>
 __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_constant__ GradArgs p) {
-  const int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  await_previous();
-  if (w >= (int64_t)p.units * p.T) return;
-  const int u = (int)(w / p.T), j = (int)(w - (int64_t)u * p.T);
+  using D = Drafts<TD>;
+  extern __shared__ __align__(128) char sm[];
+  const int u = blockIdx.x / p.chunks, chunk = blockIdx.x - u * p.chunks;
+  const int r0 = chunk * kChunkRows, rows = min(p.rows - r0, kChunkRows), strips = (rows + 15) / 16;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const GradUnit x(p, u);
-  float4 dk, dv;
-  grad_kv(p, u, x, j, load4(p.kn.at(x.b, x.l, j, x.h), lane), load4(p.vn.at(x.b, x.l, j, x.h), lane), lane, &dk, &dv);
-  store4(p.dkn.at(x.b, x.l, j, x.h), lane, dk);
-  store4(p.dvn.at(x.b, x.l, j, x.h), lane, dv);
+  float2* info = reinterpret_cast<float2*>(sm + D::kInfoOff);
+  uint64_t* sees = reinterpret_cast<uint64_t*>(sm + D::kSeenOff);
+  unsigned long long* bad = reinterpret_cast<unsigned long long*>(sm + D::kBadOff);
+  if (tid == 0) *bad = 0ull;
+  await_previous();
+  release_next();
+  if (tid < kChunkRows) {
+    info[tid] = tid < rows ? p.row[(int64_t)u * p.rows + r0 + tid] : make_float2(INFINITY, 0.f);
+    sees[tid] = tid < rows && info[tid].x != INFINITY ? grad_seen(p, x.b, (r0 + tid) / p.G) : 0ull;
+  }
+  __syncthreads();
+  const int c = tid & 15;
+  for (int j = tid >> 4; j < TD; j += kThreads / 16) {  // keys with a NaN or infinity as zeros, and noted
+    uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
+    if (j < p.T) {
+      k = *(reinterpret_cast<const uint4*>(p.kn.at(x.b, x.l, j, x.h)) + c);
+      v = *(reinterpret_cast<const uint4*>(p.vn.at(x.b, x.l, j, x.h)) + c);
+    }
+    const uint32_t w[4] = {k.x, k.y, k.z, k.w};
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    const uint32_t any = __ballot_sync(kFull, odd) & (0xffffu << (lane & 16));
+    if (any) {
+      k = make_uint4(0u, 0u, 0u, 0u);
+      if (c == 0) atomicOr(bad, 1ull << j);
+    }
+    *reinterpret_cast<uint4*>(sm + D::kKeyOff + j * kPitch + 16 * c) = k;
+    *reinterpret_cast<uint4*>(sm + D::kValueOff + j * kPitch + 16 * c) = v;
+  }
+  for (int r = tid >> 4; r < 16 * strips; r += kThreads / 16) {
+    uint4 q = make_uint4(0u, 0u, 0u, 0u), g = q;
+    if (fabsf(info[r].x) < INFINITY) {
+      const int tok = (r0 + r) / p.G, qh = x.h * p.G + (r0 + r) - tok * p.G;
+      q = *(reinterpret_cast<const uint4*>(p.q.at(x.b, x.l, tok, qh)) + c);
+      g = *(reinterpret_cast<const uint4*>(p.go.at(x.b, x.l, tok, qh)) + c);
+    }
+    *reinterpret_cast<uint4*>(sm + D::kRowOff + r * kPitch + 16 * c) = q;
+    *reinterpret_cast<uint4*>(sm + D::kGradOff + r * kPitch + 16 * c) = g;
+  }
+  __syncthreads();
+  const uint32_t base = smem(sm);
+  const int g8 = lane >> 2, t4 = lane & 3;
+  // lane's address offsets of 16 x 16 blocks: rows as they lie (A), rows as columns of B, and
+  // transposed (B from [k][n], A from [k][m])
+  const int lr = lane & 7, l8 = lane >> 3 & 1, l16 = lane >> 4;
+  if (warp < strips) {
+    const int s0 = 16 * warp;
+    float s[TD / 8][4], r[TD / 8][4];
+#pragma unroll
+    for (int n = 0; n < TD / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][i] = r[n][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kD / 16; ++k) {
+      uint32_t aq[4], ag[4];
+      const uint32_t at = base + (uint32_t)((s0 + lr + 8 * l8) * kPitch + 32 * k + 16 * l16);
+      ldm4(at + D::kRowOff, aq);
+      ldm4(at + D::kGradOff, ag);
+#pragma unroll
+      for (int n = 0; n < TD / 16; ++n) {
+        uint32_t bk[4], bv[4];
+        const uint32_t to = base + (uint32_t)((16 * n + lr + 8 * l16) * kPitch + 32 * k + 16 * l8);
+        ldm4(to + D::kKeyOff, bk);
+        ldm4(to + D::kValueOff, bv);
+        mma(s[2 * n], aq, bk[0], bk[1]);
+        mma(s[2 * n + 1], aq, bk[2], bk[3]);
+        mma(r[2 * n], ag, bv[0], bv[1]);
+        mma(r[2 * n + 1], ag, bv[2], bv[3]);
+      }
+    }
+    const unsigned long long odd = *bad;
+    const float2 i0 = info[s0 + g8], i1 = info[s0 + g8 + 8];
+    const uint64_t see0 = sees[s0 + g8], see1 = sees[s0 + g8 + 8];
+    uint32_t e[TD / 8][2];
+#pragma unroll
+    for (int n = 0; n < TD / 8; ++n) {
+      float pr[4], er[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = 8 * n + 2 * t4 + (i & 1);
+        const float2 inf = i < 2 ? i0 : i1;
+        const bool on = (i < 2 ? see0 : see1) >> j & 1u;
+        pr[i] = on ? (odd >> j & 1u ? nanf("") : exp2f(fmaf(s[n][i], p.scale_log2, -inf.x))) : 0.f;
+        er[i] = on ? pr[i] * (r[n][i] - inf.y) : 0.f;
+      }
+      e[n][0] = pack2(er[0], er[1]);
+      e[n][1] = pack2(er[2], er[3]);
+      const int at = (s0 + g8) * D::kWide + 16 * n + 4 * t4;
+      *reinterpret_cast<uint32_t*>(sm + D::kPOff + at) = pack2(pr[0], pr[1]);
+      *reinterpret_cast<uint32_t*>(sm + D::kPOff + at + 8 * D::kWide) = pack2(pr[2], pr[3]);
+      *reinterpret_cast<uint32_t*>(sm + D::kEOff + at) = e[n][0];
+      *reinterpret_cast<uint32_t*>(sm + D::kEOff + at + 8 * D::kWide) = e[n][1];
+    }
+    if (p.dq.p) {
+      float* out = p.dq_new + ((int64_t)u * p.rows + r0 + s0) * kD;
+#pragma unroll 2
+      for (int d = 0; d < kD / 16; ++d) {
+        float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < TD / 16; ++k) {
+          const uint32_t a[4] = {e[2 * k][0], e[2 * k][1], e[2 * k + 1][0], e[2 * k + 1][1]};
+          uint32_t b[4];
+          ldm4t(base + (uint32_t)(D::kKeyOff + (16 * k + lr + 8 * l8) * kPitch + 32 * d + 16 * l16), b);
+          mma(a0, a, b[0], b[1]);
+          mma(a1, a, b[2], b[3]);
+        }
+        const int col = 16 * d + 2 * t4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (s0 + g8 + 8 * h < rows) {
+            float* o = out + (g8 + 8 * h) * kD + col;
+            *reinterpret_cast<float2*>(o) = make_float2(a0[2 * h], a0[2 * h + 1]);
+            *reinterpret_cast<float2*>(o + 8) = make_float2(a1[2 * h], a1[2 * h + 1]);
+          }
+      }
+    }
+  }
+  if (!p.dkn.p) return;
+  __syncthreads();
+  float dk[TD / 16][2][4], dv[TD / 16][2][4];
+#pragma unroll
+  for (int i = 0; i < TD / 16; ++i)
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dk[i][n][k] = dv[i][n][k] = 0.f;
+  for (int k = 0; k < strips; ++k) {
+    uint32_t bq[4], bg[4];
+    const uint32_t at = base + (uint32_t)((16 * k + lr + 8 * l8) * kPitch + 32 * warp + 16 * l16);
+    ldm4t(at + D::kRowOff, bq);
+    ldm4t(at + D::kGradOff, bg);
+#pragma unroll
+    for (int i = 0; i < TD / 16; ++i) {
+      uint32_t ap[4], ae[4];
+      const uint32_t to = base + (uint32_t)((16 * k + lr + 8 * l16) * D::kWide + 32 * i + 16 * l8);
+      ldm4t(to + D::kPOff, ap);
+      ldm4t(to + D::kEOff, ae);
+      mma(dv[i][0], ap, bg[0], bg[1]);
+      mma(dv[i][1], ap, bg[2], bg[3]);
+      mma(dk[i][0], ae, bq[0], bq[1]);
+      mma(dk[i][1], ae, bq[2], bq[3]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < TD / 16; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int j = 16 * i + g8 + 8 * h;
+      if (j >= p.T) continue;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int d = 16 * warp + 8 * n + 2 * t4;
+        if (p.chunks == 1) {
+          *reinterpret_cast<uint32_t*>(p.dkn.at(x.b, x.l, j, x.h) + d) =
+              pack2(dk[i][n][2 * h] * p.scale, dk[i][n][2 * h + 1] * p.scale);
+          *reinterpret_cast<uint32_t*>(p.dvn.at(x.b, x.l, j, x.h) + d) = pack2(dv[i][n][2 * h], dv[i][n][2 * h + 1]);
+        } else {
+          float* o = p.part + (((int64_t)u * p.chunks + chunk) * 2 * p.T + j) * kD + d;
+          *reinterpret_cast<float2*>(o) = make_float2(dk[i][n][2 * h], dk[i][n][2 * h + 1]);
+          *reinterpret_cast<float2*>(o + (int64_t)p.T * kD) = make_float2(dv[i][n][2 * h], dv[i][n][2 * h + 1]);
+        }
+      }
+    }
+}
+
+template <int TD>
+bool launch_drafts(const GradArgs& p, cudaStream_t st) {
+  constexpr int bytes = Drafts<TD>::kBytes;
+  static_assert(bytes <= 232448, "over the 227 KB of shared memory a CTA can have");
+  if (bytes > 48 * 1024 &&
+      cudaFuncSetAttribute(grad_drafts_kernel<TD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
+    return false;
+  return launch_kernel(true, grad_drafts_kernel<TD>, (unsigned)((int64_t)p.units * p.chunks), kThreads, bytes, st, p);
 }
 
 int grad_shape(const certkv_shape* s, int32_t tokens) {
@@ -171,27 +384,35 @@ int grad_shape(const certkv_shape* s, int32_t tokens) {
   return CERTKV_OK;
 }
 
-unsigned warps(int64_t n) { return (unsigned)((n * 32 + kThreads - 1) / kThreads); }
+constexpr int kMaxCtas = 1024;  // records are sized for at most this many
 
-template <int FMT>
-bool launch_store_grads(const GradArgs& p, cudaStream_t st) {
-  if (p.dq.p) {
-    TraceScope ts_("grad_q", st);
-    if (!launch_kernel(true, grad_q_kernel<FMT>, warps((int64_t)p.units * p.rows), kThreads, 0, st, p)) return false;
+struct GradLayout {
+  int nblk, rb, chunks;
+  size_t row, first, rec, dq_new, part, total;
+  GradLayout(int64_t units, int tokens, int rows) {
+    auto a = [](size_t x) { return (x + 255) / 256 * 256; };
+    nblk = (rows + kGradRows - 1) / kGradRows;
+    rb = (rows + nblk - 1) / nblk;
+    chunks = (rows + kChunkRows - 1) / kChunkRows;
+    const size_t n = (size_t)units * rows;
+    row = 0;
+    first = row + a(n * sizeof(float2));
+    rec = first + a(((size_t)units + 1) * sizeof(int64_t));
+    dq_new = rec + ((size_t)units * nblk + kMaxCtas) * rb * kD * sizeof(float);
+    part = dq_new + n * kD * sizeof(float);
+    total = part + (chunks > 1 ? (size_t)units * chunks * 2 * tokens * kD * sizeof(float) : 0);
   }
-  if (p.dks) {
-    TraceScope ts_("grad_store", st);
-    if (!launch_kernel(true, grad_store_kernel<FMT>, p.units, kThreads, 0, st, p)) return false;
-  }
-  return true;
-}
+};
+
+unsigned warps(int64_t n) { return (unsigned)((n * 32 + kThreads - 1) / kThreads); }
 
 }  // namespace
 }  // namespace certkv
 
 extern "C" size_t certkv_tree_grad_workspace_bytes(const certkv_shape* shape, int32_t tokens) {
-  if (certkv::grad_shape(shape, tokens)) return 0;
-  return (size_t)shape->batch * shape->layers * shape->hq * tokens * sizeof(float2);
+  using namespace certkv;
+  if (grad_shape(shape, tokens)) return 0;
+  return GradLayout((int64_t)shape->batch * shape->layers * shape->hkv, tokens, tokens * (shape->hq / shape->hkv)).total;
 }
 
 extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, const certkv_rows* q,
@@ -244,21 +465,46 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   p.scale_log2 = (float)((scale > 0.0f ? scale : 1.0 / sqrt((double)kD)) * 1.4426950408889634);
   p.dks = reinterpret_cast<uint16_t*>(dk_store);
   p.dvs = reinterpret_cast<uint16_t*>(dv_store);
-  p.row = reinterpret_cast<float2*>(workspace);
-  if ((int64_t)p.units * p.rows * 32 / kThreads >= INT32_MAX) return CERTKV_EINVAL;
+  const GradLayout ly(p.units, tokens, p.rows);
+  p.nblk = ly.nblk;
+  p.rb = ly.rb;
+  p.chunks = ly.chunks;
+  char* ws = reinterpret_cast<char*>(workspace);
+  p.row = reinterpret_cast<float2*>(ws + ly.row);
+  p.first = reinterpret_cast<int64_t*>(ws + ly.first);
+  p.rec = reinterpret_cast<float*>(ws + ly.rec);
+  p.dq_new = reinterpret_cast<float*>(ws + ly.dq_new);
+  p.part = reinterpret_cast<float*>(ws + ly.part);
+  // warps of the merge, blocks of the drafts' kernel
+  const int64_t n = (int64_t)p.units * p.rows;
+  if ((n + 2 * (int64_t)p.units * tokens) * 32 / kThreads >= INT32_MAX - 1) return CERTKV_EINVAL;
+  int sms = grad_ctas();
+  if (sms < 1) return CERTKV_ECUDA;
+  sms = std::min(sms, kMaxCtas);
+  const bool fused = p.dks && p.rows <= kGradFused;
+  p.groups = fused ? sms : std::max(sms / p.nblk, 1);
+  // a CTA counts its tiles and blocks of rows in 32 bits
+  if ((int64_t)p.units * (p.st.max_pages + 2) / p.groups * ((p.rows + kGradFused - 1) / kGradFused) >= (1 << 29))
+    return CERTKV_EINVAL;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   {
     TraceScope ts_("grad_rows", st);
-    if (!launch_kernel(false, grad_rows_kernel, warps((int64_t)p.units * p.rows), kThreads, 0, st, p))
-      return cuda_failed();
+    if (!launch_kernel(false, grad_rows_kernel, warps(n) + 1, kThreads, 0, st, p)) return cuda_failed();
   }
-  if (!(store->format == CERTKV_STORE_BF16  ? launch_store_grads<CERTKV_STORE_BF16>(p, st)
-        : store->format == CERTKV_STORE_FP8 ? launch_store_grads<CERTKV_STORE_FP8>(p, st)
-                                            : launch_store_grads<CERTKV_STORE_FP4>(p, st)))
-    return cuda_failed();
-  if (p.dkn.p) {
+  if (p.dks) {
+    GradArgs all = p;
+    all.groups = sms;
+    if (!launch_grad_kv(all, store->format, st)) return cuda_failed();
+  }
+  if (p.dq.p && !fused && !launch_grad_q(p, store->format, st)) return cuda_failed();
+  if (p.kn.p && (p.dq.p || p.dkn.p)) {
     TraceScope ts_("grad_drafts", st);
-    launch_kernel(true, grad_drafts_kernel, warps((int64_t)p.units * p.T), kThreads, 0, st, p);
+    if (!(tokens <= 16 ? launch_drafts<16>(p, st) : launch_drafts<64>(p, st))) return cuda_failed();
+  }
+  if (p.dq.p || (p.dkn.p && p.chunks > 1)) {
+    TraceScope ts_("grad_merge", st);
+    const int64_t w = (p.dq.p ? n : 0) + (p.dkn.p && p.chunks > 1 ? 2 * (int64_t)p.units * tokens : 0);
+    launch_kernel(true, grad_merge_kernel, warps(w), kThreads, 0, st, p);
   }
   return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA;
 }

@@ -9,9 +9,16 @@
 
 namespace certkv {
 
+constexpr int kGradTile = 128;    // slots of a tile: two pages
+constexpr int kGradRows = 128;    // query rows of a block of the query kernel, at most
+constexpr int kGradFused = 64;    // up to this many rows a segment's gradients come from one pass
+
 struct GradArgs {
   int L, H, G, T;    // layers, KV heads, query heads per KV head, drafted tokens
   int units, rows;   // B L H, T G query rows per unit
+  int nblk, rb;      // row blocks of a unit, rows of a block (the last may have fewer)
+  int groups;        // shares of the tiles; their CTAs leave records
+  int chunks;        // of the drafts' kernel: 128 rows each
   Rows q, kn, vn, o, go, dq, dkn, dvn;  // kn.p null: the drafts have no keys of their own
   const uint64_t* mask;
   const float *lse, *dlse;
@@ -19,7 +26,11 @@ struct GradArgs {
   Store st;
   uint16_t *dks, *dvs;  // the store's gradients (null: not asked for)
   // workspace
-  float2* row;  // [units][rows] log-sum-exp (log2 domain; +inf: the row takes no part), delta
+  float2* row;     // [units][rows] log-sum-exp (log2 domain), delta; see grad_rows_kernel
+  int64_t* first;  // [units + 1] tiles of the segments before
+  float* rec;      // [groups + units][nblk][rb][128] dq / scale over a share's tiles
+  float* dq_new;   // [units][rows][128] the same over the drafts
+  float* part;     // [units][chunks][2][T][128] the drafts' dk / scale and dv over 128 rows
 };
 
 struct GradUnit {
@@ -37,5 +48,18 @@ __device__ __forceinline__ uint64_t grad_seen(const GradArgs& p, int b, int t) {
   const uint64_t all = ~0ull >> (64 - p.T);
   return (p.mask ? p.mask[(int64_t)b * p.T + t] : ~0ull >> (63 - t)) & all;
 }
+
+// Tiles of a share: equal consecutive parts of all tiles.
+__device__ __forceinline__ int64_t tiles_per_share(const GradArgs& p) {
+  return max((p.first[p.units] + p.groups - 1) / p.groups, (int64_t)1);
+}
+// Record of the share's part of unit u, row block blk.
+__device__ __forceinline__ int64_t grad_record(const GradArgs& p, int share, int u, int blk) {
+  return (((int64_t)share + u) * p.nblk + blk) * p.rb;
+}
+
+bool launch_grad_q(const GradArgs& p, int format, cudaStream_t st);
+bool launch_grad_kv(const GradArgs& p, int format, cudaStream_t st);
+int grad_ctas();  // SMs of the current device, with the kernels set up for it (0 on an error)
 
 }  // namespace certkv

@@ -1,0 +1,345 @@
+// grad_q.cu — the queries' gradients over the stored slots on the 5th-generation tensor cores.
+//
+// A CTA holds up to 128 query rows of a unit, and their output's gradients, as the M = 128 rows
+// of the MMAs, and walks a share of all tiles of 128 slots:
+//   S = Q K^T,  R = dO V^T,  e = 2^(S - lse) (R - delta),  dQ += e K,
+// with e rounded once to bf16 and handed over in tensor memory, over S.  Neither a maximum nor
+// a rescaling is needed, the log-sum-exp is known, so a tile is formed in one pass.
+// Tensor memory: S of even tiles | S of odd tiles | R | dQ, 128 columns each.  S of the next
+// tile is made while e of this one is, R of the next as soon as R of this one has been read,
+// dQ of this one under e of the next.
+//
+// 8- and 4-bit stores: codes are exact in bf16 (gt::codes_to_bf16); a key's fp32 scale multiplies
+// its logit and its e, a value's its R, all in fp32.
+//
+// CTAs of the same share and different row blocks are neighbours: they read the same tiles at
+// about the same time, so all but the first find them in L2.
+//
+// Every wait is bounded; on a timeout the roles stop waiting, the rows in question read NaN and
+// the store's status word gets CERTKV_STATUS_TIMEOUT.
+#include <atomic>
+
+#include "../../include/certkv.h"
+#include "grad_tc.cuh"
+#include "internal.cuh"
+
+namespace certkv {
+namespace {
+
+using gt::bar;
+constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps;
+constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
+constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
+static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
+              "a larger split would wait for registers for ever");
+constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
+
+template <int FMT>
+struct Plan {
+  static constexpr int kKeys = FMT == CERTKV_STORE_BF16 ? 3 : 2;  // places of the rings
+  static constexpr int kValues = 2;
+  static constexpr int kKeyOff = 2 * kOperand;  // behind the rows and their gradients
+  static constexpr int kValueOff = kKeyOff + kKeys * kOperand;
+  static constexpr int kMiscOff = kValueOff + kValues * kOperand;
+};
+template <int FMT>
+struct Misc {
+  uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
+  uint64_t q_full, s_full, p_full, o_full, done;
+  uint32_t tmem;
+  int abort;
+  typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kKeys];
+};
+template <int FMT>
+constexpr int smem_bytes() {
+  return Plan<FMT>::kMiscOff + (int)sizeof(Misc<FMT>) + 1024;
+}
+static_assert(smem_bytes<CERTKV_STORE_BF16>() <= 232448 && smem_bytes<CERTKV_STORE_FP8>() <= 232448,
+              "over the 227 KB of shared memory a CTA can have");
+
+__device__ __forceinline__ void softmax_sync() {
+  asm volatile("bar.sync 1, %0;" ::"n"(kSoftWarps * 32) : "memory");
+}
+
+// Issues the MMAs of the share's tiles; the whole warp runs, one lane issues.
+template <int FMT>
+struct Issuer {
+  Misc<FMT>* m;
+  uint32_t tmem, base;
+  bool ok = true;
+  static __device__ __forceinline__ uint32_t uni(uint32_t x) { return __shfl_sync(kFull, x, 0); }
+  __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
+    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(b), phase & 1u, &m->abort));
+  }
+  __device__ __forceinline__ uint32_t key(uint32_t t, uint32_t lbo) const {
+    return uni(um::desc_lo(base + Plan<FMT>::kKeyOff, lbo) + (t % Plan<FMT>::kKeys) * (kOperand >> 4));
+  }
+  __device__ __forceinline__ void s(uint32_t t) {
+    wait(&m->k_full[t % Plan<FMT>::kKeys], t / Plan<FMT>::kKeys);
+    if (!ok) return;
+    um::fence_after();
+    um::mma_s(uni(tmem + 128u * (t & 1u)), uni(um::desc_lo(base, 16)), key(t, 16), um::kDescHi, um::idesc(true, false));
+  }
+  __device__ __forceinline__ void r(uint32_t t) {
+    const uint32_t place = t % Plan<FMT>::kValues;
+    wait(&m->v_full[place], t / Plan<FMT>::kValues);
+    if (!ok) return;
+    um::fence_after();
+    um::mma_s(uni(tmem + kColR), uni(um::desc_lo(base + kOperand, 16)),
+              uni(um::desc_lo(base + Plan<FMT>::kValueOff, 16) + place * (kOperand >> 4)), um::kDescHi,
+              um::idesc(true, false));
+    um::commit(uni(bar(&m->s_full)));
+    um::commit(uni(bar(&m->v_empty[place])));
+  }
+  __device__ __forceinline__ void run(gt::Walk walk) {
+    gt::Item it;
+    uint32_t t = 0, item = 0;
+    while (ok && walk.next(&it)) {
+      const int n = it.kb - it.ka;
+      wait(&m->q_full, item++);
+      s(t);
+      r(t);
+      for (int i = 0; ok && i < n; ++i, ++t) {
+        const bool more = i + 1 < n;
+        if (more) s(t + 1);
+        wait(&m->p_full, t);
+        if (more) r(t + 1);
+        if (!ok) break;
+        um::fence_after();
+        um::mma_o(uni(tmem + kColQ), uni(tmem + 128u * (t & 1u)), key(t, kHalf), um::kDescHi, um::idesc(true, true),
+                  uni(i > 0));
+        um::commit(uni(bar(&m->k_empty[t % Plan<FMT>::kKeys])));
+        if (!more) um::commit(uni(bar(&m->o_full)));
+      }
+    }
+    um::commit(bar(&m->done));  // everything issued above has finished
+    volatile int dummy = 0;
+    tc::mbar_wait(bar(&m->done), 0, &dummy);
+    __syncwarp();
+  }
+};
+
+// e of 32 columns of a row: the packed A operand.
+template <int FMT>
+__device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, const typename gt::FactsOf<FMT>::type& f, int c,
+                                        float sl, float nlse, float ndelta, uint32_t (&e)[16]) {
+  constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
+  uint32_t s[32], r[32];
+  um::ld32(tS, s);
+  um::ld32(tR, r);
+  const float2 nl = make_float2(nlse, nlse), nd = make_float2(ndelta, ndelta), sl2 = make_float2(sl, sl);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float4 ksl, ks, vs;
+    if constexpr (kQuant) {
+      ksl = *reinterpret_cast<const float4*>(&f.ksl[32 * c + 4 * j]);
+      ks = *reinterpret_cast<const float4*>(&f.ks[32 * c + 4 * j]);
+      vs = *reinterpret_cast<const float4*>(&f.vs[32 * c + 4 * j]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = 4 * j + 2 * i;
+      float2 x = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
+      float2 y = make_float2(__uint_as_float(r[at]), __uint_as_float(r[at + 1]));
+      if constexpr (kQuant) {
+        x = ffma2(x, i ? make_float2(ksl.z, ksl.w) : make_float2(ksl.x, ksl.y), nl);
+        y = ffma2(y, i ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), nd);
+      } else {
+        x = ffma2(x, sl2, nl);
+        y = fadd2(y, nd);
+      }
+      x.x = um::ex2(x.x);
+      x.y = um::ex2(x.y);
+      x = fmul2(x, y);
+      if constexpr (kQuant) x = fmul2(x, i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y));
+      e[2 * j + i] = gt::pack2(x.x, x.y);
+    }
+  }
+  const uint32_t live = f.live[c];
+  if (live != kFull) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      e[j] &= (live >> (2 * j) & 1u ? 0xffffu : 0u) | (live >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ void softmax(const GradArgs& p, Misc<FMT>* m, uint32_t base, uint32_t tmem, int tid,
+                                        int share, int blk) {
+  constexpr int kKeys = Plan<FMT>::kKeys;
+  volatile int* ab = &m->abort;
+  const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
+  const int row = quad * 32 + lane;
+  const uint32_t at = (uint32_t)(quad * 32) << 16;  // this warp's lanes of tensor memory
+  const int rows = min(p.rb, p.rows - blk * p.rb);
+  uint32_t t = 0, item = 0;
+  bool ok = true;
+  gt::Walk walk(p, share);
+  gt::Item it;
+  while (walk.next(&it)) {
+    const gt::Item now = it;
+    const GradUnit x(p, now.u);
+    const float2* info = p.row + (int64_t)now.u * p.rows + blk * p.rb;
+    // rows and their gradients into shared memory, 16 lanes a row; a row that takes no part, or
+    // that holds a NaN or infinity, as zeros: what is summed over rows and slots stays clean
+#pragma unroll 1
+    for (int a = 0; a < 2; ++a) {
+      const Rows& src = a ? p.go : p.q;
+      const int c = tid & 15;
+      uint4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = (tid >> 4) + 16 * i;
+        v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows && fabsf(info[r].x) < INFINITY) {
+          const int br = blk * p.rb + r, tok = br / p.G, g = br - tok * p.G;
+          v[i] = __ldg(reinterpret_cast<const uint4*>(src.at(x.b, x.l, tok, x.h * p.G + g)) + c);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = (tid >> 4) + 16 * i;
+        sts128(base + (uint32_t)(a * kOperand + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)), v[i].x, v[i].y,
+               v[i].z, v[i].w);
+      }
+    }
+    const float2 mine = row < rows ? info[row] : make_float2(INFINITY, 0.f);
+    um::fence_async();
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(bar(&m->q_full));
+    for (int k = now.ka; ok && k < now.kb; ++k, ++t) {
+      const uint32_t place = t % kKeys;
+      ok = __all_sync(kFull, tc::mbar_wait(bar(&m->k_full[place]), (t / kKeys) & 1u, ab)) &&
+           __all_sync(kFull, tc::mbar_wait(bar(&m->s_full), t & 1u, ab));
+      if (!ok) break;
+      um::fence_after();
+#pragma unroll 1
+      for (int c = 2 * half; c < 2 * half + 2; ++c) {
+        uint32_t e[16];
+        const uint32_t tS = tmem + at + 128u * (t & 1u) + 32u * c;
+        columns<FMT>(tS, tmem + at + kColR + 32u * c, m->facts[place], c, p.scale_log2, -mine.x, -mine.y, e);
+        um::st16(tS, e);
+      }
+      um::wait_st();
+      um::fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar(&m->p_full));
+    }
+    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(&m->o_full), item & 1u, ab));
+    ++item;
+    um::fence_after();
+    float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + 64 * half;
+    const bool good = ok && *ab == 0;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+      uint32_t r[16];
+      um::ld16(tmem + at + kColQ + 64u * half + 16u * c, r);
+      if (row < rows) {
+        if (!good) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) r[j] = 0x7fc00000u;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; j += 8)  // whole sectors
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 16 * c + j), "r"(r[j]),
+                       "r"(r[j + 1]), "r"(r[j + 2]), "r"(r[j + 3]), "r"(r[j + 4]), "r"(r[j + 5]), "r"(r[j + 6]),
+                       "r"(r[j + 7])
+                       : "memory");
+      }
+    }
+    um::fence_before();
+    softmax_sync();  // every warp has read its part of dQ, and nothing reads the rows any more
+    um::fence_after();
+  }
+}
+
+// grid = groups nblk (one CTA per SM), block = kThreads.
+template <int FMT>
+__global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_constant__ GradArgs p) {
+  extern __shared__ char smem_raw[];
+  char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  Misc<FMT>* m = reinterpret_cast<Misc<FMT>*>(sm + Plan<FMT>::kMiscOff);
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 3; ++i) {
+      tc::mbar_init(bar(&m->k_full[i]), kGroupWarps);
+      tc::mbar_init(bar(&m->k_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(bar(&m->v_full[i]), kGroupWarps);
+      tc::mbar_init(bar(&m->v_empty[i]), 1);
+    }
+    tc::mbar_init(bar(&m->q_full), kSoftWarps);
+    tc::mbar_init(bar(&m->s_full), 1);
+    tc::mbar_init(bar(&m->p_full), kSoftWarps);
+    tc::mbar_init(bar(&m->o_full), 1);
+    tc::mbar_init(bar(&m->done), 1);
+    m->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  release_next();
+  await_previous();
+  const int share = blockIdx.x / p.nblk, blk = blockIdx.x - share * p.nblk;
+  if (tiles_per_share(p) * share >= p.first[p.units]) return;  // uniform, before any barrier
+  if (warp == kSoftWarps + kLoadWarps) um::alloc(tc::saddr(&m->tmem), 512);
+  um::fence_before();
+  __syncthreads();
+  um::fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&m->tmem);
+  const uint32_t base = tc::saddr(sm);
+  if (warp < kSoftWarps) {
+    gt::regs_up<kSoftRegs>();
+    softmax<FMT>(p, m, base, tmem, threadIdx.x, share, blk);
+  } else if (warp < kSoftWarps + kLoadWarps) {
+    gt::regs_down<kLoadRegs>();
+    const int tid = (int)threadIdx.x - kSoftWarps * 32;
+    if (tid < kGroupWarps * 32) {
+      gt::Feeder<FMT, Plan<FMT>::kKeys, true> f{p, m->k_full, m->k_empty, m->facts, &m->abort, base + Plan<FMT>::kKeyOff,
+                                                false, tid};
+      f.run(gt::Walk(p, share));
+    } else {
+      gt::Feeder<FMT, Plan<FMT>::kValues, false> f{p, m->v_full, m->v_empty, nullptr, &m->abort,
+                                                   base + Plan<FMT>::kValueOff, true, tid - kGroupWarps * 32};
+      f.run(gt::Walk(p, share));
+    }
+  } else {
+    gt::regs_down<kIssueRegs>();
+    if (warp == kSoftWarps + kLoadWarps) {
+      Issuer<FMT> is{m, tmem, base};
+      is.run(gt::Walk(p, share));
+    }
+    __syncwarp();
+  }
+  um::fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && m->abort && p.st.status) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
+  if (warp == kSoftWarps + kLoadWarps) {
+    um::fence_after();
+    um::dealloc(tmem, 512);
+  }
+}
+
+template <int FMT>
+bool launch(const GradArgs& p, cudaStream_t st) {
+  static std::atomic<uint64_t> ready{0};  // devices on which the shared memory is opted in to
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev > 63 || !(ready.load() >> dev & 1u)) {
+    if (cudaFuncSetAttribute(grad_q_kernel<FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<FMT>()) !=
+        cudaSuccess)
+      return false;
+    if (dev < 64) ready.fetch_or(1ull << dev);
+  }
+  return launch_kernel(true, grad_q_kernel<FMT>, (unsigned)(p.groups * p.nblk), kThreads, smem_bytes<FMT>(), st, p);
+}
+
+}  // namespace
+
+bool launch_grad_q(const GradArgs& p, int format, cudaStream_t st) {
+  TraceScope ts_("grad_q", st);
+  return format == CERTKV_STORE_BF16  ? launch<CERTKV_STORE_BF16>(p, st)
+         : format == CERTKV_STORE_FP8 ? launch<CERTKV_STORE_FP8>(p, st)
+                                      : launch<CERTKV_STORE_FP4>(p, st);
+}
+
+}  // namespace certkv

@@ -55,6 +55,7 @@
 #include "common.cuh"
 #include "follow.cuh"
 #include "internal.cuh"
+#include "operand.cuh"
 #include "tma.cuh"
 #include "tree.cuh"
 #include "umma.cuh"
@@ -63,10 +64,8 @@ namespace certkv {
 namespace {
 
 constexpr int kSoftWarps = 8;
-constexpr int kGroupWarps = 4, kLoadGroups = 2, kLoadWarps = kGroupWarps * kLoadGroups;
+constexpr int kLoadGroups = 2, kLoadWarps = kGroupWarps * kLoadGroups;
 constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
-// A loader thread's (slot, 16-element) pieces of an operand, kStep slots apart.
-constexpr int kPieces = 128 * 8 / (kGroupWarps * 32), kStep = 128 / kPieces;
 // Registers a thread: the launch gives 96 (640 threads), which the roles share
 // out among themselves.  A spill costs more here than elsewhere: next to 200 KB
 // of shared memory the L1 holds hardly any of it.  256 segments of 13107 slots, 256
@@ -74,8 +73,6 @@ constexpr int kPieces = 128 * 8 / (kGroupWarps * 32), kStep = 128 / kPieces;
 constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
               "a larger split would wait for registers for ever");
-constexpr int kHalf = 128 * 128;     // bytes of 128 rows x 64 16-bit elements
-constexpr int kOperand = 2 * kHalf;  // 128 rows x 128 elements
 constexpr int kAhead = 6;            // tiles the L2 prefetch runs ahead
 // Shared memory: the query blocks (two when both streams hold rows of their
 // own), then a ring of operands, then Misc.  Operand i is place i % 4.
@@ -143,10 +140,6 @@ __device__ __forceinline__ uint32_t bar(const uint64_t* b) { return tc::saddr(b)
 __device__ __forceinline__ void softmax_sync() {
   asm volatile("bar.sync 1, %0;" ::"n"(kSoftWarps * 32) : "memory");
 }
-__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w)
-               : "memory");
-}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -157,41 +150,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // |e| < 127
-
-// A loader thread's part of an operand: elements 16 sub .. 16 sub + 15 of the
-// rows grp, grp + kStep ..  A quarter warp holds the same half of two
-// neighbouring rows, which the swizzle puts into different banks.
-struct Piece {
-  int grp, sub;
-  uint32_t at0, at1;  // its two 16-byte chunks of row grp in a swizzled operand
-  __device__ __forceinline__ explicit Piece(int tid) {
-    const int lane = tid & 31;
-    grp = 4 * (tid >> 5) + 2 * (lane >> 4) + ((lane >> 2) & 1);
-    sub = (lane & 3) + 4 * ((lane >> 3) & 1);
-    const int c = 2 * (sub & 3), x = grp & 7;
-    const uint32_t r = (uint32_t)((sub >> 2) * kHalf + grp * 128);
-    at0 = r + (uint32_t)((c ^ x) << 4);
-    at1 = r + (uint32_t)(((c + 1) ^ x) << 4);
-  }
-  // row grp + kStep q of the operand at `to`
-  __device__ __forceinline__ void put(uint32_t to, int q, const uint32_t (&w)[8]) const {
-    sts128(to + at0 + (uint32_t)(q * kStep * 128), w[0], w[1], w[2], w[3]);
-    sts128(to + at1 + (uint32_t)(q * kStep * 128), w[4], w[5], w[6], w[7]);
-  }
-  // the eight lanes of a row
-  __device__ __forceinline__ static uint32_t row_max(uint32_t x) {
-    x = max(x, __shfl_xor_sync(kFull, x, 1));
-    x = max(x, __shfl_xor_sync(kFull, x, 2));
-    return max(x, __shfl_xor_sync(kFull, x, 8));
-  }
-};
-
-__device__ __forceinline__ void load32g(const void* p, uint32_t (&w)[8]) {
-  const uint4* q = reinterpret_cast<const uint4*>(p);
-  const uint4 a = __ldg(q), b = __ldg(q + 1);
-  w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-  w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-}
 
 // Largest magnitude of sixteen bf16 as fp32 bits (a NaN or infinity: >= 0x7f800000).
 __device__ __forceinline__ uint32_t top16(const uint32_t (&w)[8]) {
@@ -214,41 +172,6 @@ __device__ __forceinline__ int exponent(float x) {
   const int e = (__float_as_int(x) >> 23) & 255;
   return e == 0 || e == 255 ? 0 : e - 127;
 }
-
-// Raw codes of this thread's pieces of one operand.
-template <int FMT>
-struct Raw {
-  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
-  uint32_t w[kPieces][kWords];
-  uint32_t g[FMT == CERTKV_STORE_FP4 ? kPieces : 1];
-
-  // the tile's pages a, b (-1: none), live slots from its first on
-  __device__ __forceinline__ void load(const Piece& pc, int a, int b, int live, const uint8_t* codes,
-                                       const uint8_t* group) {
-#pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-      const int page = q < kPieces / 2 ? a : b, row = pc.grp + kStep * (q % (kPieces / 2));
-      const bool on = page >= 0 && pc.grp + kStep * q < live;
-      const int64_t at = (int64_t)page * kPage + row;
-#pragma unroll
-      for (int j = 0; j < kWords; ++j) w[q][j] = 0u;
-      if (on) {
-        if constexpr (FMT == CERTKV_STORE_FP8) {
-          const uint4 x = __ldg(reinterpret_cast<const uint4*>(codes + at * 128 + pc.sub * 16));
-          w[q][0] = x.x;
-          w[q][1] = x.y;
-          w[q][2] = x.z;
-          w[q][3] = x.w;
-        } else {
-          const uint2 x = __ldg(reinterpret_cast<const uint2*>(codes + at * 64 + pc.sub * 8));
-          w[q][0] = x.x;
-          w[q][1] = x.y;
-        }
-      }
-      if constexpr (FMT == CERTKV_STORE_FP4) g[q] = on ? (uint32_t)__ldg(group + at * kGroups + pc.sub) : 0u;
-    }
-  }
-};
 
 // Piece q as f16: codes, with their group scale (exact).
 template <int FMT>

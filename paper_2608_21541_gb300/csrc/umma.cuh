@@ -190,6 +190,37 @@ __device__ __forceinline__ void mma_o2(uint32_t d, uint32_t a, uint32_t b, uint3
       ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
       : "memory");
 }
+// One k-step (16 of k) of D (+)= A B by the one lane that calls: A in shared memory or
+// (mma_ts) in tensor memory; the low words of the descriptors, hi common to both.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 da, db;\n"
+      "setp.ne.b32 p, %5, 0;\nmov.b64 da, {%1, %3};\nmov.b64 db, {%2, %3};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 db;\n"
+      "setp.ne.b32 p, %5, 0;\nmov.b64 db, {%2, %3};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
+      : "memory");
+}
+// The same instruction descriptor for bf16 operands with N = n columns (a multiple of 16 up
+// to 256) and either operand MN-major.
+__host__ __device__ constexpr uint32_t idesc_n(uint32_t n, bool a_mn, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
+         ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// Whether this lane is the one that commit() below, too, elects.
+__device__ __forceinline__ bool elected() {
+  uint32_t e;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(e));
+  return e != 0;
+}
+
 // The whole warp calls; the lane that issues the MMAs commits them.
 __device__ __forceinline__ void commit(uint32_t mbar) {
   asm volatile(
