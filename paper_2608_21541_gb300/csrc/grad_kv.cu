@@ -26,11 +26,14 @@
 namespace certkv {
 namespace {
 
-using gt::bar;
-constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps, kRowWarps = 2;
-constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
-constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
-static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
+// Warps: softmax, loaders, then the issuer and two that bring rows, then four that write the slots'
+// gradients.
+constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps, kRowWarps = 2, kDrainWarps = 4;
+constexpr int kIssue = kSoftWarps + kLoadWarps, kDrain = kIssue + 4;
+constexpr int kThreads = (kDrain + kDrainWarps) * 32;  // whole warpgroups
+constexpr int kSoftRegs = 96, kLoadRegs = 80, kIssueRegs = 64, kDrainRegs = 64;
+static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs + kDrainWarps * 32 * kDrainRegs <=
+                  kThreads * 80,
               "a larger split would wait for registers for ever");
 constexpr int kCols = kGradFused;       // query rows of a block
 constexpr int kRowHalf = kCols * 128;   // bytes of a block's 64 rows x 64 elements
@@ -52,7 +55,7 @@ struct Misc {
   uint64_t b_full[4], b_empty[4];
   uint64_t s_full[2], p_full[2], o_full, drained, done;
   uint32_t tmem;
-  int abort;
+  int abort, last;  // last: a flag that nobody sets
   alignas(16) float nlse[Plan<FUSED>::kBlocks][kCols], ndelta[Plan<FUSED>::kBlocks][kCols];  // negated
 };
 template <bool FUSED>
@@ -81,7 +84,8 @@ struct Steps {
   int k, j, n;
   uint32_t i = 0, t = 0, item = 0;
   __device__ __forceinline__ Steps(const GradArgs& p_, int share) : p(p_), walk(p_, share) {
-    it.ka = it.kb = k = j = 0;
+    it = {0, 0, 0};
+    k = j = 0;
     n = blocks_of(p_);
   }
   __device__ __forceinline__ bool next(Step* s) {
@@ -106,43 +110,48 @@ struct Steps {
 // zeros.
 template <bool FUSED>
 struct RowFeeder {
+  using P = Plan<FUSED>;
+  using M = Misc<FUSED>;
   const GradArgs& p;
-  Misc<FUSED>* m;
-  uint32_t ring;
+  uint32_t base;
   int tid;  // of 64
+  uint32_t over_g;  // 65536 / G, rounded up
   uint32_t n = 0;
   bool pending = false;
 
   __device__ __forceinline__ void hand_over(uint32_t i) const {
-    um::fence_async();
     __syncwarp();
-    if ((tid & 31) == 0) tc::mbar_arrive(bar(&m->b_full[i % Plan<FUSED>::kBlocks]));
+    if ((tid & 31) == 0) tc::mbar_arrive(GRAD_AT(b_full) + 8u * (i % Plan<FUSED>::kBlocks));
   }
   __device__ __forceinline__ bool block(int u, int j) {
     constexpr uint32_t kPlaces = Plan<FUSED>::kBlocks;
     const uint32_t place = n % kPlaces, phase = ((n / kPlaces) & 1u) ^ 1u;
-    if (pending && !__all_sync(kFull, tc::mbar_test(bar(&m->b_empty[place]), phase))) {
+    if (pending && !__all_sync(kFull, tc::mbar_test(GRAD_AT(b_empty) + 8u * place, phase))) {
       gt::cp_wait<0>();
       hand_over(n - 1);
       pending = false;
     }
-    if (!__all_sync(kFull, tc::mbar_wait(bar(&m->b_empty[place]), phase, &m->abort))) return false;
     const GradUnit x(p, u);
-    const int rows = rows_of_block(p, j);
+    const int rows = rows_of_block(p, j), lane = tid & 31;
     const float2* info = p.row + (int64_t)u * p.rows + j * kCols;
-    const float2 mine = tid < rows ? info[tid] : make_float2(INFINITY, 0.f);
-    m->nlse[place][tid] = -mine.x;
-    m->ndelta[place][tid] = -mine.y;
-    const uint32_t to = ring + place * kBlock;
+    const float2 lo = lane < rows ? info[lane] : make_float2(INFINITY, 0.f);
+    const float2 hi = lane + 32 < rows ? info[lane + 32] : make_float2(INFINITY, 0.f);
+    const uint64_t good = __ballot_sync(kFull, fabsf(lo.x) < INFINITY) |
+                          (uint64_t)__ballot_sync(kFull, fabsf(hi.x) < INFINITY) << 32;
+    if (!gt::wait_all(GRAD_AT(b_empty) + 8u * place, phase, GRAD_AT(abort))) return false;
+    gt::sts32(GRAD_AT(nlse) + 4 * (place * kCols + tid), __float_as_uint(tid < 32 ? -lo.x : -hi.x));
+    gt::sts32(GRAD_AT(ndelta) + 4 * (place * kCols + tid), __float_as_uint(tid < 32 ? -lo.y : -hi.y));
+    const uint32_t to = base + P::kBlockOff + place * kBlock;
     const int c = tid & 15;
-#pragma unroll 4
+    const uint16_t *q0 = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *g0 = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
+#pragma unroll 8
     for (int i = 0; i < 16; ++i) {
-      const int r = (tid >> 4) + 4 * i;
-      const bool on = r < rows && fabsf(info[min(r, rows - 1)].x) < INFINITY;
-      const int br = j * kCols + min(r, rows - 1), tok = br / p.G, qh = x.h * p.G + br - tok * p.G;
+      const int r = (tid >> 4) + 4 * i, br = j * kCols + r;
+      const bool on = good >> r & 1u;
+      const int tok = (int)((uint32_t)br * over_g >> 16), g = br - tok * p.G;  // br < 2^11, G <= 32: exact
       const uint32_t at = to + (uint32_t)((c >> 3) * kRowHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-      gt::cp16(at, p.q.at(x.b, x.l, tok, qh) + 8 * c, on);
-      gt::cp16(at + 2 * kRowHalf, p.go.at(x.b, x.l, tok, qh) + 8 * c, on);
+      gt::cp16(at, on ? q0 + tok * p.q.st + g * p.q.sh : q0, on);
+      gt::cp16(at + 2 * kRowHalf, on ? g0 + tok * p.go.st + g * p.go.sh : g0, on);
     }
     gt::cp_commit();
     if (pending) {
@@ -170,77 +179,62 @@ struct RowFeeder {
 template <bool FUSED>
 struct Issuer {
   using P = Plan<FUSED>;
+  using M = Misc<FUSED>;
   const GradArgs& p;
-  Misc<FUSED>* m;
   uint32_t tmem, base;
   bool ok = true;
   uint32_t tiles = 0;  // whose products have been begun
   uint32_t odd = 0;    // parities of p_full
-  __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
-    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(b), phase & 1u, &m->abort));
+  static __device__ __forceinline__ uint32_t uni(uint32_t x) { return __shfl_sync(kFull, x, 0); }
+  __device__ __forceinline__ void wait(uint32_t mbar, uint32_t phase) {
+    if (ok) ok = gt::wait_all(mbar, phase & 1u, GRAD_AT(abort));
   }
   __device__ __forceinline__ uint32_t buffer(const Step& s) const { return FUSED ? 0u : s.i & 1u; }
   __device__ __forceinline__ uint32_t columns(const Step& s) const { return up16(rows_of_block(p, s.j)); }
   // S and R of a block
   __device__ __forceinline__ void logits(const Step& s) {
     if (s.j == 0) {
-      wait(&m->k_full[s.t % P::kKeys], s.t / P::kKeys);
-      wait(&m->v_full[s.t % P::kValues], s.t / P::kValues);
+      wait(GRAD_AT(k_full) + 8u * (s.t % P::kKeys), s.t / P::kKeys);
+      wait(GRAD_AT(v_full) + 8u * (s.t % P::kValues), s.t / P::kValues);
     }
-    if (!FUSED || s.first) wait(&m->b_full[s.blk % P::kBlocks], s.blk / P::kBlocks);
+    if (!FUSED || s.first) wait(GRAD_AT(b_full) + 8u * (s.blk % P::kBlocks), s.blk / P::kBlocks);
     if (!ok) return;
+    um::fence_async();  // the loaders' writes, before the tensor core's reads
     um::fence_after();
-    if (um::elected()) {
-      const uint32_t d = tmem + 128u * buffer(s), id = um::idesc_n(columns(s), false, false);
-      const uint32_t k = um::desc_lo(base + (s.t % P::kKeys) * kOperand, 16);
-      const uint32_t v = um::desc_lo(base + P::kValueOff + (s.t % P::kValues) * kOperand, 16);
-      const uint32_t q = um::desc_lo(base + P::kBlockOff + (s.blk % P::kBlocks) * kBlock, 16);
-#pragma unroll
-      for (uint32_t i = 0; i < 8; ++i)
-        um::mma_ss(d, k + 2 * (i & 3) + (i >> 2) * (kHalf >> 4), q + 2 * (i & 3) + (i >> 2) * (kRowHalf >> 4),
-                   um::kDescHi, id, i > 0);
-#pragma unroll
-      for (uint32_t i = 0; i < 8; ++i)
-        um::mma_ss(d + 64, v + 2 * (i & 3) + (i >> 2) * (kHalf >> 4),
-                   q + (2 * kRowHalf >> 4) + 2 * (i & 3) + (i >> 2) * (kRowHalf >> 4), um::kDescHi, id, i > 0);
-    }
-    __syncwarp();
-    um::commit(bar(&m->s_full[buffer(s)]));
+    const uint32_t d = uni(tmem + 128u * buffer(s)), id = uni(um::idesc_n(columns(s), false, false));
+    const uint32_t k = uni(um::desc_lo(base, 16) + (s.t % P::kKeys) * (kOperand >> 4));
+    const uint32_t v = uni(um::desc_lo(base + P::kValueOff, 16) + (s.t % P::kValues) * (kOperand >> 4));
+    const uint32_t q = uni(um::desc_lo(base + P::kBlockOff, 16) + (s.blk % P::kBlocks) * (kBlock >> 4));
+    um::mma_s64(d, k, q, um::kDescHi, id, 0u);
+    um::mma_s64(uni(d + 64), v, uni(q + (2 * kRowHalf >> 4)), um::kDescHi, id, 0u);
+    um::commit(uni(GRAD_AT(s_full) + 8u * (buffer(s))));
     if (s.j + 1 == s.n) {
-      um::commit(bar(&m->v_empty[s.t % P::kValues]));
-      if (!FUSED) um::commit(bar(&m->k_empty[s.t % P::kKeys]));
+      um::commit(uni(GRAD_AT(v_empty) + 8u * (s.t % P::kValues)));
+      if (!FUSED) um::commit(uni(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys)));
     }
   }
   // what p and e of a block go into
   __device__ __forceinline__ void products(const Step& s) {
     const uint32_t x = buffer(s);
-    wait(&m->p_full[x], odd >> x & 1u);
+    wait(GRAD_AT(p_full) + 8u * (x), odd >> x & 1u);
     odd ^= 1u << x;
-    if (s.j == 0 && tiles++ > 0) wait(&m->drained, tiles - 2);
+    if (s.j == 0 && tiles++ > 0) wait(GRAD_AT(drained), tiles - 2);
     if (!ok) return;
+    if (FUSED) um::fence_async();
     um::fence_after();
-    if (um::elected()) {
-      const uint32_t a = tmem + 128u * x, steps = columns(s) / 16;
-      const uint32_t q = um::desc_lo(base + P::kBlockOff + (s.blk % P::kBlocks) * kBlock, kRowHalf);
-      constexpr uint32_t id = um::idesc_n(128, false, true);
-      // 16 rows a step: 8 columns of every 32 for p, 16 on for e; 2048 bytes of the block
-      for (uint32_t i = 0; i < steps; ++i)
-        um::mma_ts(tmem + kColV, a + 32 * (i >> 1) + 8 * (i & 1), q + (2 * kRowHalf >> 4) + 128 * i, um::kDescHi, id,
-                   s.j > 0 || i > 0);
-      for (uint32_t i = 0; i < steps; ++i)
-        um::mma_ts(tmem + kColK, a + 16 + 32 * (i >> 1) + 8 * (i & 1), q + 128 * i, um::kDescHi, id, s.j > 0 || i > 0);
-      if (FUSED) {
-        const uint32_t k = um::desc_lo(base + (s.t % P::kKeys) * kOperand, kHalf);
-        const uint32_t e = um::desc_lo(base + P::kEOff, 16), idq = um::idesc_n(columns(s), true, true);
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-          um::mma_ss(tmem + kColQ, k + 128 * i, e + 128 * i, um::kDescHi, idq, !s.first || i > 0);
-      }
+    const uint32_t a = uni(tmem + 128u * x), steps = uni(columns(s) / 16), acc = uni(s.j > 0);
+    const uint32_t q = uni(um::desc_lo(base + P::kBlockOff, kRowHalf) + (s.blk % P::kBlocks) * (kBlock >> 4));
+    constexpr uint32_t id = um::idesc_n(128, false, true);
+    um::mma_p64(uni(tmem + kColV), a, uni(q + (2 * kRowHalf >> 4)), um::kDescHi, id, acc, steps);
+    um::mma_p64(uni(tmem + kColK), uni(a + 16), q, um::kDescHi, id, acc, steps);
+    if (FUSED) {
+      const uint32_t k = uni(um::desc_lo(base, kHalf) + (s.t % P::kKeys) * (kOperand >> 4));
+      um::mma_mn(uni(tmem + kColQ), k, uni(um::desc_lo(base + P::kEOff, 16)), um::kDescHi,
+                 uni(um::idesc_n(columns(s), true, true)), uni(!s.first));
     }
-    __syncwarp();
-    if (FUSED) um::commit(bar(&m->k_empty[s.t % P::kKeys]));
-    if (!FUSED || s.last) um::commit(bar(&m->b_empty[s.blk % P::kBlocks]));
-    if (s.j + 1 == s.n) um::commit(bar(&m->o_full));
+    if (FUSED) um::commit(uni(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys)));
+    if (!FUSED || s.last) um::commit(uni(GRAD_AT(b_empty) + 8u * (s.blk % P::kBlocks)));
+    if (s.j + 1 == s.n) um::commit(uni(GRAD_AT(o_full)));
   }
   __device__ __forceinline__ void run(int share) {
     Steps<FUSED> steps(p, share);
@@ -257,9 +251,8 @@ struct Issuer {
       if (more && !ahead) logits(nxt);
       cur = nxt;
     }
-    um::commit(bar(&m->done));  // everything issued above has finished
-    volatile int dummy = 0;
-    tc::mbar_wait(bar(&m->done), 0, &dummy);
+    um::commit(GRAD_AT(done));  // everything issued above has finished
+    gt::wait(GRAD_AT(done), 0, GRAD_AT(last));
     __syncwarp();
   }
 };
@@ -267,10 +260,10 @@ struct Issuer {
 // The slot of a softmax thread.
 template <int FMT>
 struct Slot {
-  int64_t at;        // of the pool, -1: none
+  int at;            // of the pool, -1: none
   float ks, vs;      // scales of its key and value
   __device__ __forceinline__ void load(const GradArgs& p, int u, int s, int count) {
-    at = s < count ? p.st.slot(u, s) : -1;
+    at = s < count ? (int)p.st.slot(u, s) : -1;  // pools have fewer than 2^31 slots
     ks = vs = gt::kCodeScale<FMT>;
     if (FMT != CERTKV_STORE_BF16 && at >= 0) {
       ks *= __ldg(p.st.ks + at);
@@ -279,25 +272,21 @@ struct Slot {
   }
 };
 
-__device__ __forceinline__ void store_row_part(uint16_t* to, const uint32_t (&w)[16]) {
-#pragma unroll
-  for (int j = 0; j < 16; j += 8)  // whole sectors
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 2 * j), "r"(w[j]), "r"(w[j + 1]),
-                 "r"(w[j + 2]), "r"(w[j + 3]), "r"(w[j + 4]), "r"(w[j + 5]), "r"(w[j + 6]), "r"(w[j + 7])
-                 : "memory");
+__device__ __forceinline__ void store_sector(uint16_t* to, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
 }
 
 template <int FMT, bool FUSED>
-__device__ __forceinline__ void softmax(const GradArgs& p, Misc<FUSED>* m, uint32_t base, uint32_t tmem, int tid,
-                                        int share) {
+__device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share) {
   using P = Plan<FUSED>;
+  using M = Misc<FUSED>;
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
-  volatile int* ab = &m->abort;
   const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
   const int row = quad * 32 + lane;  // slot of the tile
   const uint32_t at = (uint32_t)(quad * 32) << 16;
   const int blocks = blocks_of(p);
-  const bool want_q = FUSED && p.dq.p;
   uint32_t i = 0, t = 0, item = 0;
   bool ok = true;
   gt::Walk walk(p, share);
@@ -317,8 +306,8 @@ __device__ __forceinline__ void softmax(const GradArgs& p, Misc<FUSED>* m, uint3
         const uint32_t x = FUSED ? 0u : i & 1u, use = FUSED ? i : i >> 1, blk = FUSED ? item : i;
         const uint32_t place = blk % P::kBlocks;
         if (!FUSED || k == now.ka)
-          ok = __all_sync(kFull, tc::mbar_wait(bar(&m->b_full[place]), (blk / P::kBlocks) & 1u, ab));
-        ok = ok && __all_sync(kFull, tc::mbar_wait(bar(&m->s_full[x]), use & 1u, ab));
+          ok = gt::wait_all(GRAD_AT(b_full) + 8u * place, (blk / P::kBlocks) & 1u, GRAD_AT(abort));
+        ok = ok && gt::wait_all(GRAD_AT(s_full) + 8u * x, use & 1u, GRAD_AT(abort));
         if (!ok) break;
         um::fence_after();
         if (32 * half < rows_of_block(p, j)) {
@@ -326,12 +315,12 @@ __device__ __forceinline__ void softmax(const GradArgs& p, Misc<FUSED>* m, uint3
           uint32_t s[32], r[32], pw[16], ew[16], qw[16];
           um::ld32(tS, s);
           um::ld32(tS + 64u, r);
-          const float* nlse = &m->nlse[place][32 * half];
-          const float* ndelta = &m->ndelta[place][32 * half];
+          const uint32_t nlse = GRAD_AT(nlse) + 4 * (place * kCols + 32 * half);
+          const uint32_t ndelta = GRAD_AT(ndelta) + 4 * (place * kCols + 32 * half);
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
-            const float4 l4 = *reinterpret_cast<const float4*>(nlse + 4 * c);
-            const float4 d4 = *reinterpret_cast<const float4*>(ndelta + 4 * c);
+            const float4 l4 = gt::lds128(nlse + 16 * c);
+            const float4 d4 = gt::lds128(ndelta + 16 * c);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int q = 4 * c + 2 * h;
@@ -360,46 +349,66 @@ __device__ __forceinline__ void softmax(const GradArgs& p, Misc<FUSED>* m, uint3
               const uint32_t* w = kQuant ? &qw[4 * c] : &ew[4 * c];
               sts128(to + (uint32_t)(((4 * half + c) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
             }
-            um::fence_async();
           }
           um::wait_st();
         }
         um::fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(bar(&m->p_full[x]));
+        if (lane == 0) tc::mbar_arrive(GRAD_AT(p_full) + 8u * (x));
       }
-      // ---- the tile's gradients, 64 elements a thread
-      if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(&m->o_full), t & 1u, ab));
+    }
+    ++item;
+  }
+}
+
+// The four warps that write a tile's gradients, a slot a thread, while the softmax goes on with
+// the next tile; at an item's end (FUSED) its queries' too.
+template <int FMT, bool FUSED>
+__device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share) {
+  using P = Plan<FUSED>;
+  using M = Misc<FUSED>;
+  const int lane = tid & 31, quad = tid >> 5;
+  const uint32_t at = (uint32_t)(quad * 32) << 16;
+  uint32_t t = 0;
+  bool ok = true;
+  gt::Walk walk(p, share);
+  gt::Item it;
+  while (walk.next(&it)) {
+    const gt::Item now = it;
+    const int count = p.st.count(now.u);
+    for (int k = now.ka; k < now.kb; ++k, ++t) {
+      const int s = k * kGradTile + tid;
+      const int64_t slot = s < count ? p.st.slot(now.u, s) : -1;
+      ok = ok && gt::wait_all(GRAD_AT(o_full), t & 1u, GRAD_AT(abort));
       um::fence_after();
-      const bool good = ok && *ab == 0;
+      const bool good = ok && !gt::aborted(GRAD_AT(abort));
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        const bool key = c >= 2;
-        const int d0 = 64 * half + 32 * (c & 1);
-        uint32_t r[32], w[16];
-        um::ld32(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
+      for (int c = 0; c < 16; ++c) {
+        const bool key = c >= 8;
+        const int d0 = 16 * (c & 7);
+        uint32_t r[16], w[8];
+        um::ld16(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
         const float f = key ? p.scale : 1.f;
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
+        for (int q = 0; q < 8; ++q)
           w[q] = good ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : 0x7fc07fc0u;
-        if (live) store_row_part((key ? p.dks : p.dvs) + slot.at * kD + d0, w);
+        if (slot >= 0) store_sector((key ? p.dks : p.dvs) + slot * kD + d0, w);
       }
-      if (want_q && k + 1 == now.kb) {
-        float* out = p.rec + grad_record(p, share, now.u, 0) * kD + row;
-        const int r0 = 32 * half, rows = min(p.rows - r0, 32);
-        if (rows > 0) {
-          uint32_t r[32];
-          um::ld32(tmem + at + kColQ + (uint32_t)r0, r);
+      if (FUSED && p.dq.p && k + 1 == now.kb) {  // element tid of every row
+        float* out = p.rec + grad_record(p, share, now.u, 0) * kD + tid;
+#pragma unroll 1
+        for (int r0 = 0; r0 < p.rows; r0 += 16) {
+          uint32_t r[16];
+          um::ld16(tmem + at + kColQ + (uint32_t)r0, r);
 #pragma unroll
-          for (int q = 0; q < 32; ++q)
-            if (q < rows) out[(int64_t)(r0 + q) * kD] = good ? __uint_as_float(r[q]) : nanf("");
+          for (int q = 0; q < 16; ++q)
+            if (r0 + q < p.rows) out[(int64_t)(r0 + q) * kD] = good ? __uint_as_float(r[q]) : nanf("");
         }
       }
       um::fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bar(&m->drained));
+      if (lane == 0) tc::mbar_arrive(GRAD_AT(drained));
     }
-    ++item;
   }
 }
 
@@ -407,68 +416,72 @@ __device__ __forceinline__ void softmax(const GradArgs& p, Misc<FUSED>* m, uint3
 template <int FMT, bool FUSED>
 __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_constant__ GradArgs p) {
   using P = Plan<FUSED>;
+  using M = Misc<FUSED>;
   extern __shared__ char smem_raw[];
-  char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  Misc<FUSED>* m = reinterpret_cast<Misc<FUSED>*>(sm + P::kMiscOff);
+  const uint32_t base = (tc::saddr(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(bar(&m->k_full[i]), kGroupWarps);
-      tc::mbar_init(bar(&m->k_empty[i]), 1);
-      tc::mbar_init(bar(&m->v_full[i]), kGroupWarps);
-      tc::mbar_init(bar(&m->v_empty[i]), 1);
-      tc::mbar_init(bar(&m->s_full[i]), 1);
-      tc::mbar_init(bar(&m->p_full[i]), kSoftWarps);
+      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(k_empty) + 8u * (i), 1);
+      tc::mbar_init(GRAD_AT(v_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(v_empty) + 8u * (i), 1);
+      tc::mbar_init(GRAD_AT(s_full) + 8u * (i), 1);
+      tc::mbar_init(GRAD_AT(p_full) + 8u * (i), kSoftWarps);
     }
     for (int i = 0; i < 4; ++i) {
-      tc::mbar_init(bar(&m->b_full[i]), kRowWarps);
-      tc::mbar_init(bar(&m->b_empty[i]), 1);
+      tc::mbar_init(GRAD_AT(b_full) + 8u * (i), kRowWarps);
+      tc::mbar_init(GRAD_AT(b_empty) + 8u * (i), 1);
     }
-    tc::mbar_init(bar(&m->o_full), 1);
-    tc::mbar_init(bar(&m->drained), kSoftWarps);
-    tc::mbar_init(bar(&m->done), 1);
-    m->abort = 0;
+    tc::mbar_init(GRAD_AT(o_full), 1);
+    tc::mbar_init(GRAD_AT(drained), kDrainWarps);
+    tc::mbar_init(GRAD_AT(done), 1);
+    gt::sts32(GRAD_AT(abort), 0u);
+    gt::sts32(GRAD_AT(last), 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   release_next();
   await_previous();
   const int share = blockIdx.x;
   if (tiles_per_share(p) * share >= p.first[p.units]) return;  // uniform, before any barrier
-  if (warp == kSoftWarps + kLoadWarps) um::alloc(tc::saddr(&m->tmem), 512);
+  if (warp == kIssue) um::alloc(GRAD_AT(tmem), 512);
   um::fence_before();
   __syncthreads();
   um::fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&m->tmem);
-  const uint32_t base = tc::saddr(sm);
+  const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
   if (warp < kSoftWarps) {
     gt::regs_up<kSoftRegs>();
-    softmax<FMT, FUSED>(p, m, base, tmem, threadIdx.x, share);
+    softmax<FMT, FUSED>(p, base, tmem, threadIdx.x, share);
   } else if (warp < kSoftWarps + kLoadWarps) {
     gt::regs_down<kLoadRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
     if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, P::kKeys, false> f{p, m->k_full, m->k_empty, nullptr, &m->abort, base, false, tid};
-      f.run(gt::Walk(p, share));
+      gt::Feeder<FMT, P::kKeys, false, false> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), 0u, GRAD_AT(abort), base, tid};
+      f.run(share);
     } else {
-      gt::Feeder<FMT, P::kValues, false> f{p,  m->v_full, m->v_empty, nullptr, &m->abort, base + P::kValueOff,
-                                           true, tid - kGroupWarps * 32};
-      f.run(gt::Walk(p, share));
+      gt::Feeder<FMT, P::kValues, true, false> f{p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort),
+                                                 base + P::kValueOff, tid - kGroupWarps * 32};
+      f.run(share);
     }
-  } else {
+  } else if (warp < kDrain) {
     gt::regs_down<kIssueRegs>();
-    if (warp == kSoftWarps + kLoadWarps) {
-      Issuer<FUSED> is{p, m, tmem, base};
+    if (warp == kIssue) {
+      Issuer<FUSED> is{p, tmem, base};
       is.run(share);
-    } else if (warp <= kSoftWarps + kLoadWarps + kRowWarps) {
-      RowFeeder<FUSED> f{p, m, base + P::kBlockOff, (int)threadIdx.x - (kSoftWarps + kLoadWarps + 1) * 32};
+    } else if (warp <= kIssue + kRowWarps) {
+      RowFeeder<FUSED> f{p, base, (int)threadIdx.x - (kIssue + 1) * 32,
+                         (65536u + p.G - 1) / p.G};
       f.run(share);
     }
     __syncwarp();
+  } else {
+    gt::regs_down<kDrainRegs>();
+    drain<FMT, FUSED>(p, base, tmem, (int)threadIdx.x - kDrain * 32, share);
   }
   um::fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && m->abort && p.st.status) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
-  if (warp == kSoftWarps + kLoadWarps) {
+  if (threadIdx.x == 0 && p.st.status && gt::aborted(GRAD_AT(abort))) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
+  if (warp == kIssue) {
     um::fence_after();
     um::dealloc(tmem, 512);
   }

@@ -3,8 +3,9 @@
 // A CTA holds up to 128 query rows of a unit, and their output's gradients, as the M = 128 rows
 // of the MMAs, and walks a share of all tiles of 128 slots:
 //   S = Q K^T,  R = dO V^T,  e = 2^(S - lse) (R - delta),  dQ += e K,
-// with e rounded once to bf16 and handed over in tensor memory, over S.  Neither a maximum nor
-// a rescaling is needed, the log-sum-exp is known, so a tile is formed in one pass.
+// with e handed over in tensor memory, over S, as a bf16 part plus the bf16 rounding of its
+// remainder (2^-16).  Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so
+// a tile is formed in one pass.
 // Tensor memory: S of even tiles | S of odd tiles | R | dQ, 128 columns each.  S of the next
 // tile is made while e of this one is, R of the next as soon as R of this one has been read,
 // dQ of this one under e of the next.
@@ -26,10 +27,9 @@
 namespace certkv {
 namespace {
 
-using gt::bar;
 constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps;
 constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
-constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
+constexpr int kSoftRegs = 112, kLoadRegs = 96, kIssueRegs = 64;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
               "a larger split would wait for registers for ever");
 constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
@@ -45,10 +45,10 @@ struct Plan {
 template <int FMT>
 struct Misc {
   uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
-  uint64_t q_full, s_full, p_full, o_full, done;
+  uint64_t q_full, s_full, r_free, p_full, o_full, done;
   uint32_t tmem;
-  int abort;
-  typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kKeys];
+  int abort, last;  // last: a flag that nobody sets
+  alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kKeys];
 };
 template <int FMT>
 constexpr int smem_bytes() {
@@ -64,85 +64,105 @@ __device__ __forceinline__ void softmax_sync() {
 // Issues the MMAs of the share's tiles; the whole warp runs, one lane issues.
 template <int FMT>
 struct Issuer {
-  Misc<FMT>* m;
+  using P = Plan<FMT>;
+  using M = Misc<FMT>;
   uint32_t tmem, base;
   bool ok = true;
   static __device__ __forceinline__ uint32_t uni(uint32_t x) { return __shfl_sync(kFull, x, 0); }
-  __device__ __forceinline__ void wait(const uint64_t* b, uint32_t phase) {
-    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(b), phase & 1u, &m->abort));
+  __device__ __forceinline__ void wait(uint32_t mbar, uint32_t phase) {
+    if (ok) ok = gt::wait_all(mbar, phase & 1u, GRAD_AT(abort));
   }
   __device__ __forceinline__ uint32_t key(uint32_t t, uint32_t lbo) const {
-    return uni(um::desc_lo(base + Plan<FMT>::kKeyOff, lbo) + (t % Plan<FMT>::kKeys) * (kOperand >> 4));
+    return uni(um::desc_lo(base + P::kKeyOff, lbo) + (t % P::kKeys) * (kOperand >> 4));
+  }
+  // Whether the keys and values of tile t are in place.
+  __device__ __forceinline__ bool there(uint32_t t) const {
+    return __all_sync(kFull, tc::mbar_test(GRAD_AT(k_full) + 8u * (t % P::kKeys), (t / P::kKeys) & 1u) &&
+                                 tc::mbar_test(GRAD_AT(v_full) + 8u * (t % P::kValues), (t / P::kValues) & 1u));
   }
   __device__ __forceinline__ void s(uint32_t t) {
-    wait(&m->k_full[t % Plan<FMT>::kKeys], t / Plan<FMT>::kKeys);
+    wait(GRAD_AT(k_full) + 8u * (t % P::kKeys), t / P::kKeys);
     if (!ok) return;
+    um::fence_async();
     um::fence_after();
     um::mma_s(uni(tmem + 128u * (t & 1u)), uni(um::desc_lo(base, 16)), key(t, 16), um::kDescHi, um::idesc(true, false));
   }
   __device__ __forceinline__ void r(uint32_t t) {
-    const uint32_t place = t % Plan<FMT>::kValues;
-    wait(&m->v_full[place], t / Plan<FMT>::kValues);
+    const uint32_t place = t % P::kValues;
+    wait(GRAD_AT(v_full) + 8u * (place), t / P::kValues);
     if (!ok) return;
+    um::fence_async();
     um::fence_after();
     um::mma_s(uni(tmem + kColR), uni(um::desc_lo(base + kOperand, 16)),
-              uni(um::desc_lo(base + Plan<FMT>::kValueOff, 16) + place * (kOperand >> 4)), um::kDescHi,
+              uni(um::desc_lo(base + P::kValueOff, 16) + place * (kOperand >> 4)), um::kDescHi,
               um::idesc(true, false));
-    um::commit(uni(bar(&m->s_full)));
-    um::commit(uni(bar(&m->v_empty[place])));
+    um::commit(uni(GRAD_AT(s_full)));
+    um::commit(uni(GRAD_AT(v_empty) + 8u * (place)));
   }
   __device__ __forceinline__ void run(gt::Walk walk) {
     gt::Item it;
     uint32_t t = 0, item = 0;
     while (ok && walk.next(&it)) {
       const int n = it.kb - it.ka;
-      wait(&m->q_full, item++);
+      wait(GRAD_AT(q_full), item++);
       s(t);
       r(t);
       for (int i = 0; ok && i < n; ++i, ++t) {
-        const bool more = i + 1 < n;
-        if (more) s(t + 1);
-        wait(&m->p_full, t);
-        if (more) r(t + 1);
+        // The next tile's S and R go before this one's dQ where they can; where its keys are
+        // still on their way they may not hold up dQ, whose end gives a place back.
+        const bool more = i + 1 < n, early = more && there(t + 1);
+        if (early) {
+          s(t + 1);
+          wait(GRAD_AT(r_free), t);
+          r(t + 1);
+        }
+        wait(GRAD_AT(p_full), t);
         if (!ok) break;
         um::fence_after();
-        um::mma_o(uni(tmem + kColQ), uni(tmem + 128u * (t & 1u)), key(t, kHalf), um::kDescHi, um::idesc(true, true),
+        um::mma_o2(uni(tmem + kColQ), uni(tmem + 128u * (t & 1u)), key(t, kHalf), um::kDescHi, um::idesc(true, true),
                   uni(i > 0));
-        um::commit(uni(bar(&m->k_empty[t % Plan<FMT>::kKeys])));
-        if (!more) um::commit(uni(bar(&m->o_full)));
+        um::commit(uni(GRAD_AT(k_empty) + 8u * (t % P::kKeys)));
+        if (!more) um::commit(uni(GRAD_AT(o_full)));
+        if (more && !early) {
+          s(t + 1);
+          r(t + 1);
+        }
       }
     }
-    um::commit(bar(&m->done));  // everything issued above has finished
-    volatile int dummy = 0;
-    tc::mbar_wait(bar(&m->done), 0, &dummy);
+    um::commit(GRAD_AT(done));  // everything issued above has finished
+    gt::wait(GRAD_AT(done), 0, GRAD_AT(last));
     __syncwarp();
   }
 };
 
-// e of 32 columns of a row: the packed A operand.
-template <int FMT>
-__device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, const typename gt::FactsOf<FMT>::type& f, int c,
-                                        float sl, float nlse, float ndelta, uint32_t (&e)[16]) {
+// e of 32 columns of a row: the packed A operand and the rest of its rounding; facts: the address
+// of the tile's.  `loaded`: called
+// when the columns have been read.
+template <int FMT, class Loaded>
+__device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, uint32_t facts, int c,
+                                        float sl, float nlse, float ndelta, uint32_t (&e)[16], uint32_t (&rest)[16],
+                                        Loaded loaded) {
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
   uint32_t s[32], r[32];
   um::ld32(tS, s);
   um::ld32(tR, r);
+  loaded();
   const float2 nl = make_float2(nlse, nlse), nd = make_float2(ndelta, ndelta), sl2 = make_float2(sl, sl);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float4 ksl, ks, vs;
+    float4 ks, vs;
     if constexpr (kQuant) {
-      ksl = *reinterpret_cast<const float4*>(&f.ksl[32 * c + 4 * j]);
-      ks = *reinterpret_cast<const float4*>(&f.ks[32 * c + 4 * j]);
-      vs = *reinterpret_cast<const float4*>(&f.vs[32 * c + 4 * j]);
+      ks = gt::lds128(facts + (uint32_t)offsetof(gt::ScaledFacts, ks) + 128 * c + 16 * j);
+      vs = gt::lds128(facts + (uint32_t)offsetof(gt::ScaledFacts, vs) + 128 * c + 16 * j);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int at = 4 * j + 2 * i;
       float2 x = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
       float2 y = make_float2(__uint_as_float(r[at]), __uint_as_float(r[at + 1]));
+      const float2 k2 = i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y);
       if constexpr (kQuant) {
-        x = ffma2(x, i ? make_float2(ksl.z, ksl.w) : make_float2(ksl.x, ksl.y), nl);
+        x = ffma2(x, fmul2(k2, sl2), nl);
         y = ffma2(y, i ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), nd);
       } else {
         x = ffma2(x, sl2, nl);
@@ -151,27 +171,32 @@ __device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, const typename
       x.x = um::ex2(x.x);
       x.y = um::ex2(x.y);
       x = fmul2(x, y);
-      if constexpr (kQuant) x = fmul2(x, i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y));
+      if constexpr (kQuant) x = fmul2(x, k2);
       e[2 * j + i] = gt::pack2(x.x, x.y);
+      rest[2 * j + i] = gt::pack2(x.x - bf16lo(e[2 * j + i]), x.y - bf16hi(e[2 * j + i]));
     }
   }
-  const uint32_t live = f.live[c];
+  const uint32_t live = gt::lds32(facts + 4 * c);
   if (live != kFull) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-      e[j] &= (live >> (2 * j) & 1u ? 0xffffu : 0u) | (live >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t keep = (live >> (2 * j) & 1u ? 0xffffu : 0u) | (live >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
+      e[j] &= keep;
+      rest[j] &= keep;
+    }
   }
 }
 
 template <int FMT>
-__device__ __forceinline__ void softmax(const GradArgs& p, Misc<FMT>* m, uint32_t base, uint32_t tmem, int tid,
-                                        int share, int blk) {
-  constexpr int kKeys = Plan<FMT>::kKeys;
-  volatile int* ab = &m->abort;
+__device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share, int blk) {
+  using P = Plan<FMT>;
+  using M = Misc<FMT>;
+  constexpr int kKeys = P::kKeys;
   const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
   const int row = quad * 32 + lane;
   const uint32_t at = (uint32_t)(quad * 32) << 16;  // this warp's lanes of tensor memory
   const int rows = min(p.rb, p.rows - blk * p.rb);
+  const bool busy = quad * 32 < p.rb;  // some block has a row here
   uint32_t t = 0, item = 0;
   bool ok = true;
   gt::Walk walk(p, share);
@@ -206,30 +231,37 @@ __device__ __forceinline__ void softmax(const GradArgs& p, Misc<FMT>* m, uint32_
     const float2 mine = row < rows ? info[row] : make_float2(INFINITY, 0.f);
     um::fence_async();
     __syncwarp();
-    if (lane == 0) tc::mbar_arrive(bar(&m->q_full));
-    for (int k = now.ka; ok && k < now.kb; ++k, ++t) {
+    if (lane == 0) tc::mbar_arrive(GRAD_AT(q_full));
+    for (int k = now.ka; ok && busy && k < now.kb; ++k, ++t) {
       const uint32_t place = t % kKeys;
-      ok = __all_sync(kFull, tc::mbar_wait(bar(&m->k_full[place]), (t / kKeys) & 1u, ab)) &&
-           __all_sync(kFull, tc::mbar_wait(bar(&m->s_full), t & 1u, ab));
+      ok = gt::wait_all(GRAD_AT(k_full) + 8u * place, (t / kKeys) & 1u, GRAD_AT(abort)) &&
+           gt::wait_all(GRAD_AT(s_full), t & 1u, GRAD_AT(abort));
       if (!ok) break;
       um::fence_after();
 #pragma unroll 1
       for (int c = 2 * half; c < 2 * half + 2; ++c) {
-        uint32_t e[16];
+        uint32_t e[16], rest[16];
         const uint32_t tS = tmem + at + 128u * (t & 1u) + 32u * c;
-        columns<FMT>(tS, tmem + at + kColR + 32u * c, m->facts[place], c, p.scale_log2, -mine.x, -mine.y, e);
+        columns<FMT>(tS, tmem + at + kColR + 32u * c, GRAD_AT(facts) + place * (uint32_t)sizeof(typename gt::FactsOf<FMT>::type), c, p.scale_log2, -mine.x, -mine.y, e, rest, [&] {
+          if (c & 1) {  // this warp's half of R has been read
+            um::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(GRAD_AT(r_free));
+          }
+        });
         um::st16(tS, e);
+        um::st16(tS + 16u, rest);
       }
       um::wait_st();
       um::fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bar(&m->p_full));
+      if (lane == 0) tc::mbar_arrive(GRAD_AT(p_full));
     }
-    if (ok) ok = __all_sync(kFull, tc::mbar_wait(bar(&m->o_full), item & 1u, ab));
+    if (ok) ok = gt::wait_all(GRAD_AT(o_full), item & 1u, GRAD_AT(abort));
     ++item;
     um::fence_after();
     float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + 64 * half;
-    const bool good = ok && *ab == 0;
+    const bool good = ok && !gt::aborted(GRAD_AT(abort));
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
       uint32_t r[16];
@@ -257,62 +289,64 @@ __device__ __forceinline__ void softmax(const GradArgs& p, Misc<FMT>* m, uint32_
 template <int FMT>
 __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_constant__ GradArgs p) {
   extern __shared__ char smem_raw[];
-  char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  Misc<FMT>* m = reinterpret_cast<Misc<FMT>*>(sm + Plan<FMT>::kMiscOff);
+  using P = Plan<FMT>;
+  using M = Misc<FMT>;
+  const uint32_t base = (tc::saddr(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
-      tc::mbar_init(bar(&m->k_full[i]), kGroupWarps);
-      tc::mbar_init(bar(&m->k_empty[i]), 1);
+      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(k_empty) + 8u * (i), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(bar(&m->v_full[i]), kGroupWarps);
-      tc::mbar_init(bar(&m->v_empty[i]), 1);
+      tc::mbar_init(GRAD_AT(v_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(v_empty) + 8u * (i), 1);
     }
-    tc::mbar_init(bar(&m->q_full), kSoftWarps);
-    tc::mbar_init(bar(&m->s_full), 1);
-    tc::mbar_init(bar(&m->p_full), kSoftWarps);
-    tc::mbar_init(bar(&m->o_full), 1);
-    tc::mbar_init(bar(&m->done), 1);
-    m->abort = 0;
+    tc::mbar_init(GRAD_AT(q_full), kSoftWarps);
+    tc::mbar_init(GRAD_AT(s_full), 1);
+    tc::mbar_init(GRAD_AT(r_free), 2 * ((p.rb + 31) / 32));
+    tc::mbar_init(GRAD_AT(p_full), 2 * ((p.rb + 31) / 32));  // the warps with rows
+    tc::mbar_init(GRAD_AT(o_full), 1);
+    tc::mbar_init(GRAD_AT(done), 1);
+    gt::sts32(GRAD_AT(abort), 0u);
+    gt::sts32(GRAD_AT(last), 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   release_next();
   await_previous();
   const int share = blockIdx.x / p.nblk, blk = blockIdx.x - share * p.nblk;
   if (tiles_per_share(p) * share >= p.first[p.units]) return;  // uniform, before any barrier
-  if (warp == kSoftWarps + kLoadWarps) um::alloc(tc::saddr(&m->tmem), 512);
+  if (warp == kSoftWarps + kLoadWarps) um::alloc(GRAD_AT(tmem), 512);
   um::fence_before();
   __syncthreads();
   um::fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&m->tmem);
-  const uint32_t base = tc::saddr(sm);
+  const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
   if (warp < kSoftWarps) {
     gt::regs_up<kSoftRegs>();
-    softmax<FMT>(p, m, base, tmem, threadIdx.x, share, blk);
+    softmax<FMT>(p, base, tmem, threadIdx.x, share, blk);
   } else if (warp < kSoftWarps + kLoadWarps) {
     gt::regs_down<kLoadRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
     if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, Plan<FMT>::kKeys, true> f{p, m->k_full, m->k_empty, m->facts, &m->abort, base + Plan<FMT>::kKeyOff,
-                                                false, tid};
-      f.run(gt::Walk(p, share));
+      gt::Feeder<FMT, P::kKeys, false, true> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort),
+                                               base + P::kKeyOff, tid};
+      f.run(share);
     } else {
-      gt::Feeder<FMT, Plan<FMT>::kValues, false> f{p, m->v_full, m->v_empty, nullptr, &m->abort,
-                                                   base + Plan<FMT>::kValueOff, true, tid - kGroupWarps * 32};
-      f.run(gt::Walk(p, share));
+      gt::Feeder<FMT, P::kValues, true, false> f{p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort),
+                                                 base + P::kValueOff, tid - kGroupWarps * 32};
+      f.run(share);
     }
   } else {
     gt::regs_down<kIssueRegs>();
     if (warp == kSoftWarps + kLoadWarps) {
-      Issuer<FMT> is{m, tmem, base};
+      Issuer<FMT> is{tmem, base};
       is.run(gt::Walk(p, share));
     }
     __syncwarp();
   }
   um::fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && m->abort && p.st.status) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
+  if (threadIdx.x == 0 && p.st.status && gt::aborted(GRAD_AT(abort))) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
   if (warp == kSoftWarps + kLoadWarps) {
     um::fence_after();
     um::dealloc(tmem, 512);

@@ -2,6 +2,8 @@
 // a share's tiles, and the warps that bring keys and values into operands.
 #pragma once
 
+#include <stddef.h>
+
 #include "common.cuh"
 #include "grad.cuh"
 #include "operand.cuh"
@@ -11,7 +13,6 @@
 namespace certkv {
 namespace gt {
 
-__device__ __forceinline__ uint32_t bar(const uint64_t* b) { return tc::saddr(b); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -22,18 +23,54 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return r;
 }
 
+// A bounded wait, as tc::mbar_wait, with the abort flag in shared memory: a pointer less to keep.
+__device__ __forceinline__ bool aborted(uint32_t flag) {
+  int x;
+  asm volatile("ld.volatile.shared.b32 %0, [%1];" : "=r"(x) : "r"(flag) : "memory");
+  return x != 0;
+}
+__device__ __forceinline__ bool wait(uint32_t mbar, uint32_t parity, uint32_t flag) {
+  for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
+    if (tc::mbar_try(mbar, parity)) return true;
+    if ((i & 255u) == 255u && aborted(flag)) return false;
+  }
+  asm volatile("st.volatile.shared.b32 [%0], 1;" ::"r"(flag) : "memory");
+  return false;
+}
+// The same by a whole warp.
+__device__ __forceinline__ bool wait_all(uint32_t mbar, uint32_t parity, uint32_t flag) {
+  return __all_sync(kFull, wait(mbar, parity, flag));
+}
+
+// Shared memory by its address: generic pointers cost two registers each, and a spill next to
+// 200 KB of shared memory costs more than anything else (the L1 holds hardly any of it: 4500
+// clocks a tile).
+__device__ __forceinline__ float4 lds128(uint32_t a) {
+  float4 x;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(a) : "memory");
+  return x;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t x;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(a) : "memory");
+  return x;
+}
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t x) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory");
+}
+// The address of a field of the kernel's Misc, from `base`, Plan P and Misc M of the scope.
+#define GRAD_AT(field) (base + (uint32_t)(P::kMiscOff + offsetof(M, field)))
+
 // One segment met by a share: its tiles [ka, kb).
 struct Item {
   int u, ka, kb;
 };
 struct Walk {
   const GradArgs& p;
-  int64_t g, g1;
-  int u;
+  int u, k, left;  // segment, its next tile, tiles of the share from there on
   __device__ __forceinline__ Walk(const GradArgs& p_, int share) : p(p_) {
-    const int64_t per = tiles_per_share(p);
-    g = per * share;
-    g1 = min(p.first[p.units], g + per);
+    const int64_t per = tiles_per_share(p), g = per * share;
+    left = (int)max(min(p.first[p.units] - g, per), (int64_t)0);
     int lo = 0, hi = p.units;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -41,14 +78,15 @@ struct Walk {
       else hi = mid;
     }
     u = lo;
+    k = left > 0 ? (int)(g - p.first[lo]) : 0;
   }
   __device__ __forceinline__ bool next(Item* it) {
-    if (g >= g1) return false;
-    while (p.first[u + 1] <= g) ++u;
-    it->u = u;
-    it->ka = (int)(g - p.first[u]);
-    it->kb = (int)(it->ka + min(p.first[u + 1] - g, g1 - g));
-    g += it->kb - it->ka;
+    if (left <= 0) return false;
+    int n;
+    while ((n = (int)(p.first[u + 1] - p.first[u])) <= k) ++u, k = 0;
+    *it = {u, k, min(n, k + left)};
+    left -= it->kb - k;
+    k = it->kb;
     return true;
   }
 };
@@ -59,7 +97,7 @@ struct Facts {
 };
 struct alignas(16) ScaledFacts {  // 8- and 4-bit stores
   uint32_t live[4];
-  float ksl[kGradTile], ks[kGradTile], vs[kGradTile];  // of keys, with and without the logits' scale, and values
+  float ks[kGradTile], vs[kGradTile];  // scales of keys and values
 };
 template <int FMT>
 struct FactsOf {
@@ -110,127 +148,197 @@ __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// Tiles of a share one after the other, and where the walk stands: the tile's table entries, which
+// are looked at a tile later so that nobody waits for them, and its live slots from its first on.
+struct Tile {
+  int a, b, live;
+};
+struct Tiles {
+  const GradArgs& p;
+  Walk walk;
+  Item it = {0, 0, 0};  // ka: the next tile
+  int count = 0;
+  __device__ __forceinline__ Tiles(const GradArgs& p_, int share) : p(p_), walk(p_, share) {}
+  __device__ __forceinline__ bool next(Tile* t) {
+    if (it.ka == it.kb) {
+      if (!walk.next(&it)) return false;
+      count = p.st.count(it.u);
+    }
+    const int32_t* e = p.st.table + (int64_t)it.u * p.st.max_pages + 2 * it.ka;
+    t->live = count - it.ka * kGradTile;
+    t->a = __ldg(e);
+    t->b = t->live > kPage ? __ldg(e + 1) : -1;
+    ++it.ka;
+    return true;
+  }
+};
+// The entries of a tile that are no page of the pool become -1.
+__device__ __forceinline__ void check(const GradArgs& p, Tile& t, bool raise) {
+  const bool a = t.a >= 0 && t.a < p.st.pool_pages, b = t.b >= 0 && t.b < p.st.pool_pages;
+  if (raise && ((!a && t.live > 0) || (!b && t.live > kPage))) p.st.raise();
+  if (!a) t.a = -1;
+  if (!b) t.b = -1;
+}
+
 // A group of four warps that brings the keys, or the values, of every tile into a ring of
 // PLACES operands: rows that are not live as zeros, 8- and 4-bit codes as bf16 without their
-// row's scale.  The next tile's codes are on their way into registers, and its pages known,
-// while a place is waited for; a bf16 store's rows are copied without registers, and one
+// row's scale.  Codes of the next tile are asked for as soon as the registers of this one's are
+// free, half a tile at a time; a bf16 store's rows are copied without registers, and one
 // tile's are on their way while the one before lands.
-template <int FMT, int PLACES, bool FACTS>
+template <int FMT, int PLACES, bool VALUE, bool FACTS>
 struct Feeder {
   using F = typename FactsOf<FMT>::type;
+  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2, kSide = kPieces / 2;
+  // addresses in shared memory: barriers [PLACES], facts [PLACES] (FACTS: written by this group)
   const GradArgs& p;
-  uint64_t *full, *empty;  // [PLACES]
-  F* facts;                // [PLACES], FACTS: written by this group
-  volatile int* abort;
-  uint32_t ring;
-  bool value;
+  uint32_t full, empty, facts, abort, ring;
   int tid;  // of 128
   uint32_t t = 0;
   bool pending = false;  // a tile's copies have not been handed over
 
-  // The tile's page for slots 64 half ..
-  __device__ __forceinline__ int page(int64_t u, int k, int half, int count) const {
-    const int s = k * kGradTile + half * kPage;
-    if (s >= count) return -1;
-    const int e = __ldg(p.st.table + u * p.st.max_pages + s / kPage);
-    if (e >= 0 && e < p.st.pool_pages) return e;
-    if (tid == 0) p.st.raise();
-    return -1;
-  }
+  // The fence before the tensor core's reads is the issuer's: here it would wait for every load
+  // that is on its way (1200 clocks a tile).
   __device__ __forceinline__ void hand_over(uint32_t tile) const {
-    um::fence_async();
     __syncwarp();
-    if ((tid & 31) == 0) tc::mbar_arrive(bar(&full[tile % PLACES]));
+    if ((tid & 31) == 0) tc::mbar_arrive(full + 8 * (tile % PLACES));
   }
   // Slot tid's facts: asked for, and stated once the place is free.
   struct Fact {
     bool on;
     float ks, vs;
   };
-  __device__ __forceinline__ Fact fact(int a, int b, int live) const {
-    const int pg = tid < kPage ? a : b;
-    Fact x = {pg >= 0 && tid < live, 0.f, 0.f};
-    if (FMT != CERTKV_STORE_BF16 && x.on) {
-      x.ks = __ldg(p.st.ks + (int64_t)pg * kPage + (tid & (kPage - 1)));
-      x.vs = __ldg(p.st.vs + (int64_t)pg * kPage + (tid & (kPage - 1)));
+  __device__ __forceinline__ Fact fact(const Tile& x) const {
+    const int pg = tid < kPage ? x.a : x.b;
+    Fact f = {pg >= 0 && tid < x.live, 0.f, 0.f};
+    if (FMT != CERTKV_STORE_BF16 && f.on) {
+      f.ks = __ldg(p.st.ks + (int64_t)pg * kPage + (tid & (kPage - 1)));
+      f.vs = __ldg(p.st.vs + (int64_t)pg * kPage + (tid & (kPage - 1)));
     }
-    return x;
+    return f;
   }
   __device__ __forceinline__ void state(uint32_t place, const Fact& x) const {
-    F& f = facts[place];
-    const uint32_t word = __ballot_sync(kFull, x.on);
-    if ((tid & 31) == 0) f.live[tid >> 5] = word;
+    const uint32_t to = facts + place * (uint32_t)sizeof(F), word = __ballot_sync(kFull, x.on);
+    if ((tid & 31) == 0) sts32(to + 4 * (tid >> 5), word);
     if constexpr (FMT != CERTKV_STORE_BF16) {
-      f.ks[tid] = x.ks * kCodeScale<FMT>;
-      f.ksl[tid] = x.ks * (kCodeScale<FMT> * p.scale_log2);
-      f.vs[tid] = x.vs * kCodeScale<FMT>;
+      const uint32_t mine = to + (uint32_t)offsetof(ScaledFacts, ks) + 4 * tid;
+      sts32(mine, __float_as_uint(x.ks * kCodeScale<FMT>));
+      sts32(mine + 4 * kGradTile, __float_as_uint(x.vs * kCodeScale<FMT>));
     }
   }
-  __device__ __forceinline__ bool wait_place() {
-    const uint32_t place = t % PLACES, phase = ((t / PLACES) & 1u) ^ 1u;
-    return __all_sync(kFull, tc::mbar_wait(bar(&empty[place]), phase, abort));
+  __device__ __forceinline__ bool wait_place() const {
+    return wait_all(empty + 8 * (t % PLACES), ((t / PLACES) & 1u) ^ 1u, abort);
   }
-  __device__ __forceinline__ bool tile(int a, int b, int live) {
+  __device__ __forceinline__ bool copy(const Tile& x) {
     const uint32_t place = t % PLACES, to = ring + place * kOperand;
-    if constexpr (FMT == CERTKV_STORE_BF16) {
-      // what is on its way is not held up by the wait for a place
-      if (pending && !__all_sync(kFull, tc::mbar_test(bar(&empty[place]), ((t / PLACES) & 1u) ^ 1u))) {
-        cp_wait<0>();
-        hand_over(t - 1);
-        pending = false;
-      }
-      if (!wait_place()) return false;
-      const uint8_t* rows = value ? p.st.v : p.st.k;
-      const int c = tid & 15, r0 = tid >> 4;  // 16 lanes a row, 16 bytes each
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = r0 + 8 * i, pg = i < 8 ? a : b;
-        const bool on = pg >= 0 && r < live;
-        cp16(to + (uint32_t)((c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)),
-             rows + (on ? ((int64_t)pg * kPage + (r & (kPage - 1))) * 256 + c * 16 : 0), on);
-      }
-      cp_commit();
-      if constexpr (FACTS) state(place, fact(a, b, live));
-      if (pending) {
-        cp_wait<1>();
-        hand_over(t - 1);
-      }
-      pending = true;
-    } else {
-      const Piece pc(tid);
-      Raw<FMT> raw;
-      raw.load(pc, a, b, live, value ? p.st.v : p.st.k, value ? p.st.vg : p.st.kg);
-      const Fact x = FACTS ? fact(a, b, live) : Fact{};
-      if (!wait_place()) return false;
-      if constexpr (FACTS) state(place, x);
-#pragma unroll
-      for (int q = 0; q < kPieces; ++q) {
-        uint32_t w[8];
-        codes_to_bf16(raw.w[q], FMT == CERTKV_STORE_FP4 ? raw.g[q % (FMT == CERTKV_STORE_FP4 ? kPieces : 1)] : 0u, w);
-        pc.put(to, q, w);
-      }
-      hand_over(t);
+    // what is on its way is not held up by the wait for a place
+    if (pending && !__all_sync(kFull, tc::mbar_test(empty + 8 * place, ((t / PLACES) & 1u) ^ 1u))) {
+      cp_wait<0>();
+      hand_over(t - 1);
+      pending = false;
     }
+    if (!wait_place()) return false;
+    const uint8_t* rows = VALUE ? p.st.v : p.st.k;
+    const int c = tid & 15, r0 = tid >> 4;  // 16 lanes a row, 16 bytes each
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = r0 + 8 * i, pg = i < 8 ? x.a : x.b;
+      const bool on = pg >= 0 && r < x.live;
+      cp16(to + (uint32_t)((c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)),
+           rows + (on ? ((int64_t)pg * kPage + (r & (kPage - 1))) * 256 + c * 16 : 0), on);
+    }
+    cp_commit();
+    if constexpr (FACTS) state(place, fact(x));
+    if (pending) {
+      cp_wait<1>();
+      hand_over(t - 1);
+    }
+    pending = true;
     ++t;
     return true;
   }
-  __device__ __forceinline__ void run(Walk walk) {
-    Item it;
-    bool ok = true;
-    while (ok && walk.next(&it)) {
-      const int count = p.st.count(it.u);
-      int a = page(it.u, it.ka, 0, count), b = page(it.u, it.ka, 1, count);
-      for (int k = it.ka; ok && k < it.kb; ++k) {
-        const int a1 = k + 1 < it.kb ? page(it.u, k + 1, 0, count) : -1;
-        const int b1 = k + 1 < it.kb ? page(it.u, k + 1, 1, count) : -1;
-        ok = tile(a, b, count - k * kGradTile);
-        a = a1;
-        b = b1;
+  // This thread's codes of one page of a tile.
+  struct Codes {
+    uint32_t w[kSide][kWords], g[kSide];
+  };
+  __device__ __forceinline__ void ask(Codes& c, const Piece& pc, int page, int live) const {
+    const uint8_t *codes = VALUE ? p.st.v : p.st.k, *group = VALUE ? p.st.vg : p.st.kg;
+#pragma unroll
+    for (int q = 0; q < kSide; ++q) {
+      const int row = pc.grp + kStep * q;
+      const bool on = page >= 0 && row < live;
+      const int64_t at = (int64_t)page * kPage + row;
+      c.g[q] = 0u;
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) c.w[q][j] = 0u;
+      if (!on) continue;
+      if constexpr (FMT == CERTKV_STORE_FP8) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(codes + at * 128 + pc.sub * 16));
+        c.w[q][0] = v.x;
+        c.w[q][1] = v.y;
+        c.w[q][2] = v.z;
+        c.w[q][3] = v.w;
+      } else {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(codes + at * 64 + pc.sub * 8));
+        c.w[q][0] = v.x;
+        c.w[q][1] = v.y;
+        c.g[q] = __ldg(group + at * kGroups + pc.sub);
       }
     }
+  }
+  __device__ __forceinline__ void put(const Codes& c, const Piece& pc, uint32_t to, int side) const {
+#pragma unroll
+    for (int q = 0; q < kSide; ++q) {
+      uint32_t w[8];
+      codes_to_bf16(c.w[q], c.g[q], w);
+      pc.put(to, kSide * side + q, w);
+    }
+  }
+  __device__ __forceinline__ void run(int share) {
+    Tiles tiles(p, share);
+    const Tile none = {-1, -1, 0};  // nothing of it is asked for
+    Tile x, y;  // x: the next tile to be asked for; its pages are looked up a tile before
+    bool ok = true, more = tiles.next(&x);
     if constexpr (FMT == CERTKV_STORE_BF16) {
+      while (ok && more) {
+        more = tiles.next(&y);
+        check(p, x, tid == 0);
+        ok = copy(x);
+        x = y;
+      }
       cp_wait<0>();  // nothing lands after the CTA has gone
       if (ok && pending) hand_over(t - 1);
+    } else {
+      const Piece pc(tid);
+      Codes a, b;
+      Fact f = {};
+      if (more) {
+        check(p, x, tid == 0);
+        if (FACTS) f = fact(x);
+        ask(a, pc, x.a, x.live);
+        ask(b, pc, x.b, x.live - kPage);
+      }
+      bool asked = more;  // there is a tile in the registers
+      more = more && tiles.next(&x);
+      if (!more) x = none;
+      while (asked) {
+        const bool further = more && tiles.next(&y);
+        if (!wait_place()) break;
+        const uint32_t place = t % PLACES, to = ring + place * kOperand;
+        check(p, x, tid == 0);
+        if constexpr (FACTS) {
+          state(place, f);
+          f = fact(x);
+        }
+        put(a, pc, to, 0);
+        ask(a, pc, x.a, x.live);
+        put(b, pc, to, 1);
+        ask(b, pc, x.b, x.live - kPage);
+        hand_over(t);
+        ++t;
+        asked = more;
+        more = further;
+        x = further ? y : none;
+      }
     }
   }
 };

@@ -190,35 +190,157 @@ __device__ __forceinline__ void mma_o2(uint32_t d, uint32_t a, uint32_t b, uint3
       ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
       : "memory");
 }
-// One k-step (16 of k) of D (+)= A B by the one lane that calls: A in shared memory or
-// (mma_ts) in tensor memory; the low words of the descriptors, hi common to both.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
-  asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 da, db;\n"
-      "setp.ne.b32 p, %5, 0;\nmov.b64 da, {%1, %3};\nmov.b64 db, {%2, %3};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}\n" ::"r"(d),
-      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
-      : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
-  asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 db;\n"
-      "setp.ne.b32 p, %5, 0;\nmov.b64 db, {%2, %3};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n" ::"r"(d),
-      "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
-      : "memory");
-}
 // The same instruction descriptor for bf16 operands with N = n columns (a multiple of 16 up
 // to 256) and either operand MN-major.
 __host__ __device__ constexpr uint32_t idesc_n(uint32_t n, bool a_mn, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
          ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
-// Whether this lane is the one that commit() below, too, elects.
-__device__ __forceinline__ bool elected() {
-  uint32_t e;
-  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(e));
-  return e != 0;
+// S (+)= K Q^T over 128 elements, K 128 rows and Q 64 of them or fewer (id's N), both
+// K-major in two 64-element halves.
+__device__ __forceinline__ void mma_s64(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n"
+      ".reg .pred pe, pn, p0, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 da, db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 p0, %5, 0;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p0;\n"
+      "add.u32 x, %1, 2;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 2;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 4;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 4;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 6;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 6;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1024;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 512;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1026;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 514;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1028;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 516;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 1030;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 518;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
+      : "memory");
+}
+// The eight k-steps of a contraction over 128 slots with both operands MN-major.
+__device__ __forceinline__ void mma_mn(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n"
+      ".reg .pred pe, pn, p0, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 da, db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 p0, %5, 0;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p0;\n"
+      "add.u32 x, %1, 128;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 128;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 256;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 256;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 384;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 384;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 512;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 512;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 640;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 640;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 768;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 768;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "add.u32 x, %1, 896;\n"
+      "mov.b64 da, {x, %3};\n"
+      "add.u32 y, %2, 896;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
+      : "memory");
+}
+// n <= 4 k-steps of a contraction over 64 rows: A in tensor memory, 16 rows in each 8 of the
+// first 16 columns of every 32; B MN-major.
+__device__ __forceinline__ void mma_p64(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc, uint32_t n) {
+  asm volatile(
+      "{\n"
+      ".reg .pred pe, pn, p0, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 da, db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 p0, %5, 0;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, p0;\n"
+      "setp.gt.u32 pn, %6, 1;\n"
+      "and.pred pn, pn, pe;\n"
+      "add.u32 x, %1, 8;\n"
+      "add.u32 y, %2, 128;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pn tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "setp.gt.u32 pn, %6, 2;\n"
+      "and.pred pn, pn, pe;\n"
+      "add.u32 x, %1, 32;\n"
+      "add.u32 y, %2, 256;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pn tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "setp.gt.u32 pn, %6, 3;\n"
+      "and.pred pn, pn, pe;\n"
+      "add.u32 x, %1, 40;\n"
+      "add.u32 y, %2, 384;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pn tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc), "r"(n)
+      : "memory");
 }
 
 // The whole warp calls; the lane that issues the MMAs commits them.
