@@ -26,44 +26,47 @@
 namespace certkv {
 namespace {
 
-// Warps: softmax, loaders, then the issuer and two that bring rows, then four that write the slots'
-// gradients.
-constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps, kRowWarps = 2, kDrainWarps = 4;
-constexpr int kIssue = kSoftWarps + kLoadWarps, kDrain = kIssue + 4;
-constexpr int kThreads = (kDrain + kDrainWarps) * 32;  // whole warpgroups
-constexpr int kSoftRegs = 96, kLoadRegs = 80, kIssueRegs = 64, kDrainRegs = 64;
-static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs + kDrainWarps * 32 * kDrainRegs <=
-                  kThreads * 80,
+// Warps: softmax, loaders, four that write the slots' gradients (a whole warpgroup each: a warp
+// reaches the quarter of tensor memory that its number mod 4 says), the issuer, two that bring rows.
+constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps, kDrainWarps = 4, kRowWarps = 2;
+constexpr int kDrain = kSoftWarps + kLoadWarps, kIssue = kDrain + kDrainWarps;
+constexpr int kThreads = (kIssue + 4) * 32;
+// Registers a thread: the launch gives 80, which the roles share out among themselves.
+constexpr int kLaunchRegs = 80;
+constexpr int kSoftRegs = 96, kLoadRegs = 72, kDrainRegs = 72, kIssueRegs = 72;
+static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + kDrainWarps * 32 * kDrainRegs + 128 * kIssueRegs <=
+                  kThreads * kLaunchRegs,
               "a larger split would wait for registers for ever");
 constexpr int kCols = kGradFused;       // query rows of a block
 constexpr int kRowHalf = kCols * 128;   // bytes of a block's 64 rows x 64 elements
 constexpr int kBlock = 4 * kRowHalf;    // a block: its rows, then their gradients
 constexpr uint32_t kColV = 256, kColK = 384, kColQ = 128;  // S of block i: column 128 (i & 1), R 64 on
 
-template <bool FUSED>
+template <int FMT, bool FUSED>
 struct Plan {
   static constexpr int kKeys = FUSED ? 2 : 1, kValues = FUSED ? 2 : 1;  // places of the rings
-  static constexpr int kBlocks = FUSED ? 2 : 4;
+  static constexpr int kBlocks = !FUSED ? 4 : FMT == CERTKV_STORE_BF16 ? 2 : 1;
   static constexpr int kValueOff = kKeys * kOperand;
   static constexpr int kBlockOff = kValueOff + kValues * kOperand;
   static constexpr int kEOff = kBlockOff + kBlocks * kBlock;  // e, FUSED: [128 slots][64 rows]
-  static constexpr int kMiscOff = kEOff + (FUSED ? kHalf : 0);
+  static constexpr int kStageOff = kEOff + (FUSED ? kHalf : 0);  // of keys, then of values
+  static constexpr int kMiscOff = kStageOff + 2 * gt::kStage<FMT>;
 };
-template <bool FUSED>
+template <int FMT, bool FUSED>
 struct Misc {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t b_full[4], b_empty[4];
   uint64_t s_full[2], p_full[2], o_full, drained, done;
   uint32_t tmem;
   int abort, last;  // last: a flag that nobody sets
-  alignas(16) float nlse[Plan<FUSED>::kBlocks][kCols], ndelta[Plan<FUSED>::kBlocks][kCols];  // negated
+  alignas(16) float nlse[Plan<FMT, FUSED>::kBlocks][kCols], ndelta[Plan<FMT, FUSED>::kBlocks][kCols];  // negated
 };
-template <bool FUSED>
+template <int FMT, bool FUSED>
 constexpr int smem_bytes() {
-  return Plan<FUSED>::kMiscOff + (int)sizeof(Misc<FUSED>) + 1024;
+  static_assert(Plan<FMT, FUSED>::kMiscOff + sizeof(Misc<FMT, FUSED>) <= 232448,
+                "over the 227 KB of shared memory a CTA can have");
+  return Plan<FMT, FUSED>::kMiscOff + (int)sizeof(Misc<FMT, FUSED>);
 }
-static_assert(smem_bytes<true>() <= 232448 && smem_bytes<false>() <= 232448,
-              "over the 227 KB of shared memory a CTA can have");
 
 // Blocks of 64 rows of a unit, and the rows of block j.
 __device__ __forceinline__ int blocks_of(const GradArgs& p) { return (p.rows + kCols - 1) / kCols; }
@@ -83,14 +86,14 @@ struct Steps {
   gt::Item it;
   int k, j, n;
   uint32_t i = 0, t = 0, item = 0;
-  __device__ __forceinline__ Steps(const GradArgs& p_, int share) : p(p_), walk(p_, share) {
+  __device__ __forceinline__ Steps(const GradArgs& p_, const gt::Walk& w) : p(p_), walk(w) {
     it = {0, 0, 0};
     k = j = 0;
     n = blocks_of(p_);
   }
   __device__ __forceinline__ bool next(Step* s) {
     if (k == it.kb) {
-      if (!walk.next(&it)) return false;
+      if (!walk.next(p, &it)) return false;
       k = it.ka;
       ++item;
     }
@@ -108,10 +111,10 @@ struct Steps {
 // Two warps bring blocks of rows and their gradients into shared memory, each for a tile
 // (FUSED: for an item).  A row that takes no part, or that holds a NaN or infinity, comes as
 // zeros.
-template <bool FUSED>
+template <int FMT, bool FUSED>
 struct RowFeeder {
-  using P = Plan<FUSED>;
-  using M = Misc<FUSED>;
+  using P = Plan<FMT, FUSED>;
+  using M = Misc<FMT, FUSED>;
   const GradArgs& p;
   uint32_t base;
   int tid;  // of 64
@@ -121,10 +124,10 @@ struct RowFeeder {
 
   __device__ __forceinline__ void hand_over(uint32_t i) const {
     __syncwarp();
-    if ((tid & 31) == 0) tc::mbar_arrive(GRAD_AT(b_full) + 8u * (i % Plan<FUSED>::kBlocks));
+    if ((tid & 31) == 0) tc::mbar_arrive(GRAD_AT(b_full) + 8u * (i % P::kBlocks));
   }
   __device__ __forceinline__ bool block(int u, int j) {
-    constexpr uint32_t kPlaces = Plan<FUSED>::kBlocks;
+    constexpr uint32_t kPlaces = P::kBlocks;
     const uint32_t place = n % kPlaces, phase = ((n / kPlaces) & 1u) ^ 1u;
     if (pending && !__all_sync(kFull, tc::mbar_test(GRAD_AT(b_empty) + 8u * place, phase))) {
       gt::cp_wait<0>();
@@ -144,7 +147,7 @@ struct RowFeeder {
     const uint32_t to = base + P::kBlockOff + place * kBlock;
     const int c = tid & 15;
     const uint16_t *q0 = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *g0 = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
-#pragma unroll 8
+#pragma unroll 4
     for (int i = 0; i < 16; ++i) {
       const int r = (tid >> 4) + 4 * i, br = j * kCols + r;
       const bool on = good >> r & 1u;
@@ -162,12 +165,14 @@ struct RowFeeder {
     ++n;
     return true;
   }
-  __device__ __forceinline__ void run(int share) {
-    gt::Walk walk(p, share);
+  __device__ __forceinline__ void run(gt::Walk walk) {
     gt::Item it;
     bool ok = true;
-    while (ok && walk.next(&it)) {
+#pragma unroll 1
+    while (ok && walk.next(p, &it)) {
+#pragma unroll 1
       for (int k = it.ka; ok && k < (FUSED ? it.ka + 1 : it.kb); ++k)
+#pragma unroll 1
         for (int j = 0; ok && j < blocks_of(p); ++j) ok = block(it.u, j);
     }
     gt::cp_wait<0>();  // nothing lands after the CTA has gone
@@ -176,16 +181,15 @@ struct RowFeeder {
 };
 
 // Issues the MMAs; the whole warp runs, one lane issues.
-template <bool FUSED>
+template <int FMT, bool FUSED>
 struct Issuer {
-  using P = Plan<FUSED>;
-  using M = Misc<FUSED>;
+  using P = Plan<FMT, FUSED>;
+  using M = Misc<FMT, FUSED>;
   const GradArgs& p;
   uint32_t tmem, base;
   bool ok = true;
   uint32_t tiles = 0;  // whose products have been begun
   uint32_t odd = 0;    // parities of p_full
-  static __device__ __forceinline__ uint32_t uni(uint32_t x) { return __shfl_sync(kFull, x, 0); }
   __device__ __forceinline__ void wait(uint32_t mbar, uint32_t phase) {
     if (ok) ok = gt::wait_all(mbar, phase & 1u, GRAD_AT(abort));
   }
@@ -201,16 +205,15 @@ struct Issuer {
     if (!ok) return;
     um::fence_async();  // the loaders' writes, before the tensor core's reads
     um::fence_after();
-    const uint32_t d = uni(tmem + 128u * buffer(s)), id = uni(um::idesc_n(columns(s), false, false));
-    const uint32_t k = uni(um::desc_lo(base, 16) + (s.t % P::kKeys) * (kOperand >> 4));
-    const uint32_t v = uni(um::desc_lo(base + P::kValueOff, 16) + (s.t % P::kValues) * (kOperand >> 4));
-    const uint32_t q = uni(um::desc_lo(base + P::kBlockOff, 16) + (s.blk % P::kBlocks) * (kBlock >> 4));
-    um::mma_s64(d, k, q, um::kDescHi, id, 0u);
-    um::mma_s64(uni(d + 64), v, uni(q + (2 * kRowHalf >> 4)), um::kDescHi, id, 0u);
-    um::commit(uni(GRAD_AT(s_full) + 8u * (buffer(s))));
+    const uint32_t d = tmem + 128u * buffer(s), id = um::idesc_n(columns(s), false, false);
+    const uint32_t q = um::desc_lo(base + P::kBlockOff, 16) + (s.blk % P::kBlocks) * (kBlock >> 4);
+    um::mma_s64(d, um::desc_lo(base, 16) + (s.t % P::kKeys) * (kOperand >> 4), q, um::kDescHi, id, 0u);
+    um::mma_s64(d + 64, um::desc_lo(base + P::kValueOff, 16) + (s.t % P::kValues) * (kOperand >> 4),
+                q + (2 * kRowHalf >> 4), um::kDescHi, id, 0u);
+    um::commit(GRAD_AT(s_full) + 8u * buffer(s));
     if (s.j + 1 == s.n) {
-      um::commit(uni(GRAD_AT(v_empty) + 8u * (s.t % P::kValues)));
-      if (!FUSED) um::commit(uni(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys)));
+      um::commit(GRAD_AT(v_empty) + 8u * (s.t % P::kValues));
+      if (!FUSED) um::commit(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys));
     }
   }
   // what p and e of a block go into
@@ -222,25 +225,24 @@ struct Issuer {
     if (!ok) return;
     if (FUSED) um::fence_async();
     um::fence_after();
-    const uint32_t a = uni(tmem + 128u * x), steps = uni(columns(s) / 16), acc = uni(s.j > 0);
-    const uint32_t q = uni(um::desc_lo(base + P::kBlockOff, kRowHalf) + (s.blk % P::kBlocks) * (kBlock >> 4));
+    const uint32_t a = tmem + 128u * x, steps = columns(s) / 16, acc = s.j > 0;
+    const uint32_t q = um::desc_lo(base + P::kBlockOff, kRowHalf) + (s.blk % P::kBlocks) * (kBlock >> 4);
     constexpr uint32_t id = um::idesc_n(128, false, true);
-    um::mma_p64(uni(tmem + kColV), a, uni(q + (2 * kRowHalf >> 4)), um::kDescHi, id, acc, steps);
-    um::mma_p64(uni(tmem + kColK), uni(a + 16), q, um::kDescHi, id, acc, steps);
-    if (FUSED) {
-      const uint32_t k = uni(um::desc_lo(base, kHalf) + (s.t % P::kKeys) * (kOperand >> 4));
-      um::mma_mn(uni(tmem + kColQ), k, uni(um::desc_lo(base + P::kEOff, 16)), um::kDescHi,
-                 uni(um::idesc_n(columns(s), true, true)), uni(!s.first));
-    }
-    if (FUSED) um::commit(uni(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys)));
-    if (!FUSED || s.last) um::commit(uni(GRAD_AT(b_empty) + 8u * (s.blk % P::kBlocks)));
-    if (s.j + 1 == s.n) um::commit(uni(GRAD_AT(o_full)));
+    um::mma_p64(tmem + kColV, a, q + (2 * kRowHalf >> 4), um::kDescHi, id, acc, steps);
+    um::mma_p64(tmem + kColK, a + 16, q, um::kDescHi, id, acc, steps);
+    if (FUSED)
+      um::mma_mn(tmem + kColQ, um::desc_lo(base, kHalf) + (s.t % P::kKeys) * (kOperand >> 4),
+                 um::desc_lo(base + P::kEOff, 16), um::kDescHi, um::idesc_n(columns(s), true, true), !s.first);
+    if (FUSED) um::commit(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys));
+    if (!FUSED || s.last) um::commit(GRAD_AT(b_empty) + 8u * (s.blk % P::kBlocks));
+    if (s.j + 1 == s.n) um::commit(GRAD_AT(o_full));
   }
-  __device__ __forceinline__ void run(int share) {
-    Steps<FUSED> steps(p, share);
+  __device__ __forceinline__ void run(const gt::Walk& walk) {
+    Steps<FUSED> steps(p, walk);
     Step cur, nxt;
     bool more = steps.next(&cur);
     if (more) logits(cur);
+#pragma unroll 1
     while (ok && more) {
       more = steps.next(&nxt);
       // behind a tile's last block the next tile may still be on its way; FUSED: there is one
@@ -252,8 +254,7 @@ struct Issuer {
       cur = nxt;
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
-    gt::wait(GRAD_AT(done), 0, GRAD_AT(last));
-    __syncwarp();
+    gt::wait_all(GRAD_AT(done), 0, GRAD_AT(last));
   }
 };
 
@@ -279,29 +280,33 @@ __device__ __forceinline__ void store_sector(uint16_t* to, const uint32_t (&w)[8
 }
 
 template <int FMT, bool FUSED>
-__device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share) {
-  using P = Plan<FUSED>;
-  using M = Misc<FUSED>;
+__device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share,
+                                        gt::Walk walk) {
+  using P = Plan<FMT, FUSED>;
+  using M = Misc<FMT, FUSED>;
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
+  extern __shared__ __align__(1024) char smem[];
   const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
   const int row = quad * 32 + lane;  // slot of the tile
   const uint32_t at = (uint32_t)(quad * 32) << 16;
   const int blocks = blocks_of(p);
   uint32_t i = 0, t = 0, item = 0;
   bool ok = true;
-  gt::Walk walk(p, share);
   gt::Item it;
-  while (walk.next(&it)) {
+#pragma unroll 1
+  while (walk.next(p, &it)) {
     const gt::Item now = it;
     const int count = p.st.count(now.u);
     Slot<FMT> next;
     next.load(p, now.u, now.ka * kGradTile + row, count);
+#pragma unroll 1
     for (int k = now.ka; k < now.kb; ++k, ++t) {
       const Slot<FMT> slot = next;
       if (k + 1 < now.kb) next.load(p, now.u, (k + 1) * kGradTile + row, count);
       const bool live = slot.at >= 0;
       const float2 ksl = make_float2(slot.ks * p.scale_log2, slot.ks * p.scale_log2);
       const float2 vs = make_float2(slot.vs, slot.vs), ks = make_float2(slot.ks, slot.ks);
+#pragma unroll 1
       for (int j = 0; ok && j < blocks; ++j, ++i) {
         const uint32_t x = FUSED ? 0u : i & 1u, use = FUSED ? i : i >> 1, blk = FUSED ? item : i;
         const uint32_t place = blk % P::kBlocks;
@@ -312,42 +317,46 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
         um::fence_after();
         if (32 * half < rows_of_block(p, j)) {
           const uint32_t tS = tmem + at + 128u * x + 32u * half;
-          uint32_t s[32], r[32], pw[16], ew[16], qw[16];
+          const float* nlse = &reinterpret_cast<const M*>(smem + P::kMiscOff)->nlse[place][32 * half];
+          const float* ndelta = &reinterpret_cast<const M*>(smem + P::kMiscOff)->ndelta[place][32 * half];
+          uint32_t s[32];
           um::ld32(tS, s);
-          um::ld32(tS + 64u, r);
-          const uint32_t nlse = GRAD_AT(nlse) + 4 * (place * kCols + 32 * half);
-          const uint32_t ndelta = GRAD_AT(ndelta) + 4 * (place * kCols + 32 * half);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const float4 l4 = gt::lds128(nlse + 16 * c);
-            const float4 d4 = gt::lds128(ndelta + 16 * c);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int q = 4 * c + 2 * h;
-              float2 e = make_float2(__uint_as_float(s[q]), __uint_as_float(s[q + 1]));
-              float2 d = make_float2(__uint_as_float(r[q]), __uint_as_float(r[q + 1]));
-              e = ffma2(e, ksl, h ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y));
-              d = kQuant ? ffma2(d, vs, h ? make_float2(d4.z, d4.w) : make_float2(d4.x, d4.y))
-                         : fadd2(d, h ? make_float2(d4.z, d4.w) : make_float2(d4.x, d4.y));
-              e.x = um::ex2(e.x);
-              e.y = um::ex2(e.y);
-              d = fmul2(e, d);
-              pw[2 * c + h] = live ? gt::pack2(e.x, e.y) : 0u;
-              ew[2 * c + h] = live ? gt::pack2(d.x, d.y) : 0u;
-              if (FUSED && kQuant) {
-                d = fmul2(d, ks);
-                qw[2 * c + h] = live ? gt::pack2(d.x, d.y) : 0u;
-              }
-            }
-          }
-          um::st16(tS, pw);
-          um::st16(tS + 16u, ew);
-          if (FUSED) {
-            const uint32_t to = base + P::kEOff + (uint32_t)row * 128u;
+          for (int h = 0; h < 2; ++h) {  // 16 rows; the logits are all read before any is written over
+            uint32_t r[16], pw[8], ew[8], qw[8];
+            um::ld16(tS + 64u + 16u * h, r);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              const uint32_t* w = kQuant ? &qw[4 * c] : &ew[4 * c];
-              sts128(to + (uint32_t)(((4 * half + c) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+              const float4 l4 = *reinterpret_cast<const float4*>(nlse + 16 * h + 4 * c);
+              const float4 d4 = *reinterpret_cast<const float4*>(ndelta + 16 * h + 4 * c);
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int q = 4 * c + 2 * i;
+                float2 e = make_float2(__uint_as_float(s[16 * h + q]), __uint_as_float(s[16 * h + q + 1]));
+                float2 d = make_float2(__uint_as_float(r[q]), __uint_as_float(r[q + 1]));
+                e = ffma2(e, ksl, i ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y));
+                d = kQuant ? ffma2(d, vs, i ? make_float2(d4.z, d4.w) : make_float2(d4.x, d4.y))
+                           : fadd2(d, i ? make_float2(d4.z, d4.w) : make_float2(d4.x, d4.y));
+                e.x = um::ex2(e.x);
+                e.y = um::ex2(e.y);
+                d = fmul2(e, d);
+                pw[2 * c + i] = live ? gt::pack2(e.x, e.y) : 0u;
+                ew[2 * c + i] = live ? gt::pack2(d.x, d.y) : 0u;
+                if (FUSED && kQuant) {
+                  d = fmul2(d, ks);
+                  qw[2 * c + i] = live ? gt::pack2(d.x, d.y) : 0u;
+                }
+              }
+            }
+            um::st8(tS + 8u * h, pw);
+            um::st8(tS + 16u + 8u * h, ew);
+            if (FUSED) {
+              const uint32_t to = base + P::kEOff + (uint32_t)row * 128u;
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const uint32_t* w = kQuant ? &qw[4 * c] : &ew[4 * c];
+                sts128(to + (uint32_t)(((4 * half + 2 * h + c) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+              }
             }
           }
           um::wait_st();
@@ -364,18 +373,20 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
 // The four warps that write a tile's gradients, a slot a thread, while the softmax goes on with
 // the next tile; at an item's end (FUSED) its queries' too.
 template <int FMT, bool FUSED>
-__device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share) {
-  using P = Plan<FUSED>;
-  using M = Misc<FUSED>;
+__device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share,
+                                        gt::Walk walk) {
+  using P = Plan<FMT, FUSED>;
+  using M = Misc<FMT, FUSED>;
   const int lane = tid & 31, quad = tid >> 5;
   const uint32_t at = (uint32_t)(quad * 32) << 16;
   uint32_t t = 0;
   bool ok = true;
-  gt::Walk walk(p, share);
   gt::Item it;
-  while (walk.next(&it)) {
+#pragma unroll 1
+  while (walk.next(p, &it)) {
     const gt::Item now = it;
     const int count = p.st.count(now.u);
+#pragma unroll 1
     for (int k = now.ka; k < now.kb; ++k, ++t) {
       const int s = k * kGradTile + tid;
       const int64_t slot = s < count ? p.st.slot(now.u, s) : -1;
@@ -415,11 +426,11 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
 // grid = groups (one CTA per SM), block = kThreads.
 template <int FMT, bool FUSED>
 __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_constant__ GradArgs p) {
-  using P = Plan<FUSED>;
-  using M = Misc<FUSED>;
-  extern __shared__ char smem_raw[];
-  const uint32_t base = (tc::saddr(smem_raw) + 1023u) & ~1023u;
-  const int warp = threadIdx.x >> 5;
+  using P = Plan<FMT, FUSED>;
+  using M = Misc<FMT, FUSED>;
+  extern __shared__ __align__(1024) char smem[];
+  const uint32_t base = tc::saddr(smem);
+  const int warp = __shfl_sync(kFull, (int)threadIdx.x >> 5, 0);  // so that the compiler, too, knows it uniform
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(GRAD_AT(k_full) + 8u * (i), kGroupWarps);
@@ -443,40 +454,39 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
   release_next();
   await_previous();
   const int share = blockIdx.x;
-  if (tiles_per_share(p) * share >= p.first[p.units]) return;  // uniform, before any barrier
+  const gt::Walk walk = gt::Walk::of(p, share);
+  if (walk.left == 0) return;  // uniform, before any barrier
   if (warp == kIssue) um::alloc(GRAD_AT(tmem), 512);
   um::fence_before();
   __syncthreads();
   um::fence_after();
   const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
   if (warp < kSoftWarps) {
-    gt::regs_up<kSoftRegs>();
-    softmax<FMT, FUSED>(p, base, tmem, threadIdx.x, share);
+    gt::registers<kSoftRegs, kLaunchRegs>();
+    softmax<FMT, FUSED>(p, base, tmem, threadIdx.x, share, walk);
   } else if (warp < kSoftWarps + kLoadWarps) {
-    gt::regs_down<kLoadRegs>();
+    gt::registers<kLoadRegs, kLaunchRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
     if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, P::kKeys, false, false> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), 0u, GRAD_AT(abort), base, tid};
-      f.run(share);
+      gt::Feeder<FMT, P::kKeys, false, false> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), 0u, GRAD_AT(abort), base, base + P::kStageOff, tid};
+      f.run(walk);
     } else {
       gt::Feeder<FMT, P::kValues, true, false> f{p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort),
-                                                 base + P::kValueOff, tid - kGroupWarps * 32};
-      f.run(share);
+                                                 base + P::kValueOff, base + P::kStageOff + gt::kStage<FMT>, tid - kGroupWarps * 32};
+      f.run(walk);
     }
-  } else if (warp < kDrain) {
-    gt::regs_down<kIssueRegs>();
-    if (warp == kIssue) {
-      Issuer<FUSED> is{p, tmem, base};
-      is.run(share);
-    } else if (warp <= kIssue + kRowWarps) {
-      RowFeeder<FUSED> f{p, base, (int)threadIdx.x - (kIssue + 1) * 32,
-                         (65536u + p.G - 1) / p.G};
-      f.run(share);
-    }
-    __syncwarp();
+  } else if (warp < kIssue) {
+    gt::registers<kDrainRegs, kLaunchRegs>();
+    drain<FMT, FUSED>(p, base, tmem, (int)threadIdx.x - kDrain * 32, share, walk);
   } else {
-    gt::regs_down<kDrainRegs>();
-    drain<FMT, FUSED>(p, base, tmem, (int)threadIdx.x - kDrain * 32, share);
+    gt::registers<kIssueRegs, kLaunchRegs>();
+    if (warp == kIssue) {
+      Issuer<FMT, FUSED> is{p, tmem, base};
+      is.run(walk);
+    } else if (warp <= kIssue + kRowWarps) {
+      RowFeeder<FMT, FUSED> f{p, base, (int)threadIdx.x - (kIssue + 1) * 32, (65536u + p.G - 1) / p.G};
+      f.run(walk);
+    }
   }
   um::fence_before();
   __syncthreads();
@@ -494,11 +504,11 @@ bool launch(const GradArgs& p, cudaStream_t st) {
   if (cudaGetDevice(&dev) != cudaSuccess) return false;
   if (dev > 63 || !(ready.load() >> dev & 1u)) {
     if (cudaFuncSetAttribute(grad_kv_kernel<FMT, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             smem_bytes<FUSED>()) != cudaSuccess)
+                             smem_bytes<FMT, FUSED>()) != cudaSuccess)
       return false;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
-  return launch_kernel(true, grad_kv_kernel<FMT, FUSED>, (unsigned)p.groups, kThreads, smem_bytes<FUSED>(), st, p);
+  return launch_kernel(true, grad_kv_kernel<FMT, FUSED>, (unsigned)p.groups, kThreads, smem_bytes<FMT, FUSED>(), st, p);
 }
 template <int FMT>
 bool launch_rows(const GradArgs& p, cudaStream_t st) {

@@ -28,9 +28,11 @@ namespace certkv {
 namespace {
 
 constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps;
-constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups
-constexpr int kSoftRegs = 112, kLoadRegs = 96, kIssueRegs = 64;
-static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * 96,
+constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups, the issuer's the last
+// Registers a thread: the launch gives 96, which the roles share out among themselves.
+constexpr int kLaunchRegs = 96;
+constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
+static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs,
               "a larger split would wait for registers for ever");
 constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
 
@@ -40,7 +42,8 @@ struct Plan {
   static constexpr int kValues = 2;
   static constexpr int kKeyOff = 2 * kOperand;  // behind the rows and their gradients
   static constexpr int kValueOff = kKeyOff + kKeys * kOperand;
-  static constexpr int kMiscOff = kValueOff + kValues * kOperand;
+  static constexpr int kStageOff = kValueOff + kValues * kOperand;  // of keys, then of values
+  static constexpr int kMiscOff = kStageOff + 2 * gt::kStage<FMT>;
 };
 template <int FMT>
 struct Misc {
@@ -52,9 +55,10 @@ struct Misc {
 };
 template <int FMT>
 constexpr int smem_bytes() {
-  return Plan<FMT>::kMiscOff + (int)sizeof(Misc<FMT>) + 1024;
+  return Plan<FMT>::kMiscOff + (int)sizeof(Misc<FMT>);
 }
-static_assert(smem_bytes<CERTKV_STORE_BF16>() <= 232448 && smem_bytes<CERTKV_STORE_FP8>() <= 232448,
+static_assert(smem_bytes<CERTKV_STORE_BF16>() <= 232448 && smem_bytes<CERTKV_STORE_FP8>() <= 232448 &&
+                  smem_bytes<CERTKV_STORE_FP4>() <= 232448,
               "over the 227 KB of shared memory a CTA can have");
 
 __device__ __forceinline__ void softmax_sync() {
@@ -68,115 +72,142 @@ struct Issuer {
   using M = Misc<FMT>;
   uint32_t tmem, base;
   bool ok = true;
-  static __device__ __forceinline__ uint32_t uni(uint32_t x) { return __shfl_sync(kFull, x, 0); }
   __device__ __forceinline__ void wait(uint32_t mbar, uint32_t phase) {
-    if (ok) ok = gt::wait_all(mbar, phase & 1u, GRAD_AT(abort));
+    if (ok) ok = gt::wait_all(mbar, phase, GRAD_AT(abort));
   }
-  __device__ __forceinline__ uint32_t key(uint32_t t, uint32_t lbo) const {
-    return uni(um::desc_lo(base + P::kKeyOff, lbo) + (t % P::kKeys) * (kOperand >> 4));
+  // A place of a ring and the parity of its use.
+  template <int N>
+  struct Place {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void operator++() {
+      if (++slot == N) slot = 0, phase ^= 1u;
+    }
+  };
+  Place<P::kKeys> sk, qk;  // of the next S, of the next dQ
+  Place<P::kValues> rv;    // of the next R
+  static __device__ __forceinline__ bool test(uint32_t mbar, uint32_t phase) {
+    return __all_sync(kFull, tc::mbar_test(mbar, phase));
   }
-  // Whether the keys and values of tile t are in place.
-  __device__ __forceinline__ bool there(uint32_t t) const {
-    return __all_sync(kFull, tc::mbar_test(GRAD_AT(k_full) + 8u * (t % P::kKeys), (t / P::kKeys) & 1u) &&
-                                 tc::mbar_test(GRAD_AT(v_full) + 8u * (t % P::kValues), (t / P::kValues) & 1u));
+  // The keys and values of the next tile.
+  __device__ __forceinline__ bool there() const {
+    return test(GRAD_AT(k_full) + 8u * sk.slot, sk.phase) && test(GRAD_AT(v_full) + 8u * rv.slot, rv.phase);
   }
+  __device__ __forceinline__ void await() {
+    wait(GRAD_AT(k_full) + 8u * sk.slot, sk.phase);
+    wait(GRAD_AT(v_full) + 8u * rv.slot, rv.phase);
+  }
+  // S of tile t, whose keys and values are there, and its R
   __device__ __forceinline__ void s(uint32_t t) {
-    wait(GRAD_AT(k_full) + 8u * (t % P::kKeys), t / P::kKeys);
     if (!ok) return;
-    um::fence_async();
+    um::fence_async();  // the loaders' writes, before the tensor core's reads
     um::fence_after();
-    um::mma_s(uni(tmem + 128u * (t & 1u)), uni(um::desc_lo(base, 16)), key(t, 16), um::kDescHi, um::idesc(true, false));
+    um::mma_s(tmem + 128u * (t & 1u), um::desc_lo(base, 16), um::desc_lo(base + P::kKeyOff, 16) + sk.slot * (kOperand >> 4),
+              um::kDescHi, um::idesc(true, false));
+    ++sk;
   }
-  __device__ __forceinline__ void r(uint32_t t) {
-    const uint32_t place = t % P::kValues;
-    wait(GRAD_AT(v_full) + 8u * (place), t / P::kValues);
+  __device__ __forceinline__ void r() {
     if (!ok) return;
-    um::fence_async();
     um::fence_after();
-    um::mma_s(uni(tmem + kColR), uni(um::desc_lo(base + kOperand, 16)),
-              uni(um::desc_lo(base + P::kValueOff, 16) + place * (kOperand >> 4)), um::kDescHi,
-              um::idesc(true, false));
-    um::commit(uni(GRAD_AT(s_full)));
-    um::commit(uni(GRAD_AT(v_empty) + 8u * (place)));
+    um::mma_s(tmem + kColR, um::desc_lo(base + kOperand, 16),
+              um::desc_lo(base + P::kValueOff, 16) + rv.slot * (kOperand >> 4), um::kDescHi, um::idesc(true, false));
+    um::commit(GRAD_AT(s_full));
+    um::commit(GRAD_AT(v_empty) + 8u * rv.slot);
+    ++rv;
   }
-  __device__ __forceinline__ void run(gt::Walk walk) {
+  __device__ __forceinline__ void run(const GradArgs& p, gt::Walk walk) {
     gt::Item it;
     uint32_t t = 0, item = 0;
-    while (ok && walk.next(&it)) {
+#pragma unroll 1
+    while (ok && walk.next(p, &it)) {
       const int n = it.kb - it.ka;
-      wait(GRAD_AT(q_full), item++);
+      wait(GRAD_AT(q_full), item++ & 1u);
+      await();
       s(t);
-      r(t);
+      r();
+#pragma unroll 1
       for (int i = 0; ok && i < n; ++i, ++t) {
-        // The next tile's S and R go before this one's dQ where they can; where its keys are
-        // still on their way they may not hold up dQ, whose end gives a place back.
-        const bool more = i + 1 < n, early = more && there(t + 1);
-        if (early) {
-          s(t + 1);
-          wait(GRAD_AT(r_free), t);
-          r(t + 1);
+        // S of the next tile goes when its keys and values are there, R when this tile's has been
+        // read, dQ of this tile when e is there, in whatever order these come: each gives back
+        // what another role waits for.
+        const bool more = i + 1 < n;
+        bool has_s = !more, has_r = !more;
+#pragma unroll 1
+        for (uint32_t look = 0; ok; ++look) {
+          if (!has_s && there()) {
+            s(t + 1);
+            has_s = true;
+          }
+          if (has_s && !has_r && test(GRAD_AT(r_free), t & 1u)) {
+            r();
+            has_r = true;
+          }
+          if (test(GRAD_AT(p_full), t & 1u)) break;
+          ok = gt::patience(look, GRAD_AT(abort));
         }
-        wait(GRAD_AT(p_full), t);
         if (!ok) break;
         um::fence_after();
-        um::mma_o2(uni(tmem + kColQ), uni(tmem + 128u * (t & 1u)), key(t, kHalf), um::kDescHi, um::idesc(true, true),
-                  uni(i > 0));
-        um::commit(uni(GRAD_AT(k_empty) + 8u * (t % P::kKeys)));
-        if (!more) um::commit(uni(GRAD_AT(o_full)));
-        if (more && !early) {
+        um::mma_o2(tmem + kColQ, tmem + 128u * (t & 1u), um::desc_lo(base + P::kKeyOff, kHalf) + qk.slot * (kOperand >> 4),
+                   um::kDescHi, um::idesc(true, true), i > 0);
+        um::commit(GRAD_AT(k_empty) + 8u * qk.slot);
+        ++qk;
+        if (!more) um::commit(GRAD_AT(o_full));
+        if (!has_s) {
+          await();
           s(t + 1);
-          r(t + 1);
         }
+        if (!has_r) r();
       }
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
-    gt::wait(GRAD_AT(done), 0, GRAD_AT(last));
-    __syncwarp();
+    gt::wait_all(GRAD_AT(done), 0, GRAD_AT(last));
   }
 };
 
-// e of 32 columns of a row: the packed A operand and the rest of its rounding; facts: the address
-// of the tile's.  `loaded`: called
+// e of 32 columns of a row: the packed A operand and the rest of its rounding.  `loaded`: called
 // when the columns have been read.
 template <int FMT, class Loaded>
-__device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, uint32_t facts, int c,
+__device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, const typename gt::FactsOf<FMT>::type& f, int c,
                                         float sl, float nlse, float ndelta, uint32_t (&e)[16], uint32_t (&rest)[16],
                                         Loaded loaded) {
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
-  uint32_t s[32], r[32];
-  um::ld32(tS, s);
-  um::ld32(tR, r);
-  loaded();
   const float2 nl = make_float2(nlse, nlse), nd = make_float2(ndelta, ndelta), sl2 = make_float2(sl, sl);
+  uint32_t s[32];
+  um::ld32(tS, s);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float4 ks, vs;
-    if constexpr (kQuant) {
-      ks = gt::lds128(facts + (uint32_t)offsetof(gt::ScaledFacts, ks) + 128 * c + 16 * j);
-      vs = gt::lds128(facts + (uint32_t)offsetof(gt::ScaledFacts, vs) + 128 * c + 16 * j);
-    }
+  for (int h = 0; h < 2; ++h) {
+    uint32_t r[16];
+    um::ld16(tR + 16u * h, r);
+    if (h) loaded();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int at = 4 * j + 2 * i;
-      float2 x = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
-      float2 y = make_float2(__uint_as_float(r[at]), __uint_as_float(r[at + 1]));
-      const float2 k2 = i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y);
+    for (int j = 4 * h; j < 4 * h + 4; ++j) {
+      float4 ks, vs;
       if constexpr (kQuant) {
-        x = ffma2(x, fmul2(k2, sl2), nl);
-        y = ffma2(y, i ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), nd);
-      } else {
-        x = ffma2(x, sl2, nl);
-        y = fadd2(y, nd);
+        ks = *reinterpret_cast<const float4*>(&f.ks[32 * c + 4 * j]);
+        vs = *reinterpret_cast<const float4*>(&f.vs[32 * c + 4 * j]);
       }
-      x.x = um::ex2(x.x);
-      x.y = um::ex2(x.y);
-      x = fmul2(x, y);
-      if constexpr (kQuant) x = fmul2(x, k2);
-      e[2 * j + i] = gt::pack2(x.x, x.y);
-      rest[2 * j + i] = gt::pack2(x.x - bf16lo(e[2 * j + i]), x.y - bf16hi(e[2 * j + i]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = 4 * j + 2 * i, ar = at - 16 * h;
+        float2 x = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
+        float2 y = make_float2(__uint_as_float(r[ar]), __uint_as_float(r[ar + 1]));
+        const float2 k2 = i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y);
+        if constexpr (kQuant) {
+          x = ffma2(x, fmul2(k2, sl2), nl);
+          y = ffma2(y, i ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), nd);
+        } else {
+          x = ffma2(x, sl2, nl);
+          y = fadd2(y, nd);
+        }
+        x.x = um::ex2(x.x);
+        x.y = um::ex2(x.y);
+        x = fmul2(x, y);
+        if constexpr (kQuant) x = fmul2(x, k2);
+        e[2 * j + i] = gt::pack2(x.x, x.y);
+        rest[2 * j + i] = gt::pack2(x.x - bf16lo(e[2 * j + i]), x.y - bf16hi(e[2 * j + i]));
+      }
     }
   }
-  const uint32_t live = gt::lds32(facts + 4 * c);
+  const uint32_t live = f.live[c];
   if (live != kFull) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -188,10 +219,12 @@ __device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, uint32_t facts
 }
 
 template <int FMT>
-__device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share, int blk) {
+__device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share, int blk,
+                                        gt::Walk walk) {
   using P = Plan<FMT>;
   using M = Misc<FMT>;
   constexpr int kKeys = P::kKeys;
+  extern __shared__ __align__(1024) char smem[];
   const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
   const int row = quad * 32 + lane;
   const uint32_t at = (uint32_t)(quad * 32) << 16;  // this warp's lanes of tensor memory
@@ -199,9 +232,9 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
   const bool busy = quad * 32 < p.rb;  // some block has a row here
   uint32_t t = 0, item = 0;
   bool ok = true;
-  gt::Walk walk(p, share);
   gt::Item it;
-  while (walk.next(&it)) {
+#pragma unroll 1
+  while (walk.next(p, &it)) {
     const gt::Item now = it;
     const GradUnit x(p, now.u);
     const float2* info = p.row + (int64_t)now.u * p.rows + blk * p.rb;
@@ -232,6 +265,7 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     um::fence_async();
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(GRAD_AT(q_full));
+#pragma unroll 1
     for (int k = now.ka; ok && busy && k < now.kb; ++k, ++t) {
       const uint32_t place = t % kKeys;
       ok = gt::wait_all(GRAD_AT(k_full) + 8u * place, (t / kKeys) & 1u, GRAD_AT(abort)) &&
@@ -242,7 +276,7 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
       for (int c = 2 * half; c < 2 * half + 2; ++c) {
         uint32_t e[16], rest[16];
         const uint32_t tS = tmem + at + 128u * (t & 1u) + 32u * c;
-        columns<FMT>(tS, tmem + at + kColR + 32u * c, GRAD_AT(facts) + place * (uint32_t)sizeof(typename gt::FactsOf<FMT>::type), c, p.scale_log2, -mine.x, -mine.y, e, rest, [&] {
+        columns<FMT>(tS, tmem + at + kColR + 32u * c, reinterpret_cast<const M*>(smem + P::kMiscOff)->facts[place], c, p.scale_log2, -mine.x, -mine.y, e, rest, [&] {
           if (c & 1) {  // this warp's half of R has been read
             um::fence_before();
             __syncwarp();
@@ -288,11 +322,11 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
 // grid = groups nblk (one CTA per SM), block = kThreads.
 template <int FMT>
 __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_constant__ GradArgs p) {
-  extern __shared__ char smem_raw[];
+  extern __shared__ __align__(1024) char smem[];
   using P = Plan<FMT>;
   using M = Misc<FMT>;
-  const uint32_t base = (tc::saddr(smem_raw) + 1023u) & ~1023u;
-  const int warp = threadIdx.x >> 5;
+  const uint32_t base = tc::saddr(smem);
+  const int warp = __shfl_sync(kFull, (int)threadIdx.x >> 5, 0);  // so that the compiler, too, knows it uniform
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
       tc::mbar_init(GRAD_AT(k_full) + 8u * (i), kGroupWarps);
@@ -315,34 +349,35 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_consta
   release_next();
   await_previous();
   const int share = blockIdx.x / p.nblk, blk = blockIdx.x - share * p.nblk;
-  if (tiles_per_share(p) * share >= p.first[p.units]) return;  // uniform, before any barrier
+  const gt::Walk walk = gt::Walk::of(p, share);
+  if (walk.left == 0) return;  // uniform, before any barrier
   if (warp == kSoftWarps + kLoadWarps) um::alloc(GRAD_AT(tmem), 512);
   um::fence_before();
   __syncthreads();
   um::fence_after();
   const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
   if (warp < kSoftWarps) {
-    gt::regs_up<kSoftRegs>();
-    softmax<FMT>(p, base, tmem, threadIdx.x, share, blk);
+    gt::registers<kSoftRegs, kLaunchRegs>();
+    softmax<FMT>(p, base, tmem, threadIdx.x, share, blk, walk);
   } else if (warp < kSoftWarps + kLoadWarps) {
-    gt::regs_down<kLoadRegs>();
+    gt::registers<kLoadRegs, kLaunchRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
     if (tid < kGroupWarps * 32) {
       gt::Feeder<FMT, P::kKeys, false, true> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort),
-                                               base + P::kKeyOff, tid};
-      f.run(share);
+                                               base + P::kKeyOff, base + P::kStageOff, tid};
+      f.run(walk);
     } else {
       gt::Feeder<FMT, P::kValues, true, false> f{p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort),
-                                                 base + P::kValueOff, tid - kGroupWarps * 32};
-      f.run(share);
+                                                 base + P::kValueOff, base + P::kStageOff + gt::kStage<FMT>,
+                                                 tid - kGroupWarps * 32};
+      f.run(walk);
     }
   } else {
-    gt::regs_down<kIssueRegs>();
+    gt::registers<kIssueRegs, kLaunchRegs>();
     if (warp == kSoftWarps + kLoadWarps) {
       Issuer<FMT> is{tmem, base};
-      is.run(gt::Walk(p, share));
+      is.run(p, walk);
     }
-    __syncwarp();
   }
   um::fence_before();
   __syncthreads();

@@ -30,10 +30,18 @@ __device__ __forceinline__ bool aborted(uint32_t flag) {
   return x != 0;
 }
 __device__ __forceinline__ bool wait(uint32_t mbar, uint32_t parity, uint32_t flag) {
+#pragma unroll 1
   for (uint32_t i = 0; i < tc::kSpinLimit; ++i) {
     if (tc::mbar_try(mbar, parity)) return true;
     if ((i & 255u) == 255u && aborted(flag)) return false;
   }
+  asm volatile("st.volatile.shared.b32 [%0], 1;" ::"r"(flag) : "memory");
+  return false;
+}
+// Looks without a limit of their own: false when the role is to stop.
+__device__ __forceinline__ bool patience(uint32_t look, uint32_t flag) {
+  if ((look & 255u) == 255u && aborted(flag)) return false;
+  if (look < tc::kSpinLimit) return true;
   asm volatile("st.volatile.shared.b32 [%0], 1;" ::"r"(flag) : "memory");
   return false;
 }
@@ -65,24 +73,28 @@ __device__ __forceinline__ void sts32(uint32_t a, uint32_t x) {
 struct Item {
   int u, ka, kb;
 };
+// Where a share begins: worked out once, by everybody, and walked on from by each role.
 struct Walk {
-  const GradArgs& p;
   int u, k, left;  // segment, its next tile, tiles of the share from there on
-  __device__ __forceinline__ Walk(const GradArgs& p_, int share) : p(p_) {
+  static __device__ __forceinline__ Walk of(const GradArgs& p, int share) {
     const int64_t per = tiles_per_share(p), g = per * share;
-    left = (int)max(min(p.first[p.units] - g, per), (int64_t)0);
+    Walk w;
+    w.left = (int)max(min(p.first[p.units] - g, per), (int64_t)0);
     int lo = 0, hi = p.units;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (p.first[mid] <= g) lo = mid;
       else hi = mid;
     }
-    u = lo;
-    k = left > 0 ? (int)(g - p.first[lo]) : 0;
+    w.u = lo;
+    w.k = w.left > 0 ? (int)(g - p.first[lo]) : 0;
+    return w;
   }
-  __device__ __forceinline__ bool next(Item* it) {
+  __device__ __forceinline__ bool next(const GradArgs& p, Item* it) {
     if (left <= 0) return false;
     int n;
+#pragma unroll 1
     while ((n = (int)(p.first[u + 1] - p.first[u])) <= k) ++u, k = 0;
     *it = {u, k, min(n, k + left)};
     left -= it->kb - k;
@@ -142,6 +154,10 @@ __device__ __forceinline__ void codes_to_bf16(const uint32_t (&c)[2], uint32_t g
 __device__ __forceinline__ void cp16(uint32_t to, const void* from, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
 }
+template <int N>
+__device__ __forceinline__ void cp_small(uint32_t to, const void* from, bool on) {  // 4 or 8 bytes
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(N), "r"(on ? N : 0) : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {
@@ -158,10 +174,10 @@ struct Tiles {
   Walk walk;
   Item it = {0, 0, 0};  // ka: the next tile
   int count = 0;
-  __device__ __forceinline__ Tiles(const GradArgs& p_, int share) : p(p_), walk(p_, share) {}
+  __device__ __forceinline__ Tiles(const GradArgs& p_, const Walk& w) : p(p_), walk(w) {}
   __device__ __forceinline__ bool next(Tile* t) {
     if (it.ka == it.kb) {
-      if (!walk.next(&it)) return false;
+      if (!walk.next(p, &it)) return false;
       count = p.st.count(it.u);
     }
     const int32_t* e = p.st.table + (int64_t)it.u * p.st.max_pages + 2 * it.ka;
@@ -182,17 +198,21 @@ __device__ __forceinline__ void check(const GradArgs& p, Tile& t, bool raise) {
 
 // A group of four warps that brings the keys, or the values, of every tile into a ring of
 // PLACES operands: rows that are not live as zeros, 8- and 4-bit codes as bf16 without their
-// row's scale.  Codes of the next tile are asked for as soon as the registers of this one's are
-// free, half a tile at a time; a bf16 store's rows are copied without registers, and one
-// tile's are on their way while the one before lands.
+// row's scale.  All reads of memory are asynchronous copies.  A bf16 store's rows go straight
+// to their place, one tile's under way while the one before lands.  Codes go to a stretch of
+// shared memory of each thread's own, the next tile's while this one's place is waited for; the
+// loop that expands them is short: straight-line code for a whole tile, with the codes in
+// registers, took the instruction caches of an SM more time than all else (8-bit 395 -> 700 us
+// with two tiles in registers).
 template <int FMT, int PLACES, bool VALUE, bool FACTS>
 struct Feeder {
   using F = typename FactsOf<FMT>::type;
-  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2, kSide = kPieces / 2;
+  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
   // addresses in shared memory: barriers [PLACES], facts [PLACES] (FACTS: written by this group)
   const GradArgs& p;
   uint32_t full, empty, facts, abort, ring;
-  int tid;  // of 128
+  uint32_t stage;  // kStage<FMT> bytes (8- and 4-bit stores)
+  int tid;         // of 128
   uint32_t t = 0;
   bool pending = false;  // a tile's copies have not been handed over
 
@@ -239,7 +259,7 @@ struct Feeder {
     if (!wait_place()) return false;
     const uint8_t* rows = VALUE ? p.st.v : p.st.k;
     const int c = tid & 15, r0 = tid >> 4;  // 16 lanes a row, 16 bytes each
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < 16; ++i) {
       const int r = r0 + 8 * i, pg = i < 8 ? x.a : x.b;
       const bool on = pg >= 0 && r < x.live;
@@ -256,49 +276,55 @@ struct Feeder {
     ++t;
     return true;
   }
-  // This thread's codes of one page of a tile.
-  struct Codes {
-    uint32_t w[kSide][kWords], g[kSide];
-  };
-  __device__ __forceinline__ void ask(Codes& c, const Piece& pc, int page, int live) const {
+  // This thread's pieces of tile x (checked), on their way into its stretch of memory: piece q at
+  // 16 or 8 (128 q + tid), of four bits the word with its group scale behind them.
+  __device__ __forceinline__ void ask(const Piece& pc, const Tile& x) const {
     const uint8_t *codes = VALUE ? p.st.v : p.st.k, *group = VALUE ? p.st.vg : p.st.kg;
-#pragma unroll
-    for (int q = 0; q < kSide; ++q) {
-      const int row = pc.grp + kStep * q;
-      const bool on = page >= 0 && row < live;
-      const int64_t at = (int64_t)page * kPage + row;
-      c.g[q] = 0u;
-#pragma unroll
-      for (int j = 0; j < kWords; ++j) c.w[q][j] = 0u;
-      if (!on) continue;
+#pragma unroll 2
+    for (int q = 0; q < kPieces; ++q) {
+      const int pg = q < kPieces / 2 ? x.a : x.b, row = pc.grp + kStep * (q % (kPieces / 2));
+      const bool on = pg >= 0 && pc.grp + kStep * q < x.live;
+      const int64_t at = on ? (int64_t)pg * kPage + row : 0;
       if constexpr (FMT == CERTKV_STORE_FP8) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(codes + at * 128 + pc.sub * 16));
-        c.w[q][0] = v.x;
-        c.w[q][1] = v.y;
-        c.w[q][2] = v.z;
-        c.w[q][3] = v.w;
+        cp16(stage + 16 * (128 * q + tid), codes + at * 128 + pc.sub * 16, on);
       } else {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(codes + at * 64 + pc.sub * 8));
-        c.w[q][0] = v.x;
-        c.w[q][1] = v.y;
-        c.g[q] = __ldg(group + at * kGroups + pc.sub);
+        cp_small<8>(stage + 8 * (128 * q + tid), codes + at * 64 + pc.sub * 8, on);
+        cp_small<4>(stage + 8 * 128 * kPieces + 4 * (128 * q + tid), group + at * kGroups + (pc.sub & 4), on);
       }
     }
+    cp_commit();
   }
-  __device__ __forceinline__ void put(const Codes& c, const Piece& pc, uint32_t to, int side) const {
-#pragma unroll
-    for (int q = 0; q < kSide; ++q) {
-      uint32_t w[8];
-      codes_to_bf16(c.w[q], c.g[q], w);
-      pc.put(to, kSide * side + q, w);
+  // Piece q of them.
+  __device__ __forceinline__ void piece(int q, uint32_t (&c)[kWords], uint32_t& g) const {
+    if constexpr (FMT == CERTKV_STORE_FP8) {
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
+                   : "r"(stage + 16 * (128 * q + tid)));
+    } else {
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(stage + 8 * (128 * q + tid)));
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(g) : "r"(stage + 8 * 128 * kPieces + 4 * (128 * q + tid)));
     }
   }
-  __device__ __forceinline__ void run(int share) {
-    Tiles tiles(p, share);
-    const Tile none = {-1, -1, 0};  // nothing of it is asked for
+  __device__ __forceinline__ void expand(const Piece& pc, uint32_t to) const {
+    uint32_t c[2][kWords], g[2] = {0u, 0u};
+    piece(0, c[0], g[0]);
+#pragma unroll 1
+    for (int q = 0; q < kPieces; q += 2)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // the next piece is on its way while this one is expanded
+        uint32_t w[8];
+        piece(min(q + i + 1, kPieces - 1), c[i ^ 1], g[i ^ 1]);
+        codes_to_bf16(c[i], g[i] >> (8 * (pc.sub & 3)) & 255u, w);
+        pc.put(to, q + i, w);
+      }
+  }
+  __device__ __forceinline__ void run(const Walk& walk) {
+    Tiles tiles(p, walk);
     Tile x, y;  // x: the next tile to be asked for; its pages are looked up a tile before
-    bool ok = true, more = tiles.next(&x);
+    bool more = tiles.next(&x);
     if constexpr (FMT == CERTKV_STORE_BF16) {
+      bool ok = true;
+#pragma unroll 1
       while (ok && more) {
         more = tiles.next(&y);
         check(p, x, tid == 0);
@@ -309,47 +335,40 @@ struct Feeder {
       if (ok && pending) hand_over(t - 1);
     } else {
       const Piece pc(tid);
-      Codes a, b;
       Fact f = {};
-      if (more) {
-        check(p, x, tid == 0);
-        if (FACTS) f = fact(x);
-        ask(a, pc, x.a, x.live);
-        ask(b, pc, x.b, x.live - kPage);
-      }
-      bool asked = more;  // there is a tile in the registers
-      more = more && tiles.next(&x);
-      if (!more) x = none;
-      while (asked) {
-        const bool further = more && tiles.next(&y);
-        if (!wait_place()) break;
-        const uint32_t place = t % PLACES, to = ring + place * kOperand;
-        check(p, x, tid == 0);
-        if constexpr (FACTS) {
-          state(place, f);
-          f = fact(x);
+      bool asked = false;
+#pragma unroll 1
+      while (true) {
+        if (asked) {
+          if (!wait_place()) break;
+          cp_wait<0>();
+          const uint32_t place = t % PLACES;
+          if constexpr (FACTS) state(place, f);
+          expand(pc, ring + place * kOperand);
+          hand_over(t);
+          ++t;
         }
-        put(a, pc, to, 0);
-        ask(a, pc, x.a, x.live);
-        put(b, pc, to, 1);
-        ask(b, pc, x.b, x.live - kPage);
-        hand_over(t);
-        ++t;
         asked = more;
-        more = further;
-        x = further ? y : none;
+        if (!more) break;
+        Tile now = x;
+        check(p, now, tid == 0);
+        more = tiles.next(&x);
+        if (FACTS) f = fact(now);
+        ask(pc, now);
       }
+      cp_wait<0>();
     }
   }
 };
+// Bytes of a group's stretches.
+template <int FMT>
+constexpr int kStage = FMT == CERTKV_STORE_BF16 ? 0 : FMT == CERTKV_STORE_FP8 ? 128 * 128 : 128 * 96;
 
-template <int N>
-__device__ __forceinline__ void regs_up() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ __forceinline__ void regs_down() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+// A warpgroup's registers, from those of the launch up or down; the launch's must cover all.
+template <int N, int LAUNCH>
+__device__ __forceinline__ void registers() {
+  if constexpr (N > LAUNCH) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+  if constexpr (N < LAUNCH) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
 }  // namespace gt
