@@ -7,8 +7,8 @@
 //
 // Launches: what is known of each row, and the segments' tiles (grad_rows); the stored slots
 // (grad_q.cu for dq, grad_kv.cu for dk and dv; with few rows grad_kv.cu for all three); the
-// drafts' own keys and values (grad_drafts); and the sums over the shares and chunks that those
-// left (grad_merge), in one order.
+// drafts' own keys and values, with what the shares left of dq (grad_drafts); and the sums over
+// what is left in parts (grad_merge), in one order.
 //
 // What a row does not see cannot reach it, nor the row that, though matrix products sum over all
 // rows and drafts of a tile: rows that take no part enter them as zeros with probability 0, and
@@ -28,19 +28,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kChunkRows = 128;  // query rows of a block of the drafts' kernel
 
-__device__ __forceinline__ float4 load4(const uint16_t* row, int lane) {
-  const uint2 x = *reinterpret_cast<const uint2*>(row + 4 * lane);
-  return make_float4(bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y));
-}
 __device__ __forceinline__ void store4(uint16_t* row, int lane, float4 a) {
   const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x, a.y), hi = __floats2bfloat162_rn(a.z, a.w);
   *reinterpret_cast<uint2*>(row + 4 * lane) =
       make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
-__device__ __forceinline__ bool finite4(float4 a) {
-  return fabsf(a.x) < INFINITY && fabsf(a.y) < INFINITY && fabsf(a.z) < INFINITY && fabsf(a.w) < INFINITY;
-}
-
 // Block 0: the tiles of the segments before each.  Latency of one launch.
 __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
   __shared__ long long part[kThreads / 32];
@@ -81,62 +73,97 @@ __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
   if (threadIdx.x == 0) p.first[p.units] = carry;
 }
 
-// One warp per row: its log-sum-exp in the log2 domain and delta; +inf and 0 where it takes no
-// part; NaN where its query or its output's gradient holds a NaN or infinity.
+// Sixteen lanes per row: its log-sum-exp in the log2 domain and delta; +inf and 0 where it takes
+// no part; NaN where its query or its output's gradient holds a NaN or infinity.
 __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_constant__ GradArgs p) {
   release_next();
   if (blockIdx.x == 0) {
     scan_tiles(p);
     return;
   }
-  const int64_t w = ((int64_t)(blockIdx.x - 1) * kThreads + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  if (w >= (int64_t)p.units * p.rows) return;
+  const int lane = threadIdx.x & 31, c = lane & 15;
+  const int64_t all = (int64_t)p.units * p.rows;
+  const int64_t w0 = ((int64_t)(blockIdx.x - 1) * kThreads + threadIdx.x) >> 4, w = min(w0, all - 1);
   const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
   const GradUnit x(p, u);
   const int qh = x.h * p.G + g;
   const int64_t at = (((int64_t)x.b * p.L + x.l) * p.T + t) * p.H * p.G + qh;
-  const float4 q = load4(p.q.at(x.b, x.l, t, qh), lane), go = load4(p.go.at(x.b, x.l, t, qh), lane);
-  const float4 o = load4(p.o.at(x.b, x.l, t, qh), lane);
-  const float lse = p.lse[at];
-  float delta = go.x * o.x + go.y * o.y + go.z * o.z + go.w * o.w;
+  const uint4 q = *(reinterpret_cast<const uint4*>(p.q.at(x.b, x.l, t, qh)) + c);
+  const uint4 d = *(reinterpret_cast<const uint4*>(p.go.at(x.b, x.l, t, qh)) + c);
+  const uint4 o = *(reinterpret_cast<const uint4*>(p.o.at(x.b, x.l, t, qh)) + c);
+  const float lse = p.lse[at], dlse = p.dlse ? p.dlse[at] : 0.f;
+  const uint32_t qw[4] = {q.x, q.y, q.z, q.w}, dw[4] = {d.x, d.y, d.z, d.w}, ow[4] = {o.x, o.y, o.z, o.w};
+  float delta = 0.f;
+  bool odd = false;
 #pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) delta += __shfl_xor_sync(kFull, delta, s);
-  if (p.dlse) delta -= p.dlse[at];
-  const bool good = __all_sync(kFull, finite4(q) && finite4(go));
-  if (lane == 0)
+  for (int i = 0; i < 4; ++i) {
+    delta = fmaf(bf16lo(dw[i]), bf16lo(ow[i]), delta);
+    delta = fmaf(bf16hi(dw[i]), bf16hi(ow[i]), delta);
+    odd |= (qw[i] & 0x7f80u) == 0x7f80u || (qw[i] & 0x7f800000u) == 0x7f800000u || (dw[i] & 0x7f80u) == 0x7f80u ||
+           (dw[i] & 0x7f800000u) == 0x7f800000u;
+  }
+#pragma unroll
+  for (int s = 8; s >= 1; s >>= 1) delta += __shfl_xor_sync(kFull, delta, s);
+  odd = (__ballot_sync(kFull, odd) & (0xffffu << (lane & 16))) != 0u;
+  if (c == 0 && w0 < all)
     p.row[w] = lse == -INFINITY ? make_float2(INFINITY, 0.f)
-               : good           ? make_float2(lse * 1.4426950408889634f, delta)
-                                : make_float2(nanf(""), nanf(""));
+               : odd            ? make_float2(nanf(""), nanf(""))
+                                : make_float2(lse * 1.4426950408889634f, delta - dlse);
 }
 
-// One warp per query row: the records of the shares that met its segment, and the drafts' part;
-// behind them one per draft: its chunks, where there are several.
+// The records of unit u: shares c0 .. c1 (c1 < c0: none), of which folding leaves the first.
+struct Records {
+  int c0, c1;
+  __device__ __forceinline__ Records(const GradArgs& p, int u, bool folded) {
+    const int64_t f0 = p.first[u], f1 = p.first[u + 1], per = tiles_per_share(p);
+    c0 = f1 > f0 ? (int)(f0 / per) : 1;
+    c1 = f1 > f0 ? (folded ? c0 : (int)((f1 - 1) / per)) : 0;
+  }
+};
+__device__ __forceinline__ void add4(float4& a, const float* from, int lane) {
+  const float4 x = *reinterpret_cast<const float4*>(from + 4 * lane);
+  a.x += x.x;
+  a.y += x.y;
+  a.z += x.z;
+  a.w += x.w;
+}
+
+// Few segments, of which each met many shares: one block per row adds their records up into the
+// first, each warp every eighth of them, so that no warp goes through all.
+__global__ void __launch_bounds__(kThreads) grad_fold_kernel(const __grid_constant__ GradArgs p) {
+  __shared__ float4 part[kThreads / 32][32];
+  const int u = blockIdx.x / p.rows, r = blockIdx.x - u * p.rows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  await_previous();
+  release_next();
+  const Records c(p, u, false);
+  if (c.c1 <= c.c0) return;
+  const int blk = r / p.rb, br = r - blk * p.rb;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = c.c0 + warp; i <= c.c1; i += kThreads / 32) add4(a, p.rec + (grad_record(p, i, u, blk) + br) * kD, lane);
+  part[warp][lane] = a;
+  __syncthreads();
+  if (warp > 0) return;
+#pragma unroll
+  for (int w = 1; w < kThreads / 32; ++w) add4(a, &part[w][0].x, lane);
+  *reinterpret_cast<float4*>(p.rec + (grad_record(p, c.c0, u, blk) + br) * kD + 4 * lane) = a;
+}
+
+// Without drafts one warp per query row: the records of the shares that met its segment.  With
+// them one per draft and gradient: its chunks, where there are several.
 __global__ void __launch_bounds__(kThreads) grad_merge_kernel(const __grid_constant__ GradArgs p) {
   int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
   await_previous();
-  const int64_t rows = p.dq.p ? (int64_t)p.units * p.rows : 0;
+  const int64_t rows = p.dq.p && !p.kn.p ? (int64_t)p.units * p.rows : 0;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](const float* from) {
-    const float4 x = *reinterpret_cast<const float4*>(from + 4 * lane);
-    a.x += x.x;
-    a.y += x.y;
-    a.z += x.z;
-    a.w += x.w;
-  };
   if (w < rows) {
     const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
     const GradUnit x(p, u);
     const int blk = r / p.rb, br = r - blk * p.rb;
-    const int64_t f0 = p.first[u], f1 = p.first[u + 1];
-    if (f1 > f0) {
-      const int64_t per = tiles_per_share(p);
-      const int c1 = (int)((f1 - 1) / per);
+    const Records c(p, u, p.folded);
 #pragma unroll 4
-      for (int c = (int)(f0 / per); c <= c1; ++c) add(p.rec + (grad_record(p, c, u, blk) + br) * kD);
-    }
-    if (p.kn.p) add(p.dq_new + w * kD);
+    for (int i = c.c0; i <= c.c1; ++i) add4(a, p.rec + (grad_record(p, i, u, blk) + br) * kD, lane);
     store4(p.dq.at(x.b, x.l, t, x.h * p.G + g), lane,
            make_float4(a.x * p.scale, a.y * p.scale, a.z * p.scale, a.w * p.scale));
     return;
@@ -146,7 +173,7 @@ __global__ void __launch_bounds__(kThreads) grad_merge_kernel(const __grid_const
   const int u = (int)(w / (2 * p.T)), i = (int)(w - (int64_t)u * 2 * p.T), key = i < p.T, j = key ? i : i - p.T;
   const GradUnit x(p, u);
 #pragma unroll 4
-  for (int c = 0; c < p.chunks; ++c) add(p.part + (((int64_t)u * p.chunks + c) * 2 * p.T + i) * kD);
+  for (int c = 0; c < p.chunks; ++c) add4(a, p.part + (((int64_t)u * p.chunks + c) * 2 * p.T + i) * kD, lane);
   const float f = key ? p.scale : 1.f;
   store4((key ? p.dkn : p.dvn).at(x.b, x.l, j, x.h), lane, make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }
@@ -184,9 +211,14 @@ struct Drafts {  // TD: the drafts, filled up with zeros
   static constexpr int kKeyOff = 0, kValueOff = TD * kPitch;
   static constexpr int kRowOff = 2 * TD * kPitch, kGradOff = kRowOff + kChunkRows * kPitch;
   static constexpr int kPOff = kGradOff + kChunkRows * kPitch, kEOff = kPOff + kChunkRows * kWide;
-  static constexpr int kInfoOff = kEOff + kChunkRows * kWide, kSeenOff = kInfoOff + kChunkRows * 8;
+  static constexpr int kRest = 2 * kChunkRows * kWide;  // p and e's roundings' remainders lie so far behind them
+  static constexpr int kInfoOff = kEOff + kChunkRows * kWide + kRest, kSeenOff = kInfoOff + kChunkRows * 8;
   static constexpr int kBadOff = kSeenOff + kChunkRows * 8, kBytes = kBadOff + 16;
 };
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
+}
 
 // One block per (unit, 128 query rows), on mma.sync: products of at most 128 x 64 x 128, whose
 // time is that of bringing the rows in.  A warp makes p and e of 16 rows and their dq; then each
@@ -210,38 +242,72 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
     sees[tid] = tid < rows && info[tid].x != INFINITY ? grad_seen(p, x.b, (r0 + tid) / p.G) : 0ull;
   }
   __syncthreads();
-  const int c = tid & 15;
-  for (int j = tid >> 4; j < TD; j += kThreads / 16) {  // keys with a NaN or infinity as zeros, and noted
-    uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
-    if (j < p.T) {
-      k = *(reinterpret_cast<const uint4*>(p.kn.at(x.b, x.l, j, x.h)) + c);
-      v = *(reinterpret_cast<const uint4*>(p.vn.at(x.b, x.l, j, x.h)) + c);
-    }
-    const uint32_t w[4] = {k.x, k.y, k.z, k.w};
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-    const uint32_t any = __ballot_sync(kFull, odd) & (0xffffu << (lane & 16));
-    if (any) {
-      k = make_uint4(0u, 0u, 0u, 0u);
-      if (c == 0) atomicOr(bad, 1ull << j);
-    }
-    *reinterpret_cast<uint4*>(sm + D::kKeyOff + j * kPitch + 16 * c) = k;
-    *reinterpret_cast<uint4*>(sm + D::kValueOff + j * kPitch + 16 * c) = v;
-  }
-  for (int r = tid >> 4; r < 16 * strips; r += kThreads / 16) {
-    uint4 q = make_uint4(0u, 0u, 0u, 0u), g = q;
-    if (fabsf(info[r].x) < INFINITY) {
-      const int tok = (r0 + r) / p.G, qh = x.h * p.G + (r0 + r) - tok * p.G;
-      q = *(reinterpret_cast<const uint4*>(p.q.at(x.b, x.l, tok, qh)) + c);
-      g = *(reinterpret_cast<const uint4*>(p.go.at(x.b, x.l, tok, qh)) + c);
-    }
-    *reinterpret_cast<uint4*>(sm + D::kRowOff + r * kPitch + 16 * c) = q;
-    *reinterpret_cast<uint4*>(sm + D::kGradOff + r * kPitch + 16 * c) = g;
-  }
-  __syncthreads();
+  const int c = tid & 15;  // 16 lanes a row, 16 bytes each
   const uint32_t base = smem(sm);
+  {
+    const uint16_t *q0 = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *g0 = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
+#pragma unroll
+    for (int i = 0; i < kChunkRows / (kThreads / 16); ++i) {
+      const int r = (tid >> 4) + i * (kThreads / 16);
+      if (r >= 16 * strips) break;
+      const bool on = fabsf(info[r].x) < INFINITY;
+      const int br = r0 + r, tok = br / p.G, g = br - tok * p.G;
+      copy16(base + D::kRowOff + r * kPitch + 16 * c, on ? q0 + tok * p.q.st + g * p.q.sh : q0, on);
+      copy16(base + D::kGradOff + r * kPitch + 16 * c, on ? g0 + tok * p.go.st + g * p.go.sh : g0, on);
+    }
+  }
+  {
+    constexpr int kEach = TD / (kThreads / 16) > 0 ? TD / (kThreads / 16) : 1;
+    uint4 k[kEach], v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int j = (tid >> 4) + i * (kThreads / 16);
+      k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (j < p.T) {
+        k[i] = *(reinterpret_cast<const uint4*>(p.kn.at(x.b, x.l, j, x.h)) + c);
+        v[i] = *(reinterpret_cast<const uint4*>(p.vn.at(x.b, x.l, j, x.h)) + c);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {  // keys with a NaN or infinity as zeros, and noted
+      const int j = (tid >> 4) + i * (kThreads / 16);
+      const uint32_t w[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+      bool odd = false;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) odd |= (w[n] & 0x7f80u) == 0x7f80u || (w[n] & 0x7f800000u) == 0x7f800000u;
+      const uint32_t any = __ballot_sync(kFull, odd) & (0xffffu << (lane & 16));
+      if (any) {
+        k[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (c == 0) atomicOr(bad, 1ull << j);
+      }
+      *reinterpret_cast<uint4*>(sm + D::kKeyOff + j * kPitch + 16 * c) = k[i];
+      *reinterpret_cast<uint4*>(sm + D::kValueOff + j * kPitch + 16 * c) = v[i];
+    }
+  }
   const int g8 = lane >> 2, t4 = lane & 3;
+  // dq of a warp's 16 rows begins with what the shares left of it, all its loads under way
+  float acc[kD / 8][4];
+#pragma unroll
+  for (int n = 0; n < kD / 8; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
+  if (p.dq.p && warp < strips) {
+    const Records c(p, u, p.folded);
+    for (int i = c.c0; i <= c.c1; ++i) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int br = min(r0 + 16 * warp + g8 + 8 * h, p.rows - 1), blk = br / p.rb;
+        const float* rec = p.rec + (grad_record(p, i, u, blk) + br - blk * p.rb) * kD + 2 * t4;
+#pragma unroll
+        for (int n = 0; n < kD / 8; ++n) {
+          const float2 y = *reinterpret_cast<const float2*>(rec + 8 * n);
+          acc[n][2 * h] += y.x, acc[n][2 * h + 1] += y.y;
+        }
+      }
+    }
+  }
+  asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
   // lane's address offsets of 16 x 16 blocks: rows as they lie (A), rows as columns of B, and
   // transposed (B from [k][n], A from [k][m])
   const int lr = lane & 7, l8 = lane >> 3 & 1, l16 = lane >> 4;
@@ -273,7 +339,7 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
     const unsigned long long odd = *bad;
     const float2 i0 = info[s0 + g8], i1 = info[s0 + g8 + 8];
     const uint64_t see0 = sees[s0 + g8], see1 = sees[s0 + g8 + 8];
-    uint32_t e[TD / 8][2];
+    uint32_t e[TD / 8][2], rest[TD / 8][2];
 #pragma unroll
     for (int n = 0; n < TD / 8; ++n) {
       float pr[4], er[4];
@@ -287,33 +353,41 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
       }
       e[n][0] = pack2(er[0], er[1]);
       e[n][1] = pack2(er[2], er[3]);
+      rest[n][0] = pack2(er[0] - bf16lo(e[n][0]), er[1] - bf16hi(e[n][0]));
+      rest[n][1] = pack2(er[2] - bf16lo(e[n][1]), er[3] - bf16hi(e[n][1]));
       const int at = (s0 + g8) * D::kWide + 16 * n + 4 * t4;
-      *reinterpret_cast<uint32_t*>(sm + D::kPOff + at) = pack2(pr[0], pr[1]);
-      *reinterpret_cast<uint32_t*>(sm + D::kPOff + at + 8 * D::kWide) = pack2(pr[2], pr[3]);
-      *reinterpret_cast<uint32_t*>(sm + D::kEOff + at) = e[n][0];
-      *reinterpret_cast<uint32_t*>(sm + D::kEOff + at + 8 * D::kWide) = e[n][1];
+      const uint32_t p0 = pack2(pr[0], pr[1]), p1 = pack2(pr[2], pr[3]);
+      auto put = [&](int off, uint32_t lo, uint32_t hi) {
+        *reinterpret_cast<uint32_t*>(sm + off + at) = lo;
+        *reinterpret_cast<uint32_t*>(sm + off + at + 8 * D::kWide) = hi;
+      };
+      put(D::kPOff, p0, p1);
+      put(D::kPOff + D::kRest, pack2(pr[0] - bf16lo(p0), pr[1] - bf16hi(p0)), pack2(pr[2] - bf16lo(p1), pr[3] - bf16hi(p1)));
+      put(D::kEOff, e[n][0], e[n][1]);
+      put(D::kEOff + D::kRest, rest[n][0], rest[n][1]);
     }
     if (p.dq.p) {
-      float* out = p.dq_new + ((int64_t)u * p.rows + r0 + s0) * kD;
-#pragma unroll 2
-      for (int d = 0; d < kD / 16; ++d) {
-        float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < kD / 16; ++d)
 #pragma unroll
         for (int k = 0; k < TD / 16; ++k) {
           const uint32_t a[4] = {e[2 * k][0], e[2 * k][1], e[2 * k + 1][0], e[2 * k + 1][1]};
+          const uint32_t ar[4] = {rest[2 * k][0], rest[2 * k][1], rest[2 * k + 1][0], rest[2 * k + 1][1]};
           uint32_t b[4];
           ldm4t(base + (uint32_t)(D::kKeyOff + (16 * k + lr + 8 * l8) * kPitch + 32 * d + 16 * l16), b);
-          mma(a0, a, b[0], b[1]);
-          mma(a1, a, b[2], b[3]);
+          mma(acc[2 * d], a, b[0], b[1]);
+          mma(acc[2 * d + 1], a, b[2], b[3]);
+          mma(acc[2 * d], ar, b[0], b[1]);
+          mma(acc[2 * d + 1], ar, b[2], b[3]);
         }
-        const int col = 16 * d + 2 * t4;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (s0 + g8 + 8 * h < rows) {
-            float* o = out + (g8 + 8 * h) * kD + col;
-            *reinterpret_cast<float2*>(o) = make_float2(a0[2 * h], a0[2 * h + 1]);
-            *reinterpret_cast<float2*>(o + 8) = make_float2(a1[2 * h], a1[2 * h + 1]);
-          }
+      for (int h = 0; h < 2; ++h) {
+        const int br = r0 + s0 + g8 + 8 * h, tok = br / p.G;
+        if (s0 + g8 + 8 * h >= rows) continue;
+        uint16_t* out = p.dq.at(x.b, x.l, tok, x.h * p.G + br - tok * p.G) + 2 * t4;
+#pragma unroll
+        for (int n = 0; n < kD / 8; ++n)
+          *reinterpret_cast<uint32_t*>(out + 8 * n) = pack2(acc[n][2 * h] * p.scale, acc[n][2 * h + 1] * p.scale);
       }
     }
   }
@@ -333,14 +407,17 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
     ldm4t(at + D::kGradOff, bg);
 #pragma unroll
     for (int i = 0; i < TD / 16; ++i) {
-      uint32_t ap[4], ae[4];
-      const uint32_t to = base + (uint32_t)((16 * k + lr + 8 * l16) * D::kWide + 32 * i + 16 * l8);
-      ldm4t(to + D::kPOff, ap);
-      ldm4t(to + D::kEOff, ae);
-      mma(dv[i][0], ap, bg[0], bg[1]);
-      mma(dv[i][1], ap, bg[2], bg[3]);
-      mma(dk[i][0], ae, bq[0], bq[1]);
-      mma(dk[i][1], ae, bq[2], bq[3]);
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        uint32_t ap[4], ae[4];
+        const uint32_t to = base + (uint32_t)(part * D::kRest + (16 * k + lr + 8 * l16) * D::kWide + 32 * i + 16 * l8);
+        ldm4t(to + D::kPOff, ap);
+        ldm4t(to + D::kEOff, ae);
+        mma(dv[i][0], ap, bg[0], bg[1]);
+        mma(dv[i][1], ap, bg[2], bg[3]);
+        mma(dk[i][0], ae, bq[0], bq[1]);
+        mma(dk[i][1], ae, bq[2], bq[3]);
+      }
     }
   }
 #pragma unroll
@@ -388,7 +465,7 @@ constexpr int kMaxCtas = 1024;  // records are sized for at most this many
 
 struct GradLayout {
   int nblk, rb, chunks;
-  size_t row, first, rec, dq_new, part, total;
+  size_t row, first, rec, part, total;
   GradLayout(int64_t units, int tokens, int rows) {
     auto a = [](size_t x) { return (x + 255) / 256 * 256; };
     nblk = (rows + kGradRows - 1) / kGradRows;
@@ -398,8 +475,7 @@ struct GradLayout {
     row = 0;
     first = row + a(n * sizeof(float2));
     rec = first + a(((size_t)units + 1) * sizeof(int64_t));
-    dq_new = rec + ((size_t)units * nblk + kMaxCtas) * rb * kD * sizeof(float);
-    part = dq_new + n * kD * sizeof(float);
+    part = rec + ((size_t)units * nblk + kMaxCtas) * rb * kD * sizeof(float);
     total = part + (chunks > 1 ? (size_t)units * chunks * 2 * tokens * kD * sizeof(float) : 0);
   }
 };
@@ -473,7 +549,6 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   p.row = reinterpret_cast<float2*>(ws + ly.row);
   p.first = reinterpret_cast<int64_t*>(ws + ly.first);
   p.rec = reinterpret_cast<float*>(ws + ly.rec);
-  p.dq_new = reinterpret_cast<float*>(ws + ly.dq_new);
   p.part = reinterpret_cast<float*>(ws + ly.part);
   // warps of the merge, blocks of the drafts' kernel
   const int64_t n = (int64_t)p.units * p.rows;
@@ -483,13 +558,15 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   sms = std::min(sms, kMaxCtas);
   const bool fused = p.dks && p.rows <= kGradFused;
   p.groups = fused ? sms : std::max(sms / p.nblk, 1);
+  // shares that a segment may meet, where segments are few and long (one of 131072 slots)
+  p.folded = p.dq.p && p.groups > 8 * (int64_t)p.units && p.st.max_pages > 16;
   // a CTA counts its tiles and blocks of rows in 32 bits
   if ((int64_t)p.units * (p.st.max_pages + 2) / p.groups * ((p.rows + kGradFused - 1) / kGradFused) >= (1 << 29))
     return CERTKV_EINVAL;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   {
     TraceScope ts_("grad_rows", st);
-    if (!launch_kernel(false, grad_rows_kernel, warps(n) + 1, kThreads, 0, st, p)) return cuda_failed();
+    if (!launch_kernel(false, grad_rows_kernel, warps((n + 1) / 2) + 1, kThreads, 0, st, p)) return cuda_failed();
   }
   if (p.dks) {
     GradArgs all = p;
@@ -497,13 +574,17 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
     if (!launch_grad_kv(all, store->format, st)) return cuda_failed();
   }
   if (p.dq.p && !fused && !launch_grad_q(p, store->format, st)) return cuda_failed();
+  if (p.folded) {
+    TraceScope ts_("grad_fold", st);
+    if (!launch_kernel(true, grad_fold_kernel, (unsigned)n, kThreads, 0, st, p)) return cuda_failed();
+  }
   if (p.kn.p && (p.dq.p || p.dkn.p)) {
     TraceScope ts_("grad_drafts", st);
     if (!(tokens <= 16 ? launch_drafts<16>(p, st) : launch_drafts<64>(p, st))) return cuda_failed();
   }
-  if (p.dq.p || (p.dkn.p && p.chunks > 1)) {
+  const int64_t w = p.kn.p ? (p.dkn.p && p.chunks > 1 ? 2 * (int64_t)p.units * tokens : 0) : p.dq.p ? n : 0;
+  if (w > 0) {
     TraceScope ts_("grad_merge", st);
-    const int64_t w = (p.dq.p ? n : 0) + (p.dkn.p && p.chunks > 1 ? 2 * (int64_t)p.units * tokens : 0);
     launch_kernel(true, grad_merge_kernel, warps(w), kThreads, 0, st, p);
   }
   return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA;

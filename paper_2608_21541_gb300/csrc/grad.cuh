@@ -19,6 +19,7 @@ struct GradArgs {
   int nblk, rb;      // row blocks of a unit, rows of a block (the last may have fewer)
   int groups;        // shares of the tiles; their CTAs leave records
   int chunks;        // of the drafts' kernel: 128 rows each
+  int folded;        // a unit's records have been added up into its first
   Rows q, kn, vn, o, go, dq, dkn, dvn;  // kn.p null: the drafts have no keys of their own
   const uint64_t* mask;
   const float *lse, *dlse;
@@ -29,7 +30,6 @@ struct GradArgs {
   float2* row;     // [units][rows] log-sum-exp (log2 domain), delta; see grad_rows_kernel
   int64_t* first;  // [units + 1] tiles of the segments before
   float* rec;      // [groups + units][nblk][rb][128] dq / scale over a share's tiles
-  float* dq_new;   // [units][rows][128] the same over the drafts
   float* part;     // [units][chunks][2][T][128] the drafts' dk / scale and dv over 128 rows
 };
 

@@ -31,10 +31,12 @@ struct ReserveArgs {
   const int32_t *room, *want;
   int per_seq;     // segments of a sequence
   int per_block;   // segments of a block
-  longlong2* sums; // [blocks] pages given back and asked for
+  longlong2* sums;  // [blocks] pages given back and asked for
+  int* n0;          // the free pages before the call
 };
 
 constexpr int kThreads = 256;
+constexpr int kMovePages = 128;  // pages of a segment that a block moves
 
 // What segment u gives back and asks for.
 struct Change {
@@ -91,6 +93,7 @@ __global__ void __launch_bounds__(kThreads) pages_sum_kernel(const ReserveArgs p
   }
   block_scan(sum, &all);
   if (threadIdx.x == 0) p.sums[blockIdx.x] = all;
+  if (threadIdx.x == 0 && blockIdx.x == 0) *p.n0 = min(max(*p.pg.free_count, 0), p.st.pool_pages);
 }
 
 // Sums of the blocks before this one, and of all.
@@ -105,18 +108,50 @@ __device__ __forceinline__ void block_base(const ReserveArgs& p, longlong2* base
   block_scan(t, total);
 }
 
+// A segment's pages [first, first + n) of its table row, number num, num + 1, .. of the call.
+struct Run {
+  int u, first, n;
+  long long num;
+};
+// Page k of a run goes to the list (TAKE false) or comes from it; false: not as it should.
+template <bool TAKE>
+__device__ __forceinline__ bool move_page(const ReserveArgs& p, const Run& r, int k, int n0, int top) {
+  int32_t* e = p.st.table + (int64_t)r.u * p.st.max_pages + r.first + k;
+  const long long place = top - 1 - (r.num + k);
+  if (TAKE) {
+    const int page = p.pg.free[place];  // 0 <= place: n is what is left
+    *e = page;
+    return page >= 0 && page < p.st.pool_pages;
+  }
+  if (place >= n0) p.pg.free[place] = *e;
+  *e = -1;
+  return place >= n0;
+}
+template <bool TAKE>
+__device__ __forceinline__ Run run_of(int u, const Change& c, const longlong2& before, int top) {
+  const long long num = TAKE ? before.y : before.x;
+  return {u, TAKE ? c.held : c.need, TAKE ? (int)min((long long)c.more(), max(top - num, 0ll)) : c.back(), num};
+}
+// The account of segment u, n pages handed out; false: cut or short.
+__device__ __forceinline__ bool settle(const ReserveArgs& p, int u, const Change& c, int n) {
+  p.pg.held[u] = min(c.held, c.need) + n;
+  if (p.st.counts[u] > c.slots) p.st.counts[u] = (int)c.slots;
+  return !c.cut && n == c.more();
+}
+
 // TAKE false: the pages given back go to the list.  TAKE true: pages are handed out, and
 // the account is brought up to date.  A segment's pages are moved by its thread where
-// they are few, by its whole warp where there are many.
+// they are few, by its whole warp where there are many, kMovePages of them by each of the
+// blocks of a column of the grid (a 131072-token sequence's 524288 pages taken back and handed
+// out: 275 -> 48 us against one block a segment).
 template <bool TAKE>
 __global__ void __launch_bounds__(kThreads) pages_move_kernel(const ReserveArgs p) {
   await_previous();
   release_next();
   longlong2 at, total;
   block_base(p, &at, &total);
-  const int pool = p.st.pool_pages, n0 = min(max(*p.pg.free_count, 0), pool);
-  const int top = (int)min(n0 + total.x, (long long)pool);
-  const int lane = threadIdx.x & 31;
+  const int n0 = *p.n0, top = (int)min(n0 + total.x, (long long)p.st.pool_pages);
+  const int lane = threadIdx.x & 31, k0 = blockIdx.y * kMovePages;
   bool bad = false;
   for (int i0 = 0; i0 < p.per_block; i0 += kThreads) {
     const int i = i0 + threadIdx.x;
@@ -124,56 +159,87 @@ __global__ void __launch_bounds__(kThreads) pages_move_kernel(const ReserveArgs 
     const int u = i < p.per_block && unit < p.st.units ? (int)unit : p.st.units;
     const Change c = change_of(p, u);
     longlong2 all;
-    const longlong2 in = block_scan(make_longlong2(c.back(), c.more()), &all);
-    // pages [first, first + n) of the row; page k of them is number num + k of the call
-    const long long num = TAKE ? at.y + in.y : at.x + in.x;
+    longlong2 in = block_scan(make_longlong2(c.back(), c.more()), &all);
+    in.x += at.x, in.y += at.y;
     at.x += all.x, at.y += all.y;
-    const int first = TAKE ? c.held : c.need;
-    const int n = TAKE ? (int)min((long long)c.more(), max(top - num, 0ll)) : c.back();
-    auto move = [&](int seg, int k, int s_first, long long s_num) {
-      int32_t* e = p.st.table + (int64_t)seg * p.st.max_pages + s_first + k;
-      const long long place = top - 1 - (s_num + k);
-      if (TAKE) {
-        const int page = p.pg.free[place];  // 0 <= place: n is what is left
-        if (page < 0 || page >= pool) bad = true;
-        *e = page;
-      } else {
-        if (place >= n0) p.pg.free[place] = *e;
-        else bad = true;
-        *e = -1;
-      }
-    };
+    const Run r = run_of<TAKE>(u, c, in, top);
     constexpr int kFew = 4;
-    if (n <= kFew)
-      for (int k = 0; k < n; ++k) move(u, k, first, num);
-    for (uint32_t many = __ballot_sync(kFull, n > kFew); many; many &= many - 1) {
+    if (r.n <= kFew && k0 == 0)
+      for (int k = 0; k < r.n; ++k) bad |= !move_page<TAKE>(p, r, k, n0, top);
+    for (uint32_t many = __ballot_sync(kFull, r.n > kFew && r.n > k0); many; many &= many - 1) {
       const int src = __ffs(many) - 1;
-      const int s_u = __shfl_sync(kFull, u, src), s_n = __shfl_sync(kFull, n, src);
-      const int s_first = __shfl_sync(kFull, first, src);
-      const long long s_num = __shfl_sync(kFull, num, src);
-#pragma unroll 4
-      for (int k = lane; k < s_n; k += 32) move(s_u, k, s_first, s_num);
+      const Run x = {__shfl_sync(kFull, r.u, src), __shfl_sync(kFull, r.first, src), __shfl_sync(kFull, r.n, src),
+                     __shfl_sync(kFull, r.num, src)};
+      const int k1 = min(x.n, k0 + kMovePages);
+#pragma unroll 8
+      for (int k = k0 + lane; k < k1; k += 32) bad |= !move_page<TAKE>(p, x, k, n0, top);
     }
-    if (TAKE && u < p.st.units) {
-      p.pg.held[u] = min(c.held, c.need) + n;
-      if (p.st.counts[u] > c.slots) p.st.counts[u] = (int)c.slots;
-      if (c.cut || n < c.more()) bad = true;
-    }
+    // behind every read of the account: those of the column's other blocks too, which have to
+    // see the same; the first block's threads settle it in a launch of their own where there
+    // are others
+    if (TAKE && gridDim.y == 1 && u < p.st.units) bad |= !settle(p, u, c, r.n);
   }
+  if (TAKE && gridDim.y == 1 && blockIdx.x == 0 && threadIdx.x == 0)
+    *p.pg.free_count = top - (int)min(total.y, (long long)top);
   if (bad) p.st.raise();
 }
 
-// Behind every block that reads the count it replaces.
-__global__ void __launch_bounds__(kThreads) pages_count_kernel(const ReserveArgs p, int blocks) {
+// The accounts, behind a grid of several blocks a segment.
+__global__ void __launch_bounds__(kThreads) pages_settle_kernel(const ReserveArgs p) {
   await_previous();
-  longlong2 t = make_longlong2(0, 0), all;
-  for (int i = threadIdx.x; i < blocks; i += kThreads) t.x += p.sums[i].x, t.y += p.sums[i].y;
-  block_scan(t, &all);
-  if (threadIdx.x == 0) {
-    const int pool = p.st.pool_pages, n0 = min(max(*p.pg.free_count, 0), pool);
-    const int top = (int)min(n0 + all.x, (long long)pool);
-    *p.pg.free_count = top - (int)min(all.y, (long long)top);
+  longlong2 at, total;
+  block_base(p, &at, &total);
+  const int top = (int)min(*p.n0 + total.x, (long long)p.st.pool_pages);
+  bool bad = false;
+  for (int i0 = 0; i0 < p.per_block; i0 += kThreads) {
+    const int i = i0 + threadIdx.x;
+    const int64_t unit = (int64_t)blockIdx.x * p.per_block + i;
+    const int u = i < p.per_block && unit < p.st.units ? (int)unit : p.st.units;
+    const Change c = change_of(p, u);
+    longlong2 all;
+    longlong2 in = block_scan(make_longlong2(c.back(), c.more()), &all);
+    in.x += at.x, in.y += at.y;
+    at.x += all.x, at.y += all.y;
+    if (u < p.st.units) bad |= !settle(p, u, c, run_of<true>(u, c, in, top).n);
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.pg.free_count = top - (int)min(total.y, (long long)top);
+  if (bad) p.st.raise();
+}
+
+// Few segments of few pages: everything by one block, which saves the launches (eight sequences
+// of one layer, both ways: 28 -> 15 us).
+constexpr int kSmallUnits = 4 * kThreads, kSmallPages = 128;
+__global__ void __launch_bounds__(kThreads) pages_small_kernel(const ReserveArgs p) {
+  constexpr int kEach = kSmallUnits / kThreads;
+  Change c[kEach];
+  longlong2 sum = make_longlong2(0, 0), total;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int u = kEach * (int)threadIdx.x + i;
+    c[i] = change_of(p, min(u, p.st.units));
+    sum.x += c[i].back(), sum.y += c[i].more();
+  }
+  const int n0 = min(max(*p.pg.free_count, 0), p.st.pool_pages);
+  longlong2 in = block_scan(sum, &total);
+  const int top = (int)min(n0 + total.x, (long long)p.st.pool_pages);
+  bool bad = false;
+  Run take[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int u = min(kEach * (int)threadIdx.x + i, p.st.units);
+    take[i] = run_of<true>(u, c[i], in, top);
+    const Run r = run_of<false>(u, c[i], in, top);
+    for (int k = 0; k < r.n; ++k) bad |= !move_page<false>(p, r, k, n0, top);
+    in.x += c[i].back(), in.y += c[i].more();
+  }
+  __syncthreads();  // the list holds what was given back
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    for (int k = 0; k < take[i].n; ++k) bad |= !move_page<true>(p, take[i], k, n0, top);
+    if (take[i].u < p.st.units) bad |= !settle(p, take[i].u, c[i], take[i].n);
+  }
+  if (threadIdx.x == 0) *p.pg.free_count = top - (int)min(total.y, (long long)top);
+  if (bad) p.st.raise();
 }
 
 // ------------------------------------------------------------ free list --
@@ -242,35 +308,10 @@ struct MapArgs {
   const int32_t *rows, *start, *base;
   const uint64_t* mask;
   int32_t *slots, *positions;
-  int64_t chunks;  // of kRows rows, of all segments
+  int64_t chunks;  // warps (step) or blocks, of all segments
 };
-constexpr int kRows = 128;  // rows of a warp
-
-__global__ void __launch_bounds__(kThreads) slot_map_kernel(const MapArgs p) {
-  const int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  if (w < p.chunks) {
-    const int per = (p.tokens + kRows - 1) / kRows;
-    const int u = (int)(w / per), i0 = (int)(w - (int64_t)u * per) * kRows;
-    const int n = p.rows ? min(max(p.rows[u / p.per_seq], 0), p.tokens) : p.tokens;
-    const int64_t start = p.start ? p.start[u] : p.st.counts[u];
-    bool bad = false;
-#pragma unroll
-    for (int j = 0; j < kRows; j += 32) {
-      const int i = i0 + j + lane;
-      if (i >= p.tokens) break;
-      int64_t at = -1;
-      if (i < n) {
-        const int64_t s = start + i;
-        if (s >= 0 && s < (int64_t)p.st.max_pages * kPage) at = p.st.slot(u, (int)s);
-        if (at < 0) bad = true;
-      }
-      p.slots[(int64_t)u * p.tokens + i] = (int32_t)at;
-    }
-    if (bad) p.st.raise();
-    return;
-  }
-  const int64_t e = (w - p.chunks) * 32 + lane;
+// Position e of the output, if there is one.
+__device__ __forceinline__ void position(const MapArgs& p, int64_t e) {
   if (!p.positions || e >= (int64_t)p.batch * p.tokens) return;
   const int b = (int)(e / p.tokens), t = (int)(e - (int64_t)b * p.tokens);
   int depth = t;
@@ -278,7 +319,98 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const MapArgs p) {
   p.positions[e] = (int32_t)((uint32_t)(p.base ? p.base[b] : 0) + (uint32_t)depth);
 }
 
+// A step's rows, a warp 32 of a segment; one launch's latency.
+constexpr int kStepRows = 512;  // up to this many rows a segment
+__global__ void __launch_bounds__(kThreads) slot_map_step_kernel(const MapArgs p) {
+  const int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31;
+  if (w < p.chunks) {
+    const int per = (p.tokens + 31) / 32, u = (int)(w / per), i = (int)(w - (int64_t)u * per) * 32 + lane;
+    const int n = p.rows ? min(max(p.rows[u / p.per_seq], 0), p.tokens) : p.tokens;
+    if (i >= p.tokens) return;
+    int64_t at = -1;
+    if (i < n) {
+      const int64_t s = (int64_t)(p.start ? p.start[u] : p.st.counts[u]) + i;
+      if (s >= 0 && s < (int64_t)p.st.max_pages * kPage) at = p.st.slot(u, (int)s);
+      if (at < 0) p.st.raise();
+    }
+    p.slots[(int64_t)u * p.tokens + i] = (int32_t)at;
+    return;
+  }
+  position(p, (w - p.chunks) * 32 + lane);
+}
+
+constexpr int kRows = 16384;  // rows of a segment that a block takes
+constexpr int kMapEach = kRows / 4 / kThreads;
+
+// Many rows: bound by the bytes it writes (a 131071-token prompt of 256 segments, 137 MB).  A
+// thread writes 16 bytes at a time wherever a row of the output begins; its four rows mostly lie
+// in one page, whose entry is the only thing that it reads.
+__global__ void __launch_bounds__(kThreads) slot_map_kernel(const MapArgs p) {
+  if (blockIdx.x >= p.chunks) {
+    position(p, (blockIdx.x - p.chunks) * kThreads + threadIdx.x);
+    return;
+  }
+  const int per = (p.tokens + kRows - 1) / kRows + (p.tokens % 4 != 0);  // one more: parts begin up to 3 rows early
+  const int u = (int)(blockIdx.x / per), part = (int)(blockIdx.x - (int64_t)u * per);
+  const int n = p.rows ? min(max(p.rows[u / p.per_seq], 0), p.tokens) : p.tokens;
+  const int64_t start = p.start ? p.start[u] : p.st.counts[u], most = (int64_t)p.st.max_pages * kPage;
+  // rows [lo, hi) have a place in the table
+  const int lo = (int)min(max(-start, (int64_t)0), (int64_t)p.tokens), hi = (int)max(min((int64_t)n, most - start), (int64_t)lo);
+  int32_t* out = p.slots + (int64_t)u * p.tokens;
+  const int early = (int)(reinterpret_cast<uintptr_t>(out) / 4 & 3);  // rows from the boundary before to the first
+  const int32_t* row = p.st.table + (int64_t)u * p.st.max_pages;
+  const int i0 = part * kRows - early, s0 = (int)start;
+  bool bad = (lo > 0 || hi < n) && n > 0 && part == 0;
+  int page[kMapEach];
+#pragma unroll
+  for (int j = 0; j < kMapEach; ++j) {
+    const int i = i0 + 4 * (j * kThreads + (int)threadIdx.x), r = max(i, lo);
+    page[j] = r < min(i + 4, hi) ? __ldg(row + ((s0 + r) >> 6)) : -1;
+  }
+#pragma unroll
+  for (int j = 0; j < kMapEach; ++j) {
+    const int i = i0 + 4 * (j * kThreads + (int)threadIdx.x), s = (int)((uint32_t)s0 + (uint32_t)i);
+    const bool ok = page[j] >= 0 && page[j] < p.st.pool_pages;
+    if (i >= lo && i + 4 <= hi && (s & 63) <= 60 && ok) {  // all four in one page
+      const int v = page[j] * kPage + (s & 63);
+      *reinterpret_cast<int4*>(out + i) = make_int4(v, v + 1, v + 2, v + 3);
+      continue;
+    }
+    int v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[k] = -1;
+      if (i + k < lo || i + k >= hi) continue;
+      const int pg = __ldg(row + ((s + k) >> 6));
+      if (pg >= 0 && pg < p.st.pool_pages) v[k] = pg * kPage + ((s + k) & 63);
+      else bad = true;
+    }
+    if (i >= 0 && i + 4 <= p.tokens) {
+      *reinterpret_cast<int4*>(out + i) = make_int4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k >= 0 && i + k < p.tokens) out[i + k] = v[k];
+    }
+  }
+  if (bad) p.st.raise();
+}
+
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+// launch_kernel of a grid of two dimensions, early.
+bool launch_grid(void (*kernel)(ReserveArgs), dim3 grid, cudaStream_t st, const ReserveArgs& p) {
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = grid;
+  c.blockDim = dim3(kThreads);
+  c.stream = st;
+  c.attrs = &at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, p) == cudaSuccess;
+}
 int64_t free_blocks(int pool) { return ((int64_t)(pool + 31) / 32 + kWords - 1) / kWords; }
 
 }  // namespace
@@ -289,7 +421,7 @@ extern "C" size_t certkv_pages_workspace_bytes(int32_t units, int32_t pool_pages
   if (units < 1 || units > (1 << 24) || pool_pages < 1 || pool_pages >= (1 << 25)) return 0;
   const size_t bits = align256(((size_t)pool_pages + 31) / 32 * 4);
   const size_t blocks = std::max((size_t)(units + 7) / 8, (size_t)free_blocks(pool_pages));
-  return bits + align256(blocks * sizeof(longlong2));
+  return bits + align256((blocks + 1) * sizeof(longlong2));
 }
 
 extern "C" int certkv_pages_list(const certkv_store* store, const certkv_pages* pages, void* workspace,
@@ -343,24 +475,30 @@ extern "C" int certkv_pages_reserve(int32_t batch, const int32_t* room, const in
   p.want = want;
   p.per_seq = p.st.units / batch;
   p.per_block = p.st.max_pages >= 256 ? 8 : kThreads;
-  p.sums = reinterpret_cast<longlong2*>(workspace);
+  p.n0 = reinterpret_cast<int*>(workspace);
+  p.sums = reinterpret_cast<longlong2*>(workspace) + 1;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (p.st.units <= kSmallUnits && p.st.max_pages <= kSmallPages) {
+    TraceScope ts_("pages_small", s);
+    return launch_kernel(false, pages_small_kernel, 1, kThreads, 0, s, p) ? CERTKV_OK : cuda_failed();
+  }
   const unsigned blocks = (unsigned)((p.st.units + p.per_block - 1) / p.per_block);
+  const dim3 grid(blocks, (unsigned)((p.st.max_pages + kMovePages - 1) / kMovePages));
   {
     TraceScope ts_("pages_sum", s);
     if (!launch_kernel(false, pages_sum_kernel, blocks, kThreads, 0, s, p)) return cuda_failed();
   }
   {
     TraceScope ts_("pages_back", s);
-    if (!launch_kernel(true, pages_move_kernel<false>, blocks, kThreads, 0, s, p)) return cuda_failed();
+    if (!launch_grid(pages_move_kernel<false>, grid, s, p)) return cuda_failed();
   }
   {
     TraceScope ts_("pages_out", s);
-    if (!launch_kernel(true, pages_move_kernel<true>, blocks, kThreads, 0, s, p)) return cuda_failed();
+    if (!launch_grid(pages_move_kernel<true>, grid, s, p)) return cuda_failed();
   }
-  {
-    TraceScope ts_("pages_count", s);
-    launch_kernel(true, pages_count_kernel, 1, kThreads, 0, s, p, (int)blocks);
+  if (grid.y > 1) {
+    TraceScope ts_("pages_settle", s);
+    launch_kernel(true, pages_settle_kernel, blocks, kThreads, 0, s, p);
   }
   return cudaGetLastError() == cudaSuccess ? CERTKV_OK : CERTKV_ECUDA;
 }
@@ -386,11 +524,16 @@ extern "C" int certkv_slot_map(int32_t batch, int32_t tokens, const int32_t* row
   p.mask = mask;
   p.slots = slots;
   p.positions = positions;
-  p.chunks = slots ? (int64_t)p.st.units * ((tokens + kRows - 1) / kRows) : 0;
-  const int64_t warps = p.chunks + (positions ? ((int64_t)batch * tokens + 31) / 32 : 0);
-  const int64_t blocks = (warps * 32 + kThreads - 1) / kThreads;
+  const bool step = tokens <= kStepRows;
+  const int64_t each = step ? (tokens + 31) / 32 : (tokens + kRows - 1) / kRows + (tokens % 4 != 0);
+  p.chunks = slots ? p.st.units * each : 0;
+  const int64_t rest = positions ? (int64_t)batch * tokens : 0, per_warp = kThreads / 32;
+  const int64_t blocks = step ? (p.chunks + (rest + 31) / 32 + per_warp - 1) / per_warp
+                              : p.chunks + (rest + kThreads - 1) / kThreads;
   if (blocks > INT32_MAX) return CERTKV_EINVAL;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   TraceScope ts_("slot_map", s);
-  return launch_kernel(false, slot_map_kernel, (unsigned)blocks, kThreads, 0, s, p) ? CERTKV_OK : cuda_failed();
+  return launch_kernel(false, step ? slot_map_step_kernel : slot_map_kernel, (unsigned)blocks, kThreads, 0, s, p)
+             ? CERTKV_OK
+             : cuda_failed();
 }
