@@ -144,17 +144,24 @@ struct RowFeeder {
     if (!gt::wait_all(GRAD_AT(b_empty) + 8u * place, phase, GRAD_AT(abort))) return false;
     gt::sts32(GRAD_AT(nlse) + 4 * (place * kCols + tid), __float_as_uint(tid < 32 ? -lo.x : -hi.x));
     gt::sts32(GRAD_AT(ndelta) + 4 * (place * kCols + tid), __float_as_uint(tid < 32 ? -lo.y : -hi.y));
+    // four lanes a row, each every fourth 16 bytes of it: a row's address is worked out once for
+    // eight copies
     const uint32_t to = base + P::kBlockOff + place * kBlock;
-    const int c = tid & 15;
+    const int c = tid & 3;
     const uint16_t *q0 = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *g0 = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-      const int r = (tid >> 4) + 4 * i, br = j * kCols + r;
+#pragma unroll 2
+    for (int i = 0; i < 4; ++i) {
+      const int r = (tid >> 2) + 16 * i, br = j * kCols + r;
       const bool on = good >> r & 1u;
       const int tok = (int)((uint32_t)br * over_g >> 16), g = br - tok * p.G;  // br < 2^11, G <= 32: exact
-      const uint32_t at = to + (uint32_t)((c >> 3) * kRowHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-      gt::cp16(at, on ? q0 + tok * p.q.st + g * p.q.sh : q0, on);
-      gt::cp16(at + 2 * kRowHalf, on ? g0 + tok * p.go.st + g * p.go.sh : g0, on);
+      const uint16_t *q = on ? q0 + tok * p.q.st + g * p.q.sh : q0, *o = on ? g0 + tok * p.go.st + g * p.go.sh : g0;
+      const uint32_t at = to + (uint32_t)(r * 128), a0 = (uint32_t)((c ^ (r & 7)) << 4), a1 = a0 ^ 64u;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // 16 bytes number c + 4 k
+        const uint32_t d = at + (k >> 1) * kRowHalf + (k & 1 ? a1 : a0);
+        gt::cp16(d, q + 32 * k, on);
+        gt::cp16(d + 2 * kRowHalf, o + 32 * k, on);
+      }
     }
     gt::cp_commit();
     if (pending) {
