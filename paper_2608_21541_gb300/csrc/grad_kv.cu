@@ -432,7 +432,9 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
 
 // grid = groups (one CTA per SM), block = kThreads.
 template <int FMT, bool FUSED>
-__global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_constant__ GradArgs p) {
+__global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_constant__ CUtensorMap tmK,
+                                                              const __grid_constant__ CUtensorMap tmV,
+                                                              const __grid_constant__ GradArgs p) {
   using P = Plan<FMT, FUSED>;
   using M = Misc<FMT, FUSED>;
   extern __shared__ __align__(1024) char smem[];
@@ -475,10 +477,10 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
     gt::registers<kLoadRegs, kLaunchRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
     if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, P::kKeys, false, false> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), 0u, GRAD_AT(abort), base, base + P::kStageOff, tid};
+      gt::Feeder<FMT, P::kKeys, false, false> f{&tmK, p, GRAD_AT(k_full), GRAD_AT(k_empty), 0u, GRAD_AT(abort), GRAD_AT(last), base, base + P::kStageOff, tid};
       f.run(walk);
     } else {
-      gt::Feeder<FMT, P::kValues, true, false> f{p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort),
+      gt::Feeder<FMT, P::kValues, true, false> f{&tmV, p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort), GRAD_AT(last),
                                                  base + P::kValueOff, base + P::kStageOff + gt::kStage<FMT>, tid - kGroupWarps * 32};
       f.run(walk);
     }
@@ -505,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
 }
 
 template <int FMT, bool FUSED>
-bool launch(const GradArgs& p, cudaStream_t st) {
+bool launch(const CUtensorMap& mk, const CUtensorMap& mv, const GradArgs& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready{0};  // devices on which the shared memory is opted in to
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return false;
@@ -515,20 +517,23 @@ bool launch(const GradArgs& p, cudaStream_t st) {
       return false;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
-  return launch_kernel(true, grad_kv_kernel<FMT, FUSED>, (unsigned)p.groups, kThreads, smem_bytes<FMT, FUSED>(), st, p);
+  return launch_kernel(true, grad_kv_kernel<FMT, FUSED>, (unsigned)p.groups, kThreads, smem_bytes<FMT, FUSED>(), st, mk,
+                       mv, p);
 }
 template <int FMT>
-bool launch_rows(const GradArgs& p, cudaStream_t st) {
-  return p.rows <= kGradFused ? launch<FMT, true>(p, st) : launch<FMT, false>(p, st);
+bool launch_rows(const CUtensorMap& mk, const CUtensorMap& mv, const GradArgs& p, cudaStream_t st) {
+  return p.rows <= kGradFused ? launch<FMT, true>(mk, mv, p, st) : launch<FMT, false>(mk, mv, p, st);
 }
 
 }  // namespace
 
 bool launch_grad_kv(const GradArgs& p, int format, cudaStream_t st) {
+  CUtensorMap mk = {}, mv = {};
+  if (!gt::pool_maps(p, format, &mk, &mv)) return false;
   TraceScope ts_("grad_kv", st);
-  return format == CERTKV_STORE_BF16  ? launch_rows<CERTKV_STORE_BF16>(p, st)
-         : format == CERTKV_STORE_FP8 ? launch_rows<CERTKV_STORE_FP8>(p, st)
-                                      : launch_rows<CERTKV_STORE_FP4>(p, st);
+  return format == CERTKV_STORE_BF16  ? launch_rows<CERTKV_STORE_BF16>(mk, mv, p, st)
+         : format == CERTKV_STORE_FP8 ? launch_rows<CERTKV_STORE_FP8>(mk, mv, p, st)
+                                      : launch_rows<CERTKV_STORE_FP4>(mk, mv, p, st);
 }
 
 int grad_ctas() {

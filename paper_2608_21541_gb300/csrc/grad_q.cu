@@ -3,15 +3,16 @@
 // A CTA holds up to 128 query rows of a unit, and their output's gradients, as the M = 128 rows
 // of the MMAs, and walks a share of all tiles of 128 slots:
 //   S = Q K^T,  R = dO V^T,  e = 2^(S - lse) (R - delta),  dQ += e K,
-// with e handed over in tensor memory, over S, as a bf16 part plus the bf16 rounding of its
-// remainder (2^-16).  Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so
+// with e handed over in tensor memory, over S, as a bf16 part and one of its remainder (2^-15).  Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so
 // a tile is formed in one pass.
+// A thread takes 32 columns of a row, four warps share a row's.
 // Tensor memory: S of even tiles | S of odd tiles | R | dQ, 128 columns each.  S of the next
 // tile is made while e of this one is, R of the next as soon as R of this one has been read,
 // dQ of this one under e of the next.
 //
 // 8- and 4-bit stores: codes are exact in bf16 (gt::codes_to_bf16); a key's fp32 scale multiplies
-// its logit and its e, a value's its R, all in fp32.
+// its logit and its e, a value's its R, all in fp32.  The scale comes times that of the logits,
+// which is taken out of dQ again at the end.
 //
 // CTAs of the same share and different row blocks are neighbours: they read the same tiles at
 // about the same time, so all but the first find them in L2.
@@ -27,11 +28,11 @@
 namespace certkv {
 namespace {
 
-constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps;
+constexpr int kSoftWarps = 16, kLoadWarps = 2 * kGroupWarps;
 constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups, the issuer's the last
-// Registers a thread: the launch gives 96, which the roles share out among themselves.
-constexpr int kLaunchRegs = 96;
-constexpr int kSoftRegs = 112, kLoadRegs = 88, kIssueRegs = 80;
+// Registers a thread: the launch gives 72, which the roles share out among themselves.
+constexpr int kLaunchRegs = 72;
+constexpr int kSoftRegs = 80, kLoadRegs = 64, kIssueRegs = 56;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs,
               "a larger split would wait for registers for ever");
 constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
@@ -146,7 +147,7 @@ struct Issuer {
         }
         if (!ok) break;
         um::fence_after();
-        um::mma_o2(tmem + kColQ, tmem + 128u * (t & 1u), um::desc_lo(base + P::kKeyOff, kHalf) + qk.slot * (kOperand >> 4),
+        um::mma_e2(tmem + kColQ, tmem + 128u * (t & 1u), um::desc_lo(base + P::kKeyOff, kHalf) + qk.slot * (kOperand >> 4),
                    um::kDescHi, um::idesc(true, true), i > 0);
         um::commit(GRAD_AT(k_empty) + 8u * qk.slot);
         ++qk;
@@ -163,59 +164,59 @@ struct Issuer {
   }
 };
 
-// e of 32 columns of a row: the packed A operand and the rest of its rounding.  `loaded`: called
-// when the columns have been read.
+// e of 16 columns of a row, from the first column c on, over its logits: eight columns of bf16
+// and eight of what they leave.
 template <int FMT, class Loaded>
 __device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, const typename gt::FactsOf<FMT>::type& f, int c,
-                                        float sl, float nlse, float ndelta, uint32_t (&e)[16], uint32_t (&rest)[16],
-                                        Loaded loaded) {
+                                        float sl, float nlse, float ndelta, Loaded loaded) {
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
   const float2 nl = make_float2(nlse, nlse), nd = make_float2(ndelta, ndelta), sl2 = make_float2(sl, sl);
-  uint32_t s[32];
-  um::ld32(tS, s);
+  uint32_t s[16], r[16], e[16];
+  um::ld16(tS, s);
+  um::ld16(tR, r);
+  loaded();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t r[16];
-    um::ld16(tR + 16u * h, r);
-    if (h) loaded();
+  for (int j = 0; j < 4; ++j) {
+    float4 ks, vs;
+    if constexpr (kQuant) {
+      ks = *reinterpret_cast<const float4*>(&f.ks[c + 4 * j]);
+      vs = *reinterpret_cast<const float4*>(&f.vs[c + 4 * j]);
+    }
 #pragma unroll
-    for (int j = 4 * h; j < 4 * h + 4; ++j) {
-      float4 ks, vs;
+    for (int i = 0; i < 2; ++i) {
+      const int at = 4 * j + 2 * i;
+      float2 x = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
+      float2 y = make_float2(__uint_as_float(r[at]), __uint_as_float(r[at + 1]));
+      const float2 k2 = i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y);
       if constexpr (kQuant) {
-        ks = *reinterpret_cast<const float4*>(&f.ks[32 * c + 4 * j]);
-        vs = *reinterpret_cast<const float4*>(&f.vs[32 * c + 4 * j]);
+        x = ffma2(x, k2, nl);
+        y = ffma2(y, i ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), nd);
+      } else {
+        x = ffma2(x, sl2, nl);
+        y = fadd2(y, nd);
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = 4 * j + 2 * i, ar = at - 16 * h;
-        float2 x = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
-        float2 y = make_float2(__uint_as_float(r[ar]), __uint_as_float(r[ar + 1]));
-        const float2 k2 = i ? make_float2(ks.z, ks.w) : make_float2(ks.x, ks.y);
-        if constexpr (kQuant) {
-          x = ffma2(x, fmul2(k2, sl2), nl);
-          y = ffma2(y, i ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y), nd);
-        } else {
-          x = ffma2(x, sl2, nl);
-          y = fadd2(y, nd);
-        }
-        x.x = um::ex2(x.x);
-        x.y = um::ex2(x.y);
-        x = fmul2(x, y);
-        if constexpr (kQuant) x = fmul2(x, k2);
-        e[2 * j + i] = gt::pack2(x.x, x.y);
-        rest[2 * j + i] = gt::pack2(x.x - bf16lo(e[2 * j + i]), x.y - bf16hi(e[2 * j + i]));
-      }
+      x.x = um::ex2(x.x);
+      x.y = um::ex2(x.y);
+      x = fmul2(x, y);
+      if constexpr (kQuant) x = fmul2(x, k2);
+      // the upper halves as they are, then the upper halves of what that leaves: neither takes a
+      // conversion (2^-15 together, towards 0)
+      y = fadd2(x, make_float2(-__uint_as_float(__float_as_uint(x.x) & 0xffff0000u),
+                               -__uint_as_float(__float_as_uint(x.y) & 0xffff0000u)));
+      e[at / 2] = __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632);
+      e[8 + at / 2] = __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x7632);
     }
   }
-  const uint32_t live = f.live[c];
-  if (live != kFull) {
+  const uint32_t live = f.live[c / 32] >> (c & 31) & 0xffffu;
+  if (live != 0xffffu) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
+    for (int j = 0; j < 8; ++j) {
       const uint32_t keep = (live >> (2 * j) & 1u ? 0xffffu : 0u) | (live >> (2 * j + 1) & 1u ? 0xffff0000u : 0u);
       e[j] &= keep;
-      rest[j] &= keep;
+      e[8 + j] &= keep;
     }
   }
+  um::st16(tS, e);
 }
 
 template <int FMT>
@@ -225,7 +226,7 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
   using M = Misc<FMT>;
   constexpr int kKeys = P::kKeys;
   extern __shared__ __align__(1024) char smem[];
-  const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
+  const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, col = warp >> 2;  // columns 32 col ..
   const int row = quad * 32 + lane;
   const uint32_t at = (uint32_t)(quad * 32) << 16;  // this warp's lanes of tensor memory
   const int rows = min(p.rb, p.rows - blk * p.rb);
@@ -244,10 +245,10 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     for (int a = 0; a < 2; ++a) {
       const Rows& src = a ? p.go : p.q;
       const int c = tid & 15;
-      uint4 v[8];
+      uint4 v[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = (tid >> 4) + 16 * i;
+      for (int i = 0; i < 4; ++i) {
+        const int r = (tid >> 4) + 32 * i;
         v[i] = make_uint4(0u, 0u, 0u, 0u);
         if (r < rows && fabsf(info[r].x) < INFINITY) {
           const int br = blk * p.rb + r, tok = br / p.G, g = br - tok * p.G;
@@ -255,8 +256,8 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
         }
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = (tid >> 4) + 16 * i;
+      for (int i = 0; i < 4; ++i) {
+        const int r = (tid >> 4) + 32 * i;
         sts128(base + (uint32_t)(a * kOperand + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)), v[i].x, v[i].y,
                v[i].z, v[i].w);
       }
@@ -273,18 +274,15 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
       if (!ok) break;
       um::fence_after();
 #pragma unroll 1
-      for (int c = 2 * half; c < 2 * half + 2; ++c) {
-        uint32_t e[16], rest[16];
-        const uint32_t tS = tmem + at + 128u * (t & 1u) + 32u * c;
-        columns<FMT>(tS, tmem + at + kColR + 32u * c, reinterpret_cast<const M*>(smem + P::kMiscOff)->facts[place], c, p.scale_log2, -mine.x, -mine.y, e, rest, [&] {
-          if (c & 1) {  // this warp's half of R has been read
-            um::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(GRAD_AT(r_free));
-          }
+      for (int h = 0; h < 2; ++h) {
+        const int c = 32 * col + 16 * h;
+        columns<FMT>(tmem + at + 128u * (t & 1u) + c, tmem + at + kColR + c,
+                     reinterpret_cast<const M*>(smem + P::kMiscOff)->facts[place], c, p.scale_log2, -mine.x, -mine.y, [&] {
+          if (h == 0) return;
+          um::fence_before();  // this warp's part of R has been read
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(GRAD_AT(r_free));
         });
-        um::st16(tS, e);
-        um::st16(tS + 16u, rest);
       }
       um::wait_st();
       um::fence_before();
@@ -294,17 +292,17 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     if (ok) ok = gt::wait_all(GRAD_AT(o_full), item & 1u, GRAD_AT(abort));
     ++item;
     um::fence_after();
-    float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + 64 * half;
+    float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + 32 * col;
     const bool good = ok && !gt::aborted(GRAD_AT(abort));
+    const float unscale = FMT == CERTKV_STORE_BF16 ? 1.f : 1.f / p.scale_log2;
 #pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < 2; ++c) {
       uint32_t r[16];
-      um::ld16(tmem + at + kColQ + 64u * half + 16u * c, r);
+      um::ld16(tmem + at + kColQ + 32u * col + 16u * c, r);
       if (row < rows) {
-        if (!good) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) r[j] = 0x7fc00000u;
-        }
+        for (int j = 0; j < 16; ++j)
+          r[j] = good ? __float_as_uint(__uint_as_float(r[j]) * unscale) : 0x7fc00000u;
 #pragma unroll
         for (int j = 0; j < 16; j += 8)  // whole sectors
           asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 16 * c + j), "r"(r[j]),
@@ -321,7 +319,9 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
 
 // grid = groups nblk (one CTA per SM), block = kThreads.
 template <int FMT>
-__global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_constant__ GradArgs p) {
+__global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_constant__ CUtensorMap tmK,
+                                                             const __grid_constant__ CUtensorMap tmV,
+                                                             const __grid_constant__ GradArgs p) {
   extern __shared__ __align__(1024) char smem[];
   using P = Plan<FMT>;
   using M = Misc<FMT>;
@@ -338,8 +338,8 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_consta
     }
     tc::mbar_init(GRAD_AT(q_full), kSoftWarps);
     tc::mbar_init(GRAD_AT(s_full), 1);
-    tc::mbar_init(GRAD_AT(r_free), 2 * ((p.rb + 31) / 32));
-    tc::mbar_init(GRAD_AT(p_full), 2 * ((p.rb + 31) / 32));  // the warps with rows
+    tc::mbar_init(GRAD_AT(r_free), 4 * ((p.rb + 31) / 32));
+    tc::mbar_init(GRAD_AT(p_full), 4 * ((p.rb + 31) / 32));  // the warps with rows
     tc::mbar_init(GRAD_AT(o_full), 1);
     tc::mbar_init(GRAD_AT(done), 1);
     gt::sts32(GRAD_AT(abort), 0u);
@@ -363,11 +363,11 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_consta
     gt::registers<kLoadRegs, kLaunchRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
     if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, P::kKeys, false, true> f{p, GRAD_AT(k_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort),
+      gt::Feeder<FMT, P::kKeys, false, true> f{&tmK, p, GRAD_AT(k_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort), GRAD_AT(last),
                                                base + P::kKeyOff, base + P::kStageOff, tid};
       f.run(walk);
     } else {
-      gt::Feeder<FMT, P::kValues, true, false> f{p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort),
+      gt::Feeder<FMT, P::kValues, true, false> f{&tmV, p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort), GRAD_AT(last),
                                                  base + P::kValueOff, base + P::kStageOff + gt::kStage<FMT>,
                                                  tid - kGroupWarps * 32};
       f.run(walk);
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_consta
 }
 
 template <int FMT>
-bool launch(const GradArgs& p, cudaStream_t st) {
+bool launch(const CUtensorMap& mk, const CUtensorMap& mv, const GradArgs& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready{0};  // devices on which the shared memory is opted in to
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return false;
@@ -399,16 +399,19 @@ bool launch(const GradArgs& p, cudaStream_t st) {
       return false;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
-  return launch_kernel(true, grad_q_kernel<FMT>, (unsigned)(p.groups * p.nblk), kThreads, smem_bytes<FMT>(), st, p);
+  return launch_kernel(true, grad_q_kernel<FMT>, (unsigned)(p.groups * p.nblk), kThreads, smem_bytes<FMT>(), st, mk, mv,
+                       p);
 }
 
 }  // namespace
 
 bool launch_grad_q(const GradArgs& p, int format, cudaStream_t st) {
+  CUtensorMap mk = {}, mv = {};
+  if (!gt::pool_maps(p, format, &mk, &mv)) return false;
   TraceScope ts_("grad_q", st);
-  return format == CERTKV_STORE_BF16  ? launch<CERTKV_STORE_BF16>(p, st)
-         : format == CERTKV_STORE_FP8 ? launch<CERTKV_STORE_FP8>(p, st)
-                                      : launch<CERTKV_STORE_FP4>(p, st);
+  return format == CERTKV_STORE_BF16  ? launch<CERTKV_STORE_BF16>(mk, mv, p, st)
+         : format == CERTKV_STORE_FP8 ? launch<CERTKV_STORE_FP8>(mk, mv, p, st)
+                                      : launch<CERTKV_STORE_FP4>(mk, mv, p, st);
 }
 
 }  // namespace certkv

@@ -109,7 +109,7 @@ struct Facts {
 };
 struct alignas(16) ScaledFacts {  // 8- and 4-bit stores
   uint32_t live[4];
-  float ks[kGradTile], vs[kGradTile];  // scales of keys and values
+  float ks[kGradTile], vs[kGradTile];  // scales of keys, times the logits', and of values
 };
 template <int FMT>
 struct FactsOf {
@@ -198,23 +198,26 @@ __device__ __forceinline__ void check(const GradArgs& p, Tile& t, bool raise) {
 
 // A group of four warps that brings the keys, or the values, of every tile into a ring of
 // PLACES operands: rows that are not live as zeros, 8- and 4-bit codes as bf16 without their
-// row's scale.  All reads of memory are asynchronous copies.  A bf16 store's rows go straight
-// to their place, one tile's under way while the one before lands.  Codes go to a stretch of
+// row's scale.  All reads of memory are asynchronous copies.  A bf16 store's whole tiles are bulk
+// copies; its other rows go straight to their place, too, a tile's under way while the one
+// before lands (whole tiles this way took 2000 clocks to ask for).  Codes go to a stretch of
 // shared memory of each thread's own, the next tile's while this one's place is waited for; the
 // loop that expands them is short: straight-line code for a whole tile, with the codes in
 // registers, took the instruction caches of an SM more time than all else (8-bit 395 -> 700 us
 // with two tiles in registers).
 template <int FMT, int PLACES, bool VALUE, bool FACTS>
 struct Feeder {
+  const CUtensorMap* map;  // bf16 stores: of the pool
   using F = typename FactsOf<FMT>::type;
   static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
   // addresses in shared memory: barriers [PLACES], facts [PLACES] (FACTS: written by this group)
   const GradArgs& p;
-  uint32_t full, empty, facts, abort, ring;
+  uint32_t full, empty, facts, abort, last, ring;  // last: a flag that nobody sets
   uint32_t stage;  // kStage<FMT> bytes (8- and 4-bit stores)
   int tid;         // of 128
   uint32_t t = 0;
   bool pending = false;  // a tile's copies have not been handed over
+  uint32_t bulk = 0;     // places whose last tile came by bulk copies
 
   // The fence before the tensor core's reads is the issuer's: here it would wait for every load
   // that is on its way (1200 clocks a tile).
@@ -241,15 +244,41 @@ struct Feeder {
     if ((tid & 31) == 0) sts32(to + 4 * (tid >> 5), word);
     if constexpr (FMT != CERTKV_STORE_BF16) {
       const uint32_t mine = to + (uint32_t)offsetof(ScaledFacts, ks) + 4 * tid;
-      sts32(mine, __float_as_uint(x.ks * kCodeScale<FMT>));
+      sts32(mine, __float_as_uint(x.ks * (kCodeScale<FMT> * p.scale_log2)));
       sts32(mine + 4 * kGradTile, __float_as_uint(x.vs * kCodeScale<FMT>));
     }
   }
   __device__ __forceinline__ bool wait_place() const {
     return wait_all(empty + 8 * (t % PLACES), ((t / PLACES) & 1u) ^ 1u, abort);
   }
+  // A whole tile by four bulk copies, two pages x two 64-element halves.
+  __device__ __forceinline__ bool copy_whole(const Tile& x) {
+    const uint32_t place = t % PLACES, to = ring + place * kOperand;
+    if (pending) {
+      cp_wait<0>();
+      hand_over(t - 1);
+      pending = false;
+    }
+    if (!wait_place()) return false;
+    if constexpr (FACTS) state(place, fact(x));
+    __syncwarp();
+    if (tid == 0) {
+      const uint32_t full_ = full + 8 * place;
+      tc::mbar_expect_tx(full_, kOperand);
+      tc::tma_load_2d(to, map, 0, x.a * kPage, full_);
+      tc::tma_load_2d(to + kHalf, map, 64, x.a * kPage, full_);
+      tc::tma_load_2d(to + kHalf / 2, map, 0, x.b * kPage, full_);
+      tc::tma_load_2d(to + kHalf + kHalf / 2, map, 64, x.b * kPage, full_);
+    } else if ((tid & 31) == 0) {
+      tc::mbar_arrive(full + 8 * place);
+    }
+    bulk = bulk | 1u << place;
+    ++t;
+    return true;
+  }
   __device__ __forceinline__ bool copy(const Tile& x) {
     const uint32_t place = t % PLACES, to = ring + place * kOperand;
+    if (x.a >= 0 && x.b >= 0 && x.live >= kGradTile) return copy_whole(x);
     // what is on its way is not held up by the wait for a place
     if (pending && !__all_sync(kFull, tc::mbar_test(empty + 8 * place, ((t / PLACES) & 1u) ^ 1u))) {
       cp_wait<0>();
@@ -273,6 +302,7 @@ struct Feeder {
       hand_over(t - 1);
     }
     pending = true;
+    bulk &= ~(1u << place);
     ++t;
     return true;
   }
@@ -333,6 +363,9 @@ struct Feeder {
       }
       cp_wait<0>();  // nothing lands after the CTA has gone
       if (ok && pending) hand_over(t - 1);
+      if (tid == 0)
+        for (uint32_t i = t > PLACES ? t - PLACES : 0; i < t; ++i)
+          if (bulk >> (i % PLACES) & 1u) wait(full + 8 * (i % PLACES), (i / PLACES) & 1u, last);
     } else {
       const Piece pc(tid);
       Fact f = {};
@@ -369,6 +402,12 @@ template <int N, int LAUNCH>
 __device__ __forceinline__ void registers() {
   if constexpr (N > LAUNCH) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
   if constexpr (N < LAUNCH) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// The maps of a bf16 store's pools.
+inline bool pool_maps(const GradArgs& p, int format, CUtensorMap* k, CUtensorMap* v) {
+  const uint64_t rows = (uint64_t)p.st.pool_pages * kPage;
+  return format != CERTKV_STORE_BF16 || (make_row_map(k, p.st.k, rows, kPage) && make_row_map(v, p.st.v, rows, kPage));
 }
 
 }  // namespace gt

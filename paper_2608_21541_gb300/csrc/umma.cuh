@@ -343,6 +343,69 @@ __device__ __forceinline__ void mma_p64(uint32_t d, uint32_t a, uint32_t b, uint
       : "memory");
 }
 
+// The eight k-steps of a contraction over 128 slots: A in tensor memory in two parts, 16 slots of
+// the first in 8 columns, of the second in the next 8; B MN-major, 2048 bytes a k-step.
+__device__ __forceinline__ void mma_e2(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc) {
+  asm volatile(
+      "{\n"
+      ".reg .pred pe, p0, po;\n"
+      ".reg .b32 x, y;\n"
+      ".reg .b64 db;\n"
+      "elect.sync _|pe, 0xffffffff;\n"
+      "setp.ne.b32 p0, %5, 0;\n"
+      "setp.ne.b32 po, %4, 0;\n"
+      "add.u32 x, %1, 0;\n"
+      "add.u32 y, %2, 0;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, p0;\n"
+      "add.u32 x, %1, 8;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 16;\n"
+      "add.u32 y, %2, 128;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 24;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 32;\n"
+      "add.u32 y, %2, 256;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 40;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 48;\n"
+      "add.u32 y, %2, 384;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 56;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 64;\n"
+      "add.u32 y, %2, 512;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 72;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 80;\n"
+      "add.u32 y, %2, 640;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 88;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 96;\n"
+      "add.u32 y, %2, 768;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 104;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 112;\n"
+      "add.u32 y, %2, 896;\n"
+      "mov.b64 db, {y, %3};\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "add.u32 x, %1, 120;\n"
+      "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
+      "}\n"
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
+      : "memory");
+}
 // The whole warp calls; the lane that issues the MMAs commits them.
 __device__ __forceinline__ void commit(uint32_t mbar) {
   asm volatile(
