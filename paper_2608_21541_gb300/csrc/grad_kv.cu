@@ -57,6 +57,7 @@ struct Misc {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t b_full[4], b_empty[4];
   uint64_t s_full[2], p_full[2], o_full, drained, done;
+  uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   uint32_t tmem;
   int abort, last;  // last: a flag that nobody sets
   alignas(16) float nlse[Plan<FMT, FUSED>::kBlocks][kCols], ndelta[Plan<FMT, FUSED>::kBlocks][kCols];  // negated
@@ -442,12 +443,14 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
   const int warp = __shfl_sync(kFull, (int)threadIdx.x >> 5, 0);  // so that the compiler, too, knows it uniform
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), gt::kArrivals<FMT>);
       tc::mbar_init(GRAD_AT(k_empty) + 8u * (i), 1);
-      tc::mbar_init(GRAD_AT(v_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(v_full) + 8u * (i), gt::kArrivals<FMT>);
       tc::mbar_init(GRAD_AT(v_empty) + 8u * (i), 1);
       tc::mbar_init(GRAD_AT(s_full) + 8u * (i), 1);
       tc::mbar_init(GRAD_AT(p_full) + 8u * (i), kSoftWarps);
+      tc::mbar_init(GRAD_AT(st_full) + 8u * i, 1);
+      tc::mbar_init(GRAD_AT(st_empty) + 8u * i, kLoadWarps);
     }
     for (int i = 0; i < 4; ++i) {
       tc::mbar_init(GRAD_AT(b_full) + 8u * (i), kRowWarps);
@@ -470,18 +473,23 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
   __syncthreads();
   um::fence_after();
   const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
+  const gt::Stages<FMT> stages = {base + P::kStageOff, GRAD_AT(st_full), GRAD_AT(st_empty)};
   if (warp < kSoftWarps) {
     gt::registers<kSoftRegs, kLaunchRegs>();
     softmax<FMT, FUSED>(p, base, tmem, threadIdx.x, share, walk);
   } else if (warp < kSoftWarps + kLoadWarps) {
     gt::registers<kLoadRegs, kLaunchRegs>();
     const int tid = (int)threadIdx.x - kSoftWarps * 32;
-    if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, P::kKeys, false, false> f{&tmK, p, GRAD_AT(k_full), GRAD_AT(k_empty), 0u, GRAD_AT(abort), GRAD_AT(last), base, base + P::kStageOff, tid};
+    const gt::Ring keys = {GRAD_AT(k_full), GRAD_AT(k_empty), base};
+    const gt::Ring values = {GRAD_AT(v_full), GRAD_AT(v_empty), base + P::kValueOff};
+    if constexpr (FMT != CERTKV_STORE_BF16) {
+      gt::Expander<FMT, P::kKeys, P::kValues, false> f{p, keys, values, stages, 0u, GRAD_AT(abort), tid};
+      f.run(walk);
+    } else if (tid < kGroupWarps * 32) {
+      gt::Copier<P::kKeys, false> f{&tmK, p, keys, 0u, GRAD_AT(abort), GRAD_AT(last), p.st.k, tid};
       f.run(walk);
     } else {
-      gt::Feeder<FMT, P::kValues, true, false> f{&tmV, p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort), GRAD_AT(last),
-                                                 base + P::kValueOff, base + P::kStageOff + gt::kStage<FMT>, tid - kGroupWarps * 32};
+      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), GRAD_AT(last), p.st.v, tid - kGroupWarps * 32};
       f.run(walk);
     }
   } else if (warp < kIssue) {
@@ -494,6 +502,9 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
       is.run(walk);
     } else if (warp <= kIssue + kRowWarps) {
       RowFeeder<FMT, FUSED> f{p, base, (int)threadIdx.x - (kIssue + 1) * 32, (65536u + p.G - 1) / p.G};
+      f.run(walk);
+    } else if (FMT != CERTKV_STORE_BF16 && threadIdx.x % 32 == 0) {
+      gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(last)};
       f.run(walk);
     }
   }

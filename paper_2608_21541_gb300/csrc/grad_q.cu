@@ -5,7 +5,6 @@
 //   S = Q K^T,  R = dO V^T,  e = 2^(S - lse) (R - delta),  dQ += e K,
 // with e handed over in tensor memory, over S, as a bf16 part and one of its remainder (2^-15).  Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so
 // a tile is formed in one pass.
-// A thread takes 32 columns of a row, four warps share a row's.
 // Tensor memory: S of even tiles | S of odd tiles | R | dQ, 128 columns each.  S of the next
 // tile is made while e of this one is, R of the next as soon as R of this one has been read,
 // dQ of this one under e of the next.
@@ -28,13 +27,23 @@
 namespace certkv {
 namespace {
 
-constexpr int kSoftWarps = 16, kLoadWarps = 2 * kGroupWarps;
-constexpr int kThreads = (kSoftWarps + kLoadWarps + 4) * 32;  // whole warpgroups, the issuer's the last
-// Registers a thread: the launch gives 72, which the roles share out among themselves.
-constexpr int kLaunchRegs = 72;
-constexpr int kSoftRegs = 80, kLoadRegs = 64, kIssueRegs = 56;
-static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunchRegs,
-              "a larger split would wait for registers for ever");
+// Warps, whole warpgroups of them: softmax, 64 columns of a row a thread where codes are expanded
+// beside it and 32 else (1024 rows over 32768 slots, bf16: 196 -> 158 us with sixteen; 8-bit
+// trees 204 -> 208, what bounds them there being the instructions of all), loaders, the issuer.
+constexpr int kLoadWarps = 2 * kGroupWarps;
+template <int FMT>
+struct Warps {
+  static constexpr int kSoft = FMT == CERTKV_STORE_BF16 ? 16 : 8, kColumns = 512 / kSoft;
+  static constexpr int kAtOnce = FMT == CERTKV_STORE_BF16 ? 1 : 2;  // times 16 columns in flight, as registers allow
+  static constexpr int kLoad = kSoft, kIssue = kSoft + kLoadWarps, kThreads = (kIssue + 4) * 32;
+  // registers a thread: those of the launch, which the roles share out among themselves
+  static constexpr int kLaunch = FMT == CERTKV_STORE_BF16 ? 72 : 96;
+  static constexpr int kSoftRegs = FMT == CERTKV_STORE_BF16 ? 80 : 104;
+  static constexpr int kLoadRegs = FMT == CERTKV_STORE_BF16 ? 64 : 88;
+  static constexpr int kIssueRegs = FMT == CERTKV_STORE_BF16 ? 56 : 96;
+  static_assert(kSoft * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunch,
+                "a larger split would wait for registers for ever");
+};
 constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
 
 template <int FMT>
@@ -50,6 +59,7 @@ template <int FMT>
 struct Misc {
   uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
   uint64_t q_full, s_full, r_free, p_full, o_full, done;
+  uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   uint32_t tmem;
   int abort, last;  // last: a flag that nobody sets
   alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kKeys];
@@ -62,8 +72,9 @@ static_assert(smem_bytes<CERTKV_STORE_BF16>() <= 232448 && smem_bytes<CERTKV_STO
                   smem_bytes<CERTKV_STORE_FP4>() <= 232448,
               "over the 227 KB of shared memory a CTA can have");
 
+template <int FMT>
 __device__ __forceinline__ void softmax_sync() {
-  asm volatile("bar.sync 1, %0;" ::"n"(kSoftWarps * 32) : "memory");
+  asm volatile("bar.sync 1, %0;" ::"n"(Warps<FMT>::kSoft * 32) : "memory");
 }
 
 // Issues the MMAs of the share's tiles; the whole warp runs, one lane issues.
@@ -89,15 +100,9 @@ struct Issuer {
   static __device__ __forceinline__ bool test(uint32_t mbar, uint32_t phase) {
     return __all_sync(kFull, tc::mbar_test(mbar, phase));
   }
-  // The keys and values of the next tile.
-  __device__ __forceinline__ bool there() const {
-    return test(GRAD_AT(k_full) + 8u * sk.slot, sk.phase) && test(GRAD_AT(v_full) + 8u * rv.slot, rv.phase);
-  }
-  __device__ __forceinline__ void await() {
-    wait(GRAD_AT(k_full) + 8u * sk.slot, sk.phase);
-    wait(GRAD_AT(v_full) + 8u * rv.slot, rv.phase);
-  }
-  // S of tile t, whose keys and values are there, and its R
+  __device__ __forceinline__ void await_keys() { wait(GRAD_AT(k_full) + 8u * sk.slot, sk.phase); }
+  __device__ __forceinline__ void await_values() { wait(GRAD_AT(v_full) + 8u * rv.slot, rv.phase); }
+  // S of tile t, whose keys are there, and its R, whose values are
   __device__ __forceinline__ void s(uint32_t t) {
     if (!ok) return;
     um::fence_async();  // the loaders' writes, before the tensor core's reads
@@ -108,6 +113,7 @@ struct Issuer {
   }
   __device__ __forceinline__ void r() {
     if (!ok) return;
+    um::fence_async();
     um::fence_after();
     um::mma_s(tmem + kColR, um::desc_lo(base + kOperand, 16),
               um::desc_lo(base + P::kValueOff, 16) + rv.slot * (kOperand >> 4), um::kDescHi, um::idesc(true, false));
@@ -122,8 +128,9 @@ struct Issuer {
     while (ok && walk.next(p, &it)) {
       const int n = it.kb - it.ka;
       wait(GRAD_AT(q_full), item++ & 1u);
-      await();
+      await_keys();
       s(t);
+      await_values();
       r();
 #pragma unroll 1
       for (int i = 0; ok && i < n; ++i, ++t) {
@@ -134,11 +141,11 @@ struct Issuer {
         bool has_s = !more, has_r = !more;
 #pragma unroll 1
         for (uint32_t look = 0; ok; ++look) {
-          if (!has_s && there()) {
+          if (!has_s && test(GRAD_AT(k_full) + 8u * sk.slot, sk.phase)) {
             s(t + 1);
             has_s = true;
           }
-          if (has_s && !has_r && test(GRAD_AT(r_free), t & 1u)) {
+          if (has_s && !has_r && test(GRAD_AT(r_free), t & 1u) && test(GRAD_AT(v_full) + 8u * rv.slot, rv.phase)) {
             r();
             has_r = true;
           }
@@ -153,10 +160,13 @@ struct Issuer {
         ++qk;
         if (!more) um::commit(GRAD_AT(o_full));
         if (!has_s) {
-          await();
+          await_keys();
           s(t + 1);
         }
-        if (!has_r) r();
+        if (!has_r) {
+          await_values();
+          r();
+        }
       }
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
@@ -224,9 +234,10 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
                                         gt::Walk walk) {
   using P = Plan<FMT>;
   using M = Misc<FMT>;
+  using W = Warps<FMT>;
   constexpr int kKeys = P::kKeys;
   extern __shared__ __align__(1024) char smem[];
-  const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, col = warp >> 2;  // columns 32 col ..
+  const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, col = (warp >> 2) * W::kColumns;
   const int row = quad * 32 + lane;
   const uint32_t at = (uint32_t)(quad * 32) << 16;  // this warp's lanes of tensor memory
   const int rows = min(p.rb, p.rows - blk * p.rb);
@@ -245,10 +256,11 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     for (int a = 0; a < 2; ++a) {
       const Rows& src = a ? p.go : p.q;
       const int c = tid & 15;
-      uint4 v[4];
+      constexpr int kApart = W::kSoft * 2, kEach = 128 / kApart;
+      uint4 v[kEach];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = (tid >> 4) + 32 * i;
+      for (int i = 0; i < kEach; ++i) {
+        const int r = (tid >> 4) + kApart * i;
         v[i] = make_uint4(0u, 0u, 0u, 0u);
         if (r < rows && fabsf(info[r].x) < INFINITY) {
           const int br = blk * p.rb + r, tok = br / p.G, g = br - tok * p.G;
@@ -256,8 +268,8 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = (tid >> 4) + 32 * i;
+      for (int i = 0; i < kEach; ++i) {
+        const int r = (tid >> 4) + kApart * i;
         sts128(base + (uint32_t)(a * kOperand + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)), v[i].x, v[i].y,
                v[i].z, v[i].w);
       }
@@ -273,12 +285,11 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
            gt::wait_all(GRAD_AT(s_full), t & 1u, GRAD_AT(abort));
       if (!ok) break;
       um::fence_after();
-#pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
-        const int c = 32 * col + 16 * h;
+#pragma unroll W::kAtOnce
+      for (int c = col; c < col + W::kColumns; c += 16) {
         columns<FMT>(tmem + at + 128u * (t & 1u) + c, tmem + at + kColR + c,
                      reinterpret_cast<const M*>(smem + P::kMiscOff)->facts[place], c, p.scale_log2, -mine.x, -mine.y, [&] {
-          if (h == 0) return;
+          if (c + 16 < col + W::kColumns) return;
           um::fence_before();  // this warp's part of R has been read
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(GRAD_AT(r_free));
@@ -292,13 +303,13 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     if (ok) ok = gt::wait_all(GRAD_AT(o_full), item & 1u, GRAD_AT(abort));
     ++item;
     um::fence_after();
-    float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + 32 * col;
+    float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + col;
     const bool good = ok && !gt::aborted(GRAD_AT(abort));
     const float unscale = FMT == CERTKV_STORE_BF16 ? 1.f : 1.f / p.scale_log2;
 #pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < W::kColumns / 16; ++c) {
       uint32_t r[16];
-      um::ld16(tmem + at + kColQ + 32u * col + 16u * c, r);
+      um::ld16(tmem + at + kColQ + col + 16u * c, r);
       if (row < rows) {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -312,34 +323,39 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
       }
     }
     um::fence_before();
-    softmax_sync();  // every warp has read its part of dQ, and nothing reads the rows any more
+    softmax_sync<FMT>();  // every warp has read its part of dQ, and nothing reads the rows any more
     um::fence_after();
   }
 }
 
-// grid = groups nblk (one CTA per SM), block = kThreads.
+// grid = groups nblk (one CTA per SM), block = Warps<FMT>::kThreads.
 template <int FMT>
-__global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_constant__ CUtensorMap tmK,
+__global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const __grid_constant__ CUtensorMap tmK,
                                                              const __grid_constant__ CUtensorMap tmV,
                                                              const __grid_constant__ GradArgs p) {
   extern __shared__ __align__(1024) char smem[];
   using P = Plan<FMT>;
   using M = Misc<FMT>;
+  using W = Warps<FMT>;
   const uint32_t base = tc::saddr(smem);
   const int warp = __shfl_sync(kFull, (int)threadIdx.x >> 5, 0);  // so that the compiler, too, knows it uniform
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
-      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), gt::kArrivals<FMT>);
       tc::mbar_init(GRAD_AT(k_empty) + 8u * (i), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(GRAD_AT(v_full) + 8u * (i), kGroupWarps);
+      tc::mbar_init(GRAD_AT(v_full) + 8u * (i), gt::kArrivals<FMT>);
       tc::mbar_init(GRAD_AT(v_empty) + 8u * (i), 1);
     }
-    tc::mbar_init(GRAD_AT(q_full), kSoftWarps);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(GRAD_AT(st_full) + 8u * i, 1);
+      tc::mbar_init(GRAD_AT(st_empty) + 8u * i, kLoadWarps);
+    }
+    tc::mbar_init(GRAD_AT(q_full), W::kSoft);
     tc::mbar_init(GRAD_AT(s_full), 1);
-    tc::mbar_init(GRAD_AT(r_free), 4 * ((p.rb + 31) / 32));
-    tc::mbar_init(GRAD_AT(p_full), 4 * ((p.rb + 31) / 32));  // the warps with rows
+    tc::mbar_init(GRAD_AT(r_free), W::kSoft / 4 * ((p.rb + 31) / 32));
+    tc::mbar_init(GRAD_AT(p_full), W::kSoft / 4 * ((p.rb + 31) / 32));  // the warps with rows
     tc::mbar_init(GRAD_AT(o_full), 1);
     tc::mbar_init(GRAD_AT(done), 1);
     gt::sts32(GRAD_AT(abort), 0u);
@@ -351,38 +367,44 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const __grid_consta
   const int share = blockIdx.x / p.nblk, blk = blockIdx.x - share * p.nblk;
   const gt::Walk walk = gt::Walk::of(p, share);
   if (walk.left == 0) return;  // uniform, before any barrier
-  if (warp == kSoftWarps + kLoadWarps) um::alloc(GRAD_AT(tmem), 512);
+  if (warp == W::kIssue) um::alloc(GRAD_AT(tmem), 512);
   um::fence_before();
   __syncthreads();
   um::fence_after();
   const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
-  if (warp < kSoftWarps) {
-    gt::registers<kSoftRegs, kLaunchRegs>();
+  const gt::Stages<FMT> stages = {base + P::kStageOff, GRAD_AT(st_full), GRAD_AT(st_empty)};
+  if (warp < W::kSoft) {
+    gt::registers<W::kSoftRegs, W::kLaunch>();
     softmax<FMT>(p, base, tmem, threadIdx.x, share, blk, walk);
-  } else if (warp < kSoftWarps + kLoadWarps) {
-    gt::registers<kLoadRegs, kLaunchRegs>();
-    const int tid = (int)threadIdx.x - kSoftWarps * 32;
-    if (tid < kGroupWarps * 32) {
-      gt::Feeder<FMT, P::kKeys, false, true> f{&tmK, p, GRAD_AT(k_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort), GRAD_AT(last),
-                                               base + P::kKeyOff, base + P::kStageOff, tid};
+  } else if (warp < W::kIssue) {
+    gt::registers<W::kLoadRegs, W::kLaunch>();
+    const int tid = (int)threadIdx.x - W::kLoad * 32;
+    const gt::Ring keys = {GRAD_AT(k_full), GRAD_AT(k_empty), base + P::kKeyOff};
+    const gt::Ring values = {GRAD_AT(v_full), GRAD_AT(v_empty), base + P::kValueOff};
+    if constexpr (FMT != CERTKV_STORE_BF16) {
+      gt::Expander<FMT, P::kKeys, P::kValues, true> f{p, keys, values, stages, GRAD_AT(facts), GRAD_AT(abort), tid};
+      f.run(walk);
+    } else if (tid < kGroupWarps * 32) {
+      gt::Copier<P::kKeys, true> f{&tmK, p, keys, GRAD_AT(facts), GRAD_AT(abort), GRAD_AT(last), p.st.k, tid};
       f.run(walk);
     } else {
-      gt::Feeder<FMT, P::kValues, true, false> f{&tmV, p, GRAD_AT(v_full), GRAD_AT(v_empty), 0u, GRAD_AT(abort), GRAD_AT(last),
-                                                 base + P::kValueOff, base + P::kStageOff + gt::kStage<FMT>,
-                                                 tid - kGroupWarps * 32};
+      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), GRAD_AT(last), p.st.v, tid - kGroupWarps * 32};
       f.run(walk);
     }
   } else {
-    gt::registers<kIssueRegs, kLaunchRegs>();
-    if (warp == kSoftWarps + kLoadWarps) {
+    gt::registers<W::kIssueRegs, W::kLaunch>();
+    if (warp == W::kIssue) {
       Issuer<FMT> is{tmem, base};
       is.run(p, walk);
+    } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 1 && threadIdx.x % 32 == 0) {
+      gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(last)};
+      f.run(walk);
     }
   }
   um::fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && p.st.status && gt::aborted(GRAD_AT(abort))) atomicOr(p.st.status, CERTKV_STATUS_TIMEOUT);
-  if (warp == kSoftWarps + kLoadWarps) {
+  if (warp == W::kIssue) {
     um::fence_after();
     um::dealloc(tmem, 512);
   }
@@ -399,7 +421,7 @@ bool launch(const CUtensorMap& mk, const CUtensorMap& mv, const GradArgs& p, cud
       return false;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
-  return launch_kernel(true, grad_q_kernel<FMT>, (unsigned)(p.groups * p.nblk), kThreads, smem_bytes<FMT>(), st, mk, mv,
+  return launch_kernel(true, grad_q_kernel<FMT>, (unsigned)(p.groups * p.nblk), Warps<FMT>::kThreads, smem_bytes<FMT>(), st, mk, mv,
                        p);
 }
 

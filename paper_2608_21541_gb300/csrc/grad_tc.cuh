@@ -154,10 +154,6 @@ __device__ __forceinline__ void codes_to_bf16(const uint32_t (&c)[2], uint32_t g
 __device__ __forceinline__ void cp16(uint32_t to, const void* from, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
 }
-template <int N>
-__device__ __forceinline__ void cp_small(uint32_t to, const void* from, bool on) {  // 4 or 8 bytes
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(N), "r"(on ? N : 0) : "memory");
-}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {
@@ -196,25 +192,33 @@ __device__ __forceinline__ void check(const GradArgs& p, Tile& t, bool raise) {
   if (!b) t.b = -1;
 }
 
-// A group of four warps that brings the keys, or the values, of every tile into a ring of
-// PLACES operands: rows that are not live as zeros, 8- and 4-bit codes as bf16 without their
-// row's scale.  All reads of memory are asynchronous copies.  A bf16 store's whole tiles are bulk
-// copies; its other rows go straight to their place, too, a tile's under way while the one
-// before lands (whole tiles this way took 2000 clocks to ask for).  Codes go to a stretch of
-// shared memory of each thread's own, the next tile's while this one's place is waited for; the
-// loop that expands them is short: straight-line code for a whole tile, with the codes in
-// registers, took the instruction caches of an SM more time than all else (8-bit 395 -> 700 us
-// with two tiles in registers).
-template <int FMT, int PLACES, bool VALUE, bool FACTS>
-struct Feeder {
-  const CUtensorMap* map;  // bf16 stores: of the pool
-  using F = typename FactsOf<FMT>::type;
-  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
-  // addresses in shared memory: barriers [PLACES], facts [PLACES] (FACTS: written by this group)
+constexpr int kLoadThreads = 2 * kGroupWarps * 32;  // of the loaders
+// Bytes of the loaders' stretches for the keys, or the values, of a tile.
+template <int FMT>
+constexpr int kStage = FMT == CERTKV_STORE_BF16 ? 0 : 128 * (row_bytes(FMT) + (FMT == CERTKV_STORE_FP4 ? kGroups : 0));
+
+// Warps that hand an operand over.
+template <int FMT>
+constexpr int kArrivals = FMT == CERTKV_STORE_BF16 ? kGroupWarps : 2 * kGroupWarps;
+
+// Where the loaders put a tile's keys or values: a ring of operands, and its barriers; addresses
+// in shared memory.
+struct Ring {
+  uint32_t full, empty, at;
+};
+
+// A bf16 store: two groups of four warps, one for the keys and one for the values, bring every
+// tile into a ring of PLACES operands, rows that are not live as zeros.  Whole tiles are bulk
+// copies; other rows are copied 16 bytes at a time, a tile's on their way while the one before
+// lands (whole tiles this way took 2000 clocks to ask for).
+template <int PLACES, bool FACTS>
+struct Copier {
+  const CUtensorMap* map;
   const GradArgs& p;
-  uint32_t full, empty, facts, abort, last, ring;  // last: a flag that nobody sets
-  uint32_t stage;  // kStage<FMT> bytes (8- and 4-bit stores)
-  int tid;         // of 128
+  Ring ring;
+  uint32_t facts, abort, last;  // facts [PLACES] (FACTS: written by this group); last: a flag that nobody sets
+  const uint8_t* rows;
+  int tid;               // of 128
   uint32_t t = 0;
   bool pending = false;  // a tile's copies have not been handed over
   uint32_t bulk = 0;     // places whose last tile came by bulk copies
@@ -223,70 +227,49 @@ struct Feeder {
   // that is on its way (1200 clocks a tile).
   __device__ __forceinline__ void hand_over(uint32_t tile) const {
     __syncwarp();
-    if ((tid & 31) == 0) tc::mbar_arrive(full + 8 * (tile % PLACES));
+    if ((tid & 31) == 0) tc::mbar_arrive(ring.full + 8 * (tile % PLACES));
   }
-  // Slot tid's facts: asked for, and stated once the place is free.
-  struct Fact {
-    bool on;
-    float ks, vs;
-  };
-  __device__ __forceinline__ Fact fact(const Tile& x) const {
-    const int pg = tid < kPage ? x.a : x.b;
-    Fact f = {pg >= 0 && tid < x.live, 0.f, 0.f};
-    if (FMT != CERTKV_STORE_BF16 && f.on) {
-      f.ks = __ldg(p.st.ks + (int64_t)pg * kPage + (tid & (kPage - 1)));
-      f.vs = __ldg(p.st.vs + (int64_t)pg * kPage + (tid & (kPage - 1)));
-    }
-    return f;
-  }
-  __device__ __forceinline__ void state(uint32_t place, const Fact& x) const {
-    const uint32_t to = facts + place * (uint32_t)sizeof(F), word = __ballot_sync(kFull, x.on);
-    if ((tid & 31) == 0) sts32(to + 4 * (tid >> 5), word);
-    if constexpr (FMT != CERTKV_STORE_BF16) {
-      const uint32_t mine = to + (uint32_t)offsetof(ScaledFacts, ks) + 4 * tid;
-      sts32(mine, __float_as_uint(x.ks * (kCodeScale<FMT> * p.scale_log2)));
-      sts32(mine + 4 * kGradTile, __float_as_uint(x.vs * kCodeScale<FMT>));
-    }
+  __device__ __forceinline__ void state(uint32_t place, const Tile& x) const {
+    const uint32_t word = __ballot_sync(kFull, (tid < kPage ? x.a : x.b) >= 0 && tid < x.live);
+    if ((tid & 31) == 0) sts32(facts + place * (uint32_t)sizeof(Facts) + 4 * (tid >> 5), word);
   }
   __device__ __forceinline__ bool wait_place() const {
-    return wait_all(empty + 8 * (t % PLACES), ((t / PLACES) & 1u) ^ 1u, abort);
+    return wait_all(ring.empty + 8 * (t % PLACES), ((t / PLACES) & 1u) ^ 1u, abort);
   }
   // A whole tile by four bulk copies, two pages x two 64-element halves.
   __device__ __forceinline__ bool copy_whole(const Tile& x) {
-    const uint32_t place = t % PLACES, to = ring + place * kOperand;
+    const uint32_t place = t % PLACES, to = ring.at + place * kOperand, full = ring.full + 8 * place;
     if (pending) {
       cp_wait<0>();
       hand_over(t - 1);
       pending = false;
     }
     if (!wait_place()) return false;
-    if constexpr (FACTS) state(place, fact(x));
+    if constexpr (FACTS) state(place, x);
     __syncwarp();
     if (tid == 0) {
-      const uint32_t full_ = full + 8 * place;
-      tc::mbar_expect_tx(full_, kOperand);
-      tc::tma_load_2d(to, map, 0, x.a * kPage, full_);
-      tc::tma_load_2d(to + kHalf, map, 64, x.a * kPage, full_);
-      tc::tma_load_2d(to + kHalf / 2, map, 0, x.b * kPage, full_);
-      tc::tma_load_2d(to + kHalf + kHalf / 2, map, 64, x.b * kPage, full_);
+      tc::mbar_expect_tx(full, kOperand);
+      tc::tma_load_2d(to, map, 0, x.a * kPage, full);
+      tc::tma_load_2d(to + kHalf, map, 64, x.a * kPage, full);
+      tc::tma_load_2d(to + kHalf / 2, map, 0, x.b * kPage, full);
+      tc::tma_load_2d(to + kHalf + kHalf / 2, map, 64, x.b * kPage, full);
     } else if ((tid & 31) == 0) {
-      tc::mbar_arrive(full + 8 * place);
+      tc::mbar_arrive(full);
     }
-    bulk = bulk | 1u << place;
+    bulk |= 1u << place;
     ++t;
     return true;
   }
   __device__ __forceinline__ bool copy(const Tile& x) {
-    const uint32_t place = t % PLACES, to = ring + place * kOperand;
+    const uint32_t place = t % PLACES, to = ring.at + place * kOperand;
     if (x.a >= 0 && x.b >= 0 && x.live >= kGradTile) return copy_whole(x);
     // what is on its way is not held up by the wait for a place
-    if (pending && !__all_sync(kFull, tc::mbar_test(empty + 8 * place, ((t / PLACES) & 1u) ^ 1u))) {
+    if (pending && !__all_sync(kFull, tc::mbar_test(ring.empty + 8 * place, ((t / PLACES) & 1u) ^ 1u))) {
       cp_wait<0>();
       hand_over(t - 1);
       pending = false;
     }
     if (!wait_place()) return false;
-    const uint8_t* rows = VALUE ? p.st.v : p.st.k;
     const int c = tid & 15, r0 = tid >> 4;  // 16 lanes a row, 16 bytes each
 #pragma unroll 4
     for (int i = 0; i < 16; ++i) {
@@ -296,7 +279,7 @@ struct Feeder {
            rows + (on ? ((int64_t)pg * kPage + (r & (kPage - 1))) * 256 + c * 16 : 0), on);
     }
     cp_commit();
-    if constexpr (FACTS) state(place, fact(x));
+    if constexpr (FACTS) state(place, x);
     if (pending) {
       cp_wait<1>();
       hand_over(t - 1);
@@ -306,96 +289,185 @@ struct Feeder {
     ++t;
     return true;
   }
-  // This thread's pieces of tile x (checked), on their way into its stretch of memory: piece q at
-  // 16 or 8 (128 q + tid), of four bits the word with its group scale behind them.
-  __device__ __forceinline__ void ask(const Piece& pc, const Tile& x) const {
-    const uint8_t *codes = VALUE ? p.st.v : p.st.k, *group = VALUE ? p.st.vg : p.st.kg;
-#pragma unroll 2
-    for (int q = 0; q < kPieces; ++q) {
-      const int pg = q < kPieces / 2 ? x.a : x.b, row = pc.grp + kStep * (q % (kPieces / 2));
-      const bool on = pg >= 0 && pc.grp + kStep * q < x.live;
-      const int64_t at = on ? (int64_t)pg * kPage + row : 0;
-      if constexpr (FMT == CERTKV_STORE_FP8) {
-        cp16(stage + 16 * (128 * q + tid), codes + at * 128 + pc.sub * 16, on);
-      } else {
-        cp_small<8>(stage + 8 * (128 * q + tid), codes + at * 64 + pc.sub * 8, on);
-        cp_small<4>(stage + 8 * 128 * kPieces + 4 * (128 * q + tid), group + at * kGroups + (pc.sub & 4), on);
-      }
-    }
-    cp_commit();
-  }
-  // Piece q of them.
-  __device__ __forceinline__ void piece(int q, uint32_t (&c)[kWords], uint32_t& g) const {
-    if constexpr (FMT == CERTKV_STORE_FP8) {
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
-                   : "r"(stage + 16 * (128 * q + tid)));
-    } else {
-      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(stage + 8 * (128 * q + tid)));
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(g) : "r"(stage + 8 * 128 * kPieces + 4 * (128 * q + tid)));
-    }
-  }
-  __device__ __forceinline__ void expand(const Piece& pc, uint32_t to) const {
-    uint32_t c[2][kWords], g[2] = {0u, 0u};
-    piece(0, c[0], g[0]);
+  __device__ __forceinline__ void run(const Walk& walk) {
+    Tiles tiles(p, walk);
+    Tile x, y;  // the next tile's pages are looked up a tile before
+    bool ok = true, more = tiles.next(&x);
 #pragma unroll 1
-    for (int q = 0; q < kPieces; q += 2)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {  // the next piece is on its way while this one is expanded
-        uint32_t w[8];
-        piece(min(q + i + 1, kPieces - 1), c[i ^ 1], g[i ^ 1]);
-        codes_to_bf16(c[i], g[i] >> (8 * (pc.sub & 3)) & 255u, w);
-        pc.put(to, q + i, w);
-      }
+    while (ok && more) {
+      more = tiles.next(&y);
+      check(p, x, tid == 0);
+      ok = copy(x);
+      x = y;
+    }
+    cp_wait<0>();  // nothing lands after the CTA has gone
+    if (ok && pending) hand_over(t - 1);
+    if (tid == 0)
+      for (uint32_t i = t > PLACES ? t - PLACES : 0; i < t; ++i)
+        if (bulk >> (i % PLACES) & 1u) wait(ring.full + 8 * (i % PLACES), (i / PLACES) & 1u, last);
+  }
+};
+
+// 8- and 4-bit stores: the codes of a tile's values and of its keys on their way into a stretch of
+// shared memory each, page by page, by one lane's bulk copies; eight warps expand them into the
+// rings' operands, rows that are not live as zeros, codes as bf16 without their row's scale.  All
+// eight at one operand, since the keys' way from a free place to the next product is what a tile
+// waits for; its values first, whose place is free long before.  The loop that expands is short:
+// straight-line code for a whole tile, with the codes in registers, took the instruction caches
+// of an SM more time than all else (8-bit 395 -> 700 us with two tiles in registers).  Codes
+// copied 16 bytes at a time by the expanding warps took them 1400 clocks a tile to ask for.
+template <int FMT>
+struct Stages {
+  static constexpr uint32_t kPageCodes = kPage * row_bytes(FMT), kPageGroups = FMT == CERTKV_STORE_FP4 ? kPage * kGroups : 0;
+  uint32_t at;           // of the keys' stretch; kStage<FMT> bytes on that of the values
+  uint32_t full, empty;  // barriers, of keys and of values
+};
+
+template <int FMT>
+struct Stager {
+  using S = Stages<FMT>;
+  const GradArgs& p;
+  S st;
+  uint32_t abort, last;
+
+  __device__ __forceinline__ void page(int pg, int half, bool value) const {
+    if (pg < 0) return;
+    const uint32_t to = st.at + (value ? kStage<FMT> : 0u), full = st.full + 8 * value;
+    tc::bulk_load(to + half * S::kPageCodes, (value ? p.st.v : p.st.k) + (int64_t)pg * S::kPageCodes, S::kPageCodes, full);
+    if (FMT == CERTKV_STORE_FP4)
+      tc::bulk_load(to + 2 * S::kPageCodes + half * S::kPageGroups,
+                    (value ? p.st.vg : p.st.kg) + (int64_t)pg * S::kPageGroups, S::kPageGroups, full);
   }
   __device__ __forceinline__ void run(const Walk& walk) {
     Tiles tiles(p, walk);
-    Tile x, y;  // x: the next tile to be asked for; its pages are looked up a tile before
-    bool more = tiles.next(&x);
-    if constexpr (FMT == CERTKV_STORE_BF16) {
-      bool ok = true;
+    Tile x, y;
+    uint32_t t = 0;
+    bool ok = true, more = tiles.next(&x);
 #pragma unroll 1
-      while (ok && more) {
-        more = tiles.next(&y);
-        check(p, x, tid == 0);
-        ok = copy(x);
-        x = y;
+    for (; ok && more; ++t) {
+      more = tiles.next(&y);
+      check(p, x, false);
+#pragma unroll 1
+      for (int value = 1; ok && value >= 0; --value) {
+        ok = wait(st.empty + 8 * value, (t & 1u) ^ 1u, abort);
+        if (!ok) break;
+        const uint32_t bytes = ((x.a >= 0) + (x.b >= 0)) * (S::kPageCodes + S::kPageGroups);
+        tc::mbar_expect_tx(st.full + 8 * value, bytes);
+        page(x.a, 0, value);
+        page(x.b, 1, value);
       }
-      cp_wait<0>();  // nothing lands after the CTA has gone
-      if (ok && pending) hand_over(t - 1);
-      if (tid == 0)
-        for (uint32_t i = t > PLACES ? t - PLACES : 0; i < t; ++i)
-          if (bulk >> (i % PLACES) & 1u) wait(full + 8 * (i % PLACES), (i / PLACES) & 1u, last);
+      x = y;
+    }
+    // nothing lands after the CTA has gone
+    if (ok && t > 0)
+      for (int value = 0; value < 2; ++value) wait(st.full + 8 * value, (t - 1) & 1u, last);
+    if (!ok)
+      for (int i = 0; i < 4; ++i) wait(st.full + 8 * (i & 1), i >> 1, last);
+  }
+};
+
+template <int FMT, int KEYS, int VALUES, bool FACTS>
+struct Expander {
+  using S = Stages<FMT>;
+  static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
+  static constexpr int kMine = 128 * 8 / kLoadThreads, kApart = 128 / kMine;  // a thread's pieces, rows apart
+  const GradArgs& p;
+  Ring keys, values;
+  S st;
+  uint32_t facts, abort;  // facts [KEYS] (FACTS)
+  int tid;                // of 256
+  uint32_t t = 0;
+
+  // Slot tid's facts: asked for, and stated once the place is free.
+  struct Fact {
+    bool on;
+    float ks, vs;
+  };
+  __device__ __forceinline__ Fact fact(const Tile& x) const {
+    const int pg = tid < kPage ? x.a : x.b;
+    Fact f = {tid < kGradTile && pg >= 0 && tid < x.live, 0.f, 0.f};
+    if (f.on) {
+      f.ks = __ldg(p.st.ks + (int64_t)pg * kPage + (tid & (kPage - 1)));
+      f.vs = __ldg(p.st.vs + (int64_t)pg * kPage + (tid & (kPage - 1)));
+    }
+    return f;
+  }
+  __device__ __forceinline__ void state(uint32_t place, const Fact& x) const {
+    if (tid >= kGradTile) return;
+    const uint32_t to = facts + place * (uint32_t)sizeof(ScaledFacts), word = __ballot_sync(kFull, x.on);
+    if ((tid & 31) == 0) sts32(to + 4 * (tid >> 5), word);
+    const uint32_t mine = to + (uint32_t)offsetof(ScaledFacts, ks) + 4 * tid;
+    sts32(mine, __float_as_uint(x.ks * (kCodeScale<FMT> * p.scale_log2)));
+    sts32(mine + 4 * kGradTile, __float_as_uint(x.vs * kCodeScale<FMT>));
+  }
+  // Codes 16 sub .. of row r of a stretch, of four bits the word with their group's scale too.
+  __device__ __forceinline__ void piece(uint32_t from, int r, int sub, uint32_t (&c)[kWords], uint32_t& g) const {
+    if constexpr (FMT == CERTKV_STORE_FP8) {
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
+                   : "r"(from + 128 * r + 16 * sub));
     } else {
-      const Piece pc(tid);
-      Fact f = {};
-      bool asked = false;
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(from + 64 * r + 8 * sub));
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(g) : "r"(from + 2 * S::kPageCodes + 8 * r + (sub & 4)));
+    }
+  }
+  // A staged operand of tile x into place `n` of a ring, handed over.
+  __device__ __forceinline__ bool expand(const Piece& pc, const Tile& x, const Ring& ring, uint32_t n, int value) const {
+    if (!wait_all(st.full + 8 * value, t & 1u, abort)) return false;
+    const uint32_t from = st.at + (value ? kStage<FMT> : 0u), to = ring.at + n * kOperand;
+    uint32_t c[2][kWords], g[2] = {0u, 0u};
+    piece(from, pc.grp, pc.sub, c[0], g[0]);
 #pragma unroll 1
-      while (true) {
-        if (asked) {
-          if (!wait_place()) break;
-          cp_wait<0>();
-          const uint32_t place = t % PLACES;
-          if constexpr (FACTS) state(place, f);
-          expand(pc, ring + place * kOperand);
-          hand_over(t);
-          ++t;
+    for (int q = 0; q < kMine; q += 2)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // the next piece is on its way while this one is expanded
+        uint32_t w[8];
+        const int r = pc.grp + kApart * (q + i);
+        piece(from, min(r + kApart, 127), pc.sub, c[i ^ 1], g[i ^ 1]);
+        codes_to_bf16(c[i], g[i] >> (8 * (pc.sub & 3)) & 255u, w);
+        if ((q < kMine / 2 ? x.a : x.b) < 0 || r >= x.live) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = 0u;
         }
-        asked = more;
-        if (!more) break;
-        Tile now = x;
-        check(p, now, tid == 0);
-        more = tiles.next(&x);
-        if (FACTS) f = fact(now);
-        ask(pc, now);
+        const uint32_t row = to + (uint32_t)((q + i) * kApart * 128);
+        sts128(row + pc.at0, w[0], w[1], w[2], w[3]);
+        sts128(row + pc.at1, w[4], w[5], w[6], w[7]);
       }
-      cp_wait<0>();
+    __syncwarp();
+    if ((tid & 31) == 0) {
+      tc::mbar_arrive(ring.full + 8 * n);
+      tc::mbar_arrive(st.empty + 8 * value);
+    }
+    return true;
+  }
+  template <int PLACES>
+  __device__ __forceinline__ bool wait_place(const Ring& ring) const {
+    return wait_all(ring.empty + 8 * (t % PLACES), ((t / PLACES) & 1u) ^ 1u, abort);
+  }
+  __device__ __forceinline__ void run(const Walk& walk) {
+    Tiles tiles(p, walk);
+    Tile x, y;  // x: this tile, checked; y: the next, whose pages are looked up a tile before
+    const Piece pc(tid);
+    bool more = tiles.next(&x), next = more && tiles.next(&y);
+    if (!more) return;
+    check(p, x, tid == 0);
+    Fact f = FACTS ? fact(x) : Fact{};
+#pragma unroll 1
+    while (more) {
+      if (!wait_place<VALUES>(values) || !expand(pc, x, values, t % VALUES, 1)) break;
+      if (!wait_place<KEYS>(keys)) break;
+      if constexpr (FACTS) state(t % KEYS, f);
+      if (!expand(pc, x, keys, t % KEYS, 0)) break;
+      ++t;
+      more = next;
+      if (!more) break;
+      x = y;
+      check(p, x, tid == 0);
+      next = tiles.next(&y);
+      if (FACTS) f = fact(x);
     }
   }
 };
-// Bytes of a group's stretches.
-template <int FMT>
-constexpr int kStage = FMT == CERTKV_STORE_BF16 ? 0 : FMT == CERTKV_STORE_FP8 ? 128 * 128 : 128 * 96;
 
 // A warpgroup's registers, from those of the launch up or down; the launch's must cover all.
 template <int N, int LAUNCH>
