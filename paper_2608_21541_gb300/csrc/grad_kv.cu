@@ -58,6 +58,7 @@ struct Misc {
   uint64_t b_full[4], b_empty[4];
   uint64_t s_full[2], p_full[2], o_full, drained, done;
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
+  int2 live[2];  // of the stretches
   uint32_t tmem;
   int abort, last;  // last: a flag that nobody sets
   alignas(16) float nlse[Plan<FMT, FUSED>::kBlocks][kCols], ndelta[Plan<FMT, FUSED>::kBlocks][kCols];  // negated
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
   __syncthreads();
   um::fence_after();
   const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
-  const gt::Stages<FMT> stages = {base + P::kStageOff, GRAD_AT(st_full), GRAD_AT(st_empty)};
+  const gt::Stages<FMT> stages = {base + P::kStageOff, GRAD_AT(st_full), GRAD_AT(st_empty), GRAD_AT(live)};
   if (warp < kSoftWarps) {
     gt::registers<kSoftRegs, kLaunchRegs>();
     softmax<FMT, FUSED>(p, base, tmem, threadIdx.x, share, walk);
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
     const gt::Ring keys = {GRAD_AT(k_full), GRAD_AT(k_empty), base};
     const gt::Ring values = {GRAD_AT(v_full), GRAD_AT(v_empty), base + P::kValueOff};
     if constexpr (FMT != CERTKV_STORE_BF16) {
-      gt::Expander<FMT, P::kKeys, P::kValues, false> f{p, keys, values, stages, 0u, GRAD_AT(abort), tid};
+      gt::Expander<FMT, P::kKeys, P::kValues> f{keys, values, stages, GRAD_AT(abort), tid};
       f.run(walk);
     } else if (tid < kGroupWarps * 32) {
       gt::Copier<P::kKeys, false> f{&tmK, p, keys, 0u, GRAD_AT(abort), GRAD_AT(last), p.st.k, tid};

@@ -60,6 +60,7 @@ struct Misc {
   uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
   uint64_t q_full, s_full, r_free, p_full, o_full, done;
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
+  int2 live[2];  // of the stretches
   uint32_t tmem;
   int abort, last;  // last: a flag that nobody sets
   alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kKeys];
@@ -341,7 +342,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
   const int warp = __shfl_sync(kFull, (int)threadIdx.x >> 5, 0);  // so that the compiler, too, knows it uniform
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
-      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), gt::kArrivals<FMT>);
+      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), gt::kArrivals<FMT> + (FMT == CERTKV_STORE_BF16 ? 0 : 1));
       tc::mbar_init(GRAD_AT(k_empty) + 8u * (i), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
   __syncthreads();
   um::fence_after();
   const uint32_t tmem = gt::lds32(GRAD_AT(tmem));
-  const gt::Stages<FMT> stages = {base + P::kStageOff, GRAD_AT(st_full), GRAD_AT(st_empty)};
+  const gt::Stages<FMT> stages = {base + P::kStageOff, GRAD_AT(st_full), GRAD_AT(st_empty), GRAD_AT(live)};
   if (warp < W::kSoft) {
     gt::registers<W::kSoftRegs, W::kLaunch>();
     softmax<FMT>(p, base, tmem, threadIdx.x, share, blk, walk);
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
     const gt::Ring keys = {GRAD_AT(k_full), GRAD_AT(k_empty), base + P::kKeyOff};
     const gt::Ring values = {GRAD_AT(v_full), GRAD_AT(v_empty), base + P::kValueOff};
     if constexpr (FMT != CERTKV_STORE_BF16) {
-      gt::Expander<FMT, P::kKeys, P::kValues, true> f{p, keys, values, stages, GRAD_AT(facts), GRAD_AT(abort), tid};
+      gt::Expander<FMT, P::kKeys, P::kValues> f{keys, values, stages, GRAD_AT(abort), tid};
       f.run(walk);
     } else if (tid < kGroupWarps * 32) {
       gt::Copier<P::kKeys, true> f{&tmK, p, keys, GRAD_AT(facts), GRAD_AT(abort), GRAD_AT(last), p.st.k, tid};
@@ -398,6 +399,10 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       is.run(p, walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 1 && threadIdx.x % 32 == 0) {
       gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(last)};
+      f.run(walk);
+    } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 2) {
+      const gt::Ring keys = {GRAD_AT(k_full), GRAD_AT(k_empty), base + P::kKeyOff};
+      gt::FactFeeder<FMT, P::kKeys> f{p, keys, GRAD_AT(facts), GRAD_AT(abort), (int)threadIdx.x & 31};
       f.run(walk);
     }
   }

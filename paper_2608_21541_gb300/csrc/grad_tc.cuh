@@ -192,6 +192,11 @@ __device__ __forceinline__ void check(const GradArgs& p, Tile& t, bool raise) {
   if (!b) t.b = -1;
 }
 
+// Live rows of a tile's page 0 or 1.
+__device__ __forceinline__ int live_rows(const Tile& t, int half) {
+  return (half ? t.b : t.a) < 0 ? 0 : max(min(t.live - kPage * half, kPage), 0);
+}
+
 constexpr int kLoadThreads = 2 * kGroupWarps * 32;  // of the loaders
 // Bytes of the loaders' stretches for the keys, or the values, of a tile.
 template <int FMT>
@@ -321,6 +326,7 @@ struct Stages {
   static constexpr uint32_t kPageCodes = kPage * row_bytes(FMT), kPageGroups = FMT == CERTKV_STORE_FP4 ? kPage * kGroups : 0;
   uint32_t at;           // of the keys' stretch; kStage<FMT> bytes on that of the values
   uint32_t full, empty;  // barriers, of keys and of values
+  uint32_t live;         // of either, live rows of each page (int2)
 };
 
 template <int FMT>
@@ -346,13 +352,14 @@ struct Stager {
 #pragma unroll 1
     for (; ok && more; ++t) {
       more = tiles.next(&y);
-      check(p, x, false);
+      check(p, x, true);
 #pragma unroll 1
       for (int value = 1; ok && value >= 0; --value) {
         ok = wait(st.empty + 8 * value, (t & 1u) ^ 1u, abort);
         if (!ok) break;
-        const uint32_t bytes = ((x.a >= 0) + (x.b >= 0)) * (S::kPageCodes + S::kPageGroups);
-        tc::mbar_expect_tx(st.full + 8 * value, bytes);
+        sts32(st.live + 8 * value, live_rows(x, 0));
+        sts32(st.live + 8 * value + 4, live_rows(x, 1));
+        tc::mbar_expect_tx(st.full + 8 * value, ((x.a >= 0) + (x.b >= 0)) * (S::kPageCodes + S::kPageGroups));
         page(x.a, 0, value);
         page(x.b, 1, value);
       }
@@ -366,40 +373,59 @@ struct Stager {
   }
 };
 
-template <int FMT, int KEYS, int VALUES, bool FACTS>
+// A warp that states the facts of a tile's slots in the keys' ring: its loads' latency is
+// nobody else's (the expanding warps waited 1000 clocks a tile for them).
+template <int FMT, int KEYS>
+struct FactFeeder {
+  const GradArgs& p;
+  Ring keys;
+  uint32_t facts, abort;  // facts [KEYS]
+  int lane;
+
+  __device__ __forceinline__ void put(uint32_t to, float4 x, float f) const {
+    sts128(to + 16 * lane, __float_as_uint(x.x * f), __float_as_uint(x.y * f), __float_as_uint(x.z * f),
+           __float_as_uint(x.w * f));
+  }
+  __device__ __forceinline__ void run(const Walk& walk) {
+    Tiles tiles(p, walk);
+    Tile x, y;
+    uint32_t t = 0;
+    bool ok = true, more = tiles.next(&x);
+#pragma unroll 1
+    for (; ok && more; ++t) {
+      more = tiles.next(&y);
+      check(p, x, false);
+      const int pg = lane < 16 ? x.a : x.b;
+      float4 ks = {0.f, 0.f, 0.f, 0.f}, vs = ks;
+      if (pg >= 0) {  // of four slots a lane; what is not live is masked
+        ks = __ldg(reinterpret_cast<const float4*>(p.st.ks + (int64_t)pg * kPage) + (lane & 15));
+        vs = __ldg(reinterpret_cast<const float4*>(p.st.vs + (int64_t)pg * kPage) + (lane & 15));
+      }
+      const uint32_t place = t % KEYS, to = facts + place * (uint32_t)sizeof(ScaledFacts);
+      ok = wait_all(keys.empty + 8 * place, ((t / KEYS) & 1u) ^ 1u, abort);
+      if (lane < 4) {
+        const int n = max(live_rows(x, lane >> 1) - 32 * (lane & 1), 0);
+        sts32(to + 4 * lane, n >= 32 ? kFull : (1u << n) - 1u);
+      }
+      put(to + (uint32_t)offsetof(ScaledFacts, ks), ks, kCodeScale<FMT> * p.scale_log2);
+      put(to + (uint32_t)offsetof(ScaledFacts, vs), vs, kCodeScale<FMT>);
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(keys.full + 8 * place);
+      x = y;
+    }
+  }
+};
+
+template <int FMT, int KEYS, int VALUES>
 struct Expander {
   using S = Stages<FMT>;
   static constexpr int kWords = FMT == CERTKV_STORE_FP8 ? 4 : 2;
   static constexpr int kMine = 128 * 8 / kLoadThreads, kApart = 128 / kMine;  // a thread's pieces, rows apart
-  const GradArgs& p;
   Ring keys, values;
   S st;
-  uint32_t facts, abort;  // facts [KEYS] (FACTS)
-  int tid;                // of 256
-  uint32_t t = 0;
+  uint32_t abort;
+  int tid;  // of 256
 
-  // Slot tid's facts: asked for, and stated once the place is free.
-  struct Fact {
-    bool on;
-    float ks, vs;
-  };
-  __device__ __forceinline__ Fact fact(const Tile& x) const {
-    const int pg = tid < kPage ? x.a : x.b;
-    Fact f = {tid < kGradTile && pg >= 0 && tid < x.live, 0.f, 0.f};
-    if (f.on) {
-      f.ks = __ldg(p.st.ks + (int64_t)pg * kPage + (tid & (kPage - 1)));
-      f.vs = __ldg(p.st.vs + (int64_t)pg * kPage + (tid & (kPage - 1)));
-    }
-    return f;
-  }
-  __device__ __forceinline__ void state(uint32_t place, const Fact& x) const {
-    if (tid >= kGradTile) return;
-    const uint32_t to = facts + place * (uint32_t)sizeof(ScaledFacts), word = __ballot_sync(kFull, x.on);
-    if ((tid & 31) == 0) sts32(to + 4 * (tid >> 5), word);
-    const uint32_t mine = to + (uint32_t)offsetof(ScaledFacts, ks) + 4 * tid;
-    sts32(mine, __float_as_uint(x.ks * (kCodeScale<FMT> * p.scale_log2)));
-    sts32(mine + 4 * kGradTile, __float_as_uint(x.vs * kCodeScale<FMT>));
-  }
   // Codes 16 sub .. of row r of a stretch, of four bits the word with their group's scale too.
   __device__ __forceinline__ void piece(uint32_t from, int r, int sub, uint32_t (&c)[kWords], uint32_t& g) const {
     if constexpr (FMT == CERTKV_STORE_FP8) {
@@ -411,10 +437,11 @@ struct Expander {
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(g) : "r"(from + 2 * S::kPageCodes + 8 * r + (sub & 4)));
     }
   }
-  // A staged operand of tile x into place `n` of a ring, handed over.
-  __device__ __forceinline__ bool expand(const Piece& pc, const Tile& x, const Ring& ring, uint32_t n, int value) const {
-    if (!wait_all(st.full + 8 * value, t & 1u, abort)) return false;
+  // The staged operand of tile t into place `n` of a ring, handed over.
+  __device__ __forceinline__ bool expand(const Piece& pc, uint32_t t, const Ring& ring, uint32_t n, int value) const {
+    if (!wait_all(ring.empty + 8 * n, ((value ? t / VALUES : t / KEYS) & 1u) ^ 1u, abort) || !wait_all(st.full + 8 * value, t & 1u, abort)) return false;
     const uint32_t from = st.at + (value ? kStage<FMT> : 0u), to = ring.at + n * kOperand;
+    const int la = (int)lds32(st.live + 8 * value), lb = kPage + (int)lds32(st.live + 8 * value + 4);
     uint32_t c[2][kWords], g[2] = {0u, 0u};
     piece(from, pc.grp, pc.sub, c[0], g[0]);
 #pragma unroll 1
@@ -425,7 +452,7 @@ struct Expander {
         const int r = pc.grp + kApart * (q + i);
         piece(from, min(r + kApart, 127), pc.sub, c[i ^ 1], g[i ^ 1]);
         codes_to_bf16(c[i], g[i] >> (8 * (pc.sub & 3)) & 255u, w);
-        if ((q < kMine / 2 ? x.a : x.b) < 0 || r >= x.live) {
+        if (r >= (q < kMine / 2 ? la : lb)) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) w[j] = 0u;
         }
@@ -440,32 +467,11 @@ struct Expander {
     }
     return true;
   }
-  template <int PLACES>
-  __device__ __forceinline__ bool wait_place(const Ring& ring) const {
-    return wait_all(ring.empty + 8 * (t % PLACES), ((t / PLACES) & 1u) ^ 1u, abort);
-  }
-  __device__ __forceinline__ void run(const Walk& walk) {
-    Tiles tiles(p, walk);
-    Tile x, y;  // x: this tile, checked; y: the next, whose pages are looked up a tile before
+  __device__ __forceinline__ void run(const Walk& walk) const {
     const Piece pc(tid);
-    bool more = tiles.next(&x), next = more && tiles.next(&y);
-    if (!more) return;
-    check(p, x, tid == 0);
-    Fact f = FACTS ? fact(x) : Fact{};
 #pragma unroll 1
-    while (more) {
-      if (!wait_place<VALUES>(values) || !expand(pc, x, values, t % VALUES, 1)) break;
-      if (!wait_place<KEYS>(keys)) break;
-      if constexpr (FACTS) state(t % KEYS, f);
-      if (!expand(pc, x, keys, t % KEYS, 0)) break;
-      ++t;
-      more = next;
-      if (!more) break;
-      x = y;
-      check(p, x, tid == 0);
-      next = tiles.next(&y);
-      if (FACTS) f = fact(x);
-    }
+    for (uint32_t t = 0; t < (uint32_t)walk.left; ++t)
+      if (!expand(pc, t, values, t % VALUES, 1) || !expand(pc, t, keys, t % KEYS, 0)) break;
   }
 };
 
