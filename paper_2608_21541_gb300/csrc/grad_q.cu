@@ -48,8 +48,11 @@ constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
 
 template <int FMT>
 struct Plan {
-  static constexpr int kKeys = FMT == CERTKV_STORE_BF16 ? 3 : 2;  // places of the rings
-  static constexpr int kValues = 2;
+  // Places of the rings.  The keys' are held from S of a tile to its dQ, the values' for R alone
+  // (8- and 4-bit stores: 2 + 2 places PLACES22 us, 3 + 1 PLACES31 us, 1024 rows over 13107 slots).
+  static constexpr int kKeys = 3;
+  static constexpr int kValues = FMT == CERTKV_STORE_BF16 ? 2 : 1;
+  static constexpr int kFacts = FMT == CERTKV_STORE_BF16 ? kKeys : 2;  // bf16: the copying warps state them
   static constexpr int kKeyOff = 2 * kOperand;  // behind the rows and their gradients
   static constexpr int kValueOff = kKeyOff + kKeys * kOperand;
   static constexpr int kStageOff = kValueOff + kValues * kOperand;  // of keys, then of values
@@ -59,11 +62,12 @@ template <int FMT>
 struct Misc {
   uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
   uint64_t q_full, s_full, r_free, p_full, o_full, done;
+  uint64_t f_full[2];                // facts (8- and 4-bit stores)
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   int2 live[2];  // of the stretches
   uint32_t tmem;
   int abort, last;  // last: a flag that nobody sets
-  alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kKeys];
+  alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kFacts];
 };
 template <int FMT>
 constexpr int smem_bytes() {
@@ -236,7 +240,6 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
   using P = Plan<FMT>;
   using M = Misc<FMT>;
   using W = Warps<FMT>;
-  constexpr int kKeys = P::kKeys;
   extern __shared__ __align__(1024) char smem[];
   const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, col = (warp >> 2) * W::kColumns;
   const int row = quad * 32 + lane;
@@ -281,8 +284,9 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     if (lane == 0) tc::mbar_arrive(GRAD_AT(q_full));
 #pragma unroll 1
     for (int k = now.ka; ok && busy && k < now.kb; ++k, ++t) {
-      const uint32_t place = t % kKeys;
-      ok = gt::wait_all(GRAD_AT(k_full) + 8u * place, (t / kKeys) & 1u, GRAD_AT(abort)) &&
+      const uint32_t place = t % P::kFacts;
+      ok = gt::wait_all((FMT == CERTKV_STORE_BF16 ? GRAD_AT(k_full) : GRAD_AT(f_full)) + 8u * place,
+                        (t / P::kFacts) & 1u, GRAD_AT(abort)) &&
            gt::wait_all(GRAD_AT(s_full), t & 1u, GRAD_AT(abort));
       if (!ok) break;
       um::fence_after();
@@ -342,7 +346,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
   const int warp = __shfl_sync(kFull, (int)threadIdx.x >> 5, 0);  // so that the compiler, too, knows it uniform
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
-      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), gt::kArrivals<FMT> + (FMT == CERTKV_STORE_BF16 ? 0 : 1));
+      tc::mbar_init(GRAD_AT(k_full) + 8u * (i), gt::kArrivals<FMT>);
       tc::mbar_init(GRAD_AT(k_empty) + 8u * (i), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -350,6 +354,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       tc::mbar_init(GRAD_AT(v_empty) + 8u * (i), 1);
     }
     for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(GRAD_AT(f_full) + 8u * i, 1);
       tc::mbar_init(GRAD_AT(st_full) + 8u * i, 1);
       tc::mbar_init(GRAD_AT(st_empty) + 8u * i, kLoadWarps);
     }
@@ -401,8 +406,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(last)};
       f.run(walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 2) {
-      const gt::Ring keys = {GRAD_AT(k_full), GRAD_AT(k_empty), base + P::kKeyOff};
-      gt::FactFeeder<FMT, P::kKeys> f{p, keys, GRAD_AT(facts), GRAD_AT(abort), (int)threadIdx.x & 31};
+      gt::FactFeeder<FMT, P::kKeys> f{p, GRAD_AT(f_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort), (int)threadIdx.x & 31};
       f.run(walk);
     }
   }

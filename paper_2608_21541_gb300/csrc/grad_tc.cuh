@@ -316,8 +316,8 @@ struct Copier {
 // 8- and 4-bit stores: the codes of a tile's values and of its keys on their way into a stretch of
 // shared memory each, page by page, by one lane's bulk copies; eight warps expand them into the
 // rings' operands, rows that are not live as zeros, codes as bf16 without their row's scale.  All
-// eight at one operand, since the keys' way from a free place to the next product is what a tile
-// waits for; its values first, whose place is free long before.  The loop that expands is short:
+// eight at one operand, since the way from a free place to the next product is what a tile
+// waits for; the keys a tile ahead of the values, whose products come later.  The loop that expands is short:
 // straight-line code for a whole tile, with the codes in registers, took the instruction caches
 // of an SM more time than all else (8-bit 395 -> 700 us with two tiles in registers).  Codes
 // copied 16 bytes at a time by the expanding warps took them 1400 clocks a tile to ask for.
@@ -336,6 +336,7 @@ struct Stager {
   S st;
   uint32_t abort, last;
 
+  // Codes of operand `value` of tile number t on their way.
   __device__ __forceinline__ void page(int pg, int half, bool value) const {
     if (pg < 0) return;
     const uint32_t to = st.at + (value ? kStage<FMT> : 0u), full = st.full + 8 * value;
@@ -344,42 +345,47 @@ struct Stager {
       tc::bulk_load(to + 2 * S::kPageCodes + half * S::kPageGroups,
                     (value ? p.st.vg : p.st.kg) + (int64_t)pg * S::kPageGroups, S::kPageGroups, full);
   }
-  __device__ __forceinline__ void run(const Walk& walk) {
+  __device__ __forceinline__ bool stage(const Tile& x, uint32_t t, bool value) const {
+    if (!wait(st.empty + 8 * value, (t & 1u) ^ 1u, abort)) return false;
+    sts32(st.live + 8 * value, live_rows(x, 0));
+    sts32(st.live + 8 * value + 4, live_rows(x, 1));
+    tc::mbar_expect_tx(st.full + 8 * value, ((x.a >= 0) + (x.b >= 0)) * (S::kPageCodes + S::kPageGroups));
+    page(x.a, 0, value);
+    page(x.b, 1, value);
+    return true;
+  }
+  __device__ __forceinline__ void run(const Walk& walk) const {
     Tiles tiles(p, walk);
-    Tile x, y;
-    uint32_t t = 0;
-    bool ok = true, more = tiles.next(&x);
+    Tile x, y;  // x: whose values are next, checked; y: whose keys are
+    uint32_t keys = 0, values = 0;  // staged
+    bool more = tiles.next(&x);
+    check(p, x, true);
+    bool ok = stage(x, keys++, false);
 #pragma unroll 1
-    for (; ok && more; ++t) {
+    while (ok && more) {
       more = tiles.next(&y);
-      check(p, x, true);
-#pragma unroll 1
-      for (int value = 1; ok && value >= 0; --value) {
-        ok = wait(st.empty + 8 * value, (t & 1u) ^ 1u, abort);
-        if (!ok) break;
-        sts32(st.live + 8 * value, live_rows(x, 0));
-        sts32(st.live + 8 * value + 4, live_rows(x, 1));
-        tc::mbar_expect_tx(st.full + 8 * value, ((x.a >= 0) + (x.b >= 0)) * (S::kPageCodes + S::kPageGroups));
-        page(x.a, 0, value);
-        page(x.b, 1, value);
-      }
+      ok = stage(x, values, true);
+      values += ok;
+      if (!ok || !more) break;
+      check(p, y, true);
+      ok = stage(y, keys, false);
+      keys += ok;
       x = y;
     }
     // nothing lands after the CTA has gone
-    if (ok && t > 0)
-      for (int value = 0; value < 2; ++value) wait(st.full + 8 * value, (t - 1) & 1u, last);
-    if (!ok)
-      for (int i = 0; i < 4; ++i) wait(st.full + 8 * (i & 1), i >> 1, last);
+    if (keys > 0) wait(st.full, (keys - 1) & 1u, last);
+    if (values > 0) wait(st.full + 8, (values - 1) & 1u, last);
   }
 };
 
-// A warp that states the facts of a tile's slots in the keys' ring: its loads' latency is
-// nobody else's (the expanding warps waited 1000 clocks a tile for them).
+// A warp that states the facts of the tiles' slots in two places of their own: its loads'
+// latency is nobody else's (the expanding warps waited 1000 clocks a tile for them).  A place is
+// free when the tile before last has given back its keys.
 template <int FMT, int KEYS>
 struct FactFeeder {
   const GradArgs& p;
-  Ring keys;
-  uint32_t facts, abort;  // facts [KEYS]
+  uint32_t full, empty;   // barriers, of the facts [2] and of the keys [KEYS]
+  uint32_t facts, abort;  // facts [2]
   int lane;
 
   __device__ __forceinline__ void put(uint32_t to, float4 x, float f) const {
@@ -401,8 +407,8 @@ struct FactFeeder {
         ks = __ldg(reinterpret_cast<const float4*>(p.st.ks + (int64_t)pg * kPage) + (lane & 15));
         vs = __ldg(reinterpret_cast<const float4*>(p.st.vs + (int64_t)pg * kPage) + (lane & 15));
       }
-      const uint32_t place = t % KEYS, to = facts + place * (uint32_t)sizeof(ScaledFacts);
-      ok = wait_all(keys.empty + 8 * place, ((t / KEYS) & 1u) ^ 1u, abort);
+      const uint32_t to = facts + (t & 1u) * (uint32_t)sizeof(ScaledFacts);
+      if (t >= 2) ok = wait_all(empty + 8 * ((t - 2) % KEYS), ((t - 2) / KEYS) & 1u, abort);
       if (lane < 4) {
         const int n = max(live_rows(x, lane >> 1) - 32 * (lane & 1), 0);
         sts32(to + 4 * lane, n >= 32 ? kFull : (1u << n) - 1u);
@@ -410,7 +416,7 @@ struct FactFeeder {
       put(to + (uint32_t)offsetof(ScaledFacts, ks), ks, kCodeScale<FMT> * p.scale_log2);
       put(to + (uint32_t)offsetof(ScaledFacts, vs), vs, kCodeScale<FMT>);
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(keys.full + 8 * place);
+      if (lane == 0) tc::mbar_arrive(full + 8 * (t & 1u));
       x = y;
     }
   }
@@ -470,8 +476,11 @@ struct Expander {
   __device__ __forceinline__ void run(const Walk& walk) const {
     const Piece pc(tid);
 #pragma unroll 1
-    for (uint32_t t = 0; t < (uint32_t)walk.left; ++t)
-      if (!expand(pc, t, values, t % VALUES, 1) || !expand(pc, t, keys, t % KEYS, 0)) break;
+    for (uint32_t t = 0, n = walk.left; t < n; ++t) {
+      if (t == 0 && !expand(pc, 0, keys, 0, 0)) break;
+      if (!expand(pc, t, values, t % VALUES, 1)) break;
+      if (t + 1 < n && !expand(pc, t + 1, keys, (t + 1) % KEYS, 0)) break;
+    }
   }
 };
 
