@@ -267,17 +267,22 @@ struct Issuer {
   }
 };
 
-// The slot of a softmax thread.
+// The slot of a softmax thread.  Its table entry is looked up a tile before its scales, and these
+// a tile before they are used, so that neither load is waited for.
 template <int FMT>
 struct Slot {
-  int at;            // of the pool, -1: none
-  float ks, vs;      // scales of its key and value
-  __device__ __forceinline__ void load(const GradArgs& p, int u, int s, int count) {
-    at = s < count ? (int)p.st.slot(u, s) : -1;  // pools have fewer than 2^31 slots
-    ks = vs = gt::kCodeScale<FMT>;
-    if (FMT != CERTKV_STORE_BF16 && at >= 0) {
-      ks *= __ldg(p.st.ks + at);
-      vs *= __ldg(p.st.vs + at);
+  bool live;
+  float ks, vs;  // scales of its key and value
+  static __device__ __forceinline__ int entry(const GradArgs& p, int u, int s, int count) {
+    return s < count ? __ldg(p.st.table + (int64_t)u * p.st.max_pages + s / kPage) : -1;
+  }
+  __device__ __forceinline__ void load(const GradArgs& p, int page, int s) {
+    live = page >= 0 && page < p.st.pool_pages;
+    ks = vs = 1.f;
+    if (FMT != CERTKV_STORE_BF16 && live) {
+      const int64_t at = (int64_t)page * kPage + s % kPage;
+      ks = __ldg(p.st.ks + at);
+      vs = __ldg(p.st.vs + at);
     }
   }
 };
@@ -307,14 +312,20 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     const gt::Item now = it;
     const int count = p.st.count(now.u);
     Slot<FMT> next;
-    next.load(p, now.u, now.ka * kGradTile + row, count);
+    int page = Slot<FMT>::entry(p, now.u, now.ka * kGradTile + row, count);
+    if (kQuant) {
+      next.load(p, page, row);
+      page = Slot<FMT>::entry(p, now.u, (now.ka + 1) * kGradTile + row, count);
+    }
 #pragma unroll 1
     for (int k = now.ka; k < now.kb; ++k, ++t) {
-      const Slot<FMT> slot = next;
-      if (k + 1 < now.kb) next.load(p, now.u, (k + 1) * kGradTile + row, count);
-      const bool live = slot.at >= 0;
-      const float2 ksl = make_float2(slot.ks * p.scale_log2, slot.ks * p.scale_log2);
-      const float2 vs = make_float2(slot.vs, slot.vs), ks = make_float2(slot.ks, slot.ks);
+      Slot<FMT> slot = next;
+      (kQuant ? next : slot).load(p, page, row);
+      page = Slot<FMT>::entry(p, now.u, (k + 1 + kQuant) * kGradTile + row, count);
+      const bool live = slot.live;
+      const float key = slot.ks * gt::kCodeScale<FMT>, value = slot.vs * gt::kCodeScale<FMT>;
+      const float2 ksl = make_float2(key * p.scale_log2, key * p.scale_log2);
+      const float2 vs = make_float2(value, value), ks = make_float2(key, key);
 #pragma unroll 1
       for (int j = 0; ok && j < blocks; ++j, ++i) {
         const uint32_t x = FUSED ? 0u : i & 1u, use = FUSED ? i : i >> 1, blk = FUSED ? item : i;
@@ -403,16 +414,21 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
       um::fence_after();
       const bool good = ok && !gt::aborted(GRAD_AT(abort));
 #pragma unroll 1
-      for (int c = 0; c < 16; ++c) {
-        const bool key = c >= 8;
-        const int d0 = 16 * (c & 7);
-        uint32_t r[16], w[8];
-        um::ld16(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
+      for (int c = 0; c < 8; ++c) {
+        const bool key = c >= 4;
+        const int d0 = 32 * (c & 3);
+        uint32_t r[32];
+        um::ld32(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
         const float f = key ? p.scale : 1.f;
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          w[q] = good ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : 0x7fc07fc0u;
-        if (slot >= 0) store_sector((key ? p.dks : p.dvs) + slot * kD + d0, w);
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            w[q] = good ? gt::pack2(__uint_as_float(r[16 * h + 2 * q]) * f, __uint_as_float(r[16 * h + 2 * q + 1]) * f)
+                        : 0x7fc07fc0u;
+          if (slot >= 0) store_sector((key ? p.dks : p.dvs) + slot * kD + d0 + 16 * h, w);
+        }
       }
       if (FUSED && p.dq.p && k + 1 == now.kb) {  // element tid of every row
         float* out = p.rec + grad_record(p, share, now.u, 0) * kD + tid;

@@ -443,43 +443,37 @@ struct Expander {
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(g) : "r"(from + 2 * S::kPageCodes + 8 * r + (sub & 4)));
     }
   }
-  // The staged operand of tile t into place `n` of a ring, handed over.
-  __device__ __forceinline__ bool expand(const Piece& pc, uint32_t t, const Ring& ring, uint32_t n, int value) const {
-    if (!wait_all(ring.empty + 8 * n, ((value ? t / VALUES : t / KEYS) & 1u) ^ 1u, abort) || !wait_all(st.full + 8 * value, t & 1u, abort)) return false;
-    const uint32_t from = st.at + (value ? kStage<FMT> : 0u), to = ring.at + n * kOperand;
-    const int la = (int)lds32(st.live + 8 * value), lb = kPage + (int)lds32(st.live + 8 * value + 4);
-    uint32_t c[2][kWords], g[2] = {0u, 0u};
-    piece(from, pc.grp, pc.sub, c[0], g[0]);
-#pragma unroll 1
-    for (int q = 0; q < kMine; q += 2)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {  // the next piece is on its way while this one is expanded
-        uint32_t w[8];
-        const int r = pc.grp + kApart * (q + i);
-        piece(from, min(r + kApart, 127), pc.sub, c[i ^ 1], g[i ^ 1]);
-        codes_to_bf16(c[i], g[i] >> (8 * (pc.sub & 3)) & 255u, w);
-        if (r >= (q < kMine / 2 ? la : lb)) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = 0u;
-        }
-        const uint32_t row = to + (uint32_t)((q + i) * kApart * 128);
-        sts128(row + pc.at0, w[0], w[1], w[2], w[3]);
-        sts128(row + pc.at1, w[4], w[5], w[6], w[7]);
-      }
-    __syncwarp();
-    if ((tid & 31) == 0) {
-      tc::mbar_arrive(ring.full + 8 * n);
-      tc::mbar_arrive(st.empty + 8 * value);
-    }
-    return true;
-  }
+  // All operands one after the other, the keys of a tile and then its values.  A thread's codes
+  // are read at once, and their stretch given back, before the place that they go to is waited for.
   __device__ __forceinline__ void run(const Walk& walk) const {
     const Piece pc(tid);
 #pragma unroll 1
-    for (uint32_t t = 0, n = walk.left; t < n; ++t) {
-      if (t == 0 && !expand(pc, 0, keys, 0, 0)) break;
-      if (!expand(pc, t, values, t % VALUES, 1)) break;
-      if (t + 1 < n && !expand(pc, t + 1, keys, (t + 1) % KEYS, 0)) break;
+    for (uint32_t i = 0, n = 2 * (uint32_t)walk.left; i < n; ++i) {
+      const uint32_t t = i >> 1, value = i & 1u, place = value ? t % VALUES : t % KEYS;
+      const Ring& ring = value ? values : keys;
+      const uint32_t from = st.at + value * kStage<FMT>, to = ring.at + place * kOperand;
+      if (!wait_all(st.full + 8 * value, t & 1u, abort)) break;
+      const int la = (int)lds32(st.live + 8 * value), lb = kPage + (int)lds32(st.live + 8 * value + 4);
+      uint32_t c[kMine][kWords], g[kMine];
+#pragma unroll
+      for (int q = 0; q < kMine; ++q) piece(from, pc.grp + kApart * q, pc.sub, c[q], g[q]);
+      __syncwarp();
+      if ((tid & 31) == 0) tc::mbar_arrive(st.empty + 8 * value);
+      if (!wait_all(ring.empty + 8 * place, ((value ? t / VALUES : t / KEYS) & 1u) ^ 1u, abort)) break;
+#pragma unroll
+      for (int q = 0; q < kMine; ++q) {
+        uint32_t w[8];
+        codes_to_bf16(c[q], g[q] >> (8 * (pc.sub & 3)) & 255u, w);
+        if (pc.grp + kApart * q >= (q < kMine / 2 ? la : lb)) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = 0u;
+        }
+        const uint32_t row = to + (uint32_t)(q * kApart * 128);
+        sts128(row + pc.at0, w[0], w[1], w[2], w[3]);
+        sts128(row + pc.at1, w[4], w[5], w[6], w[7]);
+      }
+      __syncwarp();
+      if ((tid & 31) == 0) tc::mbar_arrive(ring.full + 8 * place);
     }
   }
 };
