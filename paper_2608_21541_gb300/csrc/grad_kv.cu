@@ -45,12 +45,17 @@ constexpr uint32_t kColV = 256, kColK = 384, kColQ = 128;  // S of block i: colu
 template <int FMT, bool FUSED>
 struct Plan {
   static constexpr int kKeys = FUSED ? 2 : 1, kValues = FUSED ? 2 : 1;  // places of the rings
-  static constexpr int kBlocks = !FUSED ? 4 : FMT == CERTKV_STORE_BF16 ? 2 : 1;
+  static constexpr int kBlocks = FUSED ? (FMT == CERTKV_STORE_BF16 ? 2 : 1) : FMT == CERTKV_STORE_BF16 ? 4 : 3;
   static constexpr int kValueOff = kKeys * kOperand;
   static constexpr int kBlockOff = kValueOff + kValues * kOperand;
   static constexpr int kEOff = kBlockOff + kBlocks * kBlock;  // e, FUSED: [128 slots][64 rows]
   static constexpr int kStageOff = kEOff + (FUSED ? kHalf : 0);  // of keys, then of values
-  static constexpr int kMiscOff = kStageOff + 2 * gt::kStage<FMT>;
+  // Slots' gradients are written by sectors where the store's bytes bound the pass, and else by
+  // lines through shared memory, half a row of 32 slots a warp (64 rows over 32768 slots, bf16:
+  // 508 us by sectors, 540 by lines; over 13107 slots, 8 bits: 606 and 572).
+  static constexpr bool kLines = !FUSED || FMT != CERTKV_STORE_BF16;
+  static constexpr int kDrainOff = kStageOff + 2 * gt::kStage<FMT>;
+  static constexpr int kMiscOff = kDrainOff + (kLines ? kDrainWarps * 4096 : 0);
 };
 template <int FMT, bool FUSED>
 struct Misc {
@@ -303,7 +308,7 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
   const int warp = tid >> 5, lane = tid & 31, quad = warp & 3, half = warp >> 2;
   const int row = quad * 32 + lane;  // slot of the tile
   const uint32_t at = (uint32_t)(quad * 32) << 16;
-  const int blocks = blocks_of(p);
+  const int blocks = FUSED ? 1 : blocks_of(p);
   uint32_t i = 0, t = 0, item = 0;
   bool ok = true;
   gt::Item it;
@@ -399,6 +404,7 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
   using M = Misc<FMT, FUSED>;
   const int lane = tid & 31, quad = tid >> 5;
   const uint32_t at = (uint32_t)(quad * 32) << 16;
+  const uint32_t mine = base + P::kDrainOff + (uint32_t)quad * 4096u;
   uint32_t t = 0;
   bool ok = true;
   gt::Item it;
@@ -408,26 +414,56 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
     const int count = p.st.count(now.u);
 #pragma unroll 1
     for (int k = now.ka; k < now.kb; ++k, ++t) {
-      const int s = k * kGradTile + tid;
-      const int64_t slot = s < count ? p.st.slot(now.u, s) : -1;
+      // a warp's slots are half a page's
+      const int s = k * kGradTile + quad * 32;
+      const int page = s < count ? __ldg(p.st.table + (int64_t)now.u * p.st.max_pages + s / kPage) : -1;
       ok = ok && gt::wait_all(GRAD_AT(o_full), t & 1u, GRAD_AT(abort));
       um::fence_after();
       const bool good = ok && !gt::aborted(GRAD_AT(abort));
+      const int rows = page >= 0 && page < p.st.pool_pages ? min(count - s, 32) : 0;
+      const int64_t first = ((int64_t)page * kPage + s % kPage) * kD;
+      if constexpr (P::kLines) {
 #pragma unroll 1
-      for (int c = 0; c < 8; ++c) {
-        const bool key = c >= 4;
-        const int d0 = 32 * (c & 3);
-        uint32_t r[32];
-        um::ld32(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
-        const float f = key ? p.scale : 1.f;
+        for (int c = 0; c < 4; ++c) {  // half a row of dV or dK: written by slot, read by line
+          const bool key = c >= 2;
+          const int d0 = 64 * (c & 1);
+          const float f = key ? p.scale : 1.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[8];
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[32];
+            um::ld32(tmem + at + (key ? kColK : kColV) + (uint32_t)(d0 + 32 * h), r);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              uint32_t w[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                w[q] = good ? gt::pack2(__uint_as_float(r[8 * x + 2 * q]) * f, __uint_as_float(r[8 * x + 2 * q + 1]) * f)
+                            : 0x7fc07fc0u;
+              sts128(mine + (uint32_t)(lane * 128 + (((4 * h + x) ^ (lane & 7)) << 4)), w[0], w[1], w[2], w[3]);
+            }
+          }
+          __syncwarp();
+          uint16_t* out = (key ? p.dks : p.dvs) + first + d0 + 8 * (lane & 7);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const int row = 4 * x + (lane >> 3);
+            const float4 v = gt::lds128(mine + (uint32_t)(row * 128 + (((lane & 7) ^ (row & 7)) << 4)));
+            if (row < rows) *reinterpret_cast<float4*>(out + row * kD) = v;
+          }
+          __syncwarp();
+        }
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < 16; ++c) {  // a sector of a slot a thread
+          const bool key = c >= 8;
+          const int d0 = 16 * (c & 7);
+          uint32_t r[16], w[8];
+          um::ld16(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
+          const float f = key ? p.scale : 1.f;
 #pragma unroll
           for (int q = 0; q < 8; ++q)
-            w[q] = good ? gt::pack2(__uint_as_float(r[16 * h + 2 * q]) * f, __uint_as_float(r[16 * h + 2 * q + 1]) * f)
-                        : 0x7fc07fc0u;
-          if (slot >= 0) store_sector((key ? p.dks : p.dvs) + slot * kD + d0 + 16 * h, w);
+            w[q] = good ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : 0x7fc07fc0u;
+          if (lane < rows) store_sector((key ? p.dks : p.dvs) + first + lane * kD + d0, w);
         }
       }
       if (FUSED && p.dq.p && k + 1 == now.kb) {  // element tid of every row
