@@ -13,9 +13,11 @@
 // What a row does not see cannot reach it, nor the row that, though matrix products sum over all
 // rows and drafts of a tile: rows that take no part enter them as zeros with probability 0, and
 // rows or keys with a NaN or infinity as zeros too, with the probabilities of what sees them NaN.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "../../include/certkv.h"
 #include "common.cuh"
@@ -446,9 +448,14 @@ template <int TD>
 bool launch_drafts(const GradArgs& p, cudaStream_t st) {
   constexpr int bytes = Drafts<TD>::kBytes;
   static_assert(bytes <= 232448, "over the 227 KB of shared memory a CTA can have");
-  if (bytes > 48 * 1024 &&
-      cudaFuncSetAttribute(grad_drafts_kernel<TD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-    return false;
+  static std::atomic<uint64_t> ready{0};  // devices on which the shared memory is opted in to
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev > 63 || !(ready.load() >> dev & 1u)) {
+    if (cudaFuncSetAttribute(grad_drafts_kernel<TD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
+      return false;
+    if (dev < 64) ready.fetch_or(1ull << dev);
+  }
   return launch_kernel(true, grad_drafts_kernel<TD>, (unsigned)((int64_t)p.units * p.chunks), kThreads, bytes, st, p);
 }
 
@@ -538,7 +545,8 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   p.lse = lse;
   p.dlse = dlse;
   p.scale = (float)(scale > 0.0f ? scale : 1.0 / sqrt((double)kD));
-  p.scale_log2 = (float)((scale > 0.0f ? scale : 1.0 / sqrt((double)kD)) * 1.4426950408889634);
+  // a number whose reciprocal there is: the queries' kernel divides by it
+  p.scale_log2 = std::max((float)((scale > 0.0f ? scale : 1.0 / sqrt((double)kD)) * 1.4426950408889634), FLT_MIN);
   p.dks = reinterpret_cast<uint16_t*>(dk_store);
   p.dvs = reinterpret_cast<uint16_t*>(dv_store);
   const GradLayout ly(p.units, tokens, p.rows);
