@@ -344,8 +344,9 @@ constexpr int kRows = 16384;  // rows of a segment that a block takes
 constexpr int kMapEach = kRows / 4 / kThreads;
 
 // Many rows: bound by the bytes it writes (a 131071-token prompt of 256 segments, 137 MB).  A
-// thread writes 16 bytes at a time wherever a row of the output begins; its four rows mostly lie
-// in one page, whose entry is the only thing that it reads.
+// thread writes 16 bytes at a time wherever a row of the output begins; its four rows lie in one
+// page or two, whose entries are the only thing that it reads (with the rows that cross from one
+// to the next on a path of their own, which every warp took, 44 us for 27).
 __global__ void __launch_bounds__(kThreads) slot_map_kernel(const MapArgs p) {
   if (blockIdx.x >= p.chunks) {
     position(p, (blockIdx.x - p.chunks) * kThreads + threadIdx.x);
@@ -362,19 +363,20 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const MapArgs p) {
   const int32_t* row = p.st.table + (int64_t)u * p.st.max_pages;
   const int i0 = part * kRows - early, s0 = (int)start;
   bool bad = (lo > 0 || hi < n) && n > 0 && part == 0;
-  int page[kMapEach];
+  int page[kMapEach], next[kMapEach];  // of a thread's first row and of its last
 #pragma unroll
   for (int j = 0; j < kMapEach; ++j) {
-    const int i = i0 + 4 * (j * kThreads + (int)threadIdx.x), r = max(i, lo);
-    page[j] = r < min(i + 4, hi) ? __ldg(row + ((s0 + r) >> 6)) : -1;
+    const int i = i0 + 4 * (j * kThreads + (int)threadIdx.x);
+    const bool all = i >= lo && i + 4 <= hi;
+    page[j] = all ? __ldg(row + ((s0 + i) >> 6)) : -1;
+    next[j] = all ? __ldg(row + ((s0 + i + 3) >> 6)) : -1;
   }
 #pragma unroll
   for (int j = 0; j < kMapEach; ++j) {
     const int i = i0 + 4 * (j * kThreads + (int)threadIdx.x), s = (int)((uint32_t)s0 + (uint32_t)i);
-    const bool ok = page[j] >= 0 && page[j] < p.st.pool_pages;
-    if (i >= lo && i + 4 <= hi && (s & 63) <= 60 && ok) {  // all four in one page
-      const int v = page[j] * kPage + (s & 63);
-      *reinterpret_cast<int4*>(out + i) = make_int4(v, v + 1, v + 2, v + 3);
+    if (page[j] >= 0 && page[j] < p.st.pool_pages && next[j] >= 0 && next[j] < p.st.pool_pages) {
+      const int v = page[j] * kPage + (s & 63), w = (next[j] - 1) * kPage + (s & 63), left = kPage - (s & 63);
+      *reinterpret_cast<int4*>(out + i) = make_int4(v, (left > 1 ? v : w) + 1, (left > 2 ? v : w) + 2, (left > 3 ? v : w) + 3);
       continue;
     }
     int v[4];
