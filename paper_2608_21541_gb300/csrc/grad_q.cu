@@ -3,11 +3,16 @@
 // A CTA holds up to 128 query rows of a unit, and their output's gradients, as the M = 128 rows
 // of the MMAs, and walks a share of all tiles of 128 slots:
 //   S = Q K^T,  R = dO V^T,  e = 2^(S - lse) (R - delta),  dQ += e K,
-// with e handed over in tensor memory, over S, as a bf16 part and one of its remainder (2^-15).  Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so
-// a tile is formed in one pass.
+// with e handed over in tensor memory, over S, as a bf16 part and one of its remainder (2^-15).
+// Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so a tile is formed in
+// one pass.
 // Tensor memory: S of even tiles | S of odd tiles | R | dQ, 128 columns each.  S of the next
-// tile is made while e of this one is, R of the next as soon as R of this one has been read,
+// tile is made while e of this one is, R of the next as soon as this one's is in registers,
 // dQ of this one under e of the next.
+//
+// bf16 stores are bound by their bytes (64 rows over 13107 slots of 256 segments: 1.72 GB in
+// 274 us, 92 % of a copy's rate), 8- and 4-bit ones by the softmax beside the expanding of codes
+// (331 and 338 us; the products of 128 rows, half of them empty there, take 235).
 //
 // 8- and 4-bit stores: codes are exact in bf16 (gt::codes_to_bf16); a key's fp32 scale multiplies
 // its logit and its e, a value's its R, all in fp32.  The scale comes times that of the logits,
@@ -28,19 +33,19 @@ namespace certkv {
 namespace {
 
 // Warps, whole warpgroups of them: softmax, 64 columns of a row a thread where codes are expanded
-// beside it and 32 else (1024 rows over 32768 slots, bf16: 196 -> 158 us with sixteen; 8-bit
-// trees 204 -> 208, what bounds them there being the instructions of all), loaders, the issuer.
+// beside it and 32 else (1024 rows over 32768 slots, bf16: 196 us with eight warps, 158 with
+// sixteen; 8-bit trees 204 and 208, what bounds them being the instructions of all), loaders, and
+// the issuer beside the warps that ask for codes and state scales.
 constexpr int kLoadWarps = 2 * kGroupWarps;
 template <int FMT>
 struct Warps {
   static constexpr int kSoft = FMT == CERTKV_STORE_BF16 ? 16 : 8, kColumns = 512 / kSoft;
-  static constexpr int kAtOnce = FMT == CERTKV_STORE_BF16 ? 1 : 2;  // times 16 columns in flight, as registers allow
   static constexpr int kLoad = kSoft, kIssue = kSoft + kLoadWarps, kThreads = (kIssue + 4) * 32;
   // registers a thread: those of the launch, which the roles share out among themselves
   static constexpr int kLaunch = FMT == CERTKV_STORE_BF16 ? 72 : 96;
-  static constexpr int kSoftRegs = FMT == CERTKV_STORE_BF16 ? 80 : 104;
-  static constexpr int kLoadRegs = FMT == CERTKV_STORE_BF16 ? 64 : 88;
-  static constexpr int kIssueRegs = FMT == CERTKV_STORE_BF16 ? 56 : 96;
+  static constexpr int kSoftRegs = FMT == CERTKV_STORE_BF16 ? 72 : 104;
+  static constexpr int kLoadRegs = FMT == CERTKV_STORE_BF16 ? 72 : 88;
+  static constexpr int kIssueRegs = FMT == CERTKV_STORE_BF16 ? 72 : 96;
   static_assert(kSoft * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + 128 * kIssueRegs <= kThreads * kLaunch,
                 "a larger split would wait for registers for ever");
 };
@@ -49,7 +54,7 @@ constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
 template <int FMT>
 struct Plan {
   // Places of the rings.  The keys' are held from S of a tile to its dQ, the values' for R alone
-  // (8- and 4-bit stores: 2 + 2 places PLACES22 us, 3 + 1 PLACES31 us, 1024 rows over 13107 slots).
+  // (8 bits, 64 rows over 13107 slots of 256 segments: 396 us with 2 + 2 places, 357 with 3 + 1).
   static constexpr int kKeys = 3;
   static constexpr int kValues = FMT == CERTKV_STORE_BF16 ? 2 : 1;
   static constexpr int kFacts = FMT == CERTKV_STORE_BF16 ? kKeys : 2;  // bf16: the copying warps state them
@@ -181,15 +186,13 @@ struct Issuer {
 
 // e of 16 columns of a row, from the first column c on, over its logits: eight columns of bf16
 // and eight of what they leave.
-template <int FMT, class Loaded>
-__device__ __forceinline__ void columns(uint32_t tS, uint32_t tR, const typename gt::FactsOf<FMT>::type& f, int c,
-                                        float sl, float nlse, float ndelta, Loaded loaded) {
+template <int FMT>
+__device__ __forceinline__ void columns(uint32_t tS, const uint32_t* r, const typename gt::FactsOf<FMT>::type& f, int c,
+                                        float sl, float nlse, float ndelta) {
   constexpr bool kQuant = FMT != CERTKV_STORE_BF16;
   const float2 nl = make_float2(nlse, nlse), nd = make_float2(ndelta, ndelta), sl2 = make_float2(sl, sl);
-  uint32_t s[16], r[16], e[16];
+  uint32_t s[16], e[16];
   um::ld16(tS, s);
-  um::ld16(tR, r);
-  loaded();
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     float4 ks, vs;
@@ -290,16 +293,17 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
            gt::wait_all(GRAD_AT(s_full), t & 1u, GRAD_AT(abort));
       if (!ok) break;
       um::fence_after();
-#pragma unroll W::kAtOnce
-      for (int c = col; c < col + W::kColumns; c += 16) {
-        columns<FMT>(tmem + at + 128u * (t & 1u) + c, tmem + at + kColR + c,
-                     reinterpret_cast<const M*>(smem + P::kMiscOff)->facts[place], c, p.scale_log2, -mine.x, -mine.y, [&] {
-          if (c + 16 < col + W::kColumns) return;
-          um::fence_before();  // this warp's part of R has been read
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(GRAD_AT(r_free));
-        });
-      }
+      uint32_t r[W::kColumns];
+#pragma unroll
+      for (int c = 0; c < W::kColumns; c += 32)
+        um::ld32(tmem + at + kColR + col + c, *reinterpret_cast<uint32_t(*)[32]>(r + c));
+      um::fence_before();  // this warp's part of R has been read
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(GRAD_AT(r_free));
+#pragma unroll
+      for (int c = 0; c < W::kColumns; c += 16)
+        columns<FMT>(tmem + at + 128u * (t & 1u) + col + c, r + c,
+                     reinterpret_cast<const M*>(smem + P::kMiscOff)->facts[place], col + c, p.scale_log2, -mine.x, -mine.y);
       um::wait_st();
       um::fence_before();
       __syncwarp();
