@@ -685,14 +685,18 @@ int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const certkv_row
  * [batch][layers][tokens][hq]; dk_new, dv_new bf16 [batch][layers][tokens][hkv];
  * dk_store, dv_store bf16 [pool_pages][64][128], 128-byte aligned: the gradient of the
  * value that a slot stands for, whatever the store's format, in the slot's place
- * (slots that are not live are not written; no page may be two segments').  dq may be
+ * (slots that are not live are not written; no page may be named twice).  dq may be
  * NULL, and both of dk_new, dv_new (must be, without k_new), and both of dk_store,
  * dv_store; not all.  Outputs are overwritten; they overlap neither one another
  * nor an input.  A row whose lse is -inf gives and gets 0; what a row does not see
- * does not touch it, nor does the row touch that.  Sums are fp32, in an order that
- * does not change from call to call; p and e enter the sums as bf16 (2^-9 of each
- * product).  Limits and refusals are those of certkv_tree_attn, on a wait that runs
- * out the rows and slots concerned get NaN (CERTKV_STATUS_TIMEOUT).  Workspace:
+ * does not touch it, nor does the row touch that; a NaN or infinity that a row holds or
+ * sees makes its dq and the gradients of what it sees NaN, wherever a sum meets it.
+ * Sums are fp32, in an order that does not change from call to call.  e enters those
+ * of dq, and p and e those of the drafts, as two bf16 parts (2^-15 of each product);
+ * p and e enter the stored slots' as one (2^-8), and so does e those of dq where the
+ * slots' are asked for and tokens G <= 64, when one pass over the store makes all.
+ * Limits and refusals are those of certkv_tree_attn; on a wait that runs out the rows
+ * and slots concerned get NaN (CERTKV_STATUS_TIMEOUT).  Workspace:
  * certkv_tree_grad_workspace_bytes(shape, tokens), 256-byte aligned. */
 size_t certkv_tree_grad_workspace_bytes(const certkv_shape* shape, int32_t tokens);
 int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, const certkv_rows* q,

@@ -296,6 +296,121 @@ def test_long_segments_are_cut(fmt, T, G):
     run(st, n, 1, 1, 2, G, T)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T,G", [(2, 4), (64, 8)])
+def test_long_segments_without_drafts(fmt, T, G):
+    st, n = store_with([20000, 37], 1, 1, 2, fmt, 325)
+    run(st, n, 1, 1, 2, G, T, new=False, pools=False)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T,G,pools", [(4, 4, True), (40, 4, True), (4, 4, False)])
+def test_nothing_live(fmt, T, G, pools):
+    """Counts of nothing, below nothing and beyond the table; pages that are none."""
+    st, n = store_with([0], 1, 1, 2, fmt, 340)
+    run(st, n, 1, 1, 2, G, T, pools=pools)
+    x, got = run(st, n, 1, 1, 2, G, T, new=False, pools=pools)
+    assert not got["dq"].float().any()
+    st, n = store_with([128, 64], 1, 1, 2, fmt, 341, room=0)
+    want = run(st, n, 1, 1, 2, G, T, pools=pools)[1]
+    st.counts[0] = 2 ** 31 - 1
+    got = run(st, n, 1, 1, 2, G, T, pools=pools)[1]
+    assert all(torch.equal(got[a], want[a]) for a in want)
+    st.counts.fill_(-2 ** 31)
+    run(st, [0, 0], 1, 1, 2, G, T, pools=pools)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_smallest_scale(fmt):
+    """The least scale there is: logits are 0, and so are the gradients that it multiplies."""
+    st, n = store_with([200, 70], 1, 1, 2, fmt, 350)
+    for T in (6, 40):
+        x, got = run(st, n, 1, 1, 2, 4, T, scale=2.0 ** -149)
+        assert not got["dq"].float().any() and not got["dk"].float().any()
+        x, got = run(st, n, 1, 1, 2, 4, T, scale=2.0 ** -149, pools=False)
+        assert not got["dq"].float().any()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T,G", [(5, 4), (40, 4)])
+def test_pools_beyond_32_bits(fmt, T, G):
+    """Pages on both sides of offsets that 32 bits cannot hold: bit for bit what they give in a
+    small pool."""
+    st, n = store_with([300, 90], 1, 1, 2, fmt, 360)
+    x = step(st, 1, 1, 2, G, T)
+    want = grads(st, x, 2)
+    old = st.k.shape[0]
+    pages = 2 ** 32 // (st.k.element_size() * st.k[0].numel()) + 70
+    far = [pages - 1 - 3 * i if i % 2 else pages - 60 - 5 * i for i in range(old)]
+    assert len(set(far)) == old and min(far) < pages - 70 < max(far)
+    at = torch.tensor(far, device="cuda")
+    big = {}
+    for name in ("k", "v", "k_scale", "v_scale", "k_group", "v_group"):
+        t = getattr(st, name)
+        if t is not None:
+            big[name] = torch.empty((pages,) + t.shape[1:], dtype=t.dtype, device="cuda")
+            big[name].view(torch.uint8)[at] = t.view(torch.uint8)
+    table = at.int()[st.table.long()]
+    large = ck.Store(table=table, counts=st.counts, format=fmt, status=st.status, **big)
+    pools = [torch.empty((pages, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for p in pools:
+        p[at] = FILL
+    got = dict(zip(("dq", "dk", "dv"), ck.certkv_tree_attn_grad(
+        x["dout"], x["q"], large, x["out"], x["lse"], hkv=2, k_new=x["k_new"], v_new=x["v_new"],
+        dk_store=pools[0], dv_store=pools[1])))
+    got.update(dk_store=pools[0][at], dv_store=pools[1][at])
+    for name in want:
+        assert torch.equal(got[name], want[name]), name
+    assert st.read_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_training_step_over_pages(fmt):
+    """Pages reserved, slots mapped, rows appended, attended to and differentiated, captured
+    together: the slots' gradients gathered by the map are those of the rows, step by step."""
+    B, L, H, G, T = 2, 1, 2, 2, 30
+    U = B * L * H
+    st = ck.Store.empty(U, 4, fmt, pool_pages=16)
+    pg = ck.certkv_pages_list(st)
+    room = torch.full((B,), T, dtype=torch.int32, device="cuda")
+    k, v = (randn((B, L, T, H, 128), 70 + i) for i in range(2))
+    q, dout = (randn((B, L, T, H * G, 128), 72 + i) for i in range(2))
+    lse, out, dq = torch.empty((B, L, T, H * G), device="cuda"), torch.empty_like(q), torch.empty_like(q)
+    slots = torch.empty((U, T), dtype=torch.int32, device="cuda")
+    pos = torch.empty((B, T), dtype=torch.int32, device="cuda")
+    pools = [torch.full((16, 64, 128), FILL, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    wss = [ck.workspace(int(n), "cuda") for n in (
+        ck.certkv_pages_workspace_bytes(st), ck.certkv_tree_workspace_bytes(B, L, H * G, H, T),
+        ck.certkv_tree_grad_workspace_bytes(B, L, H * G, H, T))]
+
+    def one():
+        ck.certkv_pages_reserve(st, pg, room, ws=wss[0])
+        ck.certkv_slot_map(st, T, batch=B, slots=slots, positions=pos)
+        ck.certkv_store_append(k, v, st)
+        ck.certkv_tree_attn(q, st, hkv=H, lse=lse, out=out, ws=wss[1])
+        ck.certkv_tree_attn_grad(dout, q, st, out, lse, hkv=H, dq=dq, dk_store=pools[0],
+                                 dv_store=pools[1], ws=wss[2])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        one()
+    for n in range(1, 5):  # 30, 60, 90 and 120 slots: pages end inside tiles
+        for t, seed in ((k, 80), (v, 81), (q, 82), (dout, 83)):
+            t.copy_(randn(tuple(t.shape), seed + 10 * n))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert st.counts.tolist() == [n * T] * U and st.read_status() == 0
+        x = dict(q=q, dout=dout, out=out, lse=lse, k_new=None, v_new=None, mask=None, scale=0.0, dlse=None)
+        check(st, [n * T] * U, x, H, dict(dq=dq, dk_store=pools[0], dv_store=pools[1]))
+        new = slots.long()
+        assert torch.equal(new.cpu(), torch.stack([st.table.cpu()[u].long()[torch.arange((n - 1) * T, n * T) // 64] * 64
+                                                   + torch.arange((n - 1) * T, n * T) % 64 for u in range(U)]))
+        rows = pools[0].view(-1, 128)[new]  # what a training step would hand on
+        assert torch.isfinite(rows.float()).all() and not (rows == FILL).all(2).any()
+
+
 def test_against_differences():
     """The change of a loss along random directions, from forward passes in 64 bits: the whole
     chain forward, then backward.  fp32 differences of bf16 passes would drown; the definition's
