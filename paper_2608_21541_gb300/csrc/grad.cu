@@ -122,8 +122,8 @@ struct Records {
     c1 = f1 > f0 ? (folded ? c0 : (int)((f1 - 1) / per)) : 0;
   }
 };
-__device__ __forceinline__ void add4(float4& a, const float* from, int lane) {
-  const float4 x = *reinterpret_cast<const float4*>(from + 4 * lane);
+__device__ __forceinline__ void add4(float4& a, const float* from) {
+  const float4 x = *reinterpret_cast<const float4*>(from);
   a.x += x.x;
   a.y += x.y;
   a.z += x.z;
@@ -139,16 +139,16 @@ __global__ void __launch_bounds__(kThreads) grad_fold_kernel(const __grid_consta
   release_next();
   const Records c(p, u, false);
   if (c.c1 <= c.c0) return;
-  const int blk = r / p.rb, br = r - blk * p.rb;
+  const int blk = r / p.rb, at = grad_at(p, r - blk * p.rb, 4 * lane);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int i = c.c0 + warp; i <= c.c1; i += kThreads / 32) add4(a, p.rec + (grad_record(p, i, u, blk) + br) * kD, lane);
+  for (int i = c.c0 + warp; i <= c.c1; i += kThreads / 32) add4(a, grad_record(p, i, u, blk) + at);
   part[warp][lane] = a;
   __syncthreads();
   if (warp > 0) return;
 #pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) add4(a, &part[w][0].x, lane);
-  *reinterpret_cast<float4*>(p.rec + (grad_record(p, c.c0, u, blk) + br) * kD + 4 * lane) = a;
+  for (int w = 1; w < kThreads / 32; ++w) add4(a, &part[w][lane].x);
+  *reinterpret_cast<float4*>(grad_record(p, c.c0, u, blk) + at) = a;
 }
 
 // Without drafts one warp per query row: the records of the shares that met its segment.  With
@@ -162,10 +162,10 @@ __global__ void __launch_bounds__(kThreads) grad_merge_kernel(const __grid_const
   if (w < rows) {
     const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
     const GradUnit x(p, u);
-    const int blk = r / p.rb, br = r - blk * p.rb;
+    const int blk = r / p.rb, at = grad_at(p, r - blk * p.rb, 4 * lane);
     const Records c(p, u, p.folded);
 #pragma unroll 4
-    for (int i = c.c0; i <= c.c1; ++i) add4(a, p.rec + (grad_record(p, i, u, blk) + br) * kD, lane);
+    for (int i = c.c0; i <= c.c1; ++i) add4(a, grad_record(p, i, u, blk) + at);
     store4(p.dq.at(x.b, x.l, t, x.h * p.G + g), lane,
            make_float4(a.x * p.scale, a.y * p.scale, a.z * p.scale, a.w * p.scale));
     return;
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads) grad_merge_kernel(const __grid_const
   const int u = (int)(w / (2 * p.T)), i = (int)(w - (int64_t)u * 2 * p.T), key = i < p.T, j = key ? i : i - p.T;
   const GradUnit x(p, u);
 #pragma unroll 4
-  for (int c = 0; c < p.chunks; ++c) add4(a, p.part + (((int64_t)u * p.chunks + c) * 2 * p.T + i) * kD, lane);
+  for (int c = 0; c < p.chunks; ++c) add4(a, p.part + (((int64_t)u * p.chunks + c) * 2 * p.T + i) * kD + 4 * lane);
   const float f = key ? p.scale : 1.f;
   store4((key ? p.dkn : p.dvn).at(x.b, x.l, j, x.h), lane, make_float4(a.x * f, a.y * f, a.z * f, a.w * f));
 }
@@ -299,10 +299,10 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int br = min(r0 + 16 * warp + g8 + 8 * h, p.rows - 1), blk = br / p.rb;
-        const float* rec = p.rec + (grad_record(p, i, u, blk) + br - blk * p.rb) * kD + 2 * t4;
+        const float* rec = grad_record(p, i, u, blk) + grad_at(p, br - blk * p.rb, 2 * t4);
 #pragma unroll
         for (int n = 0; n < kD / 8; ++n) {
-          const float2 y = *reinterpret_cast<const float2*>(rec + 8 * n);
+          const float2 y = *reinterpret_cast<const float2*>(rec + (int64_t)n * p.rb * 8);
           acc[n][2 * h] += y.x, acc[n][2 * h + 1] += y.y;
         }
       }

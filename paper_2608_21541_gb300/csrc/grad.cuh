@@ -29,7 +29,7 @@ struct GradArgs {
   // workspace
   float2* row;     // [units][rows] log-sum-exp (log2 domain), delta; see grad_rows_kernel
   int64_t* first;  // [units + 1] tiles of the segments before
-  float* rec;      // [groups + units][nblk][rb][128] dq / scale over a share's tiles
+  float* rec;      // [groups + units][nblk] records of rb rows: dq / scale over a share's tiles
   float* part;     // [units][chunks][2][T][128] the drafts' dk / scale and dv over 128 rows
 };
 
@@ -53,10 +53,13 @@ __device__ __forceinline__ uint64_t grad_seen(const GradArgs& p, int b, int t) {
 __device__ __forceinline__ int64_t tiles_per_share(const GradArgs& p) {
   return max((p.first[p.units] + p.groups - 1) / p.groups, (int64_t)1);
 }
-// Record of the share's part of unit u, row block blk.
-__device__ __forceinline__ int64_t grad_record(const GradArgs& p, int share, int u, int blk) {
-  return (((int64_t)share + u) * p.nblk + blk) * p.rb;
+// Record of the share's part of unit u, row block blk: [16][rb][8], so that a warp whose lanes are
+// rows writes whole lines (as [rb][128] it took the queries' kernel 3 us a segment).
+__device__ __forceinline__ float* grad_record(const GradArgs& p, int share, int u, int blk) {
+  return p.rec + (((int64_t)share + u) * p.nblk + blk) * p.rb * kD;
 }
+// Element d of row r of a record.
+__device__ __forceinline__ int grad_at(const GradArgs& p, int r, int d) { return ((d >> 3) * p.rb + r) * 8 + (d & 7); }
 
 bool launch_grad_q(const GradArgs& p, int format, cudaStream_t st);
 bool launch_grad_kv(const GradArgs& p, int format, cudaStream_t st);

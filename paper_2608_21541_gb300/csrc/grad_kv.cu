@@ -467,14 +467,14 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
         }
       }
       if (FUSED && p.dq.p && k + 1 == now.kb) {  // element tid of every row
-        float* out = p.rec + grad_record(p, share, now.u, 0) * kD + tid;
+        float* out = grad_record(p, share, now.u, 0) + grad_at(p, 0, tid);
 #pragma unroll 1
         for (int r0 = 0; r0 < p.rows; r0 += 16) {
           uint32_t r[16];
           um::ld16(tmem + at + kColQ + (uint32_t)r0, r);
 #pragma unroll
           for (int q = 0; q < 16; ++q)
-            if (r0 + q < p.rows) out[(int64_t)(r0 + q) * kD] = good ? __uint_as_float(r[q]) : nanf("");
+            if (r0 + q < p.rows) out[(r0 + q) * 8] = good ? __uint_as_float(r[q]) : nanf("");
         }
       }
       um::fence_before();

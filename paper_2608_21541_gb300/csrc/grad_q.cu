@@ -259,29 +259,35 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     const float2* info = p.row + (int64_t)now.u * p.rows + blk * p.rb;
     // rows and their gradients into shared memory, 16 lanes a row; a row that takes no part, or
     // that holds a NaN or infinity, as zeros: what is summed over rows and slots stays clean
-#pragma unroll 1
-    for (int a = 0; a < 2; ++a) {
-      const Rows& src = a ? p.go : p.q;
-      const int c = tid & 15;
+    const float2 mine = row < rows ? info[row] : make_float2(INFINITY, 0.f);
+    {
       constexpr int kApart = W::kSoft * 2, kEach = 128 / kApart;
-      uint4 v[kEach];
+      const int c = tid & 15, r0 = tid >> 4;
+      const uint16_t *q = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *go = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
+      float l[kEach];
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int r = (tid >> 4) + kApart * i;
-        v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < rows && fabsf(info[r].x) < INFINITY) {
-          const int br = blk * p.rb + r, tok = br / p.G, g = br - tok * p.G;
-          v[i] = __ldg(reinterpret_cast<const uint4*>(src.at(x.b, x.l, tok, x.h * p.G + g)) + c);
+      for (int i = 0; i < kEach; ++i) l[i] = r0 + kApart * i < rows ? info[r0 + kApart * i].x : INFINITY;
+#pragma unroll
+      for (int h = 0; h < kEach; h += 4) {
+        uint4 v[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[0][i] = v[1][i] = make_uint4(0u, 0u, 0u, 0u);
+          if (!(fabsf(l[h + i]) < INFINITY)) continue;
+          const int br = blk * p.rb + r0 + kApart * (h + i), tok = br / p.G, g = br - tok * p.G;
+          v[0][i] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q.st + g * p.q.sh));
+          v[1][i] = __ldg(reinterpret_cast<const uint4*>(go + tok * p.go.st + g * p.go.sh));
         }
-      }
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int r = (tid >> 4) + kApart * i;
-        sts128(base + (uint32_t)(a * kOperand + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)), v[i].x, v[i].y,
-               v[i].z, v[i].w);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            const int r = r0 + kApart * (h + i);
+            sts128(base + (uint32_t)(a * kOperand + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)), v[a][i].x,
+                   v[a][i].y, v[a][i].z, v[a][i].w);
+          }
       }
     }
-    const float2 mine = row < rows ? info[row] : make_float2(INFINITY, 0.f);
     um::fence_async();
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(GRAD_AT(q_full));
@@ -312,7 +318,7 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
     if (ok) ok = gt::wait_all(GRAD_AT(o_full), item & 1u, GRAD_AT(abort));
     ++item;
     um::fence_after();
-    float* out = p.rec + (grad_record(p, share, now.u, blk) + row) * kD + col;
+    float* out = grad_record(p, share, now.u, blk) + grad_at(p, row, col);
     const bool good = ok && !gt::aborted(GRAD_AT(abort));
     const float unscale = FMT == CERTKV_STORE_BF16 ? 1.f : 1.f / p.scale_log2;
 #pragma unroll 1
@@ -324,8 +330,8 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
         for (int j = 0; j < 16; ++j)
           r[j] = good ? __float_as_uint(__uint_as_float(r[j]) * unscale) : 0x7fc00000u;
 #pragma unroll
-        for (int j = 0; j < 16; j += 8)  // whole sectors
-          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 16 * c + j), "r"(r[j]),
+        for (int j = 0; j < 16; j += 8)  // whole lines of a warp
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + (2 * c + j / 8) * p.rb * 8), "r"(r[j]),
                        "r"(r[j + 1]), "r"(r[j + 2]), "r"(r[j + 3]), "r"(r[j + 4]), "r"(r[j + 5]), "r"(r[j + 6]),
                        "r"(r[j + 7])
                        : "memory");
