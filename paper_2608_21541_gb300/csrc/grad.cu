@@ -76,7 +76,10 @@ __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
 }
 
 // Sixteen lanes per row: its log-sum-exp in the log2 domain and delta; +inf and 0 where it takes
-// no part; NaN where its query or its output's gradient holds a NaN or infinity.
+// no part; NaN where its query or its output's gradient holds a NaN or infinity.  Both rows are
+// laid out for the matrix units (grad_pack): a unit's rows are read again for each of its tiles,
+// and as they lie, 16 bytes a copy, that took longer than the products (1024 rows over 32768
+// slots: the slots' gradients 247 us, 225 as bulk copies).
 __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_constant__ GradArgs p) {
   release_next();
   if (blockIdx.x == 0) {
@@ -84,9 +87,10 @@ __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_consta
     return;
   }
   const int lane = threadIdx.x & 31, c = lane & 15;
-  const int64_t all = (int64_t)p.units * p.rows;
+  const int64_t all = (int64_t)p.units * p.padded;
   const int64_t w0 = ((int64_t)(blockIdx.x - 1) * kThreads + threadIdx.x) >> 4, w = min(w0, all - 1);
-  const int u = (int)(w / p.rows), r = (int)(w - (int64_t)u * p.rows), t = r / p.G, g = r - t * p.G;
+  const int u = (int)(w / p.padded), to = (int)(w - (int64_t)u * p.padded), r = min(to, p.rows - 1);
+  const int t = r / p.G, g = r - t * p.G;
   const GradUnit x(p, u);
   const int qh = x.h * p.G + g;
   const int64_t at = (((int64_t)x.b * p.L + x.l) * p.T + t) * p.H * p.G + qh;
@@ -107,10 +111,20 @@ __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_consta
 #pragma unroll
   for (int s = 8; s >= 1; s >>= 1) delta += __shfl_xor_sync(kFull, delta, s);
   odd = (__ballot_sync(kFull, odd) & (0xffffu << (lane & 16))) != 0u;
-  if (c == 0 && w0 < all)
-    p.row[w] = lse == -INFINITY ? make_float2(INFINITY, 0.f)
-               : odd            ? make_float2(nanf(""), nanf(""))
-                                : make_float2(lse * 1.4426950408889634f, delta - dlse);
+  if (w0 >= all) return;
+  const float2 f = to >= p.rows || lse == -INFINITY ? make_float2(INFINITY, 0.f)
+                   : odd                            ? make_float2(nanf(""), nanf(""))
+                                                    : make_float2(lse * 1.4426950408889634f, delta - dlse);
+  if (c == 0) {
+    if (to < p.rows) p.row[(int64_t)u * p.rows + to] = f;
+    p.neg[(int64_t)(2 * u) * p.padded + to] = -f.x;
+    p.neg[(int64_t)(2 * u + 1) * p.padded + to] = -f.y;
+  }
+  const bool on = fabsf(f.x) < INFINITY;
+  const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+  const int chunk = ((c & 7) ^ (to & 7)) << 4;
+  *reinterpret_cast<uint4*>(grad_pack(p, u, c >> 3, to) + chunk) = on ? q : none;
+  *reinterpret_cast<uint4*>(grad_pack(p, u, 2 + (c >> 3), to) + chunk) = on ? d : none;
 }
 
 // The records of unit u: shares c0 .. c1 (c1 < c0: none), of which folding leaves the first.
@@ -471,17 +485,20 @@ int grad_shape(const certkv_shape* s, int32_t tokens) {
 constexpr int kMaxCtas = 1024;  // records are sized for at most this many
 
 struct GradLayout {
-  int nblk, rb, chunks;
-  size_t row, first, rec, part, total;
+  int padded, nblk, rb, chunks;
+  size_t row, first, pack, neg, rec, part, total;
   GradLayout(int64_t units, int tokens, int rows) {
     auto a = [](size_t x) { return (x + 255) / 256 * 256; };
     nblk = (rows + kGradRows - 1) / kGradRows;
-    rb = (rows + nblk - 1) / nblk;
+    rb = ((rows + nblk - 1) / nblk + 7) / 8 * 8;
+    padded = (rows + 15) / 16 * 16;
     chunks = (rows + kChunkRows - 1) / kChunkRows;
     const size_t n = (size_t)units * rows;
     row = 0;
     first = row + a(n * sizeof(float2));
-    rec = first + a(((size_t)units + 1) * sizeof(int64_t));
+    pack = first + a(((size_t)units + 1) * sizeof(int64_t));
+    neg = pack + (size_t)units * 4 * padded * 128;
+    rec = neg + a((size_t)units * 2 * padded * sizeof(float));
     part = rec + ((size_t)units * nblk + kMaxCtas) * rb * kD * sizeof(float);
     total = part + (chunks > 1 ? (size_t)units * chunks * 2 * tokens * kD * sizeof(float) : 0);
   }
@@ -550,12 +567,15 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   p.dks = reinterpret_cast<uint16_t*>(dk_store);
   p.dvs = reinterpret_cast<uint16_t*>(dv_store);
   const GradLayout ly(p.units, tokens, p.rows);
+  p.padded = ly.padded;
   p.nblk = ly.nblk;
   p.rb = ly.rb;
   p.chunks = ly.chunks;
   char* ws = reinterpret_cast<char*>(workspace);
   p.row = reinterpret_cast<float2*>(ws + ly.row);
   p.first = reinterpret_cast<int64_t*>(ws + ly.first);
+  p.pack = reinterpret_cast<uint8_t*>(ws + ly.pack);
+  p.neg = reinterpret_cast<float*>(ws + ly.neg);
   p.rec = reinterpret_cast<float*>(ws + ly.rec);
   p.part = reinterpret_cast<float*>(ws + ly.part);
   // warps of the merge, blocks of the drafts' kernel
@@ -574,7 +594,7 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   {
     TraceScope ts_("grad_rows", st);
-    if (!launch_kernel(false, grad_rows_kernel, warps((n + 1) / 2) + 1, kThreads, 0, st, p)) return cuda_failed();
+    if (!launch_kernel(false, grad_rows_kernel, warps(((int64_t)p.units * p.padded + 1) / 2) + 1, kThreads, 0, st, p)) return cuda_failed();
   }
   if (p.dks) {
     GradArgs all = p;

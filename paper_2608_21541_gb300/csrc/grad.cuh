@@ -16,7 +16,8 @@ constexpr int kGradFused = 64;    // up to this many rows a segment's gradients 
 struct GradArgs {
   int L, H, G, T;    // layers, KV heads, query heads per KV head, drafted tokens
   int units, rows;   // B L H, T G query rows per unit
-  int nblk, rb;      // row blocks of a unit, rows of a block (the last may have fewer)
+  int padded;        // rows up to a multiple of 16
+  int nblk, rb;      // row blocks of a unit, rows of a block: a multiple of 8 (the last may have fewer)
   int groups;        // shares of the tiles; their CTAs leave records
   int chunks;        // of the drafts' kernel: 128 rows each
   int folded;        // a unit's records have been added up into its first
@@ -28,6 +29,8 @@ struct GradArgs {
   uint16_t *dks, *dvs;  // the store's gradients (null: not asked for)
   // workspace
   float2* row;     // [units][rows] log-sum-exp (log2 domain), delta; see grad_rows_kernel
+  uint8_t* pack;   // [units][4][padded][128 bytes] both halves of q, then of dout; see grad_pack
+  float* neg;      // [units][2][padded] -log-sum-exp, -delta
   int64_t* first;  // [units + 1] tiles of the segments before
   float* rec;      // [groups + units][nblk] records of rb rows: dq / scale over a share's tiles
   float* part;     // [units][chunks][2][T][128] the drafts' dk / scale and dv over 128 rows
@@ -47,6 +50,14 @@ struct GradUnit {
 __device__ __forceinline__ uint64_t grad_seen(const GradArgs& p, int b, int t) {
   const uint64_t all = ~0ull >> (64 - p.T);
   return (p.mask ? p.mask[(int64_t)b * p.T + t] : ~0ull >> (63 - t)) & all;
+}
+
+// Row r of part `part` of unit u's queries and gradients (part 0 and 1: elements 0 .. 63 and 64 ..
+// of q, 2 and 3: of dout) as the matrix units take them, 16-byte chunk c at c ^ (r & 7): any
+// rows from a multiple of 8 on are one bulk copy.  Rows that take no part, or that hold a NaN or
+// infinity, are zeros, so that what is summed over rows and slots stays clean.
+__device__ __forceinline__ uint8_t* grad_pack(const GradArgs& p, int u, int part, int r) {
+  return p.pack + (((int64_t)u * 4 + part) * p.padded + r) * 128;
 }
 
 // Tiles of a share: equal consecutive parts of all tiles.

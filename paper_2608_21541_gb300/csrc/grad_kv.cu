@@ -27,8 +27,9 @@ namespace certkv {
 namespace {
 
 // Warps: softmax, loaders, four that write the slots' gradients (a whole warpgroup each: a warp
-// reaches the quarter of tensor memory that its number mod 4 says), the issuer, two that bring rows.
-constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps, kDrainWarps = 4, kRowWarps = 2;
+// reaches the quarter of tensor memory that its number mod 4 says), the issuer and a lane each that
+// asks for rows and for codes.
+constexpr int kSoftWarps = 8, kLoadWarps = 2 * kGroupWarps, kDrainWarps = 4;
 constexpr int kDrain = kSoftWarps + kLoadWarps, kIssue = kDrain + kDrainWarps;
 constexpr int kThreads = (kIssue + 4) * 32;
 // Registers a thread: the launch gives 80, which the roles share out among themselves.
@@ -115,67 +116,26 @@ struct Steps {
   }
 };
 
-// Two warps bring blocks of rows and their gradients into shared memory, each for a tile
-// (FUSED: for an item).  A row that takes no part, or that holds a NaN or infinity, comes as
-// zeros.
+// A lane that brings blocks of rows and their gradients into shared memory, each for a tile
+// (FUSED: for an item), by bulk copies.
 template <int FMT, bool FUSED>
 struct RowFeeder {
   using P = Plan<FMT, FUSED>;
   using M = Misc<FMT, FUSED>;
   const GradArgs& p;
   uint32_t base;
-  int tid;  // of 64
-  uint32_t over_g;  // 65536 / G, rounded up
   uint32_t n = 0;
-  bool pending = false;
 
-  __device__ __forceinline__ void hand_over(uint32_t i) const {
-    __syncwarp();
-    if ((tid & 31) == 0) tc::mbar_arrive(GRAD_AT(b_full) + 8u * (i % P::kBlocks));
-  }
   __device__ __forceinline__ bool block(int u, int j) {
-    constexpr uint32_t kPlaces = P::kBlocks;
-    const uint32_t place = n % kPlaces, phase = ((n / kPlaces) & 1u) ^ 1u;
-    if (pending && !__all_sync(kFull, tc::mbar_test(GRAD_AT(b_empty) + 8u * place, phase))) {
-      gt::cp_wait<0>();
-      hand_over(n - 1);
-      pending = false;
-    }
-    const GradUnit x(p, u);
-    const int rows = rows_of_block(p, j), lane = tid & 31;
-    const float2* info = p.row + (int64_t)u * p.rows + j * kCols;
-    const float2 lo = lane < rows ? info[lane] : make_float2(INFINITY, 0.f);
-    const float2 hi = lane + 32 < rows ? info[lane + 32] : make_float2(INFINITY, 0.f);
-    const uint64_t good = __ballot_sync(kFull, fabsf(lo.x) < INFINITY) |
-                          (uint64_t)__ballot_sync(kFull, fabsf(hi.x) < INFINITY) << 32;
-    if (!gt::wait_all(GRAD_AT(b_empty) + 8u * place, phase, GRAD_AT(abort))) return false;
-    gt::sts32(GRAD_AT(nlse) + 4 * (place * kCols + tid), __float_as_uint(tid < 32 ? -lo.x : -hi.x));
-    gt::sts32(GRAD_AT(ndelta) + 4 * (place * kCols + tid), __float_as_uint(tid < 32 ? -lo.y : -hi.y));
-    // four lanes a row, each every fourth 16 bytes of it: a row's address is worked out once for
-    // eight copies
-    const uint32_t to = base + P::kBlockOff + place * kBlock;
-    const int c = tid & 3;
-    const uint16_t *q0 = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *g0 = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
-#pragma unroll 2
-    for (int i = 0; i < 4; ++i) {
-      const int r = (tid >> 2) + 16 * i, br = j * kCols + r;
-      const bool on = good >> r & 1u;
-      const int tok = (int)((uint32_t)br * over_g >> 16), g = br - tok * p.G;  // br < 2^11, G <= 32: exact
-      const uint16_t *q = on ? q0 + tok * p.q.st + g * p.q.sh : q0, *o = on ? g0 + tok * p.go.st + g * p.go.sh : g0;
-      const uint32_t at = to + (uint32_t)(r * 128), a0 = (uint32_t)((c ^ (r & 7)) << 4), a1 = a0 ^ 64u;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {  // 16 bytes number c + 4 k
-        const uint32_t d = at + (k >> 1) * kRowHalf + (k & 1 ? a1 : a0);
-        gt::cp16(d, q + 32 * k, on);
-        gt::cp16(d + 2 * kRowHalf, o + 32 * k, on);
-      }
-    }
-    gt::cp_commit();
-    if (pending) {
-      gt::cp_wait<1>();
-      hand_over(n - 1);
-    }
-    pending = true;
+    const uint32_t place = n % P::kBlocks, full = GRAD_AT(b_full) + 8u * place, rows = up16(rows_of_block(p, j));
+    if (!gt::wait(GRAD_AT(b_empty) + 8u * place, ((n / P::kBlocks) & 1u) ^ 1u, GRAD_AT(abort))) return false;
+    tc::mbar_expect_tx(full, rows * (4u * 128u + 2u * 4u));
+#pragma unroll 1
+    for (int part = 0; part < 4; ++part)
+      tc::bulk_load(base + P::kBlockOff + place * kBlock + part * kRowHalf, grad_pack(p, u, part, j * kCols), rows * 128u, full);
+    const float* neg = p.neg + (int64_t)u * 2 * p.padded + j * kCols;
+    tc::bulk_load(GRAD_AT(nlse) + place * kCols * 4u, neg, rows * 4u, full);
+    tc::bulk_load(GRAD_AT(ndelta) + place * kCols * 4u, neg + p.padded, rows * 4u, full);
     ++n;
     return true;
   }
@@ -189,8 +149,8 @@ struct RowFeeder {
 #pragma unroll 1
         for (int j = 0; ok && j < blocks_of(p); ++j) ok = block(it.u, j);
     }
-    gt::cp_wait<0>();  // nothing lands after the CTA has gone
-    if (ok && pending) hand_over(n - 1);
+    for (uint32_t i = n > P::kBlocks ? n - P::kBlocks : 0; i < n; ++i)  // nothing lands after the CTA has gone
+      gt::wait(GRAD_AT(b_full) + 8u * (i % P::kBlocks), (i / P::kBlocks) & 1u, GRAD_AT(last));
   }
 };
 
@@ -506,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
       tc::mbar_init(GRAD_AT(st_empty) + 8u * i, kLoadWarps);
     }
     for (int i = 0; i < 4; ++i) {
-      tc::mbar_init(GRAD_AT(b_full) + 8u * (i), kRowWarps);
+      tc::mbar_init(GRAD_AT(b_full) + 8u * (i), 1);
       tc::mbar_init(GRAD_AT(b_empty) + 8u * (i), 1);
     }
     tc::mbar_init(GRAD_AT(o_full), 1);
@@ -553,10 +513,10 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
     if (warp == kIssue) {
       Issuer<FMT, FUSED> is{p, tmem, base};
       is.run(walk);
-    } else if (warp <= kIssue + kRowWarps) {
-      RowFeeder<FMT, FUSED> f{p, base, (int)threadIdx.x - (kIssue + 1) * 32, (65536u + p.G - 1) / p.G};
+    } else if (warp == kIssue + 1 && threadIdx.x % 32 == 0) {
+      RowFeeder<FMT, FUSED> f{p, base};
       f.run(walk);
-    } else if (FMT != CERTKV_STORE_BF16 && threadIdx.x % 32 == 0) {
+    } else if (FMT != CERTKV_STORE_BF16 && warp == kIssue + 2 && threadIdx.x % 32 == 0) {
       gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(last)};
       f.run(walk);
     }

@@ -66,7 +66,7 @@ struct Plan {
 template <int FMT>
 struct Misc {
   uint64_t k_full[3], k_empty[3], v_full[2], v_empty[2];
-  uint64_t q_full, s_full, r_free, p_full, o_full, done;
+  uint64_t q_full, q_empty, s_full, r_free, p_full, o_full, o_free, done;
   uint64_t f_full[2];                // facts (8- and 4-bit stores)
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   int2 live[2];  // of the stretches
@@ -82,10 +82,30 @@ static_assert(smem_bytes<CERTKV_STORE_BF16>() <= 232448 && smem_bytes<CERTKV_STO
                   smem_bytes<CERTKV_STORE_FP4>() <= 232448,
               "over the 227 KB of shared memory a CTA can have");
 
+// A lane that brings an item's rows and their gradients, by bulk copies, as soon as the products
+// of the item before are done with theirs.
 template <int FMT>
-__device__ __forceinline__ void softmax_sync() {
-  asm volatile("bar.sync 1, %0;" ::"n"(Warps<FMT>::kSoft * 32) : "memory");
-}
+struct RowFeeder {
+  using P = Plan<FMT>;
+  using M = Misc<FMT>;
+  const GradArgs& p;
+  uint32_t base;
+  int blk;
+  __device__ __forceinline__ void run(gt::Walk walk) const {
+    const uint32_t bytes = 128u * min(p.rb, p.padded - blk * p.rb);
+    gt::Item it;
+    uint32_t n = 0;
+#pragma unroll 1
+    while (walk.next(p, &it) && gt::wait(GRAD_AT(q_empty), (n & 1u) ^ 1u, GRAD_AT(abort))) {
+      tc::mbar_expect_tx(GRAD_AT(q_full), 4u * bytes);
+#pragma unroll 1
+      for (int part = 0; part < 4; ++part)
+        tc::bulk_load(base + part * kHalf, grad_pack(p, it.u, part, blk * p.rb), bytes, GRAD_AT(q_full));
+      ++n;
+    }
+    if (n > 0) gt::wait(GRAD_AT(q_full), (n - 1) & 1u, GRAD_AT(last));  // nothing lands after the CTA has gone
+  }
+};
 
 // Issues the MMAs of the share's tiles; the whole warp runs, one lane issues.
 template <int FMT>
@@ -112,7 +132,8 @@ struct Issuer {
   }
   __device__ __forceinline__ void await_keys() { wait(GRAD_AT(k_full) + 8u * sk.slot, sk.phase); }
   __device__ __forceinline__ void await_values() { wait(GRAD_AT(v_full) + 8u * rv.slot, rv.phase); }
-  // S of tile t, whose keys are there, and its R, whose values are
+  // S of tile t, whose keys are there, and its R, whose values are; last: nothing reads the item's
+  // rows behind it
   __device__ __forceinline__ void s(uint32_t t) {
     if (!ok) return;
     um::fence_async();  // the loaders' writes, before the tensor core's reads
@@ -121,7 +142,7 @@ struct Issuer {
               um::kDescHi, um::idesc(true, false));
     ++sk;
   }
-  __device__ __forceinline__ void r() {
+  __device__ __forceinline__ void r(bool last) {
     if (!ok) return;
     um::fence_async();
     um::fence_after();
@@ -129,6 +150,7 @@ struct Issuer {
               um::desc_lo(base + P::kValueOff, 16) + rv.slot * (kOperand >> 4), um::kDescHi, um::idesc(true, false));
     um::commit(GRAD_AT(s_full));
     um::commit(GRAD_AT(v_empty) + 8u * rv.slot);
+    if (last) um::commit(GRAD_AT(q_empty));
     ++rv;
   }
   __device__ __forceinline__ void run(const GradArgs& p, gt::Walk walk) {
@@ -137,11 +159,12 @@ struct Issuer {
 #pragma unroll 1
     while (ok && walk.next(p, &it)) {
       const int n = it.kb - it.ka;
-      wait(GRAD_AT(q_full), item++ & 1u);
+      wait(GRAD_AT(q_full), item & 1u);
       await_keys();
       s(t);
       await_values();
-      r();
+      if (t > 0) wait(GRAD_AT(r_free), (t - 1) & 1u);
+      r(n == 1);
 #pragma unroll 1
       for (int i = 0; ok && i < n; ++i, ++t) {
         // S of the next tile goes when its keys and values are there, R when this tile's has been
@@ -156,12 +179,13 @@ struct Issuer {
             has_s = true;
           }
           if (has_s && !has_r && test(GRAD_AT(r_free), t & 1u) && test(GRAD_AT(v_full) + 8u * rv.slot, rv.phase)) {
-            r();
+            r(i + 2 == n);
             has_r = true;
           }
           if (test(GRAD_AT(p_full), t & 1u)) break;
           ok = gt::patience(look, GRAD_AT(abort));
         }
+        if (i == 0 && item > 0) wait(GRAD_AT(o_free), (item - 1) & 1u);  // dQ of the item before has been read
         if (!ok) break;
         um::fence_after();
         um::mma_e2(tmem + kColQ, tmem + 128u * (t & 1u), um::desc_lo(base + P::kKeyOff, kHalf) + qk.slot * (kOperand >> 4),
@@ -175,9 +199,10 @@ struct Issuer {
         }
         if (!has_r) {
           await_values();
-          r();
+          r(i + 2 == n);
         }
       }
+      ++item;
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
     gt::wait_all(GRAD_AT(done), 0, GRAD_AT(last));
@@ -255,42 +280,7 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
 #pragma unroll 1
   while (walk.next(p, &it)) {
     const gt::Item now = it;
-    const GradUnit x(p, now.u);
-    const float2* info = p.row + (int64_t)now.u * p.rows + blk * p.rb;
-    // rows and their gradients into shared memory, 16 lanes a row; a row that takes no part, or
-    // that holds a NaN or infinity, as zeros: what is summed over rows and slots stays clean
-    const float2 mine = row < rows ? info[row] : make_float2(INFINITY, 0.f);
-    {
-      constexpr int kApart = W::kSoft * 2, kEach = 128 / kApart;
-      const int c = tid & 15, r0 = tid >> 4;
-      const uint16_t *q = p.q.at(x.b, x.l, 0, x.h * p.G) + 8 * c, *go = p.go.at(x.b, x.l, 0, x.h * p.G) + 8 * c;
-      float l[kEach];
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) l[i] = r0 + kApart * i < rows ? info[r0 + kApart * i].x : INFINITY;
-#pragma unroll
-      for (int h = 0; h < kEach; h += 4) {
-        uint4 v[2][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[0][i] = v[1][i] = make_uint4(0u, 0u, 0u, 0u);
-          if (!(fabsf(l[h + i]) < INFINITY)) continue;
-          const int br = blk * p.rb + r0 + kApart * (h + i), tok = br / p.G, g = br - tok * p.G;
-          v[0][i] = __ldg(reinterpret_cast<const uint4*>(q + tok * p.q.st + g * p.q.sh));
-          v[1][i] = __ldg(reinterpret_cast<const uint4*>(go + tok * p.go.st + g * p.go.sh));
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            const int r = r0 + kApart * (h + i);
-            sts128(base + (uint32_t)(a * kOperand + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4)), v[a][i].x,
-                   v[a][i].y, v[a][i].z, v[a][i].w);
-          }
-      }
-    }
-    um::fence_async();
-    __syncwarp();
-    if (lane == 0) tc::mbar_arrive(GRAD_AT(q_full));
+    const float2 mine = row < rows ? p.row[(int64_t)now.u * p.rows + blk * p.rb + row] : make_float2(INFINITY, 0.f);
 #pragma unroll 1
     for (int k = now.ka; ok && busy && k < now.kb; ++k, ++t) {
       const uint32_t place = t % P::kFacts;
@@ -337,9 +327,9 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
                        : "memory");
       }
     }
-    um::fence_before();
-    softmax_sync<FMT>();  // every warp has read its part of dQ, and nothing reads the rows any more
-    um::fence_after();
+    um::fence_before();  // this warp's part of dQ has been read
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(GRAD_AT(o_free));
   }
 }
 
@@ -368,7 +358,9 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       tc::mbar_init(GRAD_AT(st_full) + 8u * i, 1);
       tc::mbar_init(GRAD_AT(st_empty) + 8u * i, kLoadWarps);
     }
-    tc::mbar_init(GRAD_AT(q_full), W::kSoft);
+    tc::mbar_init(GRAD_AT(q_full), 1);
+    tc::mbar_init(GRAD_AT(q_empty), 1);
+    tc::mbar_init(GRAD_AT(o_free), W::kSoft);
     tc::mbar_init(GRAD_AT(s_full), 1);
     tc::mbar_init(GRAD_AT(r_free), W::kSoft / 4 * ((p.rb + 31) / 32));
     tc::mbar_init(GRAD_AT(p_full), W::kSoft / 4 * ((p.rb + 31) / 32));  // the warps with rows
@@ -418,6 +410,8 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 2) {
       gt::FactFeeder<FMT, P::kKeys> f{p, GRAD_AT(f_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort), (int)threadIdx.x & 31};
       f.run(walk);
+    } else if (warp == W::kIssue + 3 && threadIdx.x % 32 == 0) {
+      RowFeeder<FMT>{p, base, blk}.run(walk);
     }
   }
   um::fence_before();
