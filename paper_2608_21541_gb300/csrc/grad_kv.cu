@@ -177,7 +177,7 @@ struct Issuer {
     }
     if (!FUSED || s.first) wait(GRAD_AT(b_full) + 8u * (s.blk % P::kBlocks), s.blk / P::kBlocks);
     if (!ok) return;
-    um::fence_async();  // the loaders' writes, before the tensor core's reads
+    if (s.j == 0) um::fence_async();  // the loaders' writes, before the tensor core's reads
     um::fence_after();
     const uint32_t d = tmem + 128u * buffer(s), id = um::idesc_n(columns(s), false, false);
     const uint32_t q = um::desc_lo(base + P::kBlockOff, 16) + (s.blk % P::kBlocks) * (kBlock >> 4);
