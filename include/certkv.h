@@ -640,8 +640,8 @@ int certkv_pages_reserve(int32_t batch, const int32_t* room, const int32_t* want
  * positions (may be NULL): int32 [batch][tokens], base[b] + the depth of token t:
  * the number of other drafts that mask[b][t] names (uint64 [batch][tokens], as for
  * certkv_tree_attn; bits from `tokens` on are ignored), with mask NULL t.  base:
- * device int32 [batch], NULL: 0; positions wrap at 2^31.  mask needs tokens <= 64;
- * units * tokens < 2^40. */
+ * device int32 [batch], NULL: 0; positions wrap at 2^31.  tokens <= 2^30, with mask
+ * 64; units * tokens < 2^40. */
 int certkv_slot_map(int32_t batch, int32_t tokens, const int32_t* rows, const int32_t* start,
                     const int32_t* base, const uint64_t* mask, const certkv_store* store,
                     int32_t* slots, int32_t* positions, void* stream);

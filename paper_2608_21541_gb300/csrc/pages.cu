@@ -512,7 +512,8 @@ extern "C" int certkv_slot_map(int32_t batch, int32_t tokens, const int32_t* row
   MapArgs p;
   int rc;
   if ((rc = store_of(store, &p.st))) return rc;
-  if (batch < 1 || p.st.units % batch != 0 || tokens < 1 || (mask && tokens > 64)) return CERTKV_EINVAL;
+  if (batch < 1 || p.st.units % batch != 0 || tokens < 1 || tokens > 1 << 30 || (mask && tokens > 64))
+    return CERTKV_EINVAL;
   if (((uintptr_t)rows | (uintptr_t)start | (uintptr_t)base | (uintptr_t)slots | (uintptr_t)positions) % 4 != 0 ||
       (uintptr_t)mask % 8 != 0 || (!slots && !positions))
     return CERTKV_EINVAL;

@@ -83,6 +83,14 @@ def test_slot_map_refuses(lib):
         assert call(**kw) == ck.EINVAL, kw
 
 
+@pytest.mark.parametrize("tokens", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_slot_map_refuses_rows_past_its_counting(lib, tokens):
+    """Rows are counted in 32 bits, a block's worth past the last."""
+    st = store()
+    assert lib.certkv_slot_map(2, tokens, None, None, None, None, ctypes.byref(st), FAKE, None,
+                               None) == ck.EINVAL
+
+
 def test_binding_refuses():
     with pytest.raises(ValueError):
         ck.Pages(held=torch.zeros(4, dtype=torch.int64), free=torch.zeros(4, dtype=torch.int32),
