@@ -40,12 +40,13 @@ __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
   __shared__ long long part[kThreads / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   long long carry = 0;
-  for (int base = 0; base < p.units; base += 4 * kThreads) {
-    int n[4];
+  constexpr int kEach = 16;
+  for (int base = 0; base < p.units; base += kEach * kThreads) {
+    int n[kEach];
     long long sum = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int u = base + 4 * (int)threadIdx.x + i;
+    for (int i = 0; i < kEach; ++i) {
+      const int u = base + kEach * (int)threadIdx.x + i;
       n[i] = u < p.units ? (p.st.count(u) + kGradTile - 1) / kGradTile : 0;
       sum += n[i];
     }
@@ -65,8 +66,8 @@ __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
     }
     before += x - sum;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int u = base + 4 * (int)threadIdx.x + i;
+    for (int i = 0; i < kEach; ++i) {
+      const int u = base + kEach * (int)threadIdx.x + i;
       if (u < p.units) p.first[u] = before;
       before += n[i];
     }
@@ -309,16 +310,24 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
     for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
   if (p.dq.p && warp < strips) {
     const Records c(p, u, p.folded);
+    const float* from[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int br = min(r0 + 16 * warp + g8 + 8 * h, p.rows - 1), blk = br / p.rb;
+      from[h] = grad_record(p, c.c0, u, blk) + grad_at(p, br - blk * p.rb, 2 * t4);
+    }
+    const int64_t share = (int64_t)p.nblk * p.rb * kD;
     for (int i = c.c0; i <= c.c1; ++i) {
+      float2 y[2][kD / 8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < kD / 8; ++n) y[h][n] = __ldcg(reinterpret_cast<const float2*>(from[h] + n * p.rb * 8));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int br = min(r0 + 16 * warp + g8 + 8 * h, p.rows - 1), blk = br / p.rb;
-        const float* rec = grad_record(p, i, u, blk) + grad_at(p, br - blk * p.rb, 2 * t4);
 #pragma unroll
-        for (int n = 0; n < kD / 8; ++n) {
-          const float2 y = *reinterpret_cast<const float2*>(rec + (int64_t)n * p.rb * 8);
-          acc[n][2 * h] += y.x, acc[n][2 * h + 1] += y.y;
-        }
+        for (int n = 0; n < kD / 8; ++n) acc[n][2 * h] += y[h][n].x, acc[n][2 * h + 1] += y[h][n].y;
+        from[h] += share;
       }
     }
   }

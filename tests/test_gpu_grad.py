@@ -288,6 +288,12 @@ def test_many_segments(fmt, units, G, T):
     run(st, n, 1, 1, units, G, T)
 
 
+def test_thousands_of_segments():
+    """More than one pass of the scan over their tiles."""
+    st, n = store_with([0, 3, 64, 130, 1, 200, 5], 1, 9, 1000, "bf16", 315)
+    run(st, n, 1, 9, 1000, 1, 1)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("T,G", [(1, 4), (32, 4), (64, 8)])
 def test_long_segments_are_cut(fmt, T, G):
