@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kThreads) pages_mark_kernel(const Store st, in
   if (lane == 0) held[u] = reach;
 }
 
-constexpr int kWords = 4 * kThreads;  // words of 32 pages a block
+constexpr int kWords = kThreads;  // words of 32 pages a block
 
 __device__ __forceinline__ uint32_t free_bits(const uint32_t* used, int64_t w, int pool) {
   if (w * 32 >= pool) return 0u;
@@ -272,10 +272,8 @@ __device__ __forceinline__ uint32_t free_bits(const uint32_t* used, int64_t w, i
 __global__ void __launch_bounds__(kThreads) pages_free_sum_kernel(const uint32_t* used, int pool, longlong2* sums) {
   await_previous();
   release_next();
-  longlong2 n = make_longlong2(0, 0), all;
-  for (int i = 0; i < kWords; i += kThreads)
-    n.x += __popc(free_bits(used, (int64_t)blockIdx.x * kWords + i + threadIdx.x, pool));
-  block_scan(n, &all);
+  longlong2 all;
+  block_scan(make_longlong2(__popc(free_bits(used, (int64_t)blockIdx.x * kWords + threadIdx.x, pool)), 0), &all);
   if (threadIdx.x == 0) sums[blockIdx.x] = all;
 }
 
@@ -289,14 +287,18 @@ __global__ void __launch_bounds__(kThreads) pages_free_kernel(const uint32_t* us
   }
   block_scan(b, &base);
   const int total = (int)base.x;
-  int before = (int)base.y;
-  for (int i = 0; i < kWords; i += kThreads) {
-    const int64_t w = (int64_t)blockIdx.x * kWords + i + threadIdx.x;
-    uint32_t x = free_bits(used, w, pool);
-    longlong2 all;
-    int rank = before + (int)block_scan(make_longlong2(__popc(x), 0), &all).x;
-    before += (int)all.x;
-    for (; x; x &= x - 1) list[total - 1 - rank++] = (int32_t)(w * 32 + __ffs(x) - 1);
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * kWords + threadIdx.x;
+  const uint32_t mine = free_bits(used, w, pool);
+  longlong2 all;
+  const int rank = (int)base.y + (int)block_scan(make_longlong2(__popc(mine), 0), &all).x;
+  // a word's pages side by side (each by its thread alone, and four words a thread: 8 us more for a list
+  // of 280000 pages)
+#pragma unroll 4
+  for (int i = 0; i < 32; ++i) {
+    const uint32_t x = __shfl_sync(kFull, mine, i);
+    const int at = total - 1 - __shfl_sync(kFull, rank, i) - __popc(x & ((1u << lane) - 1u));
+    if (x >> lane & 1u) list[at] = (int32_t)((w - lane + i) * 32 + lane);
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *count = total;
 }
