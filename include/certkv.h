@@ -691,13 +691,11 @@ int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const certkv_row
  * nor an input.  A row whose lse is -inf gives and gets 0; what a row does not see
  * does not touch it, nor does the row touch that; a NaN or infinity that a row holds or
  * sees makes its dq and the gradients of what it sees NaN, wherever a sum meets it.
- * Sums are fp32, in an order that does not change from call to call.  e enters those
- * of dq, and p and e those of the drafts, as two bf16 parts (2^-15 of each product);
- * p and e enter the stored slots' as one (2^-8), and so does e those of dq where the
- * slots' are asked for and tokens G <= 64, when one pass over the store makes all.
- * Limits and refusals are those of certkv_tree_attn; on a wait that runs out the rows
- * and slots concerned get NaN (CERTKV_STATUS_TIMEOUT).  Workspace:
- * certkv_tree_grad_workspace_bytes(shape, tokens), 256-byte aligned. */
+ * Sums are fp32, in an order that does not change from call to call; p and e enter
+ * them as two bf16 parts (2^-14 of each product at most).  Limits and refusals are
+ * those of certkv_tree_attn; on a wait that runs out the rows and slots concerned get
+ * NaN (CERTKV_STATUS_TIMEOUT).  Workspace: certkv_tree_grad_workspace_bytes(shape,
+ * tokens), 256-byte aligned. */
 size_t certkv_tree_grad_workspace_bytes(const certkv_shape* shape, int32_t tokens);
 int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, const certkv_rows* q,
                           const certkv_rows* k_new, const certkv_rows* v_new,

@@ -5,15 +5,20 @@
 // each the unit's query rows in blocks of at most 64, the N columns:
 //   S = K Q^T,  R = V dO^T,  p = 2^(S - lse),  e = p (R - delta),
 //   dV += p dO,  dK += e Q,
-// p and e rounded once to bf16 and handed over in tensor memory, over S.  Blocks of 64 columns
-// leave room in tensor memory for two of them beside dV and dK, so that one block's S and R are
-// made while p and e of the other are: S, R | S, R (64 columns each) | dV | dK (128 each).
+// p and e handed over in tensor memory as two bf16 parts each, the first over S and the second
+// over R (2^-14 at most; one part each took 225 us for 279 with 1024 rows over 32768 slots, and left
+// 1.4 to 1.5 times the error).  Blocks of 64 columns leave room in tensor memory for two of them
+// beside dV and dK, so that one block's S and R are made while p and e of the other are:
+// S, R | S, R (64 columns each) | dV | dK (128 each).  Each block reads K and V from shared memory
+// again, which with the rows and their coming takes 1500 clocks of the 2270 a block's step has.
 //
 // Up to 64 rows (FUSED) a segment is one block, whose rows stay in shared memory, and
 // dQ^T += K^T e (M = 128 elements of a row) is summed over the share's tiles in the columns of
-// the second block; e times the key's scale is handed over in shared memory for it.  The store
-// is then read once for all gradients: with 64 rows or less the time is that of its bytes.
-// Reading it again for the queries' kernel would cost as much as reading it here.
+// the second block; e times the key's scale is handed over in shared memory for it, in two parts
+// too.  The store is then read once for all gradients, and over bf16 the time is that of its bytes
+// (64 rows over 13107 slots of 256 segments: 3.4 GB in 528 us, 96 % of a copy's rate; 8- and 4-bit
+// 587 and 583 us, the pace of writing four and eight times the bytes read).  Reading it again for
+// the queries' kernel would cost as much as reading it here.
 //
 // Every wait is bounded; on a timeout the roles stop waiting, the rows and slots in question get
 // NaN and the store's status word CERTKV_STATUS_TIMEOUT.
@@ -34,7 +39,7 @@ constexpr int kDrain = kSoftWarps + kLoadWarps, kIssue = kDrain + kDrainWarps;
 constexpr int kThreads = (kIssue + 4) * 32;
 // Registers a thread: the launch gives 80, which the roles share out among themselves.
 constexpr int kLaunchRegs = 80;
-constexpr int kSoftRegs = 96, kLoadRegs = 72, kDrainRegs = 72, kIssueRegs = 72;
+constexpr int kSoftRegs = 104, kLoadRegs = 64, kDrainRegs = 72, kIssueRegs = 72;
 static_assert(kSoftWarps * 32 * kSoftRegs + kLoadWarps * 32 * kLoadRegs + kDrainWarps * 32 * kDrainRegs + 128 * kIssueRegs <=
                   kThreads * kLaunchRegs,
               "a larger split would wait for registers for ever");
@@ -45,15 +50,16 @@ constexpr uint32_t kColV = 256, kColK = 384, kColQ = 128;  // S of block i: colu
 
 template <int FMT, bool FUSED>
 struct Plan {
-  static constexpr int kKeys = FUSED ? 2 : 1, kValues = FUSED ? 2 : 1;  // places of the rings
+  static constexpr int kKeys = FUSED ? 2 : 1;  // places of the rings: keys are read again for dQ
+  static constexpr int kValues = FUSED && FMT == CERTKV_STORE_BF16 ? 2 : 1;
   static constexpr int kBlocks = FUSED ? (FMT == CERTKV_STORE_BF16 ? 2 : 1) : FMT == CERTKV_STORE_BF16 ? 4 : 3;
   static constexpr int kValueOff = kKeys * kOperand;
   static constexpr int kBlockOff = kValueOff + kValues * kOperand;
-  static constexpr int kEOff = kBlockOff + kBlocks * kBlock;  // e, FUSED: [128 slots][64 rows]
-  static constexpr int kStageOff = kEOff + (FUSED ? kHalf : 0);  // of keys, then of values
-  // Slots' gradients are written by sectors where the store's bytes bound the pass, and else by
-  // lines through shared memory, half a row of 32 slots a warp (64 rows over 32768 slots, bf16:
-  // 508 us by sectors, 540 by lines; over 13107 slots, 8 bits: 606 and 572).
+  static constexpr int kEOff = kBlockOff + kBlocks * kBlock;  // e, FUSED: two parts [128 slots][64 rows]
+  static constexpr int kStageOff = kEOff + (FUSED ? 2 * kHalf : 0);  // of keys, then of values
+  // Slots' gradients are written by lines through shared memory, half a row of 32 slots a warp (64
+  // rows over 13107 slots of 256 segments, 8 bits: 572 us, 606 by sectors), but by sectors where a
+  // bf16 store's bytes bound the pass (505 us, and 540 by lines).
   static constexpr bool kLines = !FUSED || FMT != CERTKV_STORE_BF16;
   static constexpr int kDrainOff = kStageOff + 2 * gt::kStage<FMT>;
   static constexpr int kMiscOff = kDrainOff + (kLines ? kDrainWarps * 4096 : 0);
@@ -62,7 +68,7 @@ template <int FMT, bool FUSED>
 struct Misc {
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t b_full[4], b_empty[4];
-  uint64_t s_full[2], p_full[2], o_full, drained, done;
+  uint64_t s_full[2], p_full[2], o_full[2], drained[2], done;  // o_full, drained: dV, dK
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   int2 live[2];  // of the stretches
   uint32_t tmem;
@@ -195,21 +201,30 @@ struct Issuer {
     const uint32_t x = buffer(s);
     wait(GRAD_AT(p_full) + 8u * (x), odd >> x & 1u);
     odd ^= 1u << x;
-    if (s.j == 0 && tiles++ > 0) wait(GRAD_AT(drained), tiles - 2);
+    const bool begins = s.j == 0 && tiles++ > 0;  // those of the tile before are written first
+    if (begins) wait(GRAD_AT(drained), tiles - 2);
     if (!ok) return;
     if (FUSED) um::fence_async();
     um::fence_after();
     const uint32_t a = tmem + 128u * x, steps = columns(s) / 16, acc = s.j > 0;
     const uint32_t q = um::desc_lo(base + P::kBlockOff, kRowHalf) + (s.blk % P::kBlocks) * (kBlock >> 4);
     constexpr uint32_t id = um::idesc_n(128, false, true);
-    um::mma_p64(tmem + kColV, a, q + (2 * kRowHalf >> 4), um::kDescHi, id, acc, steps);
-    um::mma_p64(tmem + kColK, a + 16, q, um::kDescHi, id, acc, steps);
-    if (FUSED)
-      um::mma_mn(tmem + kColQ, um::desc_lo(base, kHalf) + (s.t % P::kKeys) * (kOperand >> 4),
-                 um::desc_lo(base + P::kEOff, 16), um::kDescHi, um::idesc_n(columns(s), true, true), !s.first);
+    um::mma_p64<8, 32, 40>(tmem + kColV, a, q + (2 * kRowHalf >> 4), um::kDescHi, id, acc, steps);
+    um::mma_p64<16, 32, 48>(tmem + kColV, a + 64, q + (2 * kRowHalf >> 4), um::kDescHi, id, 1u, steps);
+    if (s.j + 1 == s.n) um::commit(GRAD_AT(o_full));
+    if (begins) wait(GRAD_AT(drained) + 8u, tiles - 2);
+    if (!ok) return;
+    um::fence_after();
+    um::mma_p64<8, 32, 40>(tmem + kColK, a + 16, q, um::kDescHi, id, acc, steps);
+    um::mma_p64<16, 32, 48>(tmem + kColK, a + 72, q, um::kDescHi, id, 1u, steps);
+    if (FUSED) {
+      const uint32_t keys = um::desc_lo(base, kHalf) + (s.t % P::kKeys) * (kOperand >> 4), idq = um::idesc_n(columns(s), true, true);
+      um::mma_mn(tmem + kColQ, keys, um::desc_lo(base + P::kEOff, 16), um::kDescHi, idq, !s.first);
+      um::mma_mn(tmem + kColQ, keys, um::desc_lo(base + P::kEOff + kHalf, 16), um::kDescHi, idq, 1u);
+    }
     if (FUSED) um::commit(GRAD_AT(k_empty) + 8u * (s.t % P::kKeys));
     if (!FUSED || s.last) um::commit(GRAD_AT(b_empty) + 8u * (s.blk % P::kBlocks));
-    if (s.j + 1 == s.n) um::commit(GRAD_AT(o_full));
+    if (s.j + 1 == s.n) um::commit(GRAD_AT(o_full) + 8u);
   }
   __device__ __forceinline__ void run(const gt::Walk& walk) {
     Steps<FUSED> steps(p, walk);
@@ -251,6 +266,15 @@ struct Slot {
     }
   }
 };
+
+// Two values as bf16 parts, the upper halves as they are and those of what that leaves: neither
+// takes a conversion (2^-14 together, towards 0).
+__device__ __forceinline__ void split(float2 x, uint32_t& hi, uint32_t& lo) {
+  const float2 y = fadd2(x, make_float2(-__uint_as_float(__float_as_uint(x.x) & 0xffff0000u),
+                                        -__uint_as_float(__float_as_uint(x.y) & 0xffff0000u)));
+  hi = __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632);
+  lo = __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x7632);
+}
 
 __device__ __forceinline__ void store_sector(uint16_t* to, const uint32_t (&w)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
@@ -308,39 +332,36 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
           um::ld32(tS, s);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {  // 16 rows; the logits are all read before any is written over
-            uint32_t r[16], pw[8], ew[8], qw[8];
+            uint32_t r[16];
             um::ld16(tS + 64u + 16u * h, r);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const float4 l4 = *reinterpret_cast<const float4*>(nlse + 16 * h + 4 * c);
-              const float4 d4 = *reinterpret_cast<const float4*>(ndelta + 16 * h + 4 * c);
+            for (int c = 0; c < 2; ++c) {  // eight of them
+              uint32_t p1[4], p2[4], e1[4], e2[4], q1[4], q2[4];
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int q = 4 * c + 2 * i;
+              for (int i = 0; i < 4; ++i) {
+                const int q = 8 * c + 2 * i;
+                const float2 l = *reinterpret_cast<const float2*>(nlse + 16 * h + q);
                 float2 e = make_float2(__uint_as_float(s[16 * h + q]), __uint_as_float(s[16 * h + q + 1]));
                 float2 d = make_float2(__uint_as_float(r[q]), __uint_as_float(r[q + 1]));
-                e = ffma2(e, ksl, i ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y));
-                d = kQuant ? ffma2(d, vs, i ? make_float2(d4.z, d4.w) : make_float2(d4.x, d4.y))
-                           : fadd2(d, i ? make_float2(d4.z, d4.w) : make_float2(d4.x, d4.y));
-                e.x = um::ex2(e.x);
-                e.y = um::ex2(e.y);
-                d = fmul2(e, d);
-                pw[2 * c + i] = live ? gt::pack2(e.x, e.y) : 0u;
-                ew[2 * c + i] = live ? gt::pack2(d.x, d.y) : 0u;
-                if (FUSED && kQuant) {
-                  d = fmul2(d, ks);
-                  qw[2 * c + i] = live ? gt::pack2(d.x, d.y) : 0u;
-                }
+                const float2 nd = *reinterpret_cast<const float2*>(ndelta + 16 * h + q);
+                e = ffma2(e, ksl, l);
+                d = kQuant ? ffma2(d, vs, nd) : fadd2(d, nd);
+                e.x = live ? um::ex2(e.x) : 0.f;
+                e.y = live ? um::ex2(e.y) : 0.f;
+                d = live ? fmul2(e, d) : make_float2(0.f, 0.f);
+                split(e, p1[i], p2[i]);
+                split(d, e1[i], e2[i]);
+                if (FUSED && kQuant) split(fmul2(d, ks), q1[i], q2[i]);
               }
-            }
-            um::st8(tS + 8u * h, pw);
-            um::st8(tS + 16u + 8u * h, ew);
-            if (FUSED) {
-              const uint32_t to = base + P::kEOff + (uint32_t)row * 128u;
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const uint32_t* w = kQuant ? &qw[4 * c] : &ew[4 * c];
-                sts128(to + (uint32_t)(((4 * half + 2 * h + c) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+              um::st4(tS + 8u * h + 4u * c, p1);
+              um::st4(tS + 16u + 8u * h + 4u * c, e1);
+              um::st4(tS + 64u + 16u * h + 4u * c, p2);
+              um::st4(tS + 72u + 16u * h + 4u * c, e2);
+              if (FUSED) {
+                const uint32_t to = base + P::kEOff + (uint32_t)(row * 128 + (((4 * half + 2 * h + c) ^ (row & 7)) << 4));
+                const uint32_t *a = kQuant ? q1 : e1, *b = kQuant ? q2 : e2;
+                sts128(to, a[0], a[1], a[2], a[3]);
+                sts128(to + kHalf, b[0], b[1], b[2], b[3]);
               }
             }
           }
@@ -377,69 +398,69 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
       // a warp's slots are half a page's
       const int s = k * kGradTile + quad * 32;
       const int page = s < count ? __ldg(p.st.table + (int64_t)now.u * p.st.max_pages + s / kPage) : -1;
-      ok = ok && gt::wait_all(GRAD_AT(o_full), t & 1u, GRAD_AT(abort));
-      um::fence_after();
-      const bool good = ok && !gt::aborted(GRAD_AT(abort));
       const int rows = page >= 0 && page < p.st.pool_pages ? min(count - s, 32) : 0;
       const int64_t first = ((int64_t)page * kPage + s % kPage) * kD;
-      if constexpr (P::kLines) {
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {  // half a row of dV or dK: written by slot, read by line
-          const bool key = c >= 2;
-          const int d0 = 64 * (c & 1);
-          const float f = key ? p.scale : 1.f;
+      for (int key = 0; key < 2; ++key) {  // dV, then dK
+        ok = ok && gt::wait_all(GRAD_AT(o_full) + 8u * key, t & 1u, GRAD_AT(abort));
+        um::fence_after();
+        const bool good = ok && !gt::aborted(GRAD_AT(abort));
+        const uint32_t from = tmem + at + (key ? kColK : kColV);
+        uint16_t* to = (key ? p.dks : p.dvs) + first;
+        const float f = key ? p.scale : 1.f;
+        if constexpr (P::kLines) {
+#pragma unroll 1
+          for (int d0 = 0; d0 < kD; d0 += 64) {  // half a row: written by slot, read by line
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t r[32];
-            um::ld32(tmem + at + (key ? kColK : kColV) + (uint32_t)(d0 + 32 * h), r);
+            for (int h = 0; h < 2; ++h) {
+              uint32_t r[32];
+              um::ld32(from + (uint32_t)(d0 + 32 * h), r);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              uint32_t w[4];
+              for (int x = 0; x < 4; ++x) {
+                uint32_t w[4];
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-                w[q] = good ? gt::pack2(__uint_as_float(r[8 * x + 2 * q]) * f, __uint_as_float(r[8 * x + 2 * q + 1]) * f)
-                            : 0x7fc07fc0u;
-              sts128(mine + (uint32_t)(lane * 128 + (((4 * h + x) ^ (lane & 7)) << 4)), w[0], w[1], w[2], w[3]);
+                for (int q = 0; q < 4; ++q)
+                  w[q] = good ? gt::pack2(__uint_as_float(r[8 * x + 2 * q]) * f, __uint_as_float(r[8 * x + 2 * q + 1]) * f)
+                              : 0x7fc07fc0u;
+                sts128(mine + (uint32_t)(lane * 128 + (((4 * h + x) ^ (lane & 7)) << 4)), w[0], w[1], w[2], w[3]);
+              }
             }
+            __syncwarp();
+            uint16_t* out = to + d0 + 8 * (lane & 7);
+#pragma unroll 4
+            for (int x = 0; x < 8; ++x) {
+              const int row = 4 * x + (lane >> 3);
+              const float4 v = gt::lds128(mine + (uint32_t)(row * 128 + (((lane & 7) ^ (row & 7)) << 4)));
+              if (row < rows) *reinterpret_cast<float4*>(out + row * kD) = v;
+            }
+            __syncwarp();
           }
-          __syncwarp();
-          uint16_t* out = (key ? p.dks : p.dvs) + first + d0 + 8 * (lane & 7);
+        } else {
+#pragma unroll 1
+          for (int d0 = 0; d0 < kD; d0 += 16) {  // a sector of a slot a thread
+            uint32_t r[16], w[8];
+            um::ld16(from + (uint32_t)d0, r);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const int row = 4 * x + (lane >> 3);
-            const float4 v = gt::lds128(mine + (uint32_t)(row * 128 + (((lane & 7) ^ (row & 7)) << 4)));
-            if (row < rows) *reinterpret_cast<float4*>(out + row * kD) = v;
+            for (int q = 0; q < 8; ++q)
+              w[q] = good ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : 0x7fc07fc0u;
+            if (lane < rows) store_sector(to + lane * kD + d0, w);
           }
-          __syncwarp();
         }
-      } else {
+        if (FUSED && key && p.dq.p && k + 1 == now.kb) {  // element tid of every row
+          float* out = grad_record(p, share, now.u, 0) + grad_at(p, 0, tid);
 #pragma unroll 1
-        for (int c = 0; c < 16; ++c) {  // a sector of a slot a thread
-          const bool key = c >= 8;
-          const int d0 = 16 * (c & 7);
-          uint32_t r[16], w[8];
-          um::ld16(tmem + at + (key ? kColK : kColV) + (uint32_t)d0, r);
-          const float f = key ? p.scale : 1.f;
+          for (int r0 = 0; r0 < p.rows; r0 += 16) {
+            uint32_t r[16];
+            um::ld16(tmem + at + kColQ + (uint32_t)r0, r);
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            w[q] = good ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : 0x7fc07fc0u;
-          if (lane < rows) store_sector((key ? p.dks : p.dvs) + first + lane * kD + d0, w);
+            for (int q = 0; q < 16; ++q)
+              if (r0 + q < p.rows) out[(r0 + q) * 8] = good ? __uint_as_float(r[q]) : nanf("");
+          }
         }
+        um::fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(GRAD_AT(drained) + 8u * key);
       }
-      if (FUSED && p.dq.p && k + 1 == now.kb) {  // element tid of every row
-        float* out = grad_record(p, share, now.u, 0) + grad_at(p, 0, tid);
-#pragma unroll 1
-        for (int r0 = 0; r0 < p.rows; r0 += 16) {
-          uint32_t r[16];
-          um::ld16(tmem + at + kColQ + (uint32_t)r0, r);
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            if (r0 + q < p.rows) out[(r0 + q) * 8] = good ? __uint_as_float(r[q]) : nanf("");
-        }
-      }
-      um::fence_before();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(GRAD_AT(drained));
     }
   }
 }
@@ -469,8 +490,10 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
       tc::mbar_init(GRAD_AT(b_full) + 8u * (i), 1);
       tc::mbar_init(GRAD_AT(b_empty) + 8u * (i), 1);
     }
-    tc::mbar_init(GRAD_AT(o_full), 1);
-    tc::mbar_init(GRAD_AT(drained), kDrainWarps);
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(GRAD_AT(o_full) + 8u * i, 1);
+      tc::mbar_init(GRAD_AT(drained) + 8u * i, kDrainWarps);
+    }
     tc::mbar_init(GRAD_AT(done), 1);
     gt::sts32(GRAD_AT(abort), 0u);
     gt::sts32(GRAD_AT(last), 0u);

@@ -3,7 +3,7 @@
 // A CTA holds up to 128 query rows of a unit, and their output's gradients, as the M = 128 rows
 // of the MMAs, and walks a share of all tiles of 128 slots:
 //   S = Q K^T,  R = dO V^T,  e = 2^(S - lse) (R - delta),  dQ += e K,
-// with e handed over in tensor memory, over S, as a bf16 part and one of its remainder (2^-15).
+// with e handed over in tensor memory, over S, as a bf16 part and one of its remainder (2^-14).
 // Neither a maximum nor a rescaling is needed, the log-sum-exp is known, so a tile is formed in
 // one pass.
 // Tensor memory: S of even tiles | S of odd tiles | R | dQ, 128 columns each.  S of the next
@@ -243,7 +243,7 @@ __device__ __forceinline__ void columns(uint32_t tS, const uint32_t* r, const ty
       x = fmul2(x, y);
       if constexpr (kQuant) x = fmul2(x, k2);
       // the upper halves as they are, then the upper halves of what that leaves: neither takes a
-      // conversion (2^-15 together, towards 0)
+      // conversion (2^-14 together, towards 0)
       y = fadd2(x, make_float2(-__uint_as_float(__float_as_uint(x.x) & 0xffff0000u),
                                -__uint_as_float(__float_as_uint(x.y) & 0xffff0000u)));
       e[at / 2] = __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632);

@@ -305,8 +305,9 @@ __device__ __forceinline__ void mma_mn(uint32_t d, uint32_t a, uint32_t b, uint3
       ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc)
       : "memory");
 }
-// n <= 4 k-steps of a contraction over 64 rows: A in tensor memory, 16 rows in each 8 of the
-// first 16 columns of every 32; B MN-major.
+// n <= 4 k-steps of a contraction over 64 rows: A in tensor memory, 16 rows in 8 columns from 0, A1,
+// A2 and A3 on; B MN-major.
+template <uint32_t A1, uint32_t A2, uint32_t A3>
 __device__ __forceinline__ void mma_p64(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t id, uint32_t acc, uint32_t n) {
   asm volatile(
       "{\n"
@@ -322,24 +323,24 @@ __device__ __forceinline__ void mma_p64(uint32_t d, uint32_t a, uint32_t b, uint
       "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, p0;\n"
       "setp.gt.u32 pn, %6, 1;\n"
       "and.pred pn, pn, pe;\n"
-      "add.u32 x, %1, 8;\n"
+      "add.u32 x, %1, %7;\n"
       "add.u32 y, %2, 128;\n"
       "mov.b64 db, {y, %3};\n"
       "@pn tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
       "setp.gt.u32 pn, %6, 2;\n"
       "and.pred pn, pn, pe;\n"
-      "add.u32 x, %1, 32;\n"
+      "add.u32 x, %1, %8;\n"
       "add.u32 y, %2, 256;\n"
       "mov.b64 db, {y, %3};\n"
       "@pn tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
       "setp.gt.u32 pn, %6, 3;\n"
       "and.pred pn, pn, pe;\n"
-      "add.u32 x, %1, 40;\n"
+      "add.u32 x, %1, %9;\n"
       "add.u32 y, %2, 384;\n"
       "mov.b64 db, {y, %3};\n"
       "@pn tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %4, po;\n"
       "}\n"
-      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc), "r"(n)
+      ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(id), "r"(acc), "r"(n), "n"(A1), "n"(A2), "n"(A3)
       : "memory");
 }
 
@@ -464,6 +465,11 @@ __device__ __forceinline__ void st16(uint32_t a, const uint32_t (&r)[16]) {
 __device__ __forceinline__ void st8(uint32_t a, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(a), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void st4(uint32_t a, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3])
                : "memory");
 }
 __device__ __forceinline__ void wait_st() {

@@ -16,7 +16,8 @@ def gradients(q, store, counts, hkv, out, lse, dout, k_new=None, v_new=None, mas
 
     Tolerance of an element, as the sum of |terms| with these relative errors:
       2^-8 of the result: its rounding to bf16;
-      2^-8 of each p or e: its rounding to bf16 as a matrix operand;
+      2^-14 of each p or e: a matrix operand in two bf16 parts, either cut off at 8 bits, which
+        leaves 2^-7 of what it stands for;
       of each p 2^-15 mag + 2^-15, mag = scale sum |q k| + |lse|: a logit is an fp32 sum of 128
         products (128 2^-24 of their magnitudes' sum) times a rounded scale less an fp32 lse, and
         the hardware exponential is off by 2^-22;
@@ -38,7 +39,7 @@ def gradients(q, store, counts, hkv, out, lse, dout, k_new=None, v_new=None, mas
     pool = (len(kv[0]), D)
     for n in ("dk_store", "dv_store"):
         res[n] = (np.full(pool, np.nan), np.zeros(pool))
-    U = 2.0 ** -8
+    U, P = 2.0 ** -8, 2.0 ** -14
     for b in range(B):
         see = np.zeros((T, T), bool)
         for t in range(T):
@@ -71,8 +72,8 @@ def gradients(q, store, counts, hkv, out, lse, dout, k_new=None, v_new=None, mas
                     + np.abs(dr)
                 e = scale * p * pull
                 rel = 2.0 ** -15 * (mag + 1)
-                pe = p * (U + rel)
-                ee = np.abs(e) * (U + rel) + scale * p * 2.0 ** -16 * amag
+                pe = p * (P + rel)
+                ee = np.abs(e) * (P + rel) + scale * p * 2.0 ** -16 * amag
                 dq = e @ Kf
                 res["dq"][0][sl] = dq.reshape(T, G, D)
                 res["dq"][1][sl] = (U * np.abs(dq) + ee @ np.abs(Kf)).reshape(T, G, D)
