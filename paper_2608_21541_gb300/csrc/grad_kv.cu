@@ -17,7 +17,7 @@
 // the second block; e times the key's scale is handed over in shared memory for it, in two parts
 // too.  The store is then read once for all gradients, and over bf16 the time is that of its bytes
 // (64 rows over 13107 slots of 256 segments: 3.4 GB in 528 us, 96 % of a copy's rate; 8- and 4-bit
-// 587 and 583 us, the pace of writing four and eight times the bytes read).  Reading it again for
+// 587 and 583 us, the pace of writing two and four times the bytes read).  Reading it again for
 // the queries' kernel would cost as much as reading it here.
 //
 // Every wait is bounded; on a timeout the roles stop waiting, the rows and slots in question get

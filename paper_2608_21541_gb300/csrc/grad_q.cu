@@ -12,7 +12,7 @@
 //
 // bf16 stores are bound by their bytes (64 rows over 13107 slots of 256 segments: 1.72 GB in
 // 274 us, 92 % of a copy's rate), 8- and 4-bit ones by the softmax beside the expanding of codes
-// (331 and 338 us; the products of 128 rows, half of them empty there, take 235).
+// (315 and 324 us; the products of 128 rows, half of them empty there, take 235).
 //
 // 8- and 4-bit stores: codes are exact in bf16 (gt::codes_to_bf16); a key's fp32 scale multiplies
 // its logit and its e, a value's its R, all in fp32.  The scale comes times that of the logits,
