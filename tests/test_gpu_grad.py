@@ -280,6 +280,27 @@ def test_streams_graphs_and_a_shared_workspace():
             assert torch.equal(got["dk_new"], want["dk"]) and torch.equal(got["dv_new"], want["dv"])
 
 
+def test_two_calls_at_once():
+    """Calls on two streams with a workspace each, over one store and over two, equal calls alone."""
+    st, n = store_with([900, 90], 1, 2, 2, "fp8", 370)
+    other, m = store_with([40, 700], 1, 2, 2, "bf16", 371)
+    work = [(st, step(st, 1, 2, 2, 4, 40, seed=1)), (st, step(st, 1, 2, 2, 4, 7, seed=2)),
+            (other, step(other, 1, 2, 2, 4, 40, seed=3)), (other, step(other, 1, 2, 2, 2, 20, seed=4))]
+    want = [grads(s, x, 2) for s, x in work]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for a, b in ((0, 1), (0, 2), (1, 3), (2, 3)):
+        got = {}
+        for _ in range(4):
+            for i, on in ((a, streams[0]), (b, streams[1])):
+                with torch.cuda.stream(on):
+                    got[i] = grads(work[i][0], work[i][1], 2)
+        torch.cuda.synchronize()
+        for i in (a, b):
+            for name in want[i]:
+                assert torch.equal(got[i][name], want[i][name]), (a, b, name)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("units,G,T", [(300, 4, 1), (300, 4, 5), (700, 2, 64), (40, 16, 64)])
 def test_many_segments(fmt, units, G, T):
