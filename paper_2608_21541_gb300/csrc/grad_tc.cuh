@@ -316,11 +316,10 @@ struct Copier {
 // 8- and 4-bit stores: the codes of a tile's values and of its keys on their way into a stretch of
 // shared memory each, page by page, by one lane's bulk copies; eight warps expand them into the
 // rings' operands, rows that are not live as zeros, codes as bf16 without their row's scale.  All
-// eight at one operand, since the way from a free place to the next product is what a tile
-// waits for; the keys a tile ahead of the values, whose products come later.  The loop that expands is short:
-// straight-line code for a whole tile, with the codes in registers, took the instruction caches
-// of an SM more time than all else (8-bit 395 -> 700 us with two tiles in registers).  Codes
-// copied 16 bytes at a time by the expanding warps took them 1400 clocks a tile to ask for.
+// eight at one operand, since the way from a free place to the next product is what a tile waits
+// for (8-bit trees 203 us, 222 with four each for keys and for values), and one body for both: code
+// for whole tiles in registers took the instruction caches of an SM more time than all else (395 and
+// 700 us).  Codes copied 16 bytes at a time by the expanding warps took 1400 clocks a tile to ask for.
 template <int FMT>
 struct Stages {
   static constexpr uint32_t kPageCodes = kPage * row_bytes(FMT), kPageGroups = FMT == CERTKV_STORE_FP4 ? kPage * kGroups : 0;
@@ -454,7 +453,7 @@ struct Expander {
       const uint32_t from = st.at + value * kStage<FMT>, to = ring.at + place * kOperand;
       if (!wait_all(st.full + 8 * value, t & 1u, abort)) break;
       const int la = (int)lds32(st.live + 8 * value), lb = kPage + (int)lds32(st.live + 8 * value + 4);
-      uint32_t c[kMine][kWords], g[kMine];
+      uint32_t c[kMine][kWords], g[kMine] = {};
 #pragma unroll
       for (int q = 0; q < kMine; ++q) piece(from, pc.grp + kApart * q, pc.sub, c[q], g[q]);
       __syncwarp();
