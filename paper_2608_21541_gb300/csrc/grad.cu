@@ -237,9 +237,77 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(on ? 16 : 0) : "memory");
 }
 
+// N elements from d0 on of dq of a warp's 16 rows, from s0 on: what the shares left of them, all
+// loads of a share under way, and the drafts' part.
+template <int TD, int N>
+__device__ __forceinline__ void drafts_dq(const GradArgs& p, const GradUnit& x, int u, int r0, int rows, int s0, int d0,
+                                          uint32_t base) {
+  using D = Drafts<TD>;
+  const int lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
+  const int lr = lane & 7, l8 = lane >> 3 & 1, l16 = lane >> 4;
+  float acc[N / 8][4];
+  const Records part(p, u, p.folded);
+  const float* from[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int br = min(r0 + s0 + g8 + 8 * h, p.rows - 1), blk = br / p.rb;
+    from[h] = grad_record(p, part.c0, u, blk) + grad_at(p, br - blk * p.rb, d0 + 2 * t4);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int n = 0; n < N / 8; ++n) {
+      const float2 y = part.c0 <= part.c1 ? __ldcg(reinterpret_cast<const float2*>(from[h] + n * p.rb * 8)) : make_float2(0.f, 0.f);
+      acc[n][2 * h] = y.x, acc[n][2 * h + 1] = y.y;
+    }
+  const int64_t share = (int64_t)p.nblk * p.rb * kD;
+#pragma unroll 1
+  for (int i = part.c0 + 1; i <= part.c1; ++i) {
+    float2 y[2][N / 8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      from[h] += share;
+#pragma unroll
+      for (int n = 0; n < N / 8; ++n) y[h][n] = __ldcg(reinterpret_cast<const float2*>(from[h] + n * p.rb * 8));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int n = 0; n < N / 8; ++n) acc[n][2 * h] += y[h][n].x, acc[n][2 * h + 1] += y[h][n].y;
+  }
+#pragma unroll
+  for (int k = 0; k < TD / 16; ++k) {
+    uint32_t a[4], ar[4];
+    const uint32_t at = base + (uint32_t)(D::kEOff + (s0 + lr + 8 * l8) * D::kWide + 32 * k + 16 * l16);
+    ldm4(at, a);
+    ldm4(at + D::kRest, ar);
+#pragma unroll
+    for (int d = 0; d < N / 16; ++d) {
+      uint32_t b[4];
+      ldm4t(base + (uint32_t)(D::kKeyOff + (16 * k + lr + 8 * l8) * kPitch + 2 * d0 + 32 * d + 16 * l16), b);
+      mma(acc[2 * d], a, b[0], b[1]);
+      mma(acc[2 * d + 1], a, b[2], b[3]);
+      mma(acc[2 * d], ar, b[0], b[1]);
+      mma(acc[2 * d + 1], ar, b[2], b[3]);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int br = r0 + s0 + g8 + 8 * h, tok = br / p.G;
+    if (s0 + g8 + 8 * h >= rows) continue;
+    uint16_t* out = p.dq.at(x.b, x.l, tok, x.h * p.G + br - tok * p.G) + d0 + 2 * t4;
+#pragma unroll
+    for (int n = 0; n < N / 8; ++n)
+      *reinterpret_cast<uint32_t*>(out + 8 * n) = pack2(acc[n][2 * h] * p.scale, acc[n][2 * h + 1] * p.scale);
+  }
+}
+
 // One block per (unit, 128 query rows), on mma.sync: products of at most 128 x 64 x 128, whose
-// time is that of bringing the rows in.  A warp makes p and e of 16 rows and their dq; then each
-// warp 16 elements of dk and dv over all rows.
+// time is that of bringing the rows in.  A warp makes p and e of 16 rows; then each warp 16 elements
+// of dk and dv over all rows; then each its rows' dq.  All but the last runs while the last CTAs of
+// the kernel before, which leave the records, still do (8-bit trees 176 us, 181 behind them): that
+// kernel lets this one start behind its own wait for grad_rows_kernel, whose rows are thus there.
+// Where there is no kernel between the two this one is not started early.
 template <int TD>
 __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_constant__ GradArgs p) {
   using D = Drafts<TD>;
@@ -252,10 +320,8 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
   uint64_t* sees = reinterpret_cast<uint64_t*>(sm + D::kSeenOff);
   unsigned long long* bad = reinterpret_cast<unsigned long long*>(sm + D::kBadOff);
   if (tid == 0) *bad = 0ull;
-  await_previous();
-  release_next();
   if (tid < kChunkRows) {
-    info[tid] = tid < rows ? p.row[(int64_t)u * p.rows + r0 + tid] : make_float2(INFINITY, 0.f);
+    info[tid] = tid < rows ? __ldcg(p.row + (int64_t)u * p.rows + r0 + tid) : make_float2(INFINITY, 0.f);
     sees[tid] = tid < rows && info[tid].x != INFINITY ? grad_seen(p, x.b, (r0 + tid) / p.G) : 0ull;
   }
   __syncthreads();
@@ -302,42 +368,13 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
     }
   }
   const int g8 = lane >> 2, t4 = lane & 3;
-  // dq of a warp's 16 rows begins with what the shares left of it, all its loads under way
-  float acc[kD / 8][4];
-#pragma unroll
-  for (int n = 0; n < kD / 8; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
-  if (p.dq.p && warp < strips) {
-    const Records c(p, u, p.folded);
-    const float* from[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int br = min(r0 + 16 * warp + g8 + 8 * h, p.rows - 1), blk = br / p.rb;
-      from[h] = grad_record(p, c.c0, u, blk) + grad_at(p, br - blk * p.rb, 2 * t4);
-    }
-    const int64_t share = (int64_t)p.nblk * p.rb * kD;
-    for (int i = c.c0; i <= c.c1; ++i) {
-      float2 y[2][kD / 8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int n = 0; n < kD / 8; ++n) y[h][n] = __ldcg(reinterpret_cast<const float2*>(from[h] + n * p.rb * 8));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int n = 0; n < kD / 8; ++n) acc[n][2 * h] += y[h][n].x, acc[n][2 * h + 1] += y[h][n].y;
-        from[h] += share;
-      }
-    }
-  }
   asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
   __syncthreads();
   // lane's address offsets of 16 x 16 blocks: rows as they lie (A), rows as columns of B, and
   // transposed (B from [k][n], A from [k][m])
   const int lr = lane & 7, l8 = lane >> 3 & 1, l16 = lane >> 4;
+  const int s0 = 16 * warp;
   if (warp < strips) {
-    const int s0 = 16 * warp;
     float s[TD / 8][4], r[TD / 8][4];
 #pragma unroll
     for (int n = 0; n < TD / 8; ++n)
@@ -364,7 +401,6 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
     const unsigned long long odd = *bad;
     const float2 i0 = info[s0 + g8], i1 = info[s0 + g8 + 8];
     const uint64_t see0 = sees[s0 + g8], see1 = sees[s0 + g8 + 8];
-    uint32_t e[TD / 8][2], rest[TD / 8][2];
 #pragma unroll
     for (int n = 0; n < TD / 8; ++n) {
       float pr[4], er[4];
@@ -376,99 +412,87 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
         pr[i] = on ? (odd >> j & 1u ? nanf("") : exp2f(fmaf(s[n][i], p.scale_log2, -inf.x))) : 0.f;
         er[i] = on ? pr[i] * (r[n][i] - inf.y) : 0.f;
       }
-      e[n][0] = pack2(er[0], er[1]);
-      e[n][1] = pack2(er[2], er[3]);
-      rest[n][0] = pack2(er[0] - bf16lo(e[n][0]), er[1] - bf16hi(e[n][0]));
-      rest[n][1] = pack2(er[2] - bf16lo(e[n][1]), er[3] - bf16hi(e[n][1]));
       const int at = (s0 + g8) * D::kWide + 16 * n + 4 * t4;
       const uint32_t p0 = pack2(pr[0], pr[1]), p1 = pack2(pr[2], pr[3]);
+      const uint32_t e0 = pack2(er[0], er[1]), e1 = pack2(er[2], er[3]);
       auto put = [&](int off, uint32_t lo, uint32_t hi) {
         *reinterpret_cast<uint32_t*>(sm + off + at) = lo;
         *reinterpret_cast<uint32_t*>(sm + off + at + 8 * D::kWide) = hi;
       };
       put(D::kPOff, p0, p1);
       put(D::kPOff + D::kRest, pack2(pr[0] - bf16lo(p0), pr[1] - bf16hi(p0)), pack2(pr[2] - bf16lo(p1), pr[3] - bf16hi(p1)));
-      put(D::kEOff, e[n][0], e[n][1]);
-      put(D::kEOff + D::kRest, rest[n][0], rest[n][1]);
+      put(D::kEOff, e0, e1);
+      put(D::kEOff + D::kRest, pack2(er[0] - bf16lo(e0), er[1] - bf16hi(e0)), pack2(er[2] - bf16lo(e1), er[3] - bf16hi(e1)));
     }
-    if (p.dq.p) {
+  }
+  __syncthreads();
+  if (p.dkn.p) {
+    float dk[TD / 16][2][4], dv[TD / 16][2][4];
 #pragma unroll
-      for (int d = 0; d < kD / 16; ++d)
+    for (int i = 0; i < TD / 16; ++i)
 #pragma unroll
-        for (int k = 0; k < TD / 16; ++k) {
-          const uint32_t a[4] = {e[2 * k][0], e[2 * k][1], e[2 * k + 1][0], e[2 * k + 1][1]};
-          const uint32_t ar[4] = {rest[2 * k][0], rest[2 * k][1], rest[2 * k + 1][0], rest[2 * k + 1][1]};
-          uint32_t b[4];
-          ldm4t(base + (uint32_t)(D::kKeyOff + (16 * k + lr + 8 * l8) * kPitch + 32 * d + 16 * l16), b);
-          mma(acc[2 * d], a, b[0], b[1]);
-          mma(acc[2 * d + 1], a, b[2], b[3]);
-          mma(acc[2 * d], ar, b[0], b[1]);
-          mma(acc[2 * d + 1], ar, b[2], b[3]);
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) dk[i][n][k] = dv[i][n][k] = 0.f;
+    for (int k = 0; k < strips; ++k) {
+      uint32_t bq[4], bg[4];
+      const uint32_t at = base + (uint32_t)((16 * k + lr + 8 * l8) * kPitch + 32 * warp + 16 * l16);
+      ldm4t(at + D::kRowOff, bq);
+      ldm4t(at + D::kGradOff, bg);
+#pragma unroll
+      for (int i = 0; i < TD / 16; ++i) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          uint32_t ap[4], ae[4];
+          const uint32_t to = base + (uint32_t)(part * D::kRest + (16 * k + lr + 8 * l16) * D::kWide + 32 * i + 16 * l8);
+          ldm4t(to + D::kPOff, ap);
+          ldm4t(to + D::kEOff, ae);
+          mma(dv[i][0], ap, bg[0], bg[1]);
+          mma(dv[i][1], ap, bg[2], bg[3]);
+          mma(dk[i][0], ae, bq[0], bq[1]);
+          mma(dk[i][1], ae, bq[2], bq[3]);
         }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TD / 16; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int br = r0 + s0 + g8 + 8 * h, tok = br / p.G;
-        if (s0 + g8 + 8 * h >= rows) continue;
-        uint16_t* out = p.dq.at(x.b, x.l, tok, x.h * p.G + br - tok * p.G) + 2 * t4;
+        const int j = 16 * i + g8 + 8 * h;
+        if (j >= p.T) continue;
 #pragma unroll
-        for (int n = 0; n < kD / 8; ++n)
-          *reinterpret_cast<uint32_t*>(out + 8 * n) = pack2(acc[n][2 * h] * p.scale, acc[n][2 * h + 1] * p.scale);
-      }
-    }
-  }
-  if (!p.dkn.p) return;
-  __syncthreads();
-  float dk[TD / 16][2][4], dv[TD / 16][2][4];
-#pragma unroll
-  for (int i = 0; i < TD / 16; ++i)
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) dk[i][n][k] = dv[i][n][k] = 0.f;
-  for (int k = 0; k < strips; ++k) {
-    uint32_t bq[4], bg[4];
-    const uint32_t at = base + (uint32_t)((16 * k + lr + 8 * l8) * kPitch + 32 * warp + 16 * l16);
-    ldm4t(at + D::kRowOff, bq);
-    ldm4t(at + D::kGradOff, bg);
-#pragma unroll
-    for (int i = 0; i < TD / 16; ++i) {
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        uint32_t ap[4], ae[4];
-        const uint32_t to = base + (uint32_t)(part * D::kRest + (16 * k + lr + 8 * l16) * D::kWide + 32 * i + 16 * l8);
-        ldm4t(to + D::kPOff, ap);
-        ldm4t(to + D::kEOff, ae);
-        mma(dv[i][0], ap, bg[0], bg[1]);
-        mma(dv[i][1], ap, bg[2], bg[3]);
-        mma(dk[i][0], ae, bq[0], bq[1]);
-        mma(dk[i][1], ae, bq[2], bq[3]);
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < TD / 16; ++i)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int j = 16 * i + g8 + 8 * h;
-      if (j >= p.T) continue;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int d = 16 * warp + 8 * n + 2 * t4;
-        if (p.chunks == 1) {
-          *reinterpret_cast<uint32_t*>(p.dkn.at(x.b, x.l, j, x.h) + d) =
-              pack2(dk[i][n][2 * h] * p.scale, dk[i][n][2 * h + 1] * p.scale);
-          *reinterpret_cast<uint32_t*>(p.dvn.at(x.b, x.l, j, x.h) + d) = pack2(dv[i][n][2 * h], dv[i][n][2 * h + 1]);
-        } else {
-          float* o = p.part + (((int64_t)u * p.chunks + chunk) * 2 * p.T + j) * kD + d;
-          *reinterpret_cast<float2*>(o) = make_float2(dk[i][n][2 * h], dk[i][n][2 * h + 1]);
-          *reinterpret_cast<float2*>(o + (int64_t)p.T * kD) = make_float2(dv[i][n][2 * h], dv[i][n][2 * h + 1]);
+        for (int n = 0; n < 2; ++n) {
+          const int d = 16 * warp + 8 * n + 2 * t4;
+          if (p.chunks == 1) {
+            *reinterpret_cast<uint32_t*>(p.dkn.at(x.b, x.l, j, x.h) + d) =
+                pack2(dk[i][n][2 * h] * p.scale, dk[i][n][2 * h + 1] * p.scale);
+            *reinterpret_cast<uint32_t*>(p.dvn.at(x.b, x.l, j, x.h) + d) = pack2(dv[i][n][2 * h], dv[i][n][2 * h + 1]);
+          } else {
+            float* o = p.part + (((int64_t)u * p.chunks + chunk) * 2 * p.T + j) * kD + d;
+            *reinterpret_cast<float2*>(o) = make_float2(dk[i][n][2 * h], dk[i][n][2 * h + 1]);
+            *reinterpret_cast<float2*>(o + (int64_t)p.T * kD) = make_float2(dv[i][n][2 * h], dv[i][n][2 * h + 1]);
+          }
         }
       }
-    }
+  }
+  await_previous();  // the records
+  release_next();
+  if (!p.dq.p) return;
+  // a strip's elements shared out over the warps that have none of their own (1 token x 4 heads in a
+  // graph: 21 -> 15 us)
+  if (strips > 4) {
+    if (warp < strips) drafts_dq<TD, 128>(p, x, u, r0, rows, 16 * warp, 0, base);
+  } else if (strips > 2) {
+    if (warp / 2 < strips) drafts_dq<TD, 64>(p, x, u, r0, rows, 16 * (warp / 2), 64 * (warp & 1), base);
+  } else if (strips > 1) {
+    drafts_dq<TD, 32>(p, x, u, r0, rows, 16 * (warp / 4), 32 * (warp & 3), base);
+  } else {
+    drafts_dq<TD, 16>(p, x, u, r0, rows, 0, 16 * warp, base);
+  }
 }
 
 template <int TD>
-bool launch_drafts(const GradArgs& p, cudaStream_t st) {
+bool launch_drafts(const GradArgs& p, bool early, cudaStream_t st) {
   constexpr int bytes = Drafts<TD>::kBytes;
   static_assert(bytes <= 232448, "over the 227 KB of shared memory a CTA can have");
   static std::atomic<uint64_t> ready{0};  // devices on which the shared memory is opted in to
@@ -479,7 +503,7 @@ bool launch_drafts(const GradArgs& p, cudaStream_t st) {
       return false;
     if (dev < 64) ready.fetch_or(1ull << dev);
   }
-  return launch_kernel(true, grad_drafts_kernel<TD>, (unsigned)((int64_t)p.units * p.chunks), kThreads, bytes, st, p);
+  return launch_kernel(early, grad_drafts_kernel<TD>, (unsigned)((int64_t)p.units * p.chunks), kThreads, bytes, st, p);
 }
 
 int grad_shape(const certkv_shape* s, int32_t tokens) {
@@ -617,7 +641,8 @@ extern "C" int certkv_tree_attn_grad(const certkv_shape* shape, int32_t tokens, 
   }
   if (p.kn.p && (p.dq.p || p.dkn.p)) {
     TraceScope ts_("grad_drafts", st);
-    if (!(tokens <= 16 ? launch_drafts<16>(p, st) : launch_drafts<64>(p, st))) return cuda_failed();
+    const bool early = p.dks || p.dq.p;
+    if (!(tokens <= 16 ? launch_drafts<16>(p, early, st) : launch_drafts<64>(p, early, st))) return cuda_failed();
   }
   const int64_t w = p.kn.p ? (p.dkn.p && p.chunks > 1 ? 2 * (int64_t)p.units * tokens : 0) : p.dq.p ? n : 0;
   if (w > 0) {

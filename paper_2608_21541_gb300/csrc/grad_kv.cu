@@ -499,8 +499,8 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
     gt::sts32(GRAD_AT(last), 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  release_next();
   await_previous();
+  release_next();  // behind the wait: what it starts reads what was waited for here
   const int share = blockIdx.x;
   const gt::Walk walk = gt::Walk::of(p, share);
   if (walk.left == 0) return;  // uniform, before any barrier

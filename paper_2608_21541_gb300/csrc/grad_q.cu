@@ -370,8 +370,8 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
     gt::sts32(GRAD_AT(last), 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  release_next();
   await_previous();
+  release_next();  // behind the wait: what it starts reads what was waited for here
   const int share = blockIdx.x / p.nblk, blk = blockIdx.x - share * p.nblk;
   const gt::Walk walk = gt::Walk::of(p, share);
   if (walk.left == 0) return;  // uniform, before any barrier
