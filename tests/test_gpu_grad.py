@@ -309,6 +309,33 @@ def test_many_segments(fmt, units, G, T):
     run(st, n, 1, 1, units, G, T)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T,G", [(64, 32), (63, 31), (64, 17), (17, 32)])
+def test_most_rows(fmt, T, G):
+    """As many query rows of a segment as there may be, and some fewer."""
+    st, n = store_with([0, 129, 400], 1, 1, 3, fmt, 380)
+    run(st, n, 1, 1, 3, G, T, mask=words(1, T, 8))
+    run(st, n, 1, 1, 3, G, T, new=False, pools=False)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("T", [5, 40])
+def test_broadcast_inputs(fmt, T):
+    """Inputs that repeat along a dimension of stride 0: their gradients come whole, as those of
+    copies."""
+    st, n = store_with([200, 61], 2, 1, 2, fmt, 390)
+    x = step(st, 2, 1, 2, 4, T, seed=5)
+    x["dout"] = randn((2, 1, 1, 1, 128), 391).expand(2, 1, T, 8, 128)
+    x["q"] = randn((1, 1, T, 8, 128), 392).expand(2, 1, T, 8, 128)
+    x["k_new"] = randn((2, 1, 1, 2, 128), 393).expand(2, 1, T, 2, 128)
+    x["out"] = ck.certkv_tree_attn(x["q"], st, hkv=2, k_new=x["k_new"], v_new=x["v_new"], lse=x["lse"])
+    got = grads(st, x, 2)
+    check(st, n, x, 2, got)
+    y = dict(x, **{a: x[a].contiguous() for a in ("dout", "q", "k_new")})
+    want = grads(st, y, 2)
+    assert all(torch.equal(got[a], want[a]) for a in want)
+
+
 def test_thousands_of_segments():
     """More than one pass of the scan over their tiles."""
     st, n = store_with([0, 3, 64, 130, 1, 200, 5], 1, 9, 1000, "bf16", 315)
