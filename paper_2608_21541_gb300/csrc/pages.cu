@@ -315,7 +315,8 @@ struct MapArgs {
   const int32_t *rows, *start, *base;
   const uint64_t* mask;
   int32_t *slots, *positions;
-  int64_t chunks;  // warps (step) or blocks, of all segments
+  int per;         // warps (step) or blocks of a segment
+  int64_t chunks;  // of all segments
 };
 // Position e of the output, if there is one.
 __device__ __forceinline__ void position(const MapArgs& p, int64_t e) {
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(kThreads) slot_map_step_kernel(const MapArgs p
   const int64_t w = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
   if (w < p.chunks) {
-    const int per = (p.tokens + 31) / 32, u = (int)(w / per), i = (int)(w - (int64_t)u * per) * 32 + lane;
+    const int u = (int)(w / p.per), i = (int)(w - (int64_t)u * p.per) * 32 + lane;
     const int n = p.rows ? min(max(p.rows[u / p.per_seq], 0), p.tokens) : p.tokens;
     if (i >= p.tokens) return;
     int64_t at = -1;
@@ -359,8 +360,7 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const MapArgs p) {
     position(p, (blockIdx.x - p.chunks) * kThreads + threadIdx.x);
     return;
   }
-  const int per = (p.tokens + kRows - 1) / kRows + (p.tokens % 4 != 0);  // one more: parts begin up to 3 rows early
-  const int u = (int)(blockIdx.x / per), part = (int)(blockIdx.x - (int64_t)u * per);
+  const int u = (int)(blockIdx.x / p.per), part = (int)(blockIdx.x - (int64_t)u * p.per);
   const int n = p.rows ? min(max(p.rows[u / p.per_seq], 0), p.tokens) : p.tokens;
   const int64_t start = p.start ? p.start[u] : p.st.counts[u], most = (int64_t)p.st.max_pages * kPage;
   // rows [lo, hi) have a place in the table
@@ -535,8 +535,11 @@ extern "C" int certkv_slot_map(int32_t batch, int32_t tokens, const int32_t* row
   p.slots = slots;
   p.positions = positions;
   const bool step = tokens <= kStepRows;
-  const int64_t each = step ? (tokens + 31) / 32 : (tokens + kRows - 1) / kRows + (tokens % 4 != 0);
-  p.chunks = slots ? p.st.units * each : 0;
+  // one block more where a segment's entries do not begin on a 16-byte boundary: its parts then
+  // begin up to 3 rows early
+  const bool early = tokens % 4 != 0 || (uintptr_t)slots % 16 != 0;
+  p.per = step ? (tokens + 31) / 32 : (tokens + kRows - 1) / kRows + early;
+  p.chunks = slots ? (int64_t)p.st.units * p.per : 0;
   const int64_t rest = positions ? (int64_t)batch * tokens : 0, per_warp = kThreads / 32;
   const int64_t blocks = step ? (p.chunks + (rest + 31) / 32 + per_warp - 1) / per_warp
                               : p.chunks + (rest + kThreads - 1) / kThreads;
