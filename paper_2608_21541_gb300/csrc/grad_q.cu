@@ -71,7 +71,7 @@ struct Misc {
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   int2 live[2];  // of the stretches
   uint32_t tmem;
-  int abort, last;  // last: a flag that nobody sets
+  int abort;
   alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kFacts];
 };
 template <int FMT>
@@ -103,7 +103,7 @@ struct RowFeeder {
         tc::bulk_load(base + part * kHalf, grad_pack(p, it.u, part, blk * p.rb), bytes, GRAD_AT(q_full));
       ++n;
     }
-    if (n > 0) gt::wait(GRAD_AT(q_full), (n - 1) & 1u, GRAD_AT(last));  // nothing lands after the CTA has gone
+    if (n > 0) gt::finish(GRAD_AT(q_full), (n - 1) & 1u);  // nothing lands after the CTA has gone
   }
 };
 
@@ -205,7 +205,8 @@ struct Issuer {
       ++item;
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
-    gt::wait_all(GRAD_AT(done), 0, GRAD_AT(last));
+    gt::finish(GRAD_AT(done), 0);
+    __syncwarp();
   }
 };
 
@@ -367,7 +368,6 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
     tc::mbar_init(GRAD_AT(o_full), 1);
     tc::mbar_init(GRAD_AT(done), 1);
     gt::sts32(GRAD_AT(abort), 0u);
-    gt::sts32(GRAD_AT(last), 0u);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   await_previous();
@@ -393,10 +393,10 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       gt::Expander<FMT, P::kKeys, P::kValues> f{keys, values, stages, GRAD_AT(abort), tid};
       f.run(walk);
     } else if (tid < kGroupWarps * 32) {
-      gt::Copier<P::kKeys, true> f{&tmK, p, keys, GRAD_AT(facts), GRAD_AT(abort), GRAD_AT(last), p.st.k, tid};
+      gt::Copier<P::kKeys, true> f{&tmK, p, keys, GRAD_AT(facts), GRAD_AT(abort), p.st.k, tid};
       f.run(walk);
     } else {
-      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), GRAD_AT(last), p.st.v, tid - kGroupWarps * 32};
+      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), p.st.v, tid - kGroupWarps * 32};
       f.run(walk);
     }
   } else {
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       Issuer<FMT> is{tmem, base};
       is.run(p, walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 1 && threadIdx.x % 32 == 0) {
-      gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(last)};
+      gt::Stager<FMT> f{p, stages, GRAD_AT(abort)};
       f.run(walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 2) {
       gt::FactFeeder<FMT, P::kKeys> f{p, GRAD_AT(f_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort), (int)threadIdx.x & 31};

@@ -5,6 +5,7 @@
 #include <stddef.h>
 
 #include "common.cuh"
+#include "follow.cuh"
 #include "grad.cuh"
 #include "operand.cuh"
 #include "tma.cuh"
@@ -48,6 +49,11 @@ __device__ __forceinline__ bool patience(uint32_t look, uint32_t flag) {
 // The same by a whole warp.
 __device__ __forceinline__ bool wait_all(uint32_t mbar, uint32_t parity, uint32_t flag) {
   return __all_sync(kFull, wait(mbar, parity, flag));
+}
+
+// A role's last wait, for what it has on its way: no flag ends it, and it sets none.
+__device__ __forceinline__ void finish(uint32_t mbar, uint32_t parity) {
+  outlast(tc::kSpinLimit, [&] { return tc::mbar_try(mbar, parity); });
 }
 
 // Shared memory by its address: generic pointers cost two registers each, and a spill next to
@@ -221,7 +227,7 @@ struct Copier {
   const CUtensorMap* map;
   const GradArgs& p;
   Ring ring;
-  uint32_t facts, abort, last;  // facts [PLACES] (FACTS: written by this group); last: a flag that nobody sets
+  uint32_t facts, abort;  // facts [PLACES] (FACTS: written by this group)
   const uint8_t* rows;
   int tid;               // of 128
   uint32_t t = 0;
@@ -309,7 +315,7 @@ struct Copier {
     if (ok && pending) hand_over(t - 1);
     if (tid == 0)
       for (uint32_t i = t > PLACES ? t - PLACES : 0; i < t; ++i)
-        if (bulk >> (i % PLACES) & 1u) wait(ring.full + 8 * (i % PLACES), (i / PLACES) & 1u, last);
+        if (bulk >> (i % PLACES) & 1u) finish(ring.full + 8 * (i % PLACES), (i / PLACES) & 1u);
   }
 };
 
@@ -333,7 +339,7 @@ struct Stager {
   using S = Stages<FMT>;
   const GradArgs& p;
   S st;
-  uint32_t abort, last;
+  uint32_t abort;
 
   // Codes of operand `value` of tile number t on their way.
   __device__ __forceinline__ void page(int pg, int half, bool value) const {
@@ -372,8 +378,8 @@ struct Stager {
       x = y;
     }
     // nothing lands after the CTA has gone
-    if (keys > 0) wait(st.full, (keys - 1) & 1u, last);
-    if (values > 0) wait(st.full + 8, (values - 1) & 1u, last);
+    if (keys > 0) finish(st.full, (keys - 1) & 1u);
+    if (values > 0) finish(st.full + 8, (values - 1) & 1u);
   }
 };
 
