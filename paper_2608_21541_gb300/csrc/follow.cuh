@@ -1,4 +1,4 @@
-// follow.cuh — following a warp that does not wait for its followers, and waiting for one's own.
+// follow.cuh — following a warp that does not wait for its followers, and bounded looking.
 //
 // A phase parity tells only neighbouring phases of a barrier apart, so it can be waited on only
 // by those that the barrier's owner waits for in turn: a follower eight tiles behind, on a ring
@@ -25,14 +25,16 @@ __host__ __device__ inline bool follow(uint32_t t, uint32_t limit, Count count, 
   return false;
 }
 
-// Waits until `done()`: false after `limit` looks.  For what a role has on its way itself at its end:
-// the block's shared memory is another's once it has gone, so nobody else's giving up may cut this
-// short, and giving up here tells nobody.
-template <class Done>
-__host__ __device__ inline bool outlast(uint32_t limit, Done done) {
+// Looks until `done()`: true; false when `stop()` says so, which is asked every 256 looks, or after
+// `limit` of them, and then `give_up()`.
+template <class Done, class Stop, class GiveUp>
+__host__ __device__ inline bool look(uint32_t limit, Done done, Stop stop, GiveUp give_up) {
 #pragma unroll 1
-  for (uint32_t i = 0; i < limit; ++i)
+  for (uint32_t i = 0; i < limit; ++i) {
     if (done()) return true;
+    if ((i & 255u) == 255u && stop()) return false;
+  }
+  give_up();
   return false;
 }
 

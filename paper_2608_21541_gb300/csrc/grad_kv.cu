@@ -75,7 +75,7 @@ struct Misc {
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   int2 live[2];  // of the stretches
   uint32_t tmem;
-  int abort;
+  int abort, own[5];  // own: flags of the issuer, the feeder of rows, the copiers of keys and values, the stager
   alignas(16) float nlse[Plan<FMT, FUSED>::kBlocks][kCols], ndelta[Plan<FMT, FUSED>::kBlocks][kCols];  // negated
 };
 template <int FMT, bool FUSED>
@@ -159,7 +159,7 @@ struct RowFeeder {
         for (int j = 0; ok && j < blocks_of(p); ++j) ok = block(it.u, j);
     }
     for (uint32_t i = n > P::kBlocks ? n - P::kBlocks : 0; i < n; ++i)  // nothing lands after the CTA has gone
-      gt::finish(GRAD_AT(b_full) + 8u * (i % P::kBlocks), (i / P::kBlocks) & 1u);
+      gt::finish(GRAD_AT(b_full) + 8u * (i % P::kBlocks), (i / P::kBlocks) & 1u, GRAD_AT(own) + 4u);
   }
 };
 
@@ -246,7 +246,7 @@ struct Issuer {
       cur = nxt;
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
-    gt::finish(GRAD_AT(done), 0);
+    gt::finish(GRAD_AT(done), 0, GRAD_AT(own));
     __syncwarp();
   }
 };
@@ -525,10 +525,10 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
       gt::Expander<FMT, P::kKeys, P::kValues> f{keys, values, stages, GRAD_AT(abort), tid};
       f.run(walk);
     } else if (tid < kGroupWarps * 32) {
-      gt::Copier<P::kKeys, false> f{&tmK, p, keys, 0u, GRAD_AT(abort), p.st.k, tid};
+      gt::Copier<P::kKeys, false> f{&tmK, p, keys, 0u, GRAD_AT(abort), GRAD_AT(own) + 8u, p.st.k, tid};
       f.run(walk);
     } else {
-      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), p.st.v, tid - kGroupWarps * 32};
+      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), GRAD_AT(own) + 12u, p.st.v, tid - kGroupWarps * 32};
       f.run(walk);
     }
   } else if (warp < kIssue) {
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const __grid_const
       RowFeeder<FMT, FUSED> f{p, base};
       f.run(walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == kIssue + 2 && threadIdx.x % 32 == 0) {
-      gt::Stager<FMT> f{p, stages, GRAD_AT(abort)};
+      gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(own) + 16u};
       f.run(walk);
     }
   }

@@ -71,7 +71,7 @@ struct Misc {
   uint64_t st_full[2], st_empty[2];  // stretches of codes, keys' and values'
   int2 live[2];  // of the stretches
   uint32_t tmem;
-  int abort;
+  int abort, own[5];  // own: flags of the issuer, the feeder of rows, the copiers of keys and values, the stager
   alignas(16) typename gt::FactsOf<FMT>::type facts[Plan<FMT>::kFacts];
 };
 template <int FMT>
@@ -103,7 +103,7 @@ struct RowFeeder {
         tc::bulk_load(base + part * kHalf, grad_pack(p, it.u, part, blk * p.rb), bytes, GRAD_AT(q_full));
       ++n;
     }
-    if (n > 0) gt::finish(GRAD_AT(q_full), (n - 1) & 1u);  // nothing lands after the CTA has gone
+    if (n > 0) gt::finish(GRAD_AT(q_full), (n - 1) & 1u, GRAD_AT(own) + 4u);  // nothing lands after the CTA has gone
   }
 };
 
@@ -205,7 +205,7 @@ struct Issuer {
       ++item;
     }
     um::commit(GRAD_AT(done));  // everything issued above has finished
-    gt::finish(GRAD_AT(done), 0);
+    gt::finish(GRAD_AT(done), 0, GRAD_AT(own));
     __syncwarp();
   }
 };
@@ -393,10 +393,10 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       gt::Expander<FMT, P::kKeys, P::kValues> f{keys, values, stages, GRAD_AT(abort), tid};
       f.run(walk);
     } else if (tid < kGroupWarps * 32) {
-      gt::Copier<P::kKeys, true> f{&tmK, p, keys, GRAD_AT(facts), GRAD_AT(abort), p.st.k, tid};
+      gt::Copier<P::kKeys, true> f{&tmK, p, keys, GRAD_AT(facts), GRAD_AT(abort), GRAD_AT(own) + 8u, p.st.k, tid};
       f.run(walk);
     } else {
-      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), p.st.v, tid - kGroupWarps * 32};
+      gt::Copier<P::kValues, false> f{&tmV, p, values, 0u, GRAD_AT(abort), GRAD_AT(own) + 12u, p.st.v, tid - kGroupWarps * 32};
       f.run(walk);
     }
   } else {
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(Warps<FMT>::kThreads, 1) grad_q_kernel(const _
       Issuer<FMT> is{tmem, base};
       is.run(p, walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 1 && threadIdx.x % 32 == 0) {
-      gt::Stager<FMT> f{p, stages, GRAD_AT(abort)};
+      gt::Stager<FMT> f{p, stages, GRAD_AT(abort), GRAD_AT(own) + 16u};
       f.run(walk);
     } else if (FMT != CERTKV_STORE_BF16 && warp == W::kIssue + 2) {
       gt::FactFeeder<FMT, P::kKeys> f{p, GRAD_AT(f_full), GRAD_AT(k_empty), GRAD_AT(facts), GRAD_AT(abort), (int)threadIdx.x & 31};

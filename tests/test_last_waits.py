@@ -1,6 +1,6 @@
 """The last waits of a block's roles, for the copies that each has on its way itself (csrc/follow.cuh),
-on the CPU: one whose copies never land does not shorten another's.  Beside it what a flag that the
-waits share would have done."""
+on the CPU: with a flag of its own one whose copies never land does not shorten another's, as it would
+with a flag that they share."""
 import os
 import re
 import subprocess
@@ -15,21 +15,20 @@ PROGRAM = r"""
 #include <stdlib.h>
 #include "follow.cuh"
 
-// looks until a role's copies have landed; past the limit they never do
+// one wait after the other, each until a role's copies have landed; past the limit they never do
 int main(int argc, char** argv) {
   const uint32_t limit = atoi(argv[1]);
-  int flag = 0;
+  bool shared = false;
   for (int r = 2; r < argc; ++r) {
     const uint32_t lands = atoi(argv[r]);
-    uint32_t looks = 0;
-    const bool own = certkv::outlast(limit, [&] { return looks++ >= lands; });
-    bool shared = false, gave_up = false;
-    for (uint32_t i = 0; i < limit && !shared && !gave_up; ++i) {
-      shared = i >= lands;
-      if (!shared && (i & 255u) == 255u && flag) gave_up = true;
+    for (int i = 0; i < 2; ++i) {
+      bool own = false;
+      bool& flag = i ? shared : own;
+      uint32_t looks = 0;
+      const bool there = certkv::look(limit, [&] { return looks++ >= lands; }, [&] { return flag; }, [&] { flag = true; });
+      printf("%d %u ", there, looks);
     }
-    if (!shared && !gave_up) flag = 1;
-    printf("%d %u %d\n", own, looks, shared);
+    printf("\n");
   }
 }
 """
@@ -53,14 +52,18 @@ def waits(tmp_path_factory):
 @pytest.mark.parametrize("lands", [0, 1, 255, 256, 257, 3000, 4999])
 def test_a_wait_that_runs_out_does_not_shorten_another(waits, lands):
     first, second = waits(5000, 10 ** 6, lands)
-    assert first == (0, 5000, 0)
+    assert first == (0, 5000, 0, 5000)
     assert second[:2] == (1, lands + 1)
-    assert second[2] == (lands <= 255)  # with a flag between them the second would have gone early
+    assert second[2:] == ((1, lands + 1) if lands <= 255 else (0, 256))  # gone with copies on their way
 
 
-def test_the_gradients_last_waits_take_no_flag():
-    """Every wait for what is on its way at a role's end is of this kind."""
+def test_the_gradients_last_waits_have_flags_of_their_own():
+    """Every wait for what is on its way at a role's end is of this kind, and no two roles of a block
+    have the same flag."""
     for name, count in (("grad_q.cu", 2), ("grad_kv.cu", 2), ("grad_tc.cuh", 3)):
         text = open(os.path.join(CSRC, name)).read()
-        assert len(re.findall(r"(?<!void )\bfinish\([^;]*\);", text)) == count, name
+        assert len(re.findall(r"(?<!void )\bfinish\([^;]*\bown\b[^;]*\);", text)) == count, name
         assert not re.search(r"\bwait(_all)?\([^;]*\blast\b[^;]*\);", text), name
+        if name != "grad_tc.cuh":
+            flags = re.findall(r"GRAD_AT\(own\)( \+ \d+u)?", text)
+            assert len(flags) == len(set(flags)) == 5, name
