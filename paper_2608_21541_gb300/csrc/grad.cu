@@ -181,6 +181,8 @@ __global__ void __launch_bounds__(kThreads) grad_merge_kernel(const __grid_const
     const Records c(p, u, p.folded);
 #pragma unroll 4
     for (int i = c.c0; i <= c.c1; ++i) add4(a, grad_record(p, i, u, blk) + at);
+    // a row that takes no part: its zeros times a slot's NaN or infinity are NaN
+    if (p.row[(int64_t)u * p.rows + r].x == INFINITY) a = make_float4(0.f, 0.f, 0.f, 0.f);
     store4(p.dq.at(x.b, x.l, t, x.h * p.G + g), lane,
            make_float4(a.x * p.scale, a.y * p.scale, a.z * p.scale, a.w * p.scale));
     return;
@@ -238,10 +240,11 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from, bool on) {
 }
 
 // N elements from d0 on of dq of a warp's 16 rows, from s0 on: what the shares left of them, all
-// loads of a share under way, and the drafts' part.
+// loads of a share under way, and the drafts' part.  A row that takes no part gets 0, whatever its
+// zeros made of a slot's NaN or infinity.
 template <int TD, int N>
 __device__ __forceinline__ void drafts_dq(const GradArgs& p, const GradUnit& x, int u, int r0, int rows, int s0, int d0,
-                                          uint32_t base) {
+                                          uint32_t base, const float2* info) {
   using D = Drafts<TD>;
   const int lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
   const int lr = lane & 7, l8 = lane >> 3 & 1, l16 = lane >> 4;
@@ -296,9 +299,10 @@ __device__ __forceinline__ void drafts_dq(const GradArgs& p, const GradUnit& x, 
     const int br = r0 + s0 + g8 + 8 * h, tok = br / p.G;
     if (s0 + g8 + 8 * h >= rows) continue;
     uint16_t* out = p.dq.at(x.b, x.l, tok, x.h * p.G + br - tok * p.G) + d0 + 2 * t4;
+    const bool on = info[s0 + g8 + 8 * h].x != INFINITY;
 #pragma unroll
     for (int n = 0; n < N / 8; ++n)
-      *reinterpret_cast<uint32_t*>(out + 8 * n) = pack2(acc[n][2 * h] * p.scale, acc[n][2 * h + 1] * p.scale);
+      *reinterpret_cast<uint32_t*>(out + 8 * n) = on ? pack2(acc[n][2 * h] * p.scale, acc[n][2 * h + 1] * p.scale) : 0u;
   }
 }
 
@@ -481,13 +485,13 @@ __global__ void __launch_bounds__(kThreads) grad_drafts_kernel(const __grid_cons
   // a strip's elements shared out over the warps that have none of their own (1 token x 4 heads in a
   // graph: 21 -> 15 us)
   if (strips > 4) {
-    if (warp < strips) drafts_dq<TD, 128>(p, x, u, r0, rows, 16 * warp, 0, base);
+    if (warp < strips) drafts_dq<TD, 128>(p, x, u, r0, rows, 16 * warp, 0, base, info);
   } else if (strips > 2) {
-    if (warp / 2 < strips) drafts_dq<TD, 64>(p, x, u, r0, rows, 16 * (warp / 2), 64 * (warp & 1), base);
+    if (warp / 2 < strips) drafts_dq<TD, 64>(p, x, u, r0, rows, 16 * (warp / 2), 64 * (warp & 1), base, info);
   } else if (strips > 1) {
-    drafts_dq<TD, 32>(p, x, u, r0, rows, 16 * (warp / 4), 32 * (warp & 3), base);
+    drafts_dq<TD, 32>(p, x, u, r0, rows, 16 * (warp / 4), 32 * (warp & 3), base, info);
   } else {
-    drafts_dq<TD, 16>(p, x, u, r0, rows, 0, 16 * warp, base);
+    drafts_dq<TD, 16>(p, x, u, r0, rows, 0, 16 * warp, base, info);
   }
 }
 

@@ -380,8 +380,18 @@ __device__ __forceinline__ void softmax(const GradArgs& p, uint32_t base, uint32
   }
 }
 
+// Whether some row of unit u takes part; by a whole warp.
+__device__ __forceinline__ bool takes_part(const GradArgs& p, int u, int lane) {
+  const float* nlse = p.neg + (int64_t)u * 2 * p.padded;
+  bool any = false;
+#pragma unroll 1
+  for (int r = 0; !any && r < p.rows; r += 32) any = __any_sync(kFull, r + lane < p.rows && nlse[r + lane] != -INFINITY);
+  return any;
+}
+
 // The four warps that write a tile's gradients, a slot a thread, while the softmax goes on with
-// the next tile; at an item's end (FUSED) its queries' too.
+// the next tile; at an item's end (FUSED) its queries' too.  Where no row of the segment takes part
+// they are zeros, which the products, of zeros with a slot's NaN or infinity, need not be.
 template <int FMT, bool FUSED>
 __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t tmem, int tid, int share,
                                         gt::Walk walk) {
@@ -397,6 +407,7 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
   while (walk.next(p, &it)) {
     const gt::Item now = it;
     const int count = p.st.count(now.u);
+    const bool any = takes_part(p, now.u, lane);
 #pragma unroll 1
     for (int k = now.ka; k < now.kb; ++k, ++t) {
       // a warp's slots are half a page's
@@ -408,7 +419,8 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
       for (int key = 0; key < 2; ++key) {  // dV, then dK
         ok = ok && gt::wait_all(GRAD_AT(o_full) + 8u * key, t & 1u, GRAD_AT(abort));
         um::fence_after();
-        const bool good = ok && !gt::aborted(GRAD_AT(abort));
+        const bool good = ok && !gt::aborted(GRAD_AT(abort)), plain = good && any;
+        const uint32_t other = good ? 0u : 0x7fc07fc0u;
         const uint32_t from = tmem + at + (key ? kColK : kColV);
         uint16_t* to = (key ? p.dks : p.dvs) + first;
         const float f = key ? p.scale : 1.f;
@@ -424,8 +436,8 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
                 uint32_t w[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                  w[q] = good ? gt::pack2(__uint_as_float(r[8 * x + 2 * q]) * f, __uint_as_float(r[8 * x + 2 * q + 1]) * f)
-                              : 0x7fc07fc0u;
+                  w[q] = plain ? gt::pack2(__uint_as_float(r[8 * x + 2 * q]) * f, __uint_as_float(r[8 * x + 2 * q + 1]) * f)
+                               : other;
                 sts128(mine + (uint32_t)(lane * 128 + (((4 * h + x) ^ (lane & 7)) << 4)), w[0], w[1], w[2], w[3]);
               }
             }
@@ -446,7 +458,7 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
             um::ld16(from + (uint32_t)d0, r);
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-              w[q] = good ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : 0x7fc07fc0u;
+              w[q] = plain ? gt::pack2(__uint_as_float(r[2 * q]) * f, __uint_as_float(r[2 * q + 1]) * f) : other;
             if (lane < rows) store_sector(to + lane * kD + d0, w);
           }
         }
@@ -458,7 +470,7 @@ __device__ __forceinline__ void drain(const GradArgs& p, uint32_t base, uint32_t
             um::ld16(tmem + at + kColQ + (uint32_t)r0, r);
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-              if (r0 + q < p.rows) out[(r0 + q) * 8] = good ? __uint_as_float(r[q]) : nanf("");
+              if (r0 + q < p.rows) out[(r0 + q) * 8] = plain ? __uint_as_float(r[q]) : __uint_as_float(other);
           }
         }
         um::fence_before();
