@@ -77,10 +77,10 @@ __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
 }
 
 // Sixteen lanes per row: its log-sum-exp in the log2 domain and delta; +inf and 0 where it takes
-// no part; NaN where its query or its output's gradient holds a NaN or infinity.  Both rows are
-// laid out for the matrix units (grad_pack): a unit's rows are read again for each of its tiles,
-// and as they lie, 16 bytes a copy, that took longer than the products (1024 rows over 32768
-// slots: the slots' gradients 247 us, 225 as bulk copies).
+// no part; NaN where its query or its output's gradient holds a NaN or infinity, or the log-sum-exp
+// is +inf.  Both rows are laid out for the matrix units (grad_pack): a unit's rows are read again for
+// each of its tiles, and as they lie, 16 bytes a copy, that took longer than the products (1024 rows
+// over 32768 slots: the slots' gradients 247 us, 225 as bulk copies).
 __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_constant__ GradArgs p) {
   release_next();
   if (blockIdx.x == 0) {
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_consta
   odd = (__ballot_sync(kFull, odd) & (0xffffu << (lane & 16))) != 0u;
   if (w0 >= all) return;
   const float2 f = to >= p.rows || lse == -INFINITY ? make_float2(INFINITY, 0.f)
-                   : odd                            ? make_float2(nanf(""), nanf(""))
+                   : odd || lse == INFINITY         ? make_float2(nanf(""), nanf(""))
                                                     : make_float2(lse * 1.4426950408889634f, delta - dlse);
   if (c == 0) {
     if (to < p.rows) p.row[(int64_t)u * p.rows + to] = f;
