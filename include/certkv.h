@@ -633,7 +633,7 @@ int certkv_pages_reserve(int32_t batch, const int32_t* room, const int32_t* want
                          size_t workspace_bytes, void* stream);
 
 /* Where a step's rows go, and their positions.  slots (may be NULL): int32
- * [units][tokens], the pool slot (page 64 + offset) of slot start[u] + i of segment u
+ * [units][tokens], 4-byte aligned, the pool slot (page 64 + offset) of slot start[u] + i of segment u
  * for i < rows[b], -1 for the others and where there is no page (a row i < rows[b]
  * without a page raises CERTKV_STATUS_STORE).  start: device int32 [units], NULL:
  * counts; rows: device int32 [batch] (clamped to 0..tokens), NULL: tokens.
@@ -692,8 +692,8 @@ int certkv_tree_attn(const certkv_shape* shape, int32_t tokens, const certkv_row
  * does not touch it, nor does the row touch that; a NaN or infinity that a row holds or
  * sees makes its dq and the gradients of what it sees NaN, wherever a sum meets it.
  * Sums are fp32, in an order that does not change from call to call; p and e enter
- * them as two bf16 parts (2^-14 of each product at most).  Limits and refusals are
- * those of certkv_tree_attn; on a wait that runs out the rows and slots concerned get
+ * them as two bf16 parts, cut off towards 0 (2^-14 of each product at most).  Limits
+ * and refusals are those of certkv_tree_attn; on a wait that runs out the rows and slots concerned get
  * NaN (CERTKV_STATUS_TIMEOUT).  Workspace: certkv_tree_grad_workspace_bytes(shape,
  * tokens), 256-byte aligned. */
 size_t certkv_tree_grad_workspace_bytes(const certkv_shape* shape, int32_t tokens);

@@ -80,7 +80,8 @@ __device__ __forceinline__ void scan_tiles(const GradArgs& p) {
 // no part; NaN where its query or its output's gradient holds a NaN or infinity, or the log-sum-exp
 // is +inf.  Both rows are laid out for the matrix units (grad_pack): a unit's rows are read again for
 // each of its tiles, and as they lie, 16 bytes a copy, that took longer than the products (1024 rows
-// over 32768 slots: the slots' gradients 247 us, 225 as bulk copies).
+// over 32768 slots: the slots' gradients 247 us, 225 as bulk copies, both with p and e in one part; 279
+// with the two that they have).
 __global__ void __launch_bounds__(kThreads) grad_rows_kernel(const __grid_constant__ GradArgs p) {
   release_next();
   if (blockIdx.x == 0) {
@@ -309,7 +310,7 @@ __device__ __forceinline__ void drafts_dq(const GradArgs& p, const GradUnit& x, 
 // One block per (unit, 128 query rows), on mma.sync: products of at most 128 x 64 x 128, whose
 // time is that of bringing the rows in.  A warp makes p and e of 16 rows; then each warp 16 elements
 // of dk and dv over all rows; then each its rows' dq.  All but the last runs while the last CTAs of
-// the kernel before, which leave the records, still do (8-bit trees 176 us, 181 behind them): that
+// the kernel before, which leave the records, still do (8-bit trees 173 us, 180 behind them): that
 // kernel lets this one start behind its own wait for grad_rows_kernel, whose rows are thus there.
 // Where there is no kernel between the two this one is not started early.
 template <int TD>

@@ -16,8 +16,8 @@
 // dQ^T += K^T e (M = 128 elements of a row) is summed over the share's tiles in the columns of
 // the second block; e times the key's scale is handed over in shared memory for it, in two parts
 // too.  The store is then read once for all gradients, and over bf16 the time is that of its bytes
-// (64 rows over 13107 slots of 256 segments: 3.4 GB in 528 us, 96 % of a copy's rate; 8- and 4-bit
-// 587 and 583 us, the pace of writing two and four times the bytes read).  Reading it again for
+// (64 rows over 13107 slots of 256 segments: 3.4 GB in 530 us, 96 % of a copy's rate; 8- and 4-bit
+// 589 and 586 us, the pace of writing two and four times the bytes read).  Reading it again for
 // the queries' kernel would cost as much as reading it here.
 //
 // Every wait is bounded; on a timeout the roles stop waiting, the rows and slots in question get
@@ -60,9 +60,10 @@ struct Plan {
   static constexpr int kBlockOff = kValueOff + kValues * kOperand;
   static constexpr int kEOff = kBlockOff + kBlocks * kBlock;  // e, FUSED: two parts [128 slots][64 rows]
   static constexpr int kStageOff = kEOff + (FUSED ? 2 * kHalf : 0);  // of keys, then of values
-  // Slots' gradients are written by lines through shared memory, half a row of 32 slots a warp (64
-  // rows over 13107 slots of 256 segments, 8 bits: 572 us, 606 by sectors), but by sectors where a
-  // bf16 store's bytes bound the pass (505 us, and 540 by lines).
+  // Slots' gradients are written by lines through shared memory, half a row of 32 slots a warp (over
+  // 13107 slots of 256 segments, 8 bits, 64 rows 589 us, 645 by sectors; 4 bits 586 and 603), but by
+  // sectors where a bf16 store's bytes bound the pass (64 rows 530 us, and by lines, which leave room
+  // for one block of rows only, 553; 4 rows 573 and 553).
   static constexpr bool kLines = !FUSED || FMT != CERTKV_STORE_BF16;
   static constexpr int kDrainOff = kStageOff + 2 * gt::kStage<FMT>;
   static constexpr int kMiscOff = kDrainOff + (kLines ? kDrainWarps * 4096 : 0);

@@ -11,8 +11,9 @@
 // dQ of this one under e of the next.
 //
 // bf16 stores are bound by their bytes (64 rows over 13107 slots of 256 segments: 1.72 GB in
-// 274 us, 92 % of a copy's rate), 8- and 4-bit ones by the softmax beside the expanding of codes
-// (315 and 324 us; the products of 128 rows, half of them empty there, take 235).
+// 281 us, 90 % of a copy's rate), 8- and 4-bit ones by what a tile goes through, expanding of codes,
+// S and R, softmax, dQ, with no unit full (317 and 326 us; the products of 128 rows, half of them
+// empty there, take 235, and 4 rows as long as 64: 309 and 327).
 //
 // 8- and 4-bit stores: codes are exact in bf16 (gt::codes_to_bf16); a key's fp32 scale multiplies
 // its logit and its e, a value's its R, all in fp32.  The scale comes times that of the logits,
@@ -34,7 +35,7 @@ namespace {
 
 // Warps, whole warpgroups of them: softmax, 64 columns of a row a thread where codes are expanded
 // beside it and 32 else (1024 rows over 32768 slots, bf16: 196 us with eight warps, 158 with
-// sixteen; 8-bit trees 204 and 208, what bounds them being the instructions of all), loaders, and
+// sixteen, 150 since; 8-bit trees 204 and 208, 152 since with eight), loaders, and
 // the issuer beside the warps that ask for codes and state scales.
 constexpr int kLoadWarps = 2 * kGroupWarps;
 template <int FMT>
@@ -54,7 +55,8 @@ constexpr uint32_t kColR = 256, kColQ = 384;  // S of tile t: column 128 (t & 1)
 template <int FMT>
 struct Plan {
   // Places of the rings.  The keys' are held from S of a tile to its dQ, the values' for R alone
-  // (8 bits, 64 rows over 13107 slots of 256 segments: 396 us with 2 + 2 places, 357 with 3 + 1).
+  // (8 bits, 64 rows over 13107 slots of 256 segments: 396 us with 2 + 2 places, 357 with 3 + 1;
+  // 317 since).
   static constexpr int kKeys = 3;
   static constexpr int kValues = FMT == CERTKV_STORE_BF16 ? 2 : 1;
   static constexpr int kFacts = FMT == CERTKV_STORE_BF16 ? kKeys : 2;  // bf16: the copying warps state them

@@ -143,7 +143,7 @@ __device__ __forceinline__ bool settle(const ReserveArgs& p, int u, const Change
 // the account is brought up to date.  A segment's pages are moved by its thread where
 // they are few, by a warp where there are many, the block's warps taking turns, kMovePages of them
 // by each of the blocks of a column of the grid (a 131072-token sequence's 524288 pages taken back
-// and handed out: 275 us with one block a segment, 48 with one warp a block, 37 so).
+// and handed out: 275 us with one block a segment, 48 with one warp a block, 35 so).
 template <bool TAKE>
 __global__ void __launch_bounds__(kThreads) pages_move_kernel(const ReserveArgs p) {
   await_previous();
@@ -211,8 +211,12 @@ __global__ void __launch_bounds__(kThreads) pages_settle_kernel(const ReserveArg
   if (bad) p.st.raise();
 }
 
-// Few segments of few pages: everything by one block, which saves the launches (eight sequences
-// of one layer, both ways: 28 -> 15 us).
+// Few segments of few pages: everything by one block, which saves the launches.  The host knows sizes
+// but not how much moves, and a step, which is what most calls are, moves a page or so of some segments
+// (us a call, and by the launches below: 64 segments x 16 entries, one page each 3.9 and 6.6; 1024 x 128,
+// one 4.7 and 6.7, four 8.8 and 7.7, eight 16.1 and 16.2).  Sequences that begin or end whole pay for
+// it, since a thread moves its segments' pages one after the other: 64 x 16 pages 12 and 10, 64 x 128
+// 56 and 13, 256 x 128 67 and 30, 1024 x 64 112 and 22, 1024 x 128 222 and 30.
 constexpr int kSmallUnits = 4 * kThreads, kSmallPages = 128;
 __global__ void __launch_bounds__(kThreads) pages_small_kernel(const ReserveArgs p) {
   constexpr int kEach = kSmallUnits / kThreads;
